@@ -72,7 +72,8 @@ enum dwconv_status {
     DWCONV_ERR_WORKSPACE = 5,  /* workspace NULL, too small or not 16-byte aligned */
     DWCONV_ERR_ALIGN     = 6,  /* a tensor pointer is not element-aligned          */
     DWCONV_ERR_LAUNCH    = 7,  /* HIP reported an error when launching             */
-    DWCONV_ERR_SCRATCH   = 8   /* dwconv_bwd_weight_noalloc: shape needs more than the built-in scratch */
+    DWCONV_ERR_SCRATCH   = 8,  /* dwconv_bwd_weight_noalloc: shape needs more than the built-in scratch */
+    DWCONV_ERR_VALUE     = 9   /* a scalar argument or stride is out of its range (dwconv_block.h) */
 };
 
 /*

@@ -58,7 +58,7 @@ def sources():
 
 
 def dependencies():
-    return sources() + [FASTCALL_SOURCE] + sorted(glob.glob(os.path.join(CSRC, "*.h"))) + [os.path.join(HERE, "..", "include", "dwconv.h")]
+    return sources() + [FASTCALL_SOURCE] + sorted(glob.glob(os.path.join(CSRC, "*.h"))) + [os.path.join(HERE, "..", "include", n) for n in ("dwconv.h", "dwconv_block.h")]
 
 
 def fastcall_mark() -> str | None:
@@ -124,7 +124,7 @@ def build(verbose: bool = False, extra_flags=(), jobs: int | None = None, increm
     srcs = sources()
     objs = [os.path.join(OBJ_DIR, os.path.basename(p)[:-4] + ".o") for p in srcs]
 
-    headers = sorted(glob.glob(os.path.join(CSRC, "*.h"))) + [os.path.join(HERE, "..", "include", "dwconv.h")]
+    headers = sorted(glob.glob(os.path.join(CSRC, "*.h"))) + [os.path.join(HERE, "..", "include", n) for n in ("dwconv.h", "dwconv_block.h")]
     newest_header = max(os.path.getmtime(h) for h in headers)
 
     def compile_one(pair):

@@ -569,9 +569,10 @@ const char *dwconv_status_string(int status)
     case DWCONV_ERR_SHAPE: return "B, C, L and K must be >= 1 and B*C*L must fit 2^40 elements";
     case DWCONV_ERR_PAD: return "pad_left must lie in [0, K-1]";
     case DWCONV_ERR_DTYPE: return "dtype must be DWCONV_F32 or DWCONV_BF16";
-    case DWCONV_ERR_WORKSPACE: return "workspace is NULL, smaller than dwconv_bwd_weight_workspace_bytes() or not 16-byte aligned";
+    case DWCONV_ERR_WORKSPACE: return "workspace is NULL, smaller than the call needs (its ..._workspace_bytes()) or not 16-byte aligned";
     case DWCONV_ERR_ALIGN: return "a tensor pointer is not aligned to its element size";
     case DWCONV_ERR_LAUNCH: return "HIP reported an error at kernel launch";
+    case DWCONV_ERR_VALUE: return "a scalar argument or stride is out of its range";
     case DWCONV_ERR_SCRATCH: return "this shape needs more partial-sum space than the library's built-in scratch holds "
                                     "(dwconv_noalloc_scratch_bytes()): use dwconv_bwd_weight with a workspace";
     default: return "unknown status";

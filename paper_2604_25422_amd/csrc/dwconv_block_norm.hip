@@ -1,0 +1,172 @@
+// Norms, gate and residual: validation, plans and launches (declared in include/dwconv_block.h).
+#include "dwconv_block_host.hip.h"
+#include "dwconv_block_norm.hip.h"
+
+using namespace blkhost;
+using namespace dwconv;
+
+namespace {
+
+struct NormPlan {
+    int E, NT, lx;              // tile kernel; E = 0: the streaming one
+    int row_tiles;
+    long long tiles;
+    int blocks;
+};
+
+NormPlan plan_norm(int B, int C, int L, int dtype, bool backward)
+{
+    NormPlan s{};
+    const int V = dtype == DWCONV_F32 ? 4 : 8;
+    const int most = backward ? (dtype == DWCONV_F32 ? 8 : 6) : 8;      // packs of each tensor that the registers hold
+    if (L >= V) {
+        s.NT = 256;
+        s.lx = 2;
+        while (s.lx > 0 && (V << (s.lx - 1)) >= L) --s.lx;
+        while (s.NT < 512 && C > (s.NT >> s.lx) * most) s.NT *= 2;
+        while (s.lx > 0 && C > (s.NT >> s.lx) * most) --s.lx;
+        const int e = (int)ceil_div(C, s.NT >> s.lx);
+        if (e <= most) {
+            s.E = e;
+            s.row_tiles = (int)ceil_div(L, V << s.lx);
+        }
+    }
+    if (!s.E) {
+        s.NT = 256;
+        s.lx = 0;
+        while (s.lx < 6 && (1 << s.lx) < L && (256 >> (s.lx + 1)) >= 4) ++s.lx;
+        s.row_tiles = (int)ceil_div(L, 1 << s.lx);
+    }
+    s.tiles = (long long)B * s.row_tiles;
+    s.blocks = (int)std::min<long long>(s.tiles, backward ? 1024 : 1 << 20);
+    return s;
+}
+size_t red_bytes(const NormPlan &s, int V) { return (size_t)(s.NT / 64 + 1) * (V << s.lx) * sizeof(float); }
+
+template <typename T, int E, bool BLOCK> void fwd_tile(const NormFwd<T> &p, const NormPlan &s, hipStream_t st)
+{
+    const size_t lds = red_bytes(s, Pack<T>::V);
+    if (s.NT == 256) norm_fwd_tile_kernel<T, E, 256, BLOCK><<<s.blocks, 256, lds, st>>>(p);
+    else norm_fwd_tile_kernel<T, E, 512, BLOCK><<<s.blocks, 512, lds, st>>>(p);
+}
+template <typename T, bool BLOCK> void launch_fwd(const NormFwd<T> &p, const NormPlan &s, hipStream_t st)
+{
+    switch (s.E) {
+    case 0: norm_fwd_stream_kernel<T, BLOCK><<<s.blocks, 256, 0, st>>>(p); return;
+    case 1: return fwd_tile<T, 1, BLOCK>(p, s, st);
+    case 2: return fwd_tile<T, 2, BLOCK>(p, s, st);
+    case 3: return fwd_tile<T, 3, BLOCK>(p, s, st);
+    case 4: return fwd_tile<T, 4, BLOCK>(p, s, st);
+    case 5: return fwd_tile<T, 5, BLOCK>(p, s, st);
+    case 6: return fwd_tile<T, 6, BLOCK>(p, s, st);
+    case 7: return fwd_tile<T, 7, BLOCK>(p, s, st);
+    default: return fwd_tile<T, 8, BLOCK>(p, s, st);
+    }
+}
+template <typename T, int E, bool BLOCK> void bwd_tile(const NormBwd<T> &p, const NormPlan &s, hipStream_t st)
+{
+    const size_t lds = red_bytes(s, Pack<T>::V);
+    if (s.NT == 256) norm_bwd_tile_kernel<T, E, 256, BLOCK><<<s.blocks, 256, lds, st>>>(p);
+    else norm_bwd_tile_kernel<T, E, 512, BLOCK><<<s.blocks, 512, lds, st>>>(p);
+}
+template <typename T, bool BLOCK> void launch_bwd(const NormBwd<T> &p, const NormPlan &s, float *dw, float *dw_next, hipStream_t st)
+{
+    switch (s.E) {
+    case 0: norm_bwd_stream_kernel<T, BLOCK><<<s.blocks, 256, 0, st>>>(p); break;
+    case 1: bwd_tile<T, 1, BLOCK>(p, s, st); break;
+    case 2: bwd_tile<T, 2, BLOCK>(p, s, st); break;
+    case 3: bwd_tile<T, 3, BLOCK>(p, s, st); break;
+    case 4: bwd_tile<T, 4, BLOCK>(p, s, st); break;
+    case 5: bwd_tile<T, 5, BLOCK>(p, s, st); break;
+    case 6: bwd_tile<T, 6, BLOCK>(p, s, st); break;
+    default:
+        if constexpr (sizeof(T) == 4) {
+            if (s.E == 7) bwd_tile<T, 7, BLOCK>(p, s, st);
+            else bwd_tile<T, 8, BLOCK>(p, s, st);
+        }
+    }
+    norm_sums_kernel<<<dim3((unsigned)ceil_div(p.C, 32), 2), 1024, 0, st>>>(p.part, s.blocks, p.C, dw, dw_next);
+}
+
+size_t part_bytes(const NormPlan &s, int C) { return (size_t)s.blocks * 2 * C * sizeof(float); }
+
+template <typename T>
+void run_fwd(const dwconv_seq &y, const dwconv_seq &z, const dwconv_seq &res, const float *w, const float *w_next, const dwconv_seq_out &out,
+             const dwconv_seq_out &n, float *stats, int B, int C, int L, float eps, float scale, const NormPlan &s, hipStream_t st)
+{
+    const NormFwd<T> p{seq<T>(y), seq<T>(z), seq<T>(res), w, w_next, seq<T>(out), seq<T>(n), stats, B, C, L, eps, scale, s.lx, s.tiles, s.row_tiles};
+    if (y.data) launch_fwd<T, true>(p, s, st);
+    else launch_fwd<T, false>(p, s, st);
+}
+template <typename T>
+void run_bwd(const dwconv_seq &dout, const dwconv_seq &dn, const dwconv_seq &y, const dwconv_seq &z, const dwconv_seq &res, const float *w,
+             const float *w_next, const float *stats, const dwconv_seq_out &dy, const dwconv_seq_out &dz, const dwconv_seq_out &dres, float *dw,
+             float *dw_next, float *part, int B, int C, int L, float scale, const NormPlan &s, hipStream_t st)
+{
+    const NormBwd<T> p{seq<T>(dout), seq<T>(dn), seq<T>(y), seq<T>(z), seq<T>(res), w, w_next, stats, seq<T>(dy), seq<T>(dz), seq<T>(dres), part,
+                       B, C, L, scale, s.lx, s.tiles, s.row_tiles};
+    if (y.data) launch_bwd<T, true>(p, s, dw, dw_next, st);
+    else launch_bwd<T, false>(p, s, nullptr, dw_next, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dwconv_norm_workspace_bytes(int B, int C, int L, int dtype)
+{
+    if (check_dims(B, C, L) != DWCONV_OK || !dtype_ok(dtype)) return 0;
+    return (part_bytes(plan_norm(B, C, L, dtype, true), C) + 15) & ~(size_t)15;
+}
+
+int dwconv_norm_fwd(dwconv_seq y, dwconv_seq z, dwconv_seq res, const float *w, const float *w_next, dwconv_seq_out out, dwconv_seq_out n,
+                    float *stats, int B, int C, int L, float eps, float scale, int dtype, void *stream)
+{
+    if (!res.data || !w_next || !n.data) return DWCONV_ERR_NULL;
+    const bool block = y.data || z.data || w || out.data;
+    if (block && (!y.data || !z.data || !w || !out.data)) return DWCONV_ERR_NULL;
+    int rc = check_dims(B, C, L);
+    if (rc != DWCONV_OK) return rc;
+    if (!dtype_ok(dtype)) return DWCONV_ERR_DTYPE;
+    if (!(eps > 0.0f && eps < INFINITY) || !(fabsf(scale) < INFINITY)) return DWCONV_ERR_VALUE;
+    const size_t es = elem_size(dtype);
+    if ((rc = check_in(res, es)) != DWCONV_OK || (rc = check_out(n, es, B, C, L)) != DWCONV_OK) return rc;
+    if (block && ((rc = check_in(y, es)) != DWCONV_OK || (rc = check_in(z, es)) != DWCONV_OK || (rc = check_out(out, es, B, C, L)) != DWCONV_OK))
+        return rc;
+    if (!f32_ok(w) || !f32_ok(w_next) || !f32_ok(stats)) return DWCONV_ERR_ALIGN;
+    const NormPlan s = plan_norm(B, C, L, dtype, false);
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (dtype == DWCONV_F32) run_fwd<float>(y, z, res, w, w_next, out, n, stats, B, C, L, eps, scale, s, st);
+    else run_fwd<bf16_t>(y, z, res, w, w_next, out, n, stats, B, C, L, eps, scale, s, st);
+    return launch_status();
+}
+
+int dwconv_norm_bwd(dwconv_seq dout, dwconv_seq dn, dwconv_seq y, dwconv_seq z, dwconv_seq res, const float *w, const float *w_next,
+                    const float *stats, dwconv_seq_out dy, dwconv_seq_out dz, dwconv_seq_out dres, float *dw, float *dw_next, void *workspace,
+                    size_t workspace_bytes, int B, int C, int L, float scale, int dtype, void *stream)
+{
+    if (!dn.data || !res.data || !w_next || !stats || !dres.data || !dw_next) return DWCONV_ERR_NULL;
+    const bool block = y.data || z.data || w || dy.data || dz.data || dw;
+    if (block && (!y.data || !z.data || !w || !dy.data || !dz.data || !dw)) return DWCONV_ERR_NULL;
+    int rc = check_dims(B, C, L);
+    if (rc != DWCONV_OK) return rc;
+    if (!dtype_ok(dtype)) return DWCONV_ERR_DTYPE;
+    if (!(fabsf(scale) < INFINITY)) return DWCONV_ERR_VALUE;
+    const size_t es = elem_size(dtype);
+    if ((rc = check_in(dn, es)) != DWCONV_OK || (rc = check_in(res, es)) != DWCONV_OK || (rc = check_out(dres, es, B, C, L)) != DWCONV_OK) return rc;
+    if (dout.data && (rc = check_in(dout, es)) != DWCONV_OK) return rc;
+    if (block && ((rc = check_in(y, es)) != DWCONV_OK || (rc = check_in(z, es)) != DWCONV_OK || (rc = check_out(dy, es, B, C, L)) != DWCONV_OK ||
+                  (rc = check_out(dz, es, B, C, L)) != DWCONV_OK))
+        return rc;
+    for (const void *t : {(const void *)w, (const void *)w_next, (const void *)stats, (const void *)dw, (const void *)dw_next})
+        if (!f32_ok(t)) return DWCONV_ERR_ALIGN;
+    const NormPlan s = plan_norm(B, C, L, dtype, true);
+    if (!workspace || workspace_bytes < part_bytes(s, C) || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    float *part = static_cast<float *>(workspace);
+    if (dtype == DWCONV_F32) run_bwd<float>(dout, dn, y, z, res, w, w_next, stats, dy, dz, dres, dw, dw_next, part, B, C, L, scale, s, st);
+    else run_bwd<bf16_t>(dout, dn, y, z, res, w, w_next, stats, dy, dz, dres, dw, dw_next, part, B, C, L, scale, s, st);
+    return launch_status();
+}
+
+}  // extern "C"

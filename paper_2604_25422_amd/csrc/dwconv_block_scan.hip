@@ -1,0 +1,205 @@
+// Gated scan: validation, plans and launches (declared in include/dwconv_block.h).
+#include "dwconv_block_host.hip.h"
+#include "dwconv_block_scan.hip.h"
+
+using namespace blkhost;
+using namespace dwconv;
+
+namespace {
+
+struct ScanPlan {
+    int G;                      // lanes of a short row; 0: chunks
+    int W, segs, seg_groups;    // waves of a workgroup, segments of a row, groups of W chunks in a segment
+    ShortRows m;
+    int gx, gy;
+    long long M;                // rows of the sums towards dlam
+};
+
+ScanPlan plan_scan(int B, int C, int L)
+{
+    ScanPlan s{};
+    const long long rows = (long long)B * C;
+    if (L <= kScanShort) {
+        s.G = 1;
+        while (s.G * 8 < L) s.G *= 2;
+        const int per = 256 / s.G;
+        // channels of a workgroup: as many as it has rows, evenly over the workgroups; of few channels several batch entries
+        const int blocks = (int)ceil_div(C, per);
+        s.m.cb = (int)ceil_div(C, blocks);
+        s.m.nb = per / s.m.cb;
+        s.gx = (int)ceil_div(C, s.m.cb);
+        s.gy = (int)std::max(1ll, std::min<long long>({ceil_div(B, s.m.nb), ceil_div(4096, s.gx), 65535}));
+        s.M = (long long)s.gy * s.m.nb;
+        s.segs = 1;
+        return s;
+    }
+    const long long chunks = ceil_div(L, kScanChunk);
+    s.W = 1;
+    while (s.W < 16 && rows * s.W < 4096 && s.W < chunks) s.W *= 2;
+    const long long groups = ceil_div(chunks, s.W);
+    s.segs = 1;
+    if (rows * s.W < 2048) s.segs = (int)std::max(1ll, std::min<long long>({groups, ceil_div(4096, rows * s.W), kScanSegments}));
+    s.seg_groups = (int)ceil_div(groups, s.segs);
+    s.segs = (int)ceil_div(groups, s.seg_groups);
+    s.M = (long long)B * s.segs;
+    return s;
+}
+
+size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
+size_t span_bytes(const ScanPlan &s, int B, int C) { return s.segs > 1 ? up16((size_t)B * C * s.segs * sizeof(Span)) : 0; }
+size_t part_bytes(const ScanPlan &s, int C) { return up16((size_t)s.M * C * sizeof(float)); }
+constexpr long long kMaxBlocks = 1 << 20;
+
+template <typename T, int W> void launch_fwd(const ScanFwd<T> &p, const ScanPlan &s, hipStream_t st)
+{
+    const long long rows = (long long)p.B * p.C;
+    if (s.segs > 1) scan_fwd_kernel<T, W, true><<<(unsigned)std::min(rows * (s.segs - 1), kMaxBlocks), 64 * W, 0, st>>>(p);
+    scan_fwd_kernel<T, W, false><<<(unsigned)std::min(rows * s.segs, kMaxBlocks), 64 * W, 0, st>>>(p);
+}
+template <typename T> void launch_fwd(const ScanFwd<T> &p, const ScanPlan &s, hipStream_t st)
+{
+    const dim3 grid(s.gx, s.gy);
+    switch (s.G) {
+    case 1: scan_fwd_short_kernel<T, 1><<<grid, 256, 0, st>>>(p, s.m); return;
+    case 2: scan_fwd_short_kernel<T, 2><<<grid, 256, 0, st>>>(p, s.m); return;
+    case 4: scan_fwd_short_kernel<T, 4><<<grid, 256, 0, st>>>(p, s.m); return;
+    case 8: scan_fwd_short_kernel<T, 8><<<grid, 256, 0, st>>>(p, s.m); return;
+    case 16: scan_fwd_short_kernel<T, 16><<<grid, 256, 0, st>>>(p, s.m); return;
+    case 32: scan_fwd_short_kernel<T, 32><<<grid, 256, 0, st>>>(p, s.m); return;
+    }
+    switch (s.W) {
+    case 1: return launch_fwd<T, 1>(p, s, st);
+    case 2: return launch_fwd<T, 2>(p, s, st);
+    case 4: return launch_fwd<T, 4>(p, s, st);
+    case 8: return launch_fwd<T, 8>(p, s, st);
+    default: return launch_fwd<T, 16>(p, s, st);
+    }
+}
+
+template <typename T, int W> void launch_bwd(const ScanBwd<T> &p, const ScanPlan &s, hipStream_t st)
+{
+    const long long rows = (long long)p.B * p.C;
+    if (s.segs > 1) scan_bwd_kernel<T, W, true><<<(unsigned)std::min(rows * (s.segs - 1), kMaxBlocks), 64 * W, 0, st>>>(p);
+    scan_bwd_kernel<T, W, false><<<(unsigned)std::min(rows * s.segs, kMaxBlocks), 64 * W, 0, st>>>(p);
+}
+template <typename T> void launch_bwd(const ScanBwd<T> &p, const ScanPlan &s, float *dlam, hipStream_t st)
+{
+    const dim3 grid(s.gx, s.gy);
+    switch (s.G ? s.G : 64 * s.W) {
+    case 1: scan_bwd_short_kernel<T, 1><<<grid, 256, 0, st>>>(p, s.m); break;
+    case 2: scan_bwd_short_kernel<T, 2><<<grid, 256, 0, st>>>(p, s.m); break;
+    case 4: scan_bwd_short_kernel<T, 4><<<grid, 256, 0, st>>>(p, s.m); break;
+    case 8: scan_bwd_short_kernel<T, 8><<<grid, 256, 0, st>>>(p, s.m); break;
+    case 16: scan_bwd_short_kernel<T, 16><<<grid, 256, 0, st>>>(p, s.m); break;
+    case 32: scan_bwd_short_kernel<T, 32><<<grid, 256, 0, st>>>(p, s.m); break;
+    case 64: launch_bwd<T, 1>(p, s, st); break;
+    case 128: launch_bwd<T, 2>(p, s, st); break;
+    case 256: launch_bwd<T, 4>(p, s, st); break;
+    case 512: launch_bwd<T, 8>(p, s, st); break;
+    default: launch_bwd<T, 16>(p, s, st); break;
+    }
+    scan_dlam_kernel<<<(unsigned)ceil_div(p.C, 32), 1024, 0, st>>>(p.part, (int)s.M, p.C, p.lam, dlam);
+}
+
+bool rate_ok(float rate) { return rate > 0.0f && rate < INFINITY; }
+
+}  // namespace
+
+extern "C" {
+
+int dwconv_scan_states(int L) { return L < 1 || L > (1 << 30) ? 0 : (int)ceil_div(L, kScanChunk); }
+
+size_t dwconv_scan_workspace_bytes(int B, int C, int L, int backward)
+{
+    if (check_dims(B, C, L) != DWCONV_OK) return 0;
+    const ScanPlan s = plan_scan(B, C, L);
+    return span_bytes(s, B, C) + (backward ? part_bytes(s, C) : 0);
+}
+
+int dwconv_scan_fwd(dwconv_seq x, dwconv_seq r, dwconv_seq i, const float *lam, const float *h0, const int *lengths, dwconv_seq_out y,
+                    float *h_last, float *states, void *workspace, size_t workspace_bytes, int B, int C, int L, float rate, int dtype,
+                    void *stream)
+{
+    if (!x.data || !r.data || !i.data || !lam || !y.data) return DWCONV_ERR_NULL;
+    int rc = check_dims(B, C, L);
+    if (rc != DWCONV_OK) return rc;
+    if (!dtype_ok(dtype)) return DWCONV_ERR_DTYPE;
+    if (!rate_ok(rate)) return DWCONV_ERR_VALUE;
+    const size_t es = elem_size(dtype);
+    for (const dwconv_seq *t : {&x, &r, &i})
+        if ((rc = check_in(*t, es)) != DWCONV_OK) return rc;
+    if ((rc = check_out(y, es, B, C, L)) != DWCONV_OK) return rc;
+    for (const void *t : {(const void *)lam, (const void *)h0, (const void *)lengths, (const void *)h_last, (const void *)states})
+        if (!f32_ok(t)) return DWCONV_ERR_ALIGN;
+    const ScanPlan s = plan_scan(B, C, L);
+    const size_t need = span_bytes(s, B, C);
+    if (need && (!workspace || workspace_bytes < need || !aligned_to(workspace, 16))) return DWCONV_ERR_WORKSPACE;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const int ns = dwconv_scan_states(L);
+    Span *spans = static_cast<Span *>(workspace);
+    if (dtype == DWCONV_F32)
+        launch_fwd(ScanFwd<float>{seq<float>(x), seq<float>(r), seq<float>(i), lam, h0, lengths, seq<float>(y), h_last, states, spans, B, C, L, ns,
+                                  rate, s.segs, s.seg_groups}, s, st);
+    else
+        launch_fwd(ScanFwd<bf16_t>{seq<bf16_t>(x), seq<bf16_t>(r), seq<bf16_t>(i), lam, h0, lengths, seq<bf16_t>(y), h_last, states, spans, B, C, L,
+                                   ns, rate, s.segs, s.seg_groups}, s, st);
+    return launch_status();
+}
+
+int dwconv_scan_bwd(dwconv_seq dy, dwconv_seq x, dwconv_seq r, dwconv_seq i, const float *lam, const float *states, const float *dh_last,
+                    const int *lengths, dwconv_seq_out dx, dwconv_seq_out dr, dwconv_seq_out di, float *dlam, float *dh0, void *workspace,
+                    size_t workspace_bytes, int B, int C, int L, float rate, int dtype, void *stream)
+{
+    if (!dy.data || !x.data || !r.data || !i.data || !lam || !states || !dx.data || !dr.data || !di.data || !dlam) return DWCONV_ERR_NULL;
+    int rc = check_dims(B, C, L);
+    if (rc != DWCONV_OK) return rc;
+    if (!dtype_ok(dtype)) return DWCONV_ERR_DTYPE;
+    if (!rate_ok(rate)) return DWCONV_ERR_VALUE;
+    const size_t es = elem_size(dtype);
+    for (const dwconv_seq *t : {&dy, &x, &r, &i})
+        if ((rc = check_in(*t, es)) != DWCONV_OK) return rc;
+    for (const dwconv_seq_out *t : {&dx, &dr, &di})
+        if ((rc = check_out(*t, es, B, C, L)) != DWCONV_OK) return rc;
+    for (const void *t : {(const void *)lam, (const void *)states, (const void *)dh_last, (const void *)lengths, (const void *)dlam, (const void *)dh0})
+        if (!f32_ok(t)) return DWCONV_ERR_ALIGN;
+    const ScanPlan s = plan_scan(B, C, L);
+    const size_t need = span_bytes(s, B, C) + part_bytes(s, C);
+    if (!workspace || workspace_bytes < need || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const int ns = dwconv_scan_states(L);
+    float *part = static_cast<float *>(workspace);
+    Span *spans = reinterpret_cast<Span *>(static_cast<char *>(workspace) + part_bytes(s, C));
+    if (dtype == DWCONV_F32)
+        launch_bwd(ScanBwd<float>{seq<float>(dy), seq<float>(x), seq<float>(r), seq<float>(i), lam, states, dh_last, lengths, seq<float>(dx),
+                                  seq<float>(dr), seq<float>(di), dh0, part, spans, B, C, L, ns, rate, s.segs, s.seg_groups}, s, dlam, st);
+    else
+        launch_bwd(ScanBwd<bf16_t>{seq<bf16_t>(dy), seq<bf16_t>(x), seq<bf16_t>(r), seq<bf16_t>(i), lam, states, dh_last, lengths, seq<bf16_t>(dx),
+                                   seq<bf16_t>(dr), seq<bf16_t>(di), dh0, part, spans, B, C, L, ns, rate, s.segs, s.seg_groups}, s, dlam, st);
+    return launch_status();
+}
+
+int dwconv_scan_step(dwconv_seq x, dwconv_seq r, dwconv_seq i, const float *lam, float *h, const int *slots, int pool, dwconv_seq_out y, int B,
+                     int C, float rate, int dtype, void *stream)
+{
+    if (!x.data || !r.data || !i.data || !lam || !h || !y.data) return DWCONV_ERR_NULL;
+    int rc = check_dims(B, C, 1);
+    if (rc != DWCONV_OK) return rc;
+    if (pool < 1 || (!slots && pool < B)) return DWCONV_ERR_SHAPE;
+    if (!dtype_ok(dtype)) return DWCONV_ERR_DTYPE;
+    if (!rate_ok(rate)) return DWCONV_ERR_VALUE;
+    const size_t es = elem_size(dtype);
+    for (const dwconv_seq *t : {&x, &r, &i})
+        if ((rc = check_in(*t, es)) != DWCONV_OK) return rc;
+    if ((rc = check_out(y, es, B, C, 1)) != DWCONV_OK) return rc;
+    if (!f32_ok(lam) || !f32_ok(h) || !f32_ok(slots)) return DWCONV_ERR_ALIGN;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const dim3 grid((unsigned)ceil_div(C, 256), (unsigned)std::min(B, 4096));
+    if (dtype == DWCONV_F32)
+        scan_step_kernel<<<grid, 256, 0, st>>>(ScanStep<float>{seq<float>(x), seq<float>(r), seq<float>(i), lam, h, slots, seq<float>(y), B, C, pool, rate});
+    else
+        scan_step_kernel<<<grid, 256, 0, st>>>(
+            ScanStep<bf16_t>{seq<bf16_t>(x), seq<bf16_t>(r), seq<bf16_t>(i), lam, h, slots, seq<bf16_t>(y), B, C, pool, rate});
+    return launch_status();
+}
+
+}  // extern "C"
