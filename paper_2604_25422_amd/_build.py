@@ -15,6 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libdwconv_gfx950.so")
 FASTCALL_PATH = os.path.join(HERE, "_fastcall.so")       # the Python calls as one native function each (csrc/dwconv_fastcall.cpp)
 FASTCALL_SOURCE = os.path.join(CSRC, "dwconv_fastcall.cpp")
+PUBLIC_HEADERS = [os.path.join(HERE, "..", "include", n) for n in ("dwconv.h", "dwconv_block.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -58,7 +59,7 @@ def sources():
 
 
 def dependencies():
-    return sources() + [FASTCALL_SOURCE] + sorted(glob.glob(os.path.join(CSRC, "*.h"))) + [os.path.join(HERE, "..", "include", n) for n in ("dwconv.h", "dwconv_block.h")]
+    return sources() + [FASTCALL_SOURCE] + sorted(glob.glob(os.path.join(CSRC, "*.h"))) + PUBLIC_HEADERS
 
 
 def fastcall_mark() -> str | None:
@@ -76,7 +77,7 @@ def fastcall_mark() -> str | None:
 
 
 def _fastcall_is_current() -> bool:
-    if not os.path.exists(FASTCALL_PATH) or os.path.getmtime(FASTCALL_PATH) <= os.path.getmtime(FASTCALL_SOURCE):
+    if not os.path.exists(FASTCALL_PATH) or os.path.getmtime(FASTCALL_PATH) <= max(map(os.path.getmtime, [FASTCALL_SOURCE] + PUBLIC_HEADERS)):
         return False
     mark = fastcall_mark()
     with open(FASTCALL_PATH, "rb") as f:
@@ -124,7 +125,7 @@ def build(verbose: bool = False, extra_flags=(), jobs: int | None = None, increm
     srcs = sources()
     objs = [os.path.join(OBJ_DIR, os.path.basename(p)[:-4] + ".o") for p in srcs]
 
-    headers = sorted(glob.glob(os.path.join(CSRC, "*.h"))) + [os.path.join(HERE, "..", "include", n) for n in ("dwconv.h", "dwconv_block.h")]
+    headers = sorted(glob.glob(os.path.join(CSRC, "*.h"))) + PUBLIC_HEADERS
     newest_header = max(os.path.getmtime(h) for h in headers)
 
     def compile_one(pair):

@@ -34,9 +34,19 @@ _NONE = Seq(None, 0)
 _lib = None
 
 
+class _Declines:
+    """In the place of the native calls until the library is loaded, and where they cannot be (see ``binding``)."""
+    scan_fwd = scan_bwd = scan_step = norm_fwd = norm_bwd = clip_grad_norm = conv_step = staticmethod(lambda *args: None)
+
+
+_fast = _Declines
+_FAST_ADDRESSES = ("dwconv_scan_fwd", "dwconv_scan_bwd", "dwconv_scan_states", "dwconv_scan_workspace_bytes", "dwconv_scan_step", "dwconv_norm_fwd",
+                   "dwconv_norm_bwd", "dwconv_norm_workspace_bytes", "dwconv_clip_grad_norm", "dwconv_clip_workspace_bytes", "dwconv_conv_step")
+
+
 def lib():
     """The shared library, with the signatures of the block operators."""
-    global _lib
+    global _lib, _fast
     if _lib is None:
         l = binding.lib()
         vp, i, f, sz, s = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t, Seq
@@ -55,6 +65,9 @@ def lib():
                 ("dwconv_conv_ring", [s, vp, vp, vp, i, i, i, i, i, i, vp], i)):
             fn = getattr(l, name)
             fn.argtypes, fn.restype = args, res
+        if binding._fast is not binding._Declines:
+            binding._fast.setup_block(*(ctypes.cast(getattr(l, n), vp).value for n in _FAST_ADDRESSES))
+            _fast = binding._fast
         _lib = l
     return _lib
 
@@ -140,6 +153,9 @@ def scan_fwd(x, r, i, lam, h0=None, lengths=None, rate: float = 8.0, save: bool 
     """h[t] = a[t] h[t-1] + sqrt(1 - a[t]^2) sigmoid(i[t]) x[t] with a = exp(-rate softplus(lam) sigmoid(r)), along t of [B, C, L]
     tensors x, r, i of one type; lam [C], h0 [B, C] (None: zeros) fp32, lengths [B] int32 (None: L; y is 0 behind a sequence's end).
     Returns (y, h_last, states): y like x, h_last [B, C] fp32, states what ``scan_bwd`` takes (None without ``save``)."""
+    done = _fast.scan_fwd(x, r, i, lam, h0, lengths, rate, save, out, workspace)
+    if done is not None:
+        return done
     shape = B, C, L = _shape3(x, "x")
     code = _dtype_code(x)
     xs, rs, is_ = _seq(x, "x", shape, x.dtype), _seq(r, "r", shape, x.dtype), _seq(i, "i", shape, x.dtype)
@@ -156,14 +172,18 @@ def scan_fwd(x, r, i, lam, h0=None, lengths=None, rate: float = 8.0, save: bool 
 def scan_bwd(dy, x, r, i, lam, states, dh_last=None, lengths=None, rate: float = 8.0, out=None, workspace=None):
     """Gradients of ``scan_fwd`` from dy [B, C, L] and dh_last [B, C] fp32 (None: zeros): returns (dx, dr, di, dlam, dh0), the
     first three like x (or into the three tensors of ``out``), dlam [C] and dh0 [B, C] fp32."""
+    given = out if out is not None else (None,) * 3
+    if len(given) != 3:
+        raise ValueError("out must be three tensors (dx, dr, di)")
+    done = _fast.scan_bwd(dy, x, r, i, lam, states, dh_last, lengths, rate, *given, workspace)
+    if done is not None:
+        return done
     shape = B, C, L = _shape3(x, "x")
     code = _dtype_code(x)
     ins = [_seq(t, n, shape, x.dtype) for t, n in ((dy, "dy"), (x, "x"), (r, "r"), (i, "i"))]
     lamp, lp = _f32(lam, "lam", (C,)), _index(lengths, "lengths", B)
     sp, dhp = _f32(states, "states", (B, C, scan_states(L))), _f32(dh_last, "dh_last", (B, C), True)
-    outs = [_out(t, n, shape, x) for t, n in zip(out if out is not None else (None,) * 3, ("dx", "dr", "di"))]
-    if len(outs) != 3:
-        raise ValueError("out must be three tensors (dx, dr, di)")
+    outs = [_out(t, n, shape, x) for t, n in zip(given, ("dx", "dr", "di"))]
     dlam = torch.empty((C,), dtype=torch.float32, device=x.device)
     dh0 = torch.empty((B, C), dtype=torch.float32, device=x.device)
     ws, nbytes, keep = _workspace(workspace, scan_workspace_bytes(B, C, L, True), x)
@@ -175,6 +195,9 @@ def scan_bwd(dy, x, r, i, lam, states, dh_last=None, lengths=None, rate: float =
 def scan_step(x, r, i, lam, h, slots=None, rate: float = 8.0, out=None):
     """One token of the gated scan for a batch: x, r, i [B, C]; h [pool, C] fp32 is updated in place, place b of the batch in row
     slots[b] (int32; outside [0, pool): an empty place, y is 0 there) or, without slots, in row b.  Returns y like x."""
+    done = _fast.scan_step(x, r, i, lam, h, slots, rate, out)
+    if done is not None:
+        return done
     shape = B, C = _shape2(x, "x")
     code = _dtype_code(x)
     ins = [_seq(t, n, shape, x.dtype) for t, n in ((x, "x"), (r, "r"), (i, "i"))]
@@ -195,6 +218,9 @@ def norm_fwd(y, z, res, w, w_next, eps: float = 1e-6, scale: float = 1.0, save: 
     """out = res + scale silu(z) y / rms(y) w and n = out / rms(out) w_next, rms over the channels of [B, C, L] tensors; w, w_next [C]
     fp32.  y = z = w = None: no block in front, n is the norm of res and out is None.  Returns (out, n, stats), stats what
     ``norm_bwd`` takes (None without ``save``)."""
+    done = _fast.norm_fwd(y, z, res, w, w_next, eps, scale, save, out, out_n)
+    if done is not None:
+        return done
     shape = B, C, L = _shape3(res, "res")
     code = _dtype_code(res)
     rs, wnp = _seq(res, "res", shape, res.dtype), _f32(w_next, "w_next", (C,))
@@ -218,14 +244,17 @@ def norm_fwd(y, z, res, w, w_next, eps: float = 1e-6, scale: float = 1.0, save: 
 def norm_bwd(dout, dn, y, z, res, w, w_next, stats, scale: float = 1.0, out=None, workspace=None):
     """Gradients of ``norm_fwd`` from dout (None: zeros) and dn: returns (dy, dz, dres, dw, dw_next), the first three like res (or
     into the three tensors of ``out``), the last two [C] fp32.  Without a block (y = z = w = None) dy, dz and dw are None."""
+    given = out if out is not None else (None,) * 3
+    if len(given) != 3:
+        raise ValueError("out must be three tensors (dy, dz, dres)")
+    done = _fast.norm_bwd(dout, dn, y, z, res, w, w_next, stats, scale, *given, workspace)
+    if done is not None:
+        return done
     shape = B, C, L = _shape3(res, "res")
     code = _dtype_code(res)
     ds = _NONE if dout is None else _seq(dout, "dout", shape, res.dtype)
     ns, rs = _seq(dn, "dn", shape, res.dtype), _seq(res, "res", shape, res.dtype)
     wnp, sp = _f32(w_next, "w_next", (C,)), _f32(stats, "stats", (B, 2, L))
-    given = out if out is not None else (None,) * 3
-    if len(given) != 3:
-        raise ValueError("out must be three tensors (dy, dz, dres)")
     ys = zs = dys = dzs = _NONE
     wp = dy = dz = dw = None
     if y is not None or z is not None or w is not None:
@@ -259,6 +288,9 @@ def _dense(t: torch.Tensor) -> bool:
 def clip_grad_norm(grads, max_norm: float, out=None, workspace=None) -> torch.Tensor:
     """Scales all tensors of ``grads`` (fp32 or bf16, any mixture, dense) by min(1, max_norm / (norm + 1e-6)), norm the 2-norm of
     everything in them: in place, or into the tensors of ``out``, laid out alike.  Returns norm, an fp32 scalar on the GPU."""
+    done = _fast.clip_grad_norm(grads, max_norm, out, workspace)
+    if done is not None:
+        return done
     grads = [grads] if isinstance(grads, torch.Tensor) else list(grads)
     outs = grads if out is None else [out] if isinstance(out, torch.Tensor) else list(out)
     n = len(grads)
@@ -295,6 +327,9 @@ def conv_step(x, w, ring, pos, slots=None, out=None):
     """The causal convolution (``dwconv_fwd`` with pad_left = K - 1) for one token of every sequence of a batch: x [B, C], w [C, K],
     ring [pool, C, K] (the last K inputs, that of position p at p mod K; updated in place), pos [B] int32 (tokens before this one;
     advanced by the caller, once for all layers), slots as in ``scan_step``.  Returns y like x."""
+    done = _fast.conv_step(x, w, ring, pos, slots, out)
+    if done is not None:
+        return done
     shape = B, C = _shape2(x, "x")
     code = _dtype_code(x)
     xs, rp, pp, sp = _seq(x, "x", shape, x.dtype), _ring(ring, C, x.dtype), _index(pos, "pos", B), _index(slots, "slots", B)

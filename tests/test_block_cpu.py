@@ -209,3 +209,15 @@ def test_reference_of_the_norm_against_differences():
         eps = 1e-5
         num = (loss({**args, name: t + eps * d}) - loss({**args, name: t - eps * d})) / (2 * eps)
         assert abs(num - float((out["d" + name] * d).sum())) < 1e-7 * (1 + abs(num)), name
+
+
+def test_native_calls_decline_what_is_not_a_device_tensor(lib):
+    from paper_2604_25422_amd import _fastcall, block
+    assert block._fast is _fastcall
+    x, c = torch.zeros(2, 3, 8), torch.zeros(3)
+    for call in (lambda: _fastcall.scan_fwd(x, x, x, c, None, None, 8.0, True, None, None), lambda: _fastcall.scan_fwd(x), lambda: _fastcall.scan_step(x, x, x, c, x, None, 8.0, None),
+                 lambda: _fastcall.scan_bwd(x, x, x, x, c, x, None, None, 8.0, None, None, None, None), lambda: _fastcall.norm_fwd(x, x, x, c, c, 1e-6, 1.0, True, None, None),
+                 lambda: _fastcall.norm_fwd(None, x, x, c, c, 1e-6, 1.0, True, None, None), lambda: _fastcall.norm_bwd(x, x, x, x, x, c, c, x, 1.0, None, None, None, None),
+                 lambda: _fastcall.clip_grad_norm([x], 1.0, None, None), lambda: _fastcall.clip_grad_norm([], 1.0, None, None), lambda: _fastcall.clip_grad_norm([None], 1.0, [x], None),
+                 lambda: _fastcall.conv_step(x, x, x, None, None, None), lambda: _fastcall.conv_step(None, None, None, None, None, None)):
+        assert call() is None

@@ -510,3 +510,55 @@ def test_refusals():
                  lambda: block.scan_bwd(dy, x, r, i, lam, states, workspace=torch.empty(4, dtype=torch.uint8, device="cuda"))):
         with pytest.raises(binding.DwconvError):
             call()
+
+
+# ---- the native form of the calls ----
+
+def _calls():
+    x, r, i, dy, lam = scan_inputs(2, 6, 70, BF16, 301)
+    h0, dh = rand(2, 6, seed=1), rand(2, 6, seed=2)
+    lengths, slots = torch.tensor([70, 9], dtype=torch.int32, device="cuda"), torch.tensor([1, -1], dtype=torch.int32, device="cuda")
+    states = block.scan_fwd(x, r, i, lam, h0, lengths)[2]
+    y, z, res, dout, dn, w, wn = norm_inputs(2, 6, 70, F32)
+    stats, stats0 = block.norm_fwd(y, z, res, w, wn)[2], block.norm_fwd(None, None, res, None, wn)[2]
+    tok, h, ring = x[..., 0].contiguous(), rand(3, 6, seed=3), rand(3, 6, 5, seed=4, dtype=BF16)
+    taps, pos = rand(6, 5, seed=5, dtype=BF16), torch.tensor([3, 9], dtype=torch.int32, device="cuda")
+    outs = lambda t, n: [torch.full_like(t, float("nan")) for _ in range(n)]        # noqa: E731
+    space = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    return {
+        "scan_fwd": lambda: block.scan_fwd(x, r, i, lam, h0, lengths), "scan_fwd bare": lambda: block.scan_fwd(x, r, i, lam, save=False),
+        "scan_fwd out": lambda: block.scan_fwd(x, r, i, lam, out=outs(x, 1)[0], workspace=space),
+        "scan_bwd": lambda: block.scan_bwd(dy, x, r, i, lam, states, dh, lengths),
+        "scan_bwd out": lambda: block.scan_bwd(dy, x, r, i, lam, states, out=outs(x, 3), workspace=space),
+        "scan_step": lambda: (block.scan_step(tok, tok, tok, lam, g := h.clone(), slots), g), "scan_step out": lambda: (block.scan_step(tok, tok, tok, lam, h.clone(), out=outs(tok, 1)[0]),),
+        "norm_fwd": lambda: block.norm_fwd(y, z, res, w, wn, scale=0.5), "norm_fwd bare": lambda: block.norm_fwd(None, None, res, None, wn, save=False),
+        "norm_fwd out": lambda: block.norm_fwd(y, z, res, w, wn, out=outs(y, 1)[0], out_n=outs(y, 1)[0]),
+        "norm_bwd": lambda: block.norm_bwd(dout, dn, y, z, res, w, wn, stats), "norm_bwd bare": lambda: block.norm_bwd(None, dn, None, None, res, None, wn, stats0),
+        "norm_bwd out": lambda: block.norm_bwd(dout, dn, y, z, res, w, wn, stats, out=outs(y, 3), workspace=space),
+        "conv_step": lambda: (block.conv_step(tok, taps, g := ring.clone(), pos, slots), g),
+        "clip": lambda: (block.clip_grad_norm(g := [y.clone(), x.clone()], 1.0), *g), "clip out": lambda: (block.clip_grad_norm((y, x), 1.0, out=(g := outs(y, 1) + outs(x, 1))), *g),
+    }
+
+
+def test_native_calls_give_the_same(monkeypatch):
+    from paper_2604_25422_amd import _fastcall
+    block.lib()
+    assert block._fast is _fastcall
+    for name, call in _calls().items():
+        fast = call()
+        with monkeypatch.context() as m:
+            m.setattr(block, "_fast", block._Declines)
+            general = call()
+        assert len(fast) == len(general), name
+        for a, b in zip(fast, general):
+            assert (a is None) == (b is None), name
+            if a is not None:
+                assert a.dtype == b.dtype and a.shape == b.shape and not a.requires_grad and torch.equal(a, b), name
+
+
+def test_native_calls_take_what_they_should(monkeypatch):
+    """They are the ones that run: none of the calls above is left to the general form."""
+    block.lib()
+    monkeypatch.setattr(block, "_check", None)
+    for name, call in _calls().items():
+        call()
