@@ -9,45 +9,64 @@ namespace {
 
 struct NormPlan {
     int E, NT, lx;              // tile kernel; E = 0: the streaming one
-    int row_tiles;
+    int row_tiles, run;
     long long tiles;
     int blocks;
 };
+
+constexpr int kMaxE = 6;        // packs of each tensor that a lane holds
 
 NormPlan plan_norm(int B, int C, int L, int dtype, bool backward)
 {
     NormPlan s{};
     const int V = dtype == DWCONV_F32 ? 4 : 8;
-    const int most = backward ? (dtype == DWCONV_F32 ? 8 : 6) : 8;      // packs of each tensor that the registers hold
-    if (L >= V) {
-        s.NT = 256;
-        s.lx = 2;
-        while (s.lx > 0 && (V << (s.lx - 1)) >= L) --s.lx;
-        while (s.NT < 512 && C > (s.NT >> s.lx) * most) s.NT *= 2;
-        while (s.lx > 0 && C > (s.NT >> s.lx) * most) --s.lx;
-        const int e = (int)ceil_div(C, s.NT >> s.lx);
-        if (e <= most) {
-            s.E = e;
-            s.row_tiles = (int)ceil_div(L, V << s.lx);
-        }
+    s.run = 1;
+    // Rows of a tile as long as a cache line (lx = 3) where the registers hold the channels, or else half of one: what a
+    // workgroup leaves of a line is fetched by its neighbour, if that is at work at the same time.  A wave's share E of the channels
+    // goes with what a larger workgroup costs: B128 C768 L1024 bf16 forward 220 us as 512 threads and half lines, 242 us as 1024
+    // threads and whole ones (336 us with a quarter of a line); B64 C768 L1024 fp32 233 and 206 us.  Backward, fp32: B32 C256 L4096
+    // 260 us as 1024 threads and E = 2, 269 us as 512 and E = 4; B64 C384 L1024 178 us with whole lines, 200 us with half ones.  bf16:
+    // B32 C256 L4096 151 us with half lines, 161 us with whole ones; B256 C64 L1024 80 us with whole ones and E = 1, 89 us with half.
+    const bool f32 = dtype == DWCONV_F32;
+    const auto take = [&](int lx, int NT, int most) {
+        const int rows = NT >> lx;
+        if (s.E || (V << lx) > L || ceil_div(C, rows) > most || (long long)rows * L * (16 / V) >= (1ll << 31)) return;
+        s.E = (int)ceil_div(C, rows);
+        s.NT = NT;
+        s.lx = lx;
+    };
+    for (int lx = 3; lx >= 0; --lx) {
+        const int few = backward ? (f32 ? 4 : lx == 3 ? 2 : kMaxE) : kMaxE;
+        take(lx, 256, few);
+        take(lx, 512, few);
+        if (f32) take(lx, 1024, backward ? 3 : kMaxE);
+        else if (!backward && lx < 3) take(lx, 1024, kMaxE);
     }
-    if (!s.E) {
+    if (s.E) {
+        s.row_tiles = (int)ceil_div(L, V << s.lx);
+    } else {
         s.NT = 256;
-        s.lx = 0;
         while (s.lx < 6 && (1 << s.lx) < L && (256 >> (s.lx + 1)) >= 4) ++s.lx;
         s.row_tiles = (int)ceil_div(L, 1 << s.lx);
     }
     s.tiles = (long long)B * s.row_tiles;
-    s.blocks = (int)std::min<long long>(s.tiles, backward ? 1024 : 1 << 20);
+    // (a workgroup per tile, in order: workgroups that walk several drift apart, and with them the halves of a line.  B128 C768 L1024
+    // bf16 backward 431 us, 512 us with two tiles each.  Above sixteen thousand of them their sums would be a tenth of the traffic)
+    if (backward && s.E) s.run = (int)ceil_div(s.tiles, 16384);
+    s.blocks = s.E ? (int)ceil_div(s.tiles, s.run) : (int)std::min<long long>(s.tiles, backward ? 1024 : 1 << 20);
     return s;
 }
-size_t red_bytes(const NormPlan &s, int V) { return (size_t)(s.NT / 64 + 1) * (V << s.lx) * sizeof(float); }
+size_t red_bytes(const NormPlan &s, int V) { return (size_t)(s.NT / 16 + 1) * (V << s.lx) * sizeof(float); }
+
+// Runs that the workgroups' sums are first added up in (4096 sums of 768 channels twice: 18 us by norm_sums_kernel alone); 0: not worth it.
+int sum_runs(const NormPlan &s) { return s.blocks >= 512 ? 64 : 0; }
 
 template <typename T, int E, bool BLOCK> void fwd_tile(const NormFwd<T> &p, const NormPlan &s, hipStream_t st)
 {
     const size_t lds = red_bytes(s, Pack<T>::V);
     if (s.NT == 256) norm_fwd_tile_kernel<T, E, 256, BLOCK><<<s.blocks, 256, lds, st>>>(p);
-    else norm_fwd_tile_kernel<T, E, 512, BLOCK><<<s.blocks, 512, lds, st>>>(p);
+    else if (s.NT == 512) norm_fwd_tile_kernel<T, E, 512, BLOCK><<<s.blocks, 512, lds, st>>>(p);
+    else norm_fwd_tile_kernel<T, E, 1024, BLOCK><<<s.blocks, 1024, lds, st>>>(p);
 }
 template <typename T, bool BLOCK> void launch_fwd(const NormFwd<T> &p, const NormPlan &s, hipStream_t st)
 {
@@ -58,16 +77,15 @@ template <typename T, bool BLOCK> void launch_fwd(const NormFwd<T> &p, const Nor
     case 3: return fwd_tile<T, 3, BLOCK>(p, s, st);
     case 4: return fwd_tile<T, 4, BLOCK>(p, s, st);
     case 5: return fwd_tile<T, 5, BLOCK>(p, s, st);
-    case 6: return fwd_tile<T, 6, BLOCK>(p, s, st);
-    case 7: return fwd_tile<T, 7, BLOCK>(p, s, st);
-    default: return fwd_tile<T, 8, BLOCK>(p, s, st);
+    default: return fwd_tile<T, 6, BLOCK>(p, s, st);
     }
 }
 template <typename T, int E, bool BLOCK> void bwd_tile(const NormBwd<T> &p, const NormPlan &s, hipStream_t st)
 {
     const size_t lds = red_bytes(s, Pack<T>::V);
     if (s.NT == 256) norm_bwd_tile_kernel<T, E, 256, BLOCK><<<s.blocks, 256, lds, st>>>(p);
-    else norm_bwd_tile_kernel<T, E, 512, BLOCK><<<s.blocks, 512, lds, st>>>(p);
+    else if (s.NT == 512) norm_bwd_tile_kernel<T, E, 512, BLOCK><<<s.blocks, 512, lds, st>>>(p);
+    else if constexpr (sizeof(T) == 4 && E <= 3) norm_bwd_tile_kernel<T, E, 1024, BLOCK><<<s.blocks, 1024, lds, st>>>(p);
 }
 template <typename T, bool BLOCK> void launch_bwd(const NormBwd<T> &p, const NormPlan &s, float *dw, float *dw_next, hipStream_t st)
 {
@@ -78,17 +96,20 @@ template <typename T, bool BLOCK> void launch_bwd(const NormBwd<T> &p, const Nor
     case 3: bwd_tile<T, 3, BLOCK>(p, s, st); break;
     case 4: bwd_tile<T, 4, BLOCK>(p, s, st); break;
     case 5: bwd_tile<T, 5, BLOCK>(p, s, st); break;
-    case 6: bwd_tile<T, 6, BLOCK>(p, s, st); break;
-    default:
-        if constexpr (sizeof(T) == 4) {
-            if (s.E == 7) bwd_tile<T, 7, BLOCK>(p, s, st);
-            else bwd_tile<T, 8, BLOCK>(p, s, st);
-        }
+    default: bwd_tile<T, 6, BLOCK>(p, s, st); break;
     }
-    norm_sums_kernel<<<dim3((unsigned)ceil_div(p.C, 32), 2), 1024, 0, st>>>(p.part, s.blocks, p.C, dw, dw_next);
+    const float *part = p.part;
+    int M = s.blocks;
+    if (const int runs = sum_runs(s)) {
+        float *to = p.part + (size_t)s.blocks * 2 * p.C;
+        norm_runs_kernel<<<dim3((unsigned)ceil_div(2ll * p.C, 64), runs), 256, 0, st>>>(part, M, (int)ceil_div(M, runs), 2 * p.C, to);
+        part = to;
+        M = runs;
+    }
+    norm_sums_kernel<<<dim3((unsigned)ceil_div(p.C, 32), 2), 1024, 0, st>>>(part, M, p.C, dw, dw_next);
 }
 
-size_t part_bytes(const NormPlan &s, int C) { return (size_t)s.blocks * 2 * C * sizeof(float); }
+size_t part_bytes(const NormPlan &s, int C) { return (size_t)(s.blocks + sum_runs(s)) * 2 * C * sizeof(float); }
 
 template <typename T>
 void run_fwd(const dwconv_seq &y, const dwconv_seq &z, const dwconv_seq &res, const float *w, const float *w_next, const dwconv_seq_out &out,
@@ -104,7 +125,7 @@ void run_bwd(const dwconv_seq &dout, const dwconv_seq &dn, const dwconv_seq &y, 
              float *dw_next, float *part, int B, int C, int L, float scale, const NormPlan &s, hipStream_t st)
 {
     const NormBwd<T> p{seq<T>(dout), seq<T>(dn), seq<T>(y), seq<T>(z), seq<T>(res), w, w_next, stats, seq<T>(dy), seq<T>(dz), seq<T>(dres), part,
-                       B, C, L, scale, s.lx, s.tiles, s.row_tiles};
+                       B, C, L, scale, s.lx, s.tiles, s.row_tiles, s.run};
     if (y.data) launch_bwd<T, true>(p, s, dw, dw_next, st);
     else launch_bwd<T, false>(p, s, nullptr, dw_next, st);
 }

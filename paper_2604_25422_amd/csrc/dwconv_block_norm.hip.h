@@ -32,7 +32,7 @@ template <typename T> struct NormBwd {
     float scale;
     int lx;
     long long tiles;
-    int row_tiles;
+    int row_tiles, run; // run: tiles of a workgroup of the tile kernel, one behind the other
 };
 
 // 16 bytes of a row.
@@ -51,25 +51,15 @@ template <> struct Pack<bf16_t> {
         return __uint_as_float((k & 1) ? (u & 0xffff0000u) : (u << 16));
     }
 };
-__device__ __forceinline__ void load_pack(Pack<float> &e, const float *p, int left)
-{
-    if (left >= 4) e.w = *reinterpret_cast<const floatx4_any *>(p);
-    else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) e.w[k] = k < left ? p[k] : 0.0f;
-    }
+__device__ __forceinline__ void load_pack(Pack<float> &e, const float *p) { e.w = *reinterpret_cast<const floatx4_any *>(p); }
+__device__ __forceinline__ void load_pack(Pack<bf16_t> &e, const bf16_t *p) { e.w = *reinterpret_cast<const uintx4_any *>(p); }
+__device__ __forceinline__ void store_pack(float *p, const float (&v)[4]) {
+    *reinterpret_cast<floatx4_any *>(p) = floatx4_any{v[0], v[1], v[2], v[3]};
 }
-__device__ __forceinline__ void load_pack(Pack<bf16_t> &e, const bf16_t *p, int left) { e.w = load8(p, left).w; }
-__device__ __forceinline__ void store_pack(float *p, const float (&v)[4], int left)
+__device__ __forceinline__ void store_pack(bf16_t *p, const float (&v)[8])
 {
-    if (left >= 4) *reinterpret_cast<floatx4_any *>(p) = floatx4_any{v[0], v[1], v[2], v[3]};
-    else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (k < left) p[k] = v[k];
-    }
+    *reinterpret_cast<uintx4_any *>(p) = uintx4_any{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
 }
-__device__ __forceinline__ void store_pack(bf16_t *p, const float (&v)[8], int left) { store8(p, v, left); }
 
 // Workgroups go to the eight dies in turn; give every die a run of neighbouring tiles, whose rows share cache lines.
 __device__ __forceinline__ long long die_run(long long i, long long n)
@@ -78,26 +68,41 @@ __device__ __forceinline__ long long die_run(long long i, long long n)
     return k * q + (k < r ? k : r) + (i >> 3);
 }
 
-// v[k] summed over the channels of the tile (the lanes of a wave that stand at the same positions, then the waves), for the
-// positions of this lane.  red: [NT / 64 + 1][64 * V] floats (a row of at most 64 lanes).
+// v[k] summed over the channels of the tile, for the positions of this lane: over the lanes of sixteen that stand at the same
+// positions (moves inside a row of lanes, which cost no more than the addition), then over the rows of lanes in LDS, four
+// lanes a position.  red: [NT / 16 + 1][V << lx] floats; a row of the tile has at most sixteen lanes.
 template <int V, int NT> __device__ __forceinline__ void channel_sums(float (&v)[V], int lx, float *red)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = lane & ((1 << lx) - 1), T = V << lx;
-    for (int d = 1 << lx; d < 64; d *= 2) {
+    const int x = threadIdx.x & ((1 << lx) - 1), T = V << lx;
+    if (lx < 1) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) v[k] += __shfl_xor(v[k], d, 64);
+        for (int k = 0; k < V; ++k) v[k] += dpp<0xB1>(0.0f, v[k]);       // the neighbouring lane
     }
-    if (lane < (1 << lx)) {
+    if (lx < 2) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) red[wave * T + x * V + k] = v[k];
+        for (int k = 0; k < V; ++k) v[k] += dpp<0x4E>(0.0f, v[k]);       // the other two of four
+    }
+    if (lx < 3) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] += dpp<0x124>(0.0f, v[k]);      // four lanes on, round the sixteen
+    }
+    if (lx < 4) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] += dpp<0x128>(0.0f, v[k]);      // eight lanes on
+    }
+    if ((threadIdx.x & 15) < (1 << lx)) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) red[(threadIdx.x >> 4) * T + x * V + k] = v[k];
     }
     __syncthreads();
-    float *sum = red + NT / 64 * T;
-    for (int t = threadIdx.x; t < T; t += NT) {
+    float *sum = red + NT / 16 * T;
+    for (int i = threadIdx.x; i < 4 * T; i += NT) {
         float s = 0.0f;
 #pragma unroll
-        for (int w = 0; w < NT / 64; ++w) s += red[w * T + t];
-        sum[t] = s;
+        for (int r = 0; r < NT / 64; ++r) s += red[(4 * r + (i & 3)) * T + (i >> 2)];
+        s += dpp<0xB1>(0.0f, s);
+        s += dpp<0x4E>(0.0f, s);
+        if ((i & 3) == 0) sum[i >> 2] = s;
     }
     __syncthreads();
 #pragma unroll
@@ -105,76 +110,110 @@ template <int V, int NT> __device__ __forceinline__ void channel_sums(float (&v)
     // (the next use of `red` writes its first part, which nobody reads any more, and `sum` behind a barrier)
 }
 
+// What the registers hold from here on counts as new: nothing that an earlier pass made of it (widened elements, gates) is kept
+// in more registers for a later one, which makes it again.
+__device__ __forceinline__ void forget(Pack<float> &e) { asm("" : "+v"(e.w)); }
+__device__ __forceinline__ void forget(Pack<bf16_t> &e) { asm("" : "+v"(e.w)); }
+// ... and what is to be in a register here, so that the terms of a sum do not wait for it in registers of their own.
+__device__ __forceinline__ void settle(float &v) { asm volatile("" : "+v"(v)); }
+
 __device__ __forceinline__ float inv_sqrt(float v) { return 1.0f / sqrtf(v); }
+
+// Element at a workgroup's pointer and a lane's offset in bytes.
+template <typename T> __device__ __forceinline__ const T *place(const T *p, unsigned bytes)
+{
+    return reinterpret_cast<const T *>(reinterpret_cast<const char *>(p) + bytes);
+}
+template <typename T> __device__ __forceinline__ T *place(T *p, unsigned bytes) { return reinterpret_cast<T *>(reinterpret_cast<char *>(p) + bytes); }
+
+// Tiles lie end to end along a row; the last one of a row that is no whole number of tiles is moved back to end with it, so that
+// every tile is whole.  What it shares with the one before it comes out the same from both, and counts once in the parameters' sums.
+struct TileAt {
+    int b, t0, again;       // batch entry, first position, positions that the tile before has counted
+};
+__device__ __forceinline__ TileAt tile_at(long long tile, int row_tiles, int T, int L)
+{
+    const int b = (int)(tile / row_tiles), t = (int)(tile - (long long)b * row_tiles) * T, over = t + T > L ? t + T - L : 0;
+    return TileAt{b, t - over, over};
+}
 
 template <typename T, int E, int NT, bool BLOCK> __global__ __launch_bounds__(NT) void norm_fwd_tile_kernel(NormFwd<T> p)
 {
     constexpr int V = Pack<T>::V;
     extern __shared__ float red[];
     const int x = threadIdx.x & ((1 << p.lx) - 1), c0 = threadIdx.x >> p.lx, step = NT >> p.lx;
-    for (long long i = blockIdx.x; i < p.tiles; i += gridDim.x) {
-        const long long tile = die_run(i, p.tiles);
-        const int b = (int)(tile / p.row_tiles), t = ((int)(tile - (long long)b * p.row_tiles) << p.lx) * V + x * V, left = p.L - t;
-        Pack<T> y[E], z[E], res[E];
+    // a lane's place is the same in every pack and tensor: one offset that is its own, the rest is the workgroup's
+    const unsigned mine = ((unsigned)c0 * (unsigned)p.L + (unsigned)(x * V)) * (unsigned)sizeof(T);
+    const TileAt tile = tile_at(die_run(blockIdx.x, p.tiles), p.row_tiles, V << p.lx, p.L);
+    const auto at = [&](const auto &s, int e) { return place(s.p + ((long long)tile.b * s.bs + (long long)(e * step) * p.L + tile.t0), mine); };
+    // (only the last round of channels can be short)
+    const bool in = c0 + (E - 1) * step < p.C;
+    Pack<T> y[E], z[E], res[E];
+    y[E - 1] = z[E - 1] = res[E - 1] = Pack<T>{};
+    if constexpr (BLOCK) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int c = c0 + e * step, room = c < p.C ? left : 0;
-            load_pack(res[e], p.res.row(b, c, p.L) + t, room);
-            if (BLOCK) {
-                load_pack(y[e], p.y.row(b, c, p.L) + t, room);
-                load_pack(z[e], p.z.row(b, c, p.L) + t, room);
-            }
+        for (int e = 0; e < E; ++e)
+            if (e < E - 1 || in) load_pack(y[e], at(p.y, e));
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        if (e < E - 1 || in) {
+            load_pack(res[e], at(p.res, e));
+            if (BLOCK) load_pack(z[e], at(p.z, e));
         }
-        float r1[V], r2[V], o[E][V];
-        if constexpr (BLOCK) {
+    }
+    float w[E], wn[E];
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                r1[k] = 0.0f;
+    for (int e = 0; e < E; ++e) {
+        const int c = c0 + e * step;
+        const bool have = e < E - 1 || in;
+        w[e] = BLOCK && have ? p.scale * p.w[c] : 0.0f;
+        wn[e] = have ? p.w_next[c] : 0.0f;
+    }
+    float r1[V], r2[V], o[E][V];
+    if constexpr (BLOCK) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) r1[k] = fmaf(y[e][k], y[e][k], r1[k]);
-            }
-            channel_sums<V, NT>(r1, p.lx, red);
+        for (int k = 0; k < V; ++k) {
+            r1[k] = 0.0f;
 #pragma unroll
-            for (int k = 0; k < V; ++k) r1[k] = inv_sqrt(r1[k] / (float)p.C + p.eps);
+            for (int e = 0; e < E; ++e) r1[k] = fmaf(y[e][k], y[e][k], r1[k]);
         }
+        channel_sums<V, NT>(r1, p.lx, red);
 #pragma unroll
-        for (int k = 0; k < V; ++k) r2[k] = 0.0f;
+        for (int k = 0; k < V; ++k) r1[k] = inv_sqrt(r1[k] / (float)p.C + p.eps);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int c = c0 + e * step;
-            const float w = BLOCK && c < p.C ? p.scale * p.w[c] : 0.0f;
+        for (int e = 0; e < E; ++e) forget(y[e]);
+    }
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                o[e][k] = res[e][k];
-                if constexpr (BLOCK) {
-                    const float zz = z[e][k];
-                    o[e][k] = fmaf(zz * sigmoid(zz), y[e][k] * r1[k] * w, o[e][k]);
-                }
-                r2[k] = fmaf(o[e][k], o[e][k], r2[k]);
+    for (int k = 0; k < V; ++k) r2[k] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            o[e][k] = res[e][k];
+            if constexpr (BLOCK) {
+                const float zz = z[e][k];
+                o[e][k] = fmaf(zz * sigmoid(zz), y[e][k] * r1[k] * w[e], o[e][k]);
             }
-            if (BLOCK && c < p.C) store_pack(p.out.row(b, c, p.L) + t, o[e], left);
+            r2[k] = fmaf(o[e][k], o[e][k], r2[k]);
         }
-        channel_sums<V, NT>(r2, p.lx, red);
+        if (BLOCK && (e < E - 1 || in)) store_pack(at(p.out, e), o[e]);
+    }
+    channel_sums<V, NT>(r2, p.lx, red);
 #pragma unroll
-        for (int k = 0; k < V; ++k) r2[k] = inv_sqrt(r2[k] / (float)p.C + p.eps);
+    for (int k = 0; k < V; ++k) r2[k] = inv_sqrt(r2[k] / (float)p.C + p.eps);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int c = c0 + e * step;
-            if (c < p.C) {
-                const float w = p.w_next[c];
+    for (int e = 0; e < E; ++e) {
 #pragma unroll
-                for (int k = 0; k < V; ++k) o[e][k] *= r2[k] * w;
-                store_pack(p.n.row(b, c, p.L) + t, o[e], left);
-            }
-        }
-        if (p.stats && c0 == 0) {
-            float *s = p.stats + (long long)b * 2 * p.L + t;
+        for (int k = 0; k < V; ++k) o[e][k] *= r2[k] * wn[e];
+        if (e < E - 1 || in) store_pack(at(p.n, e), o[e]);
+    }
+    if (p.stats && c0 == 0) {
+        float *s = p.stats + (long long)tile.b * 2 * p.L + tile.t0 + x * V;
 #pragma unroll
-            for (int k = 0; k < V; ++k)
-                if (k < left) {
-                    if (BLOCK) s[k] = r1[k];
-                    s[p.L + k] = r2[k];
-                }
+        for (int k = 0; k < V; ++k) {
+            if (BLOCK) s[k] = r1[k];
+            s[p.L + k] = r2[k];
         }
     }
 }
@@ -184,91 +223,113 @@ template <typename T, int E, int NT, bool BLOCK> __global__ __launch_bounds__(NT
     constexpr int V = Pack<T>::V;
     extern __shared__ float red[];
     const int x = threadIdx.x & ((1 << p.lx) - 1), c0 = threadIdx.x >> p.lx, step = NT >> p.lx;
-    float sum_w[E], sum_n[E];
+    const unsigned mine = ((unsigned)c0 * (unsigned)p.L + (unsigned)(x * V)) * (unsigned)sizeof(T);
+    const bool in = c0 + (E - 1) * step < p.C;
+    float w[E], wn[E], sum_w[E], sum_n[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum_w[e] = sum_n[e] = 0.0f;
+    for (int e = 0; e < E; ++e) {
+        const int c = c0 + e * step;
+        const bool have = e < E - 1 || in;
+        w[e] = BLOCK && have ? p.scale * p.w[c] : 0.0f;
+        wn[e] = have ? p.w_next[c] : 0.0f;
+        sum_w[e] = sum_n[e] = 0.0f;
+    }
     const float inv_c = 1.0f / (float)p.C;
-    for (long long i = blockIdx.x; i < p.tiles; i += gridDim.x) {
-        const long long tile = die_run(i, p.tiles);
-        const int b = (int)(tile / p.row_tiles), t = ((int)(tile - (long long)b * p.row_tiles) << p.lx) * V + x * V, left = p.L - t;
+    const long long block = die_run(blockIdx.x, gridDim.x), end = (block + 1) * p.run < p.tiles ? (block + 1) * p.run : p.tiles;
+    for (long long i = block * p.run; i < end; ++i) {
+        const TileAt tile = tile_at(i, p.row_tiles, V << p.lx, p.L);
+        const auto at = [&](const auto &s, int e) { return place(s.p + ((long long)tile.b * s.bs + (long long)(e * step) * p.L + tile.t0), mine); };
         Pack<T> y[E], z[E], res[E], dn[E], dout[E];
+        y[E - 1] = z[E - 1] = res[E - 1] = dn[E - 1] = Pack<T>{};
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int c = c0 + e * step, room = c < p.C ? left : 0;
-            load_pack(res[e], p.res.row(b, c, p.L) + t, room);
-            load_pack(dn[e], p.dn.row(b, c, p.L) + t, room);
-            load_pack(dout[e], p.dout.row(b, c, p.L) + t, p.dout.p ? room : 0);
-            if (BLOCK) {
-                load_pack(y[e], p.y.row(b, c, p.L) + t, room);
-                load_pack(z[e], p.z.row(b, c, p.L) + t, room);
+            if (e < E - 1 || in) {
+                load_pack(res[e], at(p.res, e));
+                load_pack(dn[e], at(p.dn, e));
+                if (BLOCK) {
+                    load_pack(y[e], at(p.y, e));
+                    load_pack(z[e], at(p.z, e));
+                }
             }
         }
-        float r1[V], r2[V], m[V], o[E][V];
-        const float *s = p.stats + (long long)b * 2 * p.L + t;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            dout[e] = Pack<T>{};
+            if (p.dout.p && (e < E - 1 || in)) load_pack(dout[e], at(p.dout, e));
+        }
+        float r1[V], r2[V], m[V];
+        const float *s = p.stats + (long long)tile.b * 2 * p.L + tile.t0 + x * V;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            r1[k] = BLOCK && k < left ? s[k] : 0.0f;
-            r2[k] = k < left ? s[p.L + k] : 0.0f;
+            r1[k] = BLOCK ? s[k] : 0.0f;
+            r2[k] = s[p.L + k];
             m[k] = 0.0f;
         }
-        // the second norm: o is out / sqrt(m2 + eps), then dout + its gradient
+        const int again = tile.again - x * V;           // of this lane's positions
+        // out / sqrt(m2 + eps) of element k of pack e, and what silu gave it
+        const auto normed = [&](int e, int k, float &silu, float &g) {
+            float v = res[e][k];
+            silu = g = 0.0f;
+            if constexpr (BLOCK) {
+                g = sigmoid(z[e][k]);
+                silu = z[e][k] * g;
+                v = fmaf(silu * (y[e][k] * r1[k]), w[e], v);
+            }
+            return v * r2[k];
+        };
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int c = c0 + e * step;
-            const bool in = c < p.C;
-            const float w = BLOCK && in ? p.scale * p.w[c] : 0.0f, wn = in ? p.w_next[c] : 0.0f;
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                float v = res[e][k];
-                if constexpr (BLOCK) {
-                    const float zz = z[e][k];
-                    v = fmaf(zz * sigmoid(zz), y[e][k] * r1[k] * w, v);
-                }
-                o[e][k] = v * r2[k];
-                m[k] = fmaf(dn[e][k] * wn, o[e][k], m[k]);
-                sum_n[e] = fmaf(dn[e][k], o[e][k], sum_n[e]);
+                float silu, g;
+                const float oh = normed(e, k, silu, g), d = dn[e][k] * oh;
+                m[k] = fmaf(d, wn[e], m[k]);
+                sum_n[e] += k < again ? 0.0f : d;
             }
+            settle(sum_n[e]);
+            forget(res[e]), forget(dn[e]);
+            if (BLOCK) forget(y[e]), forget(z[e]);
+            __builtin_amdgcn_sched_barrier(0);
         }
         channel_sums<V, NT>(m, p.lx, red);
 #pragma unroll
         for (int k = 0; k < V; ++k) m[k] *= inv_c;
-        float m1[V];
+        float m1[V], dyh[E][V];
 #pragma unroll
         for (int k = 0; k < V; ++k) m1[k] = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int c = c0 + e * step;
-            const bool in = c < p.C;
-            const float w = BLOCK && in ? p.scale * p.w[c] : 0.0f, wn = in ? p.w_next[c] : 0.0f;
-            float dz[V];
+            float d[V], dz[V];
 #pragma unroll
-            for (int k = 0; k < V; ++k) o[e][k] = fmaf(r2[k], dn[e][k] * wn - o[e][k] * m[k], dout[e][k]);
-            if (in) store_pack(p.dres.row(b, c, p.L) + t, o[e], left);
-            if constexpr (BLOCK) {
-#pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    // out = .. + silu(z) yh w; d silu = sigmoid (1 + z (1 - sigmoid))
-                    const float zz = z[e][k], yh = y[e][k] * r1[k], d = o[e][k];
-                    float rest;
-                    const float g = sigmoid_both(zz, rest), silu = zz * g;
-                    dz[k] = d * (yh * w) * (g * fmaf(zz, rest, 1.0f));
-                    sum_w[e] = fmaf(d * silu, yh, sum_w[e]);
-                    o[e][k] = d * silu * w;
-                    m1[k] = fmaf(o[e][k], yh, m1[k]);
+            for (int k = 0; k < V; ++k) {
+                float silu, g;
+                const float oh = normed(e, k, silu, g);
+                d[k] = fmaf(r2[k], fmaf(-oh, m[k], dn[e][k] * wn[e]), dout[e][k]);
+                if constexpr (BLOCK) {
+                    // out = .. + silu(z) yh w; d silu = sigmoid (1 + z (1 - sigmoid)) = sigmoid + silu (1 - sigmoid)
+                    const float yh = y[e][k] * r1[k], dw = d[k] * w[e], dg = d[k] * (silu * yh);
+                    dz[k] = dw * yh * fmaf(silu, 1.0f - g, g);
+                    dyh[e][k] = dw * silu;
+                    sum_w[e] += k < again ? 0.0f : dg;
+                    m1[k] = fmaf(dg, w[e], m1[k]);
                 }
-                if (in) store_pack(p.dz.row(b, c, p.L) + t, dz, left);
             }
+            if (e < E - 1 || in) {
+                store_pack(at(p.dres, e), d);
+                if constexpr (BLOCK) store_pack(at(p.dz, e), dz);
+            }
+            if (BLOCK) settle(sum_w[e]), forget(y[e]);
+            __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (BLOCK) {
             channel_sums<V, NT>(m1, p.lx, red);
 #pragma unroll
-            for (int k = 0; k < V; ++k) m1[k] *= inv_c;
+            for (int k = 0; k < V; ++k) m1[k] *= inv_c * r1[k];
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const int c = c0 + e * step;
 #pragma unroll
-                for (int k = 0; k < V; ++k) o[e][k] = r1[k] * (o[e][k] - y[e][k] * r1[k] * m1[k]);
-                if (c < p.C) store_pack(p.dy.row(b, c, p.L) + t, o[e], left);
+                for (int k = 0; k < V; ++k) dyh[e][k] = r1[k] * fmaf(-y[e][k], m1[k], dyh[e][k]);
+                if (e < E - 1 || in) store_pack(at(p.dy, e), dyh[e]);
             }
         }
     }
@@ -287,16 +348,19 @@ template <typename T, int E, int NT, bool BLOCK> __global__ __launch_bounds__(NT
 }
 
 // Any C and L: a lane per position, 2^lx of them side by side, the channels over the other lanes, the tensors read again for
-// every sum (from the caches, where a tile still is).  red: [4 + 1][64] floats.
+// every sum (from the caches, where a tile still is).  red: [4][64] floats.
 __device__ __forceinline__ float channel_sum(float v, int lx, float *red)
 {
-    float a[1] = {v};
-    channel_sums<1, 256>(a, lx, red);
-    return a[0];
+    const int x = threadIdx.x & ((1 << lx) - 1), lane = threadIdx.x & 63;
+    for (int d = 1 << lx; d < 64; d *= 2) v += __shfl_xor(v, d, 64);
+    __syncthreads();                            // (the sums of the call before have been read)
+    if (lane < (1 << lx)) red[(threadIdx.x >> 6) * 64 + x] = v;
+    __syncthreads();
+    return (red[x] + red[64 + x]) + (red[128 + x] + red[192 + x]);
 }
 template <typename T, bool BLOCK> __global__ __launch_bounds__(256) void norm_fwd_stream_kernel(NormFwd<T> p)
 {
-    __shared__ float red[5 * 64];
+    __shared__ float red[4 * 64];
     const int x = threadIdx.x & ((1 << p.lx) - 1), c0 = threadIdx.x >> p.lx, step = 256 >> p.lx;
     for (long long i = blockIdx.x; i < p.tiles; i += gridDim.x) {
         const long long tile = die_run(i, p.tiles);
@@ -339,7 +403,7 @@ template <typename T, bool BLOCK> __global__ __launch_bounds__(256) void norm_fw
 }
 template <typename T, bool BLOCK> __global__ __launch_bounds__(256) void norm_bwd_stream_kernel(NormBwd<T> p)
 {
-    __shared__ float red[5 * 64];
+    __shared__ float red[4 * 64];
     const int x = threadIdx.x & ((1 << p.lx) - 1), c0 = threadIdx.x >> p.lx, step = 256 >> p.lx;
     float *part = p.part + (long long)blockIdx.x * 2 * p.C;
     if (x == 0)
@@ -403,6 +467,20 @@ template <typename T, bool BLOCK> __global__ __launch_bounds__(256) void norm_bw
     }
 }
 
+// Many workgroups leave many sums: runs of `rows` of them added up by workgroups of their own first.
+__global__ __launch_bounds__(256) void norm_runs_kernel(const float *part, int M, int rows, int N, float *runs)
+{
+    __shared__ float sums[4][64];
+    const int tc = threadIdx.x & 63, tm = threadIdx.x >> 6, c = blockIdx.x * 64 + tc, from = blockIdx.y * rows, to = from + rows < M ? from + rows : M;
+    float sum = 0.0f;
+    if (c < N) {
+#pragma unroll 8
+        for (int m = from + tm; m < to; m += 4) sum += part[(long long)m * N + c];
+    }
+    sums[tm][tc] = sum;
+    __syncthreads();
+    if (tm == 0 && c < N) runs[(long long)blockIdx.y * N + c] = (sums[0][tc] + sums[1][tc]) + (sums[2][tc] + sums[3][tc]);
+}
 // dw and dw_next: the workgroups' sums in a fixed order.
 __global__ __launch_bounds__(1024) void norm_sums_kernel(const float *part, int M, int C, float *dw, float *dw_next)
 {
