@@ -199,6 +199,18 @@ template <int G> __device__ __forceinline__ Span scan_down16(Span s, int lane)
 __device__ __forceinline__ float from_lane_before(float first, float v) { return dpp<0x138>(first, v); }   // lane 0: first
 __device__ __forceinline__ float from_lane_behind(float last, float v) { return dpp<0x130>(last, v); }     // lane 63: last
 
+// Sum over groups of 2^lg lanes (lg the same for the wave), in every lane of a group, in a fixed order: moves inside a row of sixteen
+// lanes come with the addition.
+__device__ __forceinline__ float group_sum(float v, int lg)
+{
+    if (lg > 0) v += dpp<0xB1>(0.0f, v);            // the neighbouring lane
+    if (lg > 1) v += dpp<0x4E>(0.0f, v);            // the other two of four
+    if (lg > 2) v += dpp<0x141>(0.0f, v);           // eight mirrored: the other four
+    if (lg > 3) v += dpp<0x140>(0.0f, v);           // sixteen mirrored
+    if (lg > 4) v += __shfl_xor(v, 16, 64);
+    if (lg > 5) v += __shfl_xor(v, 32, 64);
+    return v;
+}
 // Sum over groups of G lanes, the same in every lane of a group, in a fixed order.
 template <int G> __device__ __forceinline__ float group_sum(float v)
 {

@@ -21,10 +21,125 @@ __device__ __forceinline__ int ring_place(int pos, int K)       // pos mod K, in
     return p < 0 ? p + K : p;
 }
 
-// 2^lg lanes for each (b, c), each with every 2^lg-th place of the ring; place s holds tap (s - p - 1) mod K.
-template <typename T> __global__ __launch_bounds__(256) void conv_step_kernel(ConvStep<T> p, int lg)
+// V neighbouring elements, widened.
+typedef unsigned uintx2_any __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ void load_wide(float (&v)[4], const float *p)
 {
-    const int lane = threadIdx.x & ((1 << lg) - 1), c = (int)((blockIdx.x * 256u + threadIdx.x) >> lg);
+    const floatx4_any u = *reinterpret_cast<const floatx4_any *>(p);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = u[k];
+}
+__device__ __forceinline__ void load_wide(float (&v)[4], const bf16_t *p)
+{
+    const uintx2_any u = *reinterpret_cast<const uintx2_any *>(p);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) v[2 * k] = __uint_as_float(u[k] << 16), v[2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
+}
+__device__ __forceinline__ void load_wide(float (&v)[8], const bf16_t *p)
+{
+    const Eight<bf16_t> u = load8(p, 8);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = u[k];
+}
+
+// pos mod K of 0 <= pos < 2^31 through a quotient that is at most one too small: `inverse` is floor((2^32 - 1) / K).
+__device__ __forceinline__ int ring_place(int pos, unsigned inverse, int K)
+{
+    const unsigned p = (unsigned)pos & 0x7fffffffu, r = p - __umulhi(p, inverse) * (unsigned)K;
+    return (int)(r < (unsigned)K ? r : r - (unsigned)K);
+}
+
+// 2^lg lanes for each (b, c), each with V neighbouring places of the ring at a time.  Place k holds tap (k - p - 1) mod K, so the
+// taps a lane needs are V neighbours, rotated by the sequence's position: the workgroup's channels' taps lie in LDS, their first
+// V - 1 once more behind the last, and one staging serves every sequence the workgroup walks, U of them in flight.  Few values pass
+// through (13 MB for B256 C768 K32 bf16, 8.7 us): what it takes is a chain of three loads (slot, ring, store) and the
+// instructions around them; large pools are read at 3.1 TB/s (B1024 C512 K64 fp32 44 us).
+template <typename T, int V, int U> __global__ __launch_bounds__(256) void conv_step_kernel(ConvStep<T> p, int lg, unsigned inverse)
+{
+    extern __shared__ float taps[];
+    const int lane = threadIdx.x & ((1 << lg) - 1), row = threadIdx.x >> lg, c0 = blockIdx.x * (256 >> lg), K = p.K;
+    const bool in = c0 + row < p.C;
+    const unsigned mine = (unsigned)(row * K);              // of the workgroup's channels
+    float *w = taps + row * (K + V - 1);
+    bool staged = false;
+    // (positions, slots and the places of the rings are the workgroup's: scalar work beside the lanes')
+    for (long long b0 = (long long)blockIdx.y * U; b0 < p.B; b0 += (long long)gridDim.y * U) {
+        T *ring[U];
+        T x[U];
+        int at[U];
+        float sum[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int b = (int)(b0 + u < p.B ? b0 + u : p.B - 1), s = p.slots ? p.slots[b] : b;
+            const bool on = b0 + u < p.B && s >= 0 && s < p.pool;
+            ring[u] = on ? p.ring + ((long long)s * p.C + c0) * K : nullptr;
+            at[u] = ring_place(p.pos[b], inverse, K);
+            x[u] = T{};
+            if (on && in) x[u] = (p.x.p + ((long long)b * p.x.bs + c0))[row];
+            sum[u] = 0.0f;
+        }
+        for (int k0 = 0; k0 < K; k0 += V << lg) {
+            const int k = k0 + lane * V;
+            float v[U][V];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[u][i] = 0.0f;
+                if (!ring[u] || !in) continue;
+                if (k + V <= K) load_wide(v[u], ring[u] + (mine + (unsigned)k));
+                else {
+#pragma unroll
+                    for (int i = 0; i < V - 1; ++i)
+                        if (k + i < K) v[u][i] = ld_elem(ring[u] + (mine + (unsigned)(k + i)));
+                }
+            }
+            if (!staged) {                      // (the rings are on their way meanwhile)
+                if (in) {
+                    const T *from = p.w + (long long)c0 * K;
+                    for (int j = lane * V; j < K; j += V << lg) {
+                        float f[V] = {};
+                        if (j + V <= K) load_wide(f, from + (mine + (unsigned)j));
+                        else {
+#pragma unroll
+                            for (int i = 0; i < V - 1; ++i)
+                                if (j + i < K) f[i] = ld_elem(from + (mine + (unsigned)(j + i)));
+                        }
+#pragma unroll
+                        for (int i = 0; i < V; ++i) {
+                            if (j + i < K) w[j + i] = f[i];
+                            // (the first V - 1 again behind the last; of fewer taps they come round more than once)
+                            if (j == 0 && i < K)
+                                for (int o = i + K; o < K + V - 1; o += K) w[o] = f[i];
+                        }
+                    }
+                }
+                __syncthreads();
+                staged = true;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (!ring[u]) continue;
+                const int new_at = at[u] - k;           // of the four, where the new input goes
+                int j = k - at[u] - 1;
+                j = j < 0 ? j + K : j;
+                j = j < K ? j : K - 1;                  // (lanes behind the end of the ring: any tap, their elements are zeros)
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[u] = fmaf(i == new_at ? ld_elem(&x[u]) : v[u][i], w[j + i], sum[u]);
+                if (in && (unsigned)new_at < (unsigned)V) ring[u][mine + (unsigned)at[u]] = x[u];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            sum[u] = group_sum(sum[u], lg);
+            if (lane == 0 && in && b0 + u < p.B) st_elem(p.y.p + ((b0 + u) * p.y.bs + c0) + row, ring[u] ? sum[u] : 0.0f);
+        }
+    }
+}
+
+// Rings whose taps do not fit LDS (thousands of taps): a lane takes every 64th place and its tap from memory.
+template <typename T> __global__ __launch_bounds__(256) void conv_step_long_kernel(ConvStep<T> p)
+{
+    const int lane = threadIdx.x & 63, c = (int)((blockIdx.x * 256u + threadIdx.x) >> 6);
     if (c >= p.C) return;
     const T *w = p.w + (long long)c * p.K;
     for (int b = blockIdx.y; b < p.B; b += gridDim.y) {
@@ -34,15 +149,14 @@ template <typename T> __global__ __launch_bounds__(256) void conv_step_kernel(Co
             T *ring = p.ring + ((long long)s * p.C + c) * p.K;
             const int at = ring_place(p.pos[b], p.K);
             const T x = *p.x.row(b, c, 1);
-            for (int k = lane; k < p.K; k += 1 << lg) {
+            for (int k = lane; k < p.K; k += 64) {
                 int j = k - at - 1;
                 if (j < 0) j += p.K;
-                const float v = ld_elem(k == at ? &x : ring + k);
-                sum = fmaf(v, ld_elem(w + j), sum);
+                sum = fmaf(ld_elem(k == at ? &x : ring + k), ld_elem(w + j), sum);
                 if (k == at) ring[k] = x;
             }
         }
-        for (int d = 1; d < (1 << lg); d *= 2) sum += __shfl_xor(sum, d, 64);
+        sum = group_sum<64>(sum);
         if (lane == 0) st_elem(p.y.row(b, c, 1), sum);
     }
 }
@@ -74,6 +188,35 @@ template <typename T> __global__ __launch_bounds__(256) void conv_ring_kernel(Co
 
 }  // namespace dwconv
 
+namespace {
+
+template <typename T, int V, int U> void launch_rows(const ConvStep<T> &p, int lg, size_t lds, hipStream_t st)
+{
+    // (many sequences: enough workgroups to fill the chip, each with several rounds of sequences for its taps)
+    const long long across = ceil_div(p.C, 256 >> lg), rounds = ceil_div(p.B, U);
+    const unsigned down = (unsigned)std::max(1ll, std::min<long long>({rounds, ceil_div(4096, across), 65535}));
+    conv_step_kernel<T, V, U><<<dim3((unsigned)across, down), 256, lds, st>>>(p, lg, 0xffffffffu / (unsigned)p.K);
+}
+template <typename T, int V> void launch_step(const ConvStep<T> &p, hipStream_t st)
+{
+    int lg = 0;
+    while (lg < 6 && (V << lg) < p.K) ++lg;
+    const size_t lds = (size_t)(256 >> lg) * ((size_t)p.K + V - 1) * sizeof(float);
+    if (lds > 32 << 10) {
+        conv_step_long_kernel<<<dim3((unsigned)ceil_div((long long)p.C * 64, 256), (unsigned)std::min(p.B, 65535)), 256, 0, st>>>(p);
+        return;
+    }
+    // Sequences in flight: one where waves are few and their own work is the wait (B256 C768 K4 bf16 3.6 us, 3.9 with two, 4.8 with
+    // four; B1 C256 K64 fp32 2.6, 2.8, 3.5), two in between (B256 C768 K32 bf16 9.8, 8.7, 9.8), four for large pools (B1024 C512
+    // K64 fp32 52, 47, 44).
+    const double n = (double)p.B * p.C * p.K;
+    if (n < 2 << 20) launch_rows<T, V, 1>(p, lg, lds, st);
+    else if (n < 16 << 20) launch_rows<T, V, 2>(p, lg, lds, st);
+    else launch_rows<T, V, 4>(p, lg, lds, st);
+}
+
+}  // namespace
+
 extern "C" {
 
 int dwconv_conv_step(dwconv_seq x, const void *w, void *ring, const int *pos, const int *slots, int pool, dwconv_seq_out y, int B, int C, int K,
@@ -88,13 +231,13 @@ int dwconv_conv_step(dwconv_seq x, const void *w, void *ring, const int *pos, co
     if ((rc = check_in(x, es)) != DWCONV_OK || (rc = check_out(y, es, B, C, 1)) != DWCONV_OK) return rc;
     if (!aligned_to(w, es) || !aligned_to(ring, es) || !f32_ok(pos) || !f32_ok(slots)) return DWCONV_ERR_ALIGN;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    int lg = 0;
-    while (lg < 6 && (1 << lg) < K) ++lg;
-    const dim3 grid((unsigned)ceil_div((long long)C << lg, 256), (unsigned)std::min(B, 65535));
     if (dtype == DWCONV_F32)
-        conv_step_kernel<<<grid, 256, 0, st>>>(ConvStep<float>{seq<float>(x), (const float *)w, (float *)ring, pos, slots, seq<float>(y), B, C, K, pool}, lg);
-    else
-        conv_step_kernel<<<grid, 256, 0, st>>>(ConvStep<bf16_t>{seq<bf16_t>(x), (const bf16_t *)w, (bf16_t *)ring, pos, slots, seq<bf16_t>(y), B, C, K, pool}, lg);
+        launch_step<float, 4>(ConvStep<float>{seq<float>(x), (const float *)w, (float *)ring, pos, slots, seq<float>(y), B, C, K, pool}, st);
+    else {
+        const ConvStep<bf16_t> p{seq<bf16_t>(x), (const bf16_t *)w, (bf16_t *)ring, pos, slots, seq<bf16_t>(y), B, C, K, pool};
+        if (K < 8) launch_step<bf16_t, 4>(p, st);       // (a lane's eight would be mostly past the ring)
+        else launch_step<bf16_t, 8>(p, st);
+    }
     return launch_status();
 }
 

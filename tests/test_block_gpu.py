@@ -433,6 +433,30 @@ def test_conv_step_is_the_convolution(K, dtype):
     assert torch.equal(ring[[1, 3, 4, 6]], other[[1, 3, 4, 6]])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,C,K", [(700, 300, 11), (3, 5000, 200), (2000, 260, 33), (5, 3, 2500), (70000, 2, 3), (1, 1, 1), (2, 33, 2045)])
+def test_conv_step_of_any_batch(B, C, K, dtype):
+    """One and several sequences of a workgroup in flight, rings longer than a workgroup's lanes and than LDS, places left empty."""
+    x, w, ring = rand(B, C, seed=1, dtype=dtype), (rand(C, K, seed=2) / math.sqrt(K)).to(dtype), rand(B + 1, C, K, seed=3, dtype=dtype)
+    pos = torch.randint(0, 2 ** 31 - 1, (B,), generator=torch.Generator().manual_seed(4)).int().cuda()
+    slots = torch.randperm(B, generator=torch.Generator().manual_seed(5)).int().cuda() + 1
+    slots[::7] = -1
+    before = ring.clone()
+    y = block.conv_step(x, w, ring, pos, slots)
+    used = (slots >= 0).nonzero()[:, 0]
+    at, p = slots[used].long(), (pos[used] % K).long()
+    full = before[at].double()
+    full.scatter_(2, p[:, None, None].expand(-1, C, 1), x[used].double()[..., None])
+    order = (p[:, None] + 1 + torch.arange(K, device="cuda")) % K
+    terms = torch.gather(full, 2, order[:, None, :].expand(-1, C, -1)) * w.double()
+    # (a sum of K rounded products in any order)
+    ref.check(y[used], terms.sum(-1).cpu(), terms.abs().sum(-1).cpu() * (K + 2) * ref.U / 2, dtype, "y")
+    assert (y[slots < 0] == 0).all()
+    want = before.clone()
+    want[at] = full.to(dtype)
+    assert torch.equal(ring, want)
+
+
 def test_conv_step_at_any_position():
     """Positions up to the largest int32, and no slots: the place in the ring is the position's remainder."""
     B, C, K = 3, 20, 7
