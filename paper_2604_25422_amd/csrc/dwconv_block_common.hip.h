@@ -92,6 +92,102 @@ __device__ __forceinline__ void store8(bf16_t *p, const float (&v)[8], int left)
     }
 }
 
+// 16 bytes of a row or of a dense tensor.
+template <typename T> struct Pack;
+template <> struct Pack<float> {
+    static constexpr int V = 4;
+    floatx4_any w;
+    __device__ __forceinline__ float operator[](int k) const { return w[k]; }
+};
+template <> struct Pack<bf16_t> {
+    static constexpr int V = 8;
+    uintx4_any w;
+    __device__ __forceinline__ float operator[](int k) const
+    {
+        const unsigned u = w[k >> 1];
+        return __uint_as_float((k & 1) ? (u & 0xffff0000u) : (u << 16));
+    }
+};
+__device__ __forceinline__ void load_pack(Pack<float> &e, const float *p) { e.w = *reinterpret_cast<const floatx4_any *>(p); }
+__device__ __forceinline__ void load_pack(Pack<bf16_t> &e, const bf16_t *p) { e.w = *reinterpret_cast<const uintx4_any *>(p); }
+__device__ __forceinline__ void store_pack(float *p, const float (&v)[4]) {
+    *reinterpret_cast<floatx4_any *>(p) = floatx4_any{v[0], v[1], v[2], v[3]};
+}
+__device__ __forceinline__ void store_pack(bf16_t *p, const float (&v)[8])
+{
+    *reinterpret_cast<uintx4_any *>(p) = uintx4_any{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+}
+// ... past the caches: what nobody reads soon does not push out what somebody will.
+__device__ __forceinline__ void store_pack_streaming(float *p, const float (&v)[4])
+{
+    __builtin_nontemporal_store(floatx4_any{v[0], v[1], v[2], v[3]}, reinterpret_cast<floatx4_any *>(p));
+}
+__device__ __forceinline__ void store_pack_streaming(bf16_t *p, const float (&v)[8])
+{
+    __builtin_nontemporal_store(uintx4_any{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])},
+                                reinterpret_cast<uintx4_any *>(p));
+}
+
+// The eight elements at position t of a row of L >= 8, as far as the row goes (zeros behind it): where it ends among them, the row's
+// last eight, moved down.
+__device__ __forceinline__ Eight<float> load_row8(const float *row, int t, int L)
+{
+    Eight<float> e{};
+    if (t + 8 <= L) return load8(row + t, 8);
+    if (t < L) {
+        e = load8(row + (L - 8), 8);
+        const int by = t - (L - 8);
+        if (by & 4) e.lo = e.hi, e.hi = floatx4_any{};
+        if (by & 2) e.lo = floatx4_any{e.lo[2], e.lo[3], e.hi[0], e.hi[1]}, e.hi = floatx4_any{e.hi[2], e.hi[3], 0.0f, 0.0f};
+        if (by & 1) e.lo = floatx4_any{e.lo[1], e.lo[2], e.lo[3], e.hi[0]}, e.hi = floatx4_any{e.hi[1], e.hi[2], e.hi[3], 0.0f};
+    }
+    return e;
+}
+__device__ __forceinline__ Eight<bf16_t> load_row8(const bf16_t *row, int t, int L)
+{
+    Eight<bf16_t> e{};
+    if (t + 8 <= L) return load8(row + t, 8);
+    if (t < L) {
+        e = load8(row + (L - 8), 8);
+        const int by = t - (L - 8);
+        if (by & 4) e.w = uintx4_any{e.w[2], e.w[3], 0u, 0u};
+        if (by & 2) e.w = uintx4_any{e.w[1], e.w[2], e.w[3], 0u};
+        if (by & 1)
+            e.w = uintx4_any{__funnelshift_r(e.w[0], e.w[1], 16), __funnelshift_r(e.w[1], e.w[2], 16), __funnelshift_r(e.w[2], e.w[3], 16),
+                             e.w[3] >> 16};
+    }
+    return e;
+}
+// Eight outputs at position t, as far as the row goes: the rest of a row as four, two and one.
+__device__ __forceinline__ void store_row8(float *row, const float (&v)[8], int t, int L)
+{
+    if (t + 8 <= L) {
+        store8(row + t, v, 8);
+    } else if (t < L) {
+        float *p = row + t;
+        floatx4_any f = {v[0], v[1], v[2], v[3]};
+        const int n = L - t;
+        if (n & 4) *reinterpret_cast<floatx4_any *>(p) = f, p += 4, f = floatx4_any{v[4], v[5], v[6], v[7]};
+        if (n & 2) p[0] = f[0], p[1] = f[1], p += 2, f[0] = f[2];
+        if (n & 1) p[0] = f[0];
+    }
+}
+__device__ __forceinline__ void store_row8(bf16_t *row, const float (&v)[8], int t, int L)
+{
+    if (t + 8 <= L) {
+        store8(row + t, v, 8);
+    } else if (t < L) {
+        typedef unsigned uintx2_any __attribute__((ext_vector_type(2), aligned(2)));
+        typedef unsigned uint_any __attribute__((aligned(2)));
+        bf16_t *p = row + t;
+        uintx2_any u = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        const int n = L - t;
+        if (n & 4) *reinterpret_cast<uintx2_any *>(p) = u, p += 4, u = uintx2_any{pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+        if (n & 2) *reinterpret_cast<uint_any *>(p) = u[0], p += 2, u[0] = u[1];
+        if (n & 1) p->bits = (uint16_t)u[0];
+    }
+}
+
 // ---- functions of a gate ----
 // The hardware's exp2, reciprocal and square root are within about one unit of the last place.
 
@@ -103,11 +199,12 @@ __device__ __forceinline__ float rcp_hw(float v) { return __builtin_amdgcn_rcpf(
 // 1 / (1 + exp(-v)).  (exp overflows to infinity below -88, whose reciprocal is the 0 that is meant.)
 __device__ __forceinline__ float sigmoid(float v) { return rcp_hw(1.0f + exp2_hw(v * -kLog2e)); }
 
-// sigmoid(v), and 1 - sigmoid(v) without the cancellation: e / (1 + e) with e = exp(-v), which is 1 where e overflows.
+// sigmoid(v), and 1 - sigmoid(v) = e / (1 + e) with e = exp(-v), without the cancellation.  Where e overflows sigmoid(v) is 0 and the
+// other no number that a product with it depends on, but finite; a NaN stays one in both.
 __device__ __forceinline__ float sigmoid_both(float v, float &rest)
 {
     const float e = exp2_hw(v * -kLog2e), s = rcp_hw(1.0f + e);
-    rest = e > 1e30f ? 1.0f : e * s;            // (a NaN stays one)
+    rest = fminf(e, 3e38f) * s;
     return s;
 }
 
@@ -139,8 +236,15 @@ template <bool NEAR> __device__ __forceinline__ float decay(float q, float &E)
     return a;
 }
 
-// log(1 + exp(v)), once per row.
-__device__ __forceinline__ float softplus(float v) { return v > 20.0f ? v : log1pf(expf(v)); }
+// log(1 + e) with e = exp(v), once per row.  e through an exponent in two parts; log(1 + e) as log(u) e / (u - 1) with the rounded
+// u = 1 + e, which is e where u is 1: what u has lost of e is lost in u - 1 as well.
+__device__ __forceinline__ float softplus(float v)
+{
+    const float t = v * kLog2e, lo = fmaf(v, kLog2e, -t) + v * 1.925963033e-8f;         // log2(e) = kLog2e + 1.9e-8
+    const float h = exp2_hw(t), e = fmaf(h, lo * 0.6931471806f, h), u = 1.0f + e;
+    const float l = __builtin_amdgcn_logf(u) * 0.6931471806f * (e / (u - 1.0f));
+    return v > 20.0f ? v : u == 1.0f ? e : l;
+}
 
 // ---- lanes ----
 
@@ -159,43 +263,53 @@ struct Span {
 };
 __device__ __forceinline__ Span join(Span before, Span s) { return Span{s.A * before.A, fmaf(s.A, before.H, s.H)}; }
 
+// One step of a scan over all 64 lanes: s joined with what the lane that `FROM` names holds, where there is one; the other lanes keep
+// theirs.  The move comes with the operation; the wait states are those between an instruction and a move of its result.
+#define DWCONV_SPAN_STEP(FROM)                                                                     \
+    asm("s_nop 1\n\tv_fmac_f32_dpp %0, %0, %1 " FROM "\n\tv_mul_f32_dpp %1, %1, %1 " FROM : "+v"(s.H), "+v"(s.A))
+#define DWCONV_ALL " row_mask:0xf bank_mask:0xf"
+
 // The spans of the G lanes of a group (G = 64: the wave) joined with all those in front of them in the group.
 template <int G> __device__ __forceinline__ Span scan_up(Span s, int lane)
 {
-    const int in_group = lane & (G - 1);
-#define DWCONV_STEP(D)                                                                        \
-    if constexpr (G > D) {                                                                    \
-        Span o{dpp<0x110 + D>(1.0f, s.A), dpp<0x110 + D>(0.0f, s.H)};                         \
-        if (G < 16 && in_group < D) o = Span{1.0f, 0.0f};                                     \
-        s = join(o, s);                                                                       \
+    if constexpr (G >= 16) {
+        DWCONV_SPAN_STEP("row_shr:1" DWCONV_ALL);
+        DWCONV_SPAN_STEP("row_shr:2" DWCONV_ALL);
+        DWCONV_SPAN_STEP("row_shr:4" DWCONV_ALL);
+        DWCONV_SPAN_STEP("row_shr:8" DWCONV_ALL);
+        // (the last lane of sixteen into the next sixteen; of thirty-two into the upper half)
+        if constexpr (G > 16) DWCONV_SPAN_STEP("row_bcast:15 row_mask:0xa bank_mask:0xf");
+        if constexpr (G > 32) DWCONV_SPAN_STEP("row_bcast:31 row_mask:0xc bank_mask:0xf");
+        asm("s_nop 1" : "+v"(s.H), "+v"(s.A));      // (whatever takes them may be a move)
+    } else {
+        const int in_group = lane & (G - 1);
+        const auto step = [&](Span o, int d) { s = in_group < d ? s : join(o, s); };
+        if constexpr (G > 1) step(Span{dpp<0x111>(1.0f, s.A), dpp<0x111>(0.0f, s.H)}, 1);
+        if constexpr (G > 2) step(Span{dpp<0x112>(1.0f, s.A), dpp<0x112>(0.0f, s.H)}, 2);
+        if constexpr (G > 4) step(Span{dpp<0x114>(1.0f, s.A), dpp<0x114>(0.0f, s.H)}, 4);
     }
-    DWCONV_STEP(1)
-    DWCONV_STEP(2)
-    DWCONV_STEP(4)
-    DWCONV_STEP(8)
-#undef DWCONV_STEP
-    // (the last lane of sixteen into the next sixteen; of thirty-two into the upper half)
-    if constexpr (G > 16) s = join(Span{dpp<0x142, 0xa>(1.0f, s.A), dpp<0x142, 0xa>(0.0f, s.H)}, s);
-    if constexpr (G > 32) s = join(Span{dpp<0x143, 0xc>(1.0f, s.A), dpp<0x143, 0xc>(0.0f, s.H)}, s);
     return s;
 }
 // The same from the other end: joined with all those behind them in the sixteen lanes of a row (or in the group).
 template <int G> __device__ __forceinline__ Span scan_down16(Span s, int lane)
 {
-    const int in_group = lane & (G - 1);
-#define DWCONV_STEP(D)                                                                        \
-    if constexpr (G > D) {                                                                    \
-        Span o{dpp<0x100 + D>(1.0f, s.A), dpp<0x100 + D>(0.0f, s.H)};                         \
-        if (G < 16 && in_group >= G - D) o = Span{1.0f, 0.0f};                                \
-        s = join(o, s);                                                                       \
+    if constexpr (G >= 16) {
+        DWCONV_SPAN_STEP("row_shl:1" DWCONV_ALL);
+        DWCONV_SPAN_STEP("row_shl:2" DWCONV_ALL);
+        DWCONV_SPAN_STEP("row_shl:4" DWCONV_ALL);
+        DWCONV_SPAN_STEP("row_shl:8" DWCONV_ALL);
+        asm("s_nop 1" : "+v"(s.H), "+v"(s.A));
+    } else {
+        const int in_group = lane & (G - 1);
+        const auto step = [&](Span o, int d) { s = in_group >= G - d ? s : join(o, s); };
+        if constexpr (G > 1) step(Span{dpp<0x101>(1.0f, s.A), dpp<0x101>(0.0f, s.H)}, 1);
+        if constexpr (G > 2) step(Span{dpp<0x102>(1.0f, s.A), dpp<0x102>(0.0f, s.H)}, 2);
+        if constexpr (G > 4) step(Span{dpp<0x104>(1.0f, s.A), dpp<0x104>(0.0f, s.H)}, 4);
     }
-    DWCONV_STEP(1)
-    DWCONV_STEP(2)
-    DWCONV_STEP(4)
-    DWCONV_STEP(8)
-#undef DWCONV_STEP
     return s;
 }
+#undef DWCONV_ALL
+#undef DWCONV_SPAN_STEP
 __device__ __forceinline__ float from_lane_before(float first, float v) { return dpp<0x138>(first, v); }   // lane 0: first
 __device__ __forceinline__ float from_lane_behind(float last, float v) { return dpp<0x130>(last, v); }     // lane 63: last
 

@@ -35,32 +35,6 @@ template <typename T> struct NormBwd {
     int row_tiles, run; // run: tiles of a workgroup of the tile kernel, one behind the other
 };
 
-// 16 bytes of a row.
-template <typename T> struct Pack;
-template <> struct Pack<float> {
-    static constexpr int V = 4;
-    floatx4_any w;
-    __device__ __forceinline__ float operator[](int k) const { return w[k]; }
-};
-template <> struct Pack<bf16_t> {
-    static constexpr int V = 8;
-    uintx4_any w;
-    __device__ __forceinline__ float operator[](int k) const
-    {
-        const unsigned u = w[k >> 1];
-        return __uint_as_float((k & 1) ? (u & 0xffff0000u) : (u << 16));
-    }
-};
-__device__ __forceinline__ void load_pack(Pack<float> &e, const float *p) { e.w = *reinterpret_cast<const floatx4_any *>(p); }
-__device__ __forceinline__ void load_pack(Pack<bf16_t> &e, const bf16_t *p) { e.w = *reinterpret_cast<const uintx4_any *>(p); }
-__device__ __forceinline__ void store_pack(float *p, const float (&v)[4]) {
-    *reinterpret_cast<floatx4_any *>(p) = floatx4_any{v[0], v[1], v[2], v[3]};
-}
-__device__ __forceinline__ void store_pack(bf16_t *p, const float (&v)[8])
-{
-    *reinterpret_cast<uintx4_any *>(p) = uintx4_any{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-}
-
 // Workgroups go to the eight dies in turn; give every die a run of neighbouring tiles, whose rows share cache lines.
 __device__ __forceinline__ long long die_run(long long i, long long n)
 {

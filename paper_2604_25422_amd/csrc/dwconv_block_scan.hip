@@ -15,7 +15,8 @@ struct ScanPlan {
     long long M;                // rows of the sums towards dlam
 };
 
-ScanPlan plan_scan(int B, int C, int L)
+// (the sizes of workspaces go by segs and M, which do not depend on the type)
+ScanPlan plan_scan(int B, int C, int L, int dtype, bool backward)
 {
     ScanPlan s{};
     const long long rows = (long long)B * C;
@@ -34,13 +35,29 @@ ScanPlan plan_scan(int B, int C, int L)
         return s;
     }
     const long long chunks = ceil_div(L, kScanChunk);
-    s.W = 1;
-    while (s.W < 16 && rows * s.W < 4096 && s.W < chunks) s.W *= 2;
-    const long long groups = ceil_div(chunks, s.W);
-    s.segs = 1;
-    if (rows * s.W < 2048) s.segs = (int)std::max(1ll, std::min<long long>({groups, ceil_div(4096, rows * s.W), kScanSegments}));
-    s.seg_groups = (int)ceil_div(groups, s.segs);
-    s.segs = (int)ceil_div(groups, s.seg_groups);
+    // Few long rows are cut into segments for the whole chip to work at them, though a first pass then forms the gates of all but one a
+    // second time: B1 C32 L40000 fp32 12.4 us forward (17.2 whole), 18.3 backward (32.7); B2 C64 L65537 bf16 45 us backward (58),
+    // but 30 us forward (26.5 whole, half of the chip idle).
+    if (rows < (backward ? 129 : 128) && chunks > (backward ? 32 : 64)) {
+        const long long most = std::min<long long>(kScanSegments, chunks);
+        s.W = 1;
+        while (s.W < 8 && rows * most * s.W < 4096 && most * s.W < chunks) s.W *= 2;
+        const long long groups = ceil_div(chunks, s.W);
+        s.seg_groups = (int)ceil_div(groups, most);
+        s.segs = (int)ceil_div(groups, s.seg_groups);
+    } else {
+        // Waves of a row: as many as fill the chip (backward, whose registers let fewer be resident, half of that); in fp32 more of
+        // them even where rows abound, whose longer runs memory likes better (B32 C256 L4096 forward 97 us with four, 105 with
+        // one, backward 183 and 195; bf16, bound by the gates: 55 and 57, 101 and 136), but not with one group for a row
+        // backward (B64 C768 L1024 fp32 260 us with one, 275 with two).
+        const long long want = backward ? 2048 : 4096;
+        const int most = backward ? 8 : 16, rich = dtype == DWCONV_F32 ? 4 : 1;
+        s.W = 1;
+        while (s.W < most && s.W < chunks && rows * s.W < want) s.W *= 2;
+        while (s.W < rich && s.W * (backward ? 2 : 1) < chunks) s.W *= 2;
+        s.segs = 1;
+        s.seg_groups = (int)ceil_div(chunks, s.W);
+    }
     s.M = (long long)B * s.segs;
     return s;
 }
@@ -53,7 +70,8 @@ constexpr long long kMaxBlocks = 1 << 20;
 template <typename T, int W> void launch_fwd(const ScanFwd<T> &p, const ScanPlan &s, hipStream_t st)
 {
     const long long rows = (long long)p.B * p.C;
-    if (s.segs > 1) scan_fwd_kernel<T, W, true><<<(unsigned)std::min(rows * (s.segs - 1), kMaxBlocks), 64 * W, 0, st>>>(p);
+    if constexpr (W <= 8)               // (plan_scan: more waves only for whole rows)
+        if (s.segs > 1) scan_fwd_kernel<T, W, true><<<(unsigned)std::min(rows * (s.segs - 1), kMaxBlocks), 64 * W, 0, st>>>(p);
     scan_fwd_kernel<T, W, false><<<(unsigned)std::min(rows * s.segs, kMaxBlocks), 64 * W, 0, st>>>(p);
 }
 template <typename T> void launch_fwd(const ScanFwd<T> &p, const ScanPlan &s, hipStream_t st)
@@ -95,8 +113,7 @@ template <typename T> void launch_bwd(const ScanBwd<T> &p, const ScanPlan &s, fl
     case 64: launch_bwd<T, 1>(p, s, st); break;
     case 128: launch_bwd<T, 2>(p, s, st); break;
     case 256: launch_bwd<T, 4>(p, s, st); break;
-    case 512: launch_bwd<T, 8>(p, s, st); break;
-    default: launch_bwd<T, 16>(p, s, st); break;
+    default: launch_bwd<T, 8>(p, s, st); break;
     }
     scan_dlam_kernel<<<(unsigned)ceil_div(p.C, 32), 1024, 0, st>>>(p.part, (int)s.M, p.C, p.lam, dlam);
 }
@@ -112,7 +129,7 @@ int dwconv_scan_states(int L) { return L < 1 || L > (1 << 30) ? 0 : (int)ceil_di
 size_t dwconv_scan_workspace_bytes(int B, int C, int L, int backward)
 {
     if (check_dims(B, C, L) != DWCONV_OK) return 0;
-    const ScanPlan s = plan_scan(B, C, L);
+    const ScanPlan s = plan_scan(B, C, L, DWCONV_F32, backward != 0);
     return span_bytes(s, B, C) + (backward ? part_bytes(s, C) : 0);
 }
 
@@ -131,7 +148,7 @@ int dwconv_scan_fwd(dwconv_seq x, dwconv_seq r, dwconv_seq i, const float *lam, 
     if ((rc = check_out(y, es, B, C, L)) != DWCONV_OK) return rc;
     for (const void *t : {(const void *)lam, (const void *)h0, (const void *)lengths, (const void *)h_last, (const void *)states})
         if (!f32_ok(t)) return DWCONV_ERR_ALIGN;
-    const ScanPlan s = plan_scan(B, C, L);
+    const ScanPlan s = plan_scan(B, C, L, dtype, false);
     const size_t need = span_bytes(s, B, C);
     if (need && (!workspace || workspace_bytes < need || !aligned_to(workspace, 16))) return DWCONV_ERR_WORKSPACE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
@@ -162,7 +179,7 @@ int dwconv_scan_bwd(dwconv_seq dy, dwconv_seq x, dwconv_seq r, dwconv_seq i, con
         if ((rc = check_out(*t, es, B, C, L)) != DWCONV_OK) return rc;
     for (const void *t : {(const void *)lam, (const void *)states, (const void *)dh_last, (const void *)lengths, (const void *)dlam, (const void *)dh0})
         if (!f32_ok(t)) return DWCONV_ERR_ALIGN;
-    const ScanPlan s = plan_scan(B, C, L);
+    const ScanPlan s = plan_scan(B, C, L, dtype, true);
     const size_t need = span_bytes(s, B, C) + part_bytes(s, C);
     if (!workspace || workspace_bytes < need || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
     const hipStream_t st = static_cast<hipStream_t>(stream);

@@ -86,6 +86,18 @@ __device__ __forceinline__ Span span_of(const float (&a)[8], const float (&u)[8]
     return s;
 }
 
+// Rows that one lane holds may be shorter than its eight positions.
+template <bool SHORT, typename T> __device__ __forceinline__ Eight<T> load_eight(const T *row, int t, int L)
+{
+    if constexpr (SHORT) return load8(row + t, L - t);
+    else return load_row8(row, t, L);
+}
+template <bool SHORT, typename T> __device__ __forceinline__ void store_eight(T *row, const float (&v)[8], int t, int L)
+{
+    if constexpr (SHORT) store8(row + t, v, L - t);
+    else store_row8(row, v, t, L);
+}
+
 // What the backward pass keeps of eight positions.
 struct GateGrads {
     float a[8];         // decay
@@ -104,12 +116,13 @@ __device__ __forceinline__ void grads_begin(const Eight<T> &x, const Eight<T> &r
         float rest_i, E;
         const float q = rho * sigmoid_both(r[k], w.rest[k]), si = sigmoid_both(i[k], rest_i);
         w.a[k] = decay<NEAR>(q, E);
-        // beta^2, and 1 / beta of it held to the smallest normal number, so that a beta of 0 stays 0 (a comparison keeps a NaN)
-        const float s = -E * (2.0f + E), rs = __builtin_amdgcn_rsqf(s < 1.17549435e-38f ? 1.17549435e-38f : s);
-        w.in[k] = s * rs * si;
+        // beta^2 = s, and 1 / beta of s held to the smallest normal number, so that a beta of 0 stays 0 (a NaN stays in s itself);
+        // a u / (1 - a^2) = a x sigmoid(i) / beta
+        const float s = -E * (2.0f + E), over = __builtin_amdgcn_rsqf(fmaxf(s, 1.17549435e-38f)) * si;
+        w.in[k] = s * over;
         u[k] = w.in[k] * x[k];
         w.gi[k] = u[k] * rest_i;
-        pull[k] = w.a[k] * (rs * rs * u[k]);
+        pull[k] = w.a[k] * (over * x[k]);
         w.e[k] = q * w.a[k];
     }
     if (left < 8) {
@@ -143,8 +156,8 @@ __device__ __forceinline__ Span back_span(const float (&a)[8], const float (&dy)
     return s;
 }
 // Gradients of eight positions from v behind them, 0 from `left` on; returns their sum of dq q.
-template <typename T>
-__device__ __forceinline__ float grads_store(const GateGrads &w, const float (&dy)[8], float v, T *dx, T *dr, T *di, int left, int room)
+template <bool SHORT = false, typename T>
+__device__ __forceinline__ float grads_store(const GateGrads &w, const float (&dy)[8], float v, T *dx, T *dr, T *di, int left, int t, int L)
 {
     float g[8], out[8], sum = 0.0f;
 #pragma unroll
@@ -159,17 +172,17 @@ __device__ __forceinline__ float grads_store(const GateGrads &w, const float (&d
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) out[k] = g[k] * w.in[k];
-    store8(dx, out, room);
+    store_eight<SHORT>(dx, out, t, L);
 #pragma unroll
     for (int k = 0; k < 8; ++k) out[k] = g[k] * w.gi[k];
-    store8(di, out, room);
+    store_eight<SHORT>(di, out, t, L);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const float d = g[k] * w.e[k];
         sum += d;
         out[k] = d * w.rest[k];
     }
-    store8(dr, out, room);
+    store_eight<SHORT>(dr, out, t, L);
     return sum;
 }
 
@@ -187,10 +200,11 @@ template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) vo
     __shared__ Span totals[2][W];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int segs = SPANS ? p.segs - 1 : p.segs;
-    const long long units = (long long)p.B * p.C * segs;
+    const unsigned units = (unsigned)(p.B * p.C) * (unsigned)segs;         // (below 2^32: cut are only calls of few rows)
     int side = 0;
-    for (long long unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const int row = (int)(unit / segs), seg = (int)(unit - (long long)row * segs), b = row / p.C, c = row - b * p.C;
+    for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
+        const int row = (int)(segs == 1 ? unit : unit / (unsigned)segs), seg = (int)(unit - (unsigned)row * (unsigned)segs);
+        const int b = (int)((unsigned)row / (unsigned)p.C), c = row - b * p.C;
         const int n = row_length(p.lengths, b, p.L);
         const float rho = decay_rate(p.rate, p.lam[c]);
         const T *x = p.x.row(b, c, p.L), *r = p.r.row(b, c, p.L), *i = p.i.row(b, c, p.L);
@@ -202,19 +216,19 @@ template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) vo
         if (!SPANS && seg > 0) carry = through_segments(p.spans + (long long)row * p.segs, seg, 1, carry, lane);
         Span all{1.0f, 0.0f};
         int t = t0 + wave * kScanChunk + lane * 8;
-        Eight<T> xn = load8(x + t, n - t), rn = load8(r + t, n - t), in = load8(i + t, n - t);
+        Eight<T> xn = load_row8(x, t, p.L), rn = load_row8(r, t, p.L), in = load_row8(i, t, p.L);
         for (int tg = t0; tg < t1; tg += group, t += group) {
             if (tg >= n) {                      // (the same for the whole workgroup)
                 if (SPANS) break;
                 if (lane == 0 && p.states && tg + wave * kScanChunk < p.L) p.states[(long long)row * p.nstates + t / kScanChunk] = carry;
                 const float zero[8] = {};
-                store8(y + t, zero, p.L - t);
+                store_row8(y, zero, t, p.L);
                 continue;
             }
             float a[8], u[8];
             gates(xn, rn, in, rho, n - t, a, u);
             const int tn = t + group;
-            if (tg + group < t1) xn = load8(x + tn, n - tn), rn = load8(r + tn, n - tn), in = load8(i + tn, n - tn);
+            if (tg + group < t1) xn = load_row8(x, tn, p.L), rn = load_row8(r, tn, p.L), in = load_row8(i, tn, p.L);
             const Span s = scan_up<64>(span_of(a, u), lane);
             const Span total{lane_value(s.A, 63), lane_value(s.H, 63)};
             if constexpr (SPANS && W == 1) {
@@ -248,7 +262,7 @@ template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) vo
                 for (int k = 0; k < 8; ++k)
                     if (k >= n - t) out[k] = 0.0f;
             }
-            store8(y + t, out, p.L - t);
+            store_row8(y, out, t, p.L);
         }
         if (threadIdx.x == 0) {
             if (SPANS) p.spans[(long long)row * p.segs + seg] = all;
@@ -264,10 +278,11 @@ template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) vo
     __shared__ float sums[W];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int segs = SPANS ? p.segs - 1 : p.segs;
-    const long long units = (long long)p.B * p.C * segs;
+    const unsigned units = (unsigned)(p.B * p.C) * (unsigned)segs;
     int side = 0;
-    for (long long unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const int row = (int)(unit / segs), seg = (int)(unit - (long long)row * segs) + (SPANS ? 1 : 0), b = row / p.C, c = row - b * p.C;
+    for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
+        const int row = (int)(segs == 1 ? unit : unit / (unsigned)segs), seg = (int)(unit - (unsigned)row * (unsigned)segs) + (SPANS ? 1 : 0);
+        const int b = (int)((unsigned)row / (unsigned)p.C), c = row - b * p.C;
         const int n = row_length(p.lengths, b, p.L);
         const float rho = decay_rate(p.rate, p.lam[c]);
         const T *dy = p.dy.row(b, c, p.L), *x = p.x.row(b, c, p.L), *r = p.r.row(b, c, p.L), *i = p.i.row(b, c, p.L);
@@ -281,8 +296,8 @@ template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) vo
         Span all{1.0f, 0.0f};
         float sum = 0.0f;
         int tg = t0 + (groups - 1) * group, t = tg + wave * kScanChunk + lane * 8;
-        Eight<T> dn = load8(dy + t, n - t), xn, rn = load8(r + t, n - t), in;
-        if (!SPANS) xn = load8(x + t, n - t), in = load8(i + t, n - t);
+        Eight<T> dn = load_row8(dy, t, p.L), xn, rn = load_row8(r, t, p.L), in;
+        if (!SPANS) xn = load_row8(x, t, p.L), in = load_row8(i, t, p.L);
         float hn = !SPANS && t < n ? p.states[(long long)row * p.nstates + t / kScanChunk] : 0.0f;
         for (; tg >= t0; tg -= group, t -= group) {
             const int tn = t - group;
@@ -290,14 +305,14 @@ template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) vo
             if (tg >= n) {
                 if (!SPANS) {
                     const float zero[8] = {};
-                    store8(dx + t, zero, p.L - t);
-                    store8(dr + t, zero, p.L - t);
-                    store8(di + t, zero, p.L - t);
+                    store_row8(dx, zero, t, p.L);
+                    store_row8(dr, zero, t, p.L);
+                    store_row8(di, zero, t, p.L);
                 }
                 if (more) {
-                    dn = load8(dy + tn, n - tn), rn = load8(r + tn, n - tn);
+                    dn = load_row8(dy, tn, p.L), rn = load_row8(r, tn, p.L);
                     if (!SPANS) {
-                        xn = load8(x + tn, n - tn), in = load8(i + tn, n - tn);
+                        xn = load_row8(x, tn, p.L), in = load_row8(i, tn, p.L);
                         hn = tn < n ? p.states[(long long)row * p.nstates + tn / kScanChunk] : 0.0f;
                     }
                 }
@@ -307,6 +322,11 @@ template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) vo
             float d[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) d[k] = dn[k];
+            if (n - t < 8) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k >= n - t) d[k] = 0.0f;
+            }
             if constexpr (SPANS) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
@@ -314,13 +334,13 @@ template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) vo
                     w.a[k] = decay<false>(rho * sigmoid(rn[k]), E);
                     if (k >= n - t) w.a[k] = 1.0f;
                 }
-                if (more) dn = load8(dy + tn, n - tn), rn = load8(r + tn, n - tn);
+                if (more) dn = load_row8(dy, tn, p.L), rn = load_row8(r, tn, p.L);
             } else {
                 float u[8], pull[8];
                 grads_begin(xn, rn, in, rho, n - t, w, u, pull);
                 const float h = hn;
                 if (more) {
-                    dn = load8(dy + tn, n - tn), rn = load8(r + tn, n - tn), xn = load8(x + tn, n - tn), in = load8(i + tn, n - tn);
+                    dn = load_row8(dy, tn, p.L), rn = load_row8(r, tn, p.L), xn = load_row8(x, tn, p.L), in = load_row8(i, tn, p.L);
                     hn = tn < n ? p.states[(long long)row * p.nstates + tn / kScanChunk] : 0.0f;
                 }
                 const Span s = scan_up<64>(span_of(w.a, u), lane);
@@ -355,7 +375,7 @@ template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) vo
             if constexpr (W == 1) carry = fmaf(row16[0].A, v0, row16[0].H);
             const float mine = lane >= 32 ? (lane >= 48 ? v3 : v2) : (lane >= 16 ? v1 : v0);
             v = from_lane_behind(v, fmaf(s.A, mine, s.H));
-            sum += grads_store(w, d, v, dx + t, dr + t, di + t, n - t, p.L - t);
+            sum += grads_store(w, d, v, dx, dr, di, n - t, t, p.L);
         }
         if (SPANS) {
             if (threadIdx.x == 0) p.spans[(long long)row * p.segs + seg] = all;
@@ -391,8 +411,8 @@ template <typename T, int G> __global__ __launch_bounds__(256) void scan_fwd_sho
         const bool off = idle || b0 + sub >= p.B;
         const int bc = off ? 0 : (int)(b0 + sub), cc = off ? 0 : c, n = off ? 0 : row_length(p.lengths, bc, p.L), left = n - t;
         const long long row = (long long)bc * p.C + cc;
-        const Eight<T> x = load8(p.x.row(bc, cc, p.L) + t, left), r = load8(p.r.row(bc, cc, p.L) + t, left),
-                       i = load8(p.i.row(bc, cc, p.L) + t, left);
+        const Eight<T> x = load_eight<G == 1>(p.x.row(bc, cc, p.L), t, off ? 0 : p.L), r = load_eight<G == 1>(p.r.row(bc, cc, p.L), t, off ? 0 : p.L),
+                       i = load_eight<G == 1>(p.i.row(bc, cc, p.L), t, off ? 0 : p.L);
         const float h0 = p.h0 && !off ? p.h0[row] : 0.0f;
         float a[8], u[8], out[8];
         gates<false>(x, r, i, rho, left, a, u);
@@ -406,7 +426,7 @@ template <typename T, int G> __global__ __launch_bounds__(256) void scan_fwd_sho
             out[k] = k < left ? h : 0.0f;
         }
         if (off) continue;                      // (the moves between lanes are done)
-        store8(p.y.row(bc, cc, p.L) + t, out, p.L - t);
+        store_eight<G == 1>(p.y.row(bc, cc, p.L), out, t, p.L);
         if (t == 0 && p.states) p.states[row] = h0;
         if ((lane & (G - 1)) == G - 1 && p.h_last) p.h_last[row] = end;
     }
@@ -423,14 +443,14 @@ template <typename T, int G> __global__ __launch_bounds__(256) void scan_bwd_sho
         const bool off = idle || b0 + sub >= p.B;
         const int bc = off ? 0 : (int)(b0 + sub), cc = off ? 0 : c, n = off ? 0 : row_length(p.lengths, bc, p.L), left = n - t;
         const long long row = (long long)bc * p.C + cc;
-        const Eight<T> dyr = load8(p.dy.row(bc, cc, p.L) + t, left), x = load8(p.x.row(bc, cc, p.L) + t, left),
-                       r = load8(p.r.row(bc, cc, p.L) + t, left), i = load8(p.i.row(bc, cc, p.L) + t, left);
+        const Eight<T> dyr = load_eight<G == 1>(p.dy.row(bc, cc, p.L), t, off ? 0 : p.L), x = load_eight<G == 1>(p.x.row(bc, cc, p.L), t, off ? 0 : p.L),
+                       r = load_eight<G == 1>(p.r.row(bc, cc, p.L), t, off ? 0 : p.L), i = load_eight<G == 1>(p.i.row(bc, cc, p.L), t, off ? 0 : p.L);
         const float h0 = off ? 0.0f : p.states[row], dh = p.dh_last && !off ? p.dh_last[row] : 0.0f;
         GateGrads w;
         float u[8], pull[8], d[8];
         grads_begin<false>(x, r, i, rho, left, w, u, pull);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) d[k] = dyr[k];
+        for (int k = 0; k < 8; ++k) d[k] = k < left ? dyr[k] : 0.0f;
         const Span s = scan_up<G>(span_of(w.a, u), lane);
         float h = from_lane_before(h0, fmaf(s.A, h0, s.H));
         if ((lane & (G - 1)) == 0) h = h0;
@@ -445,7 +465,7 @@ template <typename T, int G> __global__ __launch_bounds__(256) void scan_bwd_sho
         float v = from_lane_behind(dh, front);
         if ((lane & (G - 1)) == G - 1) v = dh;
         if (off) continue;
-        sum += grads_store(w, d, v, p.dx.row(bc, cc, p.L) + t, p.dr.row(bc, cc, p.L) + t, p.di.row(bc, cc, p.L) + t, left, p.L - t);
+        sum += grads_store<G == 1>(w, d, v, p.dx.row(bc, cc, p.L), p.dr.row(bc, cc, p.L), p.di.row(bc, cc, p.L), left, t, p.L);
         if (t == 0 && p.dh0) p.dh0[row] = front;
     }
     sum = group_sum<G>(sum);

@@ -68,7 +68,9 @@ def test_scan_lengths(L, dtype):
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("B,C,L", [(1, 1, 9000), (1, 3, 40001), (2, 1, 70000), (300, 1, 17), (1, 300, 5), (7, 129, 260), (513, 9, 600), (1, 1, 1),
-                                   (70, 64, 1030), (33, 64, 2100)])
+                                   (70, 64, 1030), (33, 64, 2100),
+                                   # (one to sixteen waves a row, one group of them and several; segments of one and of several groups)
+                                   (9, 256, 700), (5, 260, 1100), (5, 130, 2100), (3, 100, 4200), (2, 70, 9000), (1, 129, 17000), (1, 64, 34000), (1, 127, 33500)])
 def test_scan_shapes(B, C, L, dtype):
     x, r, i, dy, lam = scan_inputs(B, C, L, dtype, 7)
     check_scan(x, r, i, dy, lam, rand(B, C, seed=1), rand(B, C, seed=2))
