@@ -70,6 +70,15 @@ template <typename T, int E, bool BLOCK> void fwd_tile(const NormFwd<T> &p, cons
 }
 template <typename T, bool BLOCK> void launch_fwd(const NormFwd<T> &p, const NormPlan &s, hipStream_t st)
 {
+    if (p.L == 1 && p.C <= 8 * 256) {
+        const int grid = std::min(p.B, 1 << 20), e = (int)ceil_div(p.C, 256);
+        if (e == 1) norm_fwd_token_kernel<T, 1, BLOCK><<<grid, 64, 0, st>>>(p);
+        else if (e == 2) norm_fwd_token_kernel<T, 2, BLOCK><<<grid, 64, 0, st>>>(p);
+        else if (e == 3) norm_fwd_token_kernel<T, 3, BLOCK><<<grid, 64, 0, st>>>(p);
+        else if (e == 4) norm_fwd_token_kernel<T, 4, BLOCK><<<grid, 64, 0, st>>>(p);
+        else norm_fwd_token_kernel<T, 8, BLOCK><<<grid, 64, 0, st>>>(p);
+        return;
+    }
     switch (s.E) {
     case 0: norm_fwd_stream_kernel<T, BLOCK><<<s.blocks, 256, 0, st>>>(p); return;
     case 1: return fwd_tile<T, 1, BLOCK>(p, s, st);

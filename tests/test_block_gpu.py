@@ -248,7 +248,7 @@ def test_scan_step_is_the_scan():
 
 # ---- norms ----
 
-NORM_SHAPES = [(2, 1, 1), (3, 5, 1), (2, 768, 1), (2, 5000, 1), (3, 7, 2), (2, 33, 3), (2, 64, 7), (2, 100, 8), (3, 129, 9), (2, 256, 33),
+NORM_SHAPES = [(2, 1, 1), (3, 5, 1), (2, 768, 1), (2, 5000, 1), (70, 33, 1), (3, 254, 1), (3, 257, 1), (2, 1023, 1), (2, 1030, 1), (2, 2047, 1), (3, 7, 2), (2, 33, 3), (2, 64, 7), (2, 100, 8), (3, 129, 9), (2, 256, 33),
                (1, 768, 100), (2, 700, 65), (1, 1100, 40), (1, 2300, 17), (1, 4200, 35), (1, 9000, 20), (40, 3, 100), (5, 32, 257),
                # (every number of rounds of channels, in workgroups of each size, and tiles that share a workgroup)
                (2, 20, 70), (2, 60, 64), (2, 130, 40), (1, 200, 66), (1, 390, 34), (1, 500, 31), (1, 650, 64), (1, 1500, 33), (1, 3300, 16), (17000, 3, 9)]
@@ -277,7 +277,7 @@ def test_norm(B, C, L, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("C,L", [(12, 1), (12, 5), (12, 70), (700, 30), (5000, 21)])
+@pytest.mark.parametrize("C,L", [(12, 1), (11, 1), (12, 5), (12, 70), (700, 30), (5000, 21)])
 @pytest.mark.parametrize("kind", ["slice", "odd"])
 def test_norm_layouts(C, L, kind, dtype):
     y, z, res, dout, dn, w, wn = norm_inputs(3, C, L, dtype)
