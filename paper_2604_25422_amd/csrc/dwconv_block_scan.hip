@@ -13,7 +13,9 @@ struct ScanPlan {
     ShortRows m;
     int gx, gy;
     long long M;                // rows of the sums towards dlam
+    bool whole;                 // workgroups have a channel's whole batch and write dlam themselves
 };
+constexpr int kScanBatch = 8;   // rows of a channel that one workgroup takes so
 
 // (the sizes of workspaces go by segs and M, which do not depend on the type)
 ScanPlan plan_scan(int B, int C, int L, int dtype, bool backward)
@@ -24,6 +26,18 @@ ScanPlan plan_scan(int B, int C, int L, int dtype, bool backward)
         s.G = 1;
         while (s.G * 8 < L) s.G *= 2;
         const int per = 256 / s.G;
+        // A launch less where one workgroup can have the whole batch of its channels: a launch takes the host 3.5 us, what these
+        // calls take the device is less.  (Of larger calls only while neighbouring rows make whole runs of memory.)
+        if (backward && B <= per && (B <= kScanBatch || rows * L <= 1 << 20)) {
+            s.m.nb = B;
+            s.m.cb = std::min(C, per / B);
+            s.gx = (int)ceil_div(C, s.m.cb);
+            s.gy = 1;
+            s.segs = 1;
+            s.M = B;
+            s.whole = true;
+            return s;
+        }
         // channels of a workgroup: as many as it has rows, evenly over the workgroups; of few channels several batch entries
         const int blocks = (int)ceil_div(C, per);
         s.m.cb = (int)ceil_div(C, blocks);
@@ -35,6 +49,15 @@ ScanPlan plan_scan(int B, int C, int L, int dtype, bool backward)
         return s;
     }
     const long long chunks = ceil_div(L, kScanChunk);
+    // (likewise, a wave a row: B4 C64 L1024 fp32 11.5 -> 8.3 us a call, but B8 C768 L1024 31.8 -> 36.4)
+    if (backward && B <= kScanBatch && chunks <= 2 && rows * L <= 1 << 20) {
+        s.W = 1;
+        s.segs = 1;
+        s.seg_groups = (int)chunks;
+        s.M = B;
+        s.whole = true;
+        return s;
+    }
     // Few long rows are cut into segments for the whole chip to work at them, though a first pass then forms the gates of all but one a
     // second time: B1 C32 L40000 fp32 12.4 us forward (17.2 whole), 18.3 backward (32.7); B2 C64 L65537 bf16 45 us backward (58),
     // but 30 us forward (26.5 whole, half of the chip idle).
@@ -100,9 +123,14 @@ template <typename T, int W> void launch_bwd(const ScanBwd<T> &p, const ScanPlan
     if (s.segs > 1) scan_bwd_kernel<T, W, true><<<(unsigned)std::min(rows * (s.segs - 1), kMaxBlocks), 64 * W, 0, st>>>(p);
     scan_bwd_kernel<T, W, false><<<(unsigned)std::min(rows * s.segs, kMaxBlocks), 64 * W, 0, st>>>(p);
 }
-template <typename T> void launch_bwd(const ScanBwd<T> &p, const ScanPlan &s, float *dlam, hipStream_t st)
+template <typename T> void launch_bwd(ScanBwd<T> p, const ScanPlan &s, float *dlam, hipStream_t st)
 {
     const dim3 grid(s.gx, s.gy);
+    p.dlam = s.whole ? dlam : nullptr;
+    if (!s.G && s.whole) {
+        scan_bwd_kernel<T, 1, false, kScanBatch><<<p.C, 64 * p.B, 0, st>>>(p);
+        return;
+    }
     switch (s.G ? s.G : 64 * s.W) {
     case 1: scan_bwd_short_kernel<T, 1><<<grid, 256, 0, st>>>(p, s.m); break;
     case 2: scan_bwd_short_kernel<T, 2><<<grid, 256, 0, st>>>(p, s.m); break;
@@ -115,7 +143,7 @@ template <typename T> void launch_bwd(const ScanBwd<T> &p, const ScanPlan &s, fl
     case 256: launch_bwd<T, 4>(p, s, st); break;
     default: launch_bwd<T, 8>(p, s, st); break;
     }
-    scan_dlam_kernel<<<(unsigned)ceil_div(p.C, 32), 1024, 0, st>>>(p.part, (int)s.M, p.C, p.lam, dlam);
+    if (!s.whole) scan_dlam_kernel<<<(unsigned)ceil_div(p.C, 32), 1024, 0, st>>>(p.part, (int)s.M, p.C, p.lam, dlam);
 }
 
 bool rate_ok(float rate) { return rate > 0.0f && rate < INFINITY; }
@@ -188,10 +216,10 @@ int dwconv_scan_bwd(dwconv_seq dy, dwconv_seq x, dwconv_seq r, dwconv_seq i, con
     Span *spans = reinterpret_cast<Span *>(static_cast<char *>(workspace) + part_bytes(s, C));
     if (dtype == DWCONV_F32)
         launch_bwd(ScanBwd<float>{seq<float>(dy), seq<float>(x), seq<float>(r), seq<float>(i), lam, states, dh_last, lengths, seq<float>(dx),
-                                  seq<float>(dr), seq<float>(di), dh0, part, spans, B, C, L, ns, rate, s.segs, s.seg_groups}, s, dlam, st);
+                                  seq<float>(dr), seq<float>(di), dh0, part, nullptr, spans, B, C, L, ns, rate, s.segs, s.seg_groups}, s, dlam, st);
     else
         launch_bwd(ScanBwd<bf16_t>{seq<bf16_t>(dy), seq<bf16_t>(x), seq<bf16_t>(r), seq<bf16_t>(i), lam, states, dh_last, lengths, seq<bf16_t>(dx),
-                                   seq<bf16_t>(dr), seq<bf16_t>(di), dh0, part, spans, B, C, L, ns, rate, s.segs, s.seg_groups}, s, dlam, st);
+                                   seq<bf16_t>(dr), seq<bf16_t>(di), dh0, part, nullptr, spans, B, C, L, ns, rate, s.segs, s.seg_groups}, s, dlam, st);
     return launch_status();
 }
 

@@ -37,6 +37,7 @@ template <typename T> struct ScanBwd {
     const int *lengths;
     SeqOut<T> dx, dr, di;
     float *dh0, *part;          // part: sums towards dlam, [B * segs, C]
+    float *dlam;                // of workgroups that have a channel's whole batch
     Span *spans;
     int B, C, L, nstates;
     float rate;
@@ -97,6 +98,9 @@ template <bool SHORT, typename T> __device__ __forceinline__ void store_eight(T 
     if constexpr (SHORT) store8(row + t, v, L - t);
     else store_row8(row, v, t, L);
 }
+
+// d softplus(lam) / softplus(lam): the sum of dq q is dlam through it.  (It tends to 1 as lam falls, where both are exp(lam) and at last 0.)
+__device__ __forceinline__ float dlam_factor(float lam) { return lam < -15.0f ? 1.0f : 1.0f / (1.0f + expf(-lam)) / softplus(lam); }
 
 // What the backward pass keeps of eight positions.
 struct GateGrads {
@@ -271,17 +275,19 @@ template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) vo
     }
 }
 
-// SPANS: only the spans of v over the segments but the first.
-template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) void scan_bwd_kernel(ScanBwd<T> p)
+// SPANS: only the spans of v over the segments but the first.  BATCH > 0 (W = 1): a workgroup has the rows of a channel, a wave for each
+// of at most BATCH batch entries, and writes dlam itself.
+template <typename T, int W, bool SPANS, int BATCH = 0> __global__ __launch_bounds__(64 * (BATCH ? BATCH : W)) void scan_bwd_kernel(ScanBwd<T> p)
 {
     __shared__ Span totals[2][W];
-    __shared__ float sums[W];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ float sums[BATCH ? BATCH : W];
+    const int lane = threadIdx.x & 63, wave = BATCH ? 0 : threadIdx.x >> 6;
     const int segs = SPANS ? p.segs - 1 : p.segs;
-    const unsigned units = (unsigned)(p.B * p.C) * (unsigned)segs;
+    const unsigned units = BATCH ? (unsigned)p.C : (unsigned)(p.B * p.C) * (unsigned)segs;
     int side = 0;
     for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const int row = (int)(segs == 1 ? unit : unit / (unsigned)segs), seg = (int)(unit - (unsigned)row * (unsigned)segs) + (SPANS ? 1 : 0);
+        const int row = BATCH ? (int)(threadIdx.x >> 6) * p.C + (int)unit : (int)(segs == 1 ? unit : unit / (unsigned)segs);
+        const int seg = BATCH ? 0 : (int)(unit - (unsigned)row * (unsigned)segs) + (SPANS ? 1 : 0);
         const int b = (int)((unsigned)row / (unsigned)p.C), c = row - b * p.C;
         const int n = row_length(p.lengths, b, p.L);
         const float rho = decay_rate(p.rate, p.lam[c]);
@@ -380,18 +386,20 @@ template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) vo
         if (SPANS) {
             if (threadIdx.x == 0) p.spans[(long long)row * p.segs + seg] = all;
         } else {
-            if (threadIdx.x == 0 && p.dh0 && seg == 0) p.dh0[row] = carry;
+            if ((BATCH ? lane : (int)threadIdx.x) == 0 && p.dh0 && seg == 0) p.dh0[row] = carry;
             sum = group_sum<64>(sum);
-            if constexpr (W > 1) {
-                if (lane == 0) sums[wave] = sum;
+            if constexpr (W > 1 || BATCH > 0) {
+                if (lane == 0) sums[threadIdx.x >> 6] = sum;
                 __syncthreads();
                 if (threadIdx.x == 0) {
                     sum = 0.0f;
-                    for (int o = 0; o < W; ++o) sum += sums[o];
+                    for (int o = 0; o < (BATCH ? p.B : W); ++o) sum += sums[o];
                 }
                 __syncthreads();
             }
-            if (threadIdx.x == 0) p.part[((long long)b * p.segs + seg) * p.C + c] = sum;
+            if constexpr (BATCH > 0) {
+                if (threadIdx.x == 0) p.dlam[c] = sum * dlam_factor(p.lam[c]);
+            } else if (threadIdx.x == 0) p.part[((long long)b * p.segs + seg) * p.C + c] = sum;
         }
     }
 }
@@ -469,7 +477,19 @@ template <typename T, int G> __global__ __launch_bounds__(256) void scan_bwd_sho
         if (t == 0 && p.dh0) p.dh0[row] = front;
     }
     sum = group_sum<G>(sum);
-    if (t == 0 && !idle) p.part[((long long)blockIdx.y * m.nb + sub) * p.C + c] = sum;
+    if (!p.dlam) {
+        if (t == 0 && !idle) p.part[((long long)blockIdx.y * m.nb + sub) * p.C + c] = sum;
+        return;
+    }
+    // (the workgroup has had the whole batch of its channels)
+    __shared__ float sums[256 / G];
+    if (t == 0) sums[g] = sum;
+    __syncthreads();
+    if (t == 0 && sub == 0 && !idle) {
+        sum = 0.0f;
+        for (int k = 0; k < m.nb; ++k) sum += sums[k * m.cb + g];
+        p.dlam[c] = sum * dlam_factor(p.lam[c]);
+    }
 }
 
 // dlam[c]: the sums of its rows of part [M, C] in a fixed order, times d softplus / softplus.
@@ -487,10 +507,7 @@ __global__ __launch_bounds__(1024) void scan_dlam_kernel(const float *part, int 
     if (tm == 0 && c < C) {
         float all = 0.0f;
         for (int k = 0; k < 32; ++k) all += sums[k][tc];
-        const float l = lam[c];
-        // (the quotient tends to 1 as lam falls, where both are exp(lam) and at last 0)
-        const float f = l < -15.0f ? 1.0f : 1.0f / (1.0f + expf(-l)) / softplus(l);
-        dlam[c] = all * f;
+        dlam[c] = all * dlam_factor(lam[c]);
     }
 }
 

@@ -70,7 +70,9 @@ def test_scan_lengths(L, dtype):
 @pytest.mark.parametrize("B,C,L", [(1, 1, 9000), (1, 3, 40001), (2, 1, 70000), (300, 1, 17), (1, 300, 5), (7, 129, 260), (513, 9, 600), (1, 1, 1),
                                    (70, 64, 1030), (33, 64, 2100),
                                    # (one to sixteen waves a row, one group of them and several; segments of one and of several groups)
-                                   (9, 256, 700), (5, 260, 1100), (5, 130, 2100), (3, 100, 4200), (2, 70, 9000), (1, 129, 17000), (1, 64, 34000), (1, 127, 33500)])
+                                   (9, 256, 700), (5, 260, 1100), (5, 130, 2100), (3, 100, 4200), (2, 70, 9000), (1, 129, 17000), (1, 64, 34000), (1, 127, 33500),
+                                   # (a channel's batch in one workgroup, and just not)
+                                   (8, 3, 257), (8, 70, 1024), (9, 70, 1024), (1, 7, 1000), (8, 33, 200), (9, 33, 200), (200, 3, 4), (256, 2, 8), (257, 2, 8), (32, 40, 60)])
 def test_scan_shapes(B, C, L, dtype):
     x, r, i, dy, lam = scan_inputs(B, C, L, dtype, 7)
     check_scan(x, r, i, dy, lam, rand(B, C, seed=1), rand(B, C, seed=2))
