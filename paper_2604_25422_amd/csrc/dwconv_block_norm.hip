@@ -9,7 +9,7 @@ namespace {
 
 struct NormPlan {
     int E, NT, lx;              // tile kernel; E = 0: the streaming one
-    int row_tiles, run;
+    int row_tiles;
     long long tiles;
     int blocks;
 };
@@ -20,13 +20,15 @@ NormPlan plan_norm(int B, int C, int L, int dtype, bool backward)
 {
     NormPlan s{};
     const int V = dtype == DWCONV_F32 ? 4 : 8;
-    s.run = 1;
     // Rows of a tile as long as a cache line (lx = 3) where the registers hold the channels, or else half of one: what a
     // workgroup leaves of a line is fetched by its neighbour, if that is at work at the same time.  A wave's share E of the channels
-    // goes with what a larger workgroup costs: B128 C768 L1024 bf16 forward 220 us as 512 threads and half lines, 242 us as 1024
-    // threads and whole ones (336 us with a quarter of a line); B64 C768 L1024 fp32 233 and 206 us.  Backward, fp32: B32 C256 L4096
-    // 260 us as 1024 threads and E = 2, 269 us as 512 and E = 4; B64 C384 L1024 178 us with whole lines, 200 us with half ones.  bf16:
-    // B32 C256 L4096 151 us with half lines, 161 us with whole ones; B256 C64 L1024 80 us with whole ones and E = 1, 89 us with half.
+    // goes with what a larger workgroup costs.
+    // Forward: B128 C768 L1024 bf16 220 us as 512 threads and half lines, 242 us as 1024 threads and whole ones (336 us with a quarter
+    // of a line); B64 C768 L1024 fp32 233 and 206 us.
+    // Backward, fp32: B64 C384 L1024 171 us as 512 threads and whole lines, 178 us as 1024, 192 us with half lines; B16384 C128 L48
+    // 675 us as 512 threads, 695 us as 256; below half a line larger workgroups win: B64 C1024 L1024 591 us as 1024 threads, 661 us as
+    // 512.  bf16: whole lines only as 256 threads (B32 C256 L4096 155 us as 512, 143 us with half lines; B256 C64 L1024 65 us, 72 us
+    // with half lines as 256 and 77 us with whole ones as 512); B128 C768 L1024 402 us with half lines, 490 us with quarters.
     const bool f32 = dtype == DWCONV_F32;
     const auto take = [&](int lx, int NT, int most) {
         const int rows = NT >> lx;
@@ -36,35 +38,44 @@ NormPlan plan_norm(int B, int C, int L, int dtype, bool backward)
         s.lx = lx;
     };
     for (int lx = 3; lx >= 0; --lx) {
-        const int few = backward ? (f32 ? 4 : lx == 3 ? 2 : kMaxE) : kMaxE;
-        take(lx, 256, few);
-        take(lx, 512, few);
-        if (f32) take(lx, 1024, backward ? 3 : kMaxE);
-        else if (!backward && lx < 3) take(lx, 1024, kMaxE);
+        if (!backward) {
+            take(lx, 256, kMaxE);
+            take(lx, 512, kMaxE);
+            if (f32 || lx < 3) take(lx, 1024, kMaxE);
+        } else if (f32) {
+            take(lx, 256, 2);
+            take(lx, 512, lx >= 2 ? kMaxE : 2);
+            if (lx < 2) take(lx, 1024, 3);
+        } else {
+            take(lx, 256, lx == 3 ? kMaxE : 3);
+            if (lx < 3) take(lx, 512, kMaxE);
+        }
     }
-    if (s.E) {
-        s.row_tiles = (int)ceil_div(L, V << s.lx);
-    } else {
+    if (s.E) s.row_tiles = (int)ceil_div(L, V << s.lx);
+    // (a grid has fewer than 2^32 threads: more tiles than that, each of a few elements then, go to the kernel that walks them)
+    if (s.E && (long long)B * s.row_tiles >= 1ll << 22) s.E = s.lx = 0;
+    if (!s.E) {
         s.NT = 256;
         while (s.lx < 6 && (1 << s.lx) < L && (256 >> (s.lx + 1)) >= 4) ++s.lx;
         s.row_tiles = (int)ceil_div(L, 1 << s.lx);
     }
     s.tiles = (long long)B * s.row_tiles;
     // (a workgroup per tile, in order: workgroups that walk several drift apart, and with them the halves of a line.  B128 C768 L1024
-    // bf16 backward 431 us, 512 us with two tiles each.  Above sixteen thousand of them their sums would be a tenth of the traffic)
-    if (backward && s.E) s.run = (int)ceil_div(s.tiles, 16384);
-    s.blocks = s.E ? (int)ceil_div(s.tiles, s.run) : (int)std::min<long long>(s.tiles, backward ? 1024 : 1 << 20);
+    // bf16 backward, of an earlier form of the kernel: 431 us, 512 us with two tiles each)
+    s.blocks = s.E ? (int)s.tiles : (int)std::min<long long>(s.tiles, backward ? 1024 : 1 << 20);
     return s;
 }
-size_t red_bytes(const NormPlan &s, int V) { return (size_t)(s.NT / 16 + 1) * (V << s.lx) * sizeof(float); }
+size_t red_bytes(const NormPlan &s, int V, int sums) { return (size_t)(s.NT / 16 + 1) * sums * (V << s.lx) * sizeof(float); }
 
 // Runs that the workgroups' sums are first added up in (4096 sums of 768 channels twice: 18 us by norm_sums_kernel alone); 0: not worth it.
 int sum_runs(const NormPlan &s) { return s.blocks >= 512 ? 64 : 0; }
 
 template <typename T, int E, bool BLOCK> void fwd_tile(const NormFwd<T> &p, const NormPlan &s, hipStream_t st)
 {
-    const size_t lds = red_bytes(s, Pack<T>::V);
-    if (s.NT == 256) norm_fwd_tile_kernel<T, E, 256, BLOCK><<<s.blocks, 256, lds, st>>>(p);
+    const size_t lds = red_bytes(s, Pack<T>::V, 1);
+    // (what plan_norm takes: larger workgroups only where smaller ones would have too many packs)
+    if constexpr (E <= 3) norm_fwd_tile_kernel<T, E, 256, BLOCK><<<s.blocks, 256, lds, st>>>(p);
+    else if (s.NT == 256) norm_fwd_tile_kernel<T, E, 256, BLOCK><<<s.blocks, 256, lds, st>>>(p);
     else if (s.NT == 512) norm_fwd_tile_kernel<T, E, 512, BLOCK><<<s.blocks, 512, lds, st>>>(p);
     else norm_fwd_tile_kernel<T, E, 1024, BLOCK><<<s.blocks, 1024, lds, st>>>(p);
 }
@@ -91,10 +102,15 @@ template <typename T, bool BLOCK> void launch_fwd(const NormFwd<T> &p, const Nor
 }
 template <typename T, int E, bool BLOCK> void bwd_tile(const NormBwd<T> &p, const NormPlan &s, hipStream_t st)
 {
-    const size_t lds = red_bytes(s, Pack<T>::V);
-    if (s.NT == 256) norm_bwd_tile_kernel<T, E, 256, BLOCK><<<s.blocks, 256, lds, st>>>(p);
-    else if (s.NT == 512) norm_bwd_tile_kernel<T, E, 512, BLOCK><<<s.blocks, 512, lds, st>>>(p);
-    else if constexpr (sizeof(T) == 4 && E <= 3) norm_bwd_tile_kernel<T, E, 1024, BLOCK><<<s.blocks, 1024, lds, st>>>(p);
+    const size_t lds = red_bytes(s, Pack<T>::V, BLOCK ? 4 : 1) + (size_t)E * (2 * (s.NT >> s.lx) + s.NT) * sizeof(float);
+    constexpr bool F32 = sizeof(T) == 4;
+    if (s.NT == 256) {
+        if constexpr (!F32 || E <= 2) norm_bwd_tile_kernel<T, E, 256, BLOCK><<<s.blocks, 256, lds, st>>>(p);
+    } else if (s.NT == 512) {
+        if constexpr (E >= 2) norm_bwd_tile_kernel<T, E, 512, BLOCK><<<s.blocks, 512, lds, st>>>(p);
+    } else if constexpr (F32 && (E == 2 || E == 3)) {
+        norm_bwd_tile_kernel<T, E, 1024, BLOCK><<<s.blocks, 1024, lds, st>>>(p);
+    }
 }
 template <typename T, bool BLOCK> void launch_bwd(const NormBwd<T> &p, const NormPlan &s, float *dw, float *dw_next, hipStream_t st)
 {
@@ -134,7 +150,7 @@ void run_bwd(const dwconv_seq &dout, const dwconv_seq &dn, const dwconv_seq &y, 
              float *dw_next, float *part, int B, int C, int L, float scale, const NormPlan &s, hipStream_t st)
 {
     const NormBwd<T> p{seq<T>(dout), seq<T>(dn), seq<T>(y), seq<T>(z), seq<T>(res), w, w_next, stats, seq<T>(dy), seq<T>(dz), seq<T>(dres), part,
-                       B, C, L, scale, s.lx, s.tiles, s.row_tiles, s.run};
+                       B, C, L, scale, s.lx, s.tiles, s.row_tiles};
     if (y.data) launch_bwd<T, true>(p, s, dw, dw_next, st);
     else launch_bwd<T, false>(p, s, nullptr, dw_next, st);
 }

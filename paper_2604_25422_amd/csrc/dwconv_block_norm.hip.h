@@ -2,11 +2,10 @@
 //
 // The means run over the channels, L elements apart in memory, and all positions are independent: a workgroup takes a few
 // neighbouring positions of one batch entry with all their channels, a tile whose rows are whole vectors, and holds it in
-// registers from the load to the store, so that the two sums of the forward pass (y^2, then out^2) and the two of the backward
+// registers from the load to the store, so that the two sums of the forward pass (y^2, then out^2) and those of the backward
 // pass (both forward means come from it as `stats`) cost no second read.  Lane x of a tile's row has 16 bytes of positions, the rows
 // go over the other lanes and E times round; sums over channels go over the lanes of a wave, then over the waves in LDS, in a fixed
-// order.  Parameter gradients are summed over the positions of a lane and over the tiles a workgroup walks, then over the
-// lanes of a row, and a second launch adds the workgroups' sums.
+// order.  Parameter gradients are summed over the positions of a lane and the lanes of a row; further launches add the tiles' sums.
 #pragma once
 #include "dwconv_block_common.hip.h"
 
@@ -32,7 +31,7 @@ template <typename T> struct NormBwd {
     float scale;
     int lx;
     long long tiles;
-    int row_tiles, run; // run: tiles of a workgroup of the tile kernel, one behind the other
+    int row_tiles;
 };
 
 // Workgroups go to the eight dies in turn; give every die a run of neighbouring tiles, whose rows share cache lines.
@@ -42,54 +41,70 @@ __device__ __forceinline__ long long die_run(long long i, long long n)
     return k * q + (k < r ? k : r) + (i >> 3);
 }
 
-// v[k] summed over the channels of the tile, for the positions of this lane: over the lanes of sixteen that stand at the same
-// positions (moves inside a row of lanes, which cost no more than the addition), then over the rows of lanes in LDS, four
-// lanes a position.  red: [NT / 16 + 1][V << lx] floats; a row of the tile has at most sixteen lanes.
-template <int V, int NT> __device__ __forceinline__ void channel_sums(float (&v)[V], int lx, float *red)
+// S sums v[s][k] over the channels of the tile, for the positions of this lane: over the lanes of sixteen that stand at the same
+// positions (moves inside a row of lanes, which cost no more than the addition), then over the rows of lanes in LDS, four lanes a
+// position.  red: [NT / 16 + 1][S][V << lx] floats; a row of the tile has at most sixteen lanes.
+template <int S, int V, int NT> __device__ __forceinline__ void channel_sums(float (&v)[S][V], int lx, float *red)
 {
-    const int x = threadIdx.x & ((1 << lx) - 1), T = V << lx;
-    if (lx < 1) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) v[k] += dpp<0xB1>(0.0f, v[k]);       // the neighbouring lane
-    }
-    if (lx < 2) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) v[k] += dpp<0x4E>(0.0f, v[k]);       // the other two of four
-    }
-    if (lx < 3) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) v[k] += dpp<0x124>(0.0f, v[k]);      // four lanes on, round the sixteen
-    }
-    if (lx < 4) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) v[k] += dpp<0x128>(0.0f, v[k]);      // eight lanes on
-    }
+    const int x = threadIdx.x & ((1 << lx) - 1), T = V << lx, all = S * T;
+#define DWCONV_ADD(CTRL)                                                       \
+    _Pragma("unroll") for (int s = 0; s < S; ++s)                              \
+        _Pragma("unroll") for (int k = 0; k < V; ++k) v[s][k] += dpp<CTRL>(0.0f, v[s][k]);
+    if (lx < 1) { DWCONV_ADD(0xB1) }        // the neighbouring lane
+    if (lx < 2) { DWCONV_ADD(0x4E) }        // the other two of four
+    if (lx < 3) { DWCONV_ADD(0x124) }       // four lanes on, round the sixteen
+    if (lx < 4) { DWCONV_ADD(0x128) }       // eight lanes on
+#undef DWCONV_ADD
     if ((threadIdx.x & 15) < (1 << lx)) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) red[(threadIdx.x >> 4) * T + x * V + k] = v[k];
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int k = 0; k < V; ++k) red[(threadIdx.x >> 4) * all + s * T + x * V + k] = v[s][k];
     }
     __syncthreads();
-    float *sum = red + NT / 16 * T;
-    for (int i = threadIdx.x; i < 4 * T; i += NT) {
+    float *sum = red + NT / 16 * all;
+    for (int i = threadIdx.x; i < 4 * all; i += NT) {
         float s = 0.0f;
 #pragma unroll
-        for (int r = 0; r < NT / 64; ++r) s += red[(4 * r + (i & 3)) * T + (i >> 2)];
+        for (int r = 0; r < NT / 64; ++r) s += red[(4 * r + (i & 3)) * all + (i >> 2)];
         s += dpp<0xB1>(0.0f, s);
         s += dpp<0x4E>(0.0f, s);
         if ((i & 3) == 0) sum[i >> 2] = s;
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < V; ++k) v[k] = sum[x * V + k];
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[s][k] = sum[s * T + x * V + k];
     // (the next use of `red` writes its first part, which nobody reads any more, and `sum` behind a barrier)
 }
+template <int V, int NT> __device__ __forceinline__ void channel_sums(float (&v)[V], int lx, float *red)
+{
+    channel_sums<1, V, NT>(reinterpret_cast<float (&)[1][V]>(v), lx, red);
+}
+
+// Element k of a pack to be stored; `before` holds element k - 1 where two share a word.
+__device__ __forceinline__ void set_pack(Pack<float> &e, int k, float &, float v) { e.w[k] = v; }
+__device__ __forceinline__ void set_pack(Pack<bf16_t> &e, int k, float &before, float v)
+{
+    if (k & 1) e.w[k >> 1] = pack_bf16(before, v);
+    else before = v;
+}
+__device__ __forceinline__ void store_packed(float *p, const Pack<float> &e) { *reinterpret_cast<floatx4_any *>(p) = e.w; }
+__device__ __forceinline__ void store_packed(bf16_t *p, const Pack<bf16_t> &e) { *reinterpret_cast<uintx4_any *>(p) = e.w; }
 
 // What the registers hold from here on counts as new: nothing that an earlier pass made of it (widened elements, gates) is kept
 // in more registers for a later one, which makes it again.
 __device__ __forceinline__ void forget(Pack<float> &e) { asm("" : "+v"(e.w)); }
 __device__ __forceinline__ void forget(Pack<bf16_t> &e) { asm("" : "+v"(e.w)); }
+__device__ __forceinline__ void keep_bits(Pack<float> &e, unsigned mask)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) e.w[k] = __uint_as_float(__float_as_uint(e.w[k]) & mask);
+}
+__device__ __forceinline__ void keep_bits(Pack<bf16_t> &e, unsigned mask) { e.w &= mask; }
 // ... and what is to be in a register here, so that the terms of a sum do not wait for it in registers of their own.
-__device__ __forceinline__ void settle(float &v) { asm volatile("" : "+v"(v)); }
+template <typename V> __device__ __forceinline__ void settle(V &v) { asm volatile("" : "+v"(v)); }
 
 __device__ __forceinline__ float inv_sqrt(float v) { return 1.0f / sqrtf(v); }
 
@@ -192,132 +207,172 @@ template <typename T, int E, int NT, bool BLOCK> __global__ __launch_bounds__(NT
     }
 }
 
-template <typename T, int E, int NT, bool BLOCK> __global__ __launch_bounds__(NT) void norm_bwd_tile_kernel(NormBwd<T> p)
+// Both means of a position come from four sums that one pass over the tile forms at once; a second pass has the gradients.  Memory
+// bounds it where a CU has several tiles at work (B32 C256 L4096 fp32 250 us, 4.3 TB/s; B256 C192 L1024 bf16 179 us, 4.5 TB/s) and the
+// registers where it has one (B128 C768 L1024 bf16 418 us with the sums, 3.85 TB/s): 60 instructions an element then stand
+// between a tile's loads and its stores, so they are cut where they can be: the rms factors come in behind the sums, and with
+// five packs a lane or more, which a SIMD has two waves of in any case, the gates of the first pass stay for the second (B128 C768
+// 434 -> 414 us).  Three packs of bf16 fit into a SIMD's registers four times only if r2 is read twice and instructions move
+// in steps of two elements (B256 C96 L1024 126 -> 94 us).
+template <typename T, int E, int NT, bool BLOCK>
+__global__ __launch_bounds__(NT, BLOCK && sizeof(T) == 2 && E == 3 ? 4 : 1) void norm_bwd_tile_kernel(NormBwd<T> p)
 {
     constexpr int V = Pack<T>::V;
+    constexpr bool LEAN = BLOCK && sizeof(T) == 2 && E == 3;
+    constexpr bool KEEP = BLOCK && NT == 512 && E >= 5;
+    constexpr int STEP = LEAN ? 2 : 4;              // elements whose instructions may mix: with more, more registers hold what waits
     extern __shared__ float red[];
     const int x = threadIdx.x & ((1 << p.lx) - 1), c0 = threadIdx.x >> p.lx, step = NT >> p.lx;
     const unsigned mine = ((unsigned)c0 * (unsigned)p.L + (unsigned)(x * V)) * (unsigned)sizeof(T);
     const bool in = c0 + (E - 1) * step < p.C;
-    float w[E], wn[E], sum_w[E], sum_n[E];
+    const float inv_c = 1.0f / (float)p.C;
+    // behind the sums of a position in LDS: the parameters, and every lane's sums for its channels
+    float *ws = red + (NT / 16 + 1) * (BLOCK ? 4 : 1) * (V << p.lx), *wns = ws + E * step, *mine_n = wns + E * step;
+    const TileAt tile = tile_at(die_run(blockIdx.x, p.tiles), p.row_tiles, V << p.lx, p.L);
+    const auto at = [&](const auto &s, int e) { return place(s.p + ((long long)tile.b * s.bs + (long long)(e * step) * p.L + tile.t0), mine); };
+    // Loads come back in order, so what is needed first is asked for first; nothing in between waits for them.
+    for (int c = threadIdx.x; c < E * step; c += NT) {
+        if (BLOCK) ws[c] = c < p.C ? p.scale * p.w[c] : 0.0f;
+        wns[c] = c < p.C ? p.w_next[c] : 0.0f;
+    }
+    float r1[V], r2[V];
+    const float *s = p.stats + (long long)tile.b * 2 * p.L + tile.t0 + x * V;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        r1[k] = BLOCK ? s[k] : 0.0f;
+        r2[k] = s[p.L + k];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // Lanes behind the last channel load that channel and mask it, and without a gradient of out dn stands in for it and is masked:
+    // a branch here would have the first pass wait for loads that it does not need yet.
+    const unsigned there = in ? ~0u : 0u, given = p.dout.p ? ~0u : 0u;
+    const Seq<T> other = p.dout.p ? p.dout : p.dn;
+    const int c_last = min(c0, p.C - 1 - (E - 1) * step);
+    const unsigned last = ((unsigned)c_last * (unsigned)p.L + (unsigned)(x * V)) * (unsigned)sizeof(T);
+    const auto from = [&](const auto &s, int e) {
+        return place(s.p + ((long long)tile.b * s.bs + (long long)(e * step) * p.L + tile.t0), e < E - 1 ? mine : last);
+    };
+    Pack<T> y[E], z[E], res[E], dn[E], dout[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const int c = c0 + e * step;
-        const bool have = e < E - 1 || in;
-        w[e] = BLOCK && have ? p.scale * p.w[c] : 0.0f;
-        wn[e] = have ? p.w_next[c] : 0.0f;
-        sum_w[e] = sum_n[e] = 0.0f;
+        load_pack(res[e], from(p.res, e));
+        if (BLOCK) {
+            load_pack(z[e], from(p.z, e));
+            load_pack(y[e], from(p.y, e));
+        }
+        load_pack(dn[e], from(p.dn, e));
+        load_pack(dout[e], from(other, e));
+        __builtin_amdgcn_sched_barrier(0);
     }
-    const float inv_c = 1.0f / (float)p.C;
-    const long long block = die_run(blockIdx.x, gridDim.x), end = (block + 1) * p.run < p.tiles ? (block + 1) * p.run : p.tiles;
-    for (long long i = block * p.run; i < end; ++i) {
-        const TileAt tile = tile_at(i, p.row_tiles, V << p.lx, p.L);
-        const auto at = [&](const auto &s, int e) { return place(s.p + ((long long)tile.b * s.bs + (long long)(e * step) * p.L + tile.t0), mine); };
-        Pack<T> y[E], z[E], res[E], dn[E], dout[E];
-        y[E - 1] = z[E - 1] = res[E - 1] = dn[E - 1] = Pack<T>{};
+    __syncthreads();
+    const int again = tile.again - x * V;           // of this lane's positions
+    // r2 where a position counts in the sums over positions, 0 where the tile before counts it (which has the same infinities and NaN)
+    float counted[V];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            if (e < E - 1 || in) {
-                load_pack(res[e], at(p.res, e));
-                load_pack(dn[e], at(p.dn, e));
-                if (BLOCK) {
-                    load_pack(y[e], at(p.y, e));
-                    load_pack(z[e], at(p.z, e));
-                }
-            }
-        }
+    for (int k = 0; k < V; ++k) counted[k] = k < again ? 0.0f : r2[k];
+    // Both means at once: with oh = out r2, dnw = dn w_next, yh = y r1 and q = silu(z) yh w scale, the gradient of out is
+    // d = dout + r2 (dnw - oh m), m = mean(dnw oh), and that of yh yh is d q, whose mean m1 is
+    // mean(dout q) + r2 (mean(dnw q) - m mean(oh q)).  r1 and r2 come in behind the sums.
+    int c = c0;
+    constexpr int S = BLOCK ? 4 : 1;
+    float sums[S][V] = {};
+    float g[KEEP ? E : 1][V];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            dout[e] = Pack<T>{};
-            if (p.dout.p && (e < E - 1 || in)) load_pack(dout[e], at(p.dout, e));
+    for (int e = 0; e < E; ++e) {
+        settle(c);
+        const float w = BLOCK ? ws[c + e * step] : 0.0f, wn = wns[c + e * step];
+        float sum = 0.0f;
+        keep_bits(dout[e], e < E - 1 ? given : given & there);
+        if (e == E - 1) {
+            keep_bits(res[e], there), keep_bits(dn[e], there);
+            if (BLOCK) keep_bits(y[e], there), keep_bits(z[e], there);
         }
-        float r1[V], r2[V], m[V];
-        const float *s = p.stats + (long long)tile.b * 2 * p.L + tile.t0 + x * V;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            r1[k] = BLOCK ? s[k] : 0.0f;
-            r2[k] = s[p.L + k];
-            m[k] = 0.0f;
-        }
-        const int again = tile.again - x * V;           // of this lane's positions
-        // out / sqrt(m2 + eps) of element k of pack e, and what silu gave it
-        const auto normed = [&](int e, int k, float &silu, float &g) {
-            float v = res[e][k];
-            silu = g = 0.0f;
+            float v = res[e][k], q = 0.0f;
+            const float dnw = dn[e][k] * wn;
             if constexpr (BLOCK) {
-                g = sigmoid(z[e][k]);
-                silu = z[e][k] * g;
-                v = fmaf(silu * (y[e][k] * r1[k]), w[e], v);
+                const float s = sigmoid(z[e][k]);
+                if constexpr (KEEP) g[e][k] = s;
+                q = z[e][k] * s * y[e][k] * w;
+                v = fmaf(r1[k], q, v);
             }
-            return v * r2[k];
-        };
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                float silu, g;
-                const float oh = normed(e, k, silu, g), d = dn[e][k] * oh;
-                m[k] = fmaf(d, wn[e], m[k]);
-                sum_n[e] += k < again ? 0.0f : d;
+            sums[0][k] = fmaf(dnw, v, sums[0][k]);
+            sum = fmaf(dn[e][k] * counted[k], v, sum);
+            if constexpr (BLOCK) {
+                sums[1][k] = fmaf(dout[e][k], q, sums[1][k]);
+                sums[2][k] = fmaf(dnw, q, sums[2][k]);
+                sums[3][k] = fmaf(v, q, sums[3][k]);
             }
-            settle(sum_n[e]);
-            forget(res[e]), forget(dn[e]);
-            if (BLOCK) forget(y[e]), forget(z[e]);
-            __builtin_amdgcn_sched_barrier(0);
+            if (k % STEP == STEP - 1) __builtin_amdgcn_sched_barrier(0);
         }
-        channel_sums<V, NT>(m, p.lx, red);
+        mine_n[e * NT + threadIdx.x] = sum;
 #pragma unroll
-        for (int k = 0; k < V; ++k) m[k] *= inv_c;
-        float m1[V], dyh[E][V];
+        for (int s = 0; s < S; ++s)
 #pragma unroll
-        for (int k = 0; k < V; ++k) m1[k] = 0.0f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            float d[V], dz[V];
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                float silu, g;
-                const float oh = normed(e, k, silu, g);
-                d[k] = fmaf(r2[k], fmaf(-oh, m[k], dn[e][k] * wn[e]), dout[e][k]);
-                if constexpr (BLOCK) {
-                    // out = .. + silu(z) yh w; d silu = sigmoid (1 + z (1 - sigmoid)) = sigmoid + silu (1 - sigmoid)
-                    const float yh = y[e][k] * r1[k], dw = d[k] * w[e], dg = d[k] * (silu * yh);
-                    dz[k] = dw * yh * fmaf(silu, 1.0f - g, g);
-                    dyh[e][k] = dw * silu;
-                    sum_w[e] += k < again ? 0.0f : dg;
-                    m1[k] = fmaf(dg, w[e], m1[k]);
-                }
-            }
-            if (e < E - 1 || in) {
-                store_pack(at(p.dres, e), d);
-                if constexpr (BLOCK) store_pack(at(p.dz, e), dz);
-            }
-            if (BLOCK) settle(sum_w[e]), forget(y[e]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if constexpr (BLOCK) {
-            channel_sums<V, NT>(m1, p.lx, red);
-#pragma unroll
-            for (int k = 0; k < V; ++k) m1[k] *= inv_c * r1[k];
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-#pragma unroll
-                for (int k = 0; k < V; ++k) dyh[e][k] = r1[k] * fmaf(-y[e][k], m1[k], dyh[e][k]);
-                if (e < E - 1 || in) store_pack(at(p.dy, e), dyh[e]);
-            }
-        }
+            for (int k = 0; k < V; ++k) settle(sums[s][k]);
+        forget(res[e]), forget(dn[e]);
+        if (BLOCK) forget(y[e]), forget(z[e]), forget(dout[e]);
+        __builtin_amdgcn_sched_barrier(0);
     }
-    // (out's part of dw carries the scale)
+    if (LEAN) {
+        settle(s);
+#pragma unroll
+        for (int k = 0; k < V; ++k) r2[k] = s[p.L + k];
+    }
+    channel_sums<S, V, NT>(sums, p.lx, red);
+    float *part = p.part + (long long)blockIdx.x * 2 * p.C;
+    for (int c = threadIdx.x; c < p.C; c += NT) {
+        float n = 0.0f;                                 // (lane x of channel c stands at c 2^lx + x)
+        for (int i = 0; i < (1 << p.lx); ++i) n += mine_n[(c << p.lx) + i];
+        part[p.C + c] = n;
+    }
+    // d = dout + r2 (dnw + m2 out) and dy = r1 (d w silu(z) scale) + m1 y
+    float m2[V], m1[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const float m = r2[k] * sums[0][k] * inv_c;
+        m2[k] = -(r2[k] * m);
+        counted[k] = k < again ? 0.0f : r1[k];
+        if constexpr (BLOCK) m1[k] = -(r1[k] * (r1[k] * (fmaf(r2[k], fmaf(m2[k], sums[3][k], sums[2][k]), sums[1][k]) * r1[k] * inv_c)));
+    }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const int c = c0 + e * step;
-        float a = sum_w[e] * p.scale, n = sum_n[e];
-        for (int d = 1; d < (1 << p.lx); d *= 2) a += __shfl_xor(a, d, 64), n += __shfl_xor(n, d, 64);
-        if (x == 0 && c < p.C) {
-            float *part = p.part + (long long)blockIdx.x * 2 * p.C + c;
-            if (BLOCK) part[0] = a;
-            part[p.C] = n;
+        settle(c);
+        const float w = BLOCK ? ws[c + e * step] : 0.0f, wn = wns[c + e * step];
+        Pack<T> d, dz, dy;
+        float sum = 0.0f, od, odz, ody;                 // (the element before, until there are two to pack)
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            float v = res[e][k], s = 0.0f, silu = 0.0f, gated = 0.0f;
+            if constexpr (BLOCK) {
+                s = KEEP ? g[KEEP ? e : 0][k] : sigmoid(z[e][k]), silu = z[e][k] * s, gated = silu * y[e][k];
+                v = fmaf(r1[k], gated * w, v);
+            }
+            const float now = fmaf(r2[k], fmaf(v, m2[k], dn[e][k] * wn), dout[e][k]);
+            set_pack(d, k, od, now);
+            if constexpr (BLOCK) {
+                // d silu = sigmoid (1 + z (1 - sigmoid)) = sigmoid + silu (1 - sigmoid)
+                const float dw = now * w * r1[k];
+                set_pack(dz, k, odz, dw * y[e][k] * fmaf(silu, 1.0f - s, s));
+                set_pack(dy, k, ody, fmaf(y[e][k], m1[k], dw * silu));
+                sum = fmaf(now * gated, counted[k], sum);
+            }
+            if (k % STEP == STEP - 1) __builtin_amdgcn_sched_barrier(0);
         }
+        if (e < E - 1 || in) {
+            store_packed(at(p.dres, e), d);
+            if constexpr (BLOCK) {
+                store_packed(at(p.dz, e), dz);
+                store_packed(at(p.dy, e), dy);
+            }
+        }
+        if constexpr (BLOCK) {
+            settle(sum);
+            sum = group_sum(sum, p.lx) * p.scale;       // (out's part of dw carries the scale)
+            if (x == 0 && (e < E - 1 || in)) part[c + e * step] = sum;
+        }
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 

@@ -221,3 +221,10 @@ def test_native_calls_decline_what_is_not_a_device_tensor(lib):
                  lambda: _fastcall.clip_grad_norm([x], 1.0, None, None), lambda: _fastcall.clip_grad_norm([], 1.0, None, None), lambda: _fastcall.clip_grad_norm([None], 1.0, [x], None),
                  lambda: _fastcall.conv_step(x, x, x, None, None, None), lambda: _fastcall.conv_step(None, None, None, None, None, None)):
         assert call() is None
+
+
+def test_norm_workspace_of_many_tiles_is_bounded(lib):
+    # (a row of sums for every tile only while a grid has all tiles)
+    for B, L in ((1 << 30, 5), (1 << 22, 4), (1 << 22, 64)):
+        assert 0 < lib.dwconv_norm_workspace_bytes(B, 1, L, 0) <= 1100 * 2 * 4
+    assert lib.dwconv_norm_workspace_bytes((1 << 22) - 1, 1, 4, 0) >= 2 * 4 * ((1 << 22) - 1)

@@ -344,6 +344,28 @@ def test_norm_above_32_bits():
 
 # ---- clipping ----
 
+@pytest.mark.parametrize("C,L", [(1, 4), (2, 9)])
+def test_norm_of_more_tiles_than_a_grid_has(C, L):
+    B = (1 << 22) + 5
+    y, z, res, dout, dn = (torch.randn(B, C, L, device="cuda") for _ in range(5))
+    w, wn = rand(C, seed=1), rand(C, seed=2)
+    out, n, stats = block.norm_fwd(y, z, res, w, wn)
+    dy, dz, dres, dw, dwn = block.norm_bwd(dout, dn, y, z, res, w, wn, stats)
+    for at in (slice(0, 40), slice(B // 2, B // 2 + 40), slice(B - 40, B)):
+        want, err = ref.norm(*(t[at] for t in (y, z, res)), w, wn, dout=dout[at], dn=dn[at])
+        for k, v in dict(out=out, n=n, dy=dy, dz=dz, dres=dres).items():
+            ref.check(v[at], want[k], err[k], F32, k)
+    # (a workgroup adds up to 4200 tiles one by one, the rest in a tree; a term has fewer than 40 roundings)
+    y, z, res, dout, dn = (t.double() for t in (y, z, res, dout, dn))
+    wd, wnd = w.double()[:, None], wn.double()[:, None]
+    yh, silu = y * (y.square().mean(1, keepdim=True) + 1e-6).rsqrt(), z * torch.sigmoid(z)
+    o = res + silu * yh * wd
+    r2 = (o.square().mean(1, keepdim=True) + 1e-6).rsqrt()
+    d = dout + r2 * (dn * wnd - o * r2 * (dn * wnd * o * r2).mean(1, keepdim=True))
+    for got, term in ((dwn, dn * o * r2), (dw, d * silu * yh)):
+        assert ((got.double() - term.sum((0, 2))).abs() <= 4300 * 2.0 ** -24 * term.abs().sum((0, 2))).all()
+
+
 def clip_ref(grads, max_norm):
     norm = math.sqrt(math.fsum(float(g.double().square().sum()) for g in grads))
     return norm, min(1.0, max_norm / (norm + 1e-6))
