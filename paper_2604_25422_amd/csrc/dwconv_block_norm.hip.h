@@ -35,9 +35,9 @@ template <typename T> struct NormBwd {
 };
 
 // Workgroups go to the eight dies in turn; give every die a run of neighbouring tiles, whose rows share cache lines.
-__device__ __forceinline__ long long die_run(long long i, long long n)
+template <typename I> __device__ __forceinline__ I die_run(I i, I n)
 {
-    const long long q = n >> 3, r = n & 7, k = i & 7;
+    const I q = n >> 3, r = n & 7, k = i & 7;
     return k * q + (k < r ? k : r) + (i >> 3);
 }
 
@@ -120,9 +120,9 @@ template <typename T> __device__ __forceinline__ T *place(T *p, unsigned bytes) 
 struct TileAt {
     int b, t0, again;       // batch entry, first position, positions that the tile before has counted
 };
-__device__ __forceinline__ TileAt tile_at(long long tile, int row_tiles, int T, int L)
+__device__ __forceinline__ TileAt tile_at(unsigned tile, int row_tiles, int T, int L)
 {
-    const int b = (int)(tile / row_tiles), t = (int)(tile - (long long)b * row_tiles) * T, over = t + T > L ? t + T - L : 0;
+    const int b = (int)(tile / (unsigned)row_tiles), t = (int)(tile - (unsigned)b * (unsigned)row_tiles) * T, over = t + T > L ? t + T - L : 0;
     return TileAt{b, t - over, over};
 }
 
@@ -133,7 +133,7 @@ template <typename T, int E, int NT, bool BLOCK> __global__ __launch_bounds__(NT
     const int x = threadIdx.x & ((1 << p.lx) - 1), c0 = threadIdx.x >> p.lx, step = NT >> p.lx;
     // a lane's place is the same in every pack and tensor: one offset that is its own, the rest is the workgroup's
     const unsigned mine = ((unsigned)c0 * (unsigned)p.L + (unsigned)(x * V)) * (unsigned)sizeof(T);
-    const TileAt tile = tile_at(die_run(blockIdx.x, p.tiles), p.row_tiles, V << p.lx, p.L);
+    const TileAt tile = tile_at(die_run<unsigned>(blockIdx.x, (unsigned)p.tiles), p.row_tiles, V << p.lx, p.L);
     const auto at = [&](const auto &s, int e) { return place(s.p + ((long long)tile.b * s.bs + (long long)(e * step) * p.L + tile.t0), mine); };
     // (only the last round of channels can be short)
     const bool in = c0 + (E - 1) * step < p.C;
@@ -208,8 +208,8 @@ template <typename T, int E, int NT, bool BLOCK> __global__ __launch_bounds__(NT
 }
 
 // Both means of a position come from four sums that one pass over the tile forms at once; a second pass has the gradients.  Memory
-// bounds it where a CU has several tiles at work (B32 C256 L4096 fp32 250 us, 4.3 TB/s; B256 C192 L1024 bf16 179 us, 4.5 TB/s) and the
-// registers where it has one (B128 C768 L1024 bf16 418 us with the sums, 3.85 TB/s): 60 instructions an element then stand
+// bounds it where a CU has several tiles at work (B32 C256 L4097 fp32 244 us, 4.4 TB/s; B256 C192 L1024 bf16 179 us, 4.5 TB/s) and the
+// registers where it has one (B128 C768 L1024 bf16 410 us with the sums, 3.9 TB/s): 60 instructions an element then stand
 // between a tile's loads and its stores, so they are cut where they can be: the rms factors come in behind the sums, and with
 // five packs a lane or more, which a SIMD has two waves of in any case, the gates of the first pass stay for the second (B128 C768
 // 434 -> 414 us).  Three packs of bf16 fit into a SIMD's registers four times only if r2 is read twice and instructions move
@@ -228,12 +228,20 @@ __global__ __launch_bounds__(NT, BLOCK && sizeof(T) == 2 && E == 3 ? 4 : 1) void
     const float inv_c = 1.0f / (float)p.C;
     // behind the sums of a position in LDS: the parameters, and every lane's sums for its channels
     float *ws = red + (NT / 16 + 1) * (BLOCK ? 4 : 1) * (V << p.lx), *wns = ws + E * step, *mine_n = wns + E * step;
-    const TileAt tile = tile_at(die_run(blockIdx.x, p.tiles), p.row_tiles, V << p.lx, p.L);
+    const TileAt tile = tile_at(die_run<unsigned>(blockIdx.x, (unsigned)p.tiles), p.row_tiles, V << p.lx, p.L);
     const auto at = [&](const auto &s, int e) { return place(s.p + ((long long)tile.b * s.bs + (long long)(e * step) * p.L + tile.t0), mine); };
     // Loads come back in order, so what is needed first is asked for first; nothing in between waits for them.
-    for (int c = threadIdx.x; c < E * step; c += NT) {
-        if (BLOCK) ws[c] = c < p.C ? p.scale * p.w[c] : 0.0f;
-        wns[c] = c < p.C ? p.w_next[c] : 0.0f;
+    // (the parameters of two rounds wait in registers until the tile's loads are on their way)
+    float pw[2], pn[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int c = min((int)threadIdx.x + i * NT, p.C - 1);
+        pw[i] = BLOCK ? p.w[c] : 0.0f;
+        pn[i] = p.w_next[c];
+    }
+    for (int c = threadIdx.x + 2 * NT; c < p.C; c += NT) {
+        if (BLOCK) ws[c] = p.scale * p.w[c];
+        wns[c] = p.w_next[c];
     }
     float r1[V], r2[V];
     const float *s = p.stats + (long long)tile.b * 2 * p.L + tile.t0 + x * V;
@@ -264,6 +272,15 @@ __global__ __launch_bounds__(NT, BLOCK && sizeof(T) == 2 && E == 3 ? 4 : 1) void
         load_pack(dout[e], from(other, e));
         __builtin_amdgcn_sched_barrier(0);
     }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int c = threadIdx.x + i * NT;
+        if (c < E * step) {
+            if (BLOCK) ws[c] = c < p.C ? p.scale * pw[i] : 0.0f;
+            wns[c] = c < p.C ? pn[i] : 0.0f;
+        }
+    }
+    for (int c = max(p.C, 2 * NT) + threadIdx.x; c < E * step; c += NT) ws[c] = wns[c] = 0.0f;
     __syncthreads();
     const int again = tile.again - x * V;           // of this lane's positions
     // r2 where a position counts in the sums over positions, 0 where the tile before counts it (which has the same infinities and NaN)
