@@ -92,6 +92,75 @@ __device__ __forceinline__ void store8(bf16_t *p, const float (&v)[8], int left)
     }
 }
 
+// A row of L <= P elements that one lane holds: one access for a row of P, or one for each power of two in L.
+template <int BYTES> struct Words { typedef unsigned type __attribute__((ext_vector_type(BYTES / 4), aligned(2))); };
+template <> struct Words<2> { typedef unsigned short type; };
+template <> struct Words<4> { typedef unsigned type __attribute__((aligned(2))); };
+template <int P, typename T> struct Few {
+    T v[P];
+    __device__ __forceinline__ float operator[](int k) const { return ld_elem(v + k); }
+};
+template <int P, typename T, int N> __device__ __forceinline__ void load_part(Few<N, T> &e, int at, const T *row, int left)
+{
+    constexpr int BYTES = P * (int)sizeof(T) < 16 ? P * (int)sizeof(T) : 16, H = P / 2;
+    if (left >= P) {
+#pragma unroll
+        for (int k = 0; k < P * (int)sizeof(T) / BYTES; ++k) {
+            const auto w = reinterpret_cast<const typename Words<BYTES>::type *>(row)[k];
+            __builtin_memcpy((char *)(e.v + at) + k * BYTES, &w, BYTES);
+        }
+    } else if constexpr (P > 1) {
+        if (left > H) {
+            load_part<H>(e, at, row, H);
+            load_part<H>(e, at + H, row + H, left - H);
+        } else {
+            load_part<H>(e, at, row, left);
+        }
+    }
+}
+template <int P, typename T> __device__ __forceinline__ Few<P, T> load_few(const T *row, int L)
+{
+    Few<P, T> e{};
+    load_part<P>(e, 0, row, L);
+    return e;
+}
+template <int P, typename T, int N> __device__ __forceinline__ void store_part(T *row, const Few<N, T> &e, int at, int left)
+{
+    constexpr int BYTES = P * (int)sizeof(T) < 16 ? P * (int)sizeof(T) : 16, H = P / 2;
+    if (left >= P) {
+#pragma unroll
+        for (int k = 0; k < P * (int)sizeof(T) / BYTES; ++k) {
+            typename Words<BYTES>::type w;
+            __builtin_memcpy(&w, (const char *)(e.v + at) + k * BYTES, BYTES);
+            reinterpret_cast<typename Words<BYTES>::type *>(row)[k] = w;
+        }
+    } else if constexpr (P > 1) {
+        if (left > H) {
+            store_part<H>(row, e, at, H);
+            store_part<H>(row + H, e, at + H, left - H);
+        } else {
+            store_part<H>(row, e, at, left);
+        }
+    }
+}
+__device__ __forceinline__ void round_two(float *to, float a, float b) { to[0] = a, to[1] = b; }
+__device__ __forceinline__ void round_two(bf16_t *to, float a, float b)
+{
+    const unsigned w = pack_bf16(a, b);
+    to[0].bits = (uint16_t)w, to[1].bits = (uint16_t)(w >> 16);
+}
+template <int P, typename T> __device__ __forceinline__ void store_few(T *row, const float (&v)[P], int L)
+{
+    Few<P, T> e;
+    if constexpr (P == 1) {
+        st_elem(e.v, v[0]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < P; k += 2) round_two(e.v + k, v[k], v[k + 1]);
+    }
+    store_part<P>(row, e, 0, L);
+}
+
 // 16 bytes of a row or of a dense tensor.
 template <typename T> struct Pack;
 template <> struct Pack<float> {
@@ -128,35 +197,22 @@ __device__ __forceinline__ void store_pack_streaming(bf16_t *p, const float (&v)
                                 reinterpret_cast<uintx4_any *>(p));
 }
 
-// The eight elements at position t of a row of L >= 8, as far as the row goes (zeros behind it): where it ends among them, the row's
-// last eight, moved down.
-__device__ __forceinline__ Eight<float> load_row8(const float *row, int t, int L)
+// Eight elements of a row of L >= 8 around position t: where it has fewer from there on, its last eight, which move_down() puts right.
+// (Loads that ask first would make a wave wait for each before the next.)
+template <typename T> __device__ __forceinline__ Eight<T> load_row8(const T *row, int t, int L) { return load8(row + (t < L - 8 ? t : L - 8), 8); }
+// The eight elements `by` places on, zeros behind the last (0 < by < 8).
+__device__ __forceinline__ void move_down(Eight<float> &e, int by)
 {
-    Eight<float> e{};
-    if (t + 8 <= L) return load8(row + t, 8);
-    if (t < L) {
-        e = load8(row + (L - 8), 8);
-        const int by = t - (L - 8);
-        if (by & 4) e.lo = e.hi, e.hi = floatx4_any{};
-        if (by & 2) e.lo = floatx4_any{e.lo[2], e.lo[3], e.hi[0], e.hi[1]}, e.hi = floatx4_any{e.hi[2], e.hi[3], 0.0f, 0.0f};
-        if (by & 1) e.lo = floatx4_any{e.lo[1], e.lo[2], e.lo[3], e.hi[0]}, e.hi = floatx4_any{e.hi[1], e.hi[2], e.hi[3], 0.0f};
-    }
-    return e;
+    if (by & 4) e.lo = e.hi, e.hi = floatx4_any{};
+    if (by & 2) e.lo = floatx4_any{e.lo[2], e.lo[3], e.hi[0], e.hi[1]}, e.hi = floatx4_any{e.hi[2], e.hi[3], 0.0f, 0.0f};
+    if (by & 1) e.lo = floatx4_any{e.lo[1], e.lo[2], e.lo[3], e.hi[0]}, e.hi = floatx4_any{e.hi[1], e.hi[2], e.hi[3], 0.0f};
 }
-__device__ __forceinline__ Eight<bf16_t> load_row8(const bf16_t *row, int t, int L)
+__device__ __forceinline__ void move_down(Eight<bf16_t> &e, int by)
 {
-    Eight<bf16_t> e{};
-    if (t + 8 <= L) return load8(row + t, 8);
-    if (t < L) {
-        e = load8(row + (L - 8), 8);
-        const int by = t - (L - 8);
-        if (by & 4) e.w = uintx4_any{e.w[2], e.w[3], 0u, 0u};
-        if (by & 2) e.w = uintx4_any{e.w[1], e.w[2], e.w[3], 0u};
-        if (by & 1)
-            e.w = uintx4_any{__funnelshift_r(e.w[0], e.w[1], 16), __funnelshift_r(e.w[1], e.w[2], 16), __funnelshift_r(e.w[2], e.w[3], 16),
-                             e.w[3] >> 16};
-    }
-    return e;
+    if (by & 4) e.w = uintx4_any{e.w[2], e.w[3], 0u, 0u};
+    if (by & 2) e.w = uintx4_any{e.w[1], e.w[2], e.w[3], 0u};
+    if (by & 1)
+        e.w = uintx4_any{__funnelshift_r(e.w[0], e.w[1], 16), __funnelshift_r(e.w[1], e.w[2], 16), __funnelshift_r(e.w[2], e.w[3], 16), e.w[3] >> 16};
 }
 // Eight outputs at position t, as far as the row goes: the rest of a row as four, two and one.
 __device__ __forceinline__ void store_row8(float *row, const float (&v)[8], int t, int L)

@@ -89,24 +89,30 @@ size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 size_t span_bytes(const ScanPlan &s, int B, int C) { return s.segs > 1 ? up16((size_t)B * C * s.segs * sizeof(Span)) : 0; }
 size_t part_bytes(const ScanPlan &s, int C) { return up16((size_t)s.M * C * sizeof(float)); }
 constexpr long long kMaxBlocks = 1 << 20;
+template <int W> unsigned scan_grid(long long units) { return (unsigned)std::min(ceil_div(units, scan_rows(W)), kMaxBlocks); }
 
 template <typename T, int W> void launch_fwd(const ScanFwd<T> &p, const ScanPlan &s, hipStream_t st)
 {
     const long long rows = (long long)p.B * p.C;
     if constexpr (W <= 8)               // (plan_scan: more waves only for whole rows)
-        if (s.segs > 1) scan_fwd_kernel<T, W, true><<<(unsigned)std::min(rows * (s.segs - 1), kMaxBlocks), 64 * W, 0, st>>>(p);
-    scan_fwd_kernel<T, W, false><<<(unsigned)std::min(rows * s.segs, kMaxBlocks), 64 * W, 0, st>>>(p);
+        if (s.segs > 1) scan_fwd_kernel<T, W, true><<<scan_grid<W>(rows * (s.segs - 1)), 64 * W * scan_rows(W), 0, st>>>(p);
+    scan_fwd_kernel<T, W, false><<<scan_grid<W>(rows * s.segs), 64 * W * scan_rows(W), 0, st>>>(p);
 }
 template <typename T> void launch_fwd(const ScanFwd<T> &p, const ScanPlan &s, hipStream_t st)
 {
     const dim3 grid(s.gx, s.gy);
     switch (s.G) {
-    case 1: scan_fwd_short_kernel<T, 1><<<grid, 256, 0, st>>>(p, s.m); return;
-    case 2: scan_fwd_short_kernel<T, 2><<<grid, 256, 0, st>>>(p, s.m); return;
-    case 4: scan_fwd_short_kernel<T, 4><<<grid, 256, 0, st>>>(p, s.m); return;
-    case 8: scan_fwd_short_kernel<T, 8><<<grid, 256, 0, st>>>(p, s.m); return;
-    case 16: scan_fwd_short_kernel<T, 16><<<grid, 256, 0, st>>>(p, s.m); return;
-    case 32: scan_fwd_short_kernel<T, 32><<<grid, 256, 0, st>>>(p, s.m); return;
+    case 1:
+        if (p.L == 1) scan_fwd_short_kernel<T, 1, 1><<<grid, 256, 0, st>>>(p, s.m);
+        else if (p.L == 2) scan_fwd_short_kernel<T, 1, 2><<<grid, 256, 0, st>>>(p, s.m);
+        else if (p.L <= 4) scan_fwd_short_kernel<T, 1, 4><<<grid, 256, 0, st>>>(p, s.m);
+        else scan_fwd_short_kernel<T, 1, 8><<<grid, 256, 0, st>>>(p, s.m);
+        return;
+    case 2: scan_fwd_short_kernel<T, 2, 8><<<grid, 256, 0, st>>>(p, s.m); return;
+    case 4: scan_fwd_short_kernel<T, 4, 8><<<grid, 256, 0, st>>>(p, s.m); return;
+    case 8: scan_fwd_short_kernel<T, 8, 8><<<grid, 256, 0, st>>>(p, s.m); return;
+    case 16: scan_fwd_short_kernel<T, 16, 8><<<grid, 256, 0, st>>>(p, s.m); return;
+    case 32: scan_fwd_short_kernel<T, 32, 8><<<grid, 256, 0, st>>>(p, s.m); return;
     }
     switch (s.W) {
     case 1: return launch_fwd<T, 1>(p, s, st);
@@ -120,8 +126,8 @@ template <typename T> void launch_fwd(const ScanFwd<T> &p, const ScanPlan &s, hi
 template <typename T, int W> void launch_bwd(const ScanBwd<T> &p, const ScanPlan &s, hipStream_t st)
 {
     const long long rows = (long long)p.B * p.C;
-    if (s.segs > 1) scan_bwd_kernel<T, W, true><<<(unsigned)std::min(rows * (s.segs - 1), kMaxBlocks), 64 * W, 0, st>>>(p);
-    scan_bwd_kernel<T, W, false><<<(unsigned)std::min(rows * s.segs, kMaxBlocks), 64 * W, 0, st>>>(p);
+    if (s.segs > 1) scan_bwd_kernel<T, W, true><<<scan_grid<W>(rows * (s.segs - 1)), 64 * W * scan_rows(W), 0, st>>>(p);
+    scan_bwd_kernel<T, W, false><<<scan_grid<W>(rows * s.segs), 64 * W * scan_rows(W), 0, st>>>(p);
 }
 template <typename T> void launch_bwd(ScanBwd<T> p, const ScanPlan &s, float *dlam, hipStream_t st)
 {
@@ -132,12 +138,17 @@ template <typename T> void launch_bwd(ScanBwd<T> p, const ScanPlan &s, float *dl
         return;
     }
     switch (s.G ? s.G : 64 * s.W) {
-    case 1: scan_bwd_short_kernel<T, 1><<<grid, 256, 0, st>>>(p, s.m); break;
-    case 2: scan_bwd_short_kernel<T, 2><<<grid, 256, 0, st>>>(p, s.m); break;
-    case 4: scan_bwd_short_kernel<T, 4><<<grid, 256, 0, st>>>(p, s.m); break;
-    case 8: scan_bwd_short_kernel<T, 8><<<grid, 256, 0, st>>>(p, s.m); break;
-    case 16: scan_bwd_short_kernel<T, 16><<<grid, 256, 0, st>>>(p, s.m); break;
-    case 32: scan_bwd_short_kernel<T, 32><<<grid, 256, 0, st>>>(p, s.m); break;
+    case 1:
+        if (p.L == 1) scan_bwd_short_kernel<T, 1, 1><<<grid, 256, 0, st>>>(p, s.m);
+        else if (p.L == 2) scan_bwd_short_kernel<T, 1, 2><<<grid, 256, 0, st>>>(p, s.m);
+        else if (p.L <= 4) scan_bwd_short_kernel<T, 1, 4><<<grid, 256, 0, st>>>(p, s.m);
+        else scan_bwd_short_kernel<T, 1, 8><<<grid, 256, 0, st>>>(p, s.m);
+        break;
+    case 2: scan_bwd_short_kernel<T, 2, 8><<<grid, 256, 0, st>>>(p, s.m); break;
+    case 4: scan_bwd_short_kernel<T, 4, 8><<<grid, 256, 0, st>>>(p, s.m); break;
+    case 8: scan_bwd_short_kernel<T, 8, 8><<<grid, 256, 0, st>>>(p, s.m); break;
+    case 16: scan_bwd_short_kernel<T, 16, 8><<<grid, 256, 0, st>>>(p, s.m); break;
+    case 32: scan_bwd_short_kernel<T, 32, 8><<<grid, 256, 0, st>>>(p, s.m); break;
     case 64: launch_bwd<T, 1>(p, s, st); break;
     case 128: launch_bwd<T, 2>(p, s, st); break;
     case 256: launch_bwd<T, 4>(p, s, st); break;

@@ -11,6 +11,12 @@
 // The backward recurrence v[t] = a[t] (dy[t] + v[t+1]), g[t] = dy[t] + v[t+1], is the same scan from the other end; the h[t-1] that
 // the gates' gradients need is formed again from x, r, i and the state in front of each chunk, which the forward pass keeps (one
 // fp32 for 512 positions): nothing of it is rounded to the storage type, and the kernel reads four tensors instead of five.
+//
+// Memory bounds the fp32 forms (B32 C256 L4096 forward 94 us, 5.7 TB/s; backward 177 us, 5.3 TB/s) and, with the instructions of
+// the gates nearly as long, the bf16 ones (B128 C768 L1024 forward 157 to 175 us, backward 285 to 307 us, 4.6 to 4.9 TB/s).  Rows of any
+// length: those that end inside a lane's eight load their last eight and move them (B287 C480 L511 bf16 backward 282 us, 425 with
+// loads that ask where the row ends), and neighbouring rows go to one die, whose cache puts the lines together that they share
+// (L504 260 us, 356 with rows dealt out in turn).
 #pragma once
 #include "dwconv_block_common.hip.h"
 
@@ -57,66 +63,71 @@ __device__ __forceinline__ float decay_rate(float rate, float lam)
     return rho > 1e30f ? 1e30f : rho;
 }
 
-// a and u of eight positions; positions from `left` on leave the state alone.  NEAR: q < 1/2 whatever the gate is.
-template <bool NEAR, typename T>
-__device__ __forceinline__ void gates(const Eight<T> &x, const Eight<T> &r, const Eight<T> &i, float rho, int left, float (&a)[8], float (&u)[8])
+// a and u of P positions; positions from `left` on leave the state alone.  NEAR: q < 1/2 whatever the gate is.
+template <bool NEAR, typename V, int P>
+__device__ __forceinline__ void gates(const V &x, const V &r, const V &i, float rho, int left, float (&a)[P], float (&u)[P])
 {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < P; ++k) {
         float E;
         a[k] = decay<NEAR>(rho * sigmoid(r[k]), E);
         u[k] = __builtin_amdgcn_sqrtf(-E * (2.0f + E)) * sigmoid(i[k]) * x[k];
     }
-    if (left < 8) {
+    if (left < P) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < P; ++k)
             if (k >= left) a[k] = 1.0f, u[k] = 0.0f;
     }
 }
-template <typename T>
-__device__ __forceinline__ void gates(const Eight<T> &x, const Eight<T> &r, const Eight<T> &i, float rho, int left, float (&a)[8], float (&u)[8])
+template <typename V, int P>
+__device__ __forceinline__ void gates(const V &x, const V &r, const V &i, float rho, int left, float (&a)[P], float (&u)[P])
 {
     if (rho < 0.5f) gates<true>(x, r, i, rho, left, a, u);
     else gates<false>(x, r, i, rho, left, a, u);
 }
-__device__ __forceinline__ Span span_of(const float (&a)[8], const float (&u)[8])
+template <int P> __device__ __forceinline__ Span span_of(const float (&a)[P], const float (&u)[P])
 {
     Span s{a[0], u[0]};
 #pragma unroll
-    for (int k = 1; k < 8; ++k) s = Span{s.A * a[k], fmaf(a[k], s.H, u[k])};
+    for (int k = 1; k < P; ++k) s = Span{s.A * a[k], fmaf(a[k], s.H, u[k])};
     return s;
 }
 
-// Rows that one lane holds may be shorter than its eight positions.
-template <bool SHORT, typename T> __device__ __forceinline__ Eight<T> load_eight(const T *row, int t, int L)
+// What a lane takes of a row at position t, and puts there: eight positions, or ALL of a row of at most P.
+template <int P, bool ALL, typename T> __device__ __forceinline__ auto load_lane(const T *row, int t, int L)
 {
-    if constexpr (SHORT) return load8(row + t, L - t);
+    if constexpr (ALL) return load_few<P>(row, L);
     else return load_row8(row, t, L);
 }
-template <bool SHORT, typename T> __device__ __forceinline__ void store_eight(T *row, const float (&v)[8], int t, int L)
+template <bool ALL, typename T, int P> __device__ __forceinline__ void store_lane(T *row, const float (&v)[P], int t, int L)
 {
-    if constexpr (SHORT) store8(row + t, v, L - t);
+    if constexpr (ALL) store_few<P>(row, v, L);
     else store_row8(row, v, t, L);
+}
+// Puts right what load_row8 has loaded at the end of a row.
+template <typename... E> __device__ __forceinline__ void at_end(int t, int L, E &...e)
+{
+    const int by = t - (L - 8);
+    if (by > 0 && by < 8) (move_down(e, by), ...);
 }
 
 // d softplus(lam) / softplus(lam): the sum of dq q is dlam through it.  (It tends to 1 as lam falls, where both are exp(lam) and at last 0.)
 __device__ __forceinline__ float dlam_factor(float lam) { return lam < -15.0f ? 1.0f : 1.0f / (1.0f + expf(-lam)) / softplus(lam); }
 
-// What the backward pass keeps of eight positions.
-struct GateGrads {
-    float a[8];         // decay
-    float in[8];        // dx = g in
-    float gi[8];        // di = g gi
-    float e[8];         // dq q = g e
-    float rest[8];      // dr = dq q rest
+// What the backward pass keeps of P positions.
+template <int P> struct GateGrads {
+    float a[P];         // decay
+    float in[P];        // dx = g in
+    float gi[P];        // di = g gi
+    float e[P];         // dq q = g e
+    float rest[P];      // dr = dq q rest
 };
 // First half: everything but e, of which it leaves q a in e and a / (1 - a^2) u in gi's place until the states are known.
-template <bool NEAR, typename T>
-__device__ __forceinline__ void grads_begin(const Eight<T> &x, const Eight<T> &r, const Eight<T> &i, float rho, int left, GateGrads &w,
-                                            float (&u)[8], float (&pull)[8])
+template <bool NEAR, typename V, int P>
+__device__ __forceinline__ void grads_begin(const V &x, const V &r, const V &i, float rho, int left, GateGrads<P> &w, float (&u)[P], float (&pull)[P])
 {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < P; ++k) {
         float rest_i, E;
         const float q = rho * sigmoid_both(r[k], w.rest[k]), si = sigmoid_both(i[k], rest_i);
         w.a[k] = decay<NEAR>(q, E);
@@ -129,64 +140,63 @@ __device__ __forceinline__ void grads_begin(const Eight<T> &x, const Eight<T> &r
         pull[k] = w.a[k] * (over * x[k]);
         w.e[k] = q * w.a[k];
     }
-    if (left < 8) {
+    if (left < P) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < P; ++k)
             if (k >= left) w.a[k] = 1.0f, w.in[k] = w.gi[k] = w.e[k] = w.rest[k] = u[k] = pull[k] = 0.0f;
     }
 }
-template <typename T>
-__device__ __forceinline__ void grads_begin(const Eight<T> &x, const Eight<T> &r, const Eight<T> &i, float rho, int left, GateGrads &w,
-                                            float (&u)[8], float (&pull)[8])
+template <typename V, int P>
+__device__ __forceinline__ void grads_begin(const V &x, const V &r, const V &i, float rho, int left, GateGrads<P> &w, float (&u)[P], float (&pull)[P])
 {
     if (rho < 0.5f) grads_begin<true>(x, r, i, rho, left, w, u, pull);
     else grads_begin<false>(x, r, i, rho, left, w, u, pull);
 }
-// Second half, h: the state in front of the eight positions.
-__device__ __forceinline__ void grads_end(GateGrads &w, const float (&u)[8], const float (&pull)[8], float h)
+// Second half, h: the state in front of the positions.
+template <int P> __device__ __forceinline__ void grads_end(GateGrads<P> &w, const float (&u)[P], const float (&pull)[P], float h)
 {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < P; ++k) {
         w.e[k] *= pull[k] - h;
         h = fmaf(w.a[k], h, u[k]);
     }
 }
-// The span of v over eight positions, from the last to the first.
-__device__ __forceinline__ Span back_span(const float (&a)[8], const float (&dy)[8])
+// The span of v over the positions, from the last to the first.
+template <int P> __device__ __forceinline__ Span back_span(const float (&a)[P], const float (&dy)[P])
 {
-    Span s{a[7], a[7] * dy[7]};
+    Span s{a[P - 1], a[P - 1] * dy[P - 1]};
 #pragma unroll
-    for (int k = 6; k >= 0; --k) s = Span{s.A * a[k], a[k] * (dy[k] + s.H)};
+    for (int k = P - 2; k >= 0; --k) s = Span{s.A * a[k], a[k] * (dy[k] + s.H)};
     return s;
 }
-// Gradients of eight positions from v behind them, 0 from `left` on; returns their sum of dq q.
-template <bool SHORT = false, typename T>
-__device__ __forceinline__ float grads_store(const GateGrads &w, const float (&dy)[8], float v, T *dx, T *dr, T *di, int left, int t, int L)
+// Gradients of the positions from v behind them, 0 from `left` on; returns their sum of dq q.
+template <bool ALL = false, int P, typename T>
+__device__ __forceinline__ float grads_store(const GateGrads<P> &w, const float (&dy)[P], float v, T *dx, T *dr, T *di, int left, int t, int L)
 {
-    float g[8], out[8], sum = 0.0f;
+    float g[P], out[P], sum = 0.0f;
 #pragma unroll
-    for (int k = 7; k >= 0; --k) {
+    for (int k = P - 1; k >= 0; --k) {
         g[k] = dy[k] + v;
         v = w.a[k] * g[k];
     }
-    if (left < 8) {
+    if (left < P) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < P; ++k)
             if (k >= left) g[k] = 0.0f;
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) out[k] = g[k] * w.in[k];
-    store_eight<SHORT>(dx, out, t, L);
+    for (int k = 0; k < P; ++k) out[k] = g[k] * w.in[k];
+    store_lane<ALL>(dx, out, t, L);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) out[k] = g[k] * w.gi[k];
-    store_eight<SHORT>(di, out, t, L);
+    for (int k = 0; k < P; ++k) out[k] = g[k] * w.gi[k];
+    store_lane<ALL>(di, out, t, L);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < P; ++k) {
         const float d = g[k] * w.e[k];
         sum += d;
         out[k] = d * w.rest[k];
     }
-    store_eight<SHORT>(dr, out, t, L);
+    store_lane<ALL>(dr, out, t, L);
     return sum;
 }
 
@@ -198,15 +208,29 @@ __device__ __forceinline__ float through_segments(const Span *spans, int count, 
     return fmaf(lane_value(all.A, 63), h, lane_value(all.H, 63));
 }
 
-// SPANS: only the spans of the segments but the last.
-template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) void scan_fwd_kernel(ScanFwd<T> p)
+// Rows (or segments) of a workgroup: four where a wave has one to itself, or starting workgroups is what short ones cost.
+constexpr int scan_rows(int W) { return W == 1 ? 4 : 1; }
+
+// Workgroups go to the eight dies in turn.  Rows of any length share cache lines with their neighbours, so runs of sixteen workgroups'
+// work go to one die (the last, incomplete round of runs as it comes), short enough for unequal lengths to even out.
+__device__ __forceinline__ unsigned die_runs(unsigned i, unsigned n)
 {
+    return i < (n & ~127u) ? (i & ~127u) | (i & 7u) << 4 | ((i >> 3) & 15u) : i;
+}
+
+// SPANS: only the spans of the segments but the last.
+template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W * scan_rows(W)) void scan_fwd_kernel(ScanFwd<T> p)
+{
+    constexpr int R = scan_rows(W);
     __shared__ Span totals[2][W];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = R > 1 ? 0 : threadIdx.x >> 6, mine = R > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     const int segs = SPANS ? p.segs - 1 : p.segs;
     const unsigned units = (unsigned)(p.B * p.C) * (unsigned)segs;         // (below 2^32: cut are only calls of few rows)
+    const unsigned blocks = (units + R - 1) / R;
     int side = 0;
-    for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    for (unsigned block = blockIdx.x; block < blocks; block += gridDim.x) {
+        const unsigned unit = die_runs(block, blocks) * R + mine;
+        if (R > 1 && unit >= units) continue;
         const int row = (int)(segs == 1 ? unit : unit / (unsigned)segs), seg = (int)(unit - (unsigned)row * (unsigned)segs);
         const int b = (int)((unsigned)row / (unsigned)p.C), c = row - b * p.C;
         const int n = row_length(p.lengths, b, p.L);
@@ -230,6 +254,7 @@ template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) vo
                 continue;
             }
             float a[8], u[8];
+            at_end(t, p.L, xn, rn, in);
             gates(xn, rn, in, rho, n - t, a, u);
             const int tn = t + group;
             if (tg + group < t1) xn = load_row8(x, tn, p.L), rn = load_row8(r, tn, p.L), in = load_row8(i, tn, p.L);
@@ -268,7 +293,7 @@ template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) vo
             }
             store_row8(y, out, t, p.L);
         }
-        if (threadIdx.x == 0) {
+        if (lane == 0 && wave == 0) {
             if (SPANS) p.spans[(long long)row * p.segs + seg] = all;
             else if (p.h_last && t1 == p.L) p.h_last[row] = carry;
         }
@@ -277,15 +302,21 @@ template <typename T, int W, bool SPANS> __global__ __launch_bounds__(64 * W) vo
 
 // SPANS: only the spans of v over the segments but the first.  BATCH > 0 (W = 1): a workgroup has the rows of a channel, a wave for each
 // of at most BATCH batch entries, and writes dlam itself.
-template <typename T, int W, bool SPANS, int BATCH = 0> __global__ __launch_bounds__(64 * (BATCH ? BATCH : W)) void scan_bwd_kernel(ScanBwd<T> p)
+template <typename T, int W, bool SPANS, int BATCH = 0>
+__global__ __launch_bounds__(64 * (BATCH ? BATCH : W * scan_rows(W))) void scan_bwd_kernel(ScanBwd<T> p)
 {
+    constexpr int R = BATCH ? 1 : scan_rows(W);
     __shared__ Span totals[2][W];
     __shared__ float sums[BATCH ? BATCH : W];
-    const int lane = threadIdx.x & 63, wave = BATCH ? 0 : threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = BATCH || R > 1 ? 0 : threadIdx.x >> 6;
+    const int mine = R > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     const int segs = SPANS ? p.segs - 1 : p.segs;
     const unsigned units = BATCH ? (unsigned)p.C : (unsigned)(p.B * p.C) * (unsigned)segs;
+    const unsigned blocks = (units + R - 1) / R;
     int side = 0;
-    for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    for (unsigned block = blockIdx.x; block < blocks; block += gridDim.x) {
+        const unsigned unit = die_runs(block, blocks) * R + mine;
+        if (R > 1 && unit >= units) continue;
         const int row = BATCH ? (int)(threadIdx.x >> 6) * p.C + (int)unit : (int)(segs == 1 ? unit : unit / (unsigned)segs);
         const int seg = BATCH ? 0 : (int)(unit - (unsigned)row * (unsigned)segs) + (SPANS ? 1 : 0);
         const int b = (int)((unsigned)row / (unsigned)p.C), c = row - b * p.C;
@@ -324,8 +355,10 @@ template <typename T, int W, bool SPANS, int BATCH = 0> __global__ __launch_boun
                 }
                 continue;
             }
-            GateGrads w;
+            GateGrads<8> w;
             float d[8];
+            if constexpr (SPANS) at_end(t, p.L, dn, rn);
+            else at_end(t, p.L, dn, rn, xn, in);
 #pragma unroll
             for (int k = 0; k < 8; ++k) d[k] = dn[k];
             if (n - t < 8) {
@@ -384,9 +417,9 @@ template <typename T, int W, bool SPANS, int BATCH = 0> __global__ __launch_boun
             sum += grads_store(w, d, v, dx, dr, di, n - t, t, p.L);
         }
         if (SPANS) {
-            if (threadIdx.x == 0) p.spans[(long long)row * p.segs + seg] = all;
+            if (lane == 0 && wave == 0) p.spans[(long long)row * p.segs + seg] = all;
         } else {
-            if ((BATCH ? lane : (int)threadIdx.x) == 0 && p.dh0 && seg == 0) p.dh0[row] = carry;
+            if (lane == 0 && wave == 0 && p.dh0 && seg == 0) p.dh0[row] = carry;
             sum = group_sum<64>(sum);
             if constexpr (W > 1 || BATCH > 0) {
                 if (lane == 0) sums[threadIdx.x >> 6] = sum;
@@ -399,18 +432,20 @@ template <typename T, int W, bool SPANS, int BATCH = 0> __global__ __launch_boun
             }
             if constexpr (BATCH > 0) {
                 if (threadIdx.x == 0) p.dlam[c] = sum * dlam_factor(p.lam[c]);
-            } else if (threadIdx.x == 0) p.part[((long long)b * p.segs + seg) * p.C + c] = sum;
+            } else if (lane == 0 && wave == 0) p.part[((long long)b * p.segs + seg) * p.C + c] = sum;
         }
     }
 }
 
-// Rows of at most 8 G positions: groups of G lanes.  The rows of a workgroup are `cb` channels of `nb` batch entries at a time, its
+// Rows of at most 8 G positions: groups of G lanes, or a lane with P positions (B100000 C96 L1 bf16 forward 68 us, 149 us as a lane with
+// eight positions of which one is there; L4 forward 90 and 194 us, backward 163 and 338).  The rows of a workgroup are `cb` channels of `nb` batch entries at a time, its
 // lanes keep their channel; blockIdx.y and steps of gridDim.y walk the batch.
 struct ShortRows {
     int cb, nb;
 };
-template <typename T, int G> __global__ __launch_bounds__(256) void scan_fwd_short_kernel(ScanFwd<T> p, ShortRows m)
+template <typename T, int G, int P> __global__ __launch_bounds__(256) void scan_fwd_short_kernel(ScanFwd<T> p, ShortRows m)
 {
+    constexpr bool ALL = G == 1;
     const int lane = threadIdx.x & 63, g = threadIdx.x / G, t = (threadIdx.x & (G - 1)) * 8;
     const int sub = g / m.cb, c = blockIdx.x * m.cb + (g - sub * m.cb);
     const bool idle = sub >= m.nb || c >= p.C;
@@ -419,29 +454,31 @@ template <typename T, int G> __global__ __launch_bounds__(256) void scan_fwd_sho
         const bool off = idle || b0 + sub >= p.B;
         const int bc = off ? 0 : (int)(b0 + sub), cc = off ? 0 : c, n = off ? 0 : row_length(p.lengths, bc, p.L), left = n - t;
         const long long row = (long long)bc * p.C + cc;
-        const Eight<T> x = load_eight<G == 1>(p.x.row(bc, cc, p.L), t, off ? 0 : p.L), r = load_eight<G == 1>(p.r.row(bc, cc, p.L), t, off ? 0 : p.L),
-                       i = load_eight<G == 1>(p.i.row(bc, cc, p.L), t, off ? 0 : p.L);
+        auto x = load_lane<P, ALL>(p.x.row(bc, cc, p.L), t, p.L), r = load_lane<P, ALL>(p.r.row(bc, cc, p.L), t, p.L),
+             i = load_lane<P, ALL>(p.i.row(bc, cc, p.L), t, p.L);
         const float h0 = p.h0 && !off ? p.h0[row] : 0.0f;
-        float a[8], u[8], out[8];
+        float a[P], u[P], out[P];
+        if constexpr (!ALL) at_end(t, p.L, x, r, i);
         gates<false>(x, r, i, rho, left, a, u);
         const Span s = scan_up<G>(span_of(a, u), lane);
         const float end = fmaf(s.A, h0, s.H);
         float h = from_lane_before(h0, end);
         if ((lane & (G - 1)) == 0) h = h0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < P; ++k) {
             h = fmaf(a[k], h, u[k]);
             out[k] = k < left ? h : 0.0f;
         }
         if (off) continue;                      // (the moves between lanes are done)
-        store_eight<G == 1>(p.y.row(bc, cc, p.L), out, t, p.L);
+        store_lane<ALL>(p.y.row(bc, cc, p.L), out, t, p.L);
         if (t == 0 && p.states) p.states[row] = h0;
         if ((lane & (G - 1)) == G - 1 && p.h_last) p.h_last[row] = end;
     }
 }
 
-template <typename T, int G> __global__ __launch_bounds__(256) void scan_bwd_short_kernel(ScanBwd<T> p, ShortRows m)
+template <typename T, int G, int P> __global__ __launch_bounds__(256) void scan_bwd_short_kernel(ScanBwd<T> p, ShortRows m)
 {
+    constexpr bool ALL = G == 1;
     const int lane = threadIdx.x & 63, g = threadIdx.x / G, t = (threadIdx.x & (G - 1)) * 8;
     const int sub = g / m.cb, c = blockIdx.x * m.cb + (g - sub * m.cb);
     const bool idle = sub >= m.nb || c >= p.C;
@@ -451,14 +488,15 @@ template <typename T, int G> __global__ __launch_bounds__(256) void scan_bwd_sho
         const bool off = idle || b0 + sub >= p.B;
         const int bc = off ? 0 : (int)(b0 + sub), cc = off ? 0 : c, n = off ? 0 : row_length(p.lengths, bc, p.L), left = n - t;
         const long long row = (long long)bc * p.C + cc;
-        const Eight<T> dyr = load_eight<G == 1>(p.dy.row(bc, cc, p.L), t, off ? 0 : p.L), x = load_eight<G == 1>(p.x.row(bc, cc, p.L), t, off ? 0 : p.L),
-                       r = load_eight<G == 1>(p.r.row(bc, cc, p.L), t, off ? 0 : p.L), i = load_eight<G == 1>(p.i.row(bc, cc, p.L), t, off ? 0 : p.L);
+        auto dyr = load_lane<P, ALL>(p.dy.row(bc, cc, p.L), t, p.L), x = load_lane<P, ALL>(p.x.row(bc, cc, p.L), t, p.L),
+             r = load_lane<P, ALL>(p.r.row(bc, cc, p.L), t, p.L), i = load_lane<P, ALL>(p.i.row(bc, cc, p.L), t, p.L);
         const float h0 = off ? 0.0f : p.states[row], dh = p.dh_last && !off ? p.dh_last[row] : 0.0f;
-        GateGrads w;
-        float u[8], pull[8], d[8];
+        GateGrads<P> w;
+        float u[P], pull[P], d[P];
+        if constexpr (!ALL) at_end(t, p.L, dyr, x, r, i);
         grads_begin<false>(x, r, i, rho, left, w, u, pull);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) d[k] = k < left ? dyr[k] : 0.0f;
+        for (int k = 0; k < P; ++k) d[k] = k < left ? dyr[k] : 0.0f;
         const Span s = scan_up<G>(span_of(w.a, u), lane);
         float h = from_lane_before(h0, fmaf(s.A, h0, s.H));
         if ((lane & (G - 1)) == 0) h = h0;
@@ -473,7 +511,7 @@ template <typename T, int G> __global__ __launch_bounds__(256) void scan_bwd_sho
         float v = from_lane_behind(dh, front);
         if ((lane & (G - 1)) == G - 1) v = dh;
         if (off) continue;
-        sum += grads_store<G == 1>(w, d, v, p.dx.row(bc, cc, p.L), p.dr.row(bc, cc, p.L), p.di.row(bc, cc, p.L), left, t, p.L);
+        sum += grads_store<ALL>(w, d, v, p.dx.row(bc, cc, p.L), p.dr.row(bc, cc, p.L), p.di.row(bc, cc, p.L), left, t, p.L);
         if (t == 0 && p.dh0) p.dh0[row] = front;
     }
     sum = group_sum<G>(sum);
