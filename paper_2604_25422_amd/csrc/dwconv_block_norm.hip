@@ -8,7 +8,8 @@ using namespace dwconv;
 namespace {
 
 struct NormPlan {
-    int E, NT, lx;              // tile kernel; E = 0: the streaming one
+    int E, NT, lx;              // tile kernel (NT threads for a tile); E = 0: the streaming one
+    int NB;                     // tiles of a workgroup
     int row_tiles;
     long long tiles;
     int blocks;
@@ -23,6 +24,10 @@ NormPlan plan_norm(int B, int C, int L, int dtype, bool backward)
     // Rows of a tile as long as a cache line (lx = 3) where the registers hold the channels, or else half of one: what a
     // workgroup leaves of a line is fetched by its neighbour, if that is at work at the same time.  A wave's share E of the channels
     // goes with what a larger workgroup costs.
+    // Tiles of short rows go to a wave or two, several to a workgroup, whose sums wait for fewer (or for lanes without a channel):
+    // B20000 C130 L12 bf16 forward 245 us as 256 threads, 126 us as 128, 84 us as a wave; backward 224, 177 and 185 us; B10000 C384 L12
+    // fp32 backward 360 us as 512 threads, 330 us as 128.  On whole lines that is so of few channels only (B4000 C32 L128 bf16 forward
+    // 48 us as 256 threads with a pack each, 38 us as 128 with two; backward 61 us, 65 us as a wave with four).
     // Forward: B128 C768 L1024 bf16 220 us as 512 threads and half lines, 242 us as 1024 threads and whole ones (336 us with a quarter
     // of a line); B64 C768 L1024 fp32 233 and 206 us.
     // Backward, fp32: B64 C384 L1024 171 us as 512 threads and whole lines, 178 us as 1024, 192 us with half lines; B16384 C128 L48
@@ -38,19 +43,24 @@ NormPlan plan_norm(int B, int C, int L, int dtype, bool backward)
         s.lx = lx;
     };
     for (int lx = 3; lx >= 0; --lx) {
+        take(lx, 64, lx == 3 ? 2 : kMaxE);
         if (!backward) {
+            take(lx, 128, lx == 3 ? 2 : kMaxE);
             take(lx, 256, kMaxE);
             take(lx, 512, kMaxE);
             if (f32 || lx < 3) take(lx, 1024, kMaxE);
         } else if (f32) {
+            if (lx < 3) take(lx, 128, kMaxE);
             take(lx, 256, 2);
             take(lx, 512, lx >= 2 ? kMaxE : 2);
             if (lx < 2) take(lx, 1024, 3);
         } else {
+            if (lx < 3) take(lx, 128, 5);
             take(lx, 256, lx == 3 ? kMaxE : 3);
             if (lx < 3) take(lx, 512, kMaxE);
         }
     }
+    s.NB = s.E && s.NT < 256 ? 256 / s.NT : 1;
     if (s.E) s.row_tiles = (int)ceil_div(L, V << s.lx);
     // (a grid has fewer than 2^32 threads: more tiles than that, each of a few elements then, go to the kernel that walks them)
     if (s.E && (long long)B * s.row_tiles >= 1ll << 22) s.E = s.lx = 0;
@@ -62,22 +72,34 @@ NormPlan plan_norm(int B, int C, int L, int dtype, bool backward)
     s.tiles = (long long)B * s.row_tiles;
     // (a workgroup per tile, in order: workgroups that walk several drift apart, and with them the halves of a line.  B128 C768 L1024
     // bf16 backward, of an earlier form of the kernel: 431 us, 512 us with two tiles each)
-    s.blocks = s.E ? (int)s.tiles : (int)std::min<long long>(s.tiles, backward ? 1024 : 1 << 20);
+    s.blocks = s.E ? (int)ceil_div(s.tiles, s.NB) : (int)std::min<long long>(s.tiles, backward ? 1024 : 1 << 20);
     return s;
 }
 size_t red_bytes(const NormPlan &s, int V, int sums) { return (size_t)(s.NT / 16 + 1) * sums * (V << s.lx) * sizeof(float); }
 
-// Runs that the workgroups' sums are first added up in (4096 sums of 768 channels twice: 18 us by norm_sums_kernel alone); 0: not worth it.
-int sum_runs(const NormPlan &s) { return s.blocks >= 512 ? 64 : 0; }
+// Rows of sums: one a tile, or a workgroup of the streaming kernel.
+int sum_rows(const NormPlan &s) { return s.E ? (int)s.tiles : s.blocks; }
+// Runs that they are first added up in (4096 sums of 768 channels twice: 18 us by norm_sums_kernel alone); 0: not worth it.
+int sum_runs(const NormPlan &s) { return sum_rows(s) >= 65536 ? 512 : sum_rows(s) >= 512 ? 64 : 0; }
 
 template <typename T, int E, bool BLOCK> void fwd_tile(const NormFwd<T> &p, const NormPlan &s, hipStream_t st)
 {
-    const size_t lds = red_bytes(s, Pack<T>::V, 1);
+    const size_t lds = s.NB * red_bytes(s, Pack<T>::V, 1);
     // (what plan_norm takes: larger workgroups only where smaller ones would have too many packs)
-    if constexpr (E <= 3) norm_fwd_tile_kernel<T, E, 256, BLOCK><<<s.blocks, 256, lds, st>>>(p);
-    else if (s.NT == 256) norm_fwd_tile_kernel<T, E, 256, BLOCK><<<s.blocks, 256, lds, st>>>(p);
-    else if (s.NT == 512) norm_fwd_tile_kernel<T, E, 512, BLOCK><<<s.blocks, 512, lds, st>>>(p);
-    else norm_fwd_tile_kernel<T, E, 1024, BLOCK><<<s.blocks, 1024, lds, st>>>(p);
+    switch (s.NT) {
+    case 64: norm_fwd_tile_kernel<T, E, 64, 4, BLOCK><<<s.blocks, 256, lds, st>>>(p); break;
+    case 128:
+        if constexpr (E == 2 || E >= 4) norm_fwd_tile_kernel<T, E, 128, 2, BLOCK><<<s.blocks, 256, lds, st>>>(p);
+        break;
+    case 256:
+        if constexpr (E >= 2) norm_fwd_tile_kernel<T, E, 256, 1, BLOCK><<<s.blocks, 256, lds, st>>>(p);
+        break;
+    case 512:
+        if constexpr (E >= 4) norm_fwd_tile_kernel<T, E, 512, 1, BLOCK><<<s.blocks, 512, lds, st>>>(p);
+        break;
+    default:
+        if constexpr (E >= 4) norm_fwd_tile_kernel<T, E, 1024, 1, BLOCK><<<s.blocks, 1024, lds, st>>>(p);
+    }
 }
 template <typename T, bool BLOCK> void launch_fwd(const NormFwd<T> &p, const NormPlan &s, hipStream_t st)
 {
@@ -102,14 +124,21 @@ template <typename T, bool BLOCK> void launch_fwd(const NormFwd<T> &p, const Nor
 }
 template <typename T, int E, bool BLOCK> void bwd_tile(const NormBwd<T> &p, const NormPlan &s, hipStream_t st)
 {
-    const size_t lds = red_bytes(s, Pack<T>::V, BLOCK ? 4 : 1) + (size_t)E * (2 * (s.NT >> s.lx) + s.NT) * sizeof(float);
+    const size_t lds = s.NB * (red_bytes(s, Pack<T>::V, BLOCK ? 4 : 1) + (size_t)E * (2 * (s.NT >> s.lx) + s.NT) * sizeof(float));
     constexpr bool F32 = sizeof(T) == 4;
-    if (s.NT == 256) {
-        if constexpr (!F32 || E <= 2) norm_bwd_tile_kernel<T, E, 256, BLOCK><<<s.blocks, 256, lds, st>>>(p);
-    } else if (s.NT == 512) {
-        if constexpr (E >= 2) norm_bwd_tile_kernel<T, E, 512, BLOCK><<<s.blocks, 512, lds, st>>>(p);
-    } else if constexpr (F32 && (E == 2 || E == 3)) {
-        norm_bwd_tile_kernel<T, E, 1024, BLOCK><<<s.blocks, 1024, lds, st>>>(p);
+    switch (s.NT) {
+    case 64: norm_bwd_tile_kernel<T, E, 64, 4, BLOCK><<<s.blocks, 256, lds, st>>>(p); break;
+    case 128:
+        if constexpr (E >= 4 && (F32 || E < 6)) norm_bwd_tile_kernel<T, E, 128, 2, BLOCK><<<s.blocks, 256, lds, st>>>(p);
+        break;
+    case 256:
+        if constexpr (!F32 || E <= 2) norm_bwd_tile_kernel<T, E, 256, 1, BLOCK><<<s.blocks, 256, lds, st>>>(p);
+        break;
+    case 512:
+        if constexpr (E >= 2) norm_bwd_tile_kernel<T, E, 512, 1, BLOCK><<<s.blocks, 512, lds, st>>>(p);
+        break;
+    default:
+        if constexpr (F32 && (E == 2 || E == 3)) norm_bwd_tile_kernel<T, E, 1024, 1, BLOCK><<<s.blocks, 1024, lds, st>>>(p);
     }
 }
 template <typename T, bool BLOCK> void launch_bwd(const NormBwd<T> &p, const NormPlan &s, float *dw, float *dw_next, hipStream_t st)
@@ -124,9 +153,9 @@ template <typename T, bool BLOCK> void launch_bwd(const NormBwd<T> &p, const Nor
     default: bwd_tile<T, 6, BLOCK>(p, s, st); break;
     }
     const float *part = p.part;
-    int M = s.blocks;
+    int M = sum_rows(s);
     if (const int runs = sum_runs(s)) {
-        float *to = p.part + (size_t)s.blocks * 2 * p.C;
+        float *to = p.part + (size_t)M * 2 * p.C;
         norm_runs_kernel<<<dim3((unsigned)ceil_div(2ll * p.C, 64), runs), 256, 0, st>>>(part, M, (int)ceil_div(M, runs), 2 * p.C, to);
         part = to;
         M = runs;
@@ -134,7 +163,7 @@ template <typename T, bool BLOCK> void launch_bwd(const NormBwd<T> &p, const Nor
     norm_sums_kernel<<<dim3((unsigned)ceil_div(p.C, 32), 2), 1024, 0, st>>>(part, M, p.C, dw, dw_next);
 }
 
-size_t part_bytes(const NormPlan &s, int C) { return (size_t)(s.blocks + sum_runs(s)) * 2 * C * sizeof(float); }
+size_t part_bytes(const NormPlan &s, int C) { return (size_t)(sum_rows(s) + sum_runs(s)) * 2 * C * sizeof(float); }
 
 template <typename T>
 void run_fwd(const dwconv_seq &y, const dwconv_seq &z, const dwconv_seq &res, const float *w, const float *w_next, const dwconv_seq_out &out,

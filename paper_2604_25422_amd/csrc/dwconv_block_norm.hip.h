@@ -43,10 +43,10 @@ template <typename I> __device__ __forceinline__ I die_run(I i, I n)
 
 // S sums v[s][k] over the channels of the tile, for the positions of this lane: over the lanes of sixteen that stand at the same
 // positions (moves inside a row of lanes, which cost no more than the addition), then over the rows of lanes in LDS, four lanes a
-// position.  red: [NT / 16 + 1][S][V << lx] floats; a row of the tile has at most sixteen lanes.
-template <int S, int V, int NT> __device__ __forceinline__ void channel_sums(float (&v)[S][V], int lx, float *red)
+// position.  red: [NT / 16 + 1][S][V << lx] floats, NT the tile's threads; a row of the tile has at most sixteen lanes.
+template <int S, int V, int NT> __device__ __forceinline__ void channel_sums(float (&v)[S][V], int lx, int tid, float *red)
 {
-    const int x = threadIdx.x & ((1 << lx) - 1), T = V << lx, all = S * T;
+    const int x = tid & ((1 << lx) - 1), T = V << lx, all = S * T;
 #define DWCONV_ADD(CTRL)                                                       \
     _Pragma("unroll") for (int s = 0; s < S; ++s)                              \
         _Pragma("unroll") for (int k = 0; k < V; ++k) v[s][k] += dpp<CTRL>(0.0f, v[s][k]);
@@ -55,15 +55,15 @@ template <int S, int V, int NT> __device__ __forceinline__ void channel_sums(flo
     if (lx < 3) { DWCONV_ADD(0x124) }       // four lanes on, round the sixteen
     if (lx < 4) { DWCONV_ADD(0x128) }       // eight lanes on
 #undef DWCONV_ADD
-    if ((threadIdx.x & 15) < (1 << lx)) {
+    if ((tid & 15) < (1 << lx)) {
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
-            for (int k = 0; k < V; ++k) red[(threadIdx.x >> 4) * all + s * T + x * V + k] = v[s][k];
+            for (int k = 0; k < V; ++k) red[(tid >> 4) * all + s * T + x * V + k] = v[s][k];
     }
     __syncthreads();
     float *sum = red + NT / 16 * all;
-    for (int i = threadIdx.x; i < 4 * all; i += NT) {
+    for (int i = tid; i < 4 * all; i += NT) {
         float s = 0.0f;
 #pragma unroll
         for (int r = 0; r < NT / 64; ++r) s += red[(4 * r + (i & 3)) * all + (i >> 2)];
@@ -78,9 +78,9 @@ template <int S, int V, int NT> __device__ __forceinline__ void channel_sums(flo
         for (int k = 0; k < V; ++k) v[s][k] = sum[s * T + x * V + k];
     // (the next use of `red` writes its first part, which nobody reads any more, and `sum` behind a barrier)
 }
-template <int V, int NT> __device__ __forceinline__ void channel_sums(float (&v)[V], int lx, float *red)
+template <int V, int NT> __device__ __forceinline__ void channel_sums(float (&v)[V], int lx, int tid, float *red)
 {
-    channel_sums<1, V, NT>(reinterpret_cast<float (&)[1][V]>(v), lx, red);
+    channel_sums<1, V, NT>(reinterpret_cast<float (&)[1][V]>(v), lx, tid, red);
 }
 
 // Element k of a pack to be stored; `before` holds element k - 1 where two share a word.
@@ -126,14 +126,18 @@ __device__ __forceinline__ TileAt tile_at(unsigned tile, int row_tiles, int T, i
     return TileAt{b, t - over, over};
 }
 
-template <typename T, int E, int NT, bool BLOCK> __global__ __launch_bounds__(NT) void norm_fwd_tile_kernel(NormFwd<T> p)
+template <typename T, int E, int NT, int NB, bool BLOCK> __global__ __launch_bounds__(NT * NB) void norm_fwd_tile_kernel(NormFwd<T> p)
 {
     constexpr int V = Pack<T>::V;
-    extern __shared__ float red[];
-    const int x = threadIdx.x & ((1 << p.lx) - 1), c0 = threadIdx.x >> p.lx, step = NT >> p.lx;
+    extern __shared__ float shared[];
+    const int sub = NB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0, tid = NB > 1 ? threadIdx.x % NT : threadIdx.x;
+    const int x = tid & ((1 << p.lx) - 1), c0 = tid >> p.lx, step = NT >> p.lx;
+    float *red = shared + sub * ((NT / 16 + 1) * (V << p.lx));
     // a lane's place is the same in every pack and tensor: one offset that is its own, the rest is the workgroup's
     const unsigned mine = ((unsigned)c0 * (unsigned)p.L + (unsigned)(x * V)) * (unsigned)sizeof(T);
-    const TileAt tile = tile_at(die_run<unsigned>(blockIdx.x, (unsigned)p.tiles), p.row_tiles, V << p.lx, p.L);
+    const unsigned at_tile = die_run<unsigned>(blockIdx.x, gridDim.x) * NB + sub;
+    const bool live = NB == 1 || at_tile < (unsigned)p.tiles;
+    const TileAt tile = tile_at(live ? at_tile : 0, p.row_tiles, V << p.lx, p.L);
     const auto at = [&](const auto &s, int e) { return place(s.p + ((long long)tile.b * s.bs + (long long)(e * step) * p.L + tile.t0), mine); };
     // (only the last round of channels can be short)
     const bool in = c0 + (E - 1) * step < p.C;
@@ -167,7 +171,7 @@ template <typename T, int E, int NT, bool BLOCK> __global__ __launch_bounds__(NT
 #pragma unroll
             for (int e = 0; e < E; ++e) r1[k] = fmaf(y[e][k], y[e][k], r1[k]);
         }
-        channel_sums<V, NT>(r1, p.lx, red);
+        channel_sums<V, NT>(r1, p.lx, tid, red);
 #pragma unroll
         for (int k = 0; k < V; ++k) r1[k] = inv_sqrt(r1[k] / (float)p.C + p.eps);
 #pragma unroll
@@ -186,18 +190,18 @@ template <typename T, int E, int NT, bool BLOCK> __global__ __launch_bounds__(NT
             }
             r2[k] = fmaf(o[e][k], o[e][k], r2[k]);
         }
-        if (BLOCK && (e < E - 1 || in)) store_pack(at(p.out, e), o[e]);
+        if (BLOCK && live && (e < E - 1 || in)) store_pack(at(p.out, e), o[e]);
     }
-    channel_sums<V, NT>(r2, p.lx, red);
+    channel_sums<V, NT>(r2, p.lx, tid, red);
 #pragma unroll
     for (int k = 0; k < V; ++k) r2[k] = inv_sqrt(r2[k] / (float)p.C + p.eps);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
 #pragma unroll
         for (int k = 0; k < V; ++k) o[e][k] *= r2[k] * wn[e];
-        if (e < E - 1 || in) store_pack(at(p.n, e), o[e]);
+        if (live && (e < E - 1 || in)) store_pack(at(p.n, e), o[e]);
     }
-    if (p.stats && c0 == 0) {
+    if (p.stats && live && c0 == 0) {
         float *s = p.stats + (long long)tile.b * 2 * p.L + tile.t0 + x * V;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
@@ -214,32 +218,36 @@ template <typename T, int E, int NT, bool BLOCK> __global__ __launch_bounds__(NT
 // five packs a lane or more, which a SIMD has two waves of in any case, the gates of the first pass stay for the second (B128 C768
 // 434 -> 414 us).  Three packs of bf16 fit into a SIMD's registers four times only if r2 is read twice and instructions move
 // in steps of two elements (B256 C96 L1024 126 -> 94 us).
-template <typename T, int E, int NT, bool BLOCK>
-__global__ __launch_bounds__(NT, BLOCK && sizeof(T) == 2 && E == 3 ? 4 : 1) void norm_bwd_tile_kernel(NormBwd<T> p)
+template <typename T, int E, int NT, int NB, bool BLOCK>
+__global__ __launch_bounds__(NT * NB, BLOCK && NB == 1 && sizeof(T) == 2 && E == 3 ? 4 : 1) void norm_bwd_tile_kernel(NormBwd<T> p)
 {
     constexpr int V = Pack<T>::V;
-    constexpr bool LEAN = BLOCK && sizeof(T) == 2 && E == 3;
+    constexpr bool LEAN = BLOCK && NB == 1 && sizeof(T) == 2 && E == 3;
     constexpr bool KEEP = BLOCK && NT == 512 && E >= 5;
     constexpr int STEP = LEAN ? 2 : 4;              // elements whose instructions may mix: with more, more registers hold what waits
-    extern __shared__ float red[];
-    const int x = threadIdx.x & ((1 << p.lx) - 1), c0 = threadIdx.x >> p.lx, step = NT >> p.lx;
+    extern __shared__ float shared[];
+    const int sub = NB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0, tid = NB > 1 ? threadIdx.x % NT : threadIdx.x;
+    const int x = tid & ((1 << p.lx) - 1), c0 = tid >> p.lx, step = NT >> p.lx;
+    float *red = shared + sub * ((NT / 16 + 1) * (BLOCK ? 4 : 1) * (V << p.lx) + E * (2 * step + NT));
     const unsigned mine = ((unsigned)c0 * (unsigned)p.L + (unsigned)(x * V)) * (unsigned)sizeof(T);
     const bool in = c0 + (E - 1) * step < p.C;
     const float inv_c = 1.0f / (float)p.C;
     // behind the sums of a position in LDS: the parameters, and every lane's sums for its channels
     float *ws = red + (NT / 16 + 1) * (BLOCK ? 4 : 1) * (V << p.lx), *wns = ws + E * step, *mine_n = wns + E * step;
-    const TileAt tile = tile_at(die_run<unsigned>(blockIdx.x, (unsigned)p.tiles), p.row_tiles, V << p.lx, p.L);
+    const unsigned at_tile = die_run<unsigned>(blockIdx.x, gridDim.x) * NB + sub;
+    const bool live = NB == 1 || at_tile < (unsigned)p.tiles;
+    const TileAt tile = tile_at(live ? at_tile : 0, p.row_tiles, V << p.lx, p.L);
     const auto at = [&](const auto &s, int e) { return place(s.p + ((long long)tile.b * s.bs + (long long)(e * step) * p.L + tile.t0), mine); };
     // Loads come back in order, so what is needed first is asked for first; nothing in between waits for them.
     // (the parameters of two rounds wait in registers until the tile's loads are on their way)
     float pw[2], pn[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int c = min((int)threadIdx.x + i * NT, p.C - 1);
+        const int c = min(tid + i * NT, p.C - 1);
         pw[i] = BLOCK ? p.w[c] : 0.0f;
         pn[i] = p.w_next[c];
     }
-    for (int c = threadIdx.x + 2 * NT; c < p.C; c += NT) {
+    for (int c = tid + 2 * NT; c < p.C; c += NT) {
         if (BLOCK) ws[c] = p.scale * p.w[c];
         wns[c] = p.w_next[c];
     }
@@ -274,13 +282,13 @@ __global__ __launch_bounds__(NT, BLOCK && sizeof(T) == 2 && E == 3 ? 4 : 1) void
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int c = threadIdx.x + i * NT;
+        const int c = tid + i * NT;
         if (c < E * step) {
             if (BLOCK) ws[c] = c < p.C ? p.scale * pw[i] : 0.0f;
             wns[c] = c < p.C ? pn[i] : 0.0f;
         }
     }
-    for (int c = max(p.C, 2 * NT) + threadIdx.x; c < E * step; c += NT) ws[c] = wns[c] = 0.0f;
+    for (int c = max(p.C, 2 * NT) + tid; c < E * step; c += NT) ws[c] = wns[c] = 0.0f;
     __syncthreads();
     const int again = tile.again - x * V;           // of this lane's positions
     // r2 where a position counts in the sums over positions, 0 where the tile before counts it (which has the same infinities and NaN)
@@ -323,7 +331,7 @@ __global__ __launch_bounds__(NT, BLOCK && sizeof(T) == 2 && E == 3 ? 4 : 1) void
             }
             if (k % STEP == STEP - 1) __builtin_amdgcn_sched_barrier(0);
         }
-        mine_n[e * NT + threadIdx.x] = sum;
+        mine_n[e * NT + tid] = sum;
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
@@ -337,9 +345,9 @@ __global__ __launch_bounds__(NT, BLOCK && sizeof(T) == 2 && E == 3 ? 4 : 1) void
 #pragma unroll
         for (int k = 0; k < V; ++k) r2[k] = s[p.L + k];
     }
-    channel_sums<S, V, NT>(sums, p.lx, red);
-    float *part = p.part + (long long)blockIdx.x * 2 * p.C;
-    for (int c = threadIdx.x; c < p.C; c += NT) {
+    channel_sums<S, V, NT>(sums, p.lx, tid, red);
+    float *part = p.part + (long long)at_tile * 2 * p.C;
+    for (int c = tid; c < (live ? p.C : 0); c += NT) {
         float n = 0.0f;                                 // (lane x of channel c stands at c 2^lx + x)
         for (int i = 0; i < (1 << p.lx); ++i) n += mine_n[(c << p.lx) + i];
         part[p.C + c] = n;
@@ -377,7 +385,7 @@ __global__ __launch_bounds__(NT, BLOCK && sizeof(T) == 2 && E == 3 ? 4 : 1) void
             }
             if (k % STEP == STEP - 1) __builtin_amdgcn_sched_barrier(0);
         }
-        if (e < E - 1 || in) {
+        if (live && (e < E - 1 || in)) {
             store_packed(at(p.dres, e), d);
             if constexpr (BLOCK) {
                 store_packed(at(p.dz, e), dz);
@@ -387,7 +395,7 @@ __global__ __launch_bounds__(NT, BLOCK && sizeof(T) == 2 && E == 3 ? 4 : 1) void
         if constexpr (BLOCK) {
             settle(sum);
             sum = group_sum(sum, p.lx) * p.scale;       // (out's part of dw carries the scale)
-            if (x == 0 && (e < E - 1 || in)) part[c + e * step] = sum;
+            if (x == 0 && live && (e < E - 1 || in)) part[c + e * step] = sum;
         }
         __builtin_amdgcn_sched_barrier(0);
     }
