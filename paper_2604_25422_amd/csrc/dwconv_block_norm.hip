@@ -10,6 +10,7 @@ namespace {
 struct NormPlan {
     int E, NT, lx;              // tile kernel (NT threads for a tile); E = 0: the streaming one
     int NB;                     // tiles of a workgroup
+    bool short_rows;            // of less than a pack of positions
     int row_tiles;
     long long tiles;
     int blocks;
@@ -28,6 +29,8 @@ NormPlan plan_norm(int B, int C, int L, int dtype, bool backward)
     // B20000 C130 L12 bf16 forward 245 us as 256 threads, 126 us as 128, 84 us as a wave; backward 224, 177 and 185 us; B10000 C384 L12
     // fp32 backward 360 us as 512 threads, 330 us as 128.  On whole lines that is so of few channels only (B4000 C32 L128 bf16 forward
     // 48 us as 256 threads with a pack each, 38 us as 128 with two; backward 61 us, 65 us as a wave with four).
+    // Rows of less than a pack are tiles of a wave or two as well, loaded in parts, unless most of a pack would be idle (B20000 C500 L5
+    // bf16 forward 392 us by the streaming kernel, 168 us so; backward 1374 and 340 us.  B4096 C768 L1 backward 54 and 99 us).
     // Forward: B128 C768 L1024 bf16 220 us as 512 threads and half lines, 242 us as 1024 threads and whole ones (336 us with a quarter
     // of a line); B64 C768 L1024 fp32 233 and 206 us.
     // Backward, fp32: B64 C384 L1024 171 us as 512 threads and whole lines, 178 us as 1024, 192 us with half lines; B16384 C128 L48
@@ -37,7 +40,7 @@ NormPlan plan_norm(int B, int C, int L, int dtype, bool backward)
     const bool f32 = dtype == DWCONV_F32;
     const auto take = [&](int lx, int NT, int most) {
         const int rows = NT >> lx;
-        if (s.E || (V << lx) > L || ceil_div(C, rows) > most || (long long)rows * L * (16 / V) >= (1ll << 31)) return;
+        if (s.E || ((V << lx) > L && (lx || NT > 128 || 4 * L <= V)) || ceil_div(C, rows) > most || (long long)rows * L * (16 / V) >= (1ll << 31)) return;
         s.E = (int)ceil_div(C, rows);
         s.NT = NT;
         s.lx = lx;
@@ -55,7 +58,7 @@ NormPlan plan_norm(int B, int C, int L, int dtype, bool backward)
             take(lx, 512, lx >= 2 ? kMaxE : 2);
             if (lx < 2) take(lx, 1024, 3);
         } else {
-            if (lx < 3) take(lx, 128, 5);
+            if (lx < 3) take(lx, 128, L < V ? kMaxE : 5);
             take(lx, 256, lx == 3 ? kMaxE : 3);
             if (lx < 3) take(lx, 512, kMaxE);
         }
@@ -72,13 +75,14 @@ NormPlan plan_norm(int B, int C, int L, int dtype, bool backward)
     s.tiles = (long long)B * s.row_tiles;
     // (a workgroup per tile, in order: workgroups that walk several drift apart, and with them the halves of a line.  B128 C768 L1024
     // bf16 backward, of an earlier form of the kernel: 431 us, 512 us with two tiles each)
+    s.short_rows = s.E && L < V;
     s.blocks = s.E ? (int)ceil_div(s.tiles, s.NB) : (int)std::min<long long>(s.tiles, backward ? 1024 : 1 << 20);
     return s;
 }
 size_t red_bytes(const NormPlan &s, int V, int sums) { return (size_t)(s.NT / 16 + 1) * sums * (V << s.lx) * sizeof(float); }
 
-// Rows of sums: one a tile, or a workgroup of the streaming kernel.
-int sum_rows(const NormPlan &s) { return s.E ? (int)s.tiles : s.blocks; }
+// Rows of sums: one a tile, or a workgroup of tiles of short rows or of the streaming kernel.
+int sum_rows(const NormPlan &s) { return s.E && !s.short_rows ? (int)s.tiles : s.blocks; }
 // Runs that they are first added up in (4096 sums of 768 channels twice: 18 us by norm_sums_kernel alone); 0: not worth it.
 int sum_runs(const NormPlan &s) { return sum_rows(s) >= 65536 ? 512 : sum_rows(s) >= 512 ? 64 : 0; }
 
@@ -87,18 +91,23 @@ template <typename T, int E, bool BLOCK> void fwd_tile(const NormFwd<T> &p, cons
     const size_t lds = s.NB * red_bytes(s, Pack<T>::V, 1);
     // (what plan_norm takes: larger workgroups only where smaller ones would have too many packs)
     switch (s.NT) {
-    case 64: norm_fwd_tile_kernel<T, E, 64, 4, BLOCK><<<s.blocks, 256, lds, st>>>(p); break;
+    case 64:
+        if (s.short_rows) norm_fwd_tile_kernel<T, E, 64, 4, BLOCK, true><<<s.blocks, 256, lds, st>>>(p);
+        else norm_fwd_tile_kernel<T, E, 64, 4, BLOCK, false><<<s.blocks, 256, lds, st>>>(p);
+        break;
     case 128:
-        if constexpr (E == 2 || E >= 4) norm_fwd_tile_kernel<T, E, 128, 2, BLOCK><<<s.blocks, 256, lds, st>>>(p);
+        if (s.short_rows) {
+            if constexpr (E >= 4) norm_fwd_tile_kernel<T, E, 128, 2, BLOCK, true><<<s.blocks, 256, lds, st>>>(p);
+        } else if constexpr (E == 2 || E >= 4) norm_fwd_tile_kernel<T, E, 128, 2, BLOCK, false><<<s.blocks, 256, lds, st>>>(p);
         break;
     case 256:
-        if constexpr (E >= 2) norm_fwd_tile_kernel<T, E, 256, 1, BLOCK><<<s.blocks, 256, lds, st>>>(p);
+        if constexpr (E >= 2) norm_fwd_tile_kernel<T, E, 256, 1, BLOCK, false><<<s.blocks, 256, lds, st>>>(p);
         break;
     case 512:
-        if constexpr (E >= 4) norm_fwd_tile_kernel<T, E, 512, 1, BLOCK><<<s.blocks, 512, lds, st>>>(p);
+        if constexpr (E >= 4) norm_fwd_tile_kernel<T, E, 512, 1, BLOCK, false><<<s.blocks, 512, lds, st>>>(p);
         break;
     default:
-        if constexpr (E >= 4) norm_fwd_tile_kernel<T, E, 1024, 1, BLOCK><<<s.blocks, 1024, lds, st>>>(p);
+        if constexpr (E >= 4) norm_fwd_tile_kernel<T, E, 1024, 1, BLOCK, false><<<s.blocks, 1024, lds, st>>>(p);
     }
 }
 template <typename T, bool BLOCK> void launch_fwd(const NormFwd<T> &p, const NormPlan &s, hipStream_t st)
@@ -124,21 +133,26 @@ template <typename T, bool BLOCK> void launch_fwd(const NormFwd<T> &p, const Nor
 }
 template <typename T, int E, bool BLOCK> void bwd_tile(const NormBwd<T> &p, const NormPlan &s, hipStream_t st)
 {
-    const size_t lds = s.NB * (red_bytes(s, Pack<T>::V, BLOCK ? 4 : 1) + (size_t)E * (2 * (s.NT >> s.lx) + s.NT) * sizeof(float));
+    const size_t lds = s.NB * (red_bytes(s, Pack<T>::V, BLOCK ? 4 : 1) + (size_t)E * (2 * (s.NT >> s.lx) + (s.short_rows ? 2 : 1) * s.NT) * sizeof(float));
     constexpr bool F32 = sizeof(T) == 4;
     switch (s.NT) {
-    case 64: norm_bwd_tile_kernel<T, E, 64, 4, BLOCK><<<s.blocks, 256, lds, st>>>(p); break;
+    case 64:
+        if (s.short_rows) norm_bwd_tile_kernel<T, E, 64, 4, BLOCK, true><<<s.blocks, 256, lds, st>>>(p);
+        else norm_bwd_tile_kernel<T, E, 64, 4, BLOCK, false><<<s.blocks, 256, lds, st>>>(p);
+        break;
     case 128:
-        if constexpr (E >= 4 && (F32 || E < 6)) norm_bwd_tile_kernel<T, E, 128, 2, BLOCK><<<s.blocks, 256, lds, st>>>(p);
+        if (s.short_rows) {
+            if constexpr (E >= 4) norm_bwd_tile_kernel<T, E, 128, 2, BLOCK, true><<<s.blocks, 256, lds, st>>>(p);
+        } else if constexpr (E >= 4 && (F32 || E < 6)) norm_bwd_tile_kernel<T, E, 128, 2, BLOCK, false><<<s.blocks, 256, lds, st>>>(p);
         break;
     case 256:
-        if constexpr (!F32 || E <= 2) norm_bwd_tile_kernel<T, E, 256, 1, BLOCK><<<s.blocks, 256, lds, st>>>(p);
+        if constexpr (!F32 || E <= 2) norm_bwd_tile_kernel<T, E, 256, 1, BLOCK, false><<<s.blocks, 256, lds, st>>>(p);
         break;
     case 512:
-        if constexpr (E >= 2) norm_bwd_tile_kernel<T, E, 512, 1, BLOCK><<<s.blocks, 512, lds, st>>>(p);
+        if constexpr (E >= 2) norm_bwd_tile_kernel<T, E, 512, 1, BLOCK, false><<<s.blocks, 512, lds, st>>>(p);
         break;
     default:
-        if constexpr (F32 && (E == 2 || E == 3)) norm_bwd_tile_kernel<T, E, 1024, 1, BLOCK><<<s.blocks, 1024, lds, st>>>(p);
+        if constexpr (F32 && (E == 2 || E == 3)) norm_bwd_tile_kernel<T, E, 1024, 1, BLOCK, false><<<s.blocks, 1024, lds, st>>>(p);
     }
 }
 template <typename T, bool BLOCK> void launch_bwd(const NormBwd<T> &p, const NormPlan &s, float *dw, float *dw_next, hipStream_t st)

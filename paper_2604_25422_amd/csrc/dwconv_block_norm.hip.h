@@ -108,6 +108,31 @@ template <typename V> __device__ __forceinline__ void settle(V &v) { asm volatil
 
 __device__ __forceinline__ float inv_sqrt(float v) { return 1.0f / sqrtf(v); }
 
+// A pack of a row of L elements, which may be shorter (zeros behind it).
+template <bool SHORT, typename T> __device__ __forceinline__ void load_tile(Pack<T> &e, const T *p, int L)
+{
+    if constexpr (SHORT) {
+        const Few<Pack<T>::V, T> f = load_few<Pack<T>::V>(p, L);
+        __builtin_memcpy(&e.w, f.v, 16);
+    } else {
+        load_pack(e, p);
+    }
+}
+template <bool SHORT, typename T, int V> __device__ __forceinline__ void store_values(T *p, const float (&v)[V], int L)
+{
+    if constexpr (SHORT) store_few<V>(p, v, L);
+    else store_pack(p, v);
+}
+template <bool SHORT, typename T> __device__ __forceinline__ void store_tile(T *p, const Pack<T> &e, int L)
+{
+    if constexpr (SHORT) {
+        Few<Pack<T>::V, T> f;
+        __builtin_memcpy(f.v, &e.w, 16);
+        store_part<Pack<T>::V>(p, f, 0, L);
+    } else {
+        store_packed(p, e);
+    }
+}
 // Element at a workgroup's pointer and a lane's offset in bytes.
 template <typename T> __device__ __forceinline__ const T *place(const T *p, unsigned bytes)
 {
@@ -126,7 +151,7 @@ __device__ __forceinline__ TileAt tile_at(unsigned tile, int row_tiles, int T, i
     return TileAt{b, t - over, over};
 }
 
-template <typename T, int E, int NT, int NB, bool BLOCK> __global__ __launch_bounds__(NT * NB) void norm_fwd_tile_kernel(NormFwd<T> p)
+template <typename T, int E, int NT, int NB, bool BLOCK, bool SHORT> __global__ __launch_bounds__(NT * NB) void norm_fwd_tile_kernel(NormFwd<T> p)
 {
     constexpr int V = Pack<T>::V;
     extern __shared__ float shared[];
@@ -137,7 +162,7 @@ template <typename T, int E, int NT, int NB, bool BLOCK> __global__ __launch_bou
     const unsigned mine = ((unsigned)c0 * (unsigned)p.L + (unsigned)(x * V)) * (unsigned)sizeof(T);
     const unsigned at_tile = die_run<unsigned>(blockIdx.x, gridDim.x) * NB + sub;
     const bool live = NB == 1 || at_tile < (unsigned)p.tiles;
-    const TileAt tile = tile_at(live ? at_tile : 0, p.row_tiles, V << p.lx, p.L);
+    const TileAt tile = SHORT ? TileAt{live ? (int)at_tile : 0, 0, 0} : tile_at(live ? at_tile : 0, p.row_tiles, V << p.lx, p.L);
     const auto at = [&](const auto &s, int e) { return place(s.p + ((long long)tile.b * s.bs + (long long)(e * step) * p.L + tile.t0), mine); };
     // (only the last round of channels can be short)
     const bool in = c0 + (E - 1) * step < p.C;
@@ -146,13 +171,13 @@ template <typename T, int E, int NT, int NB, bool BLOCK> __global__ __launch_bou
     if constexpr (BLOCK) {
 #pragma unroll
         for (int e = 0; e < E; ++e)
-            if (e < E - 1 || in) load_pack(y[e], at(p.y, e));
+            if (e < E - 1 || in) load_tile<SHORT>(y[e], at(p.y, e), p.L);
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         if (e < E - 1 || in) {
-            load_pack(res[e], at(p.res, e));
-            if (BLOCK) load_pack(z[e], at(p.z, e));
+            load_tile<SHORT>(res[e], at(p.res, e), p.L);
+            if (BLOCK) load_tile<SHORT>(z[e], at(p.z, e), p.L);
         }
     }
     float w[E], wn[E];
@@ -190,7 +215,7 @@ template <typename T, int E, int NT, int NB, bool BLOCK> __global__ __launch_bou
             }
             r2[k] = fmaf(o[e][k], o[e][k], r2[k]);
         }
-        if (BLOCK && live && (e < E - 1 || in)) store_pack(at(p.out, e), o[e]);
+        if (BLOCK && live && (e < E - 1 || in)) store_values<SHORT>(at(p.out, e), o[e], p.L);
     }
     channel_sums<V, NT>(r2, p.lx, tid, red);
 #pragma unroll
@@ -199,12 +224,13 @@ template <typename T, int E, int NT, int NB, bool BLOCK> __global__ __launch_bou
     for (int e = 0; e < E; ++e) {
 #pragma unroll
         for (int k = 0; k < V; ++k) o[e][k] *= r2[k] * wn[e];
-        if (live && (e < E - 1 || in)) store_pack(at(p.n, e), o[e]);
+        if (live && (e < E - 1 || in)) store_values<SHORT>(at(p.n, e), o[e], p.L);
     }
     if (p.stats && live && c0 == 0) {
         float *s = p.stats + (long long)tile.b * 2 * p.L + tile.t0 + x * V;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
+            if (SHORT && k >= p.L) break;
             if (BLOCK) s[k] = r1[k];
             s[p.L + k] = r2[k];
         }
@@ -218,7 +244,7 @@ template <typename T, int E, int NT, int NB, bool BLOCK> __global__ __launch_bou
 // five packs a lane or more, which a SIMD has two waves of in any case, the gates of the first pass stay for the second (B128 C768
 // 434 -> 414 us).  Three packs of bf16 fit into a SIMD's registers four times only if r2 is read twice and instructions move
 // in steps of two elements (B256 C96 L1024 126 -> 94 us).
-template <typename T, int E, int NT, int NB, bool BLOCK>
+template <typename T, int E, int NT, int NB, bool BLOCK, bool SHORT>
 __global__ __launch_bounds__(NT * NB, BLOCK && NB == 1 && sizeof(T) == 2 && E == 3 ? 4 : 1) void norm_bwd_tile_kernel(NormBwd<T> p)
 {
     constexpr int V = Pack<T>::V;
@@ -228,7 +254,8 @@ __global__ __launch_bounds__(NT * NB, BLOCK && NB == 1 && sizeof(T) == 2 && E ==
     extern __shared__ float shared[];
     const int sub = NB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0, tid = NB > 1 ? threadIdx.x % NT : threadIdx.x;
     const int x = tid & ((1 << p.lx) - 1), c0 = tid >> p.lx, step = NT >> p.lx;
-    float *red = shared + sub * ((NT / 16 + 1) * (BLOCK ? 4 : 1) * (V << p.lx) + E * (2 * step + NT));
+    const int region = (NT / 16 + 1) * (BLOCK ? 4 : 1) * (V << p.lx) + E * (2 * step + (SHORT ? 2 : 1) * NT);
+    float *red = shared + sub * region;
     const unsigned mine = ((unsigned)c0 * (unsigned)p.L + (unsigned)(x * V)) * (unsigned)sizeof(T);
     const bool in = c0 + (E - 1) * step < p.C;
     const float inv_c = 1.0f / (float)p.C;
@@ -236,7 +263,7 @@ __global__ __launch_bounds__(NT * NB, BLOCK && NB == 1 && sizeof(T) == 2 && E ==
     float *ws = red + (NT / 16 + 1) * (BLOCK ? 4 : 1) * (V << p.lx), *wns = ws + E * step, *mine_n = wns + E * step;
     const unsigned at_tile = die_run<unsigned>(blockIdx.x, gridDim.x) * NB + sub;
     const bool live = NB == 1 || at_tile < (unsigned)p.tiles;
-    const TileAt tile = tile_at(live ? at_tile : 0, p.row_tiles, V << p.lx, p.L);
+    const TileAt tile = SHORT ? TileAt{live ? (int)at_tile : 0, 0, 0} : tile_at(live ? at_tile : 0, p.row_tiles, V << p.lx, p.L);
     const auto at = [&](const auto &s, int e) { return place(s.p + ((long long)tile.b * s.bs + (long long)(e * step) * p.L + tile.t0), mine); };
     // Loads come back in order, so what is needed first is asked for first; nothing in between waits for them.
     // (the parameters of two rounds wait in registers until the tile's loads are on their way)
@@ -255,8 +282,9 @@ __global__ __launch_bounds__(NT * NB, BLOCK && NB == 1 && sizeof(T) == 2 && E ==
     const float *s = p.stats + (long long)tile.b * 2 * p.L + tile.t0 + x * V;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-        r1[k] = BLOCK ? s[k] : 0.0f;
-        r2[k] = s[p.L + k];
+        const bool have = !SHORT || k < p.L;
+        r1[k] = BLOCK && have ? s[k] : 0.0f;
+        r2[k] = have ? s[p.L + k] : 0.0f;
     }
     __builtin_amdgcn_sched_barrier(0);
     // Lanes behind the last channel load that channel and mask it, and without a gradient of out dn stands in for it and is masked:
@@ -271,13 +299,13 @@ __global__ __launch_bounds__(NT * NB, BLOCK && NB == 1 && sizeof(T) == 2 && E ==
     Pack<T> y[E], z[E], res[E], dn[E], dout[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        load_pack(res[e], from(p.res, e));
+        load_tile<SHORT>(res[e], from(p.res, e), p.L);
         if (BLOCK) {
-            load_pack(z[e], from(p.z, e));
-            load_pack(y[e], from(p.y, e));
+            load_tile<SHORT>(z[e], from(p.z, e), p.L);
+            load_tile<SHORT>(y[e], from(p.y, e), p.L);
         }
-        load_pack(dn[e], from(p.dn, e));
-        load_pack(dout[e], from(other, e));
+        load_tile<SHORT>(dn[e], from(p.dn, e), p.L);
+        load_tile<SHORT>(dout[e], from(other, e), p.L);
         __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
@@ -331,7 +359,7 @@ __global__ __launch_bounds__(NT * NB, BLOCK && NB == 1 && sizeof(T) == 2 && E ==
             }
             if (k % STEP == STEP - 1) __builtin_amdgcn_sched_barrier(0);
         }
-        mine_n[e * NT + tid] = sum;
+        mine_n[e * NT + tid] = live ? sum : 0.0f;
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
@@ -347,9 +375,9 @@ __global__ __launch_bounds__(NT * NB, BLOCK && NB == 1 && sizeof(T) == 2 && E ==
     }
     channel_sums<S, V, NT>(sums, p.lx, tid, red);
     float *part = p.part + (long long)at_tile * 2 * p.C;
-    for (int c = tid; c < (live ? p.C : 0); c += NT) {
+    for (int c = tid; c < (!SHORT && live ? p.C : 0); c += NT) {
         float n = 0.0f;                                 // (lane x of channel c stands at c 2^lx + x)
-        for (int i = 0; i < (1 << p.lx); ++i) n += mine_n[(c << p.lx) + i];
+        for (int j = 0; j < (1 << p.lx); ++j) n += mine_n[(c << p.lx) + j];
         part[p.C + c] = n;
     }
     // d = dout + r2 (dnw + m2 out) and dy = r1 (d w silu(z) scale) + m1 y
@@ -386,18 +414,38 @@ __global__ __launch_bounds__(NT * NB, BLOCK && NB == 1 && sizeof(T) == 2 && E ==
             if (k % STEP == STEP - 1) __builtin_amdgcn_sched_barrier(0);
         }
         if (live && (e < E - 1 || in)) {
-            store_packed(at(p.dres, e), d);
+            store_tile<SHORT>(at(p.dres, e), d, p.L);
             if constexpr (BLOCK) {
-                store_packed(at(p.dz, e), dz);
-                store_packed(at(p.dy, e), dy);
+                store_tile<SHORT>(at(p.dz, e), dz, p.L);
+                store_tile<SHORT>(at(p.dy, e), dy, p.L);
             }
         }
         if constexpr (BLOCK) {
             settle(sum);
-            sum = group_sum(sum, p.lx) * p.scale;       // (out's part of dw carries the scale)
-            if (x == 0 && live && (e < E - 1 || in)) part[c + e * step] = sum;
+            if constexpr (SHORT) {
+                mine_n[(E + e) * NT + tid] = live ? sum : 0.0f;
+            } else {
+                sum = group_sum(sum, p.lx) * p.scale;   // (out's part of dw carries the scale)
+                if (x == 0 && live && (e < E - 1 || in)) part[c + e * step] = sum;
+            }
         }
         __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (SHORT) {
+        // tiles of less than a pack of positions are so small that a row of sums for each would be as much again: one for the workgroup
+        __syncthreads();
+        float *part = p.part + (long long)blockIdx.x * 2 * p.C;
+        for (int c = threadIdx.x; c < p.C; c += NT * NB) {
+            float w = 0.0f, n = 0.0f;
+#pragma unroll
+            for (int o = 0; o < NB; ++o) {
+                const float *sums_of = mine_n + (o - sub) * region;
+                n += sums_of[c];
+                if (BLOCK) w += sums_of[E * NT + c];
+            }
+            if (BLOCK) part[c] = w * p.scale;
+            part[p.C + c] = n;
+        }
     }
 }
 
