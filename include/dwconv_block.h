@@ -39,7 +39,7 @@ typedef struct dwconv_seq_out {
  *     q[t] = rate * softplus(lam[c]) * sigmoid(r[t]),   a[t] = exp(-q[t]),   u[t] = sqrt(1 - a[t]^2) * sigmoid(i[t]) * x[t]
  *     h[t] = a[t] h[t-1] + u[t],   y[t] = h[t]          for t = 0 .. n - 1 of every (b, c), h[-1] = h0[b, c]
  * x, r, i in, y out: [B, C, L].  lam [C].  h0 [B, C] fp32 or NULL (zeros).  lengths [B] int32 or NULL (all L): n is
- * lengths[b] held to [0, L]; y is 0 from n on and nothing is read there.  h_last [B, C] fp32 or NULL: h[n-1] (h0 where n = 0).
+ * lengths[b] held to [0, L]; y is 0 from n on, whatever x, r and i hold there.  h_last [B, C] fp32 or NULL: h[n-1] (h0 where n = 0).
  * states [B, C, dwconv_scan_states(L)] fp32 or NULL: h before every 512th position, which dwconv_scan_bwd takes.
  * workspace: dwconv_scan_workspace_bytes(...) bytes, 16-byte aligned; NULL where that is 0.  rate > 0 and finite.
  * What is not finite in x, r or i stays in its own row (b, c), at its position and behind it.

@@ -79,6 +79,22 @@ def test_scan_shapes(B, C, L, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("L", [1, 2, 3, 4, 5, 6, 7, 8, 9, 15, 255, 257, 263, 511])
+def test_scan_short_rows_of_many_lengths(L, dtype):
+    """Rows that a lane has whole, and rows that end inside a lane's eight, in more workgroups than a run of them has."""
+    B, C = 13, 131
+    x, r, i, dy, lam = scan_inputs(B, C, L, dtype, 61)
+    h0, dh = rand(B, C, seed=1), rand(B, C, seed=2)
+    lengths = torch.tensor([0, 1, L, L // 2, -4, L + 9, max(1, L - 1), L, 2, 3, L - 2, L, 5], dtype=torch.int32).cuda()
+    for n in (None, lengths):
+        want, err = ref.scan(x, r, i, lam, h0, n, RATE, dy, dh)
+        y, h_last, states = block.scan_fwd(x, r, i, lam, h0, n)
+        got = dict(zip(("dx", "dr", "di", "dlam", "dh0"), block.scan_bwd(dy, x, r, i, lam, states, dh, n)), y=y, h_last=h_last)
+        for k, v in got.items():
+            ref.check(v, want[k], err[k], v.dtype, k)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("L", [5, 100, 700, 5000, 33000])
 def test_scan_masked_rows(L, dtype):
     """Sequences of no position, one, all, and lengths outside [0, L]; what lies behind an end is not read."""
@@ -276,6 +292,21 @@ def test_norm(B, C, L, dtype):
         for k, v in got.items():
             assert v.dtype == (F32 if k in ("dw", "dw_next") else dtype)
             ref.check(v, want[k], err[k], v.dtype, (case, k))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("C,L", [(c, n) for c in (1, 64, 65, 150, 200, 300, 384, 385, 500, 640, 700, 768, 769) for n in (2, 3, 5, 7, 9)]
+                         + [(c, n) for c in (31, 64, 65, 96, 128, 129, 192, 193, 300, 330) for n in (12, 17, 35)] + [(16, 64), (17, 70), (32, 33), (33, 130)])
+def test_norm_of_short_rows(C, L, dtype):
+    """Tiles of a wave and of two, of less than a pack and of one, the last workgroup with fewer tiles than it has room for."""
+    y, z, res, dout, dn, w, wn = norm_inputs(5, C, L, dtype)
+    for d, a in ((dout, (y, z, res, w, wn)), (None, (None, None, res, None, wn))):
+        want, err = ref.norm(*a, eps=1e-5, scale=0.5, dout=d, dn=dn)
+        out, n, stats = block.norm_fwd(*a, eps=1e-5, scale=0.5)
+        got = dict(zip(("dy", "dz", "dres", "dw", "dw_next"), block.norm_bwd(d, dn, *a, stats, scale=0.5)), out=out, n=n)
+        for k, v in got.items():
+            if v is not None:
+                ref.check(v, want[k], err[k], v.dtype, k)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
