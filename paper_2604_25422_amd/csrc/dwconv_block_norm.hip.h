@@ -6,6 +6,7 @@
 // pass (both forward means come from it as `stats`) cost no second read.  Lane x of a tile's row has 16 bytes of positions, the rows
 // go over the other lanes and E times round; sums over channels go over the lanes of a wave, then over the waves in LDS, in a fixed
 // order.  Parameter gradients are summed over the positions of a lane and the lanes of a row; further launches add the tiles' sums.
+// Tiles of short rows (NB > 1) belong to a wave or two, several to a workgroup; rows of less than a pack (SHORT) are loaded in parts.
 #pragma once
 #include "dwconv_block_common.hip.h"
 
@@ -238,7 +239,7 @@ template <typename T, int E, int NT, int NB, bool BLOCK, bool SHORT> __global__ 
 }
 
 // Both means of a position come from four sums that one pass over the tile forms at once; a second pass has the gradients.  Memory
-// bounds it where a CU has several tiles at work (B32 C256 L4097 fp32 244 us, 4.4 TB/s; B256 C192 L1024 bf16 179 us, 4.5 TB/s) and the
+// bounds it where a CU has several tiles at work (B32 C256 L4097 fp32 250 us, 4.3 TB/s; B256 C192 L1024 bf16 179 us, 4.5 TB/s) and the
 // registers where it has one (B128 C768 L1024 bf16 410 us with the sums, 3.9 TB/s): 60 instructions an element then stand
 // between a tile's loads and its stores, so they are cut where they can be: the rms factors come in behind the sums, and with
 // five packs a lane or more, which a SIMD has two waves of in any case, the gates of the first pass stay for the second (B128 C768
