@@ -36,7 +36,7 @@ NormPlan plan_norm(int B, int C, int L, int dtype, bool backward)
     // Backward, fp32: B64 C384 L1024 171 us as 512 threads and whole lines, 178 us as 1024, 192 us with half lines; B16384 C128 L48
     // 675 us as 512 threads, 695 us as 256; below half a line larger workgroups win: B64 C1024 L1024 591 us as 1024 threads, 661 us as
     // 512.  bf16: whole lines only as 256 threads (B32 C256 L4096 155 us as 512, 143 us with half lines; B256 C64 L1024 65 us, 72 us
-    // with half lines as 256 and 77 us with whole ones as 512); B128 C768 L1024 402 us with half lines, 490 us with quarters.
+    // with half lines as 256 and 77 us with whole ones as 512); B128 C768 L1024 414 us with half lines, 501 us with quarters.
     const bool f32 = dtype == DWCONV_F32;
     const auto take = [&](int lx, int NT, int most) {
         const int rows = NT >> lx;

@@ -310,6 +310,18 @@ def test_norm_of_short_rows(C, L, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,C,L", [(70000, 3, 9), (300000, 2, 3)])
+def test_norm_of_very_many_tiles(B, C, L, dtype):
+    """Sums over more tiles than the first of their two launches has few runs for."""
+    y, z, res, dout, dn, w, wn = norm_inputs(B, C, L, dtype)
+    want, err = ref.norm(y, z, res, w, wn, eps=1e-5, scale=0.5, dout=dout, dn=dn)
+    out, n, stats = block.norm_fwd(y, z, res, w, wn, eps=1e-5, scale=0.5)
+    got = dict(zip(("dy", "dz", "dres", "dw", "dw_next"), block.norm_bwd(dout, dn, y, z, res, w, wn, stats, scale=0.5)), out=out, n=n)
+    for k, v in got.items():
+        ref.check(v, want[k], err[k], v.dtype, k)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("C,L", [(12, 1), (11, 1), (12, 5), (12, 70), (700, 30), (5000, 21)])
 @pytest.mark.parametrize("kind", ["slice", "odd"])
 def test_norm_layouts(C, L, kind, dtype):
