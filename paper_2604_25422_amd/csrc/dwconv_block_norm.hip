@@ -29,24 +29,25 @@ NormPlan plan_norm(int B, int C, int L, int dtype, bool backward)
     // B20000 C130 L12 bf16 forward 245 us as 256 threads, 126 us as 128, 84 us as a wave; backward 224, 177 and 185 us; B10000 C384 L12
     // fp32 backward 360 us as 512 threads, 330 us as 128.  On whole lines that is so of few channels only (B4000 C32 L128 bf16 forward
     // 48 us as 256 threads with a pack each, 38 us as 128 with two; backward 61 us, 65 us as a wave with four).
-    // Rows of less than a pack are tiles of a wave or two as well, loaded in parts, unless most of a pack would be idle (B20000 C500 L5
-    // bf16 forward 392 us by the streaming kernel, 168 us so; backward 1374 and 340 us.  B4096 C768 L1 backward 54 and 99 us).
+    // Rows of less than a pack are tiles of a wave or two as well, loaded in parts (B20000 C500 L5 bf16 forward 392 us by the streaming
+    // kernel, 168 us so; backward 1374 and 340 us), unless most of a pack would be idle (B4096 C768 L1 backward 54 and 99 us), and
+    // then as well where batch entries abound and their channels are few (B20000 C100 L1 89 and 58 us; but B64 C128 L1 8.8 and 10.9).
     // Forward: B128 C768 L1024 bf16 220 us as 512 threads and half lines, 242 us as 1024 threads and whole ones (336 us with a quarter
     // of a line); B64 C768 L1024 fp32 233 and 206 us.
     // Backward, fp32: B64 C384 L1024 171 us as 512 threads and whole lines, 178 us as 1024, 192 us with half lines; B16384 C128 L48
     // 675 us as 512 threads, 695 us as 256; below half a line larger workgroups win: B64 C1024 L1024 591 us as 1024 threads, 661 us as
     // 512.  bf16: whole lines only as 256 threads (B32 C256 L4096 155 us as 512, 143 us with half lines; B256 C64 L1024 65 us, 72 us
     // with half lines as 256 and 77 us with whole ones as 512); B128 C768 L1024 414 us with half lines, 501 us with quarters.
-    const bool f32 = dtype == DWCONV_F32;
+    const bool f32 = dtype == DWCONV_F32, idle = 4 * (long long)L <= V;
     const auto take = [&](int lx, int NT, int most) {
         const int rows = NT >> lx;
-        if (s.E || ((V << lx) > L && (lx || NT > 128 || 4 * L <= V)) || ceil_div(C, rows) > most || (long long)rows * L * (16 / V) >= (1ll << 31)) return;
+        if (s.E || ((V << lx) > L && (lx || NT > (idle ? 64 : 128))) || ceil_div(C, rows) > most || (idle && NT == 64 && B < 1024) || (long long)rows * L * (16 / V) >= (1ll << 31)) return;
         s.E = (int)ceil_div(C, rows);
         s.NT = NT;
         s.lx = lx;
     };
     for (int lx = 3; lx >= 0; --lx) {
-        take(lx, 64, lx == 3 ? 2 : kMaxE);
+        take(lx, 64, lx == 3 || idle ? 2 : kMaxE);
         if (!backward) {
             take(lx, 128, lx == 3 ? 2 : kMaxE);
             take(lx, 256, kMaxE);
