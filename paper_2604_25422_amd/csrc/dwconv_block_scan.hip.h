@@ -143,7 +143,7 @@ __device__ __forceinline__ void grads_begin(const V &x, const V &r, const V &i, 
     if (left < P) {
 #pragma unroll
         for (int k = 0; k < P; ++k)
-            if (k >= left) w.a[k] = 1.0f, w.in[k] = w.gi[k] = w.e[k] = w.rest[k] = u[k] = pull[k] = 0.0f;
+            if (k >= left) w.a[k] = 1.0f, w.in[k] = w.gi[k] = w.rest[k] = u[k] = pull[k] = 0.0f;
     }
 }
 template <typename V, int P>
@@ -169,9 +169,9 @@ template <int P> __device__ __forceinline__ Span back_span(const float (&a)[P], 
     for (int k = P - 2; k >= 0; --k) s = Span{s.A * a[k], a[k] * (dy[k] + s.H)};
     return s;
 }
-// Gradients of the positions from v behind them, 0 from `left` on; returns their sum of dq q.
+// Gradients of the positions from v behind them, 0 from `left` on (e with its last state too, which may be no number); returns their sum of dq q.
 template <bool ALL = false, int P, typename T>
-__device__ __forceinline__ float grads_store(const GateGrads<P> &w, const float (&dy)[P], float v, T *dx, T *dr, T *di, int left, int t, int L)
+__device__ __forceinline__ float grads_store(GateGrads<P> &w, const float (&dy)[P], float v, T *dx, T *dr, T *di, int left, int t, int L)
 {
     float g[P], out[P], sum = 0.0f;
 #pragma unroll
@@ -182,7 +182,7 @@ __device__ __forceinline__ float grads_store(const GateGrads<P> &w, const float 
     if (left < P) {
 #pragma unroll
         for (int k = 0; k < P; ++k)
-            if (k >= left) g[k] = 0.0f;
+            if (k >= left) g[k] = w.e[k] = 0.0f;
     }
 #pragma unroll
     for (int k = 0; k < P; ++k) out[k] = g[k] * w.in[k];

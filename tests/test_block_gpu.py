@@ -184,6 +184,33 @@ def test_scan_keeps_bad_values_in_their_row(L):
         t[0, 1, at] = kept
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("L", [1, 3, 5, 9, 100, 300, 700, 5000, 40000])
+def test_scan_keeps_bad_values_in_front_of_the_end(L, dtype):
+    """Behind a sequence's end outputs and gradients are 0 also where the state that reaches it is no number, and a bad state in front of a
+    sequence of no position is in no gradient but its own."""
+    B, C = 4, 3
+    x, r, i, dy, lam = scan_inputs(B, C, L, dtype, 75)
+    n = [(L + 1) // 2, L // 3, 0, L]
+    lengths = torch.tensor(n, dtype=torch.int32, device="cuda")
+    h0, dh = rand(B, C, seed=1), rand(B, C, seed=2)
+    want = block.scan_fwd(x, r, i, lam, h0, lengths)
+    clean = block.scan_bwd(dy, x, r, i, lam, want[2], dh, lengths)
+    x[0, 1, n[0] // 2] = float("nan")
+    if n[1]:
+        x[1, 1, n[1] - 1] = float("inf")
+    h0[2, 0], h0[2, 2] = float("nan"), -float("inf")
+    y, h, states = block.scan_fwd(x, r, i, lam, h0, lengths)
+    dx, dr, di, dlam, dh0 = block.scan_bwd(dy, x, r, i, lam, states, dh, lengths)
+    for b in range(B):
+        for t in (y, dx, dr, di):
+            assert (t[b, :, n[b]:] == 0).all(), b
+    assert torch.equal(dlam[[0, 2]], clean[3][[0, 2]]) and dlam[1].isnan()
+    assert torch.equal(dh0[2], dh[2])
+    for a, c in zip((dx, dr, di), clean):
+        assert torch.equal(a[:, [0, 2]], c[:, [0, 2]]) and torch.equal(a[2:], c[2:])
+
+
 def test_scan_against_differences():
     """The kernels' own forward pass, moved along a direction: 32-bit roundings of a sum of 10^4 terms of order 1 against steps of
     2^-5 give about 1e-4 of the sum's size, the third derivative 2^-10 of it."""
