@@ -63,7 +63,7 @@ template <typename T, int V, int U> __global__ __launch_bounds__(256) void conv_
     float *w = taps + row * (K + V - 1);
     bool staged = false;
     // A lane whose places would end behind the ring takes the ring's last V, of which the first `skip` are its neighbour's (B1024 C768
-    // K63 bf16 54 us, 93 us with the rest of a ring element by element).
+    // K63 bf16 56 us, 93 us with the rest of a ring element by element).
     const bool whole = K >= V;
     // (positions, slots and the places of the rings are the workgroup's: scalar work beside the lanes')
     for (long long b0 = (long long)blockIdx.y * U; b0 < p.B; b0 += (long long)gridDim.y * U) {
@@ -124,15 +124,19 @@ template <typename T, int V, int U> __global__ __launch_bounds__(256) void conv_
             for (int u = 0; u < U; ++u) {
                 if (!ring[u]) continue;
                 const int new_at = at[u] - k < skip ? -1 : at[u] - k;           // of the V, where the new input goes
-                if (skip > 0) {
-#pragma unroll
-                    for (int i = 0; i < V; ++i) v[u][i] = i < skip ? 0.0f : v[u][i];
-                }
                 int j = k - at[u] - 1;
                 j = j < 0 ? j + K : j;
-                j = j < K ? j : K - 1;                  // (lanes behind the end of the ring: any tap, their elements are zeros)
+                j = j < K ? j : K - 1;                  // (lanes behind the end of the ring: any tap)
+                float f[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum[u] = fmaf(i == new_at ? ld_elem(&x[u]) : v[u][i], w[j + i], sum[u]);
+                for (int i = 0; i < V; ++i) f[i] = w[j + i];
+                if (skip > 0 || !whole) {               // (the taps of what is not there too: they may be infinite)
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        if (i < skip || (!whole && i >= K)) v[u][i] = f[i] = 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[u] = fmaf(i == new_at ? ld_elem(&x[u]) : v[u][i], f[i], sum[u]);
                 if (in && (unsigned)new_at < (unsigned)V) ring[u][mine + (unsigned)at[u]] = x[u];
             }
         }

@@ -553,6 +553,21 @@ def test_conv_step_of_any_batch(B, C, K, dtype):
     assert torch.equal(ring, want)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("K", [1, 2, 3, 5, 7, 8, 9, 24, 31, 32, 33, 63, 100, 260, 300, 2500])
+def test_conv_step_with_an_infinite_tap(K, dtype):
+    """It meets one input of the ring and nothing else, wherever the position puts it."""
+    B, C = min(K + 2, 200), 5
+    x, ring = torch.ones(B, C, device="cuda", dtype=dtype), torch.ones(B, C, K, device="cuda", dtype=dtype)
+    pos = torch.arange(B, device="cuda", dtype=torch.int32) + max(0, K - B // 2)
+    for j in sorted({0, 1 % K, K // 2, max(0, K - 2), K - 1}):
+        w = torch.full((C, K), 0.5, device="cuda", dtype=dtype)
+        w[0, j], w[1, j], w[2, j] = float("inf"), -float("inf"), float("nan")
+        y = block.conv_step(x, w, ring, pos)
+        assert (y[:, 0] == float("inf")).all() and (y[:, 1] == -float("inf")).all() and y[:, 2].isnan().all(), j
+        assert (y[:, 3:] == torch.tensor(K * 0.5, dtype=dtype)).all(), j
+
+
 def test_conv_step_at_any_position():
     """Positions up to the largest int32, and no slots: the place in the ring is the position's remainder."""
     B, C, K = 3, 20, 7
