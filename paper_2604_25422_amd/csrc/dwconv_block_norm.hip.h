@@ -499,7 +499,7 @@ __device__ __forceinline__ void store_four(bf16_t *p, const float (&v)[4], int l
 }
 template <typename T, int E, bool BLOCK> __global__ __launch_bounds__(64) void norm_fwd_token_kernel(NormFwd<T> p)
 {
-    for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
+    for (unsigned b = blockIdx.x; b < (unsigned)p.B; b += gridDim.x) {          // (an int would wrap: 2^31 - 1 entries are allowed)
         Four<T> y[E], z[E], res[E];
         Four<float> w[E], wn[E];
         const T *py = p.y.p + (long long)b * p.y.bs, *pz = p.z.p + (long long)b * p.z.bs, *pr = p.res.p + (long long)b * p.res.bs;

@@ -564,8 +564,8 @@ template <typename T> __global__ __launch_bounds__(256) void scan_step_kernel(Sc
     const int c = blockIdx.x * 256 + threadIdx.x;
     if (c >= p.C) return;
     const float rho = decay_rate(p.rate, p.lam[c]);
-    for (int b = blockIdx.y; b < p.B; b += gridDim.y) {
-        const int s = p.slots ? p.slots[b] : b;
+    for (unsigned at_b = blockIdx.y; at_b < (unsigned)p.B; at_b += gridDim.y) {          // (an int would wrap: 2^31 - 1 entries are allowed)
+        const int b = (int)at_b, s = p.slots ? p.slots[b] : b;
         float h = 0.0f;
         if (s >= 0 && s < p.pool) {
             float *at = p.h + (long long)s * p.C + c;

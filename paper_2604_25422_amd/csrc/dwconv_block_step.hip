@@ -154,8 +154,8 @@ template <typename T> __global__ __launch_bounds__(256) void conv_step_long_kern
     const int lane = threadIdx.x & 63, c = (int)((blockIdx.x * 256u + threadIdx.x) >> 6);
     if (c >= p.C) return;
     const T *w = p.w + (long long)c * p.K;
-    for (int b = blockIdx.y; b < p.B; b += gridDim.y) {
-        const int s = p.slots ? p.slots[b] : b;
+    for (unsigned at_b = blockIdx.y; at_b < (unsigned)p.B; at_b += gridDim.y) {          // (an int would wrap: 2^31 - 1 entries are allowed)
+        const int b = (int)at_b, s = p.slots ? p.slots[b] : b;
         float sum = 0.0f;
         if (s >= 0 && s < p.pool) {
             T *ring = p.ring + ((long long)s * p.C + c) * p.K;
@@ -183,8 +183,8 @@ template <typename T> struct ConvRing {
 template <typename T> __global__ __launch_bounds__(256) void conv_ring_kernel(ConvRing<T> p)
 {
     const long long per = (long long)p.C * p.K;
-    for (int b = blockIdx.y; b < p.B; b += gridDim.y) {
-        const int s = p.slots ? p.slots[b] : b;
+    for (unsigned at_b = blockIdx.y; at_b < (unsigned)p.B; at_b += gridDim.y) {          // (an int would wrap: 2^31 - 1 entries are allowed)
+        const int b = (int)at_b, s = p.slots ? p.slots[b] : b;
         if (s < 0 || s >= p.pool) continue;
         int n = p.lengths ? p.lengths[b] : p.L;
         n = n < 0 ? 0 : n > p.L ? p.L : n;

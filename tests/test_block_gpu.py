@@ -583,6 +583,48 @@ def test_conv_step_at_any_position():
         assert torch.equal(r[b].double().cpu(), full)
 
 
+# ---- as many entries as a batch may have ----
+
+def _most(value, dtype):
+    """One value for 2^31 - 1 entries of one channel."""
+    return torch.tensor([[value]], dtype=dtype, device="cuda").expand(2 ** 31 - 1, 1)
+
+
+def test_steps_of_the_largest_batch():
+    """Nearly all places empty: the last ones are what they are in a small batch, the others 0."""
+    B, used = 2 ** 31 - 1, [5, 0, -1, 2, 6]
+    n = len(used)
+    slots = torch.full((B,), -1, dtype=torch.int32, device="cuda")
+    slots[-n:] = torch.tensor(used, dtype=torch.int32, device="cuda")
+    few = slots[-n:].clone()
+    x, r, i = (_most(v, BF16) for v in (0.75, -0.5, 1.25))
+    lam, pool = torch.tensor([-5.0], device="cuda"), rand(7, 1, seed=1)
+    h, h2 = pool.clone(), pool.clone()
+    y = block.scan_step(x, r, i, lam, h, slots)
+    y2 = block.scan_step(x[:n], r[:n], i[:n], lam, h2, few)
+    assert torch.equal(y[-n:], y2) and torch.equal(h, h2) and y2.count_nonzero() == 4 and not y[:-n].any()
+    del y
+    pos = torch.zeros(B, dtype=torch.int32, device="cuda")
+    pos[-n:] = 11
+    for K in (3, 2500):
+        w, pool = rand(1, K, seed=2, dtype=BF16), rand(7, 1, K, seed=3, dtype=BF16)
+        ring, ring2 = pool.clone(), pool.clone()
+        y = block.conv_step(x, w, ring, pos, slots)
+        y2 = block.conv_step(x[:n], w, ring2, pos[-n:], few)
+        assert torch.equal(y[-n:], y2) and torch.equal(ring, ring2) and y2.count_nonzero() == 4 and not y[:-n].any()
+        del y
+    ring, ring2 = pool.clone(), pool.clone()
+    block.conv_ring(x[..., None], ring, pos, slots)
+    block.conv_ring(x[:n, :, None], ring2, pos[-n:], few)
+    assert torch.equal(ring, ring2) and not torch.equal(ring, pool)
+
+
+def test_norm_of_the_largest_batch():
+    res, one = _most(-3.0, BF16)[..., None], torch.ones(1, device="cuda")
+    _, n, _ = block.norm_fwd(None, None, res, None, one, save=False)
+    assert bool((n == -1).all())
+
+
 # ---- together ----
 
 def test_a_token_in_a_graph():
