@@ -122,7 +122,8 @@ template <int P> struct GateGrads {
     float e[P];         // dq q = g e
     float rest[P];      // dr = dq q rest
 };
-// First half: everything but e, of which it leaves q a in e and a / (1 - a^2) u in gi's place until the states are known.
+// First half: everything but e = q a (a / (1 - a^2) u - h), of which it leaves q a in e and the other product in pull until the states are
+// known.  (a / (1 - a^2) u alone may overflow where a gate is nearly shut; q times it does not.)
 template <bool NEAR, typename V, int P>
 __device__ __forceinline__ void grads_begin(const V &x, const V &r, const V &i, float rho, int left, GateGrads<P> &w, float (&u)[P], float (&pull)[P])
 {
@@ -137,8 +138,8 @@ __device__ __forceinline__ void grads_begin(const V &x, const V &r, const V &i, 
         w.in[k] = s * over;
         u[k] = w.in[k] * x[k];
         w.gi[k] = u[k] * rest_i;
-        pull[k] = w.a[k] * (over * x[k]);
         w.e[k] = q * w.a[k];
+        pull[k] = w.e[k] * over * (w.a[k] * x[k]);
     }
     if (left < P) {
 #pragma unroll
@@ -157,7 +158,7 @@ template <int P> __device__ __forceinline__ void grads_end(GateGrads<P> &w, cons
 {
 #pragma unroll
     for (int k = 0; k < P; ++k) {
-        w.e[k] *= pull[k] - h;
+        w.e[k] = fmaf(-w.e[k], h, pull[k]);
         h = fmaf(w.a[k], h, u[k]);
     }
 }

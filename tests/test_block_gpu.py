@@ -165,6 +165,27 @@ def test_scan_of_extreme_gates(L):
         ref.check(v, want[k], 6 * err[k], F32, k, floor=2.0 ** -60 * float(want[k].abs().max()))
 
 
+@pytest.mark.parametrize("L", [1, 30, 700, 9000])
+@pytest.mark.parametrize("logit", [-200.0, -80.0, -60.0])
+def test_scan_of_large_inputs_behind_shut_gates(logit, L):
+    """x beyond 2^64 where the decay's gate is shut: 1 / sqrt(1 - a^2) times it does not fit fp32, the gradients do."""
+    x, r, i, dy, lam = scan_inputs(2, 3, L, F32, 65)
+    at = L // 2
+    x[:, 1, at], r[:, 1, at] = torch.tensor([4e27, -3e30], device="cuda"), logit
+    h0, dh = rand(2, 3, seed=1), rand(2, 3, seed=2)
+    want, err = ref.scan(x, r, i, lam, h0, None, RATE, dy, dh)
+    y, h_last, states = block.scan_fwd(x, r, i, lam, h0)
+    got = dict(zip(("dx", "dr", "di", "dlam", "dh0"), block.scan_bwd(dy, x, r, i, lam, states, dh)), y=y, h_last=h_last)
+    # (a logit v puts |v| roundings of the exponential's argument on top of the 40 of an ordinary gate)
+    for k, v in got.items():
+        c = (slice(1, 2),) if k == "dlam" else (slice(None), slice(1, 2))
+        o = ([0, 2],) if k == "dlam" else (slice(None), [0, 2])
+        ref.check(v[o], want[k][o], err[k][o], F32, k)
+        assert torch.isfinite(v[c]).all(), k
+        if logit > -87:                         # (beyond, the open part of the gate is below the smallest fp32 number: 0)
+            ref.check(v[c], want[k][c], 6 * err[k][c], F32, k, floor=max(1e-30, 2.0 ** -60 * float(want[k][c].abs().max())))
+
+
 @pytest.mark.parametrize("L", [30, 700, 9000])
 def test_scan_keeps_bad_values_in_their_row(L):
     x, r, i, dy, lam = scan_inputs(2, 3, L, F32, 71)
