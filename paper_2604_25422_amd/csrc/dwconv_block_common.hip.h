@@ -293,13 +293,13 @@ template <bool NEAR> __device__ __forceinline__ float decay(float q, float &E)
 }
 
 // log(1 + e) with e = exp(v), once per row.  e through an exponent in two parts; log(1 + e) as log(u) e / (u - 1) with the rounded
-// u = 1 + e, which is e where u is 1: what u has lost of e is lost in u - 1 as well.
+// u = 1 + e, which is e where u is 1: what u has lost of e is lost in u - 1 as well.  (Of minus infinity e is 0, and so is the result.)
 __device__ __forceinline__ float softplus(float v)
 {
     const float t = v * kLog2e, lo = fmaf(v, kLog2e, -t) + v * 1.925963033e-8f;         // log2(e) = kLog2e + 1.9e-8
     const float h = exp2_hw(t), e = fmaf(h, lo * 0.6931471806f, h), u = 1.0f + e;
     const float l = __builtin_amdgcn_logf(u) * 0.6931471806f * (e / (u - 1.0f));
-    return v > 20.0f ? v : u == 1.0f ? e : l;
+    return v > 20.0f ? v : h == 0.0f ? 0.0f : u == 1.0f ? e : l;
 }
 
 // ---- lanes ----

@@ -165,6 +165,36 @@ def test_scan_of_extreme_gates(L):
         ref.check(v, want[k], 6 * err[k], F32, k, floor=2.0 ** -60 * float(want[k].abs().max()))
 
 
+@pytest.mark.parametrize("L", [1, 5, 30, 700, 40000])
+def test_scan_of_infinite_decay_parameters(L):
+    """lam of minus infinity: no decay and no input, the state goes through; of plus infinity: the state is the input of the position."""
+    inf = float("inf")
+    x, r, i, dy, lam = scan_inputs(2, 4, L, F32, 67)
+    lam[1], lam[3] = -inf, inf
+    h0, dh = rand(2, 4, seed=1), rand(2, 4, seed=2)
+    y, h, states = block.scan_fwd(x, r, i, lam, h0)
+    dx, dr, di, dlam, dh0 = block.scan_bwd(dy, x, r, i, lam, states, dh)
+    assert (y[:, 1] == h0[:, 1, None]).all() and torch.equal(h[:, 1], h0[:, 1])
+    for t in (dx, dr, di):
+        assert (t[:, 1] == 0).all()
+    want, err = ref.scan(x[:, :3], r[:, :3], i[:, :3], lam[:3], h0[:, :3], None, RATE, dy[:, :3], dh[:, :3])
+    for k, v in dict(y=y, h_last=h, dx=dx, dr=dr, di=di, dh0=dh0).items():
+        ref.check(v[:, :3], want[k], err[k], F32, k)
+    ref.check(dlam[:3], want["dlam"], err["dlam"], F32, "dlam")
+    # (q is infinite: a is 0 and sqrt(1 - a^2) 1)
+    xi = x[:, 3].double().cpu() * torch.sigmoid(i[:, 3].double().cpu())
+    ref.check(y[:, 3], xi, 40 * ref.U * xi.abs(), F32, "y")
+    assert (dr[:, 3] == 0).all() and dlam[3] == 0 and (dh0[:, 3] == 0).all()
+    g = dy[:, 3].double().cpu()
+    g[:, -1] += dh[:, 3].double().cpu()
+    ref.check(dx[:, 3], g * torch.sigmoid(i[:, 3].double().cpu()), 40 * ref.U * g.abs(), F32, "dx")
+    ref.check(di[:, 3], g * xi * torch.sigmoid(-i[:, 3].double().cpu()), 40 * ref.U * (g * xi).abs(), F32, "di")
+    tok = [t[..., 0].contiguous() for t in (x, r, i)]
+    pool = h0.clone()
+    y1 = block.scan_step(*tok, lam, pool)
+    assert torch.equal(y1[:, 1], h0[:, 1]) and torch.equal(pool[:, 1], h0[:, 1]) and torch.isfinite(y1).all()
+
+
 @pytest.mark.parametrize("L", [1, 30, 700, 9000])
 @pytest.mark.parametrize("logit", [-200.0, -80.0, -60.0])
 def test_scan_of_large_inputs_behind_shut_gates(logit, L):
