@@ -625,9 +625,15 @@ PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
     Args g;
     const auto listed = [](PyObject *o) { return PyList_CheckExact(o) || PyTuple_CheckExact(o); };
     if (n != 4 || !blk.clip || !listed(a[0]) || (a[2] != Py_None && !listed(a[2]))) return decline();
-    const Py_ssize_t count = PySequence_Fast_GET_SIZE(a[0]);
-    if (count < 1 || count > INT_MAX || (a[2] != Py_None && PySequence_Fast_GET_SIZE(a[2]) != count)) return decline();
-    PyObject **in = PySequence_Fast_ITEMS(a[0]), **out = a[2] == Py_None ? in : PySequence_Fast_ITEMS(a[2]);
+    // (the lists' own items for the whole call: the caller holds the lists only, which other threads may change while the lock is away)
+    struct Held {
+        PyObject *items;
+        ~Held() { Py_XDECREF(items); }
+    } grads{PySequence_Tuple(a[0])}, outs{a[2] == Py_None || !grads.items ? nullptr : PySequence_Tuple(a[2])};
+    if (!grads.items || (a[2] != Py_None && !outs.items)) return nullptr;
+    const Py_ssize_t count = PyTuple_GET_SIZE(grads.items);
+    if (count < 1 || count > INT_MAX || (outs.items && PyTuple_GET_SIZE(outs.items) != count)) return decline();
+    PyObject **in = PySequence_Fast_ITEMS(grads.items), **out = outs.items ? PySequence_Fast_ITEMS(outs.items) : in;
     if (!g.call.begin(in[0])) return g.call.bad() ? nullptr : decline();
     std::vector<const void *> from(count);
     std::vector<void *> to(count);

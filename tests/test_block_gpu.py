@@ -794,6 +794,41 @@ def test_native_calls_take_what_they_should(monkeypatch):
         call()
 
 
+@pytest.mark.parametrize("given", [False, True])
+def test_native_clipping_holds_what_it_works_on(given):
+    """Lists that lose their tensors while the call runs, as another thread's clear() does where the interpreter's lock is away: the tensors live on
+    until the call is through.  (The query of the current device is Python that the call runs; it empties the lists here.)"""
+    import ctypes
+
+    lib = block.lib()
+    fast = binding._fast
+    assert fast is not binding._Declines
+    values = [rand(n, seed=n) for n in (5000, 17, 300)]
+    norm, f = clip_ref(values, 1.0)
+    grads, outs = [v.clone() for v in values], [torch.empty_like(v) for v in values]
+    kept = torch.empty(sum(v.numel() for v in values), device="cuda")
+    if not given:                               # (in place: views of one tensor, which shows what has been written)
+        grads = list(kept.split([v.numel() for v in values]))
+        for g, v in zip(grads, values):
+            g.copy_(v)
+    else:
+        outs = list(kept.split([v.numel() for v in values]))
+
+    def current_device():
+        grads.clear(), outs.clear()
+        [torch.zeros(n, device="cuda") for n in (5000, 17, 300)]
+        return binding._current_device()
+    addresses = [ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in ("dwconv_fwd", "dwconv_bwd_input", "dwconv_bwd_weight", "dwconv_bwd")]
+    fast.setup(*addresses, current_device, binding._raw_stream, binding._check)
+    try:
+        got = fast.clip_grad_norm(grads, 1.0, outs if given else None, None)
+    finally:
+        fast.setup(*addresses, binding._current_device, binding._raw_stream, binding._check)
+    assert grads == [] and got is not None and abs(float(got) - norm) <= ref.U * norm
+    want = torch.cat(values).double().cpu() * f
+    ref.check(kept, want, want.abs() * 2 * ref.U, F32, "out")
+
+
 def test_the_example_learns_and_serves():
     """Convolution, scan, norms and clipping in one model: its loss falls, and what it says token by token is what it says of the whole
     sequence.  (Logits of a model of this width pass some thousand 32-bit operations in another order: 2^-14 of the largest.)"""
