@@ -378,13 +378,13 @@ struct Args {
         ok = ok && (o == Py_True || o == Py_False);
         return o == Py_True;
     }
-    // A workspace of the caller's; None: of `need` bytes, made later.
+    // A workspace of the caller's; None: of `need` bytes, made later.  (An empty one is no request for another: block.py's turn.)
     void *workspace(PyObject *o, size_t &bytes)
     {
         bytes = 0;
         if (!ok || o == Py_None) return nullptr;
         const at::Tensor *t = plain(o, -1, call.device);
-        ok = t != nullptr;
+        ok = t && t->nbytes() > 0;
         if (!ok) return nullptr;
         bytes = t->nbytes();
         return t->mutable_data_ptr();

@@ -794,6 +794,27 @@ def test_native_calls_take_what_they_should(monkeypatch):
         call()
 
 
+@pytest.mark.parametrize("native", [True, False])
+def test_an_empty_workspace_is_too_small(native, monkeypatch):
+    """Refused by both forms of the calls, and taken where none is needed."""
+    block.lib()
+    if not native:
+        monkeypatch.setattr(block, "_fast", block._Declines)
+    x, r, i, dy, lam = scan_inputs(2, 3, 20, F32, 1)
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    y, h, states = block.scan_fwd(x, r, i, lam, workspace=none)
+    assert torch.equal(y, block.scan_fwd(x, r, i, lam)[0])
+    c = torch.ones(3, device="cuda")
+    stats = block.norm_fwd(x, r, i, c, c)[2]
+    long = [torch.zeros(1, 1, 1 << 16, device="cuda") for _ in range(3)]
+    assert block.scan_workspace_bytes(1, 1, 1 << 16, False) > 0
+    for call in (lambda: block.scan_fwd(*long, lam[:1], workspace=none), lambda: block.scan_bwd(dy, x, r, i, lam, states, workspace=none),
+                 lambda: block.norm_bwd(None, dy, x, r, i, c, c, stats, workspace=none), lambda: block.clip_grad_norm([x], 1.0, workspace=none)):
+        with pytest.raises(binding.DwconvError) as e:
+            call()
+        assert e.value.status == 5
+
+
 @pytest.mark.parametrize("given", [False, True])
 def test_native_clipping_holds_what_it_works_on(given):
     """Lists that lose their tensors while the call runs, as another thread's clear() does where the interpreter's lock is away: the tensors live on
