@@ -25,10 +25,12 @@ typedef unsigned uintx4_any __attribute__((ext_vector_type(4), aligned(2)));
 // Eight consecutive elements as loaded.
 template <typename T> struct Eight;
 template <> struct Eight<float> {
+    typedef float type;
     floatx4_any lo, hi;
     __device__ __forceinline__ float operator[](int k) const { return k < 4 ? lo[k] : hi[k - 4]; }
 };
 template <> struct Eight<bf16_t> {
+    typedef bf16_t type;
     uintx4_any w;
     __device__ __forceinline__ float operator[](int k) const
     {
@@ -97,6 +99,7 @@ template <int BYTES> struct Words { typedef unsigned type __attribute__((ext_vec
 template <> struct Words<2> { typedef unsigned short type; };
 template <> struct Words<4> { typedef unsigned type __attribute__((aligned(2))); };
 template <int P, typename T> struct Few {
+    typedef T type;
     T v[P];
     __device__ __forceinline__ float operator[](int k) const { return ld_elem(v + k); }
 };
@@ -252,16 +255,36 @@ constexpr float kLog2e = 1.44269504088896341f;
 __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
 __device__ __forceinline__ float rcp_hw(float v) { return __builtin_amdgcn_rcpf(v); }
 
-// 1 / (1 + exp(-v)).  (exp overflows to infinity below -88, whose reciprocal is the 0 that is meant.)
-__device__ __forceinline__ float sigmoid(float v) { return rcp_hw(1.0f + exp2_hw(v * -kLog2e)); }
+// What the rounded argument t of exp2 leaves of exp(-v) = exp2(t) exp(rest): about |v| 2^-24, which is as many roundings of a gate as the
+// logit has units.  (Held to a finite value, so that infinite logits do what they should; where they are large nothing depends on it.)
+__device__ __forceinline__ float rest_of_exp(float v, float t) { return __builtin_amdgcn_fmed3f(fmaf(t, -0.6931471806f, -v), -0x1p-10f, 0x1p-10f); }
 
-// sigmoid(v), and 1 - sigmoid(v) = e / (1 + e) with e = exp(-v), without the cancellation.  Where e overflows sigmoid(v) is 0 and the
-// other no number that a product with it depends on, but finite; a NaN stays one in both.
-__device__ __forceinline__ float sigmoid_both(float v, float &rest)
+// 1 / (1 + exp(-v)) of a logit of type T.  (exp overflows to infinity below -88, whose reciprocal is the 0 that is meant.)  To first order
+// exp(rest) moves it by sigmoid (1 - sigmoid) rest.  Of a bf16 logit that is left out: its own rounding is 2^15 times as much, and the bf16
+// kernels' time is their instructions'.
+template <typename T> __device__ __forceinline__ float sigmoid(float v)
 {
-    const float e = exp2_hw(v * -kLog2e), s = rcp_hw(1.0f + e);
-    rest = fminf(e, 3e38f) * s;
-    return s;
+    const float t = v * -kLog2e, s = rcp_hw(1.0f + exp2_hw(t));
+    if constexpr (sizeof(T) == 2) return s;
+    else return fmaf(fmaf(s, s, -s), rest_of_exp(v, t), s);
+}
+
+// sigmoid(v), and 1 - sigmoid(v) = e / (1 + e) with e = exp(-v), without the cancellation.  Where e overflows sigmoid(v) is 0 (in fp32 at most
+// the reciprocal of 3e38) and the other no number that a product with it depends on, but finite; a NaN stays one in both.
+template <typename T> __device__ __forceinline__ float sigmoid_both(float v, float &other)
+{
+    const float t = v * -kLog2e, e = exp2_hw(t);
+    if constexpr (sizeof(T) == 2) {
+        const float s = rcp_hw(1.0f + e);
+        other = fminf(e, 3e38f) * s;
+        return s;
+    } else {
+        float m = e > 3e38f ? 3e38f : e;
+        m = fmaf(m, rest_of_exp(v, t), m);
+        const float s = rcp_hw(1.0f + m);
+        other = m * s;
+        return s;
+    }
 }
 
 // exp(-q) - 1 for 0 <= q < 1/2: x + x^2 (the quotient (exp(x) - 1 - x) / x^2 as the polynomial of degree four through its

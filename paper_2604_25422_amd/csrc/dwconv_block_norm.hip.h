@@ -212,7 +212,7 @@ template <typename T, int E, int NT, int NB, bool BLOCK, bool SHORT> __global__ 
             o[e][k] = res[e][k];
             if constexpr (BLOCK) {
                 const float zz = z[e][k];
-                o[e][k] = fmaf(zz * sigmoid(zz), y[e][k] * r1[k] * w[e], o[e][k]);
+                o[e][k] = fmaf(zz * sigmoid<T>(zz), y[e][k] * r1[k] * w[e], o[e][k]);
             }
             r2[k] = fmaf(o[e][k], o[e][k], r2[k]);
         }
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(NT * NB, BLOCK && NB == 1 && sizeof(T) == 2 && E ==
             float v = res[e][k], q = 0.0f;
             const float dnw = dn[e][k] * wn;
             if constexpr (BLOCK) {
-                const float s = sigmoid(z[e][k]);
+                const float s = sigmoid<T>(z[e][k]);
                 if constexpr (KEEP) g[e][k] = s;
                 q = z[e][k] * s * y[e][k] * w;
                 v = fmaf(r1[k], q, v);
@@ -400,7 +400,7 @@ __global__ __launch_bounds__(NT * NB, BLOCK && NB == 1 && sizeof(T) == 2 && E ==
         for (int k = 0; k < V; ++k) {
             float v = res[e][k], s = 0.0f, silu = 0.0f, gated = 0.0f;
             if constexpr (BLOCK) {
-                s = KEEP ? g[KEEP ? e : 0][k] : sigmoid(z[e][k]), silu = z[e][k] * s, gated = silu * y[e][k];
+                s = KEEP ? g[KEEP ? e : 0][k] : sigmoid<T>(z[e][k]), silu = z[e][k] * s, gated = silu * y[e][k];
                 v = fmaf(r1[k], gated * w, v);
             }
             const float now = fmaf(r2[k], fmaf(v, m2[k], dn[e][k] * wn), dout[e][k]);
@@ -530,7 +530,7 @@ template <typename T, int E, bool BLOCK> __global__ __launch_bounds__(64) void n
                 o[e][k] = res[e][k];
                 if constexpr (BLOCK) {
                     const float zz = z[e][k];
-                    o[e][k] = fmaf(zz * sigmoid(zz), y[e][k] * r1 * (p.scale * w[e][k]), o[e][k]);
+                    o[e][k] = fmaf(zz * sigmoid<T>(zz), y[e][k] * r1 * (p.scale * w[e][k]), o[e][k]);
                 }
                 r2 = fmaf(o[e][k], o[e][k], r2);
             }
@@ -582,7 +582,7 @@ template <typename T, bool BLOCK> __global__ __launch_bounds__(256) void norm_fw
             float v = ld_elem(p.res.row(b, c, p.L) + t);
             if constexpr (BLOCK) {
                 const float zz = ld_elem(p.z.row(b, c, p.L) + t);
-                v = fmaf(zz * sigmoid(zz), ld_elem(p.y.row(b, c, p.L) + t) * r1 * (p.scale * p.w[c]), v);
+                v = fmaf(zz * sigmoid<T>(zz), ld_elem(p.y.row(b, c, p.L) + t) * r1 * (p.scale * p.w[c]), v);
             }
             return v;
         };
@@ -629,7 +629,7 @@ template <typename T, bool BLOCK> __global__ __launch_bounds__(256) void norm_bw
             if constexpr (BLOCK) {
                 h.z = ld_elem(p.z.row(b, c, p.L) + t);
                 h.yh = ld_elem(p.y.row(b, c, p.L) + t) * r1;
-                h.g = sigmoid_both(h.z, h.rest);
+                h.g = sigmoid_both<T>(h.z, h.rest);
                 v = fmaf(h.z * h.g, h.yh * (p.scale * p.w[c]), v);
             }
             h.oh = v * r2;

@@ -70,8 +70,8 @@ __device__ __forceinline__ void gates(const V &x, const V &r, const V &i, float 
 #pragma unroll
     for (int k = 0; k < P; ++k) {
         float E;
-        a[k] = decay<NEAR>(rho * sigmoid(r[k]), E);
-        u[k] = __builtin_amdgcn_sqrtf(-E * (2.0f + E)) * sigmoid(i[k]) * x[k];
+        a[k] = decay<NEAR>(rho * sigmoid<typename V::type>(r[k]), E);
+        u[k] = __builtin_amdgcn_sqrtf(-E * (2.0f + E)) * sigmoid<typename V::type>(i[k]) * x[k];
     }
     if (left < P) {
 #pragma unroll
@@ -130,7 +130,7 @@ __device__ __forceinline__ void grads_begin(const V &x, const V &r, const V &i, 
 #pragma unroll
     for (int k = 0; k < P; ++k) {
         float rest_i, E;
-        const float q = rho * sigmoid_both(r[k], w.rest[k]), si = sigmoid_both(i[k], rest_i);
+        const float q = rho * sigmoid_both<typename V::type>(r[k], w.rest[k]), si = sigmoid_both<typename V::type>(i[k], rest_i);
         w.a[k] = decay<NEAR>(q, E);
         // beta^2 = s, and 1 / beta of s held to the smallest normal number, so that a beta of 0 stays 0 (a NaN stays in s itself);
         // a u / (1 - a^2) = a x sigmoid(i) / beta
@@ -371,7 +371,7 @@ __global__ __launch_bounds__(64 * (BATCH ? BATCH : W * scan_rows(W))) void scan_
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     float E;
-                    w.a[k] = decay<false>(rho * sigmoid(rn[k]), E);
+                    w.a[k] = decay<false>(rho * sigmoid<T>(rn[k]), E);
                     if (k >= n - t) w.a[k] = 1.0f;
                 }
                 if (more) dn = load_row8(dy, tn, p.L), rn = load_row8(r, tn, p.L);
@@ -571,8 +571,8 @@ template <typename T> __global__ __launch_bounds__(256) void scan_step_kernel(Sc
         if (s >= 0 && s < p.pool) {
             float *at = p.h + (long long)s * p.C + c;
             float E;
-            const float a = decay<false>(rho * sigmoid(ld_elem(p.r.row(b, c, 1))), E);
-            const float u = __builtin_amdgcn_sqrtf(-E * (2.0f + E)) * sigmoid(ld_elem(p.i.row(b, c, 1))) * ld_elem(p.x.row(b, c, 1));
+            const float a = decay<false>(rho * sigmoid<T>(ld_elem(p.r.row(b, c, 1))), E);
+            const float u = __builtin_amdgcn_sqrtf(-E * (2.0f + E)) * sigmoid<T>(ld_elem(p.i.row(b, c, 1))) * ld_elem(p.x.row(b, c, 1));
             h = fmaf(a, *at, u);
             *at = h;
         }

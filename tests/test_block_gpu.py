@@ -216,6 +216,42 @@ def test_scan_of_large_inputs_behind_shut_gates(logit, L):
             ref.check(v[c], want[k][c], 6 * err[k][c], F32, k, floor=max(1e-30, 2.0 ** -60 * float(want[k][c].abs().max())))
 
 
+@pytest.mark.parametrize("wide", ["r", "i"])
+def test_scan_of_wide_logits_is_exact(wide):
+    """fp32 gates as exact at logits of -75 to 60 as at small ones, in rows of one position, where nothing else adds up.  A gate, and 1 minus it:
+    exponential and reciprocal within a unit (U), five roundings (U / 2).  q: 5 U of exp(lam) and its logarithm on top; sqrt(1 - a^2) and
+    its reciprocal have half of that and 2 U of their own.  So y and dx stay below 16 U of themselves, di below 22 U, dr below 32 U."""
+    B, C = 512, 96
+    x, r, i, dy, lam = scan_inputs(B, C, 1, F32, 85)
+    span = torch.linspace(-75, 60, B * C)[torch.randperm(B * C, generator=torch.Generator().manual_seed(3))].view(B, C, 1).cuda()
+    r, i = (span, i) if wide == "r" else (r, span)
+    want, _ = ref.scan(x, r, i, lam, None, None, RATE, dy)
+    y, h, states = block.scan_fwd(x, r, i, lam)
+    dx, dr, di, _, _ = block.scan_bwd(dy, x, r, i, lam, states)
+    pool = torch.zeros(B, C, device="cuda")
+    step = block.scan_step(x[..., 0], r[..., 0], i[..., 0], lam, pool)[..., None]
+    for k, v, units in (("y", y, 16), ("y", step, 16), ("dx", dx, 16), ("di", di, 22), ("dr", dr, 32)):
+        ref.check(v, want[k], units * ref.U * want[k].abs(), F32, k, floor=0.0)
+
+
+@pytest.mark.parametrize("C,L", [(64, 1), (64, 3), (64, 40), (5000, 2)])
+def test_norm_of_wide_logits_is_exact(C, L):
+    """silu(z) alone (y and w are 1, res 0), whose gate is within 5 U: with the product, the norm of y and the last sum below 9 U."""
+    B = 8
+    z = torch.linspace(-75, 60, B * C * L)[torch.randperm(B * C * L, generator=torch.Generator().manual_seed(3))].view(B, C, L).cuda()
+    one, w = torch.ones_like(z), torch.ones(C, device="cuda")
+    out, _, stats = block.norm_fwd(one, z, torch.zeros_like(z), w, w, eps=1e-30)
+    want = z.double().cpu() * torch.sigmoid(z.double().cpu())
+    ref.check(out, want, 9 * ref.U * want.abs(), F32, "out", floor=0.0)
+    # (dw of one entry and position is dout silu(z): dn is 0)
+    dout = rand(1, C, 1, seed=4)
+    part = z[:1, :, :1].contiguous()
+    _, _, s1 = block.norm_fwd(one[:1, :, :1].contiguous(), part, torch.zeros_like(part), w, w, eps=1e-30)
+    dw = block.norm_bwd(dout, torch.zeros_like(dout), one[:1, :, :1].contiguous(), part, torch.zeros_like(part), w, w, s1)[3]
+    want = dout[0, :, 0].double().cpu() * want[0, :, 0]
+    ref.check(dw, want, 12 * ref.U * want.abs(), F32, "dw", floor=0.0)
+
+
 @pytest.mark.parametrize("L", [30, 700, 9000])
 def test_scan_keeps_bad_values_in_their_row(L):
     x, r, i, dy, lam = scan_inputs(2, 3, L, F32, 71)
