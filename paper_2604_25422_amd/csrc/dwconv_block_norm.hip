@@ -84,8 +84,8 @@ size_t red_bytes(const NormPlan &s, int V, int sums) { return (size_t)(s.NT / 16
 
 // Rows of sums: one a tile, or a workgroup of tiles of short rows or of the streaming kernel.
 int sum_rows(const NormPlan &s) { return s.E && !s.short_rows ? (int)s.tiles : s.blocks; }
-// Runs that they are first added up in (4096 sums of 768 channels twice: 18 us by norm_sums_kernel alone); 0: not worth it.
-int sum_runs(const NormPlan &s) { return sum_rows(s) >= 65536 ? 512 : sum_rows(s) >= 512 ? 64 : 0; }
+// (4096 rows of 768 channels twice: 18 us by norm_sums_kernel alone)
+int runs_of(const NormPlan &s) { return sum_runs(sum_rows(s), 512); }
 
 template <typename T, int E, bool BLOCK> void fwd_tile(const NormFwd<T> &p, const NormPlan &s, hipStream_t st)
 {
@@ -169,16 +169,16 @@ template <typename T, bool BLOCK> void launch_bwd(const NormBwd<T> &p, const Nor
     }
     const float *part = p.part;
     int M = sum_rows(s);
-    if (const int runs = sum_runs(s)) {
+    if (const int runs = runs_of(s)) {
         float *to = p.part + (size_t)M * 2 * p.C;
-        norm_runs_kernel<<<dim3((unsigned)ceil_div(2ll * p.C, 64), runs), 256, 0, st>>>(part, M, (int)ceil_div(M, runs), 2 * p.C, to);
+        sum_runs_kernel<<<dim3((unsigned)ceil_div(2ll * p.C, 64), runs), 256, 0, st>>>(part, M, ceil_div(M, runs), 2 * p.C, to);
         part = to;
         M = runs;
     }
     norm_sums_kernel<<<dim3((unsigned)ceil_div(p.C, 32), 2), 1024, 0, st>>>(part, M, p.C, dw, dw_next);
 }
 
-size_t part_bytes(const NormPlan &s, int C) { return (size_t)(sum_rows(s) + sum_runs(s)) * 2 * C * sizeof(float); }
+size_t part_bytes(const NormPlan &s, int C) { return (size_t)(sum_rows(s) + runs_of(s)) * 2 * C * sizeof(float); }
 
 template <typename T>
 void run_fwd(const dwconv_seq &y, const dwconv_seq &z, const dwconv_seq &res, const float *w, const float *w_next, const dwconv_seq_out &out,

@@ -8,7 +8,7 @@
 // order.  Parameter gradients are summed over the positions of a lane and the lanes of a row; further launches add the tiles' sums.
 // Tiles of short rows (NB > 1) belong to a wave or two, several to a workgroup; rows of less than a pack (SHORT) are loaded in parts.
 #pragma once
-#include "dwconv_block_common.hip.h"
+#include "dwconv_block_sums.hip.h"
 
 namespace dwconv {
 
@@ -671,20 +671,6 @@ template <typename T, bool BLOCK> __global__ __launch_bounds__(256) void norm_bw
     }
 }
 
-// Many workgroups leave many sums: runs of `rows` of them added up by workgroups of their own first.
-__global__ __launch_bounds__(256) void norm_runs_kernel(const float *part, int M, int rows, int N, float *runs)
-{
-    __shared__ float sums[4][64];
-    const int tc = threadIdx.x & 63, tm = threadIdx.x >> 6, c = blockIdx.x * 64 + tc, from = blockIdx.y * rows, to = from + rows < M ? from + rows : M;
-    float sum = 0.0f;
-    if (c < N) {
-#pragma unroll 8
-        for (int m = from + tm; m < to; m += 4) sum += part[(long long)m * N + c];
-    }
-    sums[tm][tc] = sum;
-    __syncthreads();
-    if (tm == 0 && c < N) runs[(long long)blockIdx.y * N + c] = (sums[0][tc] + sums[1][tc]) + (sums[2][tc] + sums[3][tc]);
-}
 // dw and dw_next: the workgroups' sums in a fixed order.
 __global__ __launch_bounds__(1024) void norm_sums_kernel(const float *part, int M, int C, float *dw, float *dw_next)
 {

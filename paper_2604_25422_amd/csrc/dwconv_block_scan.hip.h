@@ -18,7 +18,7 @@
 // loads that ask where the row ends), and neighbouring rows go to one die, whose cache puts the lines together that they share
 // (L504 260 us, 356 with rows dealt out in turn).
 #pragma once
-#include "dwconv_block_common.hip.h"
+#include "dwconv_block_sums.hip.h"
 
 namespace dwconv {
 
@@ -42,7 +42,7 @@ template <typename T> struct ScanBwd {
     const float *lam, *states, *dh_last;
     const int *lengths;
     SeqOut<T> dx, dr, di;
-    float *dh0, *part;          // part: sums towards dlam, [B * segs, C]
+    float *dh0, *part;          // part: sums towards dlam, of rows' segments [B * segs, C] or workgroups of short rows
     float *dlam;                // of workgroups that have a channel's whole batch
     Span *spans;
     int B, C, L, nstates;
@@ -516,18 +516,14 @@ template <typename T, int G, int P> __global__ __launch_bounds__(256) void scan_
         if (t == 0 && p.dh0) p.dh0[row] = front;
     }
     sum = group_sum<G>(sum);
-    if (!p.dlam) {
-        if (t == 0 && !idle) p.part[((long long)blockIdx.y * m.nb + sub) * p.C + c] = sum;
-        return;
-    }
-    // (the workgroup has had the whole batch of its channels)
     __shared__ float sums[256 / G];
     if (t == 0) sums[g] = sum;
     __syncthreads();
     if (t == 0 && sub == 0 && !idle) {
         sum = 0.0f;
         for (int k = 0; k < m.nb; ++k) sum += sums[k * m.cb + g];
-        p.dlam[c] = sum * dlam_factor(p.lam[c]);
+        if (p.dlam) p.dlam[c] = sum * dlam_factor(p.lam[c]);            // (the workgroup has had the whole batch of its channels)
+        else p.part[(long long)blockIdx.y * p.C + c] = sum;
     }
 }
 

@@ -95,6 +95,26 @@ def test_scan_short_rows_of_many_lengths(L, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,C,L", [(4000, 40, 5), (4000, 7, 100), (5000, 3, 300), (66000, 1, 257)])
+def test_scan_sums_of_many_rows(B, C, L, dtype):
+    """dlam over more rows than one launch adds up: in runs, of few and of many."""
+    x, r, i, dy, lam = scan_inputs(B, C, L, dtype, 63)
+    check_scan(x, r, i, dy, lam, rand(B, C, seed=1), rand(B, C, seed=2))
+
+
+@pytest.mark.parametrize("B,C,L", [(1 << 21, 1, 1), (1 << 21, 32, 1), (1 << 18, 32, 8), (1 << 18, 1, 300), (100000, 2, 300), (60000, 1, 257), (11000, 32, 257)])
+def test_scan_sums_of_many_rows_in_short_chains(B, C, L):
+    """The same row B times over (stride 0): its terms round alike, so a chain of additions shows its length.  No term passes 400 of them."""
+    x, r, i, dy, lam = scan_inputs(1, C, L, F32, 64)
+    _, _, states = block.scan_fwd(x, r, i, lam)
+    one = block.scan_bwd(dy, x, r, i, lam, states)[3].double()
+    x, r, i, dy = (t.expand(B, C, L) for t in (x, r, i, dy))
+    _, _, states = block.scan_fwd(x, r, i, lam)
+    dlam = block.scan_bwd(dy, x, r, i, lam, states)[3].double()
+    assert ((dlam - B * one).abs() <= 400 * 2.0 ** -24 * B * one.abs()).all(), float((dlam / (B * one) - 1).abs().max())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("L", [5, 100, 700, 5000, 33000])
 def test_scan_masked_rows(L, dtype):
     """Sequences of no position, one, all, and lengths outside [0, L]; what lies behind an end is not read."""
