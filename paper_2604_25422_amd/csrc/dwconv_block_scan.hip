@@ -17,7 +17,6 @@ struct ScanPlan {
 };
 constexpr int kScanBatch = 8;   // rows of a channel that one workgroup takes so
 
-// (the sizes of workspaces go by segs and M, which do not depend on the type)
 ScanPlan plan_scan(int B, int C, int L, int dtype, bool backward)
 {
     ScanPlan s{};
@@ -59,9 +58,14 @@ ScanPlan plan_scan(int B, int C, int L, int dtype, bool backward)
         return s;
     }
     // Few long rows are cut into segments for the whole chip to work at them, though a first pass then forms the gates of all but one a
-    // second time: B1 C32 L40000 fp32 12.4 us forward (17.2 whole), 18.3 backward (32.7); B2 C64 L65537 bf16 45 us backward (58),
-    // but 30 us forward (26.5 whole, half of the chip idle).
-    if (rows < (backward ? 129 : 128) && chunks > (backward ? 32 : 64)) {
+    // second time.  Whole rows take what one of them takes until every CU has one, cut ones what all of them hold and a launch more, so
+    // where they meet hardly depends on the length (us whole / cut, tensors that are in no cache; forward bf16 L65537 128 rows 35.0 / 34.4, 144 35.3
+    // / 36.6, L131072 96 rows 46.3 / 43.0, 112 47.2 / 49.0; fp32 L65537 80 rows 37.1 / 36.3, 96 39.2 / 40.7; backward bf16 L20000 64 rows 18.2 / 16.7,
+    // 80 18.8 / 19.1, L33000 128 rows 29.9 / 29.3, 144 30.3 / 31.2, L131072 160 rows 88.4 / 86.5, 176 89.1 / 93.9; fp32 L20000 80 rows 24.1 / 23.6, 96 24.7
+    // / 25.4, L65537 128 rows 71.4 / 69.0, 160 77.6 / 83.6).
+    const bool f32 = dtype == DWCONV_F32;
+    const long long limit = !backward ? (f32 ? 84 : 114) : f32 ? 135 * (chunks - 10) / chunks : 200 * (chunks - 22) / chunks;
+    if (rows < limit && chunks > (backward ? 32 : 64)) {
         const long long most = std::min<long long>(kScanSegments, chunks);
         s.W = 1;
         while (s.W < 8 && rows * most * s.W < 4096 && most * s.W < chunks) s.W *= 2;
@@ -74,7 +78,7 @@ ScanPlan plan_scan(int B, int C, int L, int dtype, bool backward)
         // one, backward 183 and 195; bf16, bound by the gates: 55 and 57, 101 and 136), but not with one group for a row
         // backward (B64 C768 L1024 fp32 260 us with one, 275 with two).
         const long long want = backward ? 2048 : 4096;
-        const int most = backward ? 8 : 16, rich = dtype == DWCONV_F32 ? 4 : 1;
+        const int most = backward ? 8 : 16, rich = f32 ? 4 : 1;
         s.W = 1;
         while (s.W < most && s.W < chunks && rows * s.W < want) s.W *= 2;
         while (s.W < rich && s.W * (backward ? 2 : 1) < chunks) s.W *= 2;
@@ -180,8 +184,12 @@ int dwconv_scan_states(int L) { return L < 1 || L > (1 << 30) ? 0 : (int)ceil_di
 size_t dwconv_scan_workspace_bytes(int B, int C, int L, int backward)
 {
     if (check_dims(B, C, L) != DWCONV_OK) return 0;
-    const ScanPlan s = plan_scan(B, C, L, DWCONV_F32, backward != 0);
-    return span_bytes(s, B, C) + (backward ? part_bytes(s, C) : 0);
+    size_t most = 0;                    // (of either type)
+    for (const int dtype : {DWCONV_F32, DWCONV_BF16}) {
+        const ScanPlan s = plan_scan(B, C, L, dtype, backward != 0);
+        most = std::max(most, span_bytes(s, B, C) + (backward ? part_bytes(s, C) : 0));
+    }
+    return most;
 }
 
 int dwconv_scan_fwd(dwconv_seq x, dwconv_seq r, dwconv_seq i, const float *lam, const float *h0, const int *lengths, dwconv_seq_out y,

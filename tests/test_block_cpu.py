@@ -228,3 +228,19 @@ def test_norm_workspace_of_many_tiles_is_bounded(lib):
     for B, L in ((1 << 30, 5), (1 << 22, 4), (1 << 22, 64)):
         assert 0 < lib.dwconv_norm_workspace_bytes(B, 1, L, 0) <= 1100 * 2 * 4
     assert lib.dwconv_norm_workspace_bytes((1 << 22) - 1, 1, 4, 0) >= 2 * 4 * ((1 << 22) - 1)
+
+
+def test_few_long_rows_are_cut_where_that_takes_less(lib):
+    """By what the workspace has room for: the spans of segments, 8 bytes each.  (Of 65537 positions cut rows take less up to some 115
+    rows forward and 175 backward in bf16, fewer in fp32, whose workspace is the same.)"""
+    whole = lambda rows: 4 * rows                               # noqa: E731  (a sum a row towards dlam)
+    for rows in (1, 64, 104):
+        assert lib.dwconv_scan_workspace_bytes(1, rows, 65537, 0) >= 8 * rows * 32
+    for rows in (120, 127, 128, 300):
+        assert lib.dwconv_scan_workspace_bytes(1, rows, 65537, 0) == 0
+    for rows in (1, 64, 128, 144, 160):
+        assert lib.dwconv_scan_workspace_bytes(1, rows, 65537, 1) >= 8 * rows * 32
+    for rows in (192, 256, 320):
+        assert lib.dwconv_scan_workspace_bytes(1, rows, 65537, 1) == whole(rows)
+    for rows, L in ((112, 20000), (128, 20000), (1, 16384), (1, 512)):
+        assert lib.dwconv_scan_workspace_bytes(1, rows, L, 1) == (whole(rows) + 15) // 16 * 16

@@ -115,6 +115,20 @@ def test_scan_sums_of_many_rows_in_short_chains(B, C, L):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,C,L", [(1, 100, 33300), (3, 45, 33300), (1, 100, 17000)])
+def test_scan_of_rows_that_one_type_or_pass_cuts(B, C, L, dtype):
+    """Few long rows, cut into segments by one type or direction and whole in the other, in a workspace of the size that is asked for."""
+    x, r, i, dy, lam = scan_inputs(B, C, L, dtype, 66)
+    h0, dh = rand(B, C, seed=1), rand(B, C, seed=2)
+    space = [torch.full((block.scan_workspace_bytes(B, C, L, k),), 255, dtype=torch.uint8, device="cuda") for k in (False, True)]
+    want, err = ref.scan(x, r, i, lam, h0, None, RATE, dy, dh)
+    y, h_last, states = block.scan_fwd(x, r, i, lam, h0, workspace=space[0])
+    got = dict(zip(("dx", "dr", "di", "dlam", "dh0"), block.scan_bwd(dy, x, r, i, lam, states, dh, workspace=space[1])), y=y, h_last=h_last)
+    for k, v in got.items():
+        ref.check(v, want[k], err[k], v.dtype, k)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("L", [5, 100, 700, 5000, 33000])
 def test_scan_masked_rows(L, dtype):
     """Sequences of no position, one, all, and lengths outside [0, L]; what lies behind an end is not read."""
