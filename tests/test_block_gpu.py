@@ -458,6 +458,23 @@ def test_norm_of_short_rows(C, L, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("C", [1, 63, 64, 65, 127, 128, 129, 200])
+@pytest.mark.parametrize("L", [1, 2])
+@pytest.mark.parametrize("B", [1023, 1024, 1500])
+def test_norm_of_one_or_two_positions_of_many_entries(B, C, L, dtype):
+    """On both sides of 1024 entries and of 128 channels, where tiles of a wave take over from other kernels; the last workgroup with fewer tiles than
+    it has room for (1023, 1500) and not."""
+    y, z, res, dout, dn, w, wn = norm_inputs(B, C, L, dtype)
+    for d, a in ((dout, (y, z, res, w, wn)), (None, (None, None, res, None, wn))):
+        want, err = ref.norm(*a, eps=1e-5, scale=0.5, dout=d, dn=dn)
+        out, n, stats = block.norm_fwd(*a, eps=1e-5, scale=0.5)
+        got = dict(zip(("dy", "dz", "dres", "dw", "dw_next"), block.norm_bwd(d, dn, *a, stats, scale=0.5)), out=out, n=n)
+        for k, v in got.items():
+            if v is not None:
+                ref.check(v, want[k], err[k], v.dtype, k)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("B,C,L", [(70000, 3, 9), (300000, 2, 3)])
 def test_norm_of_very_many_tiles(B, C, L, dtype):
     """Sums over more tiles than the first of their two launches has few runs for."""
