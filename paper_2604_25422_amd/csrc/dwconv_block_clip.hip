@@ -189,7 +189,6 @@ int dwconv_clip_grad_norm(const void *const *in, void *const *out, const long lo
     if (!in || !out || !sizes || !dtypes || !norm) return DWCONV_ERR_NULL;
     if (count < 1) return DWCONV_ERR_SHAPE;
     if (!(max_norm > 0.0f && max_norm < INFINITY)) return DWCONV_ERR_VALUE;
-    long long launches = 1;
     for (int k = 0; k < count; ++k) {
         if (sizes[k] < 0 || sizes[k] > (1ll << 40)) return DWCONV_ERR_SHAPE;
         if (!dtype_ok(dtypes[k])) return DWCONV_ERR_DTYPE;
@@ -200,7 +199,7 @@ int dwconv_clip_grad_norm(const void *const *in, void *const *out, const long lo
     if (!aligned_to(norm, 4)) return DWCONV_ERR_ALIGN;
     if (!workspace || workspace_bytes < dwconv_clip_workspace_bytes() || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
     static thread_local ClipTable t;
-    launches = 0;
+    long long launches = 0;
     for (int k = 0; k < count || launches == 0; ++launches) k = fill_table(t, in, out, sizes, dtypes, k, count);
     if (launches > kClipSums) return DWCONV_ERR_SHAPE;
     const hipStream_t st = static_cast<hipStream_t>(stream);

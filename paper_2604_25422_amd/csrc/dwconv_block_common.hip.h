@@ -39,59 +39,28 @@ template <> struct Eight<bf16_t> {
     }
 };
 
-// Elements p[0 .. 7] of which the first `left` may be read; the others count as zeros.
-__device__ __forceinline__ Eight<float> load8(const float *p, int left)
+// Eight elements, all of which are there.
+__device__ __forceinline__ Eight<float> load8(const float *p)
 {
     Eight<float> e;
-    if (left >= 8) {
-        e.lo = *reinterpret_cast<const floatx4_any *>(p);
-        e.hi = *reinterpret_cast<const floatx4_any *>(p + 4);
-    } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            e.lo[k] = k < left ? p[k] : 0.0f;
-            e.hi[k] = k + 4 < left ? p[k + 4] : 0.0f;
-        }
-    }
+    e.lo = *reinterpret_cast<const floatx4_any *>(p);
+    e.hi = *reinterpret_cast<const floatx4_any *>(p + 4);
     return e;
 }
-__device__ __forceinline__ Eight<bf16_t> load8(const bf16_t *p, int left)
+__device__ __forceinline__ Eight<bf16_t> load8(const bf16_t *p)
 {
     Eight<bf16_t> e;
-    if (left >= 8) {
-        e.w = *reinterpret_cast<const uintx4_any *>(p);
-    } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const unsigned lo = 2 * k < left ? p[2 * k].bits : 0u, hi = 2 * k + 1 < left ? p[2 * k + 1].bits : 0u;
-            e.w[k] = lo | (hi << 16);
-        }
-    }
+    e.w = *reinterpret_cast<const uintx4_any *>(p);
     return e;
 }
-
-// Eight outputs, of which the first `left` lie inside the row.
-__device__ __forceinline__ void store8(float *p, const float (&v)[8], int left)
+__device__ __forceinline__ void store8(float *p, const float (&v)[8])
 {
-    if (left >= 8) {
-        *reinterpret_cast<floatx4_any *>(p) = floatx4_any{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<floatx4_any *>(p + 4) = floatx4_any{v[4], v[5], v[6], v[7]};
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k < left) p[k] = v[k];
-    }
+    *reinterpret_cast<floatx4_any *>(p) = floatx4_any{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<floatx4_any *>(p + 4) = floatx4_any{v[4], v[5], v[6], v[7]};
 }
-__device__ __forceinline__ void store8(bf16_t *p, const float (&v)[8], int left)
+__device__ __forceinline__ void store8(bf16_t *p, const float (&v)[8])
 {
-    if (left >= 8) {
-        *reinterpret_cast<uintx4_any *>(p) =
-            uintx4_any{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k < left) st_elem(p + k, v[k]);
-    }
+    *reinterpret_cast<uintx4_any *>(p) = uintx4_any{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
 }
 
 // A row of L <= P elements that one lane holds: one access for a row of P, or one for each power of two in L.
@@ -202,7 +171,7 @@ __device__ __forceinline__ void store_pack_streaming(bf16_t *p, const float (&v)
 
 // Eight elements of a row of L >= 8 around position t: where it has fewer from there on, its last eight, which move_down() puts right.
 // (Loads that ask first would make a wave wait for each before the next.)
-template <typename T> __device__ __forceinline__ Eight<T> load_row8(const T *row, int t, int L) { return load8(row + (t < L - 8 ? t : L - 8), 8); }
+template <typename T> __device__ __forceinline__ Eight<T> load_row8(const T *row, int t, int L) { return load8(row + (t < L - 8 ? t : L - 8)); }
 // The eight elements `by` places on, zeros behind the last (0 < by < 8).
 __device__ __forceinline__ void move_down(Eight<float> &e, int by)
 {
@@ -221,7 +190,7 @@ __device__ __forceinline__ void move_down(Eight<bf16_t> &e, int by)
 __device__ __forceinline__ void store_row8(float *row, const float (&v)[8], int t, int L)
 {
     if (t + 8 <= L) {
-        store8(row + t, v, 8);
+        store8(row + t, v);
     } else if (t < L) {
         float *p = row + t;
         floatx4_any f = {v[0], v[1], v[2], v[3]};
@@ -234,7 +203,7 @@ __device__ __forceinline__ void store_row8(float *row, const float (&v)[8], int 
 __device__ __forceinline__ void store_row8(bf16_t *row, const float (&v)[8], int t, int L)
 {
     if (t + 8 <= L) {
-        store8(row + t, v, 8);
+        store8(row + t, v);
     } else if (t < L) {
         typedef unsigned uintx2_any __attribute__((ext_vector_type(2), aligned(2)));
         typedef unsigned uint_any __attribute__((aligned(2)));

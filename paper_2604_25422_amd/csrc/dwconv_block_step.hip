@@ -37,7 +37,7 @@ __device__ __forceinline__ void load_wide(float (&v)[4], const bf16_t *p)
 }
 __device__ __forceinline__ void load_wide(float (&v)[8], const bf16_t *p)
 {
-    const Eight<bf16_t> u = load8(p, 8);
+    const Eight<bf16_t> u = load8(p);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = u[k];
 }
