@@ -248,7 +248,7 @@ template <typename T> __device__ __forceinline__ float sigmoid_both(float v, flo
         other = fminf(e, 3e38f) * s;
         return s;
     } else {
-        float m = e > 3e38f ? 3e38f : e;
+        float m = __builtin_elementwise_minimum(e, 3e38f);      // (a NaN stays)
         m = fmaf(m, rest_of_exp(v, t), m);
         const float s = rcp_hw(1.0f + m);
         other = m * s;
