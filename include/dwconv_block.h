@@ -42,7 +42,8 @@ typedef struct dwconv_seq_out {
  * lengths[b] held to [0, L]; y is 0 from n on, whatever x, r and i hold there.  h_last [B, C] fp32 or NULL: h[n-1] (h0 where n = 0).
  * states [B, C, dwconv_scan_states(L)] fp32 or NULL: h before every 512th position, which dwconv_scan_bwd takes.
  * workspace: dwconv_scan_workspace_bytes(...) bytes, 16-byte aligned; NULL where that is 0.  rate > 0 and finite.
- * What is not finite in x, r or i stays in its own row (b, c), at its position and behind it.
+ * lam may be infinite: minus infinity is a = 1 and u = 0.  What is not finite in x, r or i stays in its own row (b, c), at its position
+ * and behind it up to n.
  */
 DWCONV_API int dwconv_scan_fwd(dwconv_seq x, dwconv_seq r, dwconv_seq i, const float *lam, const float *h0, const int *lengths,
                                dwconv_seq_out y, float *h_last, float *states, void *workspace, size_t workspace_bytes,
@@ -64,7 +65,7 @@ DWCONV_API int dwconv_scan_bwd(dwconv_seq dy, dwconv_seq x, dwconv_seq r, dwconv
 /* States of a row that dwconv_scan_fwd keeps for the backward pass: ceil(L / 512); 0 on bad arguments. */
 DWCONV_API int dwconv_scan_states(int L);
 
-/* Workspace of dwconv_scan_fwd (backward = 0) and dwconv_scan_bwd (backward = 1); may be 0, as it is on bad arguments. */
+/* Workspace of dwconv_scan_fwd (backward = 0) and dwconv_scan_bwd (backward = 1) of either type; may be 0, as it is on bad arguments. */
 DWCONV_API size_t dwconv_scan_workspace_bytes(int B, int C, int L, int backward);
 
 /*
@@ -81,7 +82,8 @@ DWCONV_API int dwconv_scan_step(dwconv_seq x, dwconv_seq r, dwconv_seq i, const 
  *     out = res + scale * silu(z) * (y / sqrt(m1 + eps)) * w[c],      n = out / sqrt(m2 + eps) * w_next[c]
  * y, z, res in, out, n out: [B, C, L]; w, w_next [C] fp32; scale finite, eps > 0.  Both means are of unrounded values.
  * Without a block in front of the norm (y, z, w and out all NULL): n is the norm of res.
- * stats [B, 2, L] fp32 or NULL: 1 / sqrt(m1 + eps) and 1 / sqrt(m2 + eps), which dwconv_norm_bwd takes.
+ * stats [B, 2, L] fp32 or NULL: 1 / sqrt(m1 + eps) and 1 / sqrt(m2 + eps), which dwconv_norm_bwd takes (without a block only the second
+ * is written).
  * What is not finite stays at its own (b, t).
  */
 DWCONV_API int dwconv_norm_fwd(dwconv_seq y, dwconv_seq z, dwconv_seq res, const float *w, const float *w_next,
@@ -104,7 +106,8 @@ DWCONV_API size_t dwconv_norm_workspace_bytes(int B, int C, int L, int dtype);
  * Global norm of `count` dense tensors and clipping: total = sqrt(sum of all squares, in 64 bits),
  *     out[k] = in[k] * min(1, max_norm / (total + 1e-6)),     *norm = total (one fp32 value on the device).
  * in, out (the same pointers: in place), sizes (elements; 0 is allowed), dtypes: arrays of `count` in HOST memory, read before
- * the call returns.  count >= 1, max_norm > 0.  A total that is not finite gives the factor that the formula gives: 0 for
+ * the call returns.  count >= 1, max_norm > 0 and finite (the largest finite value: the norm alone, nothing is scaled unless that
+ * exceeds it).  A total that is not finite gives the factor that the formula gives: 0 for
  * infinity (0 * inf is NaN), NaN for NaN.  workspace: dwconv_clip_workspace_bytes(), 16-byte aligned.
  */
 DWCONV_API int dwconv_clip_grad_norm(const void *const *in, void *const *out, const long long *sizes, const int *dtypes, int count,

@@ -287,7 +287,8 @@ def _dense(t: torch.Tensor) -> bool:
 
 def clip_grad_norm(grads, max_norm: float, out=None, workspace=None) -> torch.Tensor:
     """Scales all tensors of ``grads`` (fp32 or bf16, any mixture, dense) by min(1, max_norm / (norm + 1e-6)), norm the 2-norm of
-    everything in them: in place, or into the tensors of ``out``, laid out alike.  Returns norm, an fp32 scalar on the GPU."""
+    everything in them: in place, or into the tensors of ``out``, laid out alike.  max_norm is positive and finite (the largest fp32 value:
+    the norm alone).  Returns norm, an fp32 scalar on the GPU."""
     done = _fast.clip_grad_norm(grads, max_norm, out, workspace)
     if done is not None:
         return done

@@ -6,7 +6,8 @@
 // nor vanishes there, and the order of additions does not show.  The tensors' addresses go with the launch as kernel arguments:
 // nothing is copied to the device, and nothing is remembered from call to call.
 //
-// 48 fp32 tensors of 189 MB: 33 us and 61 us, 5.7 and 6.2 TB/s; memory is what bounds both.  Whole pieces keep all their loads in flight,
+// 48 fp32 tensors of 189 MB: 35 us and 62 us, 5.4 and 6.1 TB/s, bf16 ones of 94 MB 19 and 34 us, 5.1 and 5.6 TB/s; memory is what bounds
+// both, and that the second reads what the first has read.  Whole pieces keep all their loads in flight,
 // so do the last ones of a tensor (by element they had made bf16 tensors of 94 MB 64 us instead of 52).  The scaled elements
 // are stored past the caches, which leaves the gradients that the first kernel has read in the last-level cache for the second
 // (121 us with ordinary stores).

@@ -257,7 +257,7 @@ template <typename T> __device__ __forceinline__ float sigmoid_both(float v, flo
 }
 
 // exp(-q) - 1 for 0 <= q < 1/2: x + x^2 (the quotient (exp(x) - 1 - x) / x^2 as the polynomial of degree four through its
-// Chebyshev nodes on [-1/2, 0]), 0.7e-7 of the result at most.
+// Chebyshev nodes on [-1/2, 0]), 0.8e-7 of the result at most.
 __device__ __forceinline__ float expm1_small(float q)
 {
     const float x = -q;

@@ -239,12 +239,12 @@ template <typename T, int E, int NT, int NB, bool BLOCK, bool SHORT> __global__ 
 }
 
 // Both means of a position come from four sums that one pass over the tile forms at once; a second pass has the gradients.  Memory
-// bounds it where a CU has several tiles at work (B32 C256 L4097 fp32 250 us, 4.3 TB/s; B256 C192 L1024 bf16 179 us, 4.5 TB/s) and the
+// bounds it where a CU has several tiles at work (B32 C256 L4097 fp32 249 us, 4.3 TB/s; B256 C192 L1024 bf16 166 us, 4.8 TB/s) and the
 // registers where it has one (B128 C768 L1024 bf16 410 us with the sums, 3.9 TB/s): 60 instructions an element then stand
 // between a tile's loads and its stores, so they are cut where they can be: the rms factors come in behind the sums, and with
 // five packs a lane or more, which a SIMD has two waves of in any case, the gates of the first pass stay for the second (B128 C768
 // 434 -> 414 us).  Three packs of bf16 fit into a SIMD's registers four times only if r2 is read twice and instructions move
-// in steps of two elements (B256 C96 L1024 126 -> 94 us).
+// in steps of two elements (B256 C96 L1024 126 -> 91 us).
 template <typename T, int E, int NT, int NB, bool BLOCK, bool SHORT>
 __global__ __launch_bounds__(NT * NB, BLOCK && NB == 1 && sizeof(T) == 2 && E == 3 ? 4 : 1) void norm_bwd_tile_kernel(NormBwd<T> p)
 {
@@ -451,8 +451,8 @@ __global__ __launch_bounds__(NT * NB, BLOCK && NB == 1 && sizeof(T) == 2 && E ==
 }
 
 // One position a batch entry (a token of every sequence): the channels are next to each other, four to a lane and E times round the
-// wave, which needs no other one.  B64 C768 bf16 3.0 us (5.1 by the streaming
-// kernel below): one trip to memory and two sums.
+// wave, which needs no other one.  B64 C768 bf16 3.0 to 3.6 us (5.1 by the
+// streaming kernel below): one trip to memory and two sums.
 template <typename T> struct Four;
 template <> struct Four<float> {
     floatx4_any w;
@@ -552,7 +552,8 @@ template <typename T, int E, bool BLOCK> __global__ __launch_bounds__(64) void n
 }
 
 // Any C and L: a lane per position, 2^lx of them side by side, the channels over the other lanes, the tensors read again for
-// every sum (from the caches, where a tile still is).  red: [4][64] floats.
+// every sum (from the caches, where a tile still is): forward y three times, z and res twice, backward in three passes 14 values for 5
+// (B4096 C768 L1 bf16 49 us).  red: [4][64] floats.
 __device__ __forceinline__ float channel_sum(float v, int lx, float *red)
 {
     const int x = threadIdx.x & ((1 << lx) - 1), lane = threadIdx.x & 63;

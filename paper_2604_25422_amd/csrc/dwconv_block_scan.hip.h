@@ -12,11 +12,11 @@
 // the gates' gradients need is formed again from x, r, i and the state in front of each chunk, which the forward pass keeps (one
 // fp32 for 512 positions): nothing of it is rounded to the storage type, and the kernel reads four tensors instead of five.
 //
-// Memory bounds the fp32 forms (B32 C256 L4096 forward 94 us, 5.7 TB/s; backward 177 us, 5.3 TB/s) and, with the instructions of
-// the gates nearly as long, the bf16 ones (B128 C768 L1024 forward 157 to 175 us, backward 285 to 307 us, 4.6 to 4.9 TB/s).  Rows of any
-// length: those that end inside a lane's eight load their last eight and move them (B287 C480 L511 bf16 backward 282 us, 425 with
-// loads that ask where the row ends), and neighbouring rows go to one die, whose cache puts the lines together that they share
-// (L504 260 us, 356 with rows dealt out in turn).
+// Memory bounds the fp32 forms (B32 C256 L4096 forward 95 to 105 us, 5.1 to 5.7 TB/s; backward 168 to 183 us, 5.1 to 5.6 TB/s) and, with the
+// instructions of the gates nearly as long, the bf16 ones (B128 C768 L1024 forward 155 to 176 us, backward 283 to 315 us, 4.5 to 5.1
+// TB/s).  Rows of any length: those that end inside a lane's eight load their last eight and move them (B287 C480 L511 bf16 backward
+// 269 us, 425 with loads that ask where the row ends), and neighbouring rows go to one die, whose cache puts the lines together that
+// they share (L504 239 us, 356 with rows dealt out in turn).
 #pragma once
 #include "dwconv_block_sums.hip.h"
 
@@ -438,8 +438,8 @@ __global__ __launch_bounds__(64 * (BATCH ? BATCH : W * scan_rows(W))) void scan_
     }
 }
 
-// Rows of at most 8 G positions: groups of G lanes, or a lane with P positions (B100000 C96 L1 bf16 forward 68 us, 149 us as a lane with
-// eight positions of which one is there; L4 forward 90 and 194 us, backward 163 and 338).  The rows of a workgroup are `cb` channels of `nb` batch entries at a time, its
+// Rows of at most 8 G positions: groups of G lanes, or a lane with P positions (B100000 C96 L1 bf16 forward 69 us, 149 us as a lane with
+// eight positions of which one is there; L4 forward 81 and 194 us, backward 134 and 338).  The rows of a workgroup are `cb` channels of `nb` batch entries at a time, its
 // lanes keep their channel; blockIdx.y and steps of gridDim.y walk the batch.
 struct ShortRows {
     int cb, nb;

@@ -52,8 +52,9 @@ __device__ __forceinline__ int ring_place(int pos, unsigned inverse, int K)
 // 2^lg lanes for each (b, c), each with V neighbouring places of the ring at a time.  Place k holds tap (k - p - 1) mod K, so the
 // taps a lane needs are V neighbours, rotated by the sequence's position: the workgroup's channels' taps lie in LDS, their first
 // V - 1 once more behind the last, and one staging serves every sequence the workgroup walks, U of them in flight.  Few values pass
-// through (13 MB for B256 C768 K32 bf16, 8.7 us): what it takes is a chain of three loads (slot, ring, store) and the
-// instructions around them; large pools are read at 3.1 TB/s (B1024 C512 K64 fp32 44 us).
+// through (13 MB for B256 C768 K32 bf16, 8.9 us): what it takes is a chain of three loads (slot, ring, store) and the
+// instructions around them; large pools are read at 2.9 TB/s (B1024 C512 K64 fp32 48 us; 59 of slots in any order), a round's
+// chain behind the one before.
 template <typename T, int V, int U> __global__ __launch_bounds__(256) void conv_step_kernel(ConvStep<T> p, int lg, unsigned inverse)
 {
     extern __shared__ float taps[];
@@ -218,9 +219,9 @@ template <typename T, int V> void launch_step(const ConvStep<T> &p, hipStream_t 
         conv_step_long_kernel<<<dim3((unsigned)ceil_div((long long)p.C * 64, 256), (unsigned)std::min(p.B, 65535)), 256, 0, st>>>(p);
         return;
     }
-    // Sequences in flight: one where waves are few and their own work is the wait (B256 C768 K4 bf16 3.6 us, 3.9 with two, 4.8 with
-    // four; B1 C256 K64 fp32 2.6, 2.8, 3.5), two in between (B256 C768 K32 bf16 9.8, 8.7, 9.8), four for large pools (B1024 C512
-    // K64 fp32 52, 47, 44).
+    // Sequences in flight: one where waves are few and their own work is the wait (B256 C768 K4 bf16 3.7 us, 4.0 with two, 5.0 with
+    // four; B1 C256 K64 fp32 2.7, 2.8, 3.5), two in between (B256 C768 K32 bf16 9.9, 8.9, 10.1), four for large pools (B1024 C512
+    // K64 fp32 52, 49, 48).
     const double n = (double)p.B * p.C * p.K;
     if (n < 2 << 20) launch_rows<T, V, 1>(p, lg, lds, st);
     else if (n < 16 << 20) launch_rows<T, V, 2>(p, lg, lds, st);

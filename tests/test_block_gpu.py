@@ -882,6 +882,24 @@ def test_native_calls_take_what_they_should(monkeypatch):
 
 
 @pytest.mark.parametrize("native", [True, False])
+def test_clip_for_the_norm_alone(native, monkeypatch):
+    """The largest finite limit scales nothing; an infinite one is refused, by both forms of the calls."""
+    block.lib()
+    if not native:
+        monkeypatch.setattr(block, "_fast", block._Declines)
+    grads = [rand(3000, seed=1) * 1e6, rand(70, seed=2, dtype=BF16)]
+    before, outs = [g.clone() for g in grads], [torch.full_like(g, float("nan")) for g in grads]
+    norm, f = clip_ref(grads, torch.finfo(F32).max)
+    assert f == 1
+    for out in (outs, None):
+        got = block.clip_grad_norm(grads, torch.finfo(F32).max, out=out)
+        assert abs(float(got) - norm) <= ref.U * norm
+        assert all(torch.equal(a, b) for a, b in zip(grads if out is None else out, before))
+    with pytest.raises(binding.DwconvError):
+        block.clip_grad_norm(grads, float("inf"))
+
+
+@pytest.mark.parametrize("native", [True, False])
 def test_an_empty_workspace_is_too_small(native, monkeypatch):
     """Refused by both forms of the calls, and taken where none is needed."""
     block.lib()
