@@ -1,7 +1,7 @@
 /*
  * dwconv_block.h -- C ABI of the operators around the depthwise convolution (dwconv.h) in a sequence block: a gated
- * linear recurrence along t (forward, backward, one token), the norms before and after a block fused with its gate and
- * residual (forward, backward), the global gradient norm with clipping, and the convolution's own form for one token.
+ * linear recurrence along t (forward, backward, one token), the gated delta rule (forward, backward, one token), the norms before and after a
+ * block fused with its gate and residual (forward, backward), dropout, the global gradient norm with clipping, and the convolution's own form for one token.
  *
  * The conventions of dwconv.h hold here too: device pointers on the current device, the caller owns every buffer,
  * nothing is allocated or synchronised, work is enqueued on `stream`, arguments are validated before any HIP call, the
@@ -131,6 +131,58 @@ DWCONV_API int dwconv_conv_step(dwconv_seq x, const void *w, void *ring, const i
  */
 DWCONV_API int dwconv_conv_ring(dwconv_seq x, void *ring, const int *lengths, const int *slots, int pool,
                                 int B, int C, int L, int K, int dtype, void *stream);
+
+/*
+ * Gated delta rule: a recurrence whose state is a matrix for every head.  With H heads of values, Hk of queries and keys (H a multiple
+ * of Hk; head h has those of h / (H / Hk)), a state S [DK, DV] of every (b, h), a log decay g and a strength beta of every position,
+ *     S <- exp(g[t]) S,   u = v[t] - S^T k[t],   S <- S + beta[t] k[t] u^T,   o[t] = scale S^T q[t]     for t = 0 .. n - 1.
+ * q, k [B, Hk * DK, L], v, o [B, H * DV, L] of `dtype`, head by head; g, beta [B, H, L] fp32 (dwconv_seq too).  eps > 0: q and k of a
+ * position are brought to unit length first, x / sqrt(|x|^2 + eps); eps = 0: taken as they are.  s0 [B, H, DK, DV] fp32 or NULL (zeros); lengths as in
+ * dwconv_scan_fwd (o is 0 from n on, whatever the inputs hold there); s_last [B, H, DK, DV] fp32 or NULL: the state behind n.
+ * states [B, H, dwconv_delta_states(L), DK, DV] fp32 or NULL: S in front of every 64th position, which dwconv_delta_bwd takes.
+ * DK at most 128, DV at most 65536, H at most 2^20.  g may be minus infinity (nothing in front of t is remembered).  Finite values whose results are
+ * finite give those; what is not finite may reach every position of its chunk of 64 and everything behind it, of its own head and of those that
+ * share its keys.
+ */
+DWCONV_API int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const float *s0, const int *lengths,
+                                dwconv_seq_out o, float *s_last, float *states, int B, int H, int Hk, int DK, int DV, int L, float scale,
+                                float eps, int dtype, void *stream);
+
+/*
+ * Gradients of the gated delta rule.  dout [B, H * DV, L]; ds_last [B, H, DK, DV] fp32 or NULL (zeros), the gradient of s_last; states as
+ * dwconv_delta_fwd left them for the same inputs.  dq, dk [B, Hk * DK, L] (of a shared key: summed over its heads, in order), dv [B, H * DV, L],
+ * dg, dbeta [B, H, L] fp32 (all 0 from n on), ds0 [B, H, DK, DV] fp32 or NULL.  workspace: dwconv_delta_workspace_bytes(...) bytes, 16-byte aligned.
+ * Where exp(g) is 0 in fp32, so is dg.
+ */
+DWCONV_API int dwconv_delta_bwd(dwconv_seq dout, dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const float *states,
+                                const float *ds_last, const int *lengths, dwconv_seq_out dq, dwconv_seq_out dk, dwconv_seq_out dv, float *dg,
+                                float *dbeta, float *ds0, void *workspace, size_t workspace_bytes, int B, int H, int Hk, int DK, int DV, int L,
+                                float scale, float eps, int dtype, void *stream);
+
+/* States of a head that dwconv_delta_fwd keeps for the backward pass: ceil(L / 64); 0 on bad arguments. */
+DWCONV_API int dwconv_delta_states(int L);
+
+/* Workspace of dwconv_delta_bwd; 0 on bad arguments. */
+DWCONV_API size_t dwconv_delta_workspace_bytes(int B, int H, int DK, int DV, int L);
+
+/*
+ * Gated delta rule, one token of every place b of the batch, on the states s [pool, H, DK, DV] fp32, which are updated in place; slots and pool
+ * as in dwconv_scan_step.  q, k [B, Hk * DK], v, o [B, H * DV], g, beta [B, H] fp32.
+ */
+DWCONV_API int dwconv_delta_step(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, float *s, const int *slots, int pool,
+                                 dwconv_seq_out o, int B, int H, int Hk, int DK, int DV, float scale, float eps, int dtype, void *stream);
+
+/*
+ * Dropout:  out = res + scale x / (1 - p) where an element is kept, res where it is not (whatever x holds there); res.data NULL: zeros for res.
+ * The same call on a gradient (without res) is the backward pass.  0 <= p < 1, scale finite; out may be x or res itself.
+ * An element is dropped when its 32 bits are below round(p 2^32), p as an fp32 value.  The bits are a function of rng [2] (int64 in DEVICE memory:
+ * a seed and a step, of which the lower 32 bits count; a captured graph draws another mask when the caller has changed them), of layer (0 .. 2^24 - 1,
+ * for the calls that share a seed and a step), of b and of j = c L + t, or with `tied` of j = c: whole channels are dropped.  With m = j >> 3 they
+ * come from philox4x32-10 with the key (seed low, seed high) and the counter (m low, b, step, layer << 8 | m high << 1 | half): the upper sixteen are
+ * half-word j & 7 of the block with half = 0, the lower sixteen that of the block with half = 1.
+ */
+DWCONV_API int dwconv_dropout(dwconv_seq x, dwconv_seq res, dwconv_seq_out out, const long long *rng, int layer, int B, int C, int L, float p,
+                              float scale, int tied, int dtype, void *stream);
 
 #ifdef __cplusplus
 }

@@ -1,8 +1,9 @@
 """The operators around the depthwise convolution in a sequence block, for torch device tensors: thin binding of the C ABI in
 ``include/dwconv_block.h`` (argument marshalling only, as ``binding`` is for the convolution itself).
 
-``scan_fwd`` / ``scan_bwd`` / ``scan_step``: a gated linear recurrence along t.  ``norm_fwd`` / ``norm_bwd``: the norms before
-and after a block with its gate and residual.  ``clip_grad_norm``: the global gradient norm and clipping.  ``conv_step`` /
+``scan_fwd`` / ``scan_bwd`` / ``scan_step``: a gated linear recurrence along t.  ``delta_fwd`` / ``delta_bwd`` / ``delta_step``: the gated
+delta rule, whose state is a matrix for every head.  ``norm_fwd`` / ``norm_bwd``: the norms before and after a block with its gate and residual.
+``dropout_fwd`` / ``dropout_bwd``: dropout from a counter-based generator.  ``clip_grad_norm``: the global gradient norm and clipping.  ``conv_step`` /
 ``conv_ring``: the causal convolution for one token.
 
 Sequences are [B, C, L] tensors whose positions are next to each other and whose channels lie L elements apart; the batch stride is
@@ -22,6 +23,7 @@ SYMBOLS = (
     "dwconv_scan_fwd", "dwconv_scan_bwd", "dwconv_scan_states", "dwconv_scan_workspace_bytes", "dwconv_scan_step",
     "dwconv_norm_fwd", "dwconv_norm_bwd", "dwconv_norm_workspace_bytes",
     "dwconv_clip_grad_norm", "dwconv_clip_workspace_bytes", "dwconv_conv_step", "dwconv_conv_ring",
+    "dwconv_delta_fwd", "dwconv_delta_bwd", "dwconv_delta_states", "dwconv_delta_workspace_bytes", "dwconv_delta_step", "dwconv_dropout",
 )
 
 
@@ -62,7 +64,13 @@ def lib():
                 ("dwconv_clip_grad_norm", [vp, vp, vp, vp, i, f, vp, vp, sz, vp], i),
                 ("dwconv_clip_workspace_bytes", [], sz),
                 ("dwconv_conv_step", [s, vp, vp, vp, vp, i, s, i, i, i, i, vp], i),
-                ("dwconv_conv_ring", [s, vp, vp, vp, i, i, i, i, i, i, vp], i)):
+                ("dwconv_conv_ring", [s, vp, vp, vp, i, i, i, i, i, i, vp], i),
+                ("dwconv_delta_fwd", [s, s, s, s, s, vp, vp, s, vp, vp, i, i, i, i, i, i, f, f, i, vp], i),
+                ("dwconv_delta_bwd", [s, s, s, s, s, s, vp, vp, vp, s, s, s, vp, vp, vp, vp, sz, i, i, i, i, i, i, f, f, i, vp], i),
+                ("dwconv_delta_states", [i], i),
+                ("dwconv_delta_workspace_bytes", [i, i, i, i, i], sz),
+                ("dwconv_delta_step", [s, s, s, s, s, vp, vp, i, s, i, i, i, i, i, f, f, i, vp], i),
+                ("dwconv_dropout", [s, s, s, vp, i, i, i, i, f, f, i, i, vp], i)):
             fn = getattr(l, name)
             fn.argtypes, fn.restype = args, res
         if binding._fast is not binding._Declines:
@@ -206,6 +214,123 @@ def scan_step(x, r, i, lam, h, slots=None, rate: float = 8.0, out=None):
     y, ys = _out(out, "out", shape, x)
     _check(lib().dwconv_scan_step(*ins, lamp, hp, sp, h.shape[0], ys, B, C, float(rate), code, _stream()))
     return y
+
+
+# ---- gated delta rule ----
+
+def delta_states(L: int) -> int:
+    """States of a head that ``delta_fwd`` keeps for ``delta_bwd``: one for every 64 positions."""
+    return int(lib().dwconv_delta_states(int(L)))
+
+
+def delta_workspace_bytes(B: int, H: int, DK: int, DV: int, L: int) -> int:
+    """Workspace of ``delta_bwd``."""
+    return int(lib().dwconv_delta_workspace_bytes(B, H, DK, DV, L))
+
+
+def _heads(q, v, g, key_heads, dims: int):
+    """(B, H, Hk, DK, DV) of a call: heads of values from the gate's channels, of keys as given."""
+    for t, name in ((q, "q"), (v, "v"), (g, "g")):
+        if t.dim() != dims:
+            raise ValueError(f"{name} must be a {'[B, channels, L]' if dims == 3 else '[B, channels]'} tensor")
+    B, H = int(g.shape[0]), int(g.shape[1])
+    Hk = H if key_heads is None else int(key_heads)
+    if H < 1 or Hk < 1 or H % Hk:
+        raise ValueError(f"{H} heads of values do not share {Hk} heads of keys evenly")
+    if q.shape[1] % Hk or v.shape[1] % H:
+        raise ValueError(f"q has {q.shape[1]} channels for {Hk} heads, v {v.shape[1]} for {H}")
+    return B, H, Hk, int(q.shape[1]) // Hk, int(v.shape[1]) // H
+
+
+def delta_fwd(q, k, v, g, beta, s0=None, lengths=None, key_heads=None, scale=None, eps: float = 1e-6, save: bool = True, out=None):
+    """The gated delta rule along t: with a state S [DK, DV] of every head, S <- exp(g) S, u = v - S^T k, S <- S + beta k u^T, o = scale S^T q.
+    q, k [B, key_heads * DK, L] and v [B, H * DV, L] of one type, g (log decays) and beta [B, H, L] fp32; H a multiple of key_heads (None: H),
+    neighbouring heads of values share one of keys.  scale None: DK^-1/2.  eps: q and k are brought to unit length, x / sqrt(|x|^2 + eps); 0: taken as
+    they are.  s0 [B, H, DK, DV] fp32 (None: zeros), lengths [B] int32 (None: L; o is 0 behind a sequence's end).
+    Returns (o, s_last, states): o like v, s_last [B, H, DK, DV] fp32, states what ``delta_bwd`` takes (None without ``save``)."""
+    scale = scale if scale is not None else _unit_scale(q, key_heads, g)
+    B, H, Hk, DK, DV = _heads(q, v, g, key_heads, 3)
+    L, code, keys, values = int(q.shape[2]), _dtype_code(q), (B, Hk * DK, q.shape[2]), (B, H * DV, q.shape[2])
+    ins = [_seq(q, "q", keys, q.dtype), _seq(k, "k", keys, q.dtype), _seq(v, "v", values, q.dtype),
+           _seq(g, "g", (B, H, L), torch.float32), _seq(beta, "beta", (B, H, L), torch.float32)]
+    sp, lp = _f32(s0, "s0", (B, H, DK, DV), True), _index(lengths, "lengths", B)
+    o, os_ = _out(out, "out", values, q)
+    s_last = torch.empty((B, H, DK, DV), dtype=torch.float32, device=q.device)
+    states = torch.empty((B, H, delta_states(L), DK, DV), dtype=torch.float32, device=q.device) if save else None
+    _check(lib().dwconv_delta_fwd(*ins, sp, lp, os_, s_last.data_ptr(), states.data_ptr() if save else None, B, H, Hk, DK, DV, L, float(scale),
+                                  float(eps), code, _stream()))
+    return o, s_last, states
+
+
+def delta_bwd(do, q, k, v, g, beta, states, ds_last=None, lengths=None, key_heads=None, scale=None, eps: float = 1e-6, out=None, workspace=None):
+    """Gradients of ``delta_fwd`` from do like v and ds_last [B, H, DK, DV] fp32 (None: zeros): returns (dq, dk, dv, dg, dbeta, ds0), the first
+    three like q, k, v (or into the three tensors of ``out``; those of a shared head of keys are summed over its heads), dg and dbeta [B, H, L] and
+    ds0 [B, H, DK, DV] fp32."""
+    given = out if out is not None else (None,) * 3
+    if len(given) != 3:
+        raise ValueError("out must be three tensors (dq, dk, dv)")
+    scale = scale if scale is not None else _unit_scale(q, key_heads, g)
+    B, H, Hk, DK, DV = _heads(q, v, g, key_heads, 3)
+    L, code, keys, values = int(q.shape[2]), _dtype_code(q), (B, Hk * DK, q.shape[2]), (B, H * DV, q.shape[2])
+    ins = [_seq(do, "do", values, q.dtype), _seq(q, "q", keys, q.dtype), _seq(k, "k", keys, q.dtype), _seq(v, "v", values, q.dtype),
+           _seq(g, "g", (B, H, L), torch.float32), _seq(beta, "beta", (B, H, L), torch.float32)]
+    sp = _f32(states, "states", (B, H, delta_states(L), DK, DV))
+    dsp, lp = _f32(ds_last, "ds_last", (B, H, DK, DV), True), _index(lengths, "lengths", B)
+    outs = [_out(t, n, shape, q) for t, n, shape in zip(given, ("dq", "dk", "dv"), (keys, keys, values))]
+    dg, dbeta = (torch.empty((B, H, L), dtype=torch.float32, device=q.device) for _ in range(2))
+    ds0 = torch.empty((B, H, DK, DV), dtype=torch.float32, device=q.device)
+    ws, nbytes, keep = _workspace(workspace, delta_workspace_bytes(B, H, DK, DV, L), q)
+    _check(lib().dwconv_delta_bwd(*ins, sp, dsp, lp, *(s for _, s in outs), dg.data_ptr(), dbeta.data_ptr(), ds0.data_ptr(), ws, nbytes, B, H, Hk, DK, DV,
+                                  L, float(scale), float(eps), code, _stream()))
+    return outs[0][0], outs[1][0], outs[2][0], dg, dbeta, ds0
+
+
+def delta_step(q, k, v, g, beta, s, slots=None, key_heads=None, scale=None, eps: float = 1e-6, out=None):
+    """One token of the gated delta rule for a batch: q, k [B, key_heads * DK], v [B, H * DV], g and beta [B, H] fp32; s [pool, H, DK, DV] fp32 is
+    updated in place, place b of the batch in row slots[b] as in ``scan_step``.  Returns o like v."""
+    scale = scale if scale is not None else _unit_scale(q, key_heads, g)
+    B, H, Hk, DK, DV = _heads(q, v, g, key_heads, 2)
+    code, keys, values = _dtype_code(q), (B, Hk * DK), (B, H * DV)
+    ins = [_seq(q, "q", keys, q.dtype), _seq(k, "k", keys, q.dtype), _seq(v, "v", values, q.dtype), _seq(g, "g", (B, H), torch.float32),
+           _seq(beta, "beta", (B, H), torch.float32)]
+    if s.dim() != 4:
+        raise ValueError("s must be a [pool, H, DK, DV] tensor")
+    sp, lp = _f32(s, "s", (s.shape[0], H, DK, DV)), _index(slots, "slots", B)
+    o, os_ = _out(out, "out", values, q)
+    _check(lib().dwconv_delta_step(*ins, sp, lp, s.shape[0], os_, B, H, Hk, DK, DV, float(scale), float(eps), code, _stream()))
+    return o
+
+
+def _unit_scale(q, key_heads, g):
+    """DK^-1/2."""
+    n = int(q.shape[1]) if q.dim() > 1 else 0
+    Hk = key_heads if key_heads is not None else (g.shape[1] if g.dim() > 1 else 0)
+    return (n // Hk) ** -0.5 if Hk and n >= Hk > 0 else 1.0
+
+
+# ---- dropout ----
+
+def _dropout(x, name, p, rng, layer, res, scale, tied, out):
+    shape = B, C, L = _shape3(x, name)
+    code = _dtype_code(x)
+    xs, rs = _seq(x, name, shape, x.dtype), _NONE if res is None else _seq(res, "res", shape, x.dtype)
+    rp = _plain(rng, "rng", (2,), torch.int64)
+    o, os_ = _out(out, "out", shape, x)
+    _check(lib().dwconv_dropout(xs, rs, os_, rp, int(layer), B, C, L, float(p), float(scale), int(bool(tied)), code, _stream()))
+    return o
+
+
+def dropout_fwd(x, p: float, rng, layer: int = 0, res=None, scale: float = 1.0, tied: bool = False, out=None):
+    """res + scale x / (1 - p) where an element of x [B, C, L] is kept, res (None: zeros) where it is dropped, with probability p.  ``tied``: whole
+    channels of a batch entry are.  rng [2] int64 on the GPU, a seed and a step, decides together with ``layer`` (0 .. 2^24 - 1): the same three give
+    the same mask, which is stored nowhere; a program counts the step up (``rng[1] += 1``, also between replays of a graph) and gives every layer
+    its number.  out may be x or res itself."""
+    return _dropout(x, "x", p, rng, layer, res, scale, tied, out)
+
+
+def dropout_bwd(dout, p: float, rng, layer: int = 0, scale: float = 1.0, tied: bool = False, out=None):
+    """Gradient of ``dropout_fwd`` with regard to x, from the rng that it had; that with regard to res is dout itself."""
+    return _dropout(dout, "dout", p, rng, layer, None, scale, tied, out)
 
 
 # ---- norms, gate, residual ----

@@ -1,0 +1,284 @@
+// Gated delta rule: validation, plans and launches (declared in include/dwconv_block.h), and its form for one token.
+#include "dwconv_block_host.hip.h"
+#include "dwconv_block_delta.hip.h"
+
+#include <atomic>
+
+using namespace blkhost;
+using namespace dwconv;
+
+namespace dwconv {
+
+template <typename T> struct DeltaStep {
+    Seq<T> q, k, v;
+    Seq<float> g, beta;
+    float *s;
+    const int *slots;
+    SeqOut<T> o;
+    int B, H, each, DK, DV, pool, blocks;
+    float scale, eps;
+};
+
+// One token.  A workgroup has up to 128 columns of a head's state in registers, four neighbouring ones a lane (2^lg lanes a row); with
+// S~ = exp(g) S both S~^T k and S~^T q are formed in one pass, o = scale (S~^T q + beta (k . q) u).
+struct StepLds {
+    float k[128], q[128], sums[4][3];
+    f32x4 part[2][4][32];
+};
+template <typename T, int RT> __device__ __forceinline__ void delta_step_head(const DeltaStep<T> &p, int lg, int unit, StepLds &m)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, cols = 1 << lg, at = tid & (cols - 1), r0 = tid >> lg, step = 256 >> lg;
+    const int cb = unit % p.blocks, bh = unit / p.blocks, b = bh / p.H, h = bh % p.H, hk = h / p.each;
+    const int dv = (cb << (lg + 2)) + 4 * at;
+    const int slot = p.slots ? p.slots[b] : b;
+    T *orow = p.o.p + (long long)b * p.o.bs + (long long)h * p.DV;
+    if (slot < 0 || slot >= p.pool) {
+        if (r0 == 0) store4(orow, f32x4{}, dv, p.DV);
+        return;
+    }
+    float *S = p.s + ((long long)slot * p.H + h) * p.DK * p.DV;
+    f32x4 x[RT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        const int r = r0 + i * step;
+        x[i] = r < p.DK ? load4(S + (long long)r * p.DV, dv, p.DV) : f32x4{};
+    }
+    const f32x4 v = load4(p.v.p + (long long)b * p.v.bs + (long long)h * p.DV, dv, p.DV);
+    const float g = p.g.p[(long long)b * p.g.bs + h], beta = p.beta.p[(long long)b * p.beta.bs + h];
+    float kv = 0.0f, qv = 0.0f;
+    if (tid < 128) {
+        if (tid < p.DK) {
+            kv = ld_elem(p.k.p + (long long)b * p.k.bs + (long long)hk * p.DK + tid);
+            qv = ld_elem(p.q.p + (long long)b * p.q.bs + (long long)hk * p.DK + tid);
+        }
+        m.k[tid] = kv, m.q[tid] = qv;
+        const float kk = group_sum(kv * kv, 6), qq = group_sum(qv * qv, 6), kq = group_sum(kv * qv, 6);
+        if (lane == 0) m.sums[wave][0] = kk, m.sums[wave][1] = qq, m.sums[wave][2] = kq;
+    }
+    __syncthreads();
+    const bool normed = p.eps > 0.0f;
+    const float rk = normed ? 1.0f / sqrtf(m.sums[0][0] + m.sums[1][0] + p.eps) : 1.0f, rq = p.scale * (normed ? 1.0f / sqrtf(m.sums[0][1] + m.sums[1][1] + p.eps) : 1.0f);
+    const float kq = (m.sums[0][2] + m.sums[1][2]) * rk * rq, a = exp2_of((double)(g < -128.0f ? -128.0f : g) * 1.4426950408889634);
+    f32x4 ks = {}, qs = {};
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        const int r = r0 + i * step;
+        const float kr = r < p.DK ? m.k[r] : 0.0f, qr = r < p.DK ? m.q[r] : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ks[e] = fmaf(kr, x[i][e], ks[e]), qs[e] = fmaf(qr, x[i][e], qs[e]);
+    }
+    for (int d = cols; d < 64; d *= 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ks[e] += __shfl_xor(ks[e], d, 64), qs[e] += __shfl_xor(qs[e], d, 64);
+    if (lane < cols) m.part[0][wave][lane] = ks, m.part[1][wave][lane] = qs;
+    __syncthreads();
+    ks = (m.part[0][0][at] + m.part[0][1][at]) + (m.part[0][2][at] + m.part[0][3][at]);
+    qs = (m.part[1][0][at] + m.part[1][1][at]) + (m.part[1][2][at] + m.part[1][3][at]);
+    const f32x4 u = v - ks * (a * rk), w = u * beta;
+    if (r0 == 0) store4(orow, qs * (a * rq) + w * kq, dv, p.DV);
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        const int r = r0 + i * step;
+        if (r < p.DK) store4(S + (long long)r * p.DV, x[i] * a + w * (m.k[r] * rk), dv, p.DV);
+    }
+}
+
+template <typename T, int RT> __global__ __launch_bounds__(256) void delta_step_kernel(DeltaStep<T> p, int lg)
+{
+    __shared__ StepLds m;
+    for (int unit = blockIdx.x, units = p.B * p.H * p.blocks; unit < units; unit += gridDim.x) {
+        delta_step_head<T, RT>(p, lg, unit, m);
+        __syncthreads();
+    }
+}
+
+}  // namespace dwconv
+
+namespace {
+
+constexpr int kMaxKey = 128;            // channels of a key: a state's columns are registers of a wave
+constexpr int kMaxUnits = 1 << 22;      // workgroups of a grid, whose lanes stay below 2^32
+
+int chunks_of(int L) { return (int)ceil_div(L, kDeltaChunk); }
+
+int check_heads(int B, int H, int Hk, int DK, int DV, int L)
+{
+    if (B < 1 || H < 1 || Hk < 1 || DK < 1 || DV < 1 || H > (1 << 20) || H % Hk || DK > kMaxKey || DV > (1 << 16)) return DWCONV_ERR_SHAPE;
+    int rc = check_dims(B, H * std::min(DK, 2), L);         // (the products below stay in range)
+    if (rc != DWCONV_OK) return rc;
+    if ((long long)H * DV > (1 << 25) || (long long)Hk * DK > (1 << 25)) return DWCONV_ERR_SHAPE;
+    if ((rc = check_dims(B, H * DV, L)) != DWCONV_OK || (rc = check_dims(B, Hk * DK, L)) != DWCONV_OK) return rc;
+    // one workgroup a chunk or a head; states in 64 bits of bytes
+    const long long heads = (long long)B * H;
+    if (heads > 0x7fffffffll / chunks_of(L) || heads * chunks_of(L) > (1ll << 44) / ((long long)DK * DV)) return DWCONV_ERR_SHAPE;
+    return DWCONV_OK;
+}
+bool eps_ok(float eps) { return eps >= 0.0f && eps < INFINITY; }
+bool finite_ok(float x) { return x - x == 0.0f; }
+
+// Lets a kernel have more than 64 KiB of LDS, once a device.
+template <typename Kernel> bool allow_lds(Kernel kernel, size_t bytes, std::atomic<unsigned long long> &done)
+{
+    if (bytes <= 64 * 1024) return true;
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) return false;
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+    if (done.load(std::memory_order_acquire) & bit) return true;
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return false;
+    done.fetch_or(bit, std::memory_order_release);
+    return true;
+}
+
+template <typename T, int KT> int launch_fwd(const DeltaFwd<T> &p, hipStream_t st)
+{
+    static std::atomic<unsigned long long> done{0};
+    const size_t lds = sizeof(DeltaLds<T, KT>);
+    if (!allow_lds(delta_fwd_kernel<T, KT>, lds, done)) return DWCONV_ERR_LAUNCH;
+    const int slices = (int)ceil_div(p.DV, 16), W = std::min(8, slices);
+    delta_fwd_kernel<T, KT><<<dim3((unsigned)std::min(p.B * p.H, kMaxUnits), (unsigned)ceil_div(slices, W)), 64 * W, lds, st>>>(p);
+    return launch_status();
+}
+template <typename T> int launch_fwd(const DeltaFwd<T> &p, hipStream_t st)
+{
+    return p.DK <= 32 ? launch_fwd<T, 2>(p, st) : p.DK <= 64 ? launch_fwd<T, 4>(p, st) : launch_fwd<T, 8>(p, st);
+}
+
+template <typename T, int KT> int launch_bwd(const DeltaBwd<T> &p, hipStream_t st)
+{
+    static std::atomic<unsigned long long> done[2];
+    const size_t lds = sizeof(DeltaLds<T, KT>), lds_chunk = sizeof(DeltaBwdLds<KT>);
+    static_assert(sizeof(DeltaBwdLds<KT>) <= 160 * 1024, "LDS of a CU");
+    if (!allow_lds(delta_bwd_state_kernel<T, KT>, lds, done[0]) || !allow_lds(delta_bwd_chunk_kernel<T, KT>, lds_chunk, done[1]))
+        return DWCONV_ERR_LAUNCH;
+    const int slices = (int)ceil_div(p.DV, 16), W = std::min(8, slices);
+    delta_bwd_state_kernel<T, KT><<<dim3((unsigned)std::min(p.B * p.H, kMaxUnits), (unsigned)ceil_div(slices, W)), 64 * W, lds, st>>>(p);
+    delta_bwd_chunk_kernel<T, KT><<<(unsigned)std::min(p.B * (p.H / p.each) * p.chunks, kMaxUnits), 64 * kDeltaBwdWaves(KT), lds_chunk, st>>>(p);
+    return launch_status();
+}
+template <typename T> int launch_bwd(const DeltaBwd<T> &p, hipStream_t st)
+{
+    return p.DK <= 32 ? launch_bwd<T, 2>(p, st) : p.DK <= 64 ? launch_bwd<T, 4>(p, st) : launch_bwd<T, 8>(p, st);
+}
+
+template <typename T> void launch_step(const DeltaStep<T> &in, hipStream_t st)
+{
+    DeltaStep<T> p = in;
+    // Lanes of a row, four columns each: whole rows of up to 128 columns, but 32 columns where the call would leave CUs without work.
+    int lg = 0;
+    while (lg < 5 && (4 << lg) < p.DV) ++lg;
+    while (lg > 3 && (long long)p.B * p.H * ceil_div(p.DV, 4 << lg) < 512) --lg;
+    p.blocks = (int)ceil_div(p.DV, 4 << lg);
+    const unsigned grid = (unsigned)std::min(p.B * p.H * p.blocks, kMaxUnits);
+    const int rows = (int)ceil_div(p.DK, 256 >> lg);
+    if (rows <= 1) delta_step_kernel<T, 1><<<grid, 256, 0, st>>>(p, lg);
+    else if (rows <= 2) delta_step_kernel<T, 2><<<grid, 256, 0, st>>>(p, lg);
+    else if (rows <= 4) delta_step_kernel<T, 4><<<grid, 256, 0, st>>>(p, lg);
+    else if (rows <= 8) delta_step_kernel<T, 8><<<grid, 256, 0, st>>>(p, lg);
+    else delta_step_kernel<T, 16><<<grid, 256, 0, st>>>(p, lg);
+}
+
+template <typename T> DeltaShape<T> shape(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const int *lengths, int B, int H, int Hk,
+                                          int DK, int DV, int L, float scale, float eps)
+{
+    return DeltaShape<T>{seq<T>(q), seq<T>(k), seq<T>(v), seq<float>(g), seq<float>(beta), lengths, B, H, H / Hk, DK, DV, L, chunks_of(L), scale, eps};
+}
+
+}  // namespace
+
+extern "C" {
+
+int dwconv_delta_states(int L) { return L < 1 || L > (1 << 30) ? 0 : chunks_of(L); }
+
+size_t dwconv_delta_workspace_bytes(int B, int H, int DK, int DV, int L)
+{
+    if (check_heads(B, H, H, DK, DV, L) != DWCONV_OK) return 0;
+    return ((size_t)B * H * chunks_of(L) * DK * DV * sizeof(float) + 15) & ~(size_t)15;
+}
+
+int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const float *s0, const int *lengths, dwconv_seq_out o,
+                     float *s_last, float *states, int B, int H, int Hk, int DK, int DV, int L, float scale, float eps, int dtype, void *stream)
+{
+    if (!q.data || !k.data || !v.data || !g.data || !beta.data || !o.data) return DWCONV_ERR_NULL;
+    int rc = check_heads(B, H, Hk, DK, DV, L);
+    if (rc != DWCONV_OK) return rc;
+    if (!dtype_ok(dtype)) return DWCONV_ERR_DTYPE;
+    if (!finite_ok(scale) || !eps_ok(eps)) return DWCONV_ERR_VALUE;
+    const size_t es = elem_size(dtype);
+    for (const dwconv_seq *t : {&q, &k, &v})
+        if ((rc = check_in(*t, es)) != DWCONV_OK) return rc;
+    for (const dwconv_seq *t : {&g, &beta})
+        if ((rc = check_in(*t, 4)) != DWCONV_OK) return rc;
+    if ((rc = check_out(o, es, B, H * DV, L)) != DWCONV_OK) return rc;
+    for (const void *t : {(const void *)s0, (const void *)lengths, (const void *)s_last, (const void *)states})
+        if (!f32_ok(t)) return DWCONV_ERR_ALIGN;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (dtype == DWCONV_F32) {
+        DeltaFwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps), seq<float>(o), s0, s_last, states};
+        return launch_fwd(p, st);
+    }
+    DeltaFwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps), seq<bf16_t>(o), s0, s_last, states};
+    return launch_fwd(p, st);
+}
+
+int dwconv_delta_bwd(dwconv_seq dout, dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const float *states, const float *ds_last,
+                     const int *lengths, dwconv_seq_out dq, dwconv_seq_out dk, dwconv_seq_out dv, float *dg, float *dbeta, float *ds0, void *workspace,
+                     size_t workspace_bytes, int B, int H, int Hk, int DK, int DV, int L, float scale, float eps, int dtype, void *stream)
+{
+    if (!dout.data || !q.data || !k.data || !v.data || !g.data || !beta.data || !states || !dq.data || !dk.data || !dv.data || !dg || !dbeta)
+        return DWCONV_ERR_NULL;
+    int rc = check_heads(B, H, Hk, DK, DV, L);
+    if (rc != DWCONV_OK) return rc;
+    if (!dtype_ok(dtype)) return DWCONV_ERR_DTYPE;
+    if (!finite_ok(scale) || !eps_ok(eps)) return DWCONV_ERR_VALUE;
+    const size_t es = elem_size(dtype);
+    for (const dwconv_seq *t : {&dout, &q, &k, &v})
+        if ((rc = check_in(*t, es)) != DWCONV_OK) return rc;
+    for (const dwconv_seq *t : {&g, &beta})
+        if ((rc = check_in(*t, 4)) != DWCONV_OK) return rc;
+    for (const dwconv_seq_out *t : {&dq, &dk})
+        if ((rc = check_out(*t, es, B, Hk * DK, L)) != DWCONV_OK) return rc;
+    if ((rc = check_out(dv, es, B, H * DV, L)) != DWCONV_OK) return rc;
+    for (const void *t : {(const void *)states, (const void *)ds_last, (const void *)lengths, (const void *)dg, (const void *)dbeta, (const void *)ds0})
+        if (!f32_ok(t)) return DWCONV_ERR_ALIGN;
+    const size_t need = dwconv_delta_workspace_bytes(B, H, DK, DV, L);
+    if (!workspace || workspace_bytes < need || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    float *after = static_cast<float *>(workspace);
+    if (dtype == DWCONV_F32) {
+        DeltaBwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps), seq<float>(dout), seq<float>(dq), seq<float>(dk),
+                          seq<float>(dv), states, ds_last, after, dg, dbeta, ds0};
+        return launch_bwd(p, st);
+    }
+    DeltaBwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps), seq<bf16_t>(dout), seq<bf16_t>(dq), seq<bf16_t>(dk),
+                       seq<bf16_t>(dv), states, ds_last, after, dg, dbeta, ds0};
+    return launch_bwd(p, st);
+}
+
+int dwconv_delta_step(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, float *s, const int *slots, int pool, dwconv_seq_out o, int B,
+                      int H, int Hk, int DK, int DV, float scale, float eps, int dtype, void *stream)
+{
+    if (!q.data || !k.data || !v.data || !g.data || !beta.data || !s || !o.data) return DWCONV_ERR_NULL;
+    int rc = check_heads(B, H, Hk, DK, DV, 1);
+    if (rc != DWCONV_OK) return rc;
+    if (pool < 1 || (!slots && pool < B) || (long long)pool * H > (1ll << 40) / ((long long)DK * DV)) return DWCONV_ERR_SHAPE;
+    if ((long long)B * H > 0x7fffffffll / ceil_div(DV, 32)) return DWCONV_ERR_SHAPE;
+    if (!dtype_ok(dtype)) return DWCONV_ERR_DTYPE;
+    if (!finite_ok(scale) || !eps_ok(eps)) return DWCONV_ERR_VALUE;
+    const size_t es = elem_size(dtype);
+    for (const dwconv_seq *t : {&q, &k, &v})
+        if ((rc = check_in(*t, es)) != DWCONV_OK) return rc;
+    for (const dwconv_seq *t : {&g, &beta})
+        if ((rc = check_in(*t, 4)) != DWCONV_OK) return rc;
+    if ((rc = check_out(o, es, B, H * DV, 1)) != DWCONV_OK) return rc;
+    if (!f32_ok(s) || !f32_ok(slots)) return DWCONV_ERR_ALIGN;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (dtype == DWCONV_F32)
+        launch_step(DeltaStep<float>{seq<float>(q), seq<float>(k), seq<float>(v), seq<float>(g), seq<float>(beta), s, slots, seq<float>(o), B, H, H / Hk, DK,
+                                     DV, pool, 1, scale, eps}, st);
+    else
+        launch_step(DeltaStep<bf16_t>{seq<bf16_t>(q), seq<bf16_t>(k), seq<bf16_t>(v), seq<float>(g), seq<float>(beta), s, slots, seq<bf16_t>(o), B, H, H / Hk,
+                                      DK, DV, pool, 1, scale, eps}, st);
+    return launch_status();
+}
+
+}  // extern "C"
