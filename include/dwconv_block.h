@@ -140,13 +140,14 @@ DWCONV_API int dwconv_conv_ring(dwconv_seq x, void *ring, const int *lengths, co
  * position are brought to unit length first, x / sqrt(|x|^2 + eps); eps = 0: taken as they are.  s0 [B, H, DK, DV] fp32 or NULL (zeros); lengths as in
  * dwconv_scan_fwd (o is 0 from n on, whatever the inputs hold there); s_last [B, H, DK, DV] fp32 or NULL: the state behind n.
  * states [B, H, dwconv_delta_states(L), DK, DV] fp32 or NULL: S in front of every 64th position, which dwconv_delta_bwd takes.
+ * workspace: dwconv_delta_workspace_bytes(...) bytes, 16-byte aligned.
  * DK at most 128, DV at most 65536, H at most 2^20.  g may be minus infinity (nothing in front of t is remembered).  Finite values whose results are
  * finite give those; what is not finite may reach every position of its chunk of 64 and everything behind it, of its own head and of those that
  * share its keys.
  */
 DWCONV_API int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const float *s0, const int *lengths,
-                                dwconv_seq_out o, float *s_last, float *states, int B, int H, int Hk, int DK, int DV, int L, float scale,
-                                float eps, int dtype, void *stream);
+                                dwconv_seq_out o, float *s_last, float *states, void *workspace, size_t workspace_bytes, int B, int H, int Hk,
+                                int DK, int DV, int L, float scale, float eps, int dtype, void *stream);
 
 /*
  * Gradients of the gated delta rule.  dout [B, H * DV, L]; ds_last [B, H, DK, DV] fp32 or NULL (zeros), the gradient of s_last; states as
@@ -162,8 +163,8 @@ DWCONV_API int dwconv_delta_bwd(dwconv_seq dout, dwconv_seq q, dwconv_seq k, dwc
 /* States of a head that dwconv_delta_fwd keeps for the backward pass: ceil(L / 64); 0 on bad arguments. */
 DWCONV_API int dwconv_delta_states(int L);
 
-/* Workspace of dwconv_delta_bwd; 0 on bad arguments. */
-DWCONV_API size_t dwconv_delta_workspace_bytes(int B, int H, int DK, int DV, int L);
+/* Workspace of dwconv_delta_fwd (backward = 0) and dwconv_delta_bwd (backward = 1); 0 on bad arguments. */
+DWCONV_API size_t dwconv_delta_workspace_bytes(int B, int H, int DK, int DV, int L, int backward);
 
 /*
  * Gated delta rule, one token of every place b of the batch, on the states s [pool, H, DK, DV] fp32, which are updated in place; slots and pool

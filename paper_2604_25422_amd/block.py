@@ -65,10 +65,10 @@ def lib():
                 ("dwconv_clip_workspace_bytes", [], sz),
                 ("dwconv_conv_step", [s, vp, vp, vp, vp, i, s, i, i, i, i, vp], i),
                 ("dwconv_conv_ring", [s, vp, vp, vp, i, i, i, i, i, i, vp], i),
-                ("dwconv_delta_fwd", [s, s, s, s, s, vp, vp, s, vp, vp, i, i, i, i, i, i, f, f, i, vp], i),
+                ("dwconv_delta_fwd", [s, s, s, s, s, vp, vp, s, vp, vp, vp, sz, i, i, i, i, i, i, f, f, i, vp], i),
                 ("dwconv_delta_bwd", [s, s, s, s, s, s, vp, vp, vp, s, s, s, vp, vp, vp, vp, sz, i, i, i, i, i, i, f, f, i, vp], i),
                 ("dwconv_delta_states", [i], i),
-                ("dwconv_delta_workspace_bytes", [i, i, i, i, i], sz),
+                ("dwconv_delta_workspace_bytes", [i, i, i, i, i, i], sz),
                 ("dwconv_delta_step", [s, s, s, s, s, vp, vp, i, s, i, i, i, i, i, f, f, i, vp], i),
                 ("dwconv_dropout", [s, s, s, vp, i, i, i, i, f, f, i, i, vp], i)):
             fn = getattr(l, name)
@@ -223,9 +223,8 @@ def delta_states(L: int) -> int:
     return int(lib().dwconv_delta_states(int(L)))
 
 
-def delta_workspace_bytes(B: int, H: int, DK: int, DV: int, L: int) -> int:
-    """Workspace of ``delta_bwd``."""
-    return int(lib().dwconv_delta_workspace_bytes(B, H, DK, DV, L))
+def delta_workspace_bytes(B: int, H: int, DK: int, DV: int, L: int, backward: bool) -> int:
+    return int(lib().dwconv_delta_workspace_bytes(B, H, DK, DV, L, int(backward)))
 
 
 def _heads(q, v, g, key_heads, dims: int):
@@ -242,7 +241,7 @@ def _heads(q, v, g, key_heads, dims: int):
     return B, H, Hk, int(q.shape[1]) // Hk, int(v.shape[1]) // H
 
 
-def delta_fwd(q, k, v, g, beta, s0=None, lengths=None, key_heads=None, scale=None, eps: float = 1e-6, save: bool = True, out=None):
+def delta_fwd(q, k, v, g, beta, s0=None, lengths=None, key_heads=None, scale=None, eps: float = 1e-6, save: bool = True, out=None, workspace=None):
     """The gated delta rule along t: with a state S [DK, DV] of every head, S <- exp(g) S, u = v - S^T k, S <- S + beta k u^T, o = scale S^T q.
     q, k [B, key_heads * DK, L] and v [B, H * DV, L] of one type, g (log decays) and beta [B, H, L] fp32; H a multiple of key_heads (None: H),
     neighbouring heads of values share one of keys.  scale None: DK^-1/2.  eps: q and k are brought to unit length, x / sqrt(|x|^2 + eps); 0: taken as
@@ -257,8 +256,9 @@ def delta_fwd(q, k, v, g, beta, s0=None, lengths=None, key_heads=None, scale=Non
     o, os_ = _out(out, "out", values, q)
     s_last = torch.empty((B, H, DK, DV), dtype=torch.float32, device=q.device)
     states = torch.empty((B, H, delta_states(L), DK, DV), dtype=torch.float32, device=q.device) if save else None
-    _check(lib().dwconv_delta_fwd(*ins, sp, lp, os_, s_last.data_ptr(), states.data_ptr() if save else None, B, H, Hk, DK, DV, L, float(scale),
-                                  float(eps), code, _stream()))
+    ws, nbytes, keep = _workspace(workspace, delta_workspace_bytes(B, H, DK, DV, L, False), q)
+    _check(lib().dwconv_delta_fwd(*ins, sp, lp, os_, s_last.data_ptr(), states.data_ptr() if save else None, ws, nbytes, B, H, Hk, DK, DV, L,
+                                  float(scale), float(eps), code, _stream()))
     return o, s_last, states
 
 
@@ -279,7 +279,7 @@ def delta_bwd(do, q, k, v, g, beta, states, ds_last=None, lengths=None, key_head
     outs = [_out(t, n, shape, q) for t, n, shape in zip(given, ("dq", "dk", "dv"), (keys, keys, values))]
     dg, dbeta = (torch.empty((B, H, L), dtype=torch.float32, device=q.device) for _ in range(2))
     ds0 = torch.empty((B, H, DK, DV), dtype=torch.float32, device=q.device)
-    ws, nbytes, keep = _workspace(workspace, delta_workspace_bytes(B, H, DK, DV, L), q)
+    ws, nbytes, keep = _workspace(workspace, delta_workspace_bytes(B, H, DK, DV, L, True), q)
     _check(lib().dwconv_delta_bwd(*ins, sp, dsp, lp, *(s for _, s in outs), dg.data_ptr(), dbeta.data_ptr(), ds0.data_ptr(), ws, nbytes, B, H, Hk, DK, DV,
                                   L, float(scale), float(eps), code, _stream()))
     return outs[0][0], outs[1][0], outs[2][0], dg, dbeta, ds0

@@ -129,30 +129,54 @@ template <typename Kernel> bool allow_lds(Kernel kernel, size_t bytes, std::atom
     return true;
 }
 
-template <typename T, int KT> int launch_fwd(const DeltaFwd<T> &p, hipStream_t st)
+template <typename T, int KT> int launch_pairs(const DeltaShape<T> &p, hipStream_t st)
+{
+    static std::atomic<unsigned long long> done{0};
+    const size_t lds = sizeof(PairsLds<T, KT>);
+    if (!allow_lds(delta_pairs_kernel<T, KT>, lds, done)) return DWCONV_ERR_LAUNCH;
+    delta_pairs_kernel<T, KT><<<(unsigned)std::min(p.B * p.H * p.chunks, kMaxUnits), 256, lds, st>>>(p);
+    return DWCONV_OK;
+}
+dim3 walk_grid(int B, int H, int DV, int W) { return dim3((unsigned)std::min(B * H, kMaxUnits), (unsigned)ceil_div(DV, 16 * W)); }
+bool four_waves(int DV) { return DV <= 64; }
+
+template <typename T, int KT, int W> int launch_walk(const DeltaFwd<T> &p, hipStream_t st)
 {
     static std::atomic<unsigned long long> done{0};
     const size_t lds = sizeof(DeltaLds<T, KT>);
-    if (!allow_lds(delta_fwd_kernel<T, KT>, lds, done)) return DWCONV_ERR_LAUNCH;
-    const int slices = (int)ceil_div(p.DV, 16), W = std::min(8, slices);
-    delta_fwd_kernel<T, KT><<<dim3((unsigned)std::min(p.B * p.H, kMaxUnits), (unsigned)ceil_div(slices, W)), 64 * W, lds, st>>>(p);
+    if (!allow_lds(delta_fwd_kernel<T, KT, W>, lds, done)) return DWCONV_ERR_LAUNCH;
+    delta_fwd_kernel<T, KT, W><<<walk_grid(p.B, p.H, p.DV, W), 64 * W, lds, st>>>(p);
     return launch_status();
+}
+template <typename T, int KT> int launch_fwd(const DeltaFwd<T> &p, hipStream_t st)
+{
+    const int rc = launch_pairs<T, KT>(p, st);
+    if (rc != DWCONV_OK) return rc;
+    return four_waves(p.DV) ? launch_walk<T, KT, 4>(p, st) : launch_walk<T, KT, 8>(p, st);
 }
 template <typename T> int launch_fwd(const DeltaFwd<T> &p, hipStream_t st)
 {
     return p.DK <= 32 ? launch_fwd<T, 2>(p, st) : p.DK <= 64 ? launch_fwd<T, 4>(p, st) : launch_fwd<T, 8>(p, st);
 }
 
+template <typename T, int KT, int W> int launch_walk(const DeltaBwd<T> &p, hipStream_t st)
+{
+    static std::atomic<unsigned long long> done{0};
+    const size_t lds = sizeof(DeltaLds<T, KT>);
+    if (!allow_lds(delta_bwd_state_kernel<T, KT, W>, lds, done)) return DWCONV_ERR_LAUNCH;
+    delta_bwd_state_kernel<T, KT, W><<<walk_grid(p.B, p.H, p.DV, W), 64 * W, lds, st>>>(p);
+    return DWCONV_OK;
+}
 template <typename T, int KT> int launch_bwd(const DeltaBwd<T> &p, hipStream_t st)
 {
-    static std::atomic<unsigned long long> done[2];
-    const size_t lds = sizeof(DeltaLds<T, KT>), lds_chunk = sizeof(DeltaBwdLds<KT>);
-    static_assert(sizeof(DeltaBwdLds<KT>) <= 160 * 1024, "LDS of a CU");
-    if (!allow_lds(delta_bwd_state_kernel<T, KT>, lds, done[0]) || !allow_lds(delta_bwd_chunk_kernel<T, KT>, lds_chunk, done[1]))
-        return DWCONV_ERR_LAUNCH;
-    const int slices = (int)ceil_div(p.DV, 16), W = std::min(8, slices);
-    delta_bwd_state_kernel<T, KT><<<dim3((unsigned)std::min(p.B * p.H, kMaxUnits), (unsigned)ceil_div(slices, W)), 64 * W, lds, st>>>(p);
-    delta_bwd_chunk_kernel<T, KT><<<(unsigned)std::min(p.B * (p.H / p.each) * p.chunks, kMaxUnits), 64 * kDeltaBwdWaves(KT), lds_chunk, st>>>(p);
+    static std::atomic<unsigned long long> done{0};
+    const size_t lds = sizeof(DeltaChunkLds<T, KT>);
+    static_assert(sizeof(DeltaChunkLds<T, KT>) <= 160 * 1024, "LDS of a CU");
+    if (!allow_lds(delta_bwd_chunk_kernel<T, KT>, lds, done)) return DWCONV_ERR_LAUNCH;
+    int rc = launch_pairs<T, KT>(p, st);
+    if (rc == DWCONV_OK) rc = four_waves(p.DV) ? launch_walk<T, KT, 4>(p, st) : launch_walk<T, KT, 8>(p, st);
+    if (rc != DWCONV_OK) return rc;
+    delta_bwd_chunk_kernel<T, KT><<<(unsigned)std::min(p.B * (p.H / p.each) * p.chunks, kMaxUnits), 64 * kDeltaBwdWaves(KT), lds, st>>>(p);
     return launch_status();
 }
 template <typename T> int launch_bwd(const DeltaBwd<T> &p, hipStream_t st)
@@ -178,10 +202,12 @@ template <typename T> void launch_step(const DeltaStep<T> &in, hipStream_t st)
 }
 
 template <typename T> DeltaShape<T> shape(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const int *lengths, int B, int H, int Hk,
-                                          int DK, int DV, int L, float scale, float eps)
+                                          int DK, int DV, int L, float scale, float eps, void *workspace)
 {
-    return DeltaShape<T>{seq<T>(q), seq<T>(k), seq<T>(v), seq<float>(g), seq<float>(beta), lengths, B, H, H / Hk, DK, DV, L, chunks_of(L), scale, eps};
+    return DeltaShape<T>{seq<T>(q), seq<T>(k), seq<T>(v), seq<float>(g), seq<float>(beta), lengths, B, H, H / Hk, DK, DV, L, chunks_of(L), scale, eps,
+                         static_cast<DeltaPairs *>(workspace)};
 }
+size_t pairs_bytes(int B, int H, int L) { return (size_t)B * H * chunks_of(L) * sizeof(DeltaPairs); }
 
 }  // namespace
 
@@ -189,14 +215,15 @@ extern "C" {
 
 int dwconv_delta_states(int L) { return L < 1 || L > (1 << 30) ? 0 : chunks_of(L); }
 
-size_t dwconv_delta_workspace_bytes(int B, int H, int DK, int DV, int L)
+size_t dwconv_delta_workspace_bytes(int B, int H, int DK, int DV, int L, int backward)
 {
     if (check_heads(B, H, H, DK, DV, L) != DWCONV_OK) return 0;
-    return ((size_t)B * H * chunks_of(L) * DK * DV * sizeof(float) + 15) & ~(size_t)15;
+    return pairs_bytes(B, H, L) + (backward ? ((size_t)B * H * chunks_of(L) * DK * DV * sizeof(float) + 15) & ~(size_t)15 : 0);
 }
 
 int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const float *s0, const int *lengths, dwconv_seq_out o,
-                     float *s_last, float *states, int B, int H, int Hk, int DK, int DV, int L, float scale, float eps, int dtype, void *stream)
+                     float *s_last, float *states, void *workspace, size_t workspace_bytes, int B, int H, int Hk, int DK, int DV, int L, float scale,
+                     float eps, int dtype, void *stream)
 {
     if (!q.data || !k.data || !v.data || !g.data || !beta.data || !o.data) return DWCONV_ERR_NULL;
     int rc = check_heads(B, H, Hk, DK, DV, L);
@@ -211,12 +238,13 @@ int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwc
     if ((rc = check_out(o, es, B, H * DV, L)) != DWCONV_OK) return rc;
     for (const void *t : {(const void *)s0, (const void *)lengths, (const void *)s_last, (const void *)states})
         if (!f32_ok(t)) return DWCONV_ERR_ALIGN;
+    if (!workspace || workspace_bytes < pairs_bytes(B, H, L) || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (dtype == DWCONV_F32) {
-        DeltaFwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps), seq<float>(o), s0, s_last, states};
+        DeltaFwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<float>(o), s0, s_last, states};
         return launch_fwd(p, st);
     }
-    DeltaFwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps), seq<bf16_t>(o), s0, s_last, states};
+    DeltaFwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<bf16_t>(o), s0, s_last, states};
     return launch_fwd(p, st);
 }
 
@@ -240,16 +268,16 @@ int dwconv_delta_bwd(dwconv_seq dout, dwconv_seq q, dwconv_seq k, dwconv_seq v, 
     if ((rc = check_out(dv, es, B, H * DV, L)) != DWCONV_OK) return rc;
     for (const void *t : {(const void *)states, (const void *)ds_last, (const void *)lengths, (const void *)dg, (const void *)dbeta, (const void *)ds0})
         if (!f32_ok(t)) return DWCONV_ERR_ALIGN;
-    const size_t need = dwconv_delta_workspace_bytes(B, H, DK, DV, L);
+    const size_t need = dwconv_delta_workspace_bytes(B, H, DK, DV, L, 1);
     if (!workspace || workspace_bytes < need || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    float *after = static_cast<float *>(workspace);
+    float *after = reinterpret_cast<float *>(static_cast<char *>(workspace) + pairs_bytes(B, H, L));
     if (dtype == DWCONV_F32) {
-        DeltaBwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps), seq<float>(dout), seq<float>(dq), seq<float>(dk),
+        DeltaBwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<float>(dout), seq<float>(dq), seq<float>(dk),
                           seq<float>(dv), states, ds_last, after, dg, dbeta, ds0};
         return launch_bwd(p, st);
     }
-    DeltaBwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps), seq<bf16_t>(dout), seq<bf16_t>(dq), seq<bf16_t>(dk),
+    DeltaBwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<bf16_t>(dout), seq<bf16_t>(dq), seq<bf16_t>(dk),
                        seq<bf16_t>(dv), states, ds_last, after, dg, dbeta, ds0};
     return launch_bwd(p, st);
 }

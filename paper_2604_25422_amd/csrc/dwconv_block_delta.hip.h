@@ -6,15 +6,26 @@
 //     o_i = exp(G_i) S^T q_i + sum_{j <= i} P_ij w_j,   P_ij = e(i, j) q_i . k_j,     S' = exp(G_63) S + sum_j e(63, j) k_j w_j^T,
 // so that all but the step from chunk to chunk is products of matrices.  Only differences G_i - G_j with i >= j are ever raised to a
 // power, in 64 bits up to the exponential's argument: nothing overflows however strong a decay is.
+//
+// What does not depend on the state is formed first, for all chunks at once (delta_pairs_kernel: T = (I + A)^-1 and P, 32 KB a chunk);
+// the walk from chunk to chunk is then three products deep.
+//
+// Products: fp32 calls on the fp32 matrix instruction.  bf16 calls on the bf16 one, 16 times as fast: what is stored as bf16 goes in as it is, and
+// what is fp32 (the state, w, T, P) as the exact sum of three bf16 limbs, so that sums and states are those of fp32 products to 2^-24; the products that
+// only reach an output rounded to bf16 leave out the third limb (2^-16 of them, 2^-8 of the rounding).
 #pragma once
 #include "dwconv_block_common.hip.h"
 
 namespace dwconv {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kDeltaChunk = 64;         // positions of a chunk
-constexpr int kPitch = 68;              // floats of a row of 64 in LDS
+constexpr int kPitch = 68;              // elements of a row of 64 in LDS: rows of either element size start in different banks
 
 // What the kernels take.  Heads: H of values, H / each of keys and queries.  States are [B, H, chunks, DK, DV].
 template <typename T> struct DeltaShape {
@@ -23,6 +34,7 @@ template <typename T> struct DeltaShape {
     const int *lengths;
     int B, H, each, DK, DV, L, chunks;
     float scale, eps;
+    struct DeltaPairs *pairs;           // [B, H, chunks]
     __device__ __forceinline__ int length(int b) const { return lengths ? min(max(lengths[b], 0), L) : L; }
 };
 template <typename T> struct DeltaFwd : DeltaShape<T> {
@@ -37,6 +49,20 @@ template <typename T> struct DeltaBwd : DeltaShape<T> {
     float *after, *dg, *dbeta, *ds0;    // after: [B, H, chunks, DK, DV], the gradient of the state behind a chunk
 };
 
+// The per-position values of a chunk.
+struct Gates {
+    float eG[64], eC[64];       // exp(G_t), exp(G_63 - G_t)
+    float beta[64], rk[64], iq[64], rq[64];     // 1 / lengths of k and q; scale / length of q
+    double G[64];               // sums of the log decays, times log2(e)
+};
+// What a chunk's walk needs that does not depend on the state: the lower triangles of T, P and k k^T e, in blocks of 16 row by row.
+struct DeltaPairs {
+    float t[10][256], p[10][256], kk[10][256];
+    Gates s;
+};
+
+__device__ __forceinline__ f32x4 four(const float *x, int at) { return *reinterpret_cast<const f32x4 *>(x + at); }
+
 // D += A B of 16 x 16 x 16: a[v] = A[lane % 16][4 (lane / 16) + v], b[v] = B[4 (lane / 16) + v][lane % 16], and D as B, so that one
 // product's D is the next one's B as it stands.
 __device__ __forceinline__ f32x4 mma16(f32x4 a, f32x4 b, f32x4 d)
@@ -46,16 +72,126 @@ __device__ __forceinline__ f32x4 mma16(f32x4 a, f32x4 b, f32x4 d)
     return d;
 }
 // A's operand of rows m.. and columns k.. of a matrix in LDS: as it lies, or transposed.
-__device__ __forceinline__ f32x4 rows_of(const float *x, int m, int k, int pitch, int lane)
+__device__ __forceinline__ f32x4 rows_of(const float *x, int m, int k, int lane) { return four(x, (m + (lane & 15)) * kPitch + k + 4 * (lane >> 4)); }
+__device__ __forceinline__ f32x4 columns_of(const float *x, int m, int k, int lane)
 {
-    return *reinterpret_cast<const f32x4 *>(x + (m + (lane & 15)) * pitch + k + 4 * (lane >> 4));
+    const float *p = x + (k + 4 * (lane >> 4)) * kPitch + m + (lane & 15);
+    return f32x4{p[0], p[kPitch], p[2 * kPitch], p[3 * kPitch]};
 }
-__device__ __forceinline__ f32x4 columns_of(const float *x, int m, int k, int pitch, int lane)
-{
-    const float *p = x + (k + 4 * (lane >> 4)) * pitch + m + (lane & 15);
-    return f32x4{p[0], p[pitch], p[2 * pitch], p[3 * pitch]};
-}
-__device__ __forceinline__ f32x4 four(const float *x, int at) { return *reinterpret_cast<const f32x4 *>(x + at); }
+
+// Products of 16 x 32 x 16.  An operand is 32 terms deep: lane (c, g) holds terms 4 g + v and 16 + 4 g + v of its row or column c, which is how
+// two tiles of a product lie (split()), so that a product is the next one's operand without leaving the registers.
+// In: of a matrix stored as T; Full: of one in 32 bits.  A Full matrix in LDS is `planes` matrices, `plane` elements apart.
+template <typename T> struct Mat;
+template <> struct Mat<float> {
+    typedef float Elem;
+    static constexpr int planes = 1;
+    struct Full {
+        f32x4 a, b;
+    };
+    typedef Full In;
+    static __device__ __forceinline__ In rows_in(const float *x, int m, int k, int lane) { return In{rows_of(x, m, k, lane), rows_of(x, m, k + 16, lane)}; }
+    static __device__ __forceinline__ In columns_in(const float *x, int m, int k, int lane) { return In{columns_of(x, m, k, lane), columns_of(x, m, k + 16, lane)}; }
+    template <int N = 1> static __device__ __forceinline__ Full rows(const float *x, int, int m, int k, int lane) { return rows_in(x, m, k, lane); }
+    template <int N = 1> static __device__ __forceinline__ Full columns(const float *x, int, int m, int k, int lane) { return columns_in(x, m, k, lane); }
+    template <int N = 1> static __device__ __forceinline__ Full split(f32x4 a, f32x4 b) { return Full{a, b}; }
+    static __device__ __forceinline__ In exact(f32x4 a, f32x4 b) { return In{a, b}; }
+    static __device__ __forceinline__ f32x4 wide(const float *x, int at) { return four(x, at); }
+    static __device__ __forceinline__ void put_one(float *x, int, int at, float v) { x[at] = v; }
+    template <int ORDER = 3> static __device__ __forceinline__ f32x4 mma(Full a, Full b, f32x4 d) { return mma16(a.b, b.b, mma16(a.a, b.a, d)); }
+    template <int N = 1> static __device__ __forceinline__ void put(float *x, int, int at, f32x4 v) { *reinterpret_cast<f32x4 *>(x + at) = v; }
+};
+template <> struct Mat<bf16_t> {
+    typedef short Elem;
+    static constexpr int planes = 3;
+    struct In {
+        bf16x8 l[1];
+    };
+    struct Full {
+        bf16x8 l[3];
+    };
+    static __device__ __forceinline__ bf16x8 pair(u32x2 a, u32x2 b) { return __builtin_bit_cast(bf16x8, (u32x4{a[0], a[1], b[0], b[1]})); }
+    static __device__ __forceinline__ bf16x8 row(const short *x, int m, int k, int lane)
+    {
+        const short *p = x + (m + (lane & 15)) * kPitch + k + 4 * (lane >> 4);
+        return pair(*reinterpret_cast<const u32x2 *>(p), *reinterpret_cast<const u32x2 *>(p + 16));
+    }
+    // Sixteen lanes read four rows of sixteen elements, and get four elements of a column each.
+    static __device__ __forceinline__ u32x2 turned(const short *p)
+    {
+        return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)const_cast<short *>(p)));
+    }
+    static __device__ __forceinline__ bf16x8 column(const short *x, int m, int k, int lane)
+    {
+        const short *p = x + (k + (lane >> 4) * 4 + ((lane & 15) >> 2)) * kPitch + m + 4 * (lane & 3);
+        return pair(turned(p), turned(p + 16 * kPitch));
+    }
+    static __device__ __forceinline__ In rows_in(const short *x, int m, int k, int lane) { return In{{row(x, m, k, lane)}}; }
+    static __device__ __forceinline__ In columns_in(const short *x, int m, int k, int lane) { return In{{column(x, m, k, lane)}}; }
+    template <int N = 3> static __device__ __forceinline__ Full rows(const short *x, int plane, int m, int k, int lane)
+    {
+        Full f{};
+#pragma unroll
+        for (int n = 0; n < N; ++n) f.l[n] = row(x + n * plane, m, k, lane);
+        return f;
+    }
+    template <int N = 3> static __device__ __forceinline__ Full columns(const short *x, int plane, int m, int k, int lane)
+    {
+        Full f{};
+#pragma unroll
+        for (int n = 0; n < N; ++n) f.l[n] = column(x + n * plane, m, k, lane);
+        return f;
+    }
+    // The next limb of four values: the nearest bf16 to what is left of them, which x then is without it.
+    static __device__ __forceinline__ u32x2 limb(f32x4 &x)
+    {
+        const u32x2 w = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+        x = f32x4{x[0] - __uint_as_float(w[0] << 16), x[1] - __uint_as_float(w[0] & 0xffff0000u), x[2] - __uint_as_float(w[1] << 16),
+                  x[3] - __uint_as_float(w[1] & 0xffff0000u)};
+        return w;
+    }
+    template <int N = 3> static __device__ __forceinline__ Full split(f32x4 a, f32x4 b)
+    {
+        Full f{};
+#pragma unroll
+        for (int n = 0; n < N; ++n) f.l[n] = pair(limb(a), limb(b));
+        return f;
+    }
+    // ... of values that are bf16 already.
+    static __device__ __forceinline__ In exact(f32x4 a, f32x4 b)
+    {
+        return In{{pair(u32x2{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])}, u32x2{pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])})}};
+    }
+    static __device__ __forceinline__ f32x4 wide(const short *x, int at)
+    {
+        const u32x2 u = *reinterpret_cast<const u32x2 *>(x + at);
+        return f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xffff0000u), __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xffff0000u)};
+    }
+    // One element of a Full matrix of two planes.
+    static __device__ __forceinline__ void put_one(short *x, int plane, int at, float v)
+    {
+        const unsigned w = pack_bf16(v, 0.0f);
+        x[at] = (short)w;
+        x[at + plane] = (short)pack_bf16(v - __uint_as_float(w << 16), 0.0f);
+    }
+    // Products of limbs whose numbers add up to less than ORDER, the smallest first.
+    template <int ORDER = 3, typename A, typename B> static __device__ __forceinline__ f32x4 mma(const A &a, const B &b, f32x4 d)
+    {
+        constexpr int na = sizeof(a.l) / sizeof(bf16x8), nb = sizeof(b.l) / sizeof(bf16x8);
+#pragma unroll
+        for (int s = ORDER - 1; s >= 0; --s)
+#pragma unroll
+            for (int i = 0; i < na; ++i)
+                if (s - i >= 0 && s - i < nb) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.l[i], b.l[s - i], d, 0, 0, 0);
+        return d;
+    }
+    // Four neighbours of a row of a Full matrix.
+    template <int N = 3> static __device__ __forceinline__ void put(short *x, int plane, int at, f32x4 v)
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) *reinterpret_cast<u32x2 *>(x + n * plane + at) = limb(v);
+    }
+};
 
 // Four consecutive positions of a row, those from `n` on zero (and not read).
 template <typename T> __device__ __forceinline__ f32x4 load4(const T *row, int t, int n)
@@ -92,15 +228,7 @@ template <typename T> __device__ __forceinline__ void store4(T *row, f32x4 r, in
     }
 }
 
-// The per-position values of a chunk, in LDS.
-struct Gates {
-    double G[64];               // sums of the log decays, times log2(e)
-    float eG[64], eC[64];       // exp(G_t), exp(G_63 - G_t)
-    float beta[64], rk[64], iq[64], rq[64];     // 1 / lengths of k and q; scale / length of q
-    float part[3][8][64];       // sums of every wave
-};
-
-// exp2 of a difference of such sums, without what the argument's rounding to 32 bits loses.
+// exp2 of a difference of sums of log decays, without what the argument's rounding to 32 bits loses.
 __device__ __forceinline__ float exp2_of(double d)
 {
     const float t = (float)d, rest = (float)(d - (double)t);
@@ -108,99 +236,105 @@ __device__ __forceinline__ float exp2_of(double d)
     return t < -160.0f ? 0.0f : fmaf(h, rest * 0.6931471806f, h);
 }
 
-// Rows of [channels, 64 positions] into LDS in 32 bits, zeros behind row DK and behind position n.
-template <typename T> __device__ __forceinline__ void stage(float *to, const T *from, int DK, int rows, int t0, int n, int L)
-{
-    for (int i = threadIdx.x; i < rows * 8; i += blockDim.x) {
-        const int r = i >> 3, t = t0 + (i & 7) * 8;
-        float v[8] = {};
-        if (r < DK && t < n) {
-            const T *row = from + (long long)r * L;
-            if (t + 8 <= L) {
-                const Eight<T> e = load8(row + t);
+// Rows of [channels, 64 positions] on their way into LDS as they are, N eights a lane; zeros behind row D and behind position n.
+template <typename T, int ROWS, int LANES> struct Tile {
+    static constexpr int N = (ROWS * 8 + LANES - 1) / LANES;
+    Eight<T> e[N];
+    __device__ __forceinline__ void load(const T *from, int D, int t0, int n, int L)
+    {
+        if (t0 + 64 <= L) {             // (no load asks first: none waits for another)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = t + k < n ? e[k] : 0.0f;
-            } else {
+            for (int u = 0; u < N; ++u) {
+                const int i = threadIdx.x + u * LANES, r = i >> 3;
+                e[u] = load8(from + (long long)(r < D ? r : 0) * L + t0 + (i & 7) * 8);
+            }
+        } else {
 #pragma unroll
-                for (int k = 0; k < 7; ++k)
-                    if (t + k < n) v[k] = ld_elem(row + t + k);
+            for (int u = 0; u < N; ++u) {
+                const int i = threadIdx.x + u * LANES, r = i >> 3, t = t0 + (i & 7) * 8;
+                Few<8, T> f{};
+                if (r < D && t < n) f = load_few<8>(from + (long long)r * L + t, min(8, L - t));
+                __builtin_memcpy(&e[u], &f, sizeof(f));
             }
         }
-        f32x4 *p = reinterpret_cast<f32x4 *>(to + r * kPitch + (i & 7) * 8);
-        p[0] = f32x4{v[0], v[1], v[2], v[3]};
-        p[1] = f32x4{v[4], v[5], v[6], v[7]};
     }
-}
-
-// Sums of squares over the channels, a wave's share of them.
-template <int KT> __device__ __forceinline__ void squares(Gates &s, const float *sk, const float *sq)
-{
-    const int t = threadIdx.x & 63, w = threadIdx.x >> 6, W = blockDim.x >> 6;
-    float a = 0.0f, b = 0.0f;
-    for (int r = w; r < 16 * KT; r += W) {
-        const float x = sk[r * kPitch + t], y = sq[r * kPitch + t];
-        a = fmaf(x, x, a), b = fmaf(y, y, b);
-    }
-    s.part[0][w][t] = a, s.part[1][w][t] = b;
-}
-// ... and everything else that a position has one of: by the first wave.
-template <typename T> __device__ __forceinline__ void gates(Gates &s, const DeltaShape<T> &p, int b, int h, int t0, int n)
-{
-    const int t = threadIdx.x, W = blockDim.x >> 6;
-    if (t >= 64) return;
-    float g = 0.0f, beta = 0.0f;
-    if (t0 + t < n) {
-        g = p.g.row(b, h, p.L)[t0 + t];
-        beta = p.beta.row(b, h, p.L)[t0 + t];
-    }
-    // (below -128 a decay is 0 in 32 bits; a sum with minus infinity would leave nothing of the differences behind it)
-    double G = (double)(g < -128.0f ? -128.0f : g) * 1.4426950408889634;
+    __device__ __forceinline__ void put(typename Mat<T>::Elem *to, int D, int t0, int n) const
+    {
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const double o = __shfl_up(G, d, 64);
-        if (t >= d) G += o;
+        for (int u = 0; u < N; ++u) {
+            const int i = threadIdx.x + u * LANES, r = i >> 3, left = n - t0 - (i & 7) * 8;
+            if (ROWS * 8 % LANES && r >= ROWS) continue;
+            put_eight(to + r * kPitch + (i & 7) * 8, e[u], r < D ? left : 0);
+        }
     }
-    const double whole = __shfl(G, 63, 64);
-    s.G[t] = G;
-    s.eG[t] = exp2_of(G);
-    s.eC[t] = exp2_of(whole - G);
-    s.beta[t] = beta;
-    float k2 = 0.0f, q2 = 0.0f;
-    for (int w = 0; w < W; ++w) k2 += s.part[0][w][t], q2 += s.part[1][w][t];
-    const bool unit = p.eps > 0.0f;
-    s.rk[t] = unit ? 1.0f / sqrtf(k2 + p.eps) : 1.0f;
-    s.iq[t] = unit ? 1.0f / sqrtf(q2 + p.eps) : 1.0f;
-    s.rq[t] = p.scale * s.iq[t];
-}
+    static __device__ __forceinline__ void put_eight(float *to, const Eight<float> &e, int left)
+    {
+        f32x4 a = e.lo, b = e.hi;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) a[k] = k < left ? a[k] : 0.0f, b[k] = k + 4 < left ? b[k] : 0.0f;
+        f32x4 *p = reinterpret_cast<f32x4 *>(to);
+        p[0] = a, p[1] = b;
+    }
+    static __device__ __forceinline__ void put_eight(short *to, const Eight<bf16_t> &e, int left)
+    {
+        u32x4 w = e.w;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = 2 * k + 1 < left ? w[k] : 2 * k < left ? w[k] & 0xffffu : 0u;
+        u32x2 *p = reinterpret_cast<u32x2 *>(to);
+        p[0] = u32x2{w[0], w[1]}, p[1] = u32x2{w[2], w[3]};
+    }
+};
 
 __device__ __forceinline__ void low_tile(int i, int &ti, int &tj)     // tile i of the lower triangle, row by row
 {
     ti = i >= 6 ? 3 : i >= 3 ? 2 : i >= 1 ? 1 : 0;
     tj = i - ti * (ti + 1) / 2;
 }
-// A tile of (x k^T) e, transposed: lane (c, g) has columns j = 16 tj + 4 g + v of row i = 16 ti + c.
-template <int KT> __device__ __forceinline__ f32x4 pair_tile(const float *sx, const float *sk, int ti, int tj, int lane)
-{
-    f32x4 d = {};
+// The lower triangle of a chunk's matrix on its way from a record into LDS as a Full matrix.
+template <typename T, int LANES> struct LowTiles {
+    static constexpr int N = (640 + LANES - 1) / LANES;
+    f32x4 x[N];
+    __device__ __forceinline__ void load(const float (&from)[10][256])
+    {
 #pragma unroll
-    for (int kb = 0; kb < KT; ++kb) d = mma16(columns_of(sk, 16 * tj, 16 * kb, kPitch, lane), columns_of(sx, 16 * ti, 16 * kb, kPitch, lane), d);
-    return d;
-}
-// e(i, j) where j < i (or j <= i), else 0.
-__device__ __forceinline__ f32x4 decays(const Gates &s, int ti, int tj, int lane, bool with_diagonal)
-{
-    const int i = 16 * ti + (lane & 15), j = 16 * tj + 4 * (lane >> 4);
-    f32x4 e;
+        for (int u = 0; u < N; ++u) {
+            const int i = threadIdx.x + u * LANES;
+            x[u] = four(from[0], 4 * (640 % LANES ? min(i, 639) : i));
+        }
+    }
+    __device__ __forceinline__ void put(typename Mat<T>::Elem *to) const
+    {
 #pragma unroll
-    for (int v = 0; v < 4; ++v) e[v] = j + v < i || (with_diagonal && j + v == i) ? exp2_of(s.G[i] - s.G[j + v]) : 0.0f;
-    return e;
-}
+        for (int u = 0; u < N; ++u) {
+            const int i = threadIdx.x + u * LANES;
+            if (640 % LANES && i >= 640) continue;
+            int ti, tj;
+            low_tile(i >> 6, ti, tj);
+            Mat<T>::put(to, 64 * kPitch, (16 * ti + ((i & 63) >> 2)) * kPitch + 16 * tj + 4 * (i & 3), x[u]);
+        }
+    }
+    // What a product 32 deep takes beside the triangle: blocks (0, 1) and (2, 3), zeros, written once.
+    static __device__ __forceinline__ void zeros(typename Mat<T>::Elem *to)
+    {
+        for (int i = threadIdx.x; i < 2 * 64; i += LANES)
+            Mat<T>::put(to, 64 * kPitch, ((i >> 6) * 32 + ((i & 63) >> 2)) * kPitch + (i >> 6) * 32 + 16 + 4 * (i & 3), f32x4{});
+    }
+};
+
+// ---- what does not depend on the state ----
+
+template <typename T, int KT> struct PairsLds {
+    typename Mat<T>::Elem k[16 * KT * kPitch], q[16 * KT * kPitch];
+    float a[64 * kPitch], t[64 * kPitch];
+    Gates s;
+    float part[2][4][64];
+};
 
 // T = (I + A)^-1 of A in LDS: the inverses of its diagonal blocks of 16 by substitution, a column a lane, and from them block column
-// after block column.  By all waves; T's blocks above the diagonal are not written.
+// after block column.  By four waves; T's blocks above the diagonal are not written.
 __device__ __forceinline__ void invert(const float *A, float *T)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, W = blockDim.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (wave == 0) {
         const int b = lane >> 4, c = lane & 15;
         const float *a = A + 16 * b * kPitch + 16 * b;
@@ -221,103 +355,206 @@ __device__ __forceinline__ void invert(const float *A, float *T)
         for (int i = 0; i < 16; ++i) T[(16 * b + i) * kPitch + 16 * b + c] = x[i];
     }
     __syncthreads();
-    for (int j = wave; j < 3; j += W) {
+    if (const int j = wave; j < 3) {
         f32x4 col[4];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) col[m] = f32x4{};
-#pragma unroll
         for (int m = 0; m < 4; ++m) {
+            col[m] = f32x4{};
             if (m < j) continue;
             if (m == j) {
-                col[m] = columns_of(T, 16 * j, 16 * j, kPitch, lane);       // (as B: rows 4 g + v, column c)
+                col[m] = columns_of(T, 16 * j, 16 * j, lane);       // (as B: rows 4 g + v, column c)
             } else {
                 f32x4 sum = {};
 #pragma unroll
                 for (int o = 0; o < 3; ++o)
-                    if (o >= j && o < m) sum = mma16(rows_of(A, 16 * m, 16 * o, kPitch, lane), col[o], sum);
-                const f32x4 t = mma16(rows_of(T, 16 * m, 16 * m, kPitch, lane), sum, f32x4{});
-                col[m] = -t;
+                    if (o >= j && o < m) sum = mma16(rows_of(A, 16 * m, 16 * o, lane), col[o], sum);
+                col[m] = -mma16(rows_of(T, 16 * m, 16 * m, lane), sum, f32x4{});
 #pragma unroll
-                for (int v = 0; v < 4; ++v) T[(16 * m + 4 * (lane >> 4) + v) * kPitch + 16 * j + (lane & 15)] = -t[v];
+                for (int v = 0; v < 4; ++v) T[(16 * m + 4 * (lane >> 4) + v) * kPitch + 16 * j + (lane & 15)] = col[m][v];
             }
         }
     }
     __syncthreads();
 }
 
-// Sums of 64 rows: k of a chunk (rows of sx, transposed) times a state's columns.
-template <int KT> __device__ __forceinline__ void times_state(f32x4 (&d)[4], const float *sx, const f32x4 (&S)[KT], int lane)
+// A record of every chunk with a position inside: by a workgroup of four waves.
+template <typename T, int KT> __device__ __forceinline__ void delta_pairs(const DeltaShape<T> &p, PairsLds<T, KT> &m, int unit)
 {
+    typedef Mat<T> M;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, g4 = 4 * (lane >> 4);
+    const int ch = unit % p.chunks, bh = unit / p.chunks, b = bh / p.H, h = bh % p.H, hk = h / p.each, n = p.length(b), t0 = ch * kDeltaChunk;
+    if (t0 >= n) return;
+    DeltaPairs &to = p.pairs[unit];
+    Tile<T, 16 * KT, 256> k, q;
+    k.load(p.k.row(b, hk * p.DK, p.L), p.DK, t0, n, p.L);
+    q.load(p.q.row(b, hk * p.DK, p.L), p.DK, t0, n, p.L);
+    float g = 0.0f, beta = 0.0f;
+    if (wave == 0 && t0 + lane < n) {
+        g = p.g.row(b, h, p.L)[t0 + lane];
+        beta = p.beta.row(b, h, p.L)[t0 + lane];
+    }
+    k.put(m.k, p.DK, t0, n);
+    q.put(m.q, p.DK, t0, n);
+    __syncthreads();
+    {
+        float x = 0.0f, y = 0.0f;
+#pragma unroll 8
+        for (int r = wave; r < 16 * KT; r += 4) {
+            float u, v;
+            if constexpr (sizeof(T) == 4) u = m.k[r * kPitch + lane], v = m.q[r * kPitch + lane];
+            else u = __uint_as_float((unsigned)(unsigned short)m.k[r * kPitch + lane] << 16), v = __uint_as_float((unsigned)(unsigned short)m.q[r * kPitch + lane] << 16);
+            x = fmaf(u, u, x), y = fmaf(v, v, y);
+        }
+        m.part[0][wave][lane] = x, m.part[1][wave][lane] = y;
+    }
+    if (wave == 0) {
+        // (below -128 a decay is 0 in 32 bits; a sum with minus infinity would leave nothing of the differences behind it)
+        double G = (double)(g < -128.0f ? -128.0f : g) * 1.4426950408889634;
 #pragma unroll
-    for (int kb = 0; kb < KT; ++kb)
+        for (int d = 1; d < 64; d *= 2) {
+            const double o = __shfl_up(G, d, 64);
+            if (lane >= d) G += o;
+        }
+        const double whole = __shfl(G, 63, 64);
+        m.s.G[lane] = G;
+        m.s.eG[lane] = exp2_of(G);
+        m.s.eC[lane] = exp2_of(whole - G);
+        m.s.beta[lane] = beta;
+    }
+    __syncthreads();
+    if (tid < 64) {
+        const float k2 = (m.part[0][0][tid] + m.part[0][1][tid]) + (m.part[0][2][tid] + m.part[0][3][tid]);
+        const float q2 = (m.part[1][0][tid] + m.part[1][1][tid]) + (m.part[1][2][tid] + m.part[1][3][tid]);
+        const bool unit = p.eps > 0.0f;
+        m.s.rk[tid] = unit ? 1.0f / sqrtf(k2 + p.eps) : 1.0f;
+        m.s.iq[tid] = unit ? 1.0f / sqrtf(q2 + p.eps) : 1.0f;
+        m.s.rq[tid] = p.scale * m.s.iq[tid];
+    }
+    __syncthreads();
+    for (int task = wave; task < 20; task += 4) {
+        int ti, tj;
+        low_tile(task >> 1, ti, tj);
+        const bool is_p = task & 1;
+        const int i = 16 * ti + c, j = 16 * tj + g4;        // (transposed: lane (c, g) has columns 16 tj + 4 g + v of row 16 ti + c)
+        f32x4 d = {};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) d[i] = mma16(columns_of(sx, 16 * i, 16 * kb, kPitch, lane), S[kb], d[i]);
+        for (int kb = 0; kb < KT; kb += 2)
+            d = M::mma(M::columns_in(m.k, 16 * tj, 16 * kb, lane), M::columns_in(is_p ? m.q : m.k, 16 * ti, 16 * kb, lane), d);
+        f32x4 e;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) e[v] = j + v < i || (is_p && j + v == i) ? exp2_of(m.s.G[i] - m.s.G[j + v]) : 0.0f;
+        d = d * e * four(m.s.rk, j) * (is_p ? m.s.rq[i] : m.s.rk[i]);
+        *reinterpret_cast<f32x4 *>((is_p ? to.p : to.kk)[task >> 1] + 16 * c + g4) = d;
+        if (!is_p) *reinterpret_cast<f32x4 *>(m.a + i * kPitch + j) = d * m.s.beta[i];
+    }
+    __syncthreads();
+    invert(m.a, m.t);
+    for (int i = tid; i < 640; i += 256) {
+        int ti, tj;
+        low_tile(i >> 6, ti, tj);
+        *reinterpret_cast<f32x4 *>(to.t[i >> 6] + 4 * (i & 63)) = four(m.t, (16 * ti + ((i & 63) >> 2)) * kPitch + 16 * tj + 4 * (i & 3));
+    }
+    for (int i = tid; i < (int)sizeof(Gates) / 16; i += 256) reinterpret_cast<f32x4 *>(&to.s)[i] = reinterpret_cast<const f32x4 *>(&m.s)[i];
+}
+// (a grid has fewer than 2^32 lanes in a dimension: of very many chunks or heads several to a workgroup)
+template <typename T, int KT> __global__ __launch_bounds__(256) void delta_pairs_kernel(DeltaShape<T> p)
+{
+    extern __shared__ char lds[];
+    for (int unit = blockIdx.x, units = p.B * p.H * p.chunks; unit < units; unit += gridDim.x) {
+        delta_pairs(p, *reinterpret_cast<PairsLds<T, KT> *>(lds), unit);
+        __syncthreads();
+    }
 }
 
+// ---- from chunk to chunk ----
+
 template <typename T, int KT> struct DeltaLds {
-    float k[16 * KT * kPitch], q[16 * KT * kPitch];
-    float a[64 * kPitch], p[64 * kPitch], t[64 * kPitch];
+    typename Mat<T>::Elem k[16 * KT * kPitch], q[16 * KT * kPitch];
+    typename Mat<T>::Elem t[Mat<T>::planes * 64 * kPitch], p[Mat<T>::planes * 64 * kPitch];
     Gates s;
 };
+// A chunk's data on its way into LDS, while the chunk before is worked at.
+template <typename T, int KT, int W> struct Ahead {
+    Tile<T, 16 * KT, 64 * W> k, q;
+    LowTiles<T, 64 * W> t, p;
+    static constexpr int NG = sizeof(Gates) / 16;
+    f32x4 s;
+    __device__ __forceinline__ void load(const DeltaShape<T> &a, const T *krow, const T *qrow, const DeltaPairs *r, int t0, int n)
+    {
+        k.load(krow, a.DK, t0, n, a.L);
+        q.load(qrow, a.DK, t0, n, a.L);
+        t.load(r->t);
+        p.load(r->p);
+        s = reinterpret_cast<const f32x4 *>(&r->s)[threadIdx.x < NG ? threadIdx.x : 0];
+    }
+    __device__ __forceinline__ void put(DeltaLds<T, KT> &m, int DK, int t0, int n) const
+    {
+        k.put(m.k, DK, t0, n);
+        q.put(m.q, DK, t0, n);
+        t.put(m.t);
+        p.put(m.p);
+        if (threadIdx.x < NG) reinterpret_cast<f32x4 *>(&m.s)[threadIdx.x] = s;
+    }
+};
 
-// Forward.  A workgroup has a head's state, a wave 16 of its columns in registers; it walks the head's chunks.
-template <typename T, int KT> __device__ __forceinline__ void delta_fwd_head(const DeltaFwd<T> &p, DeltaLds<T, KT> &m, int unit)
+// A wave's 16 columns of a state.  (The row's part of an address is the wave's, so that no lane holds one for every row.)
+template <int KT> __device__ __forceinline__ void load_state(f32x4 (&S)[KT], const float *from, int DK, int DV, int dv, bool in, int g4)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, W = blockDim.x >> 6, c = lane & 15, g4 = 4 * (lane >> 4);
-    const int b = unit / p.H, h = unit % p.H, hk = h / p.each, n = p.length(b);
-    const int dv = (blockIdx.y * W + wave) * 16 + c;
-    const bool in = dv < p.DV;
-    const long long head = (long long)b * p.H + h;
-    f32x4 S[KT];
+    const unsigned at = (unsigned)(g4 * DV + dv);
 #pragma unroll
     for (int kb = 0; kb < KT; ++kb)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const int r = 16 * kb + g4 + v;
-            S[kb][v] = p.s0 && in && r < p.DK ? p.s0[(head * p.DK + r) * p.DV + dv] : 0.0f;
-        }
-    const T *vrow = p.v.row(b, h * p.DV + (in ? dv : 0), p.L);
+        for (int v = 0; v < 4; ++v) S[kb][v] = in && 16 * kb + v + g4 < DK ? (from + (16 * kb + v) * DV)[at] : 0.0f;
+}
+template <int KT> __device__ __forceinline__ void store_state(const f32x4 (&S)[KT], float *to, int DK, int DV, int dv, bool in, int g4)
+{
+    if (!in) return;
+    const unsigned at = (unsigned)(g4 * DV + dv);
+#pragma unroll
+    for (int kb = 0; kb < KT; ++kb)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            if (16 * kb + v + g4 < DK) (to + (16 * kb + v) * DV)[at] = S[kb][v];
+}
+
+// Forward.  A workgroup has a head's state, a wave 16 of its columns in registers; it walks the head's chunks.
+template <typename T, int KT, int W> __device__ __forceinline__ void delta_fwd_head(const DeltaFwd<T> &p, DeltaLds<T, KT> &m, int unit)
+{
+    typedef Mat<T> M;
+    constexpr int PL = 64 * kPitch;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g4 = 4 * (lane >> 4);
+    const int b = unit / p.H, h = unit % p.H, hk = h / p.each, n = p.length(b), last = (n + 63) / 64;
+    const int dv = (blockIdx.y * W + wave) * 16 + c;
+    const bool in = dv < p.DV, active = dv - c < p.DV;
+    const long long head = (long long)b * p.H + h, size = (long long)p.DK * p.DV;
+    f32x4 S[KT] = {};
+    if (p.s0) load_state(S, p.s0 + head * size, p.DK, p.DV, dv, in, g4);
+    const T *vrow = p.v.row(b, h * p.DV + (in ? dv : 0), p.L), *krow = p.k.row(b, hk * p.DK, p.L), *qrow = p.q.row(b, hk * p.DK, p.L);
     T *orow = p.o.row(b, h * p.DV + (in ? dv : 0), p.L);
-    for (int ch = 0; ch < p.chunks; ++ch) {
+    const DeltaPairs *pairs = p.pairs + head * p.chunks;
+    Ahead<T, KT, W> next;
+    f32x4 val[4] = {};
+    if (last > 0) next.load(p, krow, qrow, pairs, 0, n);
+    for (int ch = 0; ch < last; ++ch) {
         const int t0 = ch * kDeltaChunk;
-        if (p.states && in)
-#pragma unroll
-            for (int kb = 0; kb < KT; ++kb)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const int r = 16 * kb + g4 + v;
-                    if (r < p.DK) p.states[((head * p.chunks + ch) * p.DK + r) * p.DV + dv] = S[kb][v];
-                }
-        if (t0 >= n) {
-            if (in)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) store4(orow, f32x4{}, t0 + 16 * i + g4, p.L);
-            continue;
-        }
-        stage(m.k, p.k.row(b, hk * p.DK, p.L), p.DK, 16 * KT, t0, n, p.L);
-        stage(m.q, p.q.row(b, hk * p.DK, p.L), p.DK, 16 * KT, t0, n, p.L);
-        f32x4 val[4];
+        __syncthreads();
+        next.put(m, p.DK, t0, n);
 #pragma unroll
         for (int i = 0; i < 4; ++i) val[i] = in ? load4(vrow, t0 + 16 * i + g4, n) : f32x4{};
+        if (p.states) store_state(S, p.states + (head * p.chunks + ch) * size, p.DK, p.DV, dv, in, g4);
         __syncthreads();
-        squares<KT>(m.s, m.k, m.q);
-        __syncthreads();
-        gates(m.s, p, b, h, t0, n);
-        __syncthreads();
-        for (int task = wave; task < 20; task += W) {
-            int ti, tj;
-            low_tile(task >= 10 ? task - 10 : task, ti, tj);
-            const bool is_p = task >= 10;
-            const int i = 16 * ti + c, j = 16 * tj + g4;
-            f32x4 d = pair_tile<KT>(is_p ? m.q : m.k, m.k, ti, tj, lane) * decays(m.s, ti, tj, lane, is_p) * four(m.s.rk, j);
-            d *= is_p ? m.s.rq[i] : m.s.rk[i] * m.s.beta[i];
-            *reinterpret_cast<f32x4 *>((is_p ? m.p : m.a) + i * kPitch + j) = d;
-        }
-        __syncthreads();
-        invert(m.a, m.t);
+        if (ch + 1 < last) next.load(p, krow, qrow, pairs + ch + 1, t0 + 64, n);
+        if (!active) continue;
         f32x4 r[4] = {}, w[4] = {}, o[4] = {};
-        times_state<KT>(r, m.k, S, lane);
-        times_state<KT>(o, m.q, S, lane);
+#pragma unroll
+        for (int kb = 0; kb < KT; kb += 2) {
+            const typename M::Full s = M::split(S[kb], S[kb + 1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                r[i] = M::mma(M::columns_in(m.k, 16 * i, 16 * kb, lane), s, r[i]);
+                o[i] = M::template mma<2>(M::columns_in(m.q, 16 * i, 16 * kb, lane), s, o[i]);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = 16 * i + g4;
@@ -325,151 +562,131 @@ template <typename T, int KT> __device__ __forceinline__ void delta_fwd_head(con
             o[i] *= four(m.s.eG, t) * four(m.s.rq, t);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int kb = 0; kb < 2; ++kb) {
+            const typename M::Full x = M::split(r[2 * kb], r[2 * kb + 1]);
 #pragma unroll
-            for (int j = 0; j <= i; ++j) w[i] = mma16(rows_of(m.t, 16 * i, 16 * j, kPitch, lane), r[j], w[i]);
+            for (int i = 2 * kb; i < 4; ++i) w[i] = M::mma(M::rows(m.t, PL, 16 * i, 32 * kb, lane), x, w[i]);
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int kb = 0; kb < 2; ++kb) {
+            const typename M::Full x = M::template split<2>(w[2 * kb], w[2 * kb + 1]);
 #pragma unroll
-            for (int j = 0; j <= i; ++j) o[i] = mma16(rows_of(m.p, 16 * i, 16 * j, kPitch, lane), w[j], o[i]);
+            for (int i = 2 * kb; i < 4; ++i) o[i] = M::template mma<2>(M::template rows<2>(m.p, PL, 16 * i, 32 * kb, lane), x, o[i]);
+        }
         const float eA = m.s.eG[63];
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] *= four(m.s.eC, 16 * i + g4) * four(m.s.rk, 16 * i + g4);
 #pragma unroll
-        for (int kb = 0; kb < KT; ++kb) {
-            S[kb] *= eA;
+        for (int kb = 0; kb < KT; ++kb) S[kb] *= eA;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) S[kb] = mma16(rows_of(m.k, 16 * kb, 16 * j, kPitch, lane), w[j], S[kb]);
+        for (int j = 0; j < 2; ++j) {
+            const typename M::Full x = M::split(w[2 * j], w[2 * j + 1]);
+#pragma unroll
+            for (int kb = 0; kb < KT; ++kb) S[kb] = M::mma(M::rows_in(m.k, 16 * kb, 32 * j, lane), x, S[kb]);
         }
         if (in)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = t0 + 16 * i + g4;
-                store4(orow, o[i], t, p.L);         // (k and q behind n are zeros, so these are)
-            }
-        __syncthreads();
+            for (int i = 0; i < 4; ++i) store4(orow, o[i], t0 + 16 * i + g4, p.L);        // (k and q behind n are zeros, so these are)
     }
-    if (p.s_last && in)
-#pragma unroll
-        for (int kb = 0; kb < KT; ++kb)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int r = 16 * kb + g4 + v;
-                if (r < p.DK) p.s_last[(head * p.DK + r) * p.DV + dv] = S[kb][v];
-            }
+    if (in)
+        for (int t = last * 64 + g4; t < p.L; t += 16) store4(orow, f32x4{}, t, p.L);
+    if (p.s_last) store_state(S, p.s_last + head * size, p.DK, p.DV, dv, in, g4);
 }
-// (a grid has fewer than 2^32 lanes in a dimension: of very many heads several to a workgroup)
-template <typename T, int KT> __global__ __launch_bounds__(512) void delta_fwd_kernel(DeltaFwd<T> p)
+template <typename T, int KT, int W> __global__ __launch_bounds__(64 * W) void delta_fwd_kernel(DeltaFwd<T> p)
 {
     extern __shared__ char lds[];
-    for (int unit = blockIdx.x, units = p.B * p.H; unit < units; unit += gridDim.x) delta_fwd_head(p, *reinterpret_cast<DeltaLds<T, KT> *>(lds), unit);
+    DeltaLds<T, KT> &m = *reinterpret_cast<DeltaLds<T, KT> *>(lds);
+    LowTiles<T, 64 * W>::zeros(m.t);
+    LowTiles<T, 64 * W>::zeros(m.p);
+    for (int unit = blockIdx.x, units = p.B * p.H; unit < units; unit += gridDim.x) delta_fwd_head<T, KT, W>(p, m, unit);
 }
 
 // Backward, from chunk to chunk: with dS the gradient of the state behind a chunk,
 //     dw = P^T do + exp(G_63 - G) k dS,   (I + A)^T dr = dw,   dS <- exp(G_63) dS + sum_i exp(G_i) q_i do_i^T - beta_i exp(G_i) k_i dr_i^T.
 // Leaves dS behind every chunk, and dv = beta dr.
-template <typename T, int KT> __device__ __forceinline__ void delta_bwd_head(const DeltaBwd<T> &p, DeltaLds<T, KT> &m, int unit)
+template <typename T, int KT, int W> __device__ __forceinline__ void delta_bwd_head(const DeltaBwd<T> &p, DeltaLds<T, KT> &m, int unit)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, W = blockDim.x >> 6, c = lane & 15, g4 = 4 * (lane >> 4);
-    const int b = unit / p.H, h = unit % p.H, hk = h / p.each, n = p.length(b);
+    typedef Mat<T> M;
+    constexpr int PL = 64 * kPitch;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g4 = 4 * (lane >> 4);
+    const int b = unit / p.H, h = unit % p.H, hk = h / p.each, n = p.length(b), last = (n + 63) / 64;
     const int dv = (blockIdx.y * W + wave) * 16 + c;
-    const bool in = dv < p.DV;
-    const long long head = (long long)b * p.H + h;
-    f32x4 S[KT];
-#pragma unroll
-    for (int kb = 0; kb < KT; ++kb)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const int r = 16 * kb + g4 + v;
-            S[kb][v] = p.ds_last && in && r < p.DK ? p.ds_last[(head * p.DK + r) * p.DV + dv] : 0.0f;
-        }
-    const T *orow = p.dout.row(b, h * p.DV + (in ? dv : 0), p.L);
+    const bool in = dv < p.DV, active = dv - c < p.DV;
+    const long long head = (long long)b * p.H + h, size = (long long)p.DK * p.DV;
+    f32x4 S[KT] = {};
+    if (p.ds_last) load_state(S, p.ds_last + head * size, p.DK, p.DV, dv, in, g4);
+    const T *drow = p.dout.row(b, h * p.DV + (in ? dv : 0), p.L), *krow = p.k.row(b, hk * p.DK, p.L), *qrow = p.q.row(b, hk * p.DK, p.L);
     T *vrow = p.dv.row(b, h * p.DV + (in ? dv : 0), p.L);
-    for (int ch = p.chunks - 1; ch >= 0; --ch) {
+    const DeltaPairs *pairs = p.pairs + head * p.chunks;
+    if (in)
+        for (int t = last * 64 + g4; t < p.L; t += 16) store4(vrow, f32x4{}, t, p.L);
+    Ahead<T, KT, W> next;
+    f32x4 d[4] = {};
+    if (last > 0) next.load(p, krow, qrow, pairs + last - 1, (last - 1) * 64, n);
+    for (int ch = last - 1; ch >= 0; --ch) {
         const int t0 = ch * kDeltaChunk;
-        if (t0 >= n) {
-            if (in)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) store4(vrow, f32x4{}, t0 + 16 * i + g4, p.L);
-            continue;
-        }
-        if (in)
-#pragma unroll
-            for (int kb = 0; kb < KT; ++kb)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const int r = 16 * kb + g4 + v;
-                    if (r < p.DK) p.after[((head * p.chunks + ch) * p.DK + r) * p.DV + dv] = S[kb][v];
-                }
-        stage(m.k, p.k.row(b, hk * p.DK, p.L), p.DK, 16 * KT, t0, n, p.L);
-        stage(m.q, p.q.row(b, hk * p.DK, p.L), p.DK, 16 * KT, t0, n, p.L);
-        f32x4 d[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) d[i] = in ? load4(orow, t0 + 16 * i + g4, n) : f32x4{};
         __syncthreads();
-        squares<KT>(m.s, m.k, m.q);
+        next.put(m, p.DK, t0, n);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] = in ? load4(drow, t0 + 16 * i + g4, n) : f32x4{};
+        store_state(S, p.after + (head * p.chunks + ch) * size, p.DK, p.DV, dv, in, g4);
         __syncthreads();
-        gates(m.s, p, b, h, t0, n);
-        __syncthreads();
-        for (int task = wave; task < 20; task += W) {
-            int ti, tj;
-            low_tile(task >= 10 ? task - 10 : task, ti, tj);
-            const bool is_p = task >= 10;
-            const int i = 16 * ti + c, j = 16 * tj + g4;
-            f32x4 x = pair_tile<KT>(is_p ? m.q : m.k, m.k, ti, tj, lane) * decays(m.s, ti, tj, lane, is_p) * four(m.s.rk, j);
-            x *= is_p ? m.s.rq[i] : m.s.rk[i] * m.s.beta[i];
-            *reinterpret_cast<f32x4 *>((is_p ? m.p : m.a) + i * kPitch + j) = x;
-        }
-        __syncthreads();
-        invert(m.a, m.t);
+        if (ch > 0) next.load(p, krow, qrow, pairs + ch - 1, t0 - 64, n);
+        if (!active) continue;
         f32x4 w[4] = {}, r[4] = {};
-        times_state<KT>(w, m.k, S, lane);
+#pragma unroll
+        for (int kb = 0; kb < KT; kb += 2) {
+            const typename M::Full s = M::split(S[kb], S[kb + 1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = M::mma(M::columns_in(m.k, 16 * i, 16 * kb, lane), s, w[i]);
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] *= four(m.s.eC, 16 * i + g4) * four(m.s.rk, 16 * i + g4);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int kb = 0; kb < 2; ++kb) {
+            const typename M::In x = M::exact(d[2 * kb], d[2 * kb + 1]);
 #pragma unroll
-            for (int i = j; i < 4; ++i) w[j] = mma16(columns_of(m.p, 16 * j, 16 * i, kPitch, lane), d[i], w[j]);
+            for (int j = 0; j < 2 * kb + 2; ++j) w[j] = M::mma(M::columns(m.p, PL, 16 * j, 32 * kb, lane), x, w[j]);
+        }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int kb = 0; kb < 2; ++kb) {
+            const typename M::Full x = M::split(w[2 * kb], w[2 * kb + 1]);
 #pragma unroll
-            for (int i = j; i < 4; ++i) r[j] = mma16(columns_of(m.t, 16 * j, 16 * i, kPitch, lane), w[i], r[j]);
+            for (int j = 0; j < 2 * kb + 2; ++j) r[j] = M::mma(M::columns(m.t, PL, 16 * j, 32 * kb, lane), x, r[j]);
+        }
         const float eA = m.s.eG[63];
-        f32x4 dvt[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = 16 * i + g4;
-            dvt[i] = four(m.s.beta, t) * r[i];
-            r[i] = -(dvt[i] * four(m.s.eG, t) * four(m.s.rk, t));
+            r[i] *= four(m.s.beta, t);
+            if (in) store4(vrow, r[i], t0 + t, p.L);
+            r[i] *= -four(m.s.eG, t) * four(m.s.rk, t);
             d[i] *= four(m.s.eG, t) * four(m.s.rq, t);
         }
 #pragma unroll
-        for (int kb = 0; kb < KT; ++kb) {
-            S[kb] *= eA;
+        for (int kb = 0; kb < KT; ++kb) S[kb] *= eA;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) S[kb] = mma16(rows_of(m.q, 16 * kb, 16 * j, kPitch, lane), d[j], S[kb]);
+        for (int j = 0; j < 2; ++j) {
+            const typename M::Full x = M::split(d[2 * j], d[2 * j + 1]), y = M::split(r[2 * j], r[2 * j + 1]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) S[kb] = mma16(rows_of(m.k, 16 * kb, 16 * j, kPitch, lane), r[j], S[kb]);
-        }
-        if (in)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) store4(vrow, dvt[i], t0 + 16 * i + g4, p.L);
-        __syncthreads();
-    }
-    if (p.ds0 && in)
-#pragma unroll
-        for (int kb = 0; kb < KT; ++kb)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int r = 16 * kb + g4 + v;
-                if (r < p.DK) p.ds0[(head * p.DK + r) * p.DV + dv] = S[kb][v];
+            for (int kb = 0; kb < KT; ++kb) {
+                S[kb] = M::mma(M::rows_in(m.q, 16 * kb, 32 * j, lane), x, S[kb]);
+                S[kb] = M::mma(M::rows_in(m.k, 16 * kb, 32 * j, lane), y, S[kb]);
             }
+        }
+    }
+    if (p.ds0) store_state(S, p.ds0 + head * size, p.DK, p.DV, dv, in, g4);
 }
-template <typename T, int KT> __global__ __launch_bounds__(512) void delta_bwd_state_kernel(DeltaBwd<T> p)
+template <typename T, int KT, int W> __global__ __launch_bounds__(64 * W) void delta_bwd_state_kernel(DeltaBwd<T> p)
 {
     extern __shared__ char lds[];
-    for (int unit = blockIdx.x, units = p.B * p.H; unit < units; unit += gridDim.x) delta_bwd_head(p, *reinterpret_cast<DeltaLds<T, KT> *>(lds), unit);
+    DeltaLds<T, KT> &m = *reinterpret_cast<DeltaLds<T, KT> *>(lds);
+    LowTiles<T, 64 * W>::zeros(m.t);
+    LowTiles<T, 64 * W>::zeros(m.p);
+    for (int unit = blockIdx.x, units = p.B * p.H; unit < units; unit += gridDim.x) delta_bwd_head<T, KT, W>(p, m, unit);
 }
+
+// ---- gradients within a chunk ----
 
 __device__ __forceinline__ f32x4 sum16(f32x4 x)
 {
@@ -479,16 +696,22 @@ __device__ __forceinline__ f32x4 sum16(f32x4 x)
 }
 
 constexpr int kDeltaBwdWaves(int KT) { return KT < 4 ? 4 : KT; }
-constexpr int kDeltaBwdColumns(int KT) { return KT > 4 ? 32 : 64; }     // columns of a state at a time (of DK = 128 LDS has room for 32)
 
-template <int KT> struct DeltaBwdLds {
-    static constexpr int VB = kDeltaBwdColumns(KT), kRows = VB + 4;
-    float k[16 * KT * kPitch], q[16 * KT * kPitch];
-    float a[64 * kPitch], p[64 * kPitch], t[64 * kPitch];
-    float dout[64 * kRows], dr[64 * kRows], w[64 * kRows];
-    float db[VB / 16][64], da[4][64];
+template <typename T, int KT> struct DeltaChunkLds {
+    typedef typename Mat<T>::Elem Elem;
+    static constexpr int NP = Mat<T>::planes, VB = sizeof(T) == 4 && KT > 4 ? 32 : 64;     // columns of a state at a time, as LDS has room
+    Elem k[16 * KT * kPitch], q[16 * KT * kPitch], t[NP * 64 * kPitch], p[NP * 64 * kPitch];
+    union {
+        struct {
+            Elem dout[VB * kPitch], w[NP * VB * kPitch], dr[NP * VB * kPitch];
+        };
+        struct {
+            float pairs[64 * kPitch];
+            Elem sym[(NP < 2 ? 1 : 2) * 64 * kPitch];
+        };
+    };
     Gates s;
-    float whole[8];
+    float part[3][8][64], db[VB / 16][64], da[4][64], whole[8];
 };
 
 // Backward, within a chunk, all chunks at once: from the states in front of it and the gradient of that behind it
@@ -498,10 +721,12 @@ template <int KT> struct DeltaBwdLds {
 //     dg_t = exp(G_63) <dS, S> + sum_{i >= t} x_i + sum_{j < t} y_j + sum_{i >= t > j} W_ij,
 // x_i what row i took of S and y_j what is left of column j in S'.  (As a difference of whole sums, which is shorter, it would be
 // the rounding of those where a decay is strong.)  A workgroup has a chunk of a head of keys and adds up the heads that share it, in order.
-template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(const DeltaBwd<T> &p, DeltaBwdLds<KT> &m, int unit)
+template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(const DeltaBwd<T> &p, DeltaChunkLds<T, KT> &m, int unit)
 {
-    typedef DeltaBwdLds<KT> Lds;
-    constexpr int W = kDeltaBwdWaves(KT), VB = Lds::VB, NS = VB / 16, R = Lds::kRows, NT = (10 + W - 1) / W;
+    typedef Mat<T> M;
+    typedef typename M::Full Full;
+    typedef DeltaChunkLds<T, KT> Lds;
+    constexpr int W = kDeltaBwdWaves(KT), VB = Lds::VB, NS = VB / 16, NT = (10 + W - 1) / W, PL = 64 * kPitch, VP = VB * kPitch;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g4 = 4 * (lane >> 4);
     const int ch = unit % p.chunks, bk = unit / p.chunks, Hk = p.H / p.each, b = bk / Hk, hk = bk % Hk;
     const int n = p.length(b), t0 = ch * kDeltaChunk, dk = 16 * wave + c;
@@ -513,57 +738,47 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
     };
     f32x4 dq[4] = {}, dkey[4] = {};
     if (t0 < n) {
-        stage(m.k, p.k.row(b, hk * p.DK, p.L), p.DK, 16 * KT, t0, n, p.L);
-        stage(m.q, p.q.row(b, hk * p.DK, p.L), p.DK, 16 * KT, t0, n, p.L);
+        {
+            Tile<T, 16 * KT, 64 * W> k, q;
+            k.load(p.k.row(b, hk * p.DK, p.L), p.DK, t0, n, p.L);
+            q.load(p.q.row(b, hk * p.DK, p.L), p.DK, t0, n, p.L);
+            k.put(m.k, p.DK, t0, n);
+            q.put(m.q, p.DK, t0, n);
+        }
         for (int h = hk * p.each; h < (hk + 1) * p.each; ++h) {
-            const long long head = (long long)b * p.H + h;
-            const float *before = p.states + (head * p.chunks + ch) * p.DK * p.DV, *after = p.after + (head * p.chunks + ch) * p.DK * p.DV;
-            __syncthreads();
-            squares<KT>(m.s, m.k, m.q);
-            __syncthreads();
-            gates(m.s, p, b, h, t0, n);
-            __syncthreads();
-            f32x4 kk[NT], pp[NT], dp[NT], da[NT];       // pairs of this wave's tiles, and their gradients
-#pragma unroll
-            for (int u = 0; u < NT; ++u) {
-                const int task = wave + u * W;
-                kk[u] = pp[u] = dp[u] = da[u] = f32x4{};
-                if (task >= 10) continue;
-                int ti, tj;
-                low_tile(task, ti, tj);
-                const int i = 16 * ti + c, j = 16 * tj + g4;
-                const f32x4 e = decays(m.s, ti, tj, lane, true) * four(m.s.rk, j);
-                pp[u] = pair_tile<KT>(m.q, m.k, ti, tj, lane) * e * m.s.rq[i];
-                kk[u] = pair_tile<KT>(m.k, m.k, ti, tj, lane) * e * m.s.rk[i];
-#pragma unroll
-                for (int v = 0; v < 4; ++v) kk[u][v] = j + v < i ? kk[u][v] : 0.0f;
-                *reinterpret_cast<f32x4 *>(m.p + i * kPitch + j) = pp[u];
-                *reinterpret_cast<f32x4 *>(m.a + i * kPitch + j) = kk[u] * m.s.beta[i];
+            const long long head = (long long)b * p.H + h, at = head * p.chunks + ch;
+            const float *before = p.states + at * p.DK * p.DV, *after = p.after + at * p.DK * p.DV;
+            const DeltaPairs &pairs = p.pairs[at];
+            {
+                LowTiles<T, 64 * W> t, q;
+                t.load(pairs.t);
+                q.load(pairs.p);
+                __syncthreads();
+                t.put(m.t);
+                q.put(m.p);
+                for (int i = threadIdx.x; i < (int)sizeof(Gates) / 16; i += 64 * W) reinterpret_cast<f32x4 *>(&m.s)[i] = reinterpret_cast<const f32x4 *>(&pairs.s)[i];
+                for (int i = threadIdx.x; i < NS * 64; i += 64 * W) m.db[0][i] = 0.0f;
             }
-            for (int x = threadIdx.x; x < NS * 64; x += 64 * W) m.db[0][x] = 0.0f;
             __syncthreads();
-            invert(m.a, m.t);
+            f32x4 dp[NT] = {}, da[NT] = {};             // of this wave's tiles, transposed: lane (c, g) has columns 16 tj + 4 g + v of row 16 ti + c
             f32x4 x1[4] = {}, x2[4] = {}, x3[4] = {};   // do S^T, dr S^T, w dS^T: rows of positions, 16 channels of the key
             float whole = 0.0f;
             for (int v0 = 0; v0 < p.DV; v0 += VB) {
                 // w, and dr: a wave 16 columns of either
                 for (int task = wave; task < 2 * NS; task += W) {
-                    const int sl = task >> 1, dv = v0 + 16 * sl + c;
+                    const int sl = task >> 1, dv = v0 + 16 * sl + c, row = (16 * sl + c) * kPitch + g4;
                     const bool in = dv < p.DV;
-                    const float *state = task & 1 ? after : before;
-                    f32x4 S[KT];
-#pragma unroll
-                    for (int kb = 0; kb < KT; ++kb)
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) {
-                            const int r = 16 * kb + g4 + v;
-                            S[kb][v] = in && r < p.DK ? state[(long long)r * p.DV + dv] : 0.0f;
-                        }
+                    f32x4 S[KT], val[4], x[4] = {}, y[4] = {};
+                    load_state(S, task & 1 ? after : before, p.DK, p.DV, dv, in, g4);
                     const T *vrow = p.v.row(b, h * p.DV + (in ? dv : 0), p.L);
-                    f32x4 val[4], x[4] = {}, y[4] = {};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) val[i] = in ? load4(vrow, t0 + 16 * i + g4, n) : f32x4{};
-                    times_state<KT>(x, m.k, S, lane);
+#pragma unroll
+                    for (int kb = 0; kb < KT; kb += 2) {
+                        const Full s = M::split(S[kb], S[kb + 1]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[i] = M::mma(M::columns_in(m.k, 16 * i, 16 * kb, lane), s, x[i]);
+                    }
                     if (task & 1) {
                         const T *drow = p.dout.row(b, h * p.DV + (in ? dv : 0), p.L);
                         f32x4 d[4];
@@ -571,24 +786,25 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
                         for (int i = 0; i < 4; ++i) {
                             d[i] = in ? load4(drow, t0 + 16 * i + g4, n) : f32x4{};
                             x[i] *= four(m.s.eC, 16 * i + g4) * four(m.s.rk, 16 * i + g4);
+                            M::template put<1>(m.dout, 0, row + 16 * i, d[i]);
                         }
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
+                        for (int kb = 0; kb < 2; ++kb) {
+                            const typename M::In z = M::exact(d[2 * kb], d[2 * kb + 1]);
 #pragma unroll
-                            for (int i = j; i < 4; ++i) x[j] = mma16(columns_of(m.p, 16 * j, 16 * i, kPitch, lane), d[i], x[j]);
+                            for (int j = 0; j < 2 * kb + 2; ++j) x[j] = M::mma(M::columns(m.p, PL, 16 * j, 32 * kb, lane), z, x[j]);
+                        }
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
+                        for (int kb = 0; kb < 2; ++kb) {
+                            const Full z = M::split(x[2 * kb], x[2 * kb + 1]);
 #pragma unroll
-                            for (int i = j; i < 4; ++i) y[j] = mma16(columns_of(m.t, 16 * j, 16 * i, kPitch, lane), x[i], y[j]);
+                            for (int j = 0; j < 2 * kb + 2; ++j) y[j] = M::mma(M::columns(m.t, PL, 16 * j, 32 * kb, lane), z, y[j]);
+                        }
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
+                            M::put(m.dr, VP, row + 16 * i, y[i]);
                             const f32x4 s = sum16(y[i] * val[i]);
-#pragma unroll
-                            for (int v = 0; v < 4; ++v) {
-                                m.dout[(16 * i + g4 + v) * R + 16 * sl + c] = d[i][v];
-                                m.dr[(16 * i + g4 + v) * R + 16 * sl + c] = y[i][v];
-                                if (c == 0) m.db[sl][16 * i + g4 + v] += s[v];
-                            }
+                            if (c == 0) *reinterpret_cast<f32x4 *>(&m.db[sl][16 * i + g4]) += s;
                         }
                     } else {
 #pragma unroll
@@ -597,13 +813,13 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
                             x[i] = four(m.s.beta, t) * (val[i] - four(m.s.eG, t) * four(m.s.rk, t) * x[i]);
                         }
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
+                        for (int kb = 0; kb < 2; ++kb) {
+                            const Full z = M::split(x[2 * kb], x[2 * kb + 1]);
 #pragma unroll
-                            for (int j = 0; j <= i; ++j) y[i] = mma16(rows_of(m.t, 16 * i, 16 * j, kPitch, lane), x[j], y[i]);
+                            for (int i = 2 * kb; i < 4; ++i) y[i] = M::mma(M::rows(m.t, PL, 16 * i, 32 * kb, lane), z, y[i]);
+                        }
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-#pragma unroll
-                            for (int v = 0; v < 4; ++v) m.w[(16 * i + g4 + v) * R + 16 * sl + c] = y[i][v];
+                        for (int i = 0; i < 4; ++i) M::put(m.w, VP, row + 16 * i, y[i]);
                     }
                 }
                 __syncthreads();
@@ -614,67 +830,79 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
                     int ti, tj;
                     low_tile(task, ti, tj);
 #pragma unroll
-                    for (int kb = 0; kb < NS; ++kb) {
-                        const f32x4 wj = rows_of(m.w, 16 * tj, 16 * kb, R, lane);
-                        dp[u] = mma16(wj, rows_of(m.dout, 16 * ti, 16 * kb, R, lane), dp[u]);
-                        da[u] = mma16(wj, rows_of(m.dr, 16 * ti, 16 * kb, R, lane), da[u]);
+                    for (int kb = 0; kb < VB; kb += 32) {
+                        const Full wj = M::columns(m.w, VP, 16 * tj, kb, lane);
+                        dp[u] = M::mma(wj, M::columns_in(m.dout, 16 * ti, kb, lane), dp[u]);
+                        da[u] = M::mma(wj, M::columns(m.dr, VP, 16 * ti, kb, lane), da[u]);
                     }
                 }
                 if (keys)
 #pragma unroll
-                    for (int kb = 0; kb < NS; ++kb) {
-                        const int at = v0 + 16 * kb + g4;
+                    for (int kb = 0; kb < VB; kb += 32) {
+                        const int col = v0 + kb + g4;
                         const long long row = (long long)dk * p.DV;
-                        const f32x4 s0 = key ? load4(before + row, at, p.DV) : f32x4{}, s1 = key ? load4(after + row, at, p.DV) : f32x4{};
+                        const f32x4 a = key ? load4(before + row, col, p.DV) : f32x4{}, a2 = key ? load4(before + row, col + 16, p.DV) : f32x4{};
+                        const f32x4 e = key ? load4(after + row, col, p.DV) : f32x4{}, e2 = key ? load4(after + row, col + 16, p.DV) : f32x4{};
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) whole = fmaf(s0[v], s1[v], whole);
+                        for (int v = 0; v < 4; ++v) whole = fmaf(a[v], e[v], whole), whole = fmaf(a2[v], e2[v], whole);
+                        const Full s0 = M::split(a, a2), s1 = M::split(e, e2);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            x1[i] = mma16(rows_of(m.dout, 16 * i, 16 * kb, R, lane), s0, x1[i]);
-                            x2[i] = mma16(rows_of(m.dr, 16 * i, 16 * kb, R, lane), s0, x2[i]);
-                            x3[i] = mma16(rows_of(m.w, 16 * i, 16 * kb, R, lane), s1, x3[i]);
+                            x1[i] = M::mma(M::columns_in(m.dout, 16 * i, kb, lane), s0, x1[i]);
+                            x2[i] = M::mma(M::columns(m.dr, VP, 16 * i, kb, lane), s0, x2[i]);
+                            x3[i] = M::mma(M::columns(m.w, VP, 16 * i, kb, lane), s1, x3[i]);
                         }
                     }
                 __syncthreads();
             }
-            // the pairs' gradients, in the place of the pairs
+            // the pairs' gradients, in the place of the pairs, as they are multiplied with k and q as stored
 #pragma unroll
             for (int u = 0; u < NT; ++u) {
                 const int task = wave + u * W;
                 if (task >= 10) continue;
                 int ti, tj;
                 low_tile(task, ti, tj);
-                const int i = 16 * ti + c, j = 16 * tj + g4;
-                const f32x4 e = decays(m.s, ti, tj, lane, true);
-                f32x4 dA = -da[u], dP = dp[u];
+                const int i = 16 * ti + c, j = 16 * tj + g4, rec = 16 * c + g4;
+                const f32x4 kk = four(pairs.kk[task], rec), pp = four(pairs.p[task], rec), rk = four(m.s.rk, j);
+                f32x4 dA = -da[u], dP = dp[u], e;
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
                     dA[v] = j + v < i ? dA[v] : 0.0f;
                     dP[v] = j + v <= i ? dP[v] : 0.0f;
+                    e[v] = j + v <= i ? exp2_of(m.s.G[i] - m.s.G[j + v]) : 0.0f;
                 }
-                const f32x4 x = dA * kk[u];
+                const f32x4 x = dA * kk;
                 float sum = (x[0] + x[1]) + (x[2] + x[3]);
                 sum += __shfl_xor(sum, 16, 64);
                 sum += __shfl_xor(sum, 32, 64);
                 if (lane < 16) m.da[tj][i] = sum;
-                *reinterpret_cast<f32x4 *>(m.p + i * kPitch + j) = dP * e;
-                *reinterpret_cast<f32x4 *>(m.a + i * kPitch + j) = dA * e * m.s.beta[i];
-                *reinterpret_cast<f32x4 *>(m.t + i * kPitch + j) = dP * pp[u] + x * m.s.beta[i];
+                M::template put<2>(m.p, PL, i * kPitch + j, dP * e * rk);
+                M::template put<2>(m.t, PL, i * kPitch + j, dP * e * m.s.rq[i]);
+                *reinterpret_cast<f32x4 *>(m.pairs + i * kPitch + j) = dP * pp + x * m.s.beta[i];
+                const f32x4 y = dA * e * m.s.beta[i];
+                // (of a tile on the diagonal the lower half is written here, and its mirror image by column)
+                if (ti != tj) M::template put<2>(m.sym, PL, i * kPitch + j, y * rk);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    if (ti == tj && j + v < i) M::put_one(m.sym, PL, i * kPitch + j + v, y[v] * rk[v]);
+                    if (ti != tj || j + v < i) M::put_one(m.sym, PL, (j + v) * kPitch + i, y[v] * m.s.rk[i]);
+                    if (ti == tj && j + v == i) M::put_one(m.sym, PL, i * kPitch + i, 0.0f);
+                }
             }
             if (keys) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int t = 16 * i + g4;
-                    const f32x4 kh = four(m.k, dk * kPitch + t) * four(m.s.rk, t), qh = four(m.q, dk * kPitch + t) * four(m.s.rq, t);
+                    const f32x4 kh = M::wide(m.k, dk * kPitch + t) * four(m.s.rk, t), qh = M::wide(m.q, dk * kPitch + t) * four(m.s.rq, t);
                     x1[i] *= four(m.s.eG, t);
                     x2[i] *= -four(m.s.eG, t);
                     x3[i] *= four(m.s.eC, t);
                     const f32x4 beta = four(m.s.beta, t);
-                    const f32x4 xs = sum16(qh * x1[i] + beta * (kh * x2[i])), ys = sum16(kh * x3[i]), bs = sum16(kh * x2[i]);
+                    const f32x4 bx = kh * x2[i], xs = sum16(qh * x1[i] + beta * bx), ys = sum16(kh * x3[i]), bs = sum16(bx);
                     if (c == 0) {
-                        *reinterpret_cast<f32x4 *>(&m.s.part[0][wave][t]) = xs;
-                        *reinterpret_cast<f32x4 *>(&m.s.part[1][wave][t]) = ys;
-                        *reinterpret_cast<f32x4 *>(&m.s.part[2][wave][t]) = bs;
+                        *reinterpret_cast<f32x4 *>(&m.part[0][wave][t]) = xs;
+                        *reinterpret_cast<f32x4 *>(&m.part[1][wave][t]) = ys;
+                        *reinterpret_cast<f32x4 *>(&m.part[2][wave][t]) = bs;
                     }
                     dq[i] += x1[i];
                     dkey[i] += beta * x2[i] + x3[i];
@@ -683,47 +911,45 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
                 if (lane == 0) m.whole[wave] = whole;
             }
             __syncthreads();
-            // (wave 0) sums over the rows from t on, for every column
-            if (wave == 0) {
+            // (the last wave) sums over the rows from t on, for every column
+            if (wave == W - 1) {
                 float sum = 0.0f;
 #pragma unroll 8
                 for (int i = 63; i >= 0; --i)
                     if (i >= (lane & 48)) {
-                        sum += m.t[i * kPitch + lane];
-                        m.t[i * kPitch + lane] = sum;
+                        sum += m.pairs[i * kPitch + lane];
+                        m.pairs[i * kPitch + lane] = sum;
                     }
             }
             if (keys) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int kb = 0; kb < 2; ++kb) {
+                    const typename M::In k = M::rows_in(m.k, 16 * wave, 32 * kb, lane), q = M::rows_in(m.q, 16 * wave, 32 * kb, lane);
 #pragma unroll
-                    for (int j = 0; j <= i; ++j) {
-                        const f32x4 kj = rows_of(m.k, 16 * wave, 16 * j, kPitch, lane), qi = rows_of(m.q, 16 * wave, 16 * i, kPitch, lane);
-                        dq[i] = mma16(rows_of(m.p, 16 * i, 16 * j, kPitch, lane) * four(m.s.rk, 16 * j + g4), kj, dq[i]);
-                        dkey[j] = mma16(columns_of(m.p, 16 * j, 16 * i, kPitch, lane) * four(m.s.rq, 16 * i + g4), qi, dkey[j]);
-                        const f32x4 ki = rows_of(m.k, 16 * wave, 16 * i, kPitch, lane);
-                        f32x4 down = columns_of(m.a, 16 * j, 16 * i, kPitch, lane);
-                        if (i == j) down += rows_of(m.a, 16 * i, 16 * j, kPitch, lane);
-                        else dkey[i] = mma16(rows_of(m.a, 16 * i, 16 * j, kPitch, lane) * four(m.s.rk, 16 * j + g4), kj, dkey[i]);
-                        dkey[j] = mma16(down * four(m.s.rk, 16 * i + g4), ki, dkey[j]);
+                    for (int i = 0; i < 4; ++i) {
+                        if (2 * kb <= i) dq[i] = M::template mma<2>(M::template rows<2>(m.p, PL, 16 * i, 32 * kb, lane), k, dq[i]);
+                        if (i < 2 * kb + 2) dkey[i] = M::template mma<2>(M::template columns<2>(m.t, PL, 16 * i, 32 * kb, lane), q, dkey[i]);
+                        dkey[i] = M::template mma<2>(M::template rows<2>(m.sym, PL, 16 * i, 32 * kb, lane), k, dkey[i]);
                     }
+                }
             }
             __syncthreads();
             if (wave == 0) {
                 const int t = lane;
-                float x = 0.0f, y = 0.0f, bsum = 0.0f, pairs = 0.0f, all = 0.0f;
-                for (int u = 0; u < KT; ++u) x += m.s.part[0][u][t], y += m.s.part[1][u][t], bsum += m.s.part[2][u][t], all += m.whole[u];
+                float x = 0.0f, y = 0.0f, bsum = 0.0f, below = 0.0f, all = 0.0f;
+                for (int u = 0; u < KT; ++u) x += m.part[0][u][t], y += m.part[1][u][t], bsum += m.part[2][u][t], all += m.whole[u];
                 for (int s = 0; s < NS; ++s) bsum += m.db[s][t];
                 for (int j = 0; j <= (t >> 4); ++j) bsum += m.da[j][t];
-                for (int j = 0; j < t; ++j) pairs += m.t[t * kPitch + j];
+#pragma unroll 16
+                for (int j = 0; j < 64; ++j) below += j < t ? m.pairs[t * kPitch + j] : 0.0f;
 #pragma unroll
                 for (int d = 1; d < 64; d *= 2) {
                     const float up = __shfl_down(x, d, 64), down = __shfl_up(y, d, 64);
                     if (t + d < 64) x += up;
                     if (t >= d) y += down;
                 }
-                const float below = __shfl_up(y, 1, 64);
-                const float sum = (m.s.eG[63] * all + x) + ((t > 0 ? below : 0.0f) + pairs);
+                const float left = __shfl_up(y, 1, 64);
+                const float sum = (m.s.eG[63] * all + x) + ((t > 0 ? left : 0.0f) + below);
                 if (t0 + t < p.L) {
                     // (the derivative of a decay that is 0 in 32 bits is that)
                     p.dg[head * p.L + t0 + t] = t0 + t < n && !(p.g.row(b, h, p.L)[t0 + t] < -104.0f) ? sum : 0.0f;
@@ -738,11 +964,11 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int t = 16 * i + g4;
-                    qh[i] = four(m.q, dk * kPitch + t) * four(m.s.iq, t), kh[i] = four(m.k, dk * kPitch + t) * four(m.s.rk, t);
+                    qh[i] = M::wide(m.q, dk * kPitch + t) * four(m.s.iq, t), kh[i] = M::wide(m.k, dk * kPitch + t) * four(m.s.rk, t);
                     const f32x4 a = sum16(qh[i] * dq[i]), d = sum16(kh[i] * dkey[i]);
                     if (c == 0) {
-                        *reinterpret_cast<f32x4 *>(&m.s.part[0][wave][t]) = a;
-                        *reinterpret_cast<f32x4 *>(&m.s.part[1][wave][t]) = d;
+                        *reinterpret_cast<f32x4 *>(&m.part[0][wave][t]) = a;
+                        *reinterpret_cast<f32x4 *>(&m.part[1][wave][t]) = d;
                     }
                 }
             __syncthreads();
@@ -751,7 +977,7 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
                 for (int i = 0; i < 4; ++i) {
                     const int t = 16 * i + g4;
                     f32x4 a = {}, d = {};
-                    for (int u = 0; u < KT; ++u) a += four(m.s.part[0][u], t), d += four(m.s.part[1][u], t);
+                    for (int u = 0; u < KT; ++u) a += four(m.part[0][u], t), d += four(m.part[1][u], t);
                     dq[i] -= qh[i] * a, dkey[i] -= kh[i] * d;
                 }
         }
@@ -775,8 +1001,13 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
 template <typename T, int KT> __global__ __launch_bounds__(64 * kDeltaBwdWaves(KT)) void delta_bwd_chunk_kernel(DeltaBwd<T> p)
 {
     extern __shared__ char lds[];
-    for (int unit = blockIdx.x, units = p.B * (p.H / p.each) * p.chunks; unit < units; unit += gridDim.x)
-        delta_bwd_chunk(p, *reinterpret_cast<DeltaBwdLds<KT> *>(lds), unit);
+    DeltaChunkLds<T, KT> &m = *reinterpret_cast<DeltaChunkLds<T, KT> *>(lds);
+    LowTiles<T, 64 * kDeltaBwdWaves(KT)>::zeros(m.t);
+    LowTiles<T, 64 * kDeltaBwdWaves(KT)>::zeros(m.p);
+    for (int unit = blockIdx.x, units = p.B * (p.H / p.each) * p.chunks; unit < units; unit += gridDim.x) {
+        delta_bwd_chunk(p, m, unit);
+        __syncthreads();
+    }
 }
 
 }  // namespace dwconv

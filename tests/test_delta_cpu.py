@@ -26,11 +26,11 @@ BAD_DIMS = [dict(B=0), dict(H=0), dict(Hk=0), dict(Hk=3), dict(DK=0), dict(DK=12
             dict(B=1 << 20, H=1 << 12), dict(H=(1 << 20) + 1, Hk=1), dict(H=1 << 20, Hk=1, DV=64), dict(B=1 << 15, H=1 << 10, Hk=1, L=1 << 13)]
 
 
-def fwd(lib, k=None, v=None, scale=1.0, eps=1e-6, dtype=0, **dims):
+def fwd(lib, k=None, v=None, ws=P, n=1 << 40, scale=1.0, eps=1e-6, dtype=0, **dims):
     a = dict(q=S(), k=S(), v=S(), g=S(), beta=S(), s0=None, lengths=None, o=S(), s_last=P, states=P)
     if k:
         a[k] = v
-    return lib.dwconv_delta_fwd(*a.values(), *{**DIMS, **dims}.values(), scale, eps, dtype, None)
+    return lib.dwconv_delta_fwd(*a.values(), ws, n, *{**DIMS, **dims}.values(), scale, eps, dtype, None)
 
 
 def test_forward_refusals(lib):
@@ -48,11 +48,13 @@ def test_forward_refusals(lib):
     for x in (float("nan"), float("inf")):
         assert fwd(lib, scale=x) == 9 and fwd(lib, eps=x) == 9
     assert fwd(lib, eps=-1e-6) == 9
+    need = lib.dwconv_delta_workspace_bytes(2, 4, 8, 16, 100, 0)
+    assert fwd(lib, ws=None) == 5 and fwd(lib, n=need - 1) == 5 and fwd(lib, ws=P + 8) == 5
 
 
 def test_backward_refusals(lib):
-    need = lib.dwconv_delta_workspace_bytes(2, 4, 8, 16, 100)
-    assert need == 2 * 4 * 2 * 8 * 16 * 4
+    need = lib.dwconv_delta_workspace_bytes(2, 4, 8, 16, 100, 1)
+    assert need == lib.dwconv_delta_workspace_bytes(2, 4, 8, 16, 100, 0) + 2 * 4 * 2 * 8 * 16 * 4
 
     def f(k=None, v=None, ws=P, n=1 << 40, scale=1.0, eps=1e-6, dtype=0, **dims):
         a = dict(do=S(), q=S(), k=S(), v=S(), g=S(), beta=S(), states=P, ds_last=None, lengths=None, dq=S(), dk=S(), dv=S(), dg=P, dbeta=P, ds0=P)
@@ -75,8 +77,9 @@ def test_backward_refusals(lib):
 def test_states_and_workspaces(lib):
     assert [lib.dwconv_delta_states(L) for L in (0, -1, 1, 64, 65, 1 << 30, (1 << 30) + 1)] == [0, 0, 1, 1, 2, 1 << 24, 0]
     for bad in ((0, 1, 1, 1, 1), (1, 0, 1, 1, 1), (1, 1, 0, 1, 1), (1, 1, 129, 1, 1), (1, 1, 1, 0, 1), (1, 1, 1, 1, 0)):
-        assert lib.dwconv_delta_workspace_bytes(*bad) == 0
-    assert lib.dwconv_delta_workspace_bytes(1, 1, 1, 1, 1) == 16
+        assert lib.dwconv_delta_workspace_bytes(*bad, 0) == 0 and lib.dwconv_delta_workspace_bytes(*bad, 1) == 0
+    a, b = (lib.dwconv_delta_workspace_bytes(1, 1, 1, 1, 1, x) for x in (0, 1))
+    assert a > 0 and a % 16 == 0 and b == a + 16 and lib.dwconv_delta_workspace_bytes(3, 5, 1, 1, 65, 0) == 30 * a
 
 
 def test_step_refusals(lib):

@@ -216,11 +216,11 @@ def test_bad_values_stay_in_their_head(which, bad):
 def test_repeats_and_streams(B, H, Hk, DK, DV, L):
     """The same bits on another stream, after other work, with a workspace of the caller's that holds anything."""
     q, k, v, g, beta, s0, do, ds = inputs(B, H, Hk, DK, DV, L, BF16)
-    run = lambda ws=None: (*(f := block.delta_fwd(q, k, v, g, beta, s0, key_heads=Hk)), *block.delta_bwd(do, q, k, v, g, beta, f[2], ds, key_heads=Hk, workspace=ws))  # noqa: E731
+    run = lambda ws=None: (*(f := block.delta_fwd(q, k, v, g, beta, s0, key_heads=Hk, workspace=ws)), *block.delta_bwd(do, q, k, v, g, beta, f[2], ds, key_heads=Hk, workspace=ws))  # noqa: E731
     first = run()
     torch.cuda.synchronize()
     side = torch.cuda.Stream()
-    ws = torch.full((block.delta_workspace_bytes(B, H, DK, DV, L) // 4,), float("nan"), device="cuda")
+    ws = torch.full((block.delta_workspace_bytes(B, H, DK, DV, L, True) // 4,), float("nan"), device="cuda")
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
         second = run(ws)
@@ -521,7 +521,7 @@ def test_refusals():
         lambda: block.delta_fwd(q, k, v, g, beta, lengths=torch.ones(2, device="cuda", dtype=torch.int64), key_heads=1), lambda: block.delta_step(*tok, s.double(), key_heads=1),
         lambda: block.dropout_fwd(v.half(), 0.1, rng), lambda: block.dropout_fwd(v, 0.1, rng.int()), lambda: block.dropout_fwd(v, 0.1, rng, res=v.bfloat16()),
     ), (
-        lambda: block.delta_fwd(q, k, v, g, beta, key_heads=1, eps=-1.0), lambda: block.delta_fwd(q, k, v, g, beta, key_heads=1, scale=float("nan")),
+        lambda: block.delta_fwd(q, k, v, g, beta, key_heads=1, eps=-1.0), lambda: block.delta_fwd(q, k, v, g, beta, key_heads=1, scale=float("nan")), lambda: block.delta_fwd(q, k, v, g, beta, key_heads=1, workspace=torch.empty(4, device="cuda")),
         lambda: block.delta_step(*tok, s[:1].contiguous(), key_heads=1), lambda: block.delta_bwd(do, q, k, v, g, beta, states, key_heads=1, workspace=torch.empty(4, device="cuda")),
         lambda: block.delta_fwd(*(torch.zeros(1, 129, 4, device="cuda") for _ in range(3)), g[:1, :1, :4], beta[:1, :1, :4]),
         lambda: block.dropout_fwd(v, 1.0, rng), lambda: block.dropout_fwd(v, -0.1, rng), lambda: block.dropout_fwd(v, 0.1, rng, layer=-1), lambda: block.dropout_fwd(v, 0.1, rng, layer=1 << 24),
