@@ -97,7 +97,7 @@ template <typename T, int RT> __global__ __launch_bounds__(256) void delta_step_
 namespace {
 
 constexpr int kMaxKey = 128;            // channels of a key: a state's columns are registers of a wave
-constexpr int kMaxUnits = 1 << 22;      // workgroups of a grid, whose lanes stay below 2^32
+constexpr int kMaxUnits = 1 << 22;      // workgroups of a launch, whose lanes stay below 2^32
 
 int chunks_of(int L) { return (int)ceil_div(L, kDeltaChunk); }
 
@@ -134,10 +134,10 @@ template <typename T, int KT> int launch_pairs(const DeltaShape<T> &p, hipStream
     static std::atomic<unsigned long long> done{0};
     const size_t lds = sizeof(PairsLds<T, KT>);
     if (!allow_lds(delta_pairs_kernel<T, KT>, lds, done)) return DWCONV_ERR_LAUNCH;
-    delta_pairs_kernel<T, KT><<<(unsigned)std::min(p.B * p.H * p.chunks, kMaxUnits), 256, lds, st>>>(p);
+    const int units = p.B * p.H * p.chunks;
+    for (int first = 0; first < units; first += kMaxUnits) delta_pairs_kernel<T, KT><<<std::min(units - first, kMaxUnits), 256, lds, st>>>(p, first);
     return DWCONV_OK;
 }
-dim3 walk_grid(int B, int H, int DV, int W) { return dim3((unsigned)std::min(B * H, kMaxUnits), (unsigned)ceil_div(DV, 16 * W)); }
 bool four_waves(int DV) { return DV <= 64; }
 
 template <typename T, int KT, int W> int launch_walk(const DeltaFwd<T> &p, hipStream_t st)
@@ -145,7 +145,9 @@ template <typename T, int KT, int W> int launch_walk(const DeltaFwd<T> &p, hipSt
     static std::atomic<unsigned long long> done{0};
     const size_t lds = sizeof(DeltaLds<T, KT>);
     if (!allow_lds(delta_fwd_kernel<T, KT, W>, lds, done)) return DWCONV_ERR_LAUNCH;
-    delta_fwd_kernel<T, KT, W><<<walk_grid(p.B, p.H, p.DV, W), 64 * W, lds, st>>>(p);
+    const int units = p.B * p.H, slices = (int)ceil_div(p.DV, 16 * W);
+    for (int first = 0; first < units; first += kMaxUnits)
+        delta_fwd_kernel<T, KT, W><<<dim3(std::min(units - first, kMaxUnits), slices), 64 * W, lds, st>>>(p, first);
     return launch_status();
 }
 template <typename T, int KT> int launch_fwd(const DeltaFwd<T> &p, hipStream_t st)
@@ -164,7 +166,9 @@ template <typename T, int KT, int W> int launch_walk(const DeltaBwd<T> &p, hipSt
     static std::atomic<unsigned long long> done{0};
     const size_t lds = sizeof(DeltaLds<T, KT>);
     if (!allow_lds(delta_bwd_state_kernel<T, KT, W>, lds, done)) return DWCONV_ERR_LAUNCH;
-    delta_bwd_state_kernel<T, KT, W><<<walk_grid(p.B, p.H, p.DV, W), 64 * W, lds, st>>>(p);
+    const int units = p.B * p.H, slices = (int)ceil_div(p.DV, 16 * W);
+    for (int first = 0; first < units; first += kMaxUnits)
+        delta_bwd_state_kernel<T, KT, W><<<dim3(std::min(units - first, kMaxUnits), slices), 64 * W, lds, st>>>(p, first);
     return DWCONV_OK;
 }
 template <typename T, int KT> int launch_bwd(const DeltaBwd<T> &p, hipStream_t st)
@@ -176,7 +180,9 @@ template <typename T, int KT> int launch_bwd(const DeltaBwd<T> &p, hipStream_t s
     int rc = launch_pairs<T, KT>(p, st);
     if (rc == DWCONV_OK) rc = four_waves(p.DV) ? launch_walk<T, KT, 4>(p, st) : launch_walk<T, KT, 8>(p, st);
     if (rc != DWCONV_OK) return rc;
-    delta_bwd_chunk_kernel<T, KT><<<(unsigned)std::min(p.B * (p.H / p.each) * p.chunks, kMaxUnits), 64 * kDeltaBwdWaves(KT), lds, st>>>(p);
+    const int units = p.B * (p.H / p.each) * p.chunks;
+    for (int first = 0; first < units; first += kMaxUnits)
+        delta_bwd_chunk_kernel<T, KT><<<std::min(units - first, kMaxUnits), 64 * kDeltaBwdWaves(KT), lds, st>>>(p, first);
     return launch_status();
 }
 template <typename T> int launch_bwd(const DeltaBwd<T> &p, hipStream_t st)

@@ -79,6 +79,16 @@ __device__ __forceinline__ f32x4 columns_of(const float *x, int m, int k, int la
     return f32x4{p[0], p[kPitch], p[2 * kPitch], p[3 * kPitch]};
 }
 
+// A lane's number that the compiler takes for a new one: what a loop's body derives from it (hundreds of addresses in LDS) is formed there
+// and not kept in registers, or in memory, from before the loop.
+__device__ __forceinline__ int fresh(int lane)
+{
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+// Keeps the compiler from reading far ahead of the products: it would take all operands of a loop into registers at once, and spill.
+__device__ __forceinline__ void step_done() { __builtin_amdgcn_sched_barrier(0); }
+
 // Products of 16 x 32 x 16.  An operand is 32 terms deep: lane (c, g) holds terms 4 g + v and 16 + 4 g + v of its row or column c, which is how
 // two tiles of a product lie (split()), so that a product is the next one's operand without leaving the registers.
 // In: of a matrix stored as T; Full: of one in 32 bits.  A Full matrix in LDS is `planes` matrices, `plane` elements apart.
@@ -193,38 +203,61 @@ template <> struct Mat<bf16_t> {
     }
 };
 
-// Four consecutive positions of a row, those from `n` on zero (and not read).
+// Four consecutive positions of a row.
+typedef unsigned uintx2_any __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ f32x4 load4(const float *p) { return *reinterpret_cast<const floatx4_any *>(p); }
+__device__ __forceinline__ f32x4 load4(const bf16_t *p)
+{
+    const uintx2_any u = *reinterpret_cast<const uintx2_any *>(p);
+    return f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xffff0000u), __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xffff0000u)};
+}
+__device__ __forceinline__ void store4(float *p, f32x4 v) { *reinterpret_cast<floatx4_any *>(p) = v; }
+__device__ __forceinline__ void store4(bf16_t *p, f32x4 v) { *reinterpret_cast<uintx2_any *>(p) = uintx2_any{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}; }
+// ... those from `n` on zero and not read, and not written.
 template <typename T> __device__ __forceinline__ f32x4 load4(const T *row, int t, int n)
 {
     f32x4 r = {};
-    if (t + 4 <= n) {
-        if constexpr (sizeof(T) == 4) {
-            r = *reinterpret_cast<const floatx4_any *>(row + t);
-        } else {
-            typedef unsigned uintx2_any __attribute__((ext_vector_type(2), aligned(2)));
-            const uintx2_any u = *reinterpret_cast<const uintx2_any *>(row + t);
-            r = f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xffff0000u), __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xffff0000u)};
-        }
-    } else {
+    if (t + 4 <= n) r = load4(row + t);
+    else
 #pragma unroll
         for (int k = 0; k < 3; ++k)
             if (t + k < n) r[k] = ld_elem(row + t + k);
-    }
     return r;
 }
 template <typename T> __device__ __forceinline__ void store4(T *row, f32x4 r, int t, int L)
 {
-    if (t + 4 <= L) {
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<floatx4_any *>(row + t) = r;
-        } else {
-            typedef unsigned uintx2_any __attribute__((ext_vector_type(2), aligned(2)));
-            *reinterpret_cast<uintx2_any *>(row + t) = uintx2_any{pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3])};
-        }
-    } else {
+    if (t + 4 <= L) store4(row + t, r);
+    else
 #pragma unroll
         for (int k = 0; k < 3; ++k)
             if (t + k < L) st_elem(row + t + k, r[k]);
+}
+
+// A lane's positions of a chunk, 16 i + g4 + v, of a row: zeros from position n on, and where the lane has no row (`row` is any then).  Whole chunks
+// are read without asking: a load behind a question waits for the one before.
+template <typename T> __device__ __forceinline__ void load_rows(f32x4 (&x)[4], const T *row, int t0, int g4, int n, bool in)
+{
+    if (t0 + 64 <= n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x4 v = load4(row + t0 + 16 * i + g4);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[i][k] = in ? v[k] : 0.0f;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = load4(row, t0 + 16 * i + g4, in ? n : 0);
+    }
+}
+template <typename T> __device__ __forceinline__ void store_rows(T *row, const f32x4 (&x)[4], int t0, int g4, int L, bool in)
+{
+    if (t0 + 64 <= L) {
+        if (in)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) store4(row + t0 + 16 * i + g4, x[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) store4(row, x[i], t0 + 16 * i + g4, in ? L : 0);
     }
 }
 
@@ -334,7 +367,7 @@ template <typename T, int KT> struct PairsLds {
 // after block column.  By four waves; T's blocks above the diagonal are not written.
 __device__ __forceinline__ void invert(const float *A, float *T)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (wave == 0) {
         const int b = lane >> 4, c = lane & 15;
         const float *a = A + 16 * b * kPitch + 16 * b;
@@ -381,7 +414,7 @@ __device__ __forceinline__ void invert(const float *A, float *T)
 template <typename T, int KT> __device__ __forceinline__ void delta_pairs(const DeltaShape<T> &p, PairsLds<T, KT> &m, int unit)
 {
     typedef Mat<T> M;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, g4 = 4 * (lane >> 4);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g4 = 4 * (lane >> 4);
     const int ch = unit % p.chunks, bh = unit / p.chunks, b = bh / p.H, h = bh % p.H, hk = h / p.each, n = p.length(b), t0 = ch * kDeltaChunk;
     if (t0 >= n) return;
     DeltaPairs &to = p.pairs[unit];
@@ -456,14 +489,11 @@ template <typename T, int KT> __device__ __forceinline__ void delta_pairs(const 
     }
     for (int i = tid; i < (int)sizeof(Gates) / 16; i += 256) reinterpret_cast<f32x4 *>(&to.s)[i] = reinterpret_cast<const f32x4 *>(&m.s)[i];
 }
-// (a grid has fewer than 2^32 lanes in a dimension: of very many chunks or heads several to a workgroup)
-template <typename T, int KT> __global__ __launch_bounds__(256) void delta_pairs_kernel(DeltaShape<T> p)
+// (a grid has fewer than 2^32 lanes in a dimension: of very many chunks or heads this launch has those from `first` on)
+template <typename T, int KT> __global__ __launch_bounds__(256) void delta_pairs_kernel(DeltaShape<T> p, int first)
 {
     extern __shared__ char lds[];
-    for (int unit = blockIdx.x, units = p.B * p.H * p.chunks; unit < units; unit += gridDim.x) {
-        delta_pairs(p, *reinterpret_cast<PairsLds<T, KT> *>(lds), unit);
-        __syncthreads();
-    }
+    delta_pairs(p, *reinterpret_cast<PairsLds<T, KT> *>(lds), first + (int)blockIdx.x);
 }
 
 // ---- from chunk to chunk ----
@@ -497,24 +527,48 @@ template <typename T, int KT, int W> struct Ahead {
     }
 };
 
-// A wave's 16 columns of a state.  (The row's part of an address is the wave's, so that no lane holds one for every row.)
-template <int KT> __device__ __forceinline__ void load_state(f32x4 (&S)[KT], const float *from, int DK, int DV, int dv, bool in, int g4)
+// A head's state in memory, [DK, DV]: what a lane asks for behind its end is zero, and not written.
+struct StateIn {
+    __amdgpu_buffer_rsrc_t r;
+    unsigned bytes, pitch;
+    __device__ __forceinline__ StateIn(const float *p, int DK, int DV)
+        : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(p), 0, DK * DV * 4, 0x00020000)), bytes(DK * DV * 4), pitch(DV * 4)
+    {
+    }
+    // Column dv of rows g4 + row: the lane's part of an address, and the wave's (held to the end, up to which the lane's is checked).
+    static constexpr unsigned kNone = 0x40000000u;
+    __device__ __forceinline__ unsigned lane(int g4, int dv, bool in) const { return in ? g4 * pitch + 4 * dv : kNone; }
+    __device__ __forceinline__ unsigned row(int i) const { return min(i * pitch, bytes); }
+    __device__ __forceinline__ float load(unsigned lane, unsigned row) const { return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, lane, row, 0)); }
+    __device__ __forceinline__ void store(float v, unsigned lane, unsigned row) const
+    {
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), r, lane, row, 0);
+    }
+    // Columns dv .. dv + 3 of a row, zeros from DV on.
+    __device__ __forceinline__ f32x4 four(int row, int dv, int DV) const
+    {
+        f32x4 x = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, row * pitch + 4 * dv, 0, 0));
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x[v] = dv + v < DV ? x[v] : 0.0f;
+        return x;
+    }
+};
+// A wave's 16 columns of a state.
+template <int KT> __device__ __forceinline__ void load_state(f32x4 (&S)[KT], const StateIn &from, int dv, bool in, int g4)
 {
-    const unsigned at = (unsigned)(g4 * DV + dv);
+    const unsigned at = from.lane(g4, dv, in);
 #pragma unroll
     for (int kb = 0; kb < KT; ++kb)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) S[kb][v] = in && 16 * kb + v + g4 < DK ? (from + (16 * kb + v) * DV)[at] : 0.0f;
+        for (int v = 0; v < 4; ++v) S[kb][v] = from.load(at, from.row(16 * kb + v));
 }
-template <int KT> __device__ __forceinline__ void store_state(const f32x4 (&S)[KT], float *to, int DK, int DV, int dv, bool in, int g4)
+template <int KT> __device__ __forceinline__ void store_state(const f32x4 (&S)[KT], const StateIn &to, int dv, bool in, int g4)
 {
-    if (!in) return;
-    const unsigned at = (unsigned)(g4 * DV + dv);
+    const unsigned at = to.lane(g4, dv, in);
 #pragma unroll
     for (int kb = 0; kb < KT; ++kb)
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-            if (16 * kb + v + g4 < DK) (to + (16 * kb + v) * DV)[at] = S[kb][v];
+        for (int v = 0; v < 4; ++v) to.store(S[kb][v], at, to.row(16 * kb + v));
 }
 
 // Forward.  A workgroup has a head's state, a wave 16 of its columns in registers; it walks the head's chunks.
@@ -522,13 +576,13 @@ template <typename T, int KT, int W> __device__ __forceinline__ void delta_fwd_h
 {
     typedef Mat<T> M;
     constexpr int PL = 64 * kPitch;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g4 = 4 * (lane >> 4);
+    const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane0 & 15, g4 = 4 * (lane0 >> 4);
     const int b = unit / p.H, h = unit % p.H, hk = h / p.each, n = p.length(b), last = (n + 63) / 64;
-    const int dv = (blockIdx.y * W + wave) * 16 + c;
-    const bool in = dv < p.DV, active = dv - c < p.DV;
+    const int dv0 = (blockIdx.y * W + wave) * 16, dv = dv0 + c;
+    const bool in = dv < p.DV, active = dv0 < p.DV;
     const long long head = (long long)b * p.H + h, size = (long long)p.DK * p.DV;
     f32x4 S[KT] = {};
-    if (p.s0) load_state(S, p.s0 + head * size, p.DK, p.DV, dv, in, g4);
+    if (p.s0) load_state(S, StateIn(p.s0 + head * size, p.DK, p.DV), dv, in, g4);
     const T *vrow = p.v.row(b, h * p.DV + (in ? dv : 0), p.L), *krow = p.k.row(b, hk * p.DK, p.L), *qrow = p.q.row(b, hk * p.DK, p.L);
     T *orow = p.o.row(b, h * p.DV + (in ? dv : 0), p.L);
     const DeltaPairs *pairs = p.pairs + head * p.chunks;
@@ -537,11 +591,11 @@ template <typename T, int KT, int W> __device__ __forceinline__ void delta_fwd_h
     if (last > 0) next.load(p, krow, qrow, pairs, 0, n);
     for (int ch = 0; ch < last; ++ch) {
         const int t0 = ch * kDeltaChunk;
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dv = dv0 + c;
         __syncthreads();
         next.put(m, p.DK, t0, n);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) val[i] = in ? load4(vrow, t0 + 16 * i + g4, n) : f32x4{};
-        if (p.states) store_state(S, p.states + (head * p.chunks + ch) * size, p.DK, p.DV, dv, in, g4);
+        load_rows(val, vrow, t0, g4, n, in);
+        if (p.states) store_state(S, StateIn(p.states + (head * p.chunks + ch) * size, p.DK, p.DV), dv, in, g4);
         __syncthreads();
         if (ch + 1 < last) next.load(p, krow, qrow, pairs + ch + 1, t0 + 64, n);
         if (!active) continue;
@@ -584,21 +638,19 @@ template <typename T, int KT, int W> __device__ __forceinline__ void delta_fwd_h
 #pragma unroll
             for (int kb = 0; kb < KT; ++kb) S[kb] = M::mma(M::rows_in(m.k, 16 * kb, 32 * j, lane), x, S[kb]);
         }
-        if (in)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) store4(orow, o[i], t0 + 16 * i + g4, p.L);        // (k and q behind n are zeros, so these are)
+        store_rows(orow, o, t0, g4, p.L, in);           // (k and q behind n are zeros, so these are)
     }
     if (in)
         for (int t = last * 64 + g4; t < p.L; t += 16) store4(orow, f32x4{}, t, p.L);
-    if (p.s_last) store_state(S, p.s_last + head * size, p.DK, p.DV, dv, in, g4);
+    if (p.s_last) store_state(S, StateIn(p.s_last + head * size, p.DK, p.DV), dv, in, g4);
 }
-template <typename T, int KT, int W> __global__ __launch_bounds__(64 * W) void delta_fwd_kernel(DeltaFwd<T> p)
+template <typename T, int KT, int W> __global__ __launch_bounds__(64 * W) void delta_fwd_kernel(DeltaFwd<T> p, int first)
 {
     extern __shared__ char lds[];
     DeltaLds<T, KT> &m = *reinterpret_cast<DeltaLds<T, KT> *>(lds);
     LowTiles<T, 64 * W>::zeros(m.t);
     LowTiles<T, 64 * W>::zeros(m.p);
-    for (int unit = blockIdx.x, units = p.B * p.H; unit < units; unit += gridDim.x) delta_fwd_head<T, KT, W>(p, m, unit);
+    delta_fwd_head<T, KT, W>(p, m, first + (int)blockIdx.x);
 }
 
 // Backward, from chunk to chunk: with dS the gradient of the state behind a chunk,
@@ -608,13 +660,13 @@ template <typename T, int KT, int W> __device__ __forceinline__ void delta_bwd_h
 {
     typedef Mat<T> M;
     constexpr int PL = 64 * kPitch;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g4 = 4 * (lane >> 4);
+    const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane0 & 15, g4 = 4 * (lane0 >> 4);
     const int b = unit / p.H, h = unit % p.H, hk = h / p.each, n = p.length(b), last = (n + 63) / 64;
-    const int dv = (blockIdx.y * W + wave) * 16 + c;
-    const bool in = dv < p.DV, active = dv - c < p.DV;
+    const int dv0 = (blockIdx.y * W + wave) * 16, dv = dv0 + c;
+    const bool in = dv < p.DV, active = dv0 < p.DV;
     const long long head = (long long)b * p.H + h, size = (long long)p.DK * p.DV;
     f32x4 S[KT] = {};
-    if (p.ds_last) load_state(S, p.ds_last + head * size, p.DK, p.DV, dv, in, g4);
+    if (p.ds_last) load_state(S, StateIn(p.ds_last + head * size, p.DK, p.DV), dv, in, g4);
     const T *drow = p.dout.row(b, h * p.DV + (in ? dv : 0), p.L), *krow = p.k.row(b, hk * p.DK, p.L), *qrow = p.q.row(b, hk * p.DK, p.L);
     T *vrow = p.dv.row(b, h * p.DV + (in ? dv : 0), p.L);
     const DeltaPairs *pairs = p.pairs + head * p.chunks;
@@ -625,11 +677,11 @@ template <typename T, int KT, int W> __device__ __forceinline__ void delta_bwd_h
     if (last > 0) next.load(p, krow, qrow, pairs + last - 1, (last - 1) * 64, n);
     for (int ch = last - 1; ch >= 0; --ch) {
         const int t0 = ch * kDeltaChunk;
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dv = dv0 + c;
         __syncthreads();
         next.put(m, p.DK, t0, n);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) d[i] = in ? load4(drow, t0 + 16 * i + g4, n) : f32x4{};
-        store_state(S, p.after + (head * p.chunks + ch) * size, p.DK, p.DV, dv, in, g4);
+        load_rows(d, drow, t0, g4, n, in);
+        store_state(S, StateIn(p.after + (head * p.chunks + ch) * size, p.DK, p.DV), dv, in, g4);
         __syncthreads();
         if (ch > 0) next.load(p, krow, qrow, pairs + ch - 1, t0 - 64, n);
         if (!active) continue;
@@ -659,10 +711,11 @@ template <typename T, int KT, int W> __device__ __forceinline__ void delta_bwd_h
         for (int i = 0; i < 4; ++i) {
             const int t = 16 * i + g4;
             r[i] *= four(m.s.beta, t);
-            if (in) store4(vrow, r[i], t0 + t, p.L);
+            w[i] = r[i];
             r[i] *= -four(m.s.eG, t) * four(m.s.rk, t);
             d[i] *= four(m.s.eG, t) * four(m.s.rq, t);
         }
+        store_rows(vrow, w, t0, g4, p.L, in);
 #pragma unroll
         for (int kb = 0; kb < KT; ++kb) S[kb] *= eA;
 #pragma unroll
@@ -675,15 +728,15 @@ template <typename T, int KT, int W> __device__ __forceinline__ void delta_bwd_h
             }
         }
     }
-    if (p.ds0) store_state(S, p.ds0 + head * size, p.DK, p.DV, dv, in, g4);
+    if (p.ds0) store_state(S, StateIn(p.ds0 + head * size, p.DK, p.DV), dv, in, g4);
 }
-template <typename T, int KT, int W> __global__ __launch_bounds__(64 * W) void delta_bwd_state_kernel(DeltaBwd<T> p)
+template <typename T, int KT, int W> __global__ __launch_bounds__(64 * W) void delta_bwd_state_kernel(DeltaBwd<T> p, int first)
 {
     extern __shared__ char lds[];
     DeltaLds<T, KT> &m = *reinterpret_cast<DeltaLds<T, KT> *>(lds);
     LowTiles<T, 64 * W>::zeros(m.t);
     LowTiles<T, 64 * W>::zeros(m.p);
-    for (int unit = blockIdx.x, units = p.B * p.H; unit < units; unit += gridDim.x) delta_bwd_head<T, KT, W>(p, m, unit);
+    delta_bwd_head<T, KT, W>(p, m, first + (int)blockIdx.x);
 }
 
 // ---- gradients within a chunk ----
@@ -700,18 +753,15 @@ constexpr int kDeltaBwdWaves(int KT) { return KT < 4 ? 4 : KT; }
 template <typename T, int KT> struct DeltaChunkLds {
     typedef typename Mat<T>::Elem Elem;
     static constexpr int NP = Mat<T>::planes, VB = sizeof(T) == 4 && KT > 4 ? 32 : 64;     // columns of a state at a time, as LDS has room
-    Elem k[16 * KT * kPitch], q[16 * KT * kPitch], t[NP * 64 * kPitch], p[NP * 64 * kPitch];
+    Elem k[16 * KT * kPitch], t[NP * 64 * kPitch], p[NP * 64 * kPitch];
     union {
         struct {
             Elem dout[VB * kPitch], w[NP * VB * kPitch], dr[NP * VB * kPitch];
         };
-        struct {
-            float pairs[64 * kPitch];
-            Elem sym[(NP < 2 ? 1 : 2) * 64 * kPitch];
-        };
+        float pairs[64 * kPitch];
     };
     Gates s;
-    float part[3][8][64], db[VB / 16][64], da[4][64], whole[8];
+    float part[3][8][64], db[VB / 16][64], da[4][64], dg[4][64], whole[8];
 };
 
 // Backward, within a chunk, all chunks at once: from the states in front of it and the gradient of that behind it
@@ -726,288 +776,337 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
     typedef Mat<T> M;
     typedef typename M::Full Full;
     typedef DeltaChunkLds<T, KT> Lds;
-    constexpr int W = kDeltaBwdWaves(KT), VB = Lds::VB, NS = VB / 16, NT = (10 + W - 1) / W, PL = 64 * kPitch, VP = VB * kPitch;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g4 = 4 * (lane >> 4);
+    constexpr int W = kDeltaBwdWaves(KT), VB = Lds::VB, NS = VB / 16, NT = (10 + W - 1) / W, NJ = (2 * NS + W - 1) / W, PL = 64 * kPitch, VP = VB * kPitch;
+    const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane0 & 15, g4 = 4 * (lane0 >> 4);
     const int ch = unit % p.chunks, bk = unit / p.chunks, Hk = p.H / p.each, b = bk / Hk, hk = bk % Hk;
     const int n = p.length(b), t0 = ch * kDeltaChunk, dk = 16 * wave + c;
     const bool keys = wave < KT, key = keys && dk < p.DK;
-    const auto inside = [&](f32x4 x, int t) {
-#pragma unroll
-        for (int v = 0; v < 4; ++v) x[v] = t0 + t + v < n ? x[v] : 0.0f;
-        return x;
-    };
-    f32x4 dq[4] = {}, dkey[4] = {};
-    if (t0 < n) {
-        {
-            Tile<T, 16 * KT, 64 * W> k, q;
-            k.load(p.k.row(b, hk * p.DK, p.L), p.DK, t0, n, p.L);
-            q.load(p.q.row(b, hk * p.DK, p.L), p.DK, t0, n, p.L);
-            k.put(m.k, p.DK, t0, n);
-            q.put(m.q, p.DK, t0, n);
-        }
-        for (int h = hk * p.each; h < (hk + 1) * p.each; ++h) {
-            const long long head = (long long)b * p.H + h, at = head * p.chunks + ch;
-            const float *before = p.states + at * p.DK * p.DV, *after = p.after + at * p.DK * p.DV;
-            const DeltaPairs &pairs = p.pairs[at];
-            {
-                LowTiles<T, 64 * W> t, q;
-                t.load(pairs.t);
-                q.load(pairs.p);
-                __syncthreads();
-                t.put(m.t);
-                q.put(m.p);
-                for (int i = threadIdx.x; i < (int)sizeof(Gates) / 16; i += 64 * W) reinterpret_cast<f32x4 *>(&m.s)[i] = reinterpret_cast<const f32x4 *>(&pairs.s)[i];
-                for (int i = threadIdx.x; i < NS * 64; i += 64 * W) m.db[0][i] = 0.0f;
-            }
-            __syncthreads();
-            f32x4 dp[NT] = {}, da[NT] = {};             // of this wave's tiles, transposed: lane (c, g) has columns 16 tj + 4 g + v of row 16 ti + c
-            f32x4 x1[4] = {}, x2[4] = {}, x3[4] = {};   // do S^T, dr S^T, w dS^T: rows of positions, 16 channels of the key
-            float whole = 0.0f;
-            for (int v0 = 0; v0 < p.DV; v0 += VB) {
-                // w, and dr: a wave 16 columns of either
-                for (int task = wave; task < 2 * NS; task += W) {
-                    const int sl = task >> 1, dv = v0 + 16 * sl + c, row = (16 * sl + c) * kPitch + g4;
-                    const bool in = dv < p.DV;
-                    f32x4 S[KT], val[4], x[4] = {}, y[4] = {};
-                    load_state(S, task & 1 ? after : before, p.DK, p.DV, dv, in, g4);
-                    const T *vrow = p.v.row(b, h * p.DV + (in ? dv : 0), p.L);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) val[i] = in ? load4(vrow, t0 + 16 * i + g4, n) : f32x4{};
-#pragma unroll
-                    for (int kb = 0; kb < KT; kb += 2) {
-                        const Full s = M::split(S[kb], S[kb + 1]);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) x[i] = M::mma(M::columns_in(m.k, 16 * i, 16 * kb, lane), s, x[i]);
-                    }
-                    if (task & 1) {
-                        const T *drow = p.dout.row(b, h * p.DV + (in ? dv : 0), p.L);
-                        f32x4 d[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            d[i] = in ? load4(drow, t0 + 16 * i + g4, n) : f32x4{};
-                            x[i] *= four(m.s.eC, 16 * i + g4) * four(m.s.rk, 16 * i + g4);
-                            M::template put<1>(m.dout, 0, row + 16 * i, d[i]);
-                        }
-#pragma unroll
-                        for (int kb = 0; kb < 2; ++kb) {
-                            const typename M::In z = M::exact(d[2 * kb], d[2 * kb + 1]);
-#pragma unroll
-                            for (int j = 0; j < 2 * kb + 2; ++j) x[j] = M::mma(M::columns(m.p, PL, 16 * j, 32 * kb, lane), z, x[j]);
-                        }
-#pragma unroll
-                        for (int kb = 0; kb < 2; ++kb) {
-                            const Full z = M::split(x[2 * kb], x[2 * kb + 1]);
-#pragma unroll
-                            for (int j = 0; j < 2 * kb + 2; ++j) y[j] = M::mma(M::columns(m.t, PL, 16 * j, 32 * kb, lane), z, y[j]);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            M::put(m.dr, VP, row + 16 * i, y[i]);
-                            const f32x4 s = sum16(y[i] * val[i]);
-                            if (c == 0) *reinterpret_cast<f32x4 *>(&m.db[sl][16 * i + g4]) += s;
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int t = 16 * i + g4;
-                            x[i] = four(m.s.beta, t) * (val[i] - four(m.s.eG, t) * four(m.s.rk, t) * x[i]);
-                        }
-#pragma unroll
-                        for (int kb = 0; kb < 2; ++kb) {
-                            const Full z = M::split(x[2 * kb], x[2 * kb + 1]);
-#pragma unroll
-                            for (int i = 2 * kb; i < 4; ++i) y[i] = M::mma(M::rows(m.t, PL, 16 * i, 32 * kb, lane), z, y[i]);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) M::put(m.w, VP, row + 16 * i, y[i]);
-                    }
-                }
-                __syncthreads();
-#pragma unroll
-                for (int u = 0; u < NT; ++u) {
-                    const int task = wave + u * W;
-                    if (task >= 10) continue;
-                    int ti, tj;
-                    low_tile(task, ti, tj);
-#pragma unroll
-                    for (int kb = 0; kb < VB; kb += 32) {
-                        const Full wj = M::columns(m.w, VP, 16 * tj, kb, lane);
-                        dp[u] = M::mma(wj, M::columns_in(m.dout, 16 * ti, kb, lane), dp[u]);
-                        da[u] = M::mma(wj, M::columns(m.dr, VP, 16 * ti, kb, lane), da[u]);
-                    }
-                }
-                if (keys)
-#pragma unroll
-                    for (int kb = 0; kb < VB; kb += 32) {
-                        const int col = v0 + kb + g4;
-                        const long long row = (long long)dk * p.DV;
-                        const f32x4 a = key ? load4(before + row, col, p.DV) : f32x4{}, a2 = key ? load4(before + row, col + 16, p.DV) : f32x4{};
-                        const f32x4 e = key ? load4(after + row, col, p.DV) : f32x4{}, e2 = key ? load4(after + row, col + 16, p.DV) : f32x4{};
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) whole = fmaf(a[v], e[v], whole), whole = fmaf(a2[v], e2[v], whole);
-                        const Full s0 = M::split(a, a2), s1 = M::split(e, e2);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            x1[i] = M::mma(M::columns_in(m.dout, 16 * i, kb, lane), s0, x1[i]);
-                            x2[i] = M::mma(M::columns(m.dr, VP, 16 * i, kb, lane), s0, x2[i]);
-                            x3[i] = M::mma(M::columns(m.w, VP, 16 * i, kb, lane), s1, x3[i]);
-                        }
-                    }
-                __syncthreads();
-            }
-            // the pairs' gradients, in the place of the pairs, as they are multiplied with k and q as stored
-#pragma unroll
-            for (int u = 0; u < NT; ++u) {
-                const int task = wave + u * W;
-                if (task >= 10) continue;
-                int ti, tj;
-                low_tile(task, ti, tj);
-                const int i = 16 * ti + c, j = 16 * tj + g4, rec = 16 * c + g4;
-                const f32x4 kk = four(pairs.kk[task], rec), pp = four(pairs.p[task], rec), rk = four(m.s.rk, j);
-                f32x4 dA = -da[u], dP = dp[u], e;
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    dA[v] = j + v < i ? dA[v] : 0.0f;
-                    dP[v] = j + v <= i ? dP[v] : 0.0f;
-                    e[v] = j + v <= i ? exp2_of(m.s.G[i] - m.s.G[j + v]) : 0.0f;
-                }
-                const f32x4 x = dA * kk;
-                float sum = (x[0] + x[1]) + (x[2] + x[3]);
-                sum += __shfl_xor(sum, 16, 64);
-                sum += __shfl_xor(sum, 32, 64);
-                if (lane < 16) m.da[tj][i] = sum;
-                M::template put<2>(m.p, PL, i * kPitch + j, dP * e * rk);
-                M::template put<2>(m.t, PL, i * kPitch + j, dP * e * m.s.rq[i]);
-                *reinterpret_cast<f32x4 *>(m.pairs + i * kPitch + j) = dP * pp + x * m.s.beta[i];
-                const f32x4 y = dA * e * m.s.beta[i];
-                // (of a tile on the diagonal the lower half is written here, and its mirror image by column)
-                if (ti != tj) M::template put<2>(m.sym, PL, i * kPitch + j, y * rk);
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    if (ti == tj && j + v < i) M::put_one(m.sym, PL, i * kPitch + j + v, y[v] * rk[v]);
-                    if (ti != tj || j + v < i) M::put_one(m.sym, PL, (j + v) * kPitch + i, y[v] * m.s.rk[i]);
-                    if (ti == tj && j + v == i) M::put_one(m.sym, PL, i * kPitch + i, 0.0f);
-                }
-            }
-            if (keys) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = 16 * i + g4;
-                    const f32x4 kh = M::wide(m.k, dk * kPitch + t) * four(m.s.rk, t), qh = M::wide(m.q, dk * kPitch + t) * four(m.s.rq, t);
-                    x1[i] *= four(m.s.eG, t);
-                    x2[i] *= -four(m.s.eG, t);
-                    x3[i] *= four(m.s.eC, t);
-                    const f32x4 beta = four(m.s.beta, t);
-                    const f32x4 bx = kh * x2[i], xs = sum16(qh * x1[i] + beta * bx), ys = sum16(kh * x3[i]), bs = sum16(bx);
-                    if (c == 0) {
-                        *reinterpret_cast<f32x4 *>(&m.part[0][wave][t]) = xs;
-                        *reinterpret_cast<f32x4 *>(&m.part[1][wave][t]) = ys;
-                        *reinterpret_cast<f32x4 *>(&m.part[2][wave][t]) = bs;
-                    }
-                    dq[i] += x1[i];
-                    dkey[i] += beta * x2[i] + x3[i];
-                }
-                whole = group_sum(whole, 6);
-                if (lane == 0) m.whole[wave] = whole;
-            }
-            __syncthreads();
-            // (the last wave) sums over the rows from t on, for every column
-            if (wave == W - 1) {
-                float sum = 0.0f;
-#pragma unroll 8
-                for (int i = 63; i >= 0; --i)
-                    if (i >= (lane & 48)) {
-                        sum += m.pairs[i * kPitch + lane];
-                        m.pairs[i * kPitch + lane] = sum;
-                    }
-            }
-            if (keys) {
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    const typename M::In k = M::rows_in(m.k, 16 * wave, 32 * kb, lane), q = M::rows_in(m.q, 16 * wave, 32 * kb, lane);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (2 * kb <= i) dq[i] = M::template mma<2>(M::template rows<2>(m.p, PL, 16 * i, 32 * kb, lane), k, dq[i]);
-                        if (i < 2 * kb + 2) dkey[i] = M::template mma<2>(M::template columns<2>(m.t, PL, 16 * i, 32 * kb, lane), q, dkey[i]);
-                        dkey[i] = M::template mma<2>(M::template rows<2>(m.sym, PL, 16 * i, 32 * kb, lane), k, dkey[i]);
-                    }
-                }
-            }
-            __syncthreads();
-            if (wave == 0) {
-                const int t = lane;
-                float x = 0.0f, y = 0.0f, bsum = 0.0f, below = 0.0f, all = 0.0f;
-                for (int u = 0; u < KT; ++u) x += m.part[0][u][t], y += m.part[1][u][t], bsum += m.part[2][u][t], all += m.whole[u];
-                for (int s = 0; s < NS; ++s) bsum += m.db[s][t];
-                for (int j = 0; j <= (t >> 4); ++j) bsum += m.da[j][t];
-#pragma unroll 16
-                for (int j = 0; j < 64; ++j) below += j < t ? m.pairs[t * kPitch + j] : 0.0f;
-#pragma unroll
-                for (int d = 1; d < 64; d *= 2) {
-                    const float up = __shfl_down(x, d, 64), down = __shfl_up(y, d, 64);
-                    if (t + d < 64) x += up;
-                    if (t >= d) y += down;
-                }
-                const float left = __shfl_up(y, 1, 64);
-                const float sum = (m.s.eG[63] * all + x) + ((t > 0 ? left : 0.0f) + below);
-                if (t0 + t < p.L) {
-                    // (the derivative of a decay that is 0 in 32 bits is that)
-                    p.dg[head * p.L + t0 + t] = t0 + t < n && !(p.g.row(b, h, p.L)[t0 + t] < -104.0f) ? sum : 0.0f;
-                    p.dbeta[head * p.L + t0 + t] = t0 + t < n ? bsum : 0.0f;
-                }
-            }
-        }
-        if (p.eps > 0.0f) {             // through x / |x|: what lies along x does not change it
-            f32x4 qh[4], kh[4];
-            __syncthreads();
-            if (keys)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = 16 * i + g4;
-                    qh[i] = M::wide(m.q, dk * kPitch + t) * four(m.s.iq, t), kh[i] = M::wide(m.k, dk * kPitch + t) * four(m.s.rk, t);
-                    const f32x4 a = sum16(qh[i] * dq[i]), d = sum16(kh[i] * dkey[i]);
-                    if (c == 0) {
-                        *reinterpret_cast<f32x4 *>(&m.part[0][wave][t]) = a;
-                        *reinterpret_cast<f32x4 *>(&m.part[1][wave][t]) = d;
-                    }
-                }
-            __syncthreads();
-            if (keys)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = 16 * i + g4;
-                    f32x4 a = {}, d = {};
-                    for (int u = 0; u < KT; ++u) a += four(m.part[0][u], t), d += four(m.part[1][u], t);
-                    dq[i] -= qh[i] * a, dkey[i] -= kh[i] * d;
-                }
-        }
-        if (keys)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) dq[i] *= four(m.s.rq, 16 * i + g4), dkey[i] *= four(m.s.rk, 16 * i + g4);
-    } else {
+    if (t0 >= n) {
         for (int h = hk * p.each; h < (hk + 1) * p.each; ++h) {
             const long long at = ((long long)b * p.H + h) * p.L + t0 + threadIdx.x;
             if (threadIdx.x < 64 && t0 + threadIdx.x < p.L) p.dg[at] = p.dbeta[at] = 0.0f;
         }
+        if (key)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                store4(p.dq.row(b, hk * p.DK + dk, p.L), f32x4{}, t0 + 16 * i + g4, p.L);
+                store4(p.dk.row(b, hk * p.DK + dk, p.L), f32x4{}, t0 + 16 * i + g4, p.L);
+            }
+        return;
     }
-    if (key)
+    f32x4 dq[4] = {}, dkey[4] = {};
+    Tile<T, 16 * KT, 64 * W> kt;
+    kt.load(p.k.row(b, hk * p.DK, p.L), p.DK, t0, n, p.L);
+    f32x4 q[4];                             // this wave's channels of q, as products and sums over positions take them
+    load_rows(q, p.q.row(b, hk * p.DK + (key ? dk : 0), p.L), t0, g4, n, key);
+    for (int h = hk * p.each; h < (hk + 1) * p.each; ++h) {
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dk = 16 * wave + c;
+        const long long head = (long long)b * p.H + h, at = head * p.chunks + ch;
+        const StateIn before(p.states + at * p.DK * p.DV, p.DK, p.DV), after(p.after + at * p.DK * p.DV, p.DK, p.DV);
+        const DeltaPairs &pairs = p.pairs[at];
+        // w, and dr: a wave 16 columns of either.  What that takes from memory, a step ahead.
+        f32x4 S[KT], val[4], d[4];
+        const auto fetch = [&](int v0, int task) __attribute__((always_inline)) {
+            const int dv = v0 + 16 * (task >> 1) + c;
+            const bool in = dv < p.DV && task < 2 * NS;
+            if (task & 1) load_state(S, after, dv, in, g4);
+            else load_state(S, before, dv, in, g4);
+            load_rows(val, p.v.row(b, h * p.DV + (in ? dv : 0), p.L), t0, g4, n, in);
+            if (task & 1) load_rows(d, p.dout.row(b, h * p.DV + (in ? dv : 0), p.L), t0, g4, n, in);
+        };
+        {
+            LowTiles<T, 64 * W> t, u;
+            t.load(pairs.t);
+            u.load(pairs.p);
+            const f32x4 gates = reinterpret_cast<const f32x4 *>(&pairs.s)[threadIdx.x < sizeof(Gates) / 16 ? threadIdx.x : 0];
+            fetch(0, wave);
+            __syncthreads();
+            if (h == hk * p.each) kt.put(m.k, p.DK, t0, n);
+            t.put(m.t);
+            u.put(m.p);
+            if (threadIdx.x < sizeof(Gates) / 16) reinterpret_cast<f32x4 *>(&m.s)[threadIdx.x] = gates;
+            for (int i = threadIdx.x; i < NS * 64; i += 64 * W) m.db[0][i] = 0.0f;
+        }
+        __syncthreads();
+        f32x4 dp[NT] = {}, da[NT] = {};             // of this wave's tiles, transposed: lane (c, g) has columns 16 tj + 4 g + v of row 16 ti + c
+        f32x4 x1[4] = {}, x2[4] = {}, x3[4] = {};   // do S^T, dr S^T, w dS^T: rows of positions, 16 channels of the key
+        f32x4 kk[NT], pp[NT];
+        float whole = 0.0f;
+        for (int v0 = 0; v0 < p.DV; v0 += VB) {
+            const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dk = 16 * wave + c;
+#pragma unroll
+            for (int job = 0; job < NJ; ++job) {
+                const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
+                const int task = wave + job * W, sl = task >> 1, row = (16 * sl + c) * kPitch + g4;
+                if (task >= 2 * NS) break;
+                f32x4 x[4] = {}, y[4] = {};
+#pragma unroll
+                for (int kb = 0; kb < KT; kb += 2) {
+                    const Full s = M::split(S[kb], S[kb + 1]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = M::mma(M::columns_in(m.k, 16 * i, 16 * kb, lane), s, x[i]);
+                    step_done();
+                }
+                if (task & 1) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        x[i] *= four(m.s.eC, 16 * i + g4) * four(m.s.rk, 16 * i + g4);
+                        M::template put<1>(m.dout, 0, row + 16 * i, d[i]);
+                    }
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb) {
+                        const typename M::In z = M::exact(d[2 * kb], d[2 * kb + 1]);
+#pragma unroll
+                        for (int j = 0; j < 2 * kb + 2; ++j) x[j] = M::mma(M::columns(m.p, PL, 16 * j, 32 * kb, lane), z, x[j]);
+                        step_done();
+                    }
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb) {
+                        const Full z = M::split(x[2 * kb], x[2 * kb + 1]);
+#pragma unroll
+                        for (int j = 0; j < 2 * kb + 2; ++j) y[j] = M::mma(M::columns(m.t, PL, 16 * j, 32 * kb, lane), z, y[j]);
+                        step_done();
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        M::put(m.dr, VP, row + 16 * i, y[i]);
+                        const f32x4 s = sum16(y[i] * val[i]);
+                        if (c == 0) *reinterpret_cast<f32x4 *>(&m.db[sl][16 * i + g4]) += s;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int t = 16 * i + g4;
+                        x[i] = four(m.s.beta, t) * (val[i] - four(m.s.eG, t) * four(m.s.rk, t) * x[i]);
+                    }
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb) {
+                        const Full z = M::split(x[2 * kb], x[2 * kb + 1]);
+#pragma unroll
+                        for (int i = 2 * kb; i < 4; ++i) y[i] = M::mma(M::rows(m.t, PL, 16 * i, 32 * kb, lane), z, y[i]);
+                        step_done();
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) M::put(m.w, VP, row + 16 * i, y[i]);
+                }
+                if (job + 1 < NJ) fetch(v0, task + W);
+            }
+            if (v0 + VB < p.DV) {
+                fetch(v0 + VB, wave);
+            } else {
+#pragma unroll
+                for (int u = 0; u < NT; ++u) {
+                    const int task = min(wave + u * W, 9);
+                    kk[u] = four(pairs.kk[task], 16 * c + g4), pp[u] = four(pairs.p[task], 16 * c + g4);
+                }
+            }
+            f32x4 a[VB / 16], e[VB / 16];
+            if (keys)
+#pragma unroll
+                for (int kb = 0; kb < VB / 16; ++kb) {
+                    const int col = v0 + 16 * kb + g4;
+                    a[kb] = before.four(dk, col, p.DV), e[kb] = after.four(dk, col, p.DV);
+                }
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < NT; ++u) {
+                const int task = wave + u * W;
+                if (task >= 10) continue;
+                const int lane = fresh(lane0);
+                int ti, tj;
+                low_tile(task, ti, tj);
+#pragma unroll
+                for (int kb = 0; kb < VB; kb += 32) {
+                    const Full wj = M::columns(m.w, VP, 16 * tj, kb, lane);
+                    dp[u] = M::mma(wj, M::columns_in(m.dout, 16 * ti, kb, lane), dp[u]);
+                    da[u] = M::mma(wj, M::columns(m.dr, VP, 16 * ti, kb, lane), da[u]);
+                    step_done();
+                }
+            }
+            if (keys)
+#pragma unroll
+                for (int kb = 0; kb < VB / 16; kb += 2) {
+                    const int lane = fresh(lane0);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) whole = fmaf(a[kb][v], e[kb][v], whole), whole = fmaf(a[kb + 1][v], e[kb + 1][v], whole);
+                    const Full s0 = M::split(a[kb], a[kb + 1]), s1 = M::split(e[kb], e[kb + 1]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        x1[i] = M::mma(M::columns_in(m.dout, 16 * i, 16 * kb, lane), s0, x1[i]);
+                        x2[i] = M::mma(M::columns(m.dr, VP, 16 * i, 16 * kb, lane), s0, x2[i]);
+                        x3[i] = M::mma(M::columns(m.w, VP, 16 * i, 16 * kb, lane), s1, x3[i]);
+                        step_done();
+                    }
+                }
+            __syncthreads();
+        }
+        // the pairs' gradients, in the place of the pairs
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            const int task = wave + u * W;
+            if (task >= 10) continue;
+            const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
+            int ti, tj;
+            low_tile(task, ti, tj);
+            const int i = 16 * ti + c, j = 16 * tj + g4;
+            f32x4 dA = -da[u], dP = dp[u], e;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                dA[v] = j + v < i ? dA[v] : 0.0f;
+                dP[v] = j + v <= i ? dP[v] : 0.0f;
+                e[v] = j + v <= i ? exp2_of(m.s.G[i] - m.s.G[j + v]) : 0.0f;
+            }
+            const f32x4 x = dA * kk[u];
+            float sum = (x[0] + x[1]) + (x[2] + x[3]);
+            sum += __shfl_xor(sum, 16, 64);
+            sum += __shfl_xor(sum, 32, 64);
+            if (lane < 16) m.da[tj][i] = sum;
+            M::template put<2>(m.p, PL, i * kPitch + j, dP * e);
+            M::template put<2>(m.t, PL, i * kPitch + j, dA * e * m.s.beta[i]);
+            *reinterpret_cast<f32x4 *>(m.pairs + i * kPitch + j) = dP * pp[u] + x * m.s.beta[i];
+        }
+        f32x4 kh[4], qh[4];
+        if (keys) {
+            const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
+            const int dk = 16 * wave + c;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = 16 * i + g4;
+                const f32x4 beta = four(m.s.beta, t);
+                kh[i] = M::wide(m.k, dk * kPitch + t) * four(m.s.rk, t), qh[i] = q[i] * four(m.s.rq, t);
+                x1[i] *= four(m.s.eG, t);
+                x2[i] *= -four(m.s.eG, t);
+                x3[i] *= four(m.s.eC, t);
+                const f32x4 bx = kh[i] * x2[i], xs = sum16(qh[i] * x1[i] + beta * bx), ys = sum16(kh[i] * x3[i]), bs = sum16(bx);
+                if (c == 0) {
+                    *reinterpret_cast<f32x4 *>(&m.part[0][wave][t]) = xs;
+                    *reinterpret_cast<f32x4 *>(&m.part[1][wave][t]) = ys;
+                    *reinterpret_cast<f32x4 *>(&m.part[2][wave][t]) = bs;
+                }
+                dq[i] += x1[i];
+                dkey[i] += beta * x2[i] + x3[i];
+            }
+            whole = group_sum(whole, 6);
+            if (lane == 0) m.whole[wave] = whole;
+        }
+        __syncthreads();
+        // pairs of a row from t on and a column before t: products with ones above the diagonal, then the rows from t on, a tile a wave
+        for (int task = W - 1 - wave; task < 10; task += W) {
+            const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
+            int ti, tt;
+            low_tile(task, ti, tt);
+            f32x4 x = {};
+            for (int j = 0; j <= tt; ++j) {
+                f32x4 ones;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) ones[v] = 16 * j + g4 + v < 16 * tt + c ? 1.0f : 0.0f;
+                x = mma16(rows_of(m.pairs, 16 * ti, 16 * j, lane), ones, x);
+            }
+            float sum = 0.0f;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) sum += 16 * ti + g4 + v >= 16 * tt + c ? x[v] : 0.0f;
+            sum += __shfl_xor(sum, 16, 64);
+            sum += __shfl_xor(sum, 32, 64);
+            if (lane < 16) m.dg[ti][16 * tt + c] = sum;
+        }
+        if (keys) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                const int lane = fresh(lane0);
+                const Full kz = M::template split<2>(kh[2 * kb], kh[2 * kb + 1]), qz = M::template split<2>(qh[2 * kb], qh[2 * kb + 1]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (2 * kb <= i) {
+                        dq[i] = M::template mma<2>(M::template rows<2>(m.p, PL, 16 * i, 32 * kb, lane), kz, dq[i]);
+                        dkey[i] = M::template mma<2>(M::template rows<2>(m.t, PL, 16 * i, 32 * kb, lane), kz, dkey[i]);
+                    }
+                    if (i < 2 * kb + 2) {
+                        dkey[i] = M::template mma<2>(M::template columns<2>(m.p, PL, 16 * i, 32 * kb, lane), qz, dkey[i]);
+                        dkey[i] = M::template mma<2>(M::template columns<2>(m.t, PL, 16 * i, 32 * kb, lane), kz, dkey[i]);
+                    }
+                    step_done();
+                }
+            }
+        }
+        __syncthreads();
+        if (wave == W - 1) {
+            const int t = fresh(lane0);
+            float x = 0.0f, y = 0.0f, bsum = 0.0f, below = 0.0f, all = 0.0f;
+#pragma unroll
+            for (int u = 0; u < KT; ++u) x += m.part[0][u][t], y += m.part[1][u][t], bsum += m.part[2][u][t], all += m.whole[u];
+#pragma unroll
+            for (int s = 0; s < NS; ++s) bsum += m.db[s][t];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float u = m.da[j][t], w = m.dg[j][t];
+                bsum += j <= (t >> 4) ? u : 0.0f;
+                below += j >= (t >> 4) ? w : 0.0f;
+            }
+            // (the derivative of a decay that is 0 in 32 bits is that)
+            const double G = m.s.G[t], G1 = __shfl_up(G, 1, 64);
+            const bool dead = G - (t ? G1 : 0.0) < -104.0 * 1.4426950408889634;
+#pragma unroll
+            for (int s = 1; s < 64; s *= 2) {
+                const float up = __shfl_down(x, s, 64), down = __shfl_up(y, s, 64);
+                if (t + s < 64) x += up;
+                if (t >= s) y += down;
+            }
+            const float left = __shfl_up(y, 1, 64);
+            const float sum = (m.s.eG[63] * all + x) + ((t > 0 ? left : 0.0f) + below);
+            if (t0 + t < p.L) {
+                p.dg[head * p.L + t0 + t] = t0 + t < n && !dead ? sum : 0.0f;
+                p.dbeta[head * p.L + t0 + t] = t0 + t < n ? bsum : 0.0f;
+            }
+        }
+    }
+    if (p.eps > 0.0f) {             // through x / |x|: what lies along x does not change it
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
+        const int dk = 16 * wave + c;
+        f32x4 kh[4], qh[4];
+        __syncthreads();
+        if (keys)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = 16 * i + g4;
+                qh[i] = q[i] * four(m.s.iq, t), kh[i] = M::wide(m.k, dk * kPitch + t) * four(m.s.rk, t);
+                const f32x4 a = sum16(qh[i] * dq[i]), e = sum16(kh[i] * dkey[i]);
+                if (c == 0) {
+                    *reinterpret_cast<f32x4 *>(&m.part[0][wave][t]) = a;
+                    *reinterpret_cast<f32x4 *>(&m.part[1][wave][t]) = e;
+                }
+            }
+        __syncthreads();
+        if (keys)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = 16 * i + g4;
+                f32x4 a = {}, e = {};
+#pragma unroll
+                for (int u = 0; u < KT; ++u) a += four(m.part[0][u], t), e += four(m.part[1][u], t);
+                dq[i] -= qh[i] * a, dkey[i] -= kh[i] * e;
+            }
+    }
+    if (keys) {
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
+        const int dk = 16 * wave + c;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = 16 * i + g4;
-            store4(p.dq.row(b, hk * p.DK + dk, p.L), inside(dq[i], t), t0 + t, p.L);
-            store4(p.dk.row(b, hk * p.DK + dk, p.L), inside(dkey[i], t), t0 + t, p.L);
+            dq[i] *= four(m.s.rq, t), dkey[i] *= four(m.s.rk, t);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) dq[i][v] = t0 + t + v < n ? dq[i][v] : 0.0f, dkey[i][v] = t0 + t + v < n ? dkey[i][v] : 0.0f;
         }
+        store_rows(p.dq.row(b, hk * p.DK + (key ? dk : 0), p.L), dq, t0, g4, p.L, key);
+        store_rows(p.dk.row(b, hk * p.DK + (key ? dk : 0), p.L), dkey, t0, g4, p.L, key);
+    }
 }
-template <typename T, int KT> __global__ __launch_bounds__(64 * kDeltaBwdWaves(KT)) void delta_bwd_chunk_kernel(DeltaBwd<T> p)
+template <typename T, int KT> __global__ __launch_bounds__(64 * kDeltaBwdWaves(KT)) void delta_bwd_chunk_kernel(DeltaBwd<T> p, int first)
 {
     extern __shared__ char lds[];
     DeltaChunkLds<T, KT> &m = *reinterpret_cast<DeltaChunkLds<T, KT> *>(lds);
     LowTiles<T, 64 * kDeltaBwdWaves(KT)>::zeros(m.t);
     LowTiles<T, 64 * kDeltaBwdWaves(KT)>::zeros(m.p);
-    for (int unit = blockIdx.x, units = p.B * (p.H / p.each) * p.chunks; unit < units; unit += gridDim.x) {
-        delta_bwd_chunk(p, m, unit);
-        __syncthreads();
-    }
+    delta_bwd_chunk(p, m, first + (int)blockIdx.x);
 }
 
 }  // namespace dwconv
