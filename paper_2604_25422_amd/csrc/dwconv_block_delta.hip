@@ -138,56 +138,74 @@ template <typename T, int KT> int launch_pairs(const DeltaShape<T> &p, hipStream
     for (int first = 0; first < units; first += kMaxUnits) delta_pairs_kernel<T, KT><<<std::min(units - first, kMaxUnits), 256, lds, st>>>(p, first);
     return DWCONV_OK;
 }
-bool four_waves(int DV) { return DV <= 64; }
 
-template <typename T, int KT, int W> int launch_walk(const DeltaFwd<T> &p, hipStream_t st)
+// Segments that rows of chunks are cut into.
+struct WalkPlan {
+    int segs, per;
+};
+WalkPlan plan_walk(int B, int H, int DK, int DV, int L)
 {
-    static std::atomic<unsigned long long> done{0};
-    const size_t lds = sizeof(DeltaLds<T, KT>);
-    if (!allow_lds(delta_fwd_kernel<T, KT, W>, lds, done)) return DWCONV_ERR_LAUNCH;
-    const int units = p.B * p.H, slices = (int)ceil_div(p.DV, 16 * W);
-    for (int first = 0; first < units; first += kMaxUnits)
-        delta_fwd_kernel<T, KT, W><<<dim3(std::min(units - first, kMaxUnits), slices), 64 * W, lds, st>>>(p, first);
-    return launch_status();
+    const int chunks = chunks_of(L);
+    const long long groups = (long long)B * H * ceil_div(DV, 16 * kWalkWaves);
+    const int segs = (int)std::min<long long>(512 / std::max(1ll, groups), chunks / 4);
+    if (segs < 4) return WalkPlan{1, chunks};
+    const int per = (int)ceil_div(chunks, segs);
+    return WalkPlan{(int)ceil_div(chunks, per), per};
 }
-template <typename T, int KT> int launch_fwd(const DeltaFwd<T> &p, hipStream_t st)
-{
-    const int rc = launch_pairs<T, KT>(p, st);
-    if (rc != DWCONV_OK) return rc;
-    return four_waves(p.DV) ? launch_walk<T, KT, 4>(p, st) : launch_walk<T, KT, 8>(p, st);
-}
-template <typename T> int launch_fwd(const DeltaFwd<T> &p, hipStream_t st)
-{
-    return p.DK <= 32 ? launch_fwd<T, 2>(p, st) : p.DK <= 64 ? launch_fwd<T, 4>(p, st) : launch_fwd<T, 8>(p, st);
-}
+size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
+size_t starts_bytes(const WalkPlan &w, int B, int H, int DK, int DV) { return w.segs > 1 ? up16((size_t)B * H * w.segs * DK * DV * sizeof(float)) : 0; }
+size_t spans_bytes(const WalkPlan &w, int B, int H, int DK, int DV) { return w.segs > 1 ? up16((size_t)B * H * w.segs * DK * (DV + DK) * sizeof(float)) : 0; }
 
-template <typename T, int KT, int W> int launch_walk(const DeltaBwd<T> &p, hipStream_t st)
+template <typename Kernel, typename P> int launch_segments(Kernel kernel, const P &p, const DeltaWalk &w, int columns, size_t lds, std::atomic<unsigned long long> &done, hipStream_t st)
 {
-    static std::atomic<unsigned long long> done{0};
-    const size_t lds = sizeof(DeltaLds<T, KT>);
-    if (!allow_lds(delta_bwd_state_kernel<T, KT, W>, lds, done)) return DWCONV_ERR_LAUNCH;
-    const int units = p.B * p.H, slices = (int)ceil_div(p.DV, 16 * W);
+    if (!allow_lds(kernel, lds, done)) return DWCONV_ERR_LAUNCH;
+    const int units = p.B * p.H * w.segs, groups = (int)ceil_div(columns, 16 * kWalkWaves);
     for (int first = 0; first < units; first += kMaxUnits)
-        delta_bwd_state_kernel<T, KT, W><<<dim3(std::min(units - first, kMaxUnits), slices), 64 * W, lds, st>>>(p, first);
+        kernel<<<dim3(std::min(units - first, kMaxUnits), groups), 64 * kWalkWaves, lds, st>>>(p, w, first);
     return DWCONV_OK;
 }
-template <typename T, int KT> int launch_bwd(const DeltaBwd<T> &p, hipStream_t st)
+// Columns of a pass that forms spans, up to whole slices of 16.
+int span_columns(int DK, int DV) { return 16 * (int)(ceil_div(DV, 16) + ceil_div(DK, 16)); }
+
+template <typename T, int KT> int launch_fwd(const DeltaFwd<T> &p, const DeltaWalk &w, hipStream_t st)
 {
-    static std::atomic<unsigned long long> done{0};
-    const size_t lds = sizeof(DeltaChunkLds<T, KT>);
-    static_assert(sizeof(DeltaChunkLds<T, KT>) <= 160 * 1024, "LDS of a CU");
-    if (!allow_lds(delta_bwd_chunk_kernel<T, KT>, lds, done)) return DWCONV_ERR_LAUNCH;
+    static std::atomic<unsigned long long> done[2];
+    constexpr size_t lds = sizeof(DeltaLds<T, KT, 2>);
+    static_assert(lds <= 160 * 1024, "LDS of a CU");
     int rc = launch_pairs<T, KT>(p, st);
-    if (rc == DWCONV_OK) rc = four_waves(p.DV) ? launch_walk<T, KT, 4>(p, st) : launch_walk<T, KT, 8>(p, st);
+    if (rc == DWCONV_OK && w.segs > 1) {
+        rc = launch_segments(delta_fwd_kernel<T, KT, true>, p, w, span_columns(p.DK, p.DV), lds, done[1], st);
+        delta_starts_kernel<KT, false><<<dim3(p.B * p.H, (unsigned)ceil_div(p.DV, 16)), 64 * KT, 0, st>>>(p.s0, w.spans, const_cast<float *>(w.starts), w.segs, p.DK, p.DV);
+    }
+    if (rc == DWCONV_OK) rc = launch_segments(delta_fwd_kernel<T, KT, false>, p, w, p.DV, lds, done[0], st);
+    return rc == DWCONV_OK ? launch_status() : rc;
+}
+template <typename T> int launch_fwd(const DeltaFwd<T> &p, const DeltaWalk &w, hipStream_t st)
+{
+    return p.DK <= 32 ? launch_fwd<T, 2>(p, w, st) : p.DK <= 64 ? launch_fwd<T, 4>(p, w, st) : launch_fwd<T, 8>(p, w, st);
+}
+
+template <typename T, int KT> int launch_bwd(const DeltaBwd<T> &p, const DeltaWalk &w, hipStream_t st)
+{
+    static std::atomic<unsigned long long> done[3];
+    constexpr size_t lds = sizeof(DeltaLds<T, KT, 3>), chunk = sizeof(DeltaChunkLds<T, KT>);
+    static_assert(lds <= 160 * 1024 && chunk <= 160 * 1024, "LDS of a CU");
+    int rc = launch_pairs<T, KT>(p, st);
+    if (rc == DWCONV_OK && w.segs > 1) {
+        rc = launch_segments(delta_bwd_state_kernel<T, KT, true>, p, w, span_columns(p.DK, p.DV), lds, done[1], st);
+        delta_starts_kernel<KT, true><<<dim3(p.B * p.H, (unsigned)ceil_div(p.DV, 16)), 64 * KT, 0, st>>>(p.ds_last, w.spans, const_cast<float *>(w.starts), w.segs, p.DK, p.DV);
+    }
+    if (rc == DWCONV_OK) rc = launch_segments(delta_bwd_state_kernel<T, KT, false>, p, w, p.DV, lds, done[0], st);
+    if (rc == DWCONV_OK && !allow_lds(delta_bwd_chunk_kernel<T, KT>, chunk, done[2])) rc = DWCONV_ERR_LAUNCH;
     if (rc != DWCONV_OK) return rc;
     const int units = p.B * (p.H / p.each) * p.chunks;
     for (int first = 0; first < units; first += kMaxUnits)
-        delta_bwd_chunk_kernel<T, KT><<<std::min(units - first, kMaxUnits), 64 * kDeltaBwdWaves(KT), lds, st>>>(p, first);
+        delta_bwd_chunk_kernel<T, KT><<<std::min(units - first, kMaxUnits), 64 * kDeltaBwdWaves(KT), chunk, st>>>(p, first);
     return launch_status();
 }
-template <typename T> int launch_bwd(const DeltaBwd<T> &p, hipStream_t st)
+template <typename T> int launch_bwd(const DeltaBwd<T> &p, const DeltaWalk &w, hipStream_t st)
 {
-    return p.DK <= 32 ? launch_bwd<T, 2>(p, st) : p.DK <= 64 ? launch_bwd<T, 4>(p, st) : launch_bwd<T, 8>(p, st);
+    return p.DK <= 32 ? launch_bwd<T, 2>(p, w, st) : p.DK <= 64 ? launch_bwd<T, 4>(p, w, st) : launch_bwd<T, 8>(p, w, st);
 }
 
 template <typename T> void launch_step(const DeltaStep<T> &in, hipStream_t st)
@@ -213,7 +231,20 @@ template <typename T> DeltaShape<T> shape(dwconv_seq q, dwconv_seq k, dwconv_seq
     return DeltaShape<T>{seq<T>(q), seq<T>(k), seq<T>(v), seq<float>(g), seq<float>(beta), lengths, B, H, H / Hk, DK, DV, L, chunks_of(L), scale, eps,
                          static_cast<DeltaPairs *>(workspace)};
 }
+// A workspace: records of pairs, starts and spans of segments, backward the states' gradients behind the chunks.
 size_t pairs_bytes(int B, int H, int L) { return (size_t)B * H * chunks_of(L) * sizeof(DeltaPairs); }
+size_t walk_bytes(int B, int H, int DK, int DV, int L)
+{
+    const WalkPlan w = plan_walk(B, H, DK, DV, L);
+    return starts_bytes(w, B, H, DK, DV) + spans_bytes(w, B, H, DK, DV);
+}
+size_t after_bytes(int B, int H, int DK, int DV, int L) { return up16((size_t)B * H * chunks_of(L) * DK * DV * sizeof(float)); }
+DeltaWalk walk_in(void *workspace, int B, int H, int DK, int DV, int L)
+{
+    const WalkPlan w = plan_walk(B, H, DK, DV, L);
+    char *at = static_cast<char *>(workspace) + pairs_bytes(B, H, L);
+    return DeltaWalk{w.segs, w.per, reinterpret_cast<float *>(at), reinterpret_cast<float *>(at + starts_bytes(w, B, H, DK, DV))};
+}
 
 }  // namespace
 
@@ -224,7 +255,7 @@ int dwconv_delta_states(int L) { return L < 1 || L > (1 << 30) ? 0 : chunks_of(L
 size_t dwconv_delta_workspace_bytes(int B, int H, int DK, int DV, int L, int backward)
 {
     if (check_heads(B, H, H, DK, DV, L) != DWCONV_OK) return 0;
-    return pairs_bytes(B, H, L) + (backward ? ((size_t)B * H * chunks_of(L) * DK * DV * sizeof(float) + 15) & ~(size_t)15 : 0);
+    return pairs_bytes(B, H, L) + walk_bytes(B, H, DK, DV, L) + (backward ? after_bytes(B, H, DK, DV, L) : 0);
 }
 
 int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const float *s0, const int *lengths, dwconv_seq_out o,
@@ -244,14 +275,15 @@ int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwc
     if ((rc = check_out(o, es, B, H * DV, L)) != DWCONV_OK) return rc;
     for (const void *t : {(const void *)s0, (const void *)lengths, (const void *)s_last, (const void *)states})
         if (!f32_ok(t)) return DWCONV_ERR_ALIGN;
-    if (!workspace || workspace_bytes < pairs_bytes(B, H, L) || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < dwconv_delta_workspace_bytes(B, H, DK, DV, L, 0) || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
+    const DeltaWalk walk = walk_in(workspace, B, H, DK, DV, L);
     if (dtype == DWCONV_F32) {
         DeltaFwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<float>(o), s0, s_last, states};
-        return launch_fwd(p, st);
+        return launch_fwd(p, walk, st);
     }
     DeltaFwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<bf16_t>(o), s0, s_last, states};
-    return launch_fwd(p, st);
+    return launch_fwd(p, walk, st);
 }
 
 int dwconv_delta_bwd(dwconv_seq dout, dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const float *states, const float *ds_last,
@@ -277,15 +309,16 @@ int dwconv_delta_bwd(dwconv_seq dout, dwconv_seq q, dwconv_seq k, dwconv_seq v, 
     const size_t need = dwconv_delta_workspace_bytes(B, H, DK, DV, L, 1);
     if (!workspace || workspace_bytes < need || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    float *after = reinterpret_cast<float *>(static_cast<char *>(workspace) + pairs_bytes(B, H, L));
+    const DeltaWalk walk = walk_in(workspace, B, H, DK, DV, L);
+    float *after = reinterpret_cast<float *>(static_cast<char *>(workspace) + pairs_bytes(B, H, L) + walk_bytes(B, H, DK, DV, L));
     if (dtype == DWCONV_F32) {
         DeltaBwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<float>(dout), seq<float>(dq), seq<float>(dk),
                           seq<float>(dv), states, ds_last, after, dg, dbeta, ds0};
-        return launch_bwd(p, st);
+        return launch_bwd(p, walk, st);
     }
     DeltaBwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<bf16_t>(dout), seq<bf16_t>(dq), seq<bf16_t>(dk),
                        seq<bf16_t>(dv), states, ds_last, after, dg, dbeta, ds0};
-    return launch_bwd(p, st);
+    return launch_bwd(p, walk, st);
 }
 
 int dwconv_delta_step(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, float *s, const int *slots, int pool, dwconv_seq_out o, int B,

@@ -26,6 +26,10 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kDeltaChunk = 64;         // positions of a chunk
 constexpr int kPitch = 68;              // elements of a row of 64 in LDS: rows of either element size start in different banks
+// A lower triangle of 64 x 64 in LDS: 32 columns of its upper rows, all of the lower ones.
+constexpr int kLowPitch = 36, kLow = 32 * kLowPitch + 32 * kPitch;
+__device__ __forceinline__ constexpr int low_at(int r, int c) { return r < 32 ? r * kLowPitch + c : 32 * kLowPitch + (r - 32) * kPitch + c; }
+__device__ __forceinline__ constexpr int low_pitch(int r) { return r < 32 ? kLowPitch : kPitch; }
 
 // What the kernels take.  Heads: H of values, H / each of keys and queries.  States are [B, H, chunks, DK, DV].
 template <typename T> struct DeltaShape {
@@ -72,11 +76,14 @@ __device__ __forceinline__ f32x4 mma16(f32x4 a, f32x4 b, f32x4 d)
     return d;
 }
 // A's operand of rows m.. and columns k.. of a matrix in LDS: as it lies, or transposed.
-__device__ __forceinline__ f32x4 rows_of(const float *x, int m, int k, int lane) { return four(x, (m + (lane & 15)) * kPitch + k + 4 * (lane >> 4)); }
-__device__ __forceinline__ f32x4 columns_of(const float *x, int m, int k, int lane)
+__device__ __forceinline__ f32x4 rows_of(const float *x, int m, int k, int lane, int pitch = kPitch)
 {
-    const float *p = x + (k + 4 * (lane >> 4)) * kPitch + m + (lane & 15);
-    return f32x4{p[0], p[kPitch], p[2 * kPitch], p[3 * kPitch]};
+    return four(x, (m + (lane & 15)) * pitch + k + 4 * (lane >> 4));
+}
+__device__ __forceinline__ f32x4 columns_of(const float *x, int m, int k, int lane, int pitch = kPitch)
+{
+    const float *p = x + (k + 4 * (lane >> 4)) * pitch + m + (lane & 15);
+    return f32x4{p[0], p[pitch], p[2 * pitch], p[3 * pitch]};
 }
 
 // A lane's number that the compiler takes for a new one: what a loop's body derives from it (hundreds of addresses in LDS) is formed there
@@ -102,8 +109,18 @@ template <> struct Mat<float> {
     typedef Full In;
     static __device__ __forceinline__ In rows_in(const float *x, int m, int k, int lane) { return In{rows_of(x, m, k, lane), rows_of(x, m, k + 16, lane)}; }
     static __device__ __forceinline__ In columns_in(const float *x, int m, int k, int lane) { return In{columns_of(x, m, k, lane), columns_of(x, m, k + 16, lane)}; }
-    template <int N = 1> static __device__ __forceinline__ Full rows(const float *x, int, int m, int k, int lane) { return rows_in(x, m, k, lane); }
     template <int N = 1> static __device__ __forceinline__ Full columns(const float *x, int, int m, int k, int lane) { return columns_in(x, m, k, lane); }
+    // Of a lower triangle: rows m.., columns 32 kb..; and of it transposed.
+    template <int N = 1> static __device__ __forceinline__ Full low_rows(const float *x, int m, int kb, int lane)
+    {
+        const float *p = x + low_at(m, 32 * kb);
+        return Full{rows_of(p, 0, 0, lane, low_pitch(m)), rows_of(p, 0, 16, lane, low_pitch(m))};
+    }
+    template <int N = 1> static __device__ __forceinline__ Full low_columns(const float *x, int m, int kb, int lane)
+    {
+        const float *p = x + low_at(32 * kb, m);
+        return Full{columns_of(p, 0, 0, lane, low_pitch(32 * kb)), columns_of(p, 0, 16, lane, low_pitch(32 * kb))};
+    }
     template <int N = 1> static __device__ __forceinline__ Full split(f32x4 a, f32x4 b) { return Full{a, b}; }
     static __device__ __forceinline__ In exact(f32x4 a, f32x4 b) { return In{a, b}; }
     static __device__ __forceinline__ f32x4 wide(const float *x, int at) { return four(x, at); }
@@ -121,9 +138,9 @@ template <> struct Mat<bf16_t> {
         bf16x8 l[3];
     };
     static __device__ __forceinline__ bf16x8 pair(u32x2 a, u32x2 b) { return __builtin_bit_cast(bf16x8, (u32x4{a[0], a[1], b[0], b[1]})); }
-    static __device__ __forceinline__ bf16x8 row(const short *x, int m, int k, int lane)
+    static __device__ __forceinline__ bf16x8 row(const short *x, int m, int k, int lane, int pitch = kPitch)
     {
-        const short *p = x + (m + (lane & 15)) * kPitch + k + 4 * (lane >> 4);
+        const short *p = x + (m + (lane & 15)) * pitch + k + 4 * (lane >> 4);
         return pair(*reinterpret_cast<const u32x2 *>(p), *reinterpret_cast<const u32x2 *>(p + 16));
     }
     // Sixteen lanes read four rows of sixteen elements, and get four elements of a column each.
@@ -131,18 +148,25 @@ template <> struct Mat<bf16_t> {
     {
         return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)const_cast<short *>(p)));
     }
-    static __device__ __forceinline__ bf16x8 column(const short *x, int m, int k, int lane)
+    static __device__ __forceinline__ bf16x8 column(const short *x, int m, int k, int lane, int pitch = kPitch)
     {
-        const short *p = x + (k + (lane >> 4) * 4 + ((lane & 15) >> 2)) * kPitch + m + 4 * (lane & 3);
-        return pair(turned(p), turned(p + 16 * kPitch));
+        const short *p = x + (k + (lane >> 4) * 4 + ((lane & 15) >> 2)) * pitch + m + 4 * (lane & 3);
+        return pair(turned(p), turned(p + 16 * pitch));
     }
     static __device__ __forceinline__ In rows_in(const short *x, int m, int k, int lane) { return In{{row(x, m, k, lane)}}; }
     static __device__ __forceinline__ In columns_in(const short *x, int m, int k, int lane) { return In{{column(x, m, k, lane)}}; }
-    template <int N = 3> static __device__ __forceinline__ Full rows(const short *x, int plane, int m, int k, int lane)
+    template <int N = 3> static __device__ __forceinline__ Full low_rows(const short *x, int m, int kb, int lane)
     {
         Full f{};
 #pragma unroll
-        for (int n = 0; n < N; ++n) f.l[n] = row(x + n * plane, m, k, lane);
+        for (int n = 0; n < N; ++n) f.l[n] = row(x + n * kLow + low_at(m, 32 * kb), 0, 0, lane, low_pitch(m));
+        return f;
+    }
+    template <int N = 3> static __device__ __forceinline__ Full low_columns(const short *x, int m, int kb, int lane)
+    {
+        Full f{};
+#pragma unroll
+        for (int n = 0; n < N; ++n) f.l[n] = column(x + n * kLow + low_at(32 * kb, m), 0, 0, lane, low_pitch(32 * kb));
         return f;
     }
     template <int N = 3> static __device__ __forceinline__ Full columns(const short *x, int plane, int m, int k, int lane)
@@ -323,14 +347,14 @@ __device__ __forceinline__ void low_tile(int i, int &ti, int &tj)     // tile i 
     ti = i >= 6 ? 3 : i >= 3 ? 2 : i >= 1 ? 1 : 0;
     tj = i - ti * (ti + 1) / 2;
 }
-// The lower triangle of a chunk's matrix on its way from a record into LDS as a Full matrix.
-template <typename T, int LANES> struct LowTiles {
-    static constexpr int N = (640 + LANES - 1) / LANES;
-    f32x4 x[N];
+// The lower triangle of a chunk's matrix on its way from a record into LDS as a Full matrix of N limbs.
+template <typename T, int N, int LANES> struct LowTiles {
+    static constexpr int U = (640 + LANES - 1) / LANES;
+    f32x4 x[U];
     __device__ __forceinline__ void load(const float (&from)[10][256])
     {
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
+        for (int u = 0; u < U; ++u) {
             const int i = threadIdx.x + u * LANES;
             x[u] = four(from[0], 4 * (640 % LANES ? min(i, 639) : i));
         }
@@ -338,27 +362,32 @@ template <typename T, int LANES> struct LowTiles {
     __device__ __forceinline__ void put(typename Mat<T>::Elem *to) const
     {
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
+        for (int u = 0; u < U; ++u) {
             const int i = threadIdx.x + u * LANES;
             if (640 % LANES && i >= 640) continue;
             int ti, tj;
             low_tile(i >> 6, ti, tj);
-            Mat<T>::put(to, 64 * kPitch, (16 * ti + ((i & 63) >> 2)) * kPitch + 16 * tj + 4 * (i & 3), x[u]);
+            Mat<T>::template put<N>(to, kLow, low_at(16 * ti + ((i & 63) >> 2), 16 * tj + 4 * (i & 3)), x[u]);
         }
     }
     // What a product 32 deep takes beside the triangle: blocks (0, 1) and (2, 3), zeros, written once.
     static __device__ __forceinline__ void zeros(typename Mat<T>::Elem *to)
     {
         for (int i = threadIdx.x; i < 2 * 64; i += LANES)
-            Mat<T>::put(to, 64 * kPitch, ((i >> 6) * 32 + ((i & 63) >> 2)) * kPitch + (i >> 6) * 32 + 16 + 4 * (i & 3), f32x4{});
+            Mat<T>::template put<N>(to, kLow, low_at((i >> 6) * 32 + ((i & 63) >> 2), (i >> 6) * 32 + 16 + 4 * (i & 3)), f32x4{});
     }
 };
 
 // ---- what does not depend on the state ----
 
 template <typename T, int KT> struct PairsLds {
-    typename Mat<T>::Elem k[16 * KT * kPitch], q[16 * KT * kPitch];
-    float a[64 * kPitch], t[64 * kPitch];
+    union {
+        struct {
+            typename Mat<T>::Elem k[16 * KT * kPitch], q[16 * KT * kPitch];
+        };
+        float t[kLow];          // (k and q are done with by then)
+    };
+    float a[kLow];
     Gates s;
     float part[2][4][64];
 };
@@ -370,14 +399,15 @@ __device__ __forceinline__ void invert(const float *A, float *T)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (wave == 0) {
         const int b = lane >> 4, c = lane & 15;
-        const float *a = A + 16 * b * kPitch + 16 * b;
+        const float *a = A + low_at(16 * b, 16 * b);
+        const int pitch = low_pitch(16 * b);
         float x[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             float sum = i == c ? 1.0f : 0.0f;
 #pragma unroll
             for (int j = 0; j < i; j += 4) {
-                const f32x4 r = four(a + i * kPitch, j);
+                const f32x4 r = four(a + i * pitch, j);
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
                     if (j + v < i) sum = fmaf(-r[v], x[j + v], sum);
@@ -385,7 +415,7 @@ __device__ __forceinline__ void invert(const float *A, float *T)
             x[i] = sum;
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) T[(16 * b + i) * kPitch + 16 * b + c] = x[i];
+        for (int i = 0; i < 16; ++i) T[low_at(16 * b, 16 * b) + i * pitch + c] = x[i];
     }
     __syncthreads();
     if (const int j = wave; j < 3) {
@@ -395,15 +425,15 @@ __device__ __forceinline__ void invert(const float *A, float *T)
             col[m] = f32x4{};
             if (m < j) continue;
             if (m == j) {
-                col[m] = columns_of(T, 16 * j, 16 * j, lane);       // (as B: rows 4 g + v, column c)
+                col[m] = columns_of(T + low_at(16 * j, 16 * j), 0, 0, lane, low_pitch(16 * j));       // (as B: rows 4 g + v, column c)
             } else {
                 f32x4 sum = {};
 #pragma unroll
                 for (int o = 0; o < 3; ++o)
-                    if (o >= j && o < m) sum = mma16(rows_of(A, 16 * m, 16 * o, lane), col[o], sum);
-                col[m] = -mma16(rows_of(T, 16 * m, 16 * m, lane), sum, f32x4{});
+                    if (o >= j && o < m) sum = mma16(rows_of(A + low_at(16 * m, 16 * o), 0, 0, lane, low_pitch(16 * m)), col[o], sum);
+                col[m] = -mma16(rows_of(T + low_at(16 * m, 16 * m), 0, 0, lane, low_pitch(16 * m)), sum, f32x4{});
 #pragma unroll
-                for (int v = 0; v < 4; ++v) T[(16 * m + 4 * (lane >> 4) + v) * kPitch + 16 * j + (lane & 15)] = col[m][v];
+                for (int v = 0; v < 4; ++v) T[low_at(16 * m, 16 * j) + (4 * (lane >> 4) + v) * low_pitch(16 * m) + (lane & 15)] = col[m][v];
             }
         }
     }
@@ -478,14 +508,14 @@ template <typename T, int KT> __device__ __forceinline__ void delta_pairs(const 
         for (int v = 0; v < 4; ++v) e[v] = j + v < i || (is_p && j + v == i) ? exp2_of(m.s.G[i] - m.s.G[j + v]) : 0.0f;
         d = d * e * four(m.s.rk, j) * (is_p ? m.s.rq[i] : m.s.rk[i]);
         *reinterpret_cast<f32x4 *>((is_p ? to.p : to.kk)[task >> 1] + 16 * c + g4) = d;
-        if (!is_p) *reinterpret_cast<f32x4 *>(m.a + i * kPitch + j) = d * m.s.beta[i];
+        if (!is_p) *reinterpret_cast<f32x4 *>(m.a + low_at(i, j)) = d * m.s.beta[i];
     }
     __syncthreads();
     invert(m.a, m.t);
     for (int i = tid; i < 640; i += 256) {
         int ti, tj;
         low_tile(i >> 6, ti, tj);
-        *reinterpret_cast<f32x4 *>(to.t[i >> 6] + 4 * (i & 63)) = four(m.t, (16 * ti + ((i & 63) >> 2)) * kPitch + 16 * tj + 4 * (i & 3));
+        *reinterpret_cast<f32x4 *>(to.t[i >> 6] + 4 * (i & 63)) = four(m.t, low_at(16 * ti + ((i & 63) >> 2), 16 * tj + 4 * (i & 3)));
     }
     for (int i = tid; i < (int)sizeof(Gates) / 16; i += 256) reinterpret_cast<f32x4 *>(&to.s)[i] = reinterpret_cast<const f32x4 *>(&m.s)[i];
 }
@@ -498,31 +528,44 @@ template <typename T, int KT> __global__ __launch_bounds__(256) void delta_pairs
 
 // ---- from chunk to chunk ----
 
-template <typename T, int KT> struct DeltaLds {
-    typename Mat<T>::Elem k[16 * KT * kPitch], q[16 * KT * kPitch];
-    typename Mat<T>::Elem t[Mat<T>::planes * 64 * kPitch], p[Mat<T>::planes * 64 * kPitch];
+// A walk: H heads' chunks, `segs` workgroups a row of chunks of which each has `per` of them.
+struct DeltaWalk {
+    int segs, per;
+    const float *starts;        // [B, H, segs, DK, DV]: the state that a segment starts with (one segment: the call's own)
+    float *spans;               // [B, H, segs, DK, DV + DK]: of the pass that forms them
+};
+
+// (P in as many limbs as a walk takes: two for an output, three for a gradient that goes on.)
+template <typename T, int KT, int NP> struct DeltaLds {
+    typename Mat<T>::Elem k[16 * KT * kPitch], q[16 * KT * kPitch], t[Mat<T>::planes * kLow], p[(Mat<T>::planes < NP ? Mat<T>::planes : NP) * kLow];
     Gates s;
 };
+constexpr int kWalkWaves = 4;           // of a workgroup; two of those fit a CU, one's products beside the other's way into LDS
 // A chunk's data on its way into LDS, while the chunk before is worked at.
-template <typename T, int KT, int W> struct Ahead {
-    Tile<T, 16 * KT, 64 * W> k, q;
-    LowTiles<T, 64 * W> t, p;
-    static constexpr int NG = sizeof(Gates) / 16;
+template <typename T, int KT, int NP, bool KEYS_ONLY> struct Ahead {
+    static constexpr int LANES = 64 * kWalkWaves, NG = sizeof(Gates) / 16;
+    Tile<T, 16 * KT, LANES> k, q;
+    LowTiles<T, 3, LANES> t;
+    LowTiles<T, NP, LANES> p;
     f32x4 s;
     __device__ __forceinline__ void load(const DeltaShape<T> &a, const T *krow, const T *qrow, const DeltaPairs *r, int t0, int n)
     {
         k.load(krow, a.DK, t0, n, a.L);
-        q.load(qrow, a.DK, t0, n, a.L);
         t.load(r->t);
-        p.load(r->p);
+        if constexpr (!KEYS_ONLY) {
+            q.load(qrow, a.DK, t0, n, a.L);
+            p.load(r->p);
+        }
         s = reinterpret_cast<const f32x4 *>(&r->s)[threadIdx.x < NG ? threadIdx.x : 0];
     }
-    __device__ __forceinline__ void put(DeltaLds<T, KT> &m, int DK, int t0, int n) const
+    __device__ __forceinline__ void put(DeltaLds<T, KT, NP> &m, int DK, int t0, int n) const
     {
         k.put(m.k, DK, t0, n);
-        q.put(m.q, DK, t0, n);
         t.put(m.t);
-        p.put(m.p);
+        if constexpr (!KEYS_ONLY) {
+            q.put(m.q, DK, t0, n);
+            p.put(m.p);
+        }
         if (threadIdx.x < NG) reinterpret_cast<f32x4 *>(&m.s)[threadIdx.x] = s;
     }
 };
@@ -571,34 +614,70 @@ template <int KT> __device__ __forceinline__ void store_state(const f32x4 (&S)[K
         for (int v = 0; v < 4; ++v) to.store(S[kb][v], at, to.row(16 * kb + v));
 }
 
-// Forward.  A workgroup has a head's state, a wave 16 of its columns in registers; it walks the head's chunks.
-template <typename T, int KT, int W> __device__ __forceinline__ void delta_fwd_head(const DeltaFwd<T> &p, DeltaLds<T, KT> &m, int unit)
+// A wave's columns of a walk.  A pass that forms spans walks segments on their own: DV columns that start as zeros, whose end is what the
+// segment adds, and DK columns that start as those of the identity, with nothing written, whose end is what it makes of a state.
+struct Columns {
+    int at;                     // the wave's first column of the tensors
+    bool active, in, unit;      // there is one; this lane's is one; of the identity
+    int column;                 // of a span
+    __device__ __forceinline__ Columns(int slice, int c, int DK, int DV, bool spans)
+    {
+        const int values = (DV + 15) / 16;
+        unit = spans && slice >= values;
+        at = 16 * (unit ? slice - values : slice);
+        active = at < (unit ? DK : DV);
+        in = at + c < (unit ? DK : DV);
+        column = (unit ? DV : 0) + at + c;
+    }
+};
+template <int KT> __device__ __forceinline__ void unit_state(f32x4 (&S)[KT], int column, int g4)
+{
+#pragma unroll
+    for (int kb = 0; kb < KT; ++kb)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) S[kb][v] = 16 * kb + g4 + v == column ? 1.0f : 0.0f;
+}
+
+// Forward.  A workgroup has 64 columns of a head's state, a wave 16 of them in registers; it walks the chunks of its segment.
+template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_fwd_walk(const DeltaFwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT, 2> &m, int unit)
 {
     typedef Mat<T> M;
-    constexpr int PL = 64 * kPitch;
-    const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane0 & 15, g4 = 4 * (lane0 >> 4);
-    const int b = unit / p.H, h = unit % p.H, hk = h / p.each, n = p.length(b), last = (n + 63) / 64;
-    const int dv0 = (blockIdx.y * W + wave) * 16, dv = dv0 + c;
-    const bool in = dv < p.DV, active = dv0 < p.DV;
-    const long long head = (long long)b * p.H + h, size = (long long)p.DK * p.DV;
+    const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row = unit / walk.segs, seg = unit % walk.segs, b = row / p.H, h = row % p.H, hk = h / p.each, n = p.length(b);
+    const int from = seg * walk.per, last = min(from + walk.per, (n + 63) / 64);
+    if (SPANS && seg + 1 == walk.segs) return;          // (no segment starts with what this one makes)
+    const Columns col(blockIdx.y * kWalkWaves + wave, lane0 & 15, p.DK, p.DV, SPANS);
+    const bool in = col.in;
+    const long long head = row, size = (long long)p.DK * p.DV;
     f32x4 S[KT] = {};
-    if (p.s0) load_state(S, StateIn(p.s0 + head * size, p.DK, p.DV), dv, in, g4);
-    const T *vrow = p.v.row(b, h * p.DV + (in ? dv : 0), p.L), *krow = p.k.row(b, hk * p.DK, p.L), *qrow = p.q.row(b, hk * p.DK, p.L);
-    T *orow = p.o.row(b, h * p.DV + (in ? dv : 0), p.L);
+    {
+        const int dv = col.at + (lane0 & 15), g4 = 4 * (lane0 >> 4);
+        if (SPANS) {
+            if (col.unit) unit_state(S, dv, g4);
+        } else if (walk.segs > 1) {
+            load_state(S, StateIn(walk.starts + unit * size, p.DK, p.DV), dv, in, g4);
+        } else if (p.s0) {
+            load_state(S, StateIn(p.s0 + head * size, p.DK, p.DV), dv, in, g4);
+        }
+    }
+    const bool values = in && !col.unit;
+    const int own = values ? h * p.DV + col.at + (lane0 & 15) : 0;
+    const T *vrow = p.v.row(b, own, p.L), *krow = p.k.row(b, hk * p.DK, p.L), *qrow = p.q.row(b, hk * p.DK, p.L);
+    T *orow = p.o.row(b, own, p.L);
     const DeltaPairs *pairs = p.pairs + head * p.chunks;
-    Ahead<T, KT, W> next;
+    Ahead<T, KT, 2, SPANS> next;
     f32x4 val[4] = {};
-    if (last > 0) next.load(p, krow, qrow, pairs, 0, n);
-    for (int ch = 0; ch < last; ++ch) {
+    if (from < last) next.load(p, krow, qrow, pairs + from, from * 64, n);
+    for (int ch = from; ch < last; ++ch) {
         const int t0 = ch * kDeltaChunk;
-        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dv = dv0 + c;
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dv = col.at + c;
         __syncthreads();
         next.put(m, p.DK, t0, n);
-        load_rows(val, vrow, t0, g4, n, in);
-        if (p.states) store_state(S, StateIn(p.states + (head * p.chunks + ch) * size, p.DK, p.DV), dv, in, g4);
+        load_rows(val, vrow, t0, g4, n, values);
+        if (!SPANS && p.states) store_state(S, StateIn(p.states + (head * p.chunks + ch) * size, p.DK, p.DV), dv, in, g4);
         __syncthreads();
         if (ch + 1 < last) next.load(p, krow, qrow, pairs + ch + 1, t0 + 64, n);
-        if (!active) continue;
+        if (!col.active) continue;
         f32x4 r[4] = {}, w[4] = {}, o[4] = {};
 #pragma unroll
         for (int kb = 0; kb < KT; kb += 2) {
@@ -606,26 +685,29 @@ template <typename T, int KT, int W> __device__ __forceinline__ void delta_fwd_h
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 r[i] = M::mma(M::columns_in(m.k, 16 * i, 16 * kb, lane), s, r[i]);
-                o[i] = M::template mma<2>(M::columns_in(m.q, 16 * i, 16 * kb, lane), s, o[i]);
+                if (!SPANS) o[i] = M::template mma<2>(M::columns_in(m.q, 16 * i, 16 * kb, lane), s, o[i]);
             }
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = 16 * i + g4;
             r[i] = four(m.s.beta, t) * (val[i] - four(m.s.eG, t) * four(m.s.rk, t) * r[i]);
-            o[i] *= four(m.s.eG, t) * four(m.s.rq, t);
+            if (!SPANS) o[i] *= four(m.s.eG, t) * four(m.s.rq, t);
         }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             const typename M::Full x = M::split(r[2 * kb], r[2 * kb + 1]);
 #pragma unroll
-            for (int i = 2 * kb; i < 4; ++i) w[i] = M::mma(M::rows(m.t, PL, 16 * i, 32 * kb, lane), x, w[i]);
+            for (int i = 2 * kb; i < 4; ++i) w[i] = M::mma(M::low_rows(m.t, 16 * i, kb, lane), x, w[i]);
         }
+        if (!SPANS) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const typename M::Full x = M::template split<2>(w[2 * kb], w[2 * kb + 1]);
+            for (int kb = 0; kb < 2; ++kb) {
+                const typename M::Full x = M::template split<2>(w[2 * kb], w[2 * kb + 1]);
 #pragma unroll
-            for (int i = 2 * kb; i < 4; ++i) o[i] = M::template mma<2>(M::template rows<2>(m.p, PL, 16 * i, 32 * kb, lane), x, o[i]);
+                for (int i = 2 * kb; i < 4; ++i) o[i] = M::template mma<2>(M::template low_rows<2>(m.p, 16 * i, kb, lane), x, o[i]);
+            }
+            store_rows(orow, o, t0, g4, p.L, in);       // (k and q behind n are zeros, so these are)
         }
         const float eA = m.s.eG[63];
 #pragma unroll
@@ -638,53 +720,70 @@ template <typename T, int KT, int W> __device__ __forceinline__ void delta_fwd_h
 #pragma unroll
             for (int kb = 0; kb < KT; ++kb) S[kb] = M::mma(M::rows_in(m.k, 16 * kb, 32 * j, lane), x, S[kb]);
         }
-        store_rows(orow, o, t0, g4, p.L, in);           // (k and q behind n are zeros, so these are)
     }
-    if (in)
-        for (int t = last * 64 + g4; t < p.L; t += 16) store4(orow, f32x4{}, t, p.L);
-    if (p.s_last) store_state(S, StateIn(p.s_last + head * size, p.DK, p.DV), dv, in, g4);
+    const int c = lane0 & 15, g4 = 4 * (lane0 >> 4);
+    if (SPANS) {
+        store_state(S, StateIn(walk.spans + unit * size + unit * (long long)p.DK * p.DK, p.DK, p.DV + p.DK), col.column, in, g4);
+        return;
+    }
+    if (in)                                             // (behind the sequence's end)
+        for (int t = max(last, from) * 64 + g4, to = min(p.L, seg + 1 < walk.segs ? (from + walk.per) * 64 : p.L); t < to; t += 16) store4(orow, f32x4{}, t, p.L);
+    if (p.s_last && seg + 1 == walk.segs) store_state(S, StateIn(p.s_last + head * size, p.DK, p.DV), col.at + c, in, g4);
 }
-template <typename T, int KT, int W> __global__ __launch_bounds__(64 * W) void delta_fwd_kernel(DeltaFwd<T> p, int first)
+template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWalkWaves, 2) void delta_fwd_kernel(DeltaFwd<T> p, DeltaWalk walk, int first)
 {
     extern __shared__ char lds[];
-    DeltaLds<T, KT> &m = *reinterpret_cast<DeltaLds<T, KT> *>(lds);
-    LowTiles<T, 64 * W>::zeros(m.t);
-    LowTiles<T, 64 * W>::zeros(m.p);
-    delta_fwd_head<T, KT, W>(p, m, first + (int)blockIdx.x);
+    DeltaLds<T, KT, 2> &m = *reinterpret_cast<DeltaLds<T, KT, 2> *>(lds);
+    LowTiles<T, 3, 64 * kWalkWaves>::zeros(m.t);
+    if (!SPANS) LowTiles<T, 2, 64 * kWalkWaves>::zeros(m.p);
+    delta_fwd_walk<T, KT, SPANS>(p, walk, m, first + (int)blockIdx.x);
 }
 
 // Backward, from chunk to chunk: with dS the gradient of the state behind a chunk,
 //     dw = P^T do + exp(G_63 - G) k dS,   (I + A)^T dr = dw,   dS <- exp(G_63) dS + sum_i exp(G_i) q_i do_i^T - beta_i exp(G_i) k_i dr_i^T.
 // Leaves dS behind every chunk, and dv = beta dr.
-template <typename T, int KT, int W> __device__ __forceinline__ void delta_bwd_head(const DeltaBwd<T> &p, DeltaLds<T, KT> &m, int unit)
+template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_bwd_walk(const DeltaBwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT, 3> &m, int unit)
 {
     typedef Mat<T> M;
-    constexpr int PL = 64 * kPitch;
-    const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane0 & 15, g4 = 4 * (lane0 >> 4);
-    const int b = unit / p.H, h = unit % p.H, hk = h / p.each, n = p.length(b), last = (n + 63) / 64;
-    const int dv0 = (blockIdx.y * W + wave) * 16, dv = dv0 + c;
-    const bool in = dv < p.DV, active = dv0 < p.DV;
-    const long long head = (long long)b * p.H + h, size = (long long)p.DK * p.DV;
+    const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row = unit / walk.segs, seg = unit % walk.segs, b = row / p.H, h = row % p.H, hk = h / p.each, n = p.length(b);
+    const int from = seg * walk.per, last = min(from + walk.per, (n + 63) / 64);
+    if (SPANS && seg == 0) return;
+    const Columns col(blockIdx.y * kWalkWaves + wave, lane0 & 15, p.DK, p.DV, SPANS);
+    const bool in = col.in;
+    const long long head = row, size = (long long)p.DK * p.DV;
     f32x4 S[KT] = {};
-    if (p.ds_last) load_state(S, StateIn(p.ds_last + head * size, p.DK, p.DV), dv, in, g4);
-    const T *drow = p.dout.row(b, h * p.DV + (in ? dv : 0), p.L), *krow = p.k.row(b, hk * p.DK, p.L), *qrow = p.q.row(b, hk * p.DK, p.L);
-    T *vrow = p.dv.row(b, h * p.DV + (in ? dv : 0), p.L);
+    {
+        const int dv = col.at + (lane0 & 15), g4 = 4 * (lane0 >> 4);
+        if (SPANS) {
+            if (col.unit) unit_state(S, dv, g4);
+        } else if (walk.segs > 1) {
+            load_state(S, StateIn(walk.starts + unit * size, p.DK, p.DV), dv, in, g4);
+        } else if (p.ds_last) {
+            load_state(S, StateIn(p.ds_last + head * size, p.DK, p.DV), dv, in, g4);
+        }
+    }
+    const bool values = in && !col.unit;
+    const int own = values ? h * p.DV + col.at + (lane0 & 15) : 0;
+    const T *drow = p.dout.row(b, own, p.L), *krow = p.k.row(b, hk * p.DK, p.L), *qrow = p.q.row(b, hk * p.DK, p.L);
+    T *vrow = p.dv.row(b, own, p.L);
     const DeltaPairs *pairs = p.pairs + head * p.chunks;
-    if (in)
-        for (int t = last * 64 + g4; t < p.L; t += 16) store4(vrow, f32x4{}, t, p.L);
-    Ahead<T, KT, W> next;
+    if (!SPANS && in)                                   // (behind the sequence's end)
+        for (int t = max(last, from) * 64 + 4 * (lane0 >> 4), to = min(p.L, seg + 1 < walk.segs ? (from + walk.per) * 64 : p.L); t < to; t += 16)
+            store4(vrow, f32x4{}, t, p.L);
+    Ahead<T, KT, 3, false> next;
     f32x4 d[4] = {};
-    if (last > 0) next.load(p, krow, qrow, pairs + last - 1, (last - 1) * 64, n);
-    for (int ch = last - 1; ch >= 0; --ch) {
+    if (from < last) next.load(p, krow, qrow, pairs + last - 1, (last - 1) * 64, n);
+    for (int ch = last - 1; ch >= from; --ch) {
         const int t0 = ch * kDeltaChunk;
-        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dv = dv0 + c;
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dv = col.at + c;
         __syncthreads();
         next.put(m, p.DK, t0, n);
-        load_rows(d, drow, t0, g4, n, in);
-        store_state(S, StateIn(p.after + (head * p.chunks + ch) * size, p.DK, p.DV), dv, in, g4);
+        load_rows(d, drow, t0, g4, n, values);
+        if (!SPANS) store_state(S, StateIn(p.after + (head * p.chunks + ch) * size, p.DK, p.DV), dv, in, g4);
         __syncthreads();
-        if (ch > 0) next.load(p, krow, qrow, pairs + ch - 1, t0 - 64, n);
-        if (!active) continue;
+        if (ch > from) next.load(p, krow, qrow, pairs + ch - 1, t0 - 64, n);
+        if (!col.active) continue;
         f32x4 w[4] = {}, r[4] = {};
 #pragma unroll
         for (int kb = 0; kb < KT; kb += 2) {
@@ -698,13 +797,13 @@ template <typename T, int KT, int W> __device__ __forceinline__ void delta_bwd_h
         for (int kb = 0; kb < 2; ++kb) {
             const typename M::In x = M::exact(d[2 * kb], d[2 * kb + 1]);
 #pragma unroll
-            for (int j = 0; j < 2 * kb + 2; ++j) w[j] = M::mma(M::columns(m.p, PL, 16 * j, 32 * kb, lane), x, w[j]);
+            for (int j = 0; j < 2 * kb + 2; ++j) w[j] = M::mma(M::low_columns(m.p, 16 * j, kb, lane), x, w[j]);
         }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             const typename M::Full x = M::split(w[2 * kb], w[2 * kb + 1]);
 #pragma unroll
-            for (int j = 0; j < 2 * kb + 2; ++j) r[j] = M::mma(M::columns(m.t, PL, 16 * j, 32 * kb, lane), x, r[j]);
+            for (int j = 0; j < 2 * kb + 2; ++j) r[j] = M::mma(M::low_columns(m.t, 16 * j, kb, lane), x, r[j]);
         }
         const float eA = m.s.eG[63];
 #pragma unroll
@@ -715,7 +814,7 @@ template <typename T, int KT, int W> __device__ __forceinline__ void delta_bwd_h
             r[i] *= -four(m.s.eG, t) * four(m.s.rk, t);
             d[i] *= four(m.s.eG, t) * four(m.s.rq, t);
         }
-        store_rows(vrow, w, t0, g4, p.L, in);
+        if (!SPANS) store_rows(vrow, w, t0, g4, p.L, in);
 #pragma unroll
         for (int kb = 0; kb < KT; ++kb) S[kb] *= eA;
 #pragma unroll
@@ -728,15 +827,58 @@ template <typename T, int KT, int W> __device__ __forceinline__ void delta_bwd_h
             }
         }
     }
-    if (p.ds0) store_state(S, StateIn(p.ds0 + head * size, p.DK, p.DV), dv, in, g4);
+    const int c = lane0 & 15, g4 = 4 * (lane0 >> 4);
+    if (SPANS) store_state(S, StateIn(walk.spans + unit * size + unit * (long long)p.DK * p.DK, p.DK, p.DV + p.DK), col.column, in, g4);
+    else if (p.ds0 && seg == 0) store_state(S, StateIn(p.ds0 + head * size, p.DK, p.DV), col.at + c, in, g4);
 }
-template <typename T, int KT, int W> __global__ __launch_bounds__(64 * W) void delta_bwd_state_kernel(DeltaBwd<T> p, int first)
+template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWalkWaves, 2) void delta_bwd_state_kernel(DeltaBwd<T> p, DeltaWalk walk, int first)
 {
     extern __shared__ char lds[];
-    DeltaLds<T, KT> &m = *reinterpret_cast<DeltaLds<T, KT> *>(lds);
-    LowTiles<T, 64 * W>::zeros(m.t);
-    LowTiles<T, 64 * W>::zeros(m.p);
-    delta_bwd_head<T, KT, W>(p, m, first + (int)blockIdx.x);
+    DeltaLds<T, KT, 3> &m = *reinterpret_cast<DeltaLds<T, KT, 3> *>(lds);
+    LowTiles<T, 3, 64 * kWalkWaves>::zeros(m.t);
+    LowTiles<T, 3, 64 * kWalkWaves>::zeros(m.p);
+    delta_bwd_walk<T, KT, SPANS>(p, walk, m, first + (int)blockIdx.x);
+}
+
+// The states that segments start with, one after the other (forward; backward the other way): S <- N + M S with a segment's span (N, M).  A workgroup
+// 16 columns, a wave 16 rows of them, fp32 products; the next span is on its way meanwhile.
+template <int KT, bool BACK> __global__ __launch_bounds__(64 * KT) void delta_starts_kernel(const float *s0, const float *spans, float *starts, int segs, int DK, int DV)
+{
+    __shared__ f32x4 tiles[2][KT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g4 = 4 * (lane >> 4), dv = blockIdx.y * 16 + c;
+    const bool in = dv < DV;
+    const long long head = blockIdx.x, size = (long long)DK * DV, span = size + (long long)DK * DK;
+    const auto unit = [&](int i) { return head * segs + (BACK ? segs - 1 - i : i); };
+    f32x4 S = {}, a[KT], add;
+    const auto rows = [&](const StateIn &x) __attribute__((always_inline)) {
+        const unsigned at = x.lane(g4, dv, in);
+        f32x4 r;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) r[v] = x.load(at, x.row(16 * wave + v));
+        return r;
+    };
+    const auto fetch = [&](int i) __attribute__((always_inline)) {
+        const StateIn x(spans + unit(i) * span, DK, DV + DK);
+        add = rows(x);
+#pragma unroll
+        for (int k = 0; k < KT; ++k) a[k] = x.four(16 * wave + c, DV + 16 * k + g4, DV + DK);
+    };
+    if (s0) S = rows(StateIn(s0 + head * size, DK, DV));
+    fetch(0);
+    for (int i = 0; i < segs; ++i) {
+        const StateIn to(starts + unit(i) * size, DK, DV);
+        const unsigned at = to.lane(g4, dv, in);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) to.store(S[v], at, to.row(16 * wave + v));
+        if (i + 1 == segs) break;
+        tiles[i & 1][wave][lane] = S;
+        __syncthreads();
+        f32x4 sum[2] = {add, f32x4{}};
+#pragma unroll
+        for (int k = 0; k < KT; ++k) sum[k & 1] = mma16(a[k], tiles[i & 1][k][lane], sum[k & 1]);
+        S = sum[0] + sum[1];
+        if (i + 2 < segs) fetch(i + 1);
+    }
 }
 
 // ---- gradients within a chunk ----
@@ -753,7 +895,7 @@ constexpr int kDeltaBwdWaves(int KT) { return KT < 4 ? 4 : KT; }
 template <typename T, int KT> struct DeltaChunkLds {
     typedef typename Mat<T>::Elem Elem;
     static constexpr int NP = Mat<T>::planes, VB = sizeof(T) == 4 && KT > 4 ? 32 : 64;     // columns of a state at a time, as LDS has room
-    Elem k[16 * KT * kPitch], t[NP * 64 * kPitch], p[NP * 64 * kPitch];
+    Elem k[16 * KT * kPitch], t[NP * kLow], p[NP * kLow];
     union {
         struct {
             Elem dout[VB * kPitch], w[NP * VB * kPitch], dr[NP * VB * kPitch];
@@ -776,7 +918,7 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
     typedef Mat<T> M;
     typedef typename M::Full Full;
     typedef DeltaChunkLds<T, KT> Lds;
-    constexpr int W = kDeltaBwdWaves(KT), VB = Lds::VB, NS = VB / 16, NT = (10 + W - 1) / W, NJ = (2 * NS + W - 1) / W, PL = 64 * kPitch, VP = VB * kPitch;
+    constexpr int W = kDeltaBwdWaves(KT), VB = Lds::VB, NS = VB / 16, NT = (10 + W - 1) / W, NJ = (2 * NS + W - 1) / W, VP = VB * kPitch;
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane0 & 15, g4 = 4 * (lane0 >> 4);
     const int ch = unit % p.chunks, bk = unit / p.chunks, Hk = p.H / p.each, b = bk / Hk, hk = bk % Hk;
     const int n = p.length(b), t0 = ch * kDeltaChunk, dk = 16 * wave + c;
@@ -815,7 +957,7 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
             if (task & 1) load_rows(d, p.dout.row(b, h * p.DV + (in ? dv : 0), p.L), t0, g4, n, in);
         };
         {
-            LowTiles<T, 64 * W> t, u;
+            LowTiles<T, 3, 64 * W> t, u;
             t.load(pairs.t);
             u.load(pairs.p);
             const f32x4 gates = reinterpret_cast<const f32x4 *>(&pairs.s)[threadIdx.x < sizeof(Gates) / 16 ? threadIdx.x : 0];
@@ -857,14 +999,14 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
                     for (int kb = 0; kb < 2; ++kb) {
                         const typename M::In z = M::exact(d[2 * kb], d[2 * kb + 1]);
 #pragma unroll
-                        for (int j = 0; j < 2 * kb + 2; ++j) x[j] = M::mma(M::columns(m.p, PL, 16 * j, 32 * kb, lane), z, x[j]);
+                        for (int j = 0; j < 2 * kb + 2; ++j) x[j] = M::mma(M::low_columns(m.p, 16 * j, kb, lane), z, x[j]);
                         step_done();
                     }
 #pragma unroll
                     for (int kb = 0; kb < 2; ++kb) {
                         const Full z = M::split(x[2 * kb], x[2 * kb + 1]);
 #pragma unroll
-                        for (int j = 0; j < 2 * kb + 2; ++j) y[j] = M::mma(M::columns(m.t, PL, 16 * j, 32 * kb, lane), z, y[j]);
+                        for (int j = 0; j < 2 * kb + 2; ++j) y[j] = M::mma(M::low_columns(m.t, 16 * j, kb, lane), z, y[j]);
                         step_done();
                     }
 #pragma unroll
@@ -883,7 +1025,7 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
                     for (int kb = 0; kb < 2; ++kb) {
                         const Full z = M::split(x[2 * kb], x[2 * kb + 1]);
 #pragma unroll
-                        for (int i = 2 * kb; i < 4; ++i) y[i] = M::mma(M::rows(m.t, PL, 16 * i, 32 * kb, lane), z, y[i]);
+                        for (int i = 2 * kb; i < 4; ++i) y[i] = M::mma(M::low_rows(m.t, 16 * i, kb, lane), z, y[i]);
                         step_done();
                     }
 #pragma unroll
@@ -961,8 +1103,8 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
             sum += __shfl_xor(sum, 16, 64);
             sum += __shfl_xor(sum, 32, 64);
             if (lane < 16) m.da[tj][i] = sum;
-            M::template put<2>(m.p, PL, i * kPitch + j, dP * e);
-            M::template put<2>(m.t, PL, i * kPitch + j, dA * e * m.s.beta[i]);
+            M::template put<2>(m.p, kLow, low_at(i, j), dP * e);
+            M::template put<2>(m.t, kLow, low_at(i, j), dA * e * m.s.beta[i]);
             *reinterpret_cast<f32x4 *>(m.pairs + i * kPitch + j) = dP * pp[u] + x * m.s.beta[i];
         }
         f32x4 kh[4], qh[4];
@@ -1017,12 +1159,12 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (2 * kb <= i) {
-                        dq[i] = M::template mma<2>(M::template rows<2>(m.p, PL, 16 * i, 32 * kb, lane), kz, dq[i]);
-                        dkey[i] = M::template mma<2>(M::template rows<2>(m.t, PL, 16 * i, 32 * kb, lane), kz, dkey[i]);
+                        dq[i] = M::template mma<2>(M::template low_rows<2>(m.p, 16 * i, kb, lane), kz, dq[i]);
+                        dkey[i] = M::template mma<2>(M::template low_rows<2>(m.t, 16 * i, kb, lane), kz, dkey[i]);
                     }
                     if (i < 2 * kb + 2) {
-                        dkey[i] = M::template mma<2>(M::template columns<2>(m.p, PL, 16 * i, 32 * kb, lane), qz, dkey[i]);
-                        dkey[i] = M::template mma<2>(M::template columns<2>(m.t, PL, 16 * i, 32 * kb, lane), kz, dkey[i]);
+                        dkey[i] = M::template mma<2>(M::template low_columns<2>(m.p, 16 * i, kb, lane), qz, dkey[i]);
+                        dkey[i] = M::template mma<2>(M::template low_columns<2>(m.t, 16 * i, kb, lane), kz, dkey[i]);
                     }
                     step_done();
                 }
@@ -1104,8 +1246,8 @@ template <typename T, int KT> __global__ __launch_bounds__(64 * kDeltaBwdWaves(K
 {
     extern __shared__ char lds[];
     DeltaChunkLds<T, KT> &m = *reinterpret_cast<DeltaChunkLds<T, KT> *>(lds);
-    LowTiles<T, 64 * kDeltaBwdWaves(KT)>::zeros(m.t);
-    LowTiles<T, 64 * kDeltaBwdWaves(KT)>::zeros(m.p);
+    LowTiles<T, 3, 64 * kDeltaBwdWaves(KT)>::zeros(m.t);
+    LowTiles<T, 3, 64 * kDeltaBwdWaves(KT)>::zeros(m.p);
     delta_bwd_chunk(p, m, first + (int)blockIdx.x);
 }
 
