@@ -9,6 +9,28 @@ using namespace dwconv;
 
 namespace dwconv {
 
+// Four neighbours of a row, those from n on zero and not read.
+template <typename T> __device__ __forceinline__ f32x4 load4(const T *row, int t, int n)
+{
+    f32x4 r = {};
+    if (t + 4 <= n) r = load4(row + t);
+    else
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            if (t + k < n) r[k] = ld_elem(row + t + k);
+    return r;
+}
+
+// Rows of fewer than eight positions with room for eight, which the kernels read at once.
+template <typename T> __global__ __launch_bounds__(256) void delta_pad_kernel(Seq<T> x, T *to, int C, int L, long long rows)
+{
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < rows; i += gridDim.x * 256ll) {
+        const long long b = i / C;
+        const T *row = x.p + b * x.bs + (i - b * C) * L;
+        for (int t = 0; t < 8; ++t) to[8 * i + t] = t < L ? row[t] : T{};
+    }
+}
+
 template <typename T> struct DeltaStep {
     Seq<T> q, k, v;
     Seq<float> g, beta;
@@ -228,7 +250,7 @@ template <typename T> void launch_step(const DeltaStep<T> &in, hipStream_t st)
 template <typename T> DeltaShape<T> shape(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const int *lengths, int B, int H, int Hk,
                                           int DK, int DV, int L, float scale, float eps, void *workspace)
 {
-    return DeltaShape<T>{seq<T>(q), seq<T>(k), seq<T>(v), seq<float>(g), seq<float>(beta), lengths, B, H, H / Hk, DK, DV, L, chunks_of(L), scale, eps,
+    return DeltaShape<T>{seq<T>(q), seq<T>(k), seq<T>(v), seq<float>(g), seq<float>(beta), lengths, B, H, H / Hk, DK, DV, L, chunks_of(L), L, scale, eps,
                          static_cast<DeltaPairs *>(workspace)};
 }
 // A workspace: records of pairs, starts and spans of segments, backward the states' gradients behind the chunks.
@@ -238,11 +260,32 @@ size_t walk_bytes(int B, int H, int DK, int DV, int L)
     const WalkPlan w = plan_walk(B, H, DK, DV, L);
     return starts_bytes(w, B, H, DK, DV) + spans_bytes(w, B, H, DK, DV);
 }
+constexpr int kPadded = 8;
+size_t padded_bytes(int B, int H, int DK, int DV, int L) { return L < kPadded ? up16((size_t)B * H * (2 * (DK + DV)) * kPadded * sizeof(float)) : 0; }
+// Puts short rows where they have room for eight positions.
+template <typename T> void pad(Seq<T> &x, T *&to, int B, int C, int L, hipStream_t st)
+{
+    const long long rows = (long long)B * C;
+    delta_pad_kernel<T><<<(unsigned)std::min<long long>(ceil_div(rows, 256), 1 << 20), 256, 0, st>>>(x, to, C, L, rows);
+    x = Seq<T>{to, (long long)C * kPadded};
+    to += rows * kPadded;
+}
+template <typename T> void pad_all(DeltaShape<T> &p, Seq<T> *dout, void *room, hipStream_t st)
+{
+    if (p.L >= kPadded) return;
+    T *to = static_cast<T *>(room);
+    const int keys = p.H / p.each * p.DK, values = p.H * p.DV;
+    pad(p.q, to, p.B, keys, p.L, st);
+    pad(p.k, to, p.B, keys, p.L, st);
+    pad(p.v, to, p.B, values, p.L, st);
+    if (dout) pad(*dout, to, p.B, values, p.L, st);
+    p.pitch = kPadded;
+}
 size_t after_bytes(int B, int H, int DK, int DV, int L) { return up16((size_t)B * H * chunks_of(L) * DK * DV * sizeof(float)); }
 DeltaWalk walk_in(void *workspace, int B, int H, int DK, int DV, int L)
 {
     const WalkPlan w = plan_walk(B, H, DK, DV, L);
-    char *at = static_cast<char *>(workspace) + pairs_bytes(B, H, L);
+    char *at = static_cast<char *>(workspace) + pairs_bytes(B, H, L) + padded_bytes(B, H, DK, DV, L);
     return DeltaWalk{w.segs, w.per, reinterpret_cast<float *>(at), reinterpret_cast<float *>(at + starts_bytes(w, B, H, DK, DV))};
 }
 
@@ -255,7 +298,7 @@ int dwconv_delta_states(int L) { return L < 1 || L > (1 << 30) ? 0 : chunks_of(L
 size_t dwconv_delta_workspace_bytes(int B, int H, int DK, int DV, int L, int backward)
 {
     if (check_heads(B, H, H, DK, DV, L) != DWCONV_OK) return 0;
-    return pairs_bytes(B, H, L) + walk_bytes(B, H, DK, DV, L) + (backward ? after_bytes(B, H, DK, DV, L) : 0);
+    return pairs_bytes(B, H, L) + padded_bytes(B, H, DK, DV, L) + walk_bytes(B, H, DK, DV, L) + (backward ? after_bytes(B, H, DK, DV, L) : 0);
 }
 
 int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const float *s0, const int *lengths, dwconv_seq_out o,
@@ -278,11 +321,14 @@ int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwc
     if (!workspace || workspace_bytes < dwconv_delta_workspace_bytes(B, H, DK, DV, L, 0) || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const DeltaWalk walk = walk_in(workspace, B, H, DK, DV, L);
+    void *room = static_cast<char *>(workspace) + pairs_bytes(B, H, L);
     if (dtype == DWCONV_F32) {
         DeltaFwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<float>(o), s0, s_last, states};
+        pad_all<float>(p, nullptr, room, st);
         return launch_fwd(p, walk, st);
     }
     DeltaFwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<bf16_t>(o), s0, s_last, states};
+    pad_all<bf16_t>(p, nullptr, room, st);
     return launch_fwd(p, walk, st);
 }
 
@@ -310,14 +356,17 @@ int dwconv_delta_bwd(dwconv_seq dout, dwconv_seq q, dwconv_seq k, dwconv_seq v, 
     if (!workspace || workspace_bytes < need || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const DeltaWalk walk = walk_in(workspace, B, H, DK, DV, L);
-    float *after = reinterpret_cast<float *>(static_cast<char *>(workspace) + pairs_bytes(B, H, L) + walk_bytes(B, H, DK, DV, L));
+    float *after = reinterpret_cast<float *>(static_cast<char *>(workspace) + pairs_bytes(B, H, L) + padded_bytes(B, H, DK, DV, L) + walk_bytes(B, H, DK, DV, L));
+    void *room = static_cast<char *>(workspace) + pairs_bytes(B, H, L);
     if (dtype == DWCONV_F32) {
         DeltaBwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<float>(dout), seq<float>(dq), seq<float>(dk),
                           seq<float>(dv), states, ds_last, after, dg, dbeta, ds0};
+        pad_all<float>(p, &p.dout, room, st);
         return launch_bwd(p, walk, st);
     }
     DeltaBwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<bf16_t>(dout), seq<bf16_t>(dq), seq<bf16_t>(dk),
                        seq<bf16_t>(dv), states, ds_last, after, dg, dbeta, ds0};
+    pad_all<bf16_t>(p, &p.dout, room, st);
     return launch_bwd(p, walk, st);
 }
 

@@ -37,6 +37,7 @@ template <typename T> struct DeltaShape {
     Seq<float> g, beta;
     const int *lengths;
     int B, H, each, DK, DV, L, chunks;
+    int pitch;                          // elements from row to row of q, k, v and dout: L, or 8 of rows that were shorter and are padded
     float scale, eps;
     struct DeltaPairs *pairs;           // [B, H, chunks]
     __device__ __forceinline__ int length(int b) const { return lengths ? min(max(lengths[b], 0), L) : L; }
@@ -237,17 +238,7 @@ __device__ __forceinline__ f32x4 load4(const bf16_t *p)
 }
 __device__ __forceinline__ void store4(float *p, f32x4 v) { *reinterpret_cast<floatx4_any *>(p) = v; }
 __device__ __forceinline__ void store4(bf16_t *p, f32x4 v) { *reinterpret_cast<uintx2_any *>(p) = uintx2_any{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}; }
-// ... those from `n` on zero and not read, and not written.
-template <typename T> __device__ __forceinline__ f32x4 load4(const T *row, int t, int n)
-{
-    f32x4 r = {};
-    if (t + 4 <= n) r = load4(row + t);
-    else
-#pragma unroll
-        for (int k = 0; k < 3; ++k)
-            if (t + k < n) r[k] = ld_elem(row + t + k);
-    return r;
-}
+// ... those from L on not written.
 template <typename T> __device__ __forceinline__ void store4(T *row, f32x4 r, int t, int L)
 {
     if (t + 4 <= L) store4(row + t, r);
@@ -256,23 +247,38 @@ template <typename T> __device__ __forceinline__ void store4(T *row, f32x4 r, in
         for (int k = 0; k < 3; ++k)
             if (t + k < L) st_elem(row + t + k, r[k]);
 }
-
-// A lane's positions of a chunk, 16 i + g4 + v, of a row: zeros from position n on, and where the lane has no row (`row` is any then).  Whole chunks
-// are read without asking: a load behind a question waits for the one before.
-template <typename T> __device__ __forceinline__ void load_rows(f32x4 (&x)[4], const T *row, int t0, int g4, int n, bool in)
-{
-    if (t0 + 64 <= n) {
+// A lane's positions of a chunk, 16 i + g4 + v, of a row, as loaded: without a question, since a load behind one is waited for where its ways meet.
+// What would end behind the row is its last four, put right when they are asked for.
+template <typename T> struct Rows {
+    typedef typename Words<4 * sizeof(T)>::type Raw;
+    Raw x[4];
+    __device__ __forceinline__ void load(const T *row, int t0, int g4, int pitch)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const Raw *>(row + min(t0 + 16 * i + g4, pitch - 4));
+    }
+    static __device__ __forceinline__ f32x4 wide(const Words<16>::type u) { return __builtin_bit_cast(f32x4, u); }
+    static __device__ __forceinline__ f32x4 wide(const Words<8>::type u)
+    {
+        return f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xffff0000u), __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xffff0000u)};
+    }
+    // Zeros from position n on.
+    __device__ __forceinline__ void get(f32x4 (&v)[4], int t0, int g4, int n, int pitch) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = wide(x[i]);
+        if (t0 + 64 <= n) return;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const f32x4 v = load4(row + t0 + 16 * i + g4);
+            const int t = t0 + 16 * i + g4, by = t - (pitch - 4);
+            f32x4 u = v[i];
+            if (by > 0 && by & 2) u = f32x4{u[2], u[3], 0.0f, 0.0f};
+            if (by > 0 && by & 1) u = f32x4{u[1], u[2], u[3], 0.0f};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[i][k] = in ? v[k] : 0.0f;
+            for (int k = 0; k < 4; ++k) v[i][k] = t + k < n ? u[k] : 0.0f;
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = load4(row, t0 + 16 * i + g4, in ? n : 0);
     }
-}
+};
 template <typename T> __device__ __forceinline__ void store_rows(T *row, const f32x4 (&x)[4], int t0, int g4, int L, bool in)
 {
     if (t0 + 64 <= L) {
@@ -297,46 +303,40 @@ __device__ __forceinline__ float exp2_of(double d)
 template <typename T, int ROWS, int LANES> struct Tile {
     static constexpr int N = (ROWS * 8 + LANES - 1) / LANES;
     Eight<T> e[N];
-    __device__ __forceinline__ void load(const T *from, int D, int t0, int n, int L)
-    {
-        if (t0 + 64 <= L) {             // (no load asks first: none waits for another)
-#pragma unroll
-            for (int u = 0; u < N; ++u) {
-                const int i = threadIdx.x + u * LANES, r = i >> 3;
-                e[u] = load8(from + (long long)(r < D ? r : 0) * L + t0 + (i & 7) * 8);
-            }
-        } else {
-#pragma unroll
-            for (int u = 0; u < N; ++u) {
-                const int i = threadIdx.x + u * LANES, r = i >> 3, t = t0 + (i & 7) * 8;
-                Few<8, T> f{};
-                if (r < D && t < n) f = load_few<8>(from + (long long)r * L + t, min(8, L - t));
-                __builtin_memcpy(&e[u], &f, sizeof(f));
-            }
-        }
-    }
-    __device__ __forceinline__ void put(typename Mat<T>::Elem *to, int D, int t0, int n) const
+    __device__ __forceinline__ void load(const T *from, int D, int t0, int pitch)
     {
 #pragma unroll
         for (int u = 0; u < N; ++u) {
-            const int i = threadIdx.x + u * LANES, r = i >> 3, left = n - t0 - (i & 7) * 8;
+            const int i = threadIdx.x + u * LANES, r = i >> 3;
+            e[u] = load8(from + (long long)(r < D ? r : 0) * pitch + min(t0 + (i & 7) * 8, pitch - 8));
+        }
+    }
+    __device__ __forceinline__ void put(typename Mat<T>::Elem *to, int D, int t0, int n, int pitch) const
+    {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int i = threadIdx.x + u * LANES, r = i >> 3, t = t0 + (i & 7) * 8;
             if (ROWS * 8 % LANES && r >= ROWS) continue;
-            put_eight(to + r * kPitch + (i & 7) * 8, e[u], r < D ? left : 0);
+            Eight<T> x = e[u];
+            if (t0 + 64 > pitch) move_down(x, max(t - (pitch - 8), 0) & 7);     // (a whole eight on, nothing of it is inside)
+            put_eight(to + r * kPitch + (i & 7) * 8, x, r < D ? n - t : 0);
         }
     }
     static __device__ __forceinline__ void put_eight(float *to, const Eight<float> &e, int left)
     {
         f32x4 a = e.lo, b = e.hi;
+        if (left < 8)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) a[k] = k < left ? a[k] : 0.0f, b[k] = k + 4 < left ? b[k] : 0.0f;
+            for (int k = 0; k < 4; ++k) a[k] = k < left ? a[k] : 0.0f, b[k] = k + 4 < left ? b[k] : 0.0f;
         f32x4 *p = reinterpret_cast<f32x4 *>(to);
         p[0] = a, p[1] = b;
     }
     static __device__ __forceinline__ void put_eight(short *to, const Eight<bf16_t> &e, int left)
     {
         u32x4 w = e.w;
+        if (left < 8)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = 2 * k + 1 < left ? w[k] : 2 * k < left ? w[k] & 0xffffu : 0u;
+            for (int k = 0; k < 4; ++k) w[k] = 2 * k + 1 < left ? w[k] : 2 * k < left ? w[k] & 0xffffu : 0u;
         u32x2 *p = reinterpret_cast<u32x2 *>(to);
         p[0] = u32x2{w[0], w[1]}, p[1] = u32x2{w[2], w[3]};
     }
@@ -449,15 +449,15 @@ template <typename T, int KT> __device__ __forceinline__ void delta_pairs(const 
     if (t0 >= n) return;
     DeltaPairs &to = p.pairs[unit];
     Tile<T, 16 * KT, 256> k, q;
-    k.load(p.k.row(b, hk * p.DK, p.L), p.DK, t0, n, p.L);
-    q.load(p.q.row(b, hk * p.DK, p.L), p.DK, t0, n, p.L);
+    k.load(p.k.row(b, hk * p.DK, p.pitch), p.DK, t0, p.pitch);
+    q.load(p.q.row(b, hk * p.DK, p.pitch), p.DK, t0, p.pitch);
     float g = 0.0f, beta = 0.0f;
     if (wave == 0 && t0 + lane < n) {
         g = p.g.row(b, h, p.L)[t0 + lane];
         beta = p.beta.row(b, h, p.L)[t0 + lane];
     }
-    k.put(m.k, p.DK, t0, n);
-    q.put(m.q, p.DK, t0, n);
+    k.put(m.k, p.DK, t0, n, p.pitch);
+    q.put(m.q, p.DK, t0, n, p.pitch);
     __syncthreads();
     {
         float x = 0.0f, y = 0.0f;
@@ -541,31 +541,29 @@ template <typename T, int KT, int NP> struct DeltaLds {
     Gates s;
 };
 constexpr int kWalkWaves = 4;           // of a workgroup; two of those fit a CU, one's products beside the other's way into LDS
-// A chunk's data on its way into LDS, while the chunk before is worked at.
+// A chunk's data on its way into LDS, and a wave's columns of v or dout, while the chunk before is worked at.
 template <typename T, int KT, int NP, bool KEYS_ONLY> struct Ahead {
     static constexpr int LANES = 64 * kWalkWaves, NG = sizeof(Gates) / 16;
     Tile<T, 16 * KT, LANES> k, q;
     LowTiles<T, 3, LANES> t;
     LowTiles<T, NP, LANES> p;
     f32x4 s;
-    __device__ __forceinline__ void load(const DeltaShape<T> &a, const T *krow, const T *qrow, const DeltaPairs *r, int t0, int n)
+    Rows<T> rows;
+    __device__ __forceinline__ void load(const DeltaShape<T> &a, const T *krow, const T *qrow, const T *row, const DeltaPairs *r, int t0, int g4)
     {
-        k.load(krow, a.DK, t0, n, a.L);
+        k.load(krow, a.DK, t0, a.pitch);
+        if constexpr (!KEYS_ONLY) q.load(qrow, a.DK, t0, a.pitch);
         t.load(r->t);
-        if constexpr (!KEYS_ONLY) {
-            q.load(qrow, a.DK, t0, n, a.L);
-            p.load(r->p);
-        }
+        if constexpr (!KEYS_ONLY) p.load(r->p);
         s = reinterpret_cast<const f32x4 *>(&r->s)[threadIdx.x < NG ? threadIdx.x : 0];
+        rows.load(row, t0, g4, a.pitch);
     }
-    __device__ __forceinline__ void put(DeltaLds<T, KT, NP> &m, int DK, int t0, int n) const
+    __device__ __forceinline__ void put(DeltaLds<T, KT, NP> &m, const DeltaShape<T> &a, int t0, int n) const
     {
-        k.put(m.k, DK, t0, n);
+        k.put(m.k, a.DK, t0, n, a.pitch);
+        if constexpr (!KEYS_ONLY) q.put(m.q, a.DK, t0, n, a.pitch);
         t.put(m.t);
-        if constexpr (!KEYS_ONLY) {
-            q.put(m.q, DK, t0, n);
-            p.put(m.p);
-        }
+        if constexpr (!KEYS_ONLY) p.put(m.p);
         if (threadIdx.x < NG) reinterpret_cast<f32x4 *>(&m.s)[threadIdx.x] = s;
     }
 };
@@ -574,7 +572,7 @@ template <typename T, int KT, int NP, bool KEYS_ONLY> struct Ahead {
 struct StateIn {
     __amdgpu_buffer_rsrc_t r;
     unsigned bytes, pitch;
-    __device__ __forceinline__ StateIn(const float *p, int DK, int DV)
+    __device__ __forceinline__ StateIn(const float *p, int DK, int DV)      // (p: the wave's)
         : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(p), 0, DK * DV * 4, 0x00020000)), bytes(DK * DV * 4), pitch(DV * 4)
     {
     }
@@ -662,21 +660,21 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
     }
     const bool values = in && !col.unit;
     const int own = values ? h * p.DV + col.at + (lane0 & 15) : 0;
-    const T *vrow = p.v.row(b, own, p.L), *krow = p.k.row(b, hk * p.DK, p.L), *qrow = p.q.row(b, hk * p.DK, p.L);
+    const T *vrow = p.v.row(b, own, p.pitch), *krow = p.k.row(b, hk * p.DK, p.pitch), *qrow = p.q.row(b, hk * p.DK, p.pitch);
     T *orow = p.o.row(b, own, p.L);
     const DeltaPairs *pairs = p.pairs + head * p.chunks;
     Ahead<T, KT, 2, SPANS> next;
-    f32x4 val[4] = {};
-    if (from < last) next.load(p, krow, qrow, pairs + from, from * 64, n);
+    if (from < last) next.load(p, krow, qrow, vrow, pairs + from, from * 64, 4 * (lane0 >> 4));
     for (int ch = from; ch < last; ++ch) {
         const int t0 = ch * kDeltaChunk;
         const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dv = col.at + c;
         __syncthreads();
-        next.put(m, p.DK, t0, n);
-        load_rows(val, vrow, t0, g4, n, values);
+        next.put(m, p, t0, n);
+        f32x4 val[4];
+        next.rows.get(val, t0, g4, n, p.pitch);
         if (!SPANS && p.states) store_state(S, StateIn(p.states + (head * p.chunks + ch) * size, p.DK, p.DV), dv, in, g4);
         __syncthreads();
-        if (ch + 1 < last) next.load(p, krow, qrow, pairs + ch + 1, t0 + 64, n);
+        if (ch + 1 < last) next.load(p, krow, qrow, vrow, pairs + ch + 1, t0 + 64, g4);
         if (!col.active) continue;
         f32x4 r[4] = {}, w[4] = {}, o[4] = {};
 #pragma unroll
@@ -691,6 +689,7 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = 16 * i + g4;
+            if (SPANS && col.unit) val[i] = f32x4{};
             r[i] = four(m.s.beta, t) * (val[i] - four(m.s.eG, t) * four(m.s.rk, t) * r[i]);
             if (!SPANS) o[i] *= four(m.s.eG, t) * four(m.s.rq, t);
         }
@@ -765,24 +764,27 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
     }
     const bool values = in && !col.unit;
     const int own = values ? h * p.DV + col.at + (lane0 & 15) : 0;
-    const T *drow = p.dout.row(b, own, p.L), *krow = p.k.row(b, hk * p.DK, p.L), *qrow = p.q.row(b, hk * p.DK, p.L);
+    const T *drow = p.dout.row(b, own, p.pitch), *krow = p.k.row(b, hk * p.DK, p.pitch), *qrow = p.q.row(b, hk * p.DK, p.pitch);
     T *vrow = p.dv.row(b, own, p.L);
     const DeltaPairs *pairs = p.pairs + head * p.chunks;
     if (!SPANS && in)                                   // (behind the sequence's end)
         for (int t = max(last, from) * 64 + 4 * (lane0 >> 4), to = min(p.L, seg + 1 < walk.segs ? (from + walk.per) * 64 : p.L); t < to; t += 16)
             store4(vrow, f32x4{}, t, p.L);
     Ahead<T, KT, 3, false> next;
-    f32x4 d[4] = {};
-    if (from < last) next.load(p, krow, qrow, pairs + last - 1, (last - 1) * 64, n);
+    if (from < last) next.load(p, krow, qrow, drow, pairs + last - 1, (last - 1) * 64, 4 * (lane0 >> 4));
     for (int ch = last - 1; ch >= from; --ch) {
         const int t0 = ch * kDeltaChunk;
         const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dv = col.at + c;
         __syncthreads();
-        next.put(m, p.DK, t0, n);
-        load_rows(d, drow, t0, g4, n, values);
+        next.put(m, p, t0, n);
+        f32x4 d[4];
+        next.rows.get(d, t0, g4, n, p.pitch);
+        if (SPANS && col.unit)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[i] = f32x4{};
         if (!SPANS) store_state(S, StateIn(p.after + (head * p.chunks + ch) * size, p.DK, p.DV), dv, in, g4);
         __syncthreads();
-        if (ch > from) next.load(p, krow, qrow, pairs + ch - 1, t0 - 64, n);
+        if (ch > from) next.load(p, krow, qrow, drow, pairs + ch - 1, t0 - 64, g4);
         if (!col.active) continue;
         f32x4 w[4] = {}, r[4] = {};
 #pragma unroll
@@ -938,23 +940,25 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
     }
     f32x4 dq[4] = {}, dkey[4] = {};
     Tile<T, 16 * KT, 64 * W> kt;
-    kt.load(p.k.row(b, hk * p.DK, p.L), p.DK, t0, n, p.L);
+    kt.load(p.k.row(b, hk * p.DK, p.pitch), p.DK, t0, p.pitch);
+    Rows<T> qrow;
+    qrow.load(p.q.row(b, hk * p.DK + (key ? dk : 0), p.pitch), t0, g4, p.pitch);
     f32x4 q[4];                             // this wave's channels of q, as products and sums over positions take them
-    load_rows(q, p.q.row(b, hk * p.DK + (key ? dk : 0), p.L), t0, g4, n, key);
     for (int h = hk * p.each; h < (hk + 1) * p.each; ++h) {
         const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dk = 16 * wave + c;
         const long long head = (long long)b * p.H + h, at = head * p.chunks + ch;
-        const StateIn before(p.states + at * p.DK * p.DV, p.DK, p.DV), after(p.after + at * p.DK * p.DV, p.DK, p.DV);
+        const float *states = p.states + at * p.DK * p.DV, *grads = p.after + at * p.DK * p.DV;
+        const StateIn before(states, p.DK, p.DV), after(grads, p.DK, p.DV);
         const DeltaPairs &pairs = p.pairs[at];
         // w, and dr: a wave 16 columns of either.  What that takes from memory, a step ahead.
-        f32x4 S[KT], val[4], d[4];
+        f32x4 S[KT];
+        Rows<T> vrow, drow;
         const auto fetch = [&](int v0, int task) __attribute__((always_inline)) {
             const int dv = v0 + 16 * (task >> 1) + c;
             const bool in = dv < p.DV && task < 2 * NS;
-            if (task & 1) load_state(S, after, dv, in, g4);
-            else load_state(S, before, dv, in, g4);
-            load_rows(val, p.v.row(b, h * p.DV + (in ? dv : 0), p.L), t0, g4, n, in);
-            if (task & 1) load_rows(d, p.dout.row(b, h * p.DV + (in ? dv : 0), p.L), t0, g4, n, in);
+            load_state(S, StateIn(task & 1 ? grads : states, p.DK, p.DV), dv, in, g4);
+            vrow.load(p.v.row(b, h * p.DV + (in ? dv : 0), p.pitch), t0, g4, p.pitch);
+            drow.load(p.dout.row(b, h * p.DV + (in ? dv : 0), p.pitch), t0, g4, p.pitch);
         };
         {
             LowTiles<T, 3, 64 * W> t, u;
@@ -963,7 +967,13 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
             const f32x4 gates = reinterpret_cast<const f32x4 *>(&pairs.s)[threadIdx.x < sizeof(Gates) / 16 ? threadIdx.x : 0];
             fetch(0, wave);
             __syncthreads();
-            if (h == hk * p.each) kt.put(m.k, p.DK, t0, n);
+            if (h == hk * p.each) {
+                kt.put(m.k, p.DK, t0, n, p.pitch);
+                qrow.get(q, t0, g4, n, p.pitch);
+                if (!key)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) q[i] = f32x4{};
+            }
             t.put(m.t);
             u.put(m.p);
             if (threadIdx.x < sizeof(Gates) / 16) reinterpret_cast<f32x4 *>(&m.s)[threadIdx.x] = gates;
@@ -981,7 +991,12 @@ template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(co
                 const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
                 const int task = wave + job * W, sl = task >> 1, row = (16 * sl + c) * kPitch + g4;
                 if (task >= 2 * NS) break;
-                f32x4 x[4] = {}, y[4] = {};
+                f32x4 x[4] = {}, y[4] = {}, val[4], d[4];
+                vrow.get(val, t0, g4, n, p.pitch);
+                drow.get(d, t0, g4, n, p.pitch);
+                if (v0 + 16 * sl + c >= p.DV)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) val[i] = d[i] = f32x4{};
 #pragma unroll
                 for (int kb = 0; kb < KT; kb += 2) {
                     const Full s = M::split(S[kb], S[kb + 1]);
