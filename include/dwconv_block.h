@@ -164,7 +164,7 @@ DWCONV_API int dwconv_delta_bwd(dwconv_seq dout, dwconv_seq q, dwconv_seq k, dwc
 DWCONV_API int dwconv_delta_states(int L);
 
 /* Workspace of dwconv_delta_fwd (backward = 0) and dwconv_delta_bwd (backward = 1); 0 on bad arguments. */
-DWCONV_API size_t dwconv_delta_workspace_bytes(int B, int H, int DK, int DV, int L, int backward);
+DWCONV_API size_t dwconv_delta_workspace_bytes(int B, int H, int Hk, int DK, int DV, int L, int backward);
 
 /*
  * Gated delta rule, one token of every place b of the batch, on the states s [pool, H, DK, DV] fp32, which are updated in place; slots and pool

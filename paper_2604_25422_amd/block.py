@@ -68,7 +68,7 @@ def lib():
                 ("dwconv_delta_fwd", [s, s, s, s, s, vp, vp, s, vp, vp, vp, sz, i, i, i, i, i, i, f, f, i, vp], i),
                 ("dwconv_delta_bwd", [s, s, s, s, s, s, vp, vp, vp, s, s, s, vp, vp, vp, vp, sz, i, i, i, i, i, i, f, f, i, vp], i),
                 ("dwconv_delta_states", [i], i),
-                ("dwconv_delta_workspace_bytes", [i, i, i, i, i, i], sz),
+                ("dwconv_delta_workspace_bytes", [i, i, i, i, i, i, i], sz),
                 ("dwconv_delta_step", [s, s, s, s, s, vp, vp, i, s, i, i, i, i, i, f, f, i, vp], i),
                 ("dwconv_dropout", [s, s, s, vp, i, i, i, i, f, f, i, i, vp], i)):
             fn = getattr(l, name)
@@ -223,8 +223,8 @@ def delta_states(L: int) -> int:
     return int(lib().dwconv_delta_states(int(L)))
 
 
-def delta_workspace_bytes(B: int, H: int, DK: int, DV: int, L: int, backward: bool) -> int:
-    return int(lib().dwconv_delta_workspace_bytes(B, H, DK, DV, L, int(backward)))
+def delta_workspace_bytes(B: int, H: int, key_heads: int, DK: int, DV: int, L: int, backward: bool) -> int:
+    return int(lib().dwconv_delta_workspace_bytes(B, H, key_heads, DK, DV, L, int(backward)))
 
 
 def _heads(q, v, g, key_heads, dims: int):
@@ -256,7 +256,7 @@ def delta_fwd(q, k, v, g, beta, s0=None, lengths=None, key_heads=None, scale=Non
     o, os_ = _out(out, "out", values, q)
     s_last = torch.empty((B, H, DK, DV), dtype=torch.float32, device=q.device)
     states = torch.empty((B, H, delta_states(L), DK, DV), dtype=torch.float32, device=q.device) if save else None
-    ws, nbytes, keep = _workspace(workspace, delta_workspace_bytes(B, H, DK, DV, L, False), q)
+    ws, nbytes, keep = _workspace(workspace, delta_workspace_bytes(B, H, Hk, DK, DV, L, False), q)
     _check(lib().dwconv_delta_fwd(*ins, sp, lp, os_, s_last.data_ptr(), states.data_ptr() if save else None, ws, nbytes, B, H, Hk, DK, DV, L,
                                   float(scale), float(eps), code, _stream()))
     return o, s_last, states
@@ -279,7 +279,7 @@ def delta_bwd(do, q, k, v, g, beta, states, ds_last=None, lengths=None, key_head
     outs = [_out(t, n, shape, q) for t, n, shape in zip(given, ("dq", "dk", "dv"), (keys, keys, values))]
     dg, dbeta = (torch.empty((B, H, L), dtype=torch.float32, device=q.device) for _ in range(2))
     ds0 = torch.empty((B, H, DK, DV), dtype=torch.float32, device=q.device)
-    ws, nbytes, keep = _workspace(workspace, delta_workspace_bytes(B, H, DK, DV, L, True), q)
+    ws, nbytes, keep = _workspace(workspace, delta_workspace_bytes(B, H, Hk, DK, DV, L, True), q)
     _check(lib().dwconv_delta_bwd(*ins, sp, dsp, lp, *(s for _, s in outs), dg.data_ptr(), dbeta.data_ptr(), ds0.data_ptr(), ws, nbytes, B, H, Hk, DK, DV,
                                   L, float(scale), float(eps), code, _stream()))
     return outs[0][0], outs[1][0], outs[2][0], dg, dbeta, ds0

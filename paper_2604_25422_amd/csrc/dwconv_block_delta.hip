@@ -209,7 +209,7 @@ template <typename T> int launch_fwd(const DeltaFwd<T> &p, const DeltaWalk &w, h
 
 template <typename T, int KT> int launch_bwd(const DeltaBwd<T> &p, const DeltaWalk &w, hipStream_t st)
 {
-    static std::atomic<unsigned long long> done[3];
+    static std::atomic<unsigned long long> done[4];
     constexpr size_t lds = sizeof(DeltaLds<T, KT, 3>), chunk = sizeof(DeltaChunkLds<T, KT>);
     static_assert(lds <= 160 * 1024 && chunk <= 160 * 1024, "LDS of a CU");
     int rc = launch_pairs<T, KT>(p, st);
@@ -218,11 +218,12 @@ template <typename T, int KT> int launch_bwd(const DeltaBwd<T> &p, const DeltaWa
         delta_starts_kernel<KT, true><<<dim3(p.B * p.H, (unsigned)ceil_div(p.DV, 16)), 64 * KT, 0, st>>>(p.ds_last, w.spans, const_cast<float *>(w.starts), w.segs, p.DK, p.DV);
     }
     if (rc == DWCONV_OK) rc = launch_segments(delta_bwd_state_kernel<T, KT, false>, p, w, p.DV, lds, done[0], st);
-    if (rc == DWCONV_OK && !allow_lds(delta_bwd_chunk_kernel<T, KT>, chunk, done[2])) rc = DWCONV_ERR_LAUNCH;
+    const auto kernel = p.each > 1 ? delta_bwd_chunk_kernel<T, KT, true> : delta_bwd_chunk_kernel<T, KT, false>;
+    if (rc == DWCONV_OK && !allow_lds(kernel, chunk, done[p.each > 1 ? 3 : 2])) rc = DWCONV_ERR_LAUNCH;
     if (rc != DWCONV_OK) return rc;
-    const int units = p.B * (p.H / p.each) * p.chunks;
-    for (int first = 0; first < units; first += kMaxUnits)
-        delta_bwd_chunk_kernel<T, KT><<<std::min(units - first, kMaxUnits), 64 * kDeltaBwdWaves(KT), chunk, st>>>(p, first);
+    const int units = p.B * p.H * p.chunks, shared = p.each > 1 ? units / p.each : 0;
+    for (int first = 0; first < units; first += kMaxUnits) kernel<<<std::min(units - first, kMaxUnits), 64 * kGradWaves, chunk, st>>>(p, first);
+    for (int first = 0; first < shared; first += kMaxUnits) delta_share_kernel<T><<<std::min(shared - first, kMaxUnits), 256, 0, st>>>(p, first);
     return launch_status();
 }
 template <typename T> int launch_bwd(const DeltaBwd<T> &p, const DeltaWalk &w, hipStream_t st)
@@ -282,6 +283,7 @@ template <typename T> void pad_all(DeltaShape<T> &p, Seq<T> *dout, void *room, h
     p.pitch = kPadded;
 }
 size_t after_bytes(int B, int H, int DK, int DV, int L) { return up16((size_t)B * H * chunks_of(L) * DK * DV * sizeof(float)); }
+size_t part_bytes(int B, int H, int DK, int L, bool shared) { return shared ? up16((size_t)B * H * 2 * DK * L * sizeof(float)) : 0; }
 DeltaWalk walk_in(void *workspace, int B, int H, int DK, int DV, int L)
 {
     const WalkPlan w = plan_walk(B, H, DK, DV, L);
@@ -295,10 +297,10 @@ extern "C" {
 
 int dwconv_delta_states(int L) { return L < 1 || L > (1 << 30) ? 0 : chunks_of(L); }
 
-size_t dwconv_delta_workspace_bytes(int B, int H, int DK, int DV, int L, int backward)
+size_t dwconv_delta_workspace_bytes(int B, int H, int Hk, int DK, int DV, int L, int backward)
 {
-    if (check_heads(B, H, H, DK, DV, L) != DWCONV_OK) return 0;
-    return pairs_bytes(B, H, L) + padded_bytes(B, H, DK, DV, L) + walk_bytes(B, H, DK, DV, L) + (backward ? after_bytes(B, H, DK, DV, L) : 0);
+    if (check_heads(B, H, Hk, DK, DV, L) != DWCONV_OK) return 0;
+    return pairs_bytes(B, H, L) + padded_bytes(B, H, DK, DV, L) + walk_bytes(B, H, DK, DV, L) + (backward ? after_bytes(B, H, DK, DV, L) + part_bytes(B, H, DK, L, Hk < H) : 0);
 }
 
 int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const float *s0, const int *lengths, dwconv_seq_out o,
@@ -318,7 +320,7 @@ int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwc
     if ((rc = check_out(o, es, B, H * DV, L)) != DWCONV_OK) return rc;
     for (const void *t : {(const void *)s0, (const void *)lengths, (const void *)s_last, (const void *)states})
         if (!f32_ok(t)) return DWCONV_ERR_ALIGN;
-    if (!workspace || workspace_bytes < dwconv_delta_workspace_bytes(B, H, DK, DV, L, 0) || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < dwconv_delta_workspace_bytes(B, H, Hk, DK, DV, L, 0) || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const DeltaWalk walk = walk_in(workspace, B, H, DK, DV, L);
     void *room = static_cast<char *>(workspace) + pairs_bytes(B, H, L);
@@ -352,20 +354,21 @@ int dwconv_delta_bwd(dwconv_seq dout, dwconv_seq q, dwconv_seq k, dwconv_seq v, 
     if ((rc = check_out(dv, es, B, H * DV, L)) != DWCONV_OK) return rc;
     for (const void *t : {(const void *)states, (const void *)ds_last, (const void *)lengths, (const void *)dg, (const void *)dbeta, (const void *)ds0})
         if (!f32_ok(t)) return DWCONV_ERR_ALIGN;
-    const size_t need = dwconv_delta_workspace_bytes(B, H, DK, DV, L, 1);
+    const size_t need = dwconv_delta_workspace_bytes(B, H, Hk, DK, DV, L, 1);
     if (!workspace || workspace_bytes < need || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const DeltaWalk walk = walk_in(workspace, B, H, DK, DV, L);
     float *after = reinterpret_cast<float *>(static_cast<char *>(workspace) + pairs_bytes(B, H, L) + padded_bytes(B, H, DK, DV, L) + walk_bytes(B, H, DK, DV, L));
     void *room = static_cast<char *>(workspace) + pairs_bytes(B, H, L);
+    float *part = reinterpret_cast<float *>(reinterpret_cast<char *>(after) + after_bytes(B, H, DK, DV, L));
     if (dtype == DWCONV_F32) {
         DeltaBwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<float>(dout), seq<float>(dq), seq<float>(dk),
-                          seq<float>(dv), states, ds_last, after, dg, dbeta, ds0};
+                          seq<float>(dv), states, ds_last, after, dg, dbeta, ds0, part};
         pad_all<float>(p, &p.dout, room, st);
         return launch_bwd(p, walk, st);
     }
     DeltaBwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<bf16_t>(dout), seq<bf16_t>(dq), seq<bf16_t>(dk),
-                       seq<bf16_t>(dv), states, ds_last, after, dg, dbeta, ds0};
+                       seq<bf16_t>(dv), states, ds_last, after, dg, dbeta, ds0, part};
     pad_all<bf16_t>(p, &p.dout, room, st);
     return launch_bwd(p, walk, st);
 }

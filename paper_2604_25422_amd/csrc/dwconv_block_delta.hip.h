@@ -52,6 +52,7 @@ template <typename T> struct DeltaBwd : DeltaShape<T> {
     SeqOut<T> dq, dk, dv;
     const float *states, *ds_last;
     float *after, *dg, *dbeta, *ds0;    // after: [B, H, chunks, DK, DV], the gradient of the state behind a chunk
+    float *part;                        // [B, H, 2, DK, L]: of shared keys, what each head adds to dq and dk
 };
 
 // The per-position values of a chunk.
@@ -892,7 +893,21 @@ __device__ __forceinline__ f32x4 sum16(f32x4 x)
     return x;
 }
 
-constexpr int kDeltaBwdWaves(int KT) { return KT < 4 ? 4 : KT; }
+// x[tile0 + ii] of a wave's tile0, which of KT = 8 is 0, of 4 one of two values, of 2 one of four.
+template <int KT> __device__ __forceinline__ f32x4 pick(const f32x4 (&x)[4], int ii, int tile0)
+{
+    f32x4 r = x[ii];
+    if constexpr (KT == 4) {
+        if (tile0 == 2) r = x[2 + ii];
+    } else if constexpr (KT == 2) {
+        if (tile0 == 1) r = x[1];
+        if (tile0 == 2) r = x[2];
+        if (tile0 == 3) r = x[3];
+    }
+    return r;
+}
+
+constexpr int kGradWaves = 8;           // of a workgroup
 
 template <typename T, int KT> struct DeltaChunkLds {
     typedef typename Mat<T>::Elem Elem;
@@ -905,7 +920,7 @@ template <typename T, int KT> struct DeltaChunkLds {
         float pairs[64 * kPitch];
     };
     Gates s;
-    float part[3][8][64], db[VB / 16][64], da[4][64], dg[4][64], whole[8];
+    float part[3][KT][64], db[VB / 16][64], da[4][64], dg[4][64], whole[KT];
 };
 
 // Backward, within a chunk, all chunks at once: from the states in front of it and the gradient of that behind it
@@ -914,356 +929,396 @@ template <typename T, int KT> struct DeltaChunkLds {
 // A decay at t scales what lies in front of it for what lies from it on: with W = dP P + dA A
 //     dg_t = exp(G_63) <dS, S> + sum_{i >= t} x_i + sum_{j < t} y_j + sum_{i >= t > j} W_ij,
 // x_i what row i took of S and y_j what is left of column j in S'.  (As a difference of whole sums, which is shorter, it would be
-// the rounding of those where a decay is strong.)  A workgroup has a chunk of a head of keys and adds up the heads that share it, in order.
-template <typename T, int KT> __device__ __forceinline__ void delta_bwd_chunk(const DeltaBwd<T> &p, DeltaChunkLds<T, KT> &m, int unit)
+// the rounding of those where a decay is strong.)  A workgroup has a chunk of a head.  First 16 columns of w or dr a wave, then 16 channels of the key
+// and NI of the four tiles of 16 positions.  SHARED: dq and dk of q and k of unit length go to part_q and part_k, which delta_share_kernel adds up.
+template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta_bwd_chunk(const DeltaBwd<T> &p, DeltaChunkLds<T, KT> &m, int unit)
 {
     typedef Mat<T> M;
     typedef typename M::Full Full;
     typedef DeltaChunkLds<T, KT> Lds;
-    constexpr int W = kDeltaBwdWaves(KT), VB = Lds::VB, NS = VB / 16, NT = (10 + W - 1) / W, NJ = (2 * NS + W - 1) / W, VP = VB * kPitch;
-    const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane0 & 15, g4 = 4 * (lane0 >> 4);
-    const int ch = unit % p.chunks, bk = unit / p.chunks, Hk = p.H / p.each, b = bk / Hk, hk = bk % Hk;
-    const int n = p.length(b), t0 = ch * kDeltaChunk, dk = 16 * wave + c;
-    const bool keys = wave < KT, key = keys && dk < p.DK;
+    constexpr int W = kGradWaves, VB = Lds::VB, NS = VB / 16, VP = VB * kPitch, NI = KT / 2;
+    const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int ch = unit % p.chunks, head = unit / p.chunks, b = head / p.H, h = head % p.H, hk = h / p.each;
+    const int n = p.length(b), t0 = ch * kDeltaChunk;
+    const int slice = wave % KT, tile0 = wave / KT * NI;            // this wave's channels of the key, and tiles of positions
+    T *const dq_row = SHARED ? nullptr : p.dq.row(b, hk * p.DK, p.L), *const dk_row = SHARED ? nullptr : p.dk.row(b, hk * p.DK, p.L);
+    float *const part_q = p.part + ((long long)head * 2 * p.DK) * p.L, *const part_k = part_q + (long long)p.DK * p.L;
     if (t0 >= n) {
-        for (int h = hk * p.each; h < (hk + 1) * p.each; ++h) {
-            const long long at = ((long long)b * p.H + h) * p.L + t0 + threadIdx.x;
-            if (threadIdx.x < 64 && t0 + threadIdx.x < p.L) p.dg[at] = p.dbeta[at] = 0.0f;
-        }
-        if (key)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                store4(p.dq.row(b, hk * p.DK + dk, p.L), f32x4{}, t0 + 16 * i + g4, p.L);
-                store4(p.dk.row(b, hk * p.DK + dk, p.L), f32x4{}, t0 + 16 * i + g4, p.L);
-            }
+        if (threadIdx.x < 64 && t0 + (int)threadIdx.x < p.L) p.dg[(long long)head * p.L + t0 + threadIdx.x] = p.dbeta[(long long)head * p.L + t0 + threadIdx.x] = 0.0f;
+        if (!SHARED)
+            for (int i = threadIdx.x; i < 64 * p.DK; i += 64 * W)
+                if (t0 + (i & 63) < p.L) dq_row[(long long)(i >> 6) * p.L + t0 + (i & 63)] = dk_row[(long long)(i >> 6) * p.L + t0 + (i & 63)] = T{};
         return;
     }
-    f32x4 dq[4] = {}, dkey[4] = {};
-    Tile<T, 16 * KT, 64 * W> kt;
-    kt.load(p.k.row(b, hk * p.DK, p.pitch), p.DK, t0, p.pitch);
-    Rows<T> qrow;
-    qrow.load(p.q.row(b, hk * p.DK + (key ? dk : 0), p.pitch), t0, g4, p.pitch);
-    f32x4 q[4];                             // this wave's channels of q, as products and sums over positions take them
-    for (int h = hk * p.each; h < (hk + 1) * p.each; ++h) {
-        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dk = 16 * wave + c;
-        const long long head = (long long)b * p.H + h, at = head * p.chunks + ch;
-        const float *states = p.states + at * p.DK * p.DV, *grads = p.after + at * p.DK * p.DV;
-        const StateIn before(states, p.DK, p.DV), after(grads, p.DK, p.DV);
-        const DeltaPairs &pairs = p.pairs[at];
-        // w, and dr: a wave 16 columns of either.  What that takes from memory, a step ahead.
-        f32x4 S[KT];
-        Rows<T> vrow, drow;
-        const auto fetch = [&](int v0, int task) __attribute__((always_inline)) {
-            const int dv = v0 + 16 * (task >> 1) + c;
-            const bool in = dv < p.DV && task < 2 * NS;
-            load_state(S, StateIn(task & 1 ? grads : states, p.DK, p.DV), dv, in, g4);
-            vrow.load(p.v.row(b, h * p.DV + (in ? dv : 0), p.pitch), t0, g4, p.pitch);
-            drow.load(p.dout.row(b, h * p.DV + (in ? dv : 0), p.pitch), t0, g4, p.pitch);
-        };
-        {
-            LowTiles<T, 3, 64 * W> t, u;
-            t.load(pairs.t);
-            u.load(pairs.p);
-            const f32x4 gates = reinterpret_cast<const f32x4 *>(&pairs.s)[threadIdx.x < sizeof(Gates) / 16 ? threadIdx.x : 0];
-            fetch(0, wave);
-            __syncthreads();
-            if (h == hk * p.each) {
-                kt.put(m.k, p.DK, t0, n, p.pitch);
-                qrow.get(q, t0, g4, n, p.pitch);
-                if (!key)
+    const float *states = p.states + (long long)unit * p.DK * p.DV, *grads = p.after + (long long)unit * p.DK * p.DV;
+    const StateIn before(states, p.DK, p.DV), after(grads, p.DK, p.DV);
+    const DeltaPairs &pairs = p.pairs[unit];
+    const T *const values = p.v.row(b, h * p.DV, p.pitch), *const douts = p.dout.row(b, h * p.DV, p.pitch);
+    // What w and dr take from memory, a step ahead: an even wave has 16 columns of w, an odd one of dr.
+    f32x4 S[KT];
+    Rows<T> vrow, drow;
+    const auto fetch = [&](int v0) __attribute__((always_inline)) {
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dv = v0 + 16 * (wave >> 1) + c;
+        const bool in = dv < p.DV && wave < 2 * NS;
+        load_state(S, StateIn(wave & 1 ? grads : states, p.DK, p.DV), dv, in, g4);
+        vrow.load(values + (long long)(in ? dv : 0) * p.pitch, t0, g4, p.pitch);
+        drow.load(douts + (long long)(in ? dv : 0) * p.pitch, t0, g4, p.pitch);
+    };
+    {
+        Tile<T, 16 * KT, 64 * W> kt;
+        LowTiles<T, 3, 64 * W> t, u;
+        kt.load(p.k.row(b, hk * p.DK, p.pitch), p.DK, t0, p.pitch);
+        t.load(pairs.t);
+        u.load(pairs.p);
+        const f32x4 gates = reinterpret_cast<const f32x4 *>(&pairs.s)[threadIdx.x < sizeof(Gates) / 16 ? threadIdx.x : 0];
+        fetch(0);
+        kt.put(m.k, p.DK, t0, n, p.pitch);
+        t.put(m.t);
+        u.put(m.p);
+        if (threadIdx.x < sizeof(Gates) / 16) reinterpret_cast<f32x4 *>(&m.s)[threadIdx.x] = gates;
+        if (threadIdx.x < NS * 64) m.db[0][threadIdx.x] = 0.0f;
+    }
+    __syncthreads();
+    f32x4 dp[2] = {}, da[2] = {};           // of this wave's tiles of pairs, transposed: lane (c, g) has columns 16 tj + 4 g + v of row 16 ti + c
+    f32x4 x1[NI] = {}, x2[NI] = {}, x3[NI] = {};    // do S^T, dr S^T, w dS^T: rows of positions, 16 channels of the key
+    float whole = 0.0f;
+#pragma unroll 1
+    for (int v0 = 0; v0 < p.DV; v0 += VB) {
+        if (wave < 2 * NS) {
+            const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), sl = wave >> 1, row = (16 * sl + c) * kPitch + g4;
+            f32x4 x[4] = {}, y[4] = {};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) q[i] = f32x4{};
+            for (int kb = 0; kb < KT; kb += 2) {
+                const Full s = M::split(S[kb], S[kb + 1]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = M::mma(M::columns_in(m.k, 16 * i, 16 * kb, lane), s, x[i]);
+                step_done();
             }
-            t.put(m.t);
-            u.put(m.p);
-            if (threadIdx.x < sizeof(Gates) / 16) reinterpret_cast<f32x4 *>(&m.s)[threadIdx.x] = gates;
-            for (int i = threadIdx.x; i < NS * 64; i += 64 * W) m.db[0][i] = 0.0f;
-        }
-        __syncthreads();
-        f32x4 dp[NT] = {}, da[NT] = {};             // of this wave's tiles, transposed: lane (c, g) has columns 16 tj + 4 g + v of row 16 ti + c
-        f32x4 x1[4] = {}, x2[4] = {}, x3[4] = {};   // do S^T, dr S^T, w dS^T: rows of positions, 16 channels of the key
-        f32x4 kk[NT], pp[NT];
-        float whole = 0.0f;
-        for (int v0 = 0; v0 < p.DV; v0 += VB) {
-            const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dk = 16 * wave + c;
-#pragma unroll
-            for (int job = 0; job < NJ; ++job) {
-                const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
-                const int task = wave + job * W, sl = task >> 1, row = (16 * sl + c) * kPitch + g4;
-                if (task >= 2 * NS) break;
-                f32x4 x[4] = {}, y[4] = {}, val[4], d[4];
-                vrow.get(val, t0, g4, n, p.pitch);
+            const bool out = v0 + 16 * sl + c >= p.DV;
+            if (wave & 1) {
+                f32x4 d[4];
                 drow.get(d, t0, g4, n, p.pitch);
-                if (v0 + 16 * sl + c >= p.DV)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) val[i] = d[i] = f32x4{};
-#pragma unroll
-                for (int kb = 0; kb < KT; kb += 2) {
-                    const Full s = M::split(S[kb], S[kb + 1]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = M::mma(M::columns_in(m.k, 16 * i, 16 * kb, lane), s, x[i]);
-                    step_done();
-                }
-                if (task & 1) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        x[i] *= four(m.s.eC, 16 * i + g4) * four(m.s.rk, 16 * i + g4);
-                        M::template put<1>(m.dout, 0, row + 16 * i, d[i]);
-                    }
-#pragma unroll
-                    for (int kb = 0; kb < 2; ++kb) {
-                        const typename M::In z = M::exact(d[2 * kb], d[2 * kb + 1]);
-#pragma unroll
-                        for (int j = 0; j < 2 * kb + 2; ++j) x[j] = M::mma(M::low_columns(m.p, 16 * j, kb, lane), z, x[j]);
-                        step_done();
-                    }
-#pragma unroll
-                    for (int kb = 0; kb < 2; ++kb) {
-                        const Full z = M::split(x[2 * kb], x[2 * kb + 1]);
-#pragma unroll
-                        for (int j = 0; j < 2 * kb + 2; ++j) y[j] = M::mma(M::low_columns(m.t, 16 * j, kb, lane), z, y[j]);
-                        step_done();
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        M::put(m.dr, VP, row + 16 * i, y[i]);
-                        const f32x4 s = sum16(y[i] * val[i]);
-                        if (c == 0) *reinterpret_cast<f32x4 *>(&m.db[sl][16 * i + g4]) += s;
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int t = 16 * i + g4;
-                        x[i] = four(m.s.beta, t) * (val[i] - four(m.s.eG, t) * four(m.s.rk, t) * x[i]);
-                    }
-#pragma unroll
-                    for (int kb = 0; kb < 2; ++kb) {
-                        const Full z = M::split(x[2 * kb], x[2 * kb + 1]);
-#pragma unroll
-                        for (int i = 2 * kb; i < 4; ++i) y[i] = M::mma(M::low_rows(m.t, 16 * i, kb, lane), z, y[i]);
-                        step_done();
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) M::put(m.w, VP, row + 16 * i, y[i]);
-                }
-                if (job + 1 < NJ) fetch(v0, task + W);
-            }
-            if (v0 + VB < p.DV) {
-                fetch(v0 + VB, wave);
-            } else {
-#pragma unroll
-                for (int u = 0; u < NT; ++u) {
-                    const int task = min(wave + u * W, 9);
-                    kk[u] = four(pairs.kk[task], 16 * c + g4), pp[u] = four(pairs.p[task], 16 * c + g4);
-                }
-            }
-            f32x4 a[VB / 16], e[VB / 16];
-            if (keys)
-#pragma unroll
-                for (int kb = 0; kb < VB / 16; ++kb) {
-                    const int col = v0 + 16 * kb + g4;
-                    a[kb] = before.four(dk, col, p.DV), e[kb] = after.four(dk, col, p.DV);
-                }
-            __syncthreads();
-#pragma unroll
-            for (int u = 0; u < NT; ++u) {
-                const int task = wave + u * W;
-                if (task >= 10) continue;
-                const int lane = fresh(lane0);
-                int ti, tj;
-                low_tile(task, ti, tj);
-#pragma unroll
-                for (int kb = 0; kb < VB; kb += 32) {
-                    const Full wj = M::columns(m.w, VP, 16 * tj, kb, lane);
-                    dp[u] = M::mma(wj, M::columns_in(m.dout, 16 * ti, kb, lane), dp[u]);
-                    da[u] = M::mma(wj, M::columns(m.dr, VP, 16 * ti, kb, lane), da[u]);
-                    step_done();
-                }
-            }
-            if (keys)
-#pragma unroll
-                for (int kb = 0; kb < VB / 16; kb += 2) {
-                    const int lane = fresh(lane0);
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) whole = fmaf(a[kb][v], e[kb][v], whole), whole = fmaf(a[kb + 1][v], e[kb + 1][v], whole);
-                    const Full s0 = M::split(a[kb], a[kb + 1]), s1 = M::split(e[kb], e[kb + 1]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        x1[i] = M::mma(M::columns_in(m.dout, 16 * i, 16 * kb, lane), s0, x1[i]);
-                        x2[i] = M::mma(M::columns(m.dr, VP, 16 * i, 16 * kb, lane), s0, x2[i]);
-                        x3[i] = M::mma(M::columns(m.w, VP, 16 * i, 16 * kb, lane), s1, x3[i]);
-                        step_done();
-                    }
-                }
-            __syncthreads();
-        }
-        // the pairs' gradients, in the place of the pairs
-#pragma unroll
-        for (int u = 0; u < NT; ++u) {
-            const int task = wave + u * W;
-            if (task >= 10) continue;
-            const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
-            int ti, tj;
-            low_tile(task, ti, tj);
-            const int i = 16 * ti + c, j = 16 * tj + g4;
-            f32x4 dA = -da[u], dP = dp[u], e;
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                dA[v] = j + v < i ? dA[v] : 0.0f;
-                dP[v] = j + v <= i ? dP[v] : 0.0f;
-                e[v] = j + v <= i ? exp2_of(m.s.G[i] - m.s.G[j + v]) : 0.0f;
-            }
-            const f32x4 x = dA * kk[u];
-            float sum = (x[0] + x[1]) + (x[2] + x[3]);
-            sum += __shfl_xor(sum, 16, 64);
-            sum += __shfl_xor(sum, 32, 64);
-            if (lane < 16) m.da[tj][i] = sum;
-            M::template put<2>(m.p, kLow, low_at(i, j), dP * e);
-            M::template put<2>(m.t, kLow, low_at(i, j), dA * e * m.s.beta[i]);
-            *reinterpret_cast<f32x4 *>(m.pairs + i * kPitch + j) = dP * pp[u] + x * m.s.beta[i];
-        }
-        f32x4 kh[4], qh[4];
-        if (keys) {
-            const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
-            const int dk = 16 * wave + c;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = 16 * i + g4;
-                const f32x4 beta = four(m.s.beta, t);
-                kh[i] = M::wide(m.k, dk * kPitch + t) * four(m.s.rk, t), qh[i] = q[i] * four(m.s.rq, t);
-                x1[i] *= four(m.s.eG, t);
-                x2[i] *= -four(m.s.eG, t);
-                x3[i] *= four(m.s.eC, t);
-                const f32x4 bx = kh[i] * x2[i], xs = sum16(qh[i] * x1[i] + beta * bx), ys = sum16(kh[i] * x3[i]), bs = sum16(bx);
-                if (c == 0) {
-                    *reinterpret_cast<f32x4 *>(&m.part[0][wave][t]) = xs;
-                    *reinterpret_cast<f32x4 *>(&m.part[1][wave][t]) = ys;
-                    *reinterpret_cast<f32x4 *>(&m.part[2][wave][t]) = bs;
-                }
-                dq[i] += x1[i];
-                dkey[i] += beta * x2[i] + x3[i];
-            }
-            whole = group_sum(whole, 6);
-            if (lane == 0) m.whole[wave] = whole;
-        }
-        __syncthreads();
-        // pairs of a row from t on and a column before t: products with ones above the diagonal, then the rows from t on, a tile a wave
-        for (int task = W - 1 - wave; task < 10; task += W) {
-            const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
-            int ti, tt;
-            low_tile(task, ti, tt);
-            f32x4 x = {};
-            for (int j = 0; j <= tt; ++j) {
-                f32x4 ones;
-#pragma unroll
-                for (int v = 0; v < 4; ++v) ones[v] = 16 * j + g4 + v < 16 * tt + c ? 1.0f : 0.0f;
-                x = mma16(rows_of(m.pairs, 16 * ti, 16 * j, lane), ones, x);
-            }
-            float sum = 0.0f;
-#pragma unroll
-            for (int v = 0; v < 4; ++v) sum += 16 * ti + g4 + v >= 16 * tt + c ? x[v] : 0.0f;
-            sum += __shfl_xor(sum, 16, 64);
-            sum += __shfl_xor(sum, 32, 64);
-            if (lane < 16) m.dg[ti][16 * tt + c] = sum;
-        }
-        if (keys) {
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                const int lane = fresh(lane0);
-                const Full kz = M::template split<2>(kh[2 * kb], kh[2 * kb + 1]), qz = M::template split<2>(qh[2 * kb], qh[2 * kb + 1]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    if (2 * kb <= i) {
-                        dq[i] = M::template mma<2>(M::template low_rows<2>(m.p, 16 * i, kb, lane), kz, dq[i]);
-                        dkey[i] = M::template mma<2>(M::template low_rows<2>(m.t, 16 * i, kb, lane), kz, dkey[i]);
-                    }
-                    if (i < 2 * kb + 2) {
-                        dkey[i] = M::template mma<2>(M::template low_columns<2>(m.p, 16 * i, kb, lane), qz, dkey[i]);
-                        dkey[i] = M::template mma<2>(M::template low_columns<2>(m.t, 16 * i, kb, lane), kz, dkey[i]);
-                    }
+                    if (out) d[i] = f32x4{};
+                    x[i] *= four(m.s.eC, 16 * i + g4) * four(m.s.rk, 16 * i + g4);
+                    M::template put<1>(m.dout, 0, row + 16 * i, d[i]);
+                }
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const typename M::In z = M::exact(d[2 * kb], d[2 * kb + 1]);
+#pragma unroll
+                    for (int j = 0; j < 2 * kb + 2; ++j) x[j] = M::mma(M::low_columns(m.p, 16 * j, kb, lane), z, x[j]);
+                    step_done();
+                }
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const Full z = M::split(x[2 * kb], x[2 * kb + 1]);
+#pragma unroll
+                    for (int j = 0; j < 2 * kb + 2; ++j) y[j] = M::mma(M::low_columns(m.t, 16 * j, kb, lane), z, y[j]);
+                    step_done();
+                }
+                f32x4 val[4];
+                vrow.get(val, t0, g4, n, p.pitch);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    M::put(m.dr, VP, row + 16 * i, y[i]);
+                    if (out) val[i] = f32x4{};
+                    const f32x4 s = sum16(y[i] * val[i]);
+                    if (c == 0) *reinterpret_cast<f32x4 *>(&m.db[sl][16 * i + g4]) += s;
+                }
+            } else {
+                f32x4 val[4];
+                vrow.get(val, t0, g4, n, p.pitch);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int t = 16 * i + g4;
+                    if (out) val[i] = f32x4{};
+                    x[i] = four(m.s.beta, t) * (val[i] - four(m.s.eG, t) * four(m.s.rk, t) * x[i]);
+                }
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const Full z = M::split(x[2 * kb], x[2 * kb + 1]);
+#pragma unroll
+                    for (int i = 2 * kb; i < 4; ++i) y[i] = M::mma(M::low_rows(m.t, 16 * i, kb, lane), z, y[i]);
+                    step_done();
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) M::put(m.w, VP, row + 16 * i, y[i]);
+            }
+        }
+        {
+            const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dk = 16 * slice + c;
+            f32x4 a[VB / 16], e[VB / 16];
+#pragma unroll
+            for (int kb = 0; kb < VB / 16; ++kb) a[kb] = before.four(dk, v0 + 16 * kb + g4, p.DV), e[kb] = after.four(dk, v0 + 16 * kb + g4, p.DV);
+            __syncthreads();
+#pragma unroll
+            for (int kb = 0; kb < VB / 16; kb += 2) {
+                const int lane = fresh(lane0);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) whole = fmaf(a[kb][v], e[kb][v], whole), whole = fmaf(a[kb + 1][v], e[kb + 1][v], whole);
+                const Full s0 = M::split(a[kb], a[kb + 1]), s1 = M::split(e[kb], e[kb + 1]);
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    const int ti = 16 * (tile0 + i);
+                    x1[i] = M::mma(M::columns_in(m.dout, ti, 16 * kb, lane), s0, x1[i]);
+                    x2[i] = M::mma(M::columns(m.dr, VP, ti, 16 * kb, lane), s0, x2[i]);
+                    x3[i] = M::mma(M::columns(m.w, VP, ti, 16 * kb, lane), s1, x3[i]);
                     step_done();
                 }
             }
         }
-        __syncthreads();
-        if (wave == W - 1) {
-            const int t = fresh(lane0);
-            float x = 0.0f, y = 0.0f, bsum = 0.0f, below = 0.0f, all = 0.0f;
+        if (v0 + VB < p.DV) fetch(v0 + VB);
 #pragma unroll
-            for (int u = 0; u < KT; ++u) x += m.part[0][u][t], y += m.part[1][u][t], bsum += m.part[2][u][t], all += m.whole[u];
+        for (int u = 0; u < 2; ++u) {
+            const int task = wave + u * W;
+            if (task >= 10) continue;
+            const int lane = fresh(lane0);
+            int ti, tj;
+            low_tile(task, ti, tj);
 #pragma unroll
-            for (int s = 0; s < NS; ++s) bsum += m.db[s][t];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float u = m.da[j][t], w = m.dg[j][t];
-                bsum += j <= (t >> 4) ? u : 0.0f;
-                below += j >= (t >> 4) ? w : 0.0f;
-            }
-            // (the derivative of a decay that is 0 in 32 bits is that)
-            const double G = m.s.G[t], G1 = __shfl_up(G, 1, 64);
-            const bool dead = G - (t ? G1 : 0.0) < -104.0 * 1.4426950408889634;
-#pragma unroll
-            for (int s = 1; s < 64; s *= 2) {
-                const float up = __shfl_down(x, s, 64), down = __shfl_up(y, s, 64);
-                if (t + s < 64) x += up;
-                if (t >= s) y += down;
-            }
-            const float left = __shfl_up(y, 1, 64);
-            const float sum = (m.s.eG[63] * all + x) + ((t > 0 ? left : 0.0f) + below);
-            if (t0 + t < p.L) {
-                p.dg[head * p.L + t0 + t] = t0 + t < n && !dead ? sum : 0.0f;
-                p.dbeta[head * p.L + t0 + t] = t0 + t < n ? bsum : 0.0f;
+            for (int kb = 0; kb < VB; kb += 32) {
+                const Full wj = M::columns(m.w, VP, 16 * tj, kb, lane);
+                dp[u] = M::mma(wj, M::columns_in(m.dout, 16 * ti, kb, lane), dp[u]);
+                da[u] = M::mma(wj, M::columns(m.dr, VP, 16 * ti, kb, lane), da[u]);
+                step_done();
             }
         }
-    }
-    if (p.eps > 0.0f) {             // through x / |x|: what lies along x does not change it
-        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
-        const int dk = 16 * wave + c;
-        f32x4 kh[4], qh[4];
         __syncthreads();
-        if (keys)
+    }
+    // (what the ends take from memory)
+    Rows<T> qrow;
+    f32x4 kk[2], pp[2];
+    {
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dk = 16 * slice + c;
+        qrow.load(p.q.row(b, hk * p.DK + (dk < p.DK ? dk : 0), p.pitch), t0, g4, p.pitch);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = 16 * i + g4;
-                qh[i] = q[i] * four(m.s.iq, t), kh[i] = M::wide(m.k, dk * kPitch + t) * four(m.s.rk, t);
-                const f32x4 a = sum16(qh[i] * dq[i]), e = sum16(kh[i] * dkey[i]);
-                if (c == 0) {
-                    *reinterpret_cast<f32x4 *>(&m.part[0][wave][t]) = a;
-                    *reinterpret_cast<f32x4 *>(&m.part[1][wave][t]) = e;
-                }
+        for (int u = 0; u < 2; ++u) {
+            const int task = min(wave + u * W, 9);
+            kk[u] = four(pairs.kk[task], 16 * c + g4), pp[u] = four(pairs.p[task], 16 * c + g4);
+        }
+    }
+    f32x4 kh[4], qh[4];
+    {
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dk = 16 * slice + c;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kh[i] = M::wide(m.k, dk * kPitch + 16 * i + g4) * four(m.s.rk, 16 * i + g4);
+        qrow.get(qh, t0, g4, n, p.pitch);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            qh[i] *= four(m.s.rq, 16 * i + g4);
+            if (dk >= p.DK) qh[i] = f32x4{};
+        }
+#pragma unroll
+        for (int ii = 0; ii < NI; ++ii) {
+            const int i = tile0 + ii, t = 16 * i + g4;
+            const f32x4 beta = four(m.s.beta, t), k = pick<KT>(kh, ii, tile0), q = pick<KT>(qh, ii, tile0);
+            x1[ii] *= four(m.s.eG, t);
+            x2[ii] *= -four(m.s.eG, t);
+            x3[ii] *= four(m.s.eC, t);
+            const f32x4 bx = k * x2[ii], xs = sum16(q * x1[ii] + beta * bx), ys = sum16(k * x3[ii]), bs = sum16(bx);
+            if (c == 0) {
+                *reinterpret_cast<f32x4 *>(&m.part[0][slice][t]) = xs;
+                *reinterpret_cast<f32x4 *>(&m.part[1][slice][t]) = ys;
+                *reinterpret_cast<f32x4 *>(&m.part[2][slice][t]) = bs;
+            }
+            x2[ii] = beta * x2[ii] + x3[ii];        // from here on: x1 is dq, x2 is dk
+        }
+        whole = group_sum(whole, 6);
+        if (lane == 0 && wave < KT) m.whole[slice] = whole;
+    }
+    // the pairs' gradients, in the place of the pairs
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int task = wave + u * W;
+        if (task >= 10) continue;
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
+        int ti, tj;
+        low_tile(task, ti, tj);
+        const int i = 16 * ti + c, j = 16 * tj + g4;
+        f32x4 dA = -da[u], dP = dp[u], e;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            dA[v] = j + v < i ? dA[v] : 0.0f;
+            dP[v] = j + v <= i ? dP[v] : 0.0f;
+            e[v] = j + v <= i ? exp2_of(m.s.G[i] - m.s.G[j + v]) : 0.0f;
+        }
+        const f32x4 x = dA * kk[u];
+        float sum = (x[0] + x[1]) + (x[2] + x[3]);
+        sum += __shfl_xor(sum, 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
+        if (lane < 16) m.da[tj][i] = sum;
+        M::template put<2>(m.p, kLow, low_at(i, j), dP * e);
+        M::template put<2>(m.t, kLow, low_at(i, j), dA * e * m.s.beta[i]);
+        *reinterpret_cast<f32x4 *>(m.pairs + i * kPitch + j) = dP * pp[u] + x * m.s.beta[i];
+    }
+    __syncthreads();
+    // pairs of a row from t on and a column before t: products with ones above the diagonal, then the rows from t on, a tile a wave
+    for (int task = W - 1 - wave; task < 10; task += W) {
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
+        int ti, tt;
+        low_tile(task, ti, tt);
+        f32x4 x = {};
+        for (int j = 0; j <= tt; ++j) {
+            f32x4 ones;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) ones[v] = 16 * j + g4 + v < 16 * tt + c ? 1.0f : 0.0f;
+            x = mma16(rows_of(m.pairs, 16 * ti, 16 * j, lane), ones, x);
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) sum += 16 * ti + g4 + v >= 16 * tt + c ? x[v] : 0.0f;
+        sum += __shfl_xor(sum, 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
+        if (lane < 16) m.dg[ti][16 * tt + c] = sum;
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+        const int lane = fresh(lane0);
+        const Full kz = M::template split<2>(kh[2 * kb], kh[2 * kb + 1]), qz = M::template split<2>(qh[2 * kb], qh[2 * kb + 1]);
+#pragma unroll
+        for (int ii = 0; ii < NI; ++ii) {
+            const int i = tile0 + ii;
+            if (2 * kb <= i) {
+                x1[ii] = M::template mma<2>(M::template low_rows<2>(m.p, 16 * i, kb, lane), kz, x1[ii]);
+                x2[ii] = M::template mma<2>(M::template low_rows<2>(m.t, 16 * i, kb, lane), kz, x2[ii]);
+            }
+            if (i < 2 * kb + 2) {
+                x2[ii] = M::template mma<2>(M::template low_columns<2>(m.p, 16 * i, kb, lane), qz, x2[ii]);
+                x2[ii] = M::template mma<2>(M::template low_columns<2>(m.t, 16 * i, kb, lane), kz, x2[ii]);
+            }
+            step_done();
+        }
+    }
+    // through x / |x|: what lies along x does not change it (qh is scale times the unit vector: scale^2 / scale of it goes)
+    const bool along = !SHARED && p.eps > 0.0f;
+    f32x4 dots[2][NI];
+    if (along) {
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
+#pragma unroll
+        for (int ii = 0; ii < NI; ++ii) {
+            const int t = 16 * (tile0 + ii) + g4;
+            dots[0][ii] = sum16(pick<KT>(qh, ii, tile0) * x1[ii]), dots[1][ii] = sum16(pick<KT>(kh, ii, tile0) * x2[ii]);
+        }
+    }
+    __syncthreads();
+    if (wave == W - 1) {
+        const int t = fresh(lane0);
+        float x = 0.0f, y = 0.0f, bsum = 0.0f, below = 0.0f, all = 0.0f;
+#pragma unroll
+        for (int u = 0; u < KT; ++u) x += m.part[0][u][t], y += m.part[1][u][t], bsum += m.part[2][u][t], all += m.whole[u];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) bsum += m.db[s][t];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float u = m.da[j][t], w = m.dg[j][t];
+            bsum += j <= (t >> 4) ? u : 0.0f;
+            below += j >= (t >> 4) ? w : 0.0f;
+        }
+        // (the derivative of a decay that is 0 in 32 bits is that)
+        const double G = m.s.G[t], G1 = __shfl_up(G, 1, 64);
+        const bool dead = G - (t ? G1 : 0.0) < -104.0 * 1.4426950408889634;
+#pragma unroll
+        for (int s = 1; s < 64; s *= 2) {
+            const float up = __shfl_down(x, s, 64), down = __shfl_up(y, s, 64);
+            if (t + s < 64) x += up;
+            if (t >= s) y += down;
+        }
+        const float left = __shfl_up(y, 1, 64);
+        const float sum = (m.s.eG[63] * all + x) + ((t > 0 ? left : 0.0f) + below);
+        if (t0 + t < p.L) {
+            p.dg[(long long)head * p.L + t0 + t] = t0 + t < n && !dead ? sum : 0.0f;
+            p.dbeta[(long long)head * p.L + t0 + t] = t0 + t < n ? bsum : 0.0f;
+        }
+    }
+    const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dk = 16 * slice + c;
+    if (along) {
+        __syncthreads();
+        if (c == 0)
+#pragma unroll
+            for (int ii = 0; ii < NI; ++ii) {
+                *reinterpret_cast<f32x4 *>(&m.part[0][slice][16 * (tile0 + ii) + g4]) = dots[0][ii];
+                *reinterpret_cast<f32x4 *>(&m.part[1][slice][16 * (tile0 + ii) + g4]) = dots[1][ii];
             }
         __syncthreads();
-        if (keys)
+    }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = 16 * i + g4;
+    for (int ii = 0; ii < NI; ++ii) {
+        const int t = 16 * (tile0 + ii) + g4;
+        f32x4 dq = x1[ii], dkey = x2[ii];
+        if (!SHARED) {
+            if (along) {
                 f32x4 a = {}, e = {};
 #pragma unroll
                 for (int u = 0; u < KT; ++u) a += four(m.part[0][u], t), e += four(m.part[1][u], t);
-                dq[i] -= qh[i] * a, dkey[i] -= kh[i] * e;
+                const float over = p.scale != 0.0f ? 1.0f / (p.scale * p.scale) : 0.0f;
+                dq -= pick<KT>(qh, ii, tile0) * a * over, dkey -= pick<KT>(kh, ii, tile0) * e;
             }
-    }
-    if (keys) {
-        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
-        const int dk = 16 * wave + c;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int t = 16 * i + g4;
-            dq[i] *= four(m.s.rq, t), dkey[i] *= four(m.s.rk, t);
-#pragma unroll
-            for (int v = 0; v < 4; ++v) dq[i][v] = t0 + t + v < n ? dq[i][v] : 0.0f, dkey[i][v] = t0 + t + v < n ? dkey[i][v] : 0.0f;
+            dq *= four(m.s.rq, t), dkey *= four(m.s.rk, t);
         }
-        store_rows(p.dq.row(b, hk * p.DK + (key ? dk : 0), p.L), dq, t0, g4, p.L, key);
-        store_rows(p.dk.row(b, hk * p.DK + (key ? dk : 0), p.L), dkey, t0, g4, p.L, key);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) dq[v] = t0 + t + v < n ? dq[v] : 0.0f, dkey[v] = t0 + t + v < n ? dkey[v] : 0.0f;
+        const int end = dk < p.DK ? p.L : 0;
+        if (SHARED) {
+            store4(part_q + (long long)dk * p.L, dq, t0 + t, end);
+            store4(part_k + (long long)dk * p.L, dkey, t0 + t, end);
+        } else {
+            store4(dq_row + (long long)dk * p.L, dq, t0 + t, end);
+            store4(dk_row + (long long)dk * p.L, dkey, t0 + t, end);
+        }
     }
 }
-template <typename T, int KT> __global__ __launch_bounds__(64 * kDeltaBwdWaves(KT)) void delta_bwd_chunk_kernel(DeltaBwd<T> p, int first)
+template <typename T, int KT, bool SHARED> __global__ __launch_bounds__(64 * kGradWaves) void delta_bwd_chunk_kernel(DeltaBwd<T> p, int first)
 {
     extern __shared__ char lds[];
     DeltaChunkLds<T, KT> &m = *reinterpret_cast<DeltaChunkLds<T, KT> *>(lds);
-    LowTiles<T, 3, 64 * kDeltaBwdWaves(KT)>::zeros(m.t);
-    LowTiles<T, 3, 64 * kDeltaBwdWaves(KT)>::zeros(m.p);
-    delta_bwd_chunk(p, m, first + (int)blockIdx.x);
+    LowTiles<T, 3, 64 * kGradWaves>::zeros(m.t);
+    LowTiles<T, 3, 64 * kGradWaves>::zeros(m.p);
+    delta_bwd_chunk<T, KT, SHARED>(p, m, first + (int)blockIdx.x);
+}
+
+// The gradients of a key and query that `each` heads share: theirs added up in order, and through x / |x|.  A workgroup has 64 positions of a head of keys, a
+// wave every fourth channel.
+template <typename T> __global__ __launch_bounds__(256) void delta_share_kernel(DeltaBwd<T> p, int first)
+{
+    __shared__ float sums[4][4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, unit = first + (int)blockIdx.x;
+    const int ch = unit % p.chunks, bk = unit / p.chunks, Hk = p.H / p.each, b = bk / Hk, hk = bk % Hk, t = ch * kDeltaChunk + lane, n = p.length(b);
+    const bool inside = t < n, stored = t < p.L;
+    const long long head = (long long)b * p.H + (long long)hk * p.each;
+    const T *qrow = p.q.row(b, hk * p.DK, p.pitch) + (inside ? t : 0), *krow = p.k.row(b, hk * p.DK, p.pitch) + (inside ? t : 0);
+    const auto sum = [&](int r, float &dq, float &dk) __attribute__((always_inline)) {
+        dq = dk = 0.0f;
+        if (inside)
+            for (int e = 0; e < p.each; ++e) {
+                const float *part = p.part + ((head + e) * 2 * p.DK + r) * p.L + t;
+                dq += part[0], dk += part[(long long)p.DK * p.L];
+            }
+    };
+    float qq = 0.0f, kk = 0.0f, qd = 0.0f, kd = 0.0f;
+    if (p.eps > 0.0f)
+        for (int r = wave; r < p.DK; r += 4) {
+            float dq, dk;
+            sum(r, dq, dk);
+            const float q = ld_elem(qrow + (long long)r * p.pitch), k = ld_elem(krow + (long long)r * p.pitch);
+            qq = fmaf(q, q, qq), kk = fmaf(k, k, kk), qd = fmaf(q, dq, qd), kd = fmaf(k, dk, kd);
+        }
+    sums[0][wave][lane] = qq, sums[1][wave][lane] = kk, sums[2][wave][lane] = qd, sums[3][wave][lane] = kd;
+    __syncthreads();
+    const auto all = [&](int i) { return (sums[i][0][lane] + sums[i][1][lane]) + (sums[i][2][lane] + sums[i][3][lane]); };
+    const bool unit_length = p.eps > 0.0f;
+    const float iq = unit_length ? 1.0f / sqrtf(all(0) + p.eps) : 1.0f, ik = unit_length ? 1.0f / sqrtf(all(1) + p.eps) : 1.0f;
+    const float qa = unit_length ? all(2) * iq * iq : 0.0f, ka = unit_length ? all(3) * ik * ik : 0.0f;
+    T *dq_row = p.dq.row(b, hk * p.DK, p.L) + t, *dk_row = p.dk.row(b, hk * p.DK, p.L) + t;
+    for (int r = wave; r < p.DK; r += 4) {
+        float dq, dk;
+        sum(r, dq, dk);
+        const float q = ld_elem(qrow + (long long)r * p.pitch), k = ld_elem(krow + (long long)r * p.pitch);
+        if (!stored) continue;
+        st_elem(dq_row + (long long)r * p.L, inside ? p.scale * iq * fmaf(-q, qa, dq) : 0.0f);
+        st_elem(dk_row + (long long)r * p.L, inside ? ik * fmaf(-k, ka, dk) : 0.0f);
+    }
 }
 
 }  // namespace dwconv

@@ -48,13 +48,15 @@ def test_forward_refusals(lib):
     for x in (float("nan"), float("inf")):
         assert fwd(lib, scale=x) == 9 and fwd(lib, eps=x) == 9
     assert fwd(lib, eps=-1e-6) == 9
-    need = lib.dwconv_delta_workspace_bytes(2, 4, 8, 16, 100, 0)
+    need = lib.dwconv_delta_workspace_bytes(2, 4, 2, 8, 16, 100, 0)
     assert fwd(lib, ws=None) == 5 and fwd(lib, n=need - 1) == 5 and fwd(lib, ws=P + 8) == 5
 
 
 def test_backward_refusals(lib):
-    need = lib.dwconv_delta_workspace_bytes(2, 4, 8, 16, 100, 1)
-    assert need == lib.dwconv_delta_workspace_bytes(2, 4, 8, 16, 100, 0) + 2 * 4 * 2 * 8 * 16 * 4
+    need = lib.dwconv_delta_workspace_bytes(2, 4, 2, 8, 16, 100, 1)
+    # the states' gradients behind two chunks of every head, and what each of the heads that share a key adds to its gradients
+    assert need == lib.dwconv_delta_workspace_bytes(2, 4, 2, 8, 16, 100, 0) + 2 * 4 * 2 * 8 * 16 * 4 + 2 * 4 * 2 * 8 * 100 * 4
+    assert lib.dwconv_delta_workspace_bytes(2, 4, 4, 8, 16, 100, 1) == need - 2 * 4 * 2 * 8 * 100 * 4
 
     def f(k=None, v=None, ws=P, n=1 << 40, scale=1.0, eps=1e-6, dtype=0, **dims):
         a = dict(do=S(), q=S(), k=S(), v=S(), g=S(), beta=S(), states=P, ds_last=None, lengths=None, dq=S(), dk=S(), dv=S(), dg=P, dbeta=P, ds0=P)
@@ -76,10 +78,12 @@ def test_backward_refusals(lib):
 
 def test_states_and_workspaces(lib):
     assert [lib.dwconv_delta_states(L) for L in (0, -1, 1, 64, 65, 1 << 30, (1 << 30) + 1)] == [0, 0, 1, 1, 2, 1 << 24, 0]
-    for bad in ((0, 1, 1, 1, 1), (1, 0, 1, 1, 1), (1, 1, 0, 1, 1), (1, 1, 129, 1, 1), (1, 1, 1, 0, 1), (1, 1, 1, 1, 0)):
+    for bad in ((0, 1, 1, 1, 1, 1), (1, 0, 1, 1, 1, 1), (1, 2, 0, 1, 1, 1), (1, 3, 2, 1, 1, 1), (1, 1, 1, 0, 1, 1), (1, 1, 1, 129, 1, 1), (1, 1, 1, 1, 0, 1), (1, 1, 1, 1, 1, 0)):
         assert lib.dwconv_delta_workspace_bytes(*bad, 0) == 0 and lib.dwconv_delta_workspace_bytes(*bad, 1) == 0
-    a, b = (lib.dwconv_delta_workspace_bytes(1, 1, 1, 1, 1, x) for x in (0, 1))
-    assert a > 0 and a % 16 == 0 and b == a + 16 and lib.dwconv_delta_workspace_bytes(3, 5, 1, 1, 65, 0) == 30 * a
+    a, b = (lib.dwconv_delta_workspace_bytes(1, 1, 1, 1, 1, 64, x) for x in (0, 1))
+    assert a > 0 and a % 16 == 0 and b == a + 16 and lib.dwconv_delta_workspace_bytes(3, 5, 5, 1, 1, 65, 0) == 30 * a
+    # (rows of fewer than eight positions are copied to where they have room for that)
+    assert lib.dwconv_delta_workspace_bytes(1, 1, 1, 1, 1, 7, 0) > a == lib.dwconv_delta_workspace_bytes(1, 1, 1, 1, 1, 8, 0)
 
 
 def test_step_refusals(lib):

@@ -220,7 +220,7 @@ def test_repeats_and_streams(B, H, Hk, DK, DV, L):
     first = run()
     torch.cuda.synchronize()
     side = torch.cuda.Stream()
-    ws = torch.full((block.delta_workspace_bytes(B, H, DK, DV, L, True) // 4,), float("nan"), device="cuda")
+    ws = torch.full((block.delta_workspace_bytes(B, H, Hk, DK, DV, L, True) // 4,), float("nan"), device="cuda")
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
         second = run(ws)
