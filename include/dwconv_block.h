@@ -139,7 +139,8 @@ DWCONV_API int dwconv_conv_ring(dwconv_seq x, void *ring, const int *lengths, co
  * q, k [B, Hk * DK, L], v, o [B, H * DV, L] of `dtype`, head by head; g, beta [B, H, L] fp32 (dwconv_seq too).  eps > 0: q and k of a
  * position are brought to unit length first, x / sqrt(|x|^2 + eps); eps = 0: taken as they are.  s0 [B, H, DK, DV] fp32 or NULL (zeros); lengths as in
  * dwconv_scan_fwd (o is 0 from n on, whatever the inputs hold there); s_last [B, H, DK, DV] fp32 or NULL: the state behind n.
- * states [B, H, dwconv_delta_states(L), DK, DV] fp32 or NULL: S in front of every 64th position, which dwconv_delta_bwd takes.
+ * states [B, H, dwconv_delta_states(L), DK, DV] fp32 or NULL: S in front of every 64th position that is inside its sequence, which
+ * dwconv_delta_bwd takes.
  * workspace: dwconv_delta_workspace_bytes(...) bytes, 16-byte aligned.
  * DK at most 128, DV at most 65536, H at most 2^20.  g may be minus infinity (nothing in front of t is remembered).  Finite values whose results are
  * finite give those; what is not finite may reach every position of its chunk of 64 and everything behind it, of its own head and of those that

@@ -39,11 +39,13 @@ _lib = None
 class _Declines:
     """In the place of the native calls until the library is loaded, and where they cannot be (see ``binding``)."""
     scan_fwd = scan_bwd = scan_step = norm_fwd = norm_bwd = clip_grad_norm = conv_step = staticmethod(lambda *args: None)
+    delta_fwd = delta_bwd = delta_step = dropout = scan_fwd
 
 
 _fast = _Declines
 _FAST_ADDRESSES = ("dwconv_scan_fwd", "dwconv_scan_bwd", "dwconv_scan_states", "dwconv_scan_workspace_bytes", "dwconv_scan_step", "dwconv_norm_fwd",
                    "dwconv_norm_bwd", "dwconv_norm_workspace_bytes", "dwconv_clip_grad_norm", "dwconv_clip_workspace_bytes", "dwconv_conv_step")
+_FAST_DELTA_ADDRESSES = ("dwconv_delta_fwd", "dwconv_delta_bwd", "dwconv_delta_states", "dwconv_delta_workspace_bytes", "dwconv_delta_step", "dwconv_dropout")
 
 
 def lib():
@@ -75,6 +77,7 @@ def lib():
             fn.argtypes, fn.restype = args, res
         if binding._fast is not binding._Declines:
             binding._fast.setup_block(*(ctypes.cast(getattr(l, n), vp).value for n in _FAST_ADDRESSES))
+            binding._fast.setup_delta(*(ctypes.cast(getattr(l, n), vp).value for n in _FAST_DELTA_ADDRESSES))
             _fast = binding._fast
         _lib = l
     return _lib
@@ -236,7 +239,7 @@ def _heads(q, v, g, key_heads, dims: int):
     Hk = H if key_heads is None else int(key_heads)
     if H < 1 or Hk < 1 or H % Hk:
         raise ValueError(f"{H} heads of values do not share {Hk} heads of keys evenly")
-    if q.shape[1] % Hk or v.shape[1] % H:
+    if q.shape[1] % Hk or v.shape[1] % H or q.shape[1] < Hk:
         raise ValueError(f"q has {q.shape[1]} channels for {Hk} heads, v {v.shape[1]} for {H}")
     return B, H, Hk, int(q.shape[1]) // Hk, int(v.shape[1]) // H
 
@@ -247,8 +250,11 @@ def delta_fwd(q, k, v, g, beta, s0=None, lengths=None, key_heads=None, scale=Non
     neighbouring heads of values share one of keys.  scale None: DK^-1/2.  eps: q and k are brought to unit length, x / sqrt(|x|^2 + eps); 0: taken as
     they are.  s0 [B, H, DK, DV] fp32 (None: zeros), lengths [B] int32 (None: L; o is 0 behind a sequence's end).
     Returns (o, s_last, states): o like v, s_last [B, H, DK, DV] fp32, states what ``delta_bwd`` takes (None without ``save``)."""
-    scale = scale if scale is not None else _unit_scale(q, key_heads, g)
+    done = _fast.delta_fwd(q, k, v, g, beta, s0, lengths, key_heads, scale, eps, save, out, workspace)
+    if done is not None:
+        return done
     B, H, Hk, DK, DV = _heads(q, v, g, key_heads, 3)
+    scale = DK ** -0.5 if scale is None else scale
     L, code, keys, values = int(q.shape[2]), _dtype_code(q), (B, Hk * DK, q.shape[2]), (B, H * DV, q.shape[2])
     ins = [_seq(q, "q", keys, q.dtype), _seq(k, "k", keys, q.dtype), _seq(v, "v", values, q.dtype),
            _seq(g, "g", (B, H, L), torch.float32), _seq(beta, "beta", (B, H, L), torch.float32)]
@@ -269,8 +275,11 @@ def delta_bwd(do, q, k, v, g, beta, states, ds_last=None, lengths=None, key_head
     given = out if out is not None else (None,) * 3
     if len(given) != 3:
         raise ValueError("out must be three tensors (dq, dk, dv)")
-    scale = scale if scale is not None else _unit_scale(q, key_heads, g)
+    done = _fast.delta_bwd(do, q, k, v, g, beta, states, ds_last, lengths, key_heads, scale, eps, *given, workspace)
+    if done is not None:
+        return done
     B, H, Hk, DK, DV = _heads(q, v, g, key_heads, 3)
+    scale = DK ** -0.5 if scale is None else scale
     L, code, keys, values = int(q.shape[2]), _dtype_code(q), (B, Hk * DK, q.shape[2]), (B, H * DV, q.shape[2])
     ins = [_seq(do, "do", values, q.dtype), _seq(q, "q", keys, q.dtype), _seq(k, "k", keys, q.dtype), _seq(v, "v", values, q.dtype),
            _seq(g, "g", (B, H, L), torch.float32), _seq(beta, "beta", (B, H, L), torch.float32)]
@@ -288,8 +297,11 @@ def delta_bwd(do, q, k, v, g, beta, states, ds_last=None, lengths=None, key_head
 def delta_step(q, k, v, g, beta, s, slots=None, key_heads=None, scale=None, eps: float = 1e-6, out=None):
     """One token of the gated delta rule for a batch: q, k [B, key_heads * DK], v [B, H * DV], g and beta [B, H] fp32; s [pool, H, DK, DV] fp32 is
     updated in place, place b of the batch in row slots[b] as in ``scan_step``.  Returns o like v."""
-    scale = scale if scale is not None else _unit_scale(q, key_heads, g)
+    done = _fast.delta_step(q, k, v, g, beta, s, slots, key_heads, scale, eps, out)
+    if done is not None:
+        return done
     B, H, Hk, DK, DV = _heads(q, v, g, key_heads, 2)
+    scale = DK ** -0.5 if scale is None else scale
     code, keys, values = _dtype_code(q), (B, Hk * DK), (B, H * DV)
     ins = [_seq(q, "q", keys, q.dtype), _seq(k, "k", keys, q.dtype), _seq(v, "v", values, q.dtype), _seq(g, "g", (B, H), torch.float32),
            _seq(beta, "beta", (B, H), torch.float32)]
@@ -301,16 +313,12 @@ def delta_step(q, k, v, g, beta, s, slots=None, key_heads=None, scale=None, eps:
     return o
 
 
-def _unit_scale(q, key_heads, g):
-    """DK^-1/2."""
-    n = int(q.shape[1]) if q.dim() > 1 else 0
-    Hk = key_heads if key_heads is not None else (g.shape[1] if g.dim() > 1 else 0)
-    return (n // Hk) ** -0.5 if Hk and n >= Hk > 0 else 1.0
-
-
 # ---- dropout ----
 
 def _dropout(x, name, p, rng, layer, res, scale, tied, out):
+    done = _fast.dropout(x, p, rng, layer, res, scale, tied, out)
+    if done is not None:
+        return done
     shape = B, C, L = _shape3(x, name)
     code = _dtype_code(x)
     xs, rs = _seq(x, name, shape, x.dtype), _NONE if res is None else _seq(res, "res", shape, x.dtype)

@@ -161,18 +161,31 @@ template <typename T, int KT> int launch_pairs(const DeltaShape<T> &p, hipStream
     return DWCONV_OK;
 }
 
-// Segments that rows of chunks are cut into.
+// Segments that a head's chunks are cut into.  A walk's steps are a chain: few heads leave most of the chip idle, and what a segment does to any state
+// it starts with (DV + DK columns instead of DV) can be formed for all segments at once, the states between them in a chain of its own, which takes a
+// third of a step each, and then all segments at once again.  In steps of a walk that has a CU to itself (two workgroups share one at 1.4 times that;
+// in fp32 with more than 64 channels of a key LDS has room for one), forward the pass that forms spans writes no output and takes 0.6.
+// us whole / cut (segments): bf16, DK = DV = 128, 256 chunks, 2 heads forward 1623 / 189 (32), backward 1630 / 275; 32 heads 1857 / 786 (8), 2971 / 2057; 64
+// heads 2000 / 1510 (4), 4239 / 4076; 128 heads, 64 chunks 582 / 824, 1649 / 2086; 2 heads, 8 chunks 62 / 46 (4), 93 / 83.  fp32, 64 heads 4500 / 4650, 7936 /
+// 9345.  DK = DV = 64, bf16, 128 heads 1407 / 1297 (4), 3717 / 3874; fp32 2443 / 2292, 5806 / 6221.
 struct WalkPlan {
     int segs, per;
 };
-WalkPlan plan_walk(int B, int H, int DK, int DV, int L)
+WalkPlan plan_walk(int B, int H, int DK, int DV, int L, int dtype, bool backward)
 {
     const int chunks = chunks_of(L);
-    const long long groups = (long long)B * H * ceil_div(DV, 16 * kWalkWaves);
-    const int segs = (int)std::min<long long>(512 / std::max(1ll, groups), chunks / 4);
-    if (segs < 4) return WalkPlan{1, chunks};
-    const int per = (int)ceil_div(chunks, segs);
-    return WalkPlan{(int)ceil_div(chunks, per), per};
+    const bool alone = dtype == DWCONV_F32 && DK > 64;
+    const double heads = (double)B * H, values = (double)ceil_div(DV, 16 * kWalkWaves),
+                 all = (double)ceil_div(ceil_div(DV, 16) + ceil_div(DK, 16), kWalkWaves);
+    const auto step = [&](double groups) { return groups <= 256 ? 1.0 : alone ? groups / 256 : groups <= 512 ? 1.4 : 1.4 * groups / 512; };
+    double best = chunks * step(heads * values);
+    WalkPlan w{1, chunks};
+    for (int segs = 2; segs <= 128 && segs <= chunks / 2; segs *= 2) {
+        const int per = (int)ceil_div(chunks, segs);
+        const double cost = per * ((backward ? 1.0 : 0.6) * step(heads * segs * all) + step(heads * segs * values)) + 0.3 * segs + 1.0;
+        if (cost < best) best = cost, w = WalkPlan{(int)ceil_div(chunks, per), per};
+    }
+    return w;
 }
 size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 size_t starts_bytes(const WalkPlan &w, int B, int H, int DK, int DV) { return w.segs > 1 ? up16((size_t)B * H * w.segs * DK * DV * sizeof(float)) : 0; }
@@ -223,7 +236,7 @@ template <typename T, int KT> int launch_bwd(const DeltaBwd<T> &p, const DeltaWa
     if (rc != DWCONV_OK) return rc;
     const int units = p.B * p.H * p.chunks, shared = p.each > 1 ? units / p.each : 0;
     for (int first = 0; first < units; first += kMaxUnits) kernel<<<std::min(units - first, kMaxUnits), 64 * kGradWaves, chunk, st>>>(p, first);
-    for (int first = 0; first < shared; first += kMaxUnits) delta_share_kernel<T><<<std::min(shared - first, kMaxUnits), 256, 0, st>>>(p, first);
+    for (int first = 0; first < shared; first += kMaxUnits) delta_share_kernel<T, KT><<<std::min(shared - first, kMaxUnits), 512, 0, st>>>(p, first);
     return launch_status();
 }
 template <typename T> int launch_bwd(const DeltaBwd<T> &p, const DeltaWalk &w, hipStream_t st)
@@ -256,10 +269,19 @@ template <typename T> DeltaShape<T> shape(dwconv_seq q, dwconv_seq k, dwconv_seq
 }
 // A workspace: records of pairs, starts and spans of segments, backward the states' gradients behind the chunks.
 size_t pairs_bytes(int B, int H, int L) { return (size_t)B * H * chunks_of(L) * sizeof(DeltaPairs); }
-size_t walk_bytes(int B, int H, int DK, int DV, int L)
+size_t walk_bytes(int B, int H, int DK, int DV, int L, bool backward)          // (of either type)
 {
-    const WalkPlan w = plan_walk(B, H, DK, DV, L);
-    return starts_bytes(w, B, H, DK, DV) + spans_bytes(w, B, H, DK, DV);
+    size_t most = 0;
+    for (const int dtype : {DWCONV_F32, DWCONV_BF16}) {
+        const WalkPlan w = plan_walk(B, H, DK, DV, L, dtype, backward);
+        most = std::max(most, starts_bytes(w, B, H, DK, DV) + spans_bytes(w, B, H, DK, DV));
+    }
+    return most;
+}
+DeltaWalk walk_in(char *at, int B, int H, int DK, int DV, int L, int dtype, bool backward)
+{
+    const WalkPlan w = plan_walk(B, H, DK, DV, L, dtype, backward);
+    return DeltaWalk{w.segs, w.per, reinterpret_cast<float *>(at), reinterpret_cast<float *>(at + starts_bytes(w, B, H, DK, DV))};
 }
 constexpr int kPadded = 8;
 size_t padded_bytes(int B, int H, int DK, int DV, int L) { return L < kPadded ? up16((size_t)B * H * (2 * (DK + DV)) * kPadded * sizeof(float)) : 0; }
@@ -284,12 +306,6 @@ template <typename T> void pad_all(DeltaShape<T> &p, Seq<T> *dout, void *room, h
 }
 size_t after_bytes(int B, int H, int DK, int DV, int L) { return up16((size_t)B * H * chunks_of(L) * DK * DV * sizeof(float)); }
 size_t part_bytes(int B, int H, int DK, int L, bool shared) { return shared ? up16((size_t)B * H * 2 * DK * L * sizeof(float)) : 0; }
-DeltaWalk walk_in(void *workspace, int B, int H, int DK, int DV, int L)
-{
-    const WalkPlan w = plan_walk(B, H, DK, DV, L);
-    char *at = static_cast<char *>(workspace) + pairs_bytes(B, H, L) + padded_bytes(B, H, DK, DV, L);
-    return DeltaWalk{w.segs, w.per, reinterpret_cast<float *>(at), reinterpret_cast<float *>(at + starts_bytes(w, B, H, DK, DV))};
-}
 
 }  // namespace
 
@@ -300,7 +316,7 @@ int dwconv_delta_states(int L) { return L < 1 || L > (1 << 30) ? 0 : chunks_of(L
 size_t dwconv_delta_workspace_bytes(int B, int H, int Hk, int DK, int DV, int L, int backward)
 {
     if (check_heads(B, H, Hk, DK, DV, L) != DWCONV_OK) return 0;
-    return pairs_bytes(B, H, L) + padded_bytes(B, H, DK, DV, L) + walk_bytes(B, H, DK, DV, L) + (backward ? after_bytes(B, H, DK, DV, L) + part_bytes(B, H, DK, L, Hk < H) : 0);
+    return pairs_bytes(B, H, L) + padded_bytes(B, H, DK, DV, L) + walk_bytes(B, H, DK, DV, L, backward != 0) + (backward ? after_bytes(B, H, DK, DV, L) + part_bytes(B, H, DK, L, Hk < H) : 0);
 }
 
 int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const float *s0, const int *lengths, dwconv_seq_out o,
@@ -322,8 +338,8 @@ int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwc
         if (!f32_ok(t)) return DWCONV_ERR_ALIGN;
     if (!workspace || workspace_bytes < dwconv_delta_workspace_bytes(B, H, Hk, DK, DV, L, 0) || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const DeltaWalk walk = walk_in(workspace, B, H, DK, DV, L);
-    void *room = static_cast<char *>(workspace) + pairs_bytes(B, H, L);
+    char *const room = static_cast<char *>(workspace) + pairs_bytes(B, H, L);
+    const DeltaWalk walk = walk_in(room + padded_bytes(B, H, DK, DV, L), B, H, DK, DV, L, dtype, false);
     if (dtype == DWCONV_F32) {
         DeltaFwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<float>(o), s0, s_last, states};
         pad_all<float>(p, nullptr, room, st);
@@ -357,9 +373,9 @@ int dwconv_delta_bwd(dwconv_seq dout, dwconv_seq q, dwconv_seq k, dwconv_seq v, 
     const size_t need = dwconv_delta_workspace_bytes(B, H, Hk, DK, DV, L, 1);
     if (!workspace || workspace_bytes < need || !aligned_to(workspace, 16)) return DWCONV_ERR_WORKSPACE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const DeltaWalk walk = walk_in(workspace, B, H, DK, DV, L);
-    float *after = reinterpret_cast<float *>(static_cast<char *>(workspace) + pairs_bytes(B, H, L) + padded_bytes(B, H, DK, DV, L) + walk_bytes(B, H, DK, DV, L));
-    void *room = static_cast<char *>(workspace) + pairs_bytes(B, H, L);
+    char *const room = static_cast<char *>(workspace) + pairs_bytes(B, H, L), *const spans = room + padded_bytes(B, H, DK, DV, L);
+    const DeltaWalk walk = walk_in(spans, B, H, DK, DV, L, dtype, true);
+    float *after = reinterpret_cast<float *>(spans + walk_bytes(B, H, DK, DV, L, true));
     float *part = reinterpret_cast<float *>(reinterpret_cast<char *>(after) + after_bytes(B, H, DK, DV, L));
     if (dtype == DWCONV_F32) {
         DeltaBwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<float>(dout), seq<float>(dq), seq<float>(dk),

@@ -1279,45 +1279,59 @@ template <typename T, int KT, bool SHARED> __global__ __launch_bounds__(64 * kGr
 }
 
 // The gradients of a key and query that `each` heads share: theirs added up in order, and through x / |x|.  A workgroup has 64 positions of a head of keys, a
-// wave every fourth channel.
-template <typename T> __global__ __launch_bounds__(256) void delta_share_kernel(DeltaBwd<T> p, int first)
+// wave every eighth channel, in registers.
+template <typename T, int KT> __global__ __launch_bounds__(512) void delta_share_kernel(DeltaBwd<T> p, int first)
 {
-    __shared__ float sums[4][4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, unit = first + (int)blockIdx.x;
+    constexpr int N = 2 * KT;
+    __shared__ float sums[4][8][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), unit = first + (int)blockIdx.x;
     const int ch = unit % p.chunks, bk = unit / p.chunks, Hk = p.H / p.each, b = bk / Hk, hk = bk % Hk, t = ch * kDeltaChunk + lane, n = p.length(b);
-    const bool inside = t < n, stored = t < p.L;
-    const long long head = (long long)b * p.H + (long long)hk * p.each;
-    const T *qrow = p.q.row(b, hk * p.DK, p.pitch) + (inside ? t : 0), *krow = p.k.row(b, hk * p.DK, p.pitch) + (inside ? t : 0);
-    const auto sum = [&](int r, float &dq, float &dk) __attribute__((always_inline)) {
-        dq = dk = 0.0f;
-        if (inside)
-            for (int e = 0; e < p.each; ++e) {
-                const float *part = p.part + ((head + e) * 2 * p.DK + r) * p.L + t;
-                dq += part[0], dk += part[(long long)p.DK * p.L];
+    const bool inside = t < n;
+    const long long head = (long long)b * p.H + (long long)hk * p.each, size = (long long)p.DK * p.L;
+    float dq[N], dk[N], q[N], k[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int r = wave + 8 * i;
+        const bool on = inside && r < p.DK;
+        const long long at = on ? (long long)r * p.pitch + t : 0;
+        q[i] = ld_elem(p.q.row(b, hk * p.DK, p.pitch) + at), k[i] = ld_elem(p.k.row(b, hk * p.DK, p.pitch) + at);
+        dq[i] = dk[i] = 0.0f;
+        if (!on) q[i] = k[i] = 0.0f;
+    }
+    if (inside)
+        for (int e = 0; e < p.each; ++e) {
+            const float *part = p.part + (head + e) * 2 * size + t;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const long long at = (long long)min(wave + 8 * i, p.DK - 1) * p.L;
+                dq[i] += part[at], dk[i] += part[size + at];
             }
-    };
-    float qq = 0.0f, kk = 0.0f, qd = 0.0f, kd = 0.0f;
-    if (p.eps > 0.0f)
-        for (int r = wave; r < p.DK; r += 4) {
-            float dq, dk;
-            sum(r, dq, dk);
-            const float q = ld_elem(qrow + (long long)r * p.pitch), k = ld_elem(krow + (long long)r * p.pitch);
-            qq = fmaf(q, q, qq), kk = fmaf(k, k, kk), qd = fmaf(q, dq, qd), kd = fmaf(k, dk, kd);
         }
-    sums[0][wave][lane] = qq, sums[1][wave][lane] = kk, sums[2][wave][lane] = qd, sums[3][wave][lane] = kd;
-    __syncthreads();
-    const auto all = [&](int i) { return (sums[i][0][lane] + sums[i][1][lane]) + (sums[i][2][lane] + sums[i][3][lane]); };
-    const bool unit_length = p.eps > 0.0f;
-    const float iq = unit_length ? 1.0f / sqrtf(all(0) + p.eps) : 1.0f, ik = unit_length ? 1.0f / sqrtf(all(1) + p.eps) : 1.0f;
-    const float qa = unit_length ? all(2) * iq * iq : 0.0f, ka = unit_length ? all(3) * ik * ik : 0.0f;
+    float iq = 1.0f, ik = 1.0f, qa = 0.0f, ka = 0.0f;
+    if (p.eps > 0.0f) {
+        float s[4] = {};
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[0] = fmaf(q[i], q[i], s[0]), s[1] = fmaf(k[i], k[i], s[1]), s[2] = fmaf(q[i], dq[i], s[2]), s[3] = fmaf(k[i], dk[i], s[3]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sums[j][wave][lane] = s[j];
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            s[j] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) s[j] += sums[j][w][lane];
+        }
+        iq = 1.0f / sqrtf(s[0] + p.eps), ik = 1.0f / sqrtf(s[1] + p.eps);
+        qa = s[2] * iq * iq, ka = s[3] * ik * ik;
+    }
+    if (t >= p.L) return;
     T *dq_row = p.dq.row(b, hk * p.DK, p.L) + t, *dk_row = p.dk.row(b, hk * p.DK, p.L) + t;
-    for (int r = wave; r < p.DK; r += 4) {
-        float dq, dk;
-        sum(r, dq, dk);
-        const float q = ld_elem(qrow + (long long)r * p.pitch), k = ld_elem(krow + (long long)r * p.pitch);
-        if (!stored) continue;
-        st_elem(dq_row + (long long)r * p.L, inside ? p.scale * iq * fmaf(-q, qa, dq) : 0.0f);
-        st_elem(dk_row + (long long)r * p.L, inside ? ik * fmaf(-k, ka, dk) : 0.0f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int r = wave + 8 * i;
+        if (r >= p.DK) continue;
+        st_elem(dq_row + (long long)r * p.L, inside ? p.scale * iq * fmaf(-q[i], qa, dq[i]) : 0.0f);
+        st_elem(dk_row + (long long)r * p.L, inside ? ik * fmaf(-k[i], ka, dk[i]) : 0.0f);
     }
 }
 

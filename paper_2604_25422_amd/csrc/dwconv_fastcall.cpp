@@ -19,6 +19,7 @@
 #include <torch/csrc/jit/frontend/tracer.h>
 
 #include <climits>
+#include <cmath>
 #include <vector>
 
 #include "../../include/dwconv_block.h"
@@ -288,6 +289,14 @@ struct BlockFns {
     decltype(&dwconv_clip_workspace_bytes) clip_workspace;
     decltype(&dwconv_conv_step) conv_step;
 } blk;
+struct DeltaFns {
+    decltype(&dwconv_delta_fwd) fwd;
+    decltype(&dwconv_delta_bwd) bwd;
+    decltype(&dwconv_delta_states) states;
+    decltype(&dwconv_delta_workspace_bytes) workspace;
+    decltype(&dwconv_delta_step) step;
+    decltype(&dwconv_dropout) dropout;
+} dlt;
 
 // A device tensor of any strides, or nullptr.
 const at::Tensor *on_device(PyObject *o, long device)
@@ -346,6 +355,20 @@ struct Args {
         if (ok) s.data = t->mutable_data_ptr();
         return s;
     }
+    // A sequence of `channels` channels and of a type of its own, of the call's B and L.
+    template <typename S> S seq_of(PyObject *o, int dims, int64_t channels, at::ScalarType dt, bool written)
+    {
+        S s{nullptr, (long long)channels * L};
+        if (!ok || (written && o == Py_None)) return s;
+        const at::Tensor *t = on_device(o, call.device);
+        ok = t && t->dim() == dims && t->scalar_type() == dt && t->size(0) == B && t->size(1) == channels && (dims < 3 || t->size(2) == L) &&
+             (dims < 3 || L == 1 || t->stride(2) == 1) && (channels == 1 || t->stride(1) == L);
+        if (!ok) return s;
+        if (B > 1) s.batch_stride = t->stride(0);
+        ok = !written || s.batch_stride >= (long long)channels * L;
+        if (ok) s.data = const_cast<void *>(written ? t->mutable_data_ptr() : t->const_data_ptr());
+        return s;
+    }
     // A contiguous tensor of that type and those sizes (of fewer dimensions: -1 behind).
     const at::Tensor *dense(PyObject *o, at::ScalarType dt, int64_t a, int64_t b = -1, int64_t c = -1)
     {
@@ -354,6 +377,12 @@ struct Args {
         ok = t && t->scalar_type() == dt && t->dim() == dims && t->is_contiguous() && t->size(0) == a && (dims < 2 || t->size(1) == b) &&
              (dims < 3 || t->size(2) == c);
         return ok ? t : nullptr;
+    }
+    float *dense_f32(PyObject *o, at::IntArrayRef sizes)
+    {
+        const at::Tensor *t = ok ? on_device(o, call.device) : nullptr;
+        ok = t && t->scalar_type() == at::kFloat && t->sizes() == sizes && t->is_contiguous();
+        return ok ? static_cast<float *>(const_cast<void *>(t->const_data_ptr())) : nullptr;
     }
     float *f32(PyObject *o, int64_t a, int64_t b = -1, int64_t c = -1)
     {
@@ -664,6 +693,187 @@ PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// The heads of a call of the delta rule, from q, v, g and key_heads.
+struct Heads {
+    int H = 0, Hk = 0, DK = 0, DV = 0;
+    float scale = 1.0f;
+    Heads(Args &g, PyObject *q, PyObject *v, PyObject *gate, PyObject *key_heads, PyObject *scaled, int dims)
+    {
+        const at::Tensor *qt = g.first(q, dims), *vt = g.ok ? on_device(v, g.call.device) : nullptr, *gt = g.ok ? on_device(gate, g.call.device) : nullptr;
+        g.ok = qt && vt && gt && vt->dim() == dims && gt->dim() == dims && gt->size(1) >= 1 && gt->size(1) <= INT_MAX && vt->size(1) <= INT_MAX;
+        if (!g.ok) return;
+        H = Hk = (int)gt->size(1);
+        if (key_heads != Py_None) g.ok = exact_int(key_heads, Hk);
+        g.ok = g.ok && Hk >= 1 && H % Hk == 0 && g.C % Hk == 0 && vt->size(1) % H == 0 && g.C >= Hk;
+        if (!g.ok) return;
+        DK = g.C / Hk, DV = (int)(vt->size(1) / H);
+        scale = scaled == Py_None ? (float)std::pow((double)DK, -0.5) : g.number(scaled);
+    }
+};
+template <typename S> S made_out(S s, at::Tensor &made, const at::Tensor &t, at::IntArrayRef sizes)
+{
+    if (s.data) return s;
+    made = at::empty(sizes, t.options());
+    s.data = made.mutable_data_ptr();
+    return s;
+}
+
+// (q, k, v, g, beta, s0, lengths, key_heads, scale, eps, save, out, workspace) -> (o, s_last, states)
+PyObject *delta_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    Args g;
+    if (n != 13 || !dlt.fwd) return decline();
+    if (!g.call.begin(a[0])) return g.call.bad() ? nullptr : decline();
+    const Heads hd(g, a[0], a[2], a[3], a[7], a[8], 3);
+    if (!g.ok) return decline();
+    const int keys = g.C, values = hd.H * hd.DV;
+    dwconv_seq q = g.seq_of<dwconv_seq>(a[0], 3, keys, g.type, false), k = g.seq_of<dwconv_seq>(a[1], 3, keys, g.type, false),
+               v = g.seq_of<dwconv_seq>(a[2], 3, values, g.type, false), gt = g.seq_of<dwconv_seq>(a[3], 3, hd.H, at::kFloat, false),
+               bt = g.seq_of<dwconv_seq>(a[4], 3, hd.H, at::kFloat, false);
+    const int64_t state[] = {g.B, hd.H, hd.DK, hd.DV};
+    const float *s0 = a[5] == Py_None ? nullptr : g.dense_f32(a[5], state);
+    const int *lengths = g.index(a[6]);
+    const float eps = g.number(a[9]);
+    const bool save = g.flag(a[10]);
+    dwconv_seq_out os = g.seq_of<dwconv_seq_out>(a[11], 3, values, g.type, true);
+    size_t bytes;
+    void *ws = g.workspace(a[12], bytes);
+    if (!g.ok) return decline();
+    const at::Tensor &like_q = THPVariable_Unpack(a[0]);
+    at::Tensor o, s_last, states, space;
+    int status;
+    {
+        Unlocked unlocked;
+        os = made_out(os, o, like_q, {g.B, values, g.L});
+        float *lp = make_f32(s_last, like_q, state), *sp = save ? make_f32(states, like_q, {g.B, hd.H, dlt.states(g.L), hd.DK, hd.DV}) : nullptr;
+        make_workspace(ws, bytes, dlt.workspace(g.B, hd.H, hd.Hk, hd.DK, hd.DV, g.L, 0), space, like_q);
+        status = dlt.fwd(q, k, v, gt, bt, s0, lengths, os, lp, sp, ws, bytes, g.B, hd.H, hd.Hk, hd.DK, hd.DV, g.L, hd.scale, eps, dtype_code(like_q),
+                         g.call.stream);
+    }
+    if (raised(status)) return nullptr;
+    return results<3>({result(a[11], o), result(Py_None, s_last), result(Py_None, states)});
+    END_HANDLE_TH_ERRORS
+}
+
+// (do, q, k, v, g, beta, states, ds_last, lengths, key_heads, scale, eps, dq, dk, dv (outputs or None), workspace) -> (dq, dk, dv, dg, dbeta, ds0)
+PyObject *delta_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    Args g;
+    if (n != 16 || !dlt.bwd) return decline();
+    if (!g.call.begin(a[1])) return g.call.bad() ? nullptr : decline();
+    const Heads hd(g, a[1], a[3], a[4], a[9], a[10], 3);
+    if (!g.ok) return decline();
+    const int keys = g.C, values = hd.H * hd.DV;
+    dwconv_seq d = g.seq_of<dwconv_seq>(a[0], 3, values, g.type, false), q = g.seq_of<dwconv_seq>(a[1], 3, keys, g.type, false),
+               k = g.seq_of<dwconv_seq>(a[2], 3, keys, g.type, false), v = g.seq_of<dwconv_seq>(a[3], 3, values, g.type, false),
+               gt = g.seq_of<dwconv_seq>(a[4], 3, hd.H, at::kFloat, false), bt = g.seq_of<dwconv_seq>(a[5], 3, hd.H, at::kFloat, false);
+    const int64_t state[] = {g.B, hd.H, hd.DK, hd.DV}, kept[] = {g.B, hd.H, dlt.states(g.L), hd.DK, hd.DV};
+    const float *states = g.dense_f32(a[6], kept), *ds = a[7] == Py_None ? nullptr : g.dense_f32(a[7], state);
+    const int *lengths = g.index(a[8]);
+    const float eps = g.number(a[11]);
+    dwconv_seq_out dqs = g.seq_of<dwconv_seq_out>(a[12], 3, keys, g.type, true), dks = g.seq_of<dwconv_seq_out>(a[13], 3, keys, g.type, true),
+                   dvs = g.seq_of<dwconv_seq_out>(a[14], 3, values, g.type, true);
+    size_t bytes;
+    void *ws = g.workspace(a[15], bytes);
+    if (!g.ok) return decline();
+    const at::Tensor &like_q = THPVariable_Unpack(a[1]);
+    at::Tensor dq, dk, dv, dg, dbeta, ds0, space;
+    int status;
+    {
+        Unlocked unlocked;
+        dqs = made_out(dqs, dq, like_q, {g.B, keys, g.L}), dks = made_out(dks, dk, like_q, {g.B, keys, g.L}), dvs = made_out(dvs, dv, like_q, {g.B, values, g.L});
+        float *gp = make_f32(dg, like_q, {g.B, hd.H, g.L}), *bp = make_f32(dbeta, like_q, {g.B, hd.H, g.L}), *sp = make_f32(ds0, like_q, state);
+        make_workspace(ws, bytes, dlt.workspace(g.B, hd.H, hd.Hk, hd.DK, hd.DV, g.L, 1), space, like_q);
+        status = dlt.bwd(d, q, k, v, gt, bt, states, ds, lengths, dqs, dks, dvs, gp, bp, sp, ws, bytes, g.B, hd.H, hd.Hk, hd.DK, hd.DV, g.L, hd.scale, eps,
+                         dtype_code(like_q), g.call.stream);
+    }
+    if (raised(status)) return nullptr;
+    return results<6>({result(a[12], dq), result(a[13], dk), result(a[14], dv), result(Py_None, dg), result(Py_None, dbeta), result(Py_None, ds0)});
+    END_HANDLE_TH_ERRORS
+}
+
+// (q, k, v, g, beta, s, slots, key_heads, scale, eps, out) -> o
+PyObject *delta_step(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    Args g;
+    if (n != 11 || !dlt.step) return decline();
+    if (!g.call.begin(a[0])) return g.call.bad() ? nullptr : decline();
+    const Heads hd(g, a[0], a[2], a[3], a[7], a[8], 2);
+    if (!g.ok) return decline();
+    const int keys = g.C, values = hd.H * hd.DV;
+    dwconv_seq q = g.seq_of<dwconv_seq>(a[0], 2, keys, g.type, false), k = g.seq_of<dwconv_seq>(a[1], 2, keys, g.type, false),
+               v = g.seq_of<dwconv_seq>(a[2], 2, values, g.type, false), gt = g.seq_of<dwconv_seq>(a[3], 2, hd.H, at::kFloat, false),
+               bt = g.seq_of<dwconv_seq>(a[4], 2, hd.H, at::kFloat, false);
+    const at::Tensor *pool = g.ok ? plain(a[5], 4, g.call.device) : nullptr;
+    g.ok = pool && pool->size(0) <= INT_MAX;
+    float *s = g.ok ? g.dense_f32(a[5], {pool->size(0), hd.H, hd.DK, hd.DV}) : nullptr;
+    const int *slots = g.index(a[6]);
+    const float eps = g.number(a[9]);
+    dwconv_seq_out os = g.seq_of<dwconv_seq_out>(a[10], 2, values, g.type, true);
+    if (!g.ok) return decline();
+    const at::Tensor &like_q = THPVariable_Unpack(a[0]);
+    at::Tensor o;
+    int status;
+    {
+        Unlocked unlocked;
+        os = made_out(os, o, like_q, {g.B, values});
+        status = dlt.step(q, k, v, gt, bt, s, slots, (int)pool->size(0), os, g.B, hd.H, hd.Hk, hd.DK, hd.DV, hd.scale, eps, dtype_code(like_q), g.call.stream);
+    }
+    if (raised(status)) return nullptr;
+    return result(a[10], o);
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, p, rng, layer, res, scale, tied, out) -> out
+PyObject *dropout(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    Args g;
+    if (n != 8 || !dlt.dropout) return decline();
+    if (!g.call.begin(a[0])) return g.call.bad() ? nullptr : decline();
+    const at::Tensor *x = g.first(a[0], 3);
+    dwconv_seq xs = g.seq(a[0], 3), rs{nullptr, 0};
+    const float p = g.number(a[1]);
+    const at::Tensor *rng = g.dense(a[2], at::kLong, 2);
+    int layer = 0;
+    g.ok = g.ok && exact_int(a[3], layer);
+    if (a[4] != Py_None) rs = g.seq(a[4], 3);
+    const float scale = g.number(a[5]);
+    const bool tied = g.flag(a[6]);
+    dwconv_seq_out os = g.out(a[7], 3);
+    if (!g.ok) return decline();
+    at::Tensor o;
+    int status;
+    {
+        Unlocked unlocked;
+        make(os, o, *x);
+        status = dlt.dropout(xs, rs, os, static_cast<const long long *>(rng->const_data_ptr()), layer, g.B, g.C, g.L, p, scale, tied, dtype_code(*x), g.call.stream);
+    }
+    if (raised(status)) return nullptr;
+    return result(a[7], o);
+    END_HANDLE_TH_ERRORS
+}
+
+// setup_delta(the addresses of DeltaFns in its order)
+PyObject *setup_delta(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    void *p[6];
+    if (n != 6) {
+        PyErr_SetString(PyExc_TypeError, "setup_delta takes six addresses");
+        return nullptr;
+    }
+    for (int k = 0; k < 6; ++k) {
+        p[k] = PyLong_AsVoidPtr(a[k]);
+        if (!p[k]) return PyErr_Occurred() ? nullptr : decline();
+    }
+    dlt = DeltaFns{(decltype(dlt.fwd))p[0], (decltype(dlt.bwd))p[1], (decltype(dlt.states))p[2], (decltype(dlt.workspace))p[3], (decltype(dlt.step))p[4],
+                   (decltype(dlt.dropout))p[5]};
+    Py_RETURN_NONE;
+}
+
 // setup_block(the addresses of BlockFns in its order)
 PyObject *setup_block(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -696,6 +906,11 @@ PyMethodDef methods[] = {
     {"norm_bwd", (PyCFunction)(void (*)())norm_bwd, METH_FASTCALL, nullptr},
     {"conv_step", (PyCFunction)(void (*)())conv_step, METH_FASTCALL, nullptr},
     {"clip_grad_norm", (PyCFunction)(void (*)())clip_grad_norm, METH_FASTCALL, nullptr},
+    {"setup_delta", (PyCFunction)(void (*)())setup_delta, METH_FASTCALL, nullptr},
+    {"delta_fwd", (PyCFunction)(void (*)())delta_fwd, METH_FASTCALL, nullptr},
+    {"delta_bwd", (PyCFunction)(void (*)())delta_bwd, METH_FASTCALL, nullptr},
+    {"delta_step", (PyCFunction)(void (*)())delta_step, METH_FASTCALL, nullptr},
+    {"dropout", (PyCFunction)(void (*)())dropout, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

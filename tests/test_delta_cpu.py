@@ -184,3 +184,22 @@ def test_generator_against_known_answers():
     f = 0xFFFFFFFF
     assert ref.philox((f, f, f, f), (f, f)) == [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]
     assert ref.philox((0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344), (0xA4093822, 0x299F31D0)) == [0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1]
+
+
+def test_native_calls_decline_what_is_not_a_device_tensor(lib):
+    from paper_2604_25422_amd import _fastcall, block
+    assert block._fast is _fastcall
+    x, g, n = torch.zeros(2, 4, 8), torch.zeros(2, 2, 8), None
+    for call in (lambda: _fastcall.delta_fwd(x, x, x, g, g, n, n, n, n, 1e-6, True, n, n), lambda: _fastcall.delta_fwd(x), lambda: _fastcall.delta_fwd(*[n] * 13),
+                 lambda: _fastcall.delta_bwd(x, x, x, x, g, g, x, n, n, n, n, 1e-6, n, n, n, n), lambda: _fastcall.delta_bwd(*[n] * 16),
+                 lambda: _fastcall.delta_step(x, x, x, g, g, x, n, n, n, 1e-6, n), lambda: _fastcall.delta_step(*[n] * 11),
+                 lambda: _fastcall.dropout(x, 0.1, x, 0, n, 1.0, False, n), lambda: _fastcall.dropout(*[n] * 8)):
+        assert call() is None
+
+
+def test_few_heads_are_cut_into_segments(lib):
+    """By what the workspace has room for beside a record a chunk: few heads with many chunks are, many heads are not."""
+    record = lib.dwconv_delta_workspace_bytes(1, 1, 1, 16, 16, 64, 0)
+    for heads, L, cut in ((1, 64, False), (1, 65, False), (2, 1024, True), (4, 65537, True), (32, 4096, True), (768, 1024, False), (4096, 256, False)):
+        more = lib.dwconv_delta_workspace_bytes(1, heads, heads, 128, 128, L, 0) - record * heads * -(-L // 64)
+        assert (more > 0) == cut and (not cut or more >= 4 * heads * 2 * 128 * 384), (heads, L)

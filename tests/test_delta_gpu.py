@@ -533,3 +533,107 @@ def test_refusals():
             with pytest.raises(error):
                 call()
                 pytest.fail(f"{error} {n}")
+
+
+# ---- runs of them together, and the native form of the calls ----
+
+def test_a_block_trained_and_served():
+    """Convolution, delta rule, norm with gate and residual and dropout as a block has them: gradients of the whole against autograd in 64 bits through
+    the definitions, and the same sequence token by token (without dropout) against the prompt pass."""
+    B, H, D, L, K = 2, 2, 16, 100, 4
+    C = H * D
+    x, z, w = rand(B, 3 * C, L, seed=1), rand(B, C, L, seed=2), rand(3 * C, K, seed=3) / 2
+    g, beta = -0.2 * rand(B, H, L, seed=4).abs(), torch.sigmoid(rand(B, H, L, seed=5))
+    res, wn, wn2, dn = rand(B, C, L, seed=6), 1 + 0.1 * rand(C, seed=7), 1 + 0.1 * rand(C, seed=8), rand(B, C, L, seed=9)
+    rng, p = torch.tensor([5, 1], device="cuda"), 0.2
+
+    def forward(drop):
+        u = binding.dwconv_fwd(x, w, K - 1)
+        q, k, v = u.split(C, 1)
+        o, s_last, states = block.delta_fwd(q, k, v, g, beta)
+        y = block.dropout_fwd(o, p, rng, 3) if drop else o
+        out, n, stats = block.norm_fwd(y, z, res, wn, wn2)
+        return u, o, s_last, states, y, out, n, stats
+    u, o, s_last, states, y, out, n, stats = forward(True)
+    dy, dz, dres, dwn, dwn2 = block.norm_bwd(None, dn, y, z, res, wn, wn2, stats)
+    do = block.dropout_bwd(dy, p, rng, 3)
+    q, k, v = u.split(C, 1)
+    du = torch.empty_like(u)
+    _, _, _, dg, dbeta, _ = block.delta_bwd(do, q, k, v, g, beta, states, out=tuple(du.split(C, 1)))
+    dx, dw = binding.dwconv_bwd(du, x, w, K - 1)
+
+    a = [t.double().cpu().requires_grad_() for t in (x, w, g, beta, z, res, wn, wn2)]
+    ux = torch.nn.functional.conv1d(torch.nn.functional.pad(a[0], (K - 1, 0)), a[1][:, None], groups=3 * C)
+    oo, _ = ref.one_by_one(*ux.split(C, 1), a[2], a[3])
+    kept = ref.keeps(5, 1, 3, B, C * L, p).view(B, C, L)
+    yy = torch.where(kept, oo / (1 - p), 0.0)
+    hat = yy / torch.sqrt(yy.square().mean(1, keepdim=True) + 1e-6)
+    ow = a[5] + torch.nn.functional.silu(a[4]) * hat * a[6][:, None]
+    nn = ow / torch.sqrt(ow.square().mean(1, keepdim=True) + 1e-6) * a[7][:, None]
+    want = torch.autograd.grad((nn * dn.double().cpu()).sum(), a)
+    # every stage keeps 32 bits: a few hundred roundings of 2^-24 of the largest value that a sum of these sizes has
+    for name, got, exact in (("n", n, nn.detach()), *zip(("dx", "dw", "dg", "dbeta", "dz", "dres", "dw1", "dw2"), (dx, dw, dg, dbeta, dz, dres, dwn, dwn2), want)):
+        assert float((got.double().cpu() - exact).abs().max()) <= 400 * 2.0 ** -24 * float(exact.abs().max()) * math.sqrt(exact.shape[-1]), name
+
+    u, o, s_last, _, _, _, n, _ = forward(False)
+    pool, ring, pos = torch.zeros(B, H, D, D, device="cuda"), torch.zeros(B, 3 * C, K, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    for t in range(L):
+        q, k, v = block.conv_step(x[..., t].contiguous(), w, ring, pos).split(C, 1)
+        y = block.delta_step(q, k, v, g[..., t].contiguous(), beta[..., t].contiguous(), pool)
+        _, one, _ = block.norm_fwd(y[..., None], z[..., t:t + 1].contiguous(), res[..., t:t + 1].contiguous(), wn, wn2, save=False)
+        pos += 1
+        assert float((one[..., 0] - n[..., t]).abs().max()) <= 400 * 2.0 ** -24 * float(n.abs().max()) * math.sqrt(L), t
+    assert float((pool - s_last).abs().max()) <= 400 * 2.0 ** -24 * float(s_last.abs().max()) * math.sqrt(L)
+
+
+def _calls():
+    q, k, v, g, beta, s0, do, ds = inputs(2, 4, 2, 8, 12, 70, BF16, seed=40)
+    lengths, slots = torch.tensor([70, 9], dtype=torch.int32, device="cuda"), torch.tensor([1, -1], dtype=torch.int32, device="cuda")
+    states = block.delta_fwd(q, k, v, g, beta, s0, lengths, 2)[2]
+    tok, s = [t[..., 0].contiguous() for t in (q, k, v, g, beta)], rand(3, 4, 8, 12, seed=3)
+    x, res, rng = rand(2, 5, 30, seed=4), rand(2, 5, 30, seed=5), torch.tensor([3, 9], device="cuda")
+    new = lambda *t: tuple(torch.full_like(a, float("nan")) for a in t)        # noqa: E731
+    space = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    wide = torch.cat([q, k, v], 1)
+    return {
+        # (states behind a sequence's end are not written)
+        "fwd": lambda: block.delta_fwd(q, k, v, g, beta, s0, lengths, 2)[:2], "fwd full": lambda: block.delta_fwd(q, k, v, g, beta, s0, None, 2), "fwd bare": lambda: block.delta_fwd(q, k, v, g, beta, key_heads=2, save=False)[:2],
+        "fwd out": lambda: block.delta_fwd(*wide.split((16, 16, 48), 1), g, beta, key_heads=2, scale=0.5, eps=0.0, out=new(v)[0], workspace=space),
+        "bwd": lambda: block.delta_bwd(do, q, k, v, g, beta, states, ds, lengths, 2), "bwd out": lambda: block.delta_bwd(do, q, k, v, g, beta, states, None, lengths, 2, out=new(q, k, v), workspace=space),
+        "step": lambda: (block.delta_step(*tok, a := s.clone(), slots, 2), a), "step out": lambda: (block.delta_step(*tok, a := s.clone(), key_heads=2, scale=2.0, out=new(tok[2])[0]), a),
+        "drop": lambda: (block.dropout_fwd(x, 0.3, rng), block.dropout_bwd(x, 0.3, rng, 5, 0.5, True)), "drop res": lambda: (block.dropout_fwd(x, 0.3, rng, 2, res, 0.5, False, new(x)[0]),),
+    }
+
+
+def test_native_calls_give_the_same(monkeypatch):
+    native = {name: call() for name, call in _calls().items()}
+    monkeypatch.setattr(block, "_fast", block._Declines)
+    for name, call in _calls().items():
+        for a, b in zip(native[name], call()):
+            assert (a is None and b is None) or torch.equal(a, b), name
+
+
+def test_native_calls_take_what_they_should(monkeypatch):
+    """Plain calls do not come back to Python."""
+    block.lib()
+    if block._fast is block._Declines:
+        pytest.skip("without the native calls")
+
+    def no(*args):
+        raise AssertionError("declined")
+    calls = _calls()
+    monkeypatch.setattr(block, "_seq", no)
+    for name, call in calls.items():
+        call()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_an_empty_workspace_is_too_small(native, monkeypatch):
+    q, k, v, g, beta, s0, do, ds = inputs(2, 2, 2, 8, 12, 70, F32)
+    states = block.delta_fwd(q, k, v, g, beta)[2]
+    if not native:
+        monkeypatch.setattr(block, "_fast", block._Declines)
+    empty = torch.empty(0, dtype=torch.uint8, device="cuda")
+    for call in (lambda: block.delta_fwd(q, k, v, g, beta, workspace=empty), lambda: block.delta_bwd(do, q, k, v, g, beta, states, workspace=empty)):
+        with pytest.raises(binding.DwconvError):
+            call()
