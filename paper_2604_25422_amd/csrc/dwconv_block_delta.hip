@@ -58,13 +58,10 @@ template <typename T, int RT> __device__ __forceinline__ void delta_step_head(co
         if (r0 == 0) store4(orow, f32x4{}, dv, p.DV);
         return;
     }
-    float *S = p.s + ((long long)slot * p.H + h) * p.DK * p.DV;
+    const StateIn S(p.s + ((long long)slot * p.H + h) * p.DK * p.DV, p.DK, p.DV);
     f32x4 x[RT];
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        const int r = r0 + i * step;
-        x[i] = r < p.DK ? load4(S + (long long)r * p.DV, dv, p.DV) : f32x4{};
-    }
+    for (int i = 0; i < RT; ++i) x[i] = S.four(r0 + i * step, dv, p.DV);
     const f32x4 v = load4(p.v.p + (long long)b * p.v.bs + (long long)h * p.DV, dv, p.DV);
     const float g = p.g.p[(long long)b * p.g.bs + h], beta = p.beta.p[(long long)b * p.beta.bs + h];
     float kv = 0.0f, qv = 0.0f;
@@ -101,17 +98,14 @@ template <typename T, int RT> __device__ __forceinline__ void delta_step_head(co
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
         const int r = r0 + i * step;
-        if (r < p.DK) store4(S + (long long)r * p.DV, x[i] * a + w * (m.k[r] * rk), dv, p.DV);
+        S.put_four(x[i] * a + w * ((r < p.DK ? m.k[r] : 0.0f) * rk), r, dv, p.DV);
     }
 }
 
-template <typename T, int RT> __global__ __launch_bounds__(256) void delta_step_kernel(DeltaStep<T> p, int lg)
+template <typename T, int RT> __global__ __launch_bounds__(256) void delta_step_kernel(DeltaStep<T> p, int lg, int first)
 {
     __shared__ StepLds m;
-    for (int unit = blockIdx.x, units = p.B * p.H * p.blocks; unit < units; unit += gridDim.x) {
-        delta_step_head<T, RT>(p, lg, unit, m);
-        __syncthreads();
-    }
+    delta_step_head<T, RT>(p, lg, first + (int)blockIdx.x, m);
 }
 
 }  // namespace dwconv
@@ -252,13 +246,10 @@ template <typename T> void launch_step(const DeltaStep<T> &in, hipStream_t st)
     while (lg < 5 && (4 << lg) < p.DV) ++lg;
     while (lg > 3 && (long long)p.B * p.H * ceil_div(p.DV, 4 << lg) < 512) --lg;
     p.blocks = (int)ceil_div(p.DV, 4 << lg);
-    const unsigned grid = (unsigned)std::min(p.B * p.H * p.blocks, kMaxUnits);
-    const int rows = (int)ceil_div(p.DK, 256 >> lg);
-    if (rows <= 1) delta_step_kernel<T, 1><<<grid, 256, 0, st>>>(p, lg);
-    else if (rows <= 2) delta_step_kernel<T, 2><<<grid, 256, 0, st>>>(p, lg);
-    else if (rows <= 4) delta_step_kernel<T, 4><<<grid, 256, 0, st>>>(p, lg);
-    else if (rows <= 8) delta_step_kernel<T, 8><<<grid, 256, 0, st>>>(p, lg);
-    else delta_step_kernel<T, 16><<<grid, 256, 0, st>>>(p, lg);
+    const int units = p.B * p.H * p.blocks, rows = (int)ceil_div(p.DK, 256 >> lg);
+    const auto kernel = rows <= 1 ? delta_step_kernel<T, 1> : rows <= 2 ? delta_step_kernel<T, 2> : rows <= 4 ? delta_step_kernel<T, 4>
+                                 : rows <= 8 ? delta_step_kernel<T, 8> : delta_step_kernel<T, 16>;
+    for (int first = 0; first < units; first += kMaxUnits) kernel<<<std::min(units - first, kMaxUnits), 256, 0, st>>>(p, lg, first);
 }
 
 template <typename T> DeltaShape<T> shape(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const int *lengths, int B, int H, int Hk,

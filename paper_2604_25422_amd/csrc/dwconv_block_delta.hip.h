@@ -594,6 +594,14 @@ struct StateIn {
         for (int v = 0; v < 4; ++v) x[v] = dv + v < DV ? x[v] : 0.0f;
         return x;
     }
+    __device__ __forceinline__ void put_four(f32x4 x, int row, int dv, int DV) const
+    {
+        if (dv + 4 <= DV) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), r, row * pitch + 4 * dv, 0, 0);
+        else
+#pragma unroll
+            for (int v = 0; v < 3; ++v)
+                if (dv + v < DV) store(x[v], row * pitch + 4 * (dv + v), 0);
+    }
 };
 // A wave's 16 columns of a state.
 template <int KT> __device__ __forceinline__ void load_state(f32x4 (&S)[KT], const StateIn &from, int dv, bool in, int g4)
