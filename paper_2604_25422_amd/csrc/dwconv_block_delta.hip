@@ -185,12 +185,13 @@ size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 size_t starts_bytes(const WalkPlan &w, int B, int H, int DK, int DV) { return w.segs > 1 ? up16((size_t)B * H * w.segs * DK * DV * sizeof(float)) : 0; }
 size_t spans_bytes(const WalkPlan &w, int B, int H, int DK, int DV) { return w.segs > 1 ? up16((size_t)B * H * w.segs * DK * (DV + DK) * sizeof(float)) : 0; }
 
-template <typename Kernel, typename P> int launch_segments(Kernel kernel, const P &p, const DeltaWalk &w, int columns, size_t lds, std::atomic<unsigned long long> &done, hipStream_t st)
+template <typename Kernel, typename P> int launch_segments(Kernel kernel, const P &p, DeltaWalk w, int columns, size_t lds, std::atomic<unsigned long long> &done, hipStream_t st)
 {
     if (!allow_lds(kernel, lds, done)) return DWCONV_ERR_LAUNCH;
-    const int units = p.B * p.H * w.segs, groups = (int)ceil_div(columns, 16 * kWalkWaves);
-    for (int first = 0; first < units; first += kMaxUnits)
-        kernel<<<dim3(std::min(units - first, kMaxUnits), groups), 64 * kWalkWaves, lds, st>>>(p, w, first);
+    w.units = p.B * p.H * w.segs, w.groups = (int)ceil_div(columns, 16 * kWalkWaves);
+    const long long ids = ceil_div(w.units, 8) * 8 * w.groups;
+    for (long long first = 0; first < ids; first += kMaxUnits)
+        kernel<<<(unsigned)std::min<long long>(ids - first, kMaxUnits), 64 * kWalkWaves, lds, st>>>(p, w, first);
     return DWCONV_OK;
 }
 // Columns of a pass that forms spans, up to whole slices of 16.
@@ -272,7 +273,7 @@ size_t walk_bytes(int B, int H, int DK, int DV, int L, bool backward)          /
 DeltaWalk walk_in(char *at, int B, int H, int DK, int DV, int L, int dtype, bool backward)
 {
     const WalkPlan w = plan_walk(B, H, DK, DV, L, dtype, backward);
-    return DeltaWalk{w.segs, w.per, reinterpret_cast<float *>(at), reinterpret_cast<float *>(at + starts_bytes(w, B, H, DK, DV))};
+    return DeltaWalk{w.segs, w.per, 0, 0, reinterpret_cast<float *>(at), reinterpret_cast<float *>(at + starts_bytes(w, B, H, DK, DV))};
 }
 constexpr int kPadded = 8;
 size_t padded_bytes(int B, int H, int DK, int DV, int L) { return L < kPadded ? up16((size_t)B * H * (2 * (DK + DV)) * kPadded * sizeof(float)) : 0; }

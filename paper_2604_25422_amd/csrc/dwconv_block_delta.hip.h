@@ -532,8 +532,15 @@ template <typename T, int KT> __global__ __launch_bounds__(256) void delta_pairs
 // A walk: H heads' chunks, `segs` workgroups a row of chunks of which each has `per` of them.
 struct DeltaWalk {
     int segs, per;
+    int units, groups;          // segments of all heads, workgroups of the columns of each
     const float *starts;        // [B, H, segs, DK, DV]: the state that a segment starts with (one segment: the call's own)
     float *spans;               // [B, H, segs, DK, DV + DK]: of the pass that forms them
+};
+
+// Workgroups go to the eight dies in turn, and each die has an L2 of its own: those of a segment's columns, which read the same keys, are eight apart.
+struct WalkPlace {
+    int unit, group;
+    __device__ __forceinline__ WalkPlace(long long id, int groups) : unit((int)(id / (8ll * groups)) * 8 + (int)(id & 7)), group((int)(id / 8 % groups)) {}
 };
 
 // (P in as many limbs as a walk takes: two for an output, three for a gradient that goes on.)
@@ -646,14 +653,14 @@ template <int KT> __device__ __forceinline__ void unit_state(f32x4 (&S)[KT], int
 }
 
 // Forward.  A workgroup has 64 columns of a head's state, a wave 16 of them in registers; it walks the chunks of its segment.
-template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_fwd_walk(const DeltaFwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT, 2> &m, int unit)
+template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_fwd_walk(const DeltaFwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT, 2> &m, int unit, int group)
 {
     typedef Mat<T> M;
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = unit / walk.segs, seg = unit % walk.segs, b = row / p.H, h = row % p.H, hk = h / p.each, n = p.length(b);
     const int from = seg * walk.per, last = min(from + walk.per, (n + 63) / 64);
     if (SPANS && seg + 1 == walk.segs) return;          // (no segment starts with what this one makes)
-    const Columns col(blockIdx.y * kWalkWaves + wave, lane0 & 15, p.DK, p.DV, SPANS);
+    const Columns col(group * kWalkWaves + wave, lane0 & 15, p.DK, p.DV, SPANS);
     const bool in = col.in;
     const long long head = row, size = (long long)p.DK * p.DV;
     f32x4 S[KT] = {};
@@ -738,26 +745,27 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
         for (int t = max(last, from) * 64 + g4, to = min(p.L, seg + 1 < walk.segs ? (from + walk.per) * 64 : p.L); t < to; t += 16) store4(orow, f32x4{}, t, p.L);
     if (p.s_last && seg + 1 == walk.segs) store_state(S, StateIn(p.s_last + head * size, p.DK, p.DV), col.at + c, in, g4);
 }
-template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWalkWaves, 2) void delta_fwd_kernel(DeltaFwd<T> p, DeltaWalk walk, int first)
+template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWalkWaves, 2) void delta_fwd_kernel(DeltaFwd<T> p, DeltaWalk walk, long long first)
 {
     extern __shared__ char lds[];
     DeltaLds<T, KT, 2> &m = *reinterpret_cast<DeltaLds<T, KT, 2> *>(lds);
     LowTiles<T, 3, 64 * kWalkWaves>::zeros(m.t);
     if (!SPANS) LowTiles<T, 2, 64 * kWalkWaves>::zeros(m.p);
-    delta_fwd_walk<T, KT, SPANS>(p, walk, m, first + (int)blockIdx.x);
+    const WalkPlace at(first + blockIdx.x, walk.groups);
+    if (at.unit < walk.units) delta_fwd_walk<T, KT, SPANS>(p, walk, m, at.unit, at.group);
 }
 
 // Backward, from chunk to chunk: with dS the gradient of the state behind a chunk,
 //     dw = P^T do + exp(G_63 - G) k dS,   (I + A)^T dr = dw,   dS <- exp(G_63) dS + sum_i exp(G_i) q_i do_i^T - beta_i exp(G_i) k_i dr_i^T.
 // Leaves dS behind every chunk, and dv = beta dr.
-template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_bwd_walk(const DeltaBwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT, 3> &m, int unit)
+template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_bwd_walk(const DeltaBwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT, 3> &m, int unit, int group)
 {
     typedef Mat<T> M;
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = unit / walk.segs, seg = unit % walk.segs, b = row / p.H, h = row % p.H, hk = h / p.each, n = p.length(b);
     const int from = seg * walk.per, last = min(from + walk.per, (n + 63) / 64);
     if (SPANS && seg == 0) return;
-    const Columns col(blockIdx.y * kWalkWaves + wave, lane0 & 15, p.DK, p.DV, SPANS);
+    const Columns col(group * kWalkWaves + wave, lane0 & 15, p.DK, p.DV, SPANS);
     const bool in = col.in;
     const long long head = row, size = (long long)p.DK * p.DV;
     f32x4 S[KT] = {};
@@ -842,13 +850,14 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
     if (SPANS) store_state(S, StateIn(walk.spans + unit * size + unit * (long long)p.DK * p.DK, p.DK, p.DV + p.DK), col.column, in, g4);
     else if (p.ds0 && seg == 0) store_state(S, StateIn(p.ds0 + head * size, p.DK, p.DV), col.at + c, in, g4);
 }
-template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWalkWaves, 2) void delta_bwd_state_kernel(DeltaBwd<T> p, DeltaWalk walk, int first)
+template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWalkWaves, 2) void delta_bwd_state_kernel(DeltaBwd<T> p, DeltaWalk walk, long long first)
 {
     extern __shared__ char lds[];
     DeltaLds<T, KT, 3> &m = *reinterpret_cast<DeltaLds<T, KT, 3> *>(lds);
     LowTiles<T, 3, 64 * kWalkWaves>::zeros(m.t);
     LowTiles<T, 3, 64 * kWalkWaves>::zeros(m.p);
-    delta_bwd_walk<T, KT, SPANS>(p, walk, m, first + (int)blockIdx.x);
+    const WalkPlace at(first + blockIdx.x, walk.groups);
+    if (at.unit < walk.units) delta_bwd_walk<T, KT, SPANS>(p, walk, m, at.unit, at.group);
 }
 
 // The states that segments start with, one after the other (forward; backward the other way): S <- N + M S with a segment's span (N, M).  A workgroup
