@@ -254,10 +254,10 @@ template <typename T> void launch_step(const DeltaStep<T> &in, hipStream_t st)
 }
 
 template <typename T> DeltaShape<T> shape(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const int *lengths, int B, int H, int Hk,
-                                          int DK, int DV, int L, float scale, float eps, void *workspace)
+                                          int DK, int DV, int L, float scale, float eps, void *workspace, bool backward)
 {
     return DeltaShape<T>{seq<T>(q), seq<T>(k), seq<T>(v), seq<float>(g), seq<float>(beta), lengths, B, H, H / Hk, DK, DV, L, chunks_of(L), L, scale, eps,
-                         static_cast<DeltaPairs *>(workspace)};
+                         static_cast<DeltaPairs *>(workspace), backward};
 }
 // A workspace: records of pairs, starts and spans of segments, backward the states' gradients behind the chunks.
 size_t pairs_bytes(int B, int H, int L) { return (size_t)B * H * chunks_of(L) * sizeof(DeltaPairs); }
@@ -333,11 +333,11 @@ int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwc
     char *const room = static_cast<char *>(workspace) + pairs_bytes(B, H, L);
     const DeltaWalk walk = walk_in(room + padded_bytes(B, H, DK, DV, L), B, H, DK, DV, L, dtype, false);
     if (dtype == DWCONV_F32) {
-        DeltaFwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<float>(o), s0, s_last, states};
+        DeltaFwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace, false), seq<float>(o), s0, s_last, states};
         pad_all<float>(p, nullptr, room, st);
         return launch_fwd(p, walk, st);
     }
-    DeltaFwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<bf16_t>(o), s0, s_last, states};
+    DeltaFwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace, false), seq<bf16_t>(o), s0, s_last, states};
     pad_all<bf16_t>(p, nullptr, room, st);
     return launch_fwd(p, walk, st);
 }
@@ -370,12 +370,12 @@ int dwconv_delta_bwd(dwconv_seq dout, dwconv_seq q, dwconv_seq k, dwconv_seq v, 
     float *after = reinterpret_cast<float *>(spans + walk_bytes(B, H, DK, DV, L, true));
     float *part = reinterpret_cast<float *>(reinterpret_cast<char *>(after) + after_bytes(B, H, DK, DV, L));
     if (dtype == DWCONV_F32) {
-        DeltaBwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<float>(dout), seq<float>(dq), seq<float>(dk),
+        DeltaBwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace, true), seq<float>(dout), seq<float>(dq), seq<float>(dk),
                           seq<float>(dv), states, ds_last, after, dg, dbeta, ds0, part};
         pad_all<float>(p, &p.dout, room, st);
         return launch_bwd(p, walk, st);
     }
-    DeltaBwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace), seq<bf16_t>(dout), seq<bf16_t>(dq), seq<bf16_t>(dk),
+    DeltaBwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace, true), seq<bf16_t>(dout), seq<bf16_t>(dq), seq<bf16_t>(dk),
                        seq<bf16_t>(dv), states, ds_last, after, dg, dbeta, ds0, part};
     pad_all<bf16_t>(p, &p.dout, room, st);
     return launch_bwd(p, walk, st);

@@ -40,6 +40,7 @@ template <typename T> struct DeltaShape {
     int pitch;                          // elements from row to row of q, k, v and dout: L, or 8 of rows that were shorter and are padded
     float scale, eps;
     struct DeltaPairs *pairs;           // [B, H, chunks]
+    bool keep;                          // all of a record is wanted (the forward pass does not look at k k^T)
     __device__ __forceinline__ int length(int b) const { return lengths ? min(max(lengths[b], 0), L) : L; }
 };
 template <typename T> struct DeltaFwd : DeltaShape<T> {
@@ -508,7 +509,7 @@ template <typename T, int KT> __device__ __forceinline__ void delta_pairs(const 
 #pragma unroll
         for (int v = 0; v < 4; ++v) e[v] = j + v < i || (is_p && j + v == i) ? exp2_of(m.s.G[i] - m.s.G[j + v]) : 0.0f;
         d = d * e * four(m.s.rk, j) * (is_p ? m.s.rq[i] : m.s.rk[i]);
-        *reinterpret_cast<f32x4 *>((is_p ? to.p : to.kk)[task >> 1] + 16 * c + g4) = d;
+        if (is_p || p.keep) *reinterpret_cast<f32x4 *>((is_p ? to.p : to.kk)[task >> 1] + 16 * c + g4) = d;
         if (!is_p) *reinterpret_cast<f32x4 *>(m.a + low_at(i, j)) = d * m.s.beta[i];
     }
     __syncthreads();
@@ -913,22 +914,23 @@ __device__ __forceinline__ f32x4 sum16(f32x4 x)
 // x[tile0 + ii] of a wave's tile0, which of KT = 8 is 0, of 4 one of two values, of 2 one of four.
 template <int KT> __device__ __forceinline__ f32x4 pick(const f32x4 (&x)[4], int ii, int tile0)
 {
-    f32x4 r = x[ii];
-    if constexpr (KT == 4) {
-        if (tile0 == 2) r = x[2 + ii];
-    } else if constexpr (KT == 2) {
-        if (tile0 == 1) r = x[1];
-        if (tile0 == 2) r = x[2];
-        if (tile0 == 3) r = x[3];
+    if constexpr (KT == 8) return x[ii];
+    // (values of their own: of a choice between array elements the compiler makes a choice between addresses, and the array goes to memory)
+    f32x4 y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        y[i] = x[i];
+        asm("" : "+v"(y[i]));
     }
-    return r;
+    if constexpr (KT == 4) return tile0 ? y[2 + ii] : y[ii];
+    else return tile0 & 2 ? (tile0 & 1 ? y[3] : y[2]) : (tile0 & 1 ? y[1] : y[0]);
 }
 
 constexpr int kGradWaves = 8;           // of a workgroup
 
 template <typename T, int KT> struct DeltaChunkLds {
     typedef typename Mat<T>::Elem Elem;
-    static constexpr int NP = Mat<T>::planes, VB = sizeof(T) == 4 && KT > 4 ? 32 : 64;     // columns of a state at a time, as LDS has room
+    static constexpr int NP = Mat<T>::planes, VB = sizeof(T) == 4 && KT != 4 ? 32 : 64;     // columns of a state at a time, as LDS has room
     Elem k[16 * KT * kPitch], t[NP * kLow], p[NP * kLow];
     union {
         struct {
