@@ -115,6 +115,11 @@ namespace {
 constexpr int kMaxKey = 128;            // channels of a key: a state's columns are registers of a wave
 constexpr int kMaxUnits = 1 << 22;      // workgroups of a launch, whose lanes stay below 2^32
 
+template <typename Launch> void for_units(int units, Launch launch)
+{
+    for (long long first = 0; first < units; first += kMaxUnits) launch((int)first, (int)std::min<long long>(units - first, kMaxUnits));
+}
+
 int chunks_of(int L) { return (int)ceil_div(L, kDeltaChunk); }
 
 int check_heads(int B, int H, int Hk, int DK, int DV, int L)
@@ -151,7 +156,7 @@ template <typename T, int KT> int launch_pairs(const DeltaShape<T> &p, hipStream
     const size_t lds = sizeof(PairsLds<T, KT>);
     if (!allow_lds(delta_pairs_kernel<T, KT>, lds, done)) return DWCONV_ERR_LAUNCH;
     const int units = p.B * p.H * p.chunks;
-    for (int first = 0; first < units; first += kMaxUnits) delta_pairs_kernel<T, KT><<<std::min(units - first, kMaxUnits), 256, lds, st>>>(p, first);
+    for_units(units, [&](int first, int n) { delta_pairs_kernel<T, KT><<<n, 256, lds, st>>>(p, first); });
     return DWCONV_OK;
 }
 
@@ -219,7 +224,7 @@ template <typename T, int KT> int launch_bwd(const DeltaBwd<T> &p, const DeltaWa
 {
     static std::atomic<unsigned long long> done[4];
     constexpr size_t lds = sizeof(DeltaLds<T, KT, 3>), chunk = sizeof(DeltaChunkLds<T, KT>);
-    static_assert(lds <= 160 * 1024 && chunk <= 160 * 1024, "LDS of a CU");
+    static_assert(lds <= 160 * 1024 && chunk <= 80 * 1024, "LDS of a CU");
     int rc = launch_pairs<T, KT>(p, st);
     if (rc == DWCONV_OK && w.segs > 1) {
         rc = launch_segments(delta_bwd_state_kernel<T, KT, true>, p, w, span_columns(p.DK, p.DV), lds, done[1], st);
@@ -230,8 +235,8 @@ template <typename T, int KT> int launch_bwd(const DeltaBwd<T> &p, const DeltaWa
     if (rc == DWCONV_OK && !allow_lds(kernel, chunk, done[p.each > 1 ? 3 : 2])) rc = DWCONV_ERR_LAUNCH;
     if (rc != DWCONV_OK) return rc;
     const int units = p.B * p.H * p.chunks, shared = p.each > 1 ? units / p.each : 0;
-    for (int first = 0; first < units; first += kMaxUnits) kernel<<<std::min(units - first, kMaxUnits), 64 * kGradWaves, chunk, st>>>(p, first);
-    for (int first = 0; first < shared; first += kMaxUnits) delta_share_kernel<T, KT><<<std::min(shared - first, kMaxUnits), 512, 0, st>>>(p, first);
+    for_units(units, [&](int first, int n) { kernel<<<n, 64 * kGradWaves, chunk, st>>>(p, first); });
+    for_units(shared, [&](int first, int n) { delta_share_kernel<T, KT><<<n, 512, 0, st>>>(p, first); });
     return launch_status();
 }
 template <typename T> int launch_bwd(const DeltaBwd<T> &p, const DeltaWalk &w, hipStream_t st)
@@ -250,7 +255,7 @@ template <typename T> void launch_step(const DeltaStep<T> &in, hipStream_t st)
     const int units = p.B * p.H * p.blocks, rows = (int)ceil_div(p.DK, 256 >> lg);
     const auto kernel = rows <= 1 ? delta_step_kernel<T, 1> : rows <= 2 ? delta_step_kernel<T, 2> : rows <= 4 ? delta_step_kernel<T, 4>
                                  : rows <= 8 ? delta_step_kernel<T, 8> : delta_step_kernel<T, 16>;
-    for (int first = 0; first < units; first += kMaxUnits) kernel<<<std::min(units - first, kMaxUnits), 256, 0, st>>>(p, lg, first);
+    for_units(units, [&](int first, int n) { kernel<<<n, 256, 0, st>>>(p, lg, first); });
 }
 
 template <typename T> DeltaShape<T> shape(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const int *lengths, int B, int H, int Hk,
@@ -297,6 +302,7 @@ template <typename T> void pad_all(DeltaShape<T> &p, Seq<T> *dout, void *room, h
     p.pitch = kPadded;
 }
 size_t after_bytes(int B, int H, int DK, int DV, int L) { return up16((size_t)B * H * chunks_of(L) * DK * DV * sizeof(float)); }
+size_t dr_bytes(int B, int H, int DV, int L) { return (size_t)B * H * chunks_of(L) * DV * kDeltaChunk * sizeof(float); }
 size_t part_bytes(int B, int H, int DK, int L, bool shared) { return shared ? up16((size_t)B * H * 2 * DK * L * sizeof(float)) : 0; }
 
 }  // namespace
@@ -308,7 +314,7 @@ int dwconv_delta_states(int L) { return L < 1 || L > (1 << 30) ? 0 : chunks_of(L
 size_t dwconv_delta_workspace_bytes(int B, int H, int Hk, int DK, int DV, int L, int backward)
 {
     if (check_heads(B, H, Hk, DK, DV, L) != DWCONV_OK) return 0;
-    return pairs_bytes(B, H, L) + padded_bytes(B, H, DK, DV, L) + walk_bytes(B, H, DK, DV, L, backward != 0) + (backward ? after_bytes(B, H, DK, DV, L) + part_bytes(B, H, DK, L, Hk < H) : 0);
+    return pairs_bytes(B, H, L) + padded_bytes(B, H, DK, DV, L) + walk_bytes(B, H, DK, DV, L, backward != 0) + (backward ? after_bytes(B, H, DK, DV, L) + dr_bytes(B, H, DV, L) + part_bytes(B, H, DK, L, Hk < H) : 0);
 }
 
 int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const float *s0, const int *lengths, dwconv_seq_out o,
@@ -368,15 +374,16 @@ int dwconv_delta_bwd(dwconv_seq dout, dwconv_seq q, dwconv_seq k, dwconv_seq v, 
     char *const room = static_cast<char *>(workspace) + pairs_bytes(B, H, L), *const spans = room + padded_bytes(B, H, DK, DV, L);
     const DeltaWalk walk = walk_in(spans, B, H, DK, DV, L, dtype, true);
     float *after = reinterpret_cast<float *>(spans + walk_bytes(B, H, DK, DV, L, true));
-    float *part = reinterpret_cast<float *>(reinterpret_cast<char *>(after) + after_bytes(B, H, DK, DV, L));
+    float *dr = reinterpret_cast<float *>(reinterpret_cast<char *>(after) + after_bytes(B, H, DK, DV, L));
+    float *part = reinterpret_cast<float *>(reinterpret_cast<char *>(dr) + dr_bytes(B, H, DV, L));
     if (dtype == DWCONV_F32) {
         DeltaBwd<float> p{shape<float>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace, true), seq<float>(dout), seq<float>(dq), seq<float>(dk),
-                          seq<float>(dv), states, ds_last, after, dg, dbeta, ds0, part};
+                          seq<float>(dv), states, ds_last, after, dr, dg, dbeta, ds0, part};
         pad_all<float>(p, &p.dout, room, st);
         return launch_bwd(p, walk, st);
     }
     DeltaBwd<bf16_t> p{shape<bf16_t>(q, k, v, g, beta, lengths, B, H, Hk, DK, DV, L, scale, eps, workspace, true), seq<bf16_t>(dout), seq<bf16_t>(dq), seq<bf16_t>(dk),
-                       seq<bf16_t>(dv), states, ds_last, after, dg, dbeta, ds0, part};
+                       seq<bf16_t>(dv), states, ds_last, after, dr, dg, dbeta, ds0, part};
     pad_all<bf16_t>(p, &p.dout, room, st);
     return launch_bwd(p, walk, st);
 }

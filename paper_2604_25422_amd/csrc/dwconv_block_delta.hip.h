@@ -52,15 +52,19 @@ template <typename T> struct DeltaBwd : DeltaShape<T> {
     Seq<T> dout;
     SeqOut<T> dq, dk, dv;
     const float *states, *ds_last;
-    float *after, *dg, *dbeta, *ds0;    // after: [B, H, chunks, DK, DV], the gradient of the state behind a chunk
+    float *after, *dr;                  // [B, H, chunks, DK, DV], the gradient of the state behind a chunk; [B, H, chunks, DV, 64], of beta (v - S~^T k)
+    float *dg, *dbeta, *ds0;
     float *part;                        // [B, H, 2, DK, L]: of shared keys, what each head adds to dq and dk
 };
 
 // The per-position values of a chunk.
-struct Gates {
-    float eG[64], eC[64];       // exp(G_t), exp(G_63 - G_t)
-    float beta[64], rk[64], iq[64], rq[64];     // 1 / lengths of k and q; scale / length of q
+struct ChunkGates {
     double G[64];               // sums of the log decays, times log2(e)
+    float eG[64], eC[64];       // exp(G_t), exp(G_63 - G_t)
+    float beta[64], rk[64], iq[64];     // 1 / lengths of k and q
+};
+struct Gates : ChunkGates {
+    float rq[64];               // scale / length of q
 };
 // What a chunk's walk needs that does not depend on the state: the lower triangles of T, P and k k^T e, in blocks of 16 row by row.
 struct DeltaPairs {
@@ -758,7 +762,7 @@ template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWal
 
 // Backward, from chunk to chunk: with dS the gradient of the state behind a chunk,
 //     dw = P^T do + exp(G_63 - G) k dS,   (I + A)^T dr = dw,   dS <- exp(G_63) dS + sum_i exp(G_i) q_i do_i^T - beta_i exp(G_i) k_i dr_i^T.
-// Leaves dS behind every chunk, and dv = beta dr.
+// Leaves dS behind every chunk, dr (whole, what needs it next does not form it again) and dv = beta dr.
 template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_bwd_walk(const DeltaBwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT, 3> &m, int unit, int group)
 {
     typedef Mat<T> M;
@@ -824,6 +828,11 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
             const typename M::Full x = M::split(w[2 * kb], w[2 * kb + 1]);
 #pragma unroll
             for (int j = 0; j < 2 * kb + 2; ++j) r[j] = M::mma(M::low_columns(m.t, 16 * j, kb, lane), x, r[j]);
+        }
+        if (!SPANS && in) {
+            float *to = p.dr + ((head * p.chunks + ch) * p.DV + dv) * 64 + g4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4 *>(to + 16 * i) = r[i];
         }
         const float eA = m.s.eG[63];
 #pragma unroll
@@ -911,55 +920,58 @@ __device__ __forceinline__ f32x4 sum16(f32x4 x)
     return x;
 }
 
-// x[tile0 + ii] of a wave's tile0, which of KT = 8 is 0, of 4 one of two values, of 2 one of four.
-template <int KT> __device__ __forceinline__ f32x4 pick(const f32x4 (&x)[4], int ii, int tile0)
+// x[tile0 + ii] of a wave's N tiles: all four, or two of which tile0 is 0 or 2.
+template <int N> __device__ __forceinline__ f32x4 pick(const f32x4 (&x)[4], int ii, int tile0)
 {
-    if constexpr (KT == 8) return x[ii];
+    if constexpr (N == 4) return x[ii];
     // (values of their own: of a choice between array elements the compiler makes a choice between addresses, and the array goes to memory)
-    f32x4 y[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        y[i] = x[i];
-        asm("" : "+v"(y[i]));
-    }
-    if constexpr (KT == 4) return tile0 ? y[2 + ii] : y[ii];
-    else return tile0 & 2 ? (tile0 & 1 ? y[3] : y[2]) : (tile0 & 1 ? y[1] : y[0]);
+    f32x4 low = x[ii], high = x[(2 + ii) & 3];
+    asm("" : "+v"(low));
+    asm("" : "+v"(high));
+    return tile0 ? high : low;
 }
 
-constexpr int kGradWaves = 8;           // of a workgroup
+constexpr int kGradWaves = 4;           // of a workgroup; two of those fit a CU
 
 template <typename T, int KT> struct DeltaChunkLds {
     typedef typename Mat<T>::Elem Elem;
-    static constexpr int NP = Mat<T>::planes, VB = sizeof(T) == 4 && KT != 4 ? 32 : 64;     // columns of a state at a time, as LDS has room
-    Elem k[16 * KT * kPitch], t[NP * kLow], p[NP * kLow];
+    static constexpr int NP = Mat<T>::planes, N2 = NP < 2 ? NP : 2, VB = 32;        // columns of a state at a time
+    static constexpr int G = KT < kGradWaves ? KT : kGradWaves;                     // groups of the key's channels
+    Elem k[16 * KT * kPitch], t[NP * kLow];
     union {
         struct {
             Elem dout[VB * kPitch], w[NP * VB * kPitch], dr[NP * VB * kPitch];
         };
-        float pairs[64 * kPitch];
+        struct {
+            float pairs[kLow];
+            Elem p[N2 * kLow];
+        };
     };
-    Gates s;
-    float part[3][KT][64], db[VB / 16][64], da[4][64], dg[4][64], whole[KT];
+    ChunkGates s;
+    float part[3][G][64], da[4][64], dg[4][64], whole[G];
 };
 
-// Backward, within a chunk, all chunks at once: from the states in front of it and the gradient of that behind it
+// Backward, within a chunk, all chunks at once: from the states in front of it, the gradient of that behind it and dr
 //     dP = do w^T (j <= i),   dA = -dr w^T (j < i),   dq_i = exp(G_i) S do_i + sum_j dP_ij e(i, j) k_j,
 //     dk_j = sum_i dP_ij e(i, j) q_i + sum_i (D + D^T)_ji k_i - beta_j exp(G_j) S dr_j + exp(G_63 - G_j) dS w_j,   D_ij = beta_i dA_ij e(i, j).
 // A decay at t scales what lies in front of it for what lies from it on: with W = dP P + dA A
 //     dg_t = exp(G_63) <dS, S> + sum_{i >= t} x_i + sum_{j < t} y_j + sum_{i >= t > j} W_ij,
 // x_i what row i took of S and y_j what is left of column j in S'.  (As a difference of whole sums, which is shorter, it would be
-// the rounding of those where a decay is strong.)  A workgroup has a chunk of a head.  First 16 columns of w or dr a wave, then 16 channels of the key
-// and NI of the four tiles of 16 positions.  SHARED: dq and dk of q and k of unit length go to part_q and part_k, which delta_share_kernel adds up.
+// the rounding of those where a decay is strong.)  A workgroup has a chunk of a head, 32 columns of its states at a time.  First a wave has 16 columns
+// of w, all of k^T S and two tiles of T times that (which gives the same k^T S twice, and keeps all four waves at work); then SL slices of 16
+// channels of the key and NI tiles of 16 positions.  SHARED: dq and dk of q and k of unit length go to part_q and part_k, which delta_share_kernel adds up.
 template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta_bwd_chunk(const DeltaBwd<T> &p, DeltaChunkLds<T, KT> &m, int unit)
 {
     typedef Mat<T> M;
     typedef typename M::Full Full;
     typedef DeltaChunkLds<T, KT> Lds;
-    constexpr int W = kGradWaves, VB = Lds::VB, NS = VB / 16, VP = VB * kPitch, NI = KT / 2;
+    constexpr int W = kGradWaves, VB = Lds::VB, VP = VB * kPitch, G = Lds::G, SL = KT / G, NI = G, TASKS = (10 + W - 1) / W;
+    static_assert(VB == 32 && W == 4, "a wave has 16 columns of w and half of their rows");
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int ch = unit % p.chunks, head = unit / p.chunks, b = head / p.H, h = head % p.H, hk = h / p.each;
     const int n = p.length(b), t0 = ch * kDeltaChunk;
-    const int slice = wave % KT, tile0 = wave / KT * NI;            // this wave's channels of the key, and tiles of positions
+    const int group = wave % G, slice0 = group * SL, tile0 = wave / G * NI;         // this wave's channels of the key, and tiles of positions
+    const int half = wave >> 1;
     T *const dq_row = SHARED ? nullptr : p.dq.row(b, hk * p.DK, p.L), *const dk_row = SHARED ? nullptr : p.dk.row(b, hk * p.DK, p.L);
     float *const part_q = p.part + ((long long)head * 2 * p.DK) * p.L, *const part_k = part_q + (long long)p.DK * p.L;
     if (t0 >= n) {
@@ -969,43 +981,44 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
                 if (t0 + (i & 63) < p.L) dq_row[(long long)(i >> 6) * p.L + t0 + (i & 63)] = dk_row[(long long)(i >> 6) * p.L + t0 + (i & 63)] = T{};
         return;
     }
-    const float *states = p.states + (long long)unit * p.DK * p.DV, *grads = p.after + (long long)unit * p.DK * p.DV;
-    const StateIn before(states, p.DK, p.DV), after(grads, p.DK, p.DV);
+    const StateIn before(p.states + (long long)unit * p.DK * p.DV, p.DK, p.DV), after(p.after + (long long)unit * p.DK * p.DV, p.DK, p.DV);
     const DeltaPairs &pairs = p.pairs[unit];
     const T *const values = p.v.row(b, h * p.DV, p.pitch), *const douts = p.dout.row(b, h * p.DV, p.pitch);
-    // What w and dr take from memory, a step ahead: an even wave has 16 columns of w, an odd one of dr.
-    f32x4 S[KT];
-    Rows<T> vrow, drow;
+    const float *const drs = p.dr + (long long)unit * p.DV * 64;
+    // What the first step takes from memory, ahead of it.
+    f32x4 S[KT], dr[2];
+    Rows<T> vrow;
+    Tile<T, VB, 64 * W> drow;
     const auto fetch = [&](int v0) __attribute__((always_inline)) {
-        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dv = v0 + 16 * (wave >> 1) + c;
-        const bool in = dv < p.DV && wave < 2 * NS;
-        load_state(S, StateIn(wave & 1 ? grads : states, p.DK, p.DV), dv, in, g4);
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dv = v0 + 16 * (wave & 1) + c;
+        const bool in = dv < p.DV;
+        load_state(S, before, dv, in, g4);
         vrow.load(values + (long long)(in ? dv : 0) * p.pitch, t0, g4, p.pitch);
-        drow.load(douts + (long long)(in ? dv : 0) * p.pitch, t0, g4, p.pitch);
+        drow.load(douts + (long long)v0 * p.pitch, p.DV - v0, t0, p.pitch);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) dr[i] = four(drs + (long long)(in ? dv : 0) * 64, 32 * half + 16 * i + g4);
     };
     {
         Tile<T, 16 * KT, 64 * W> kt;
-        LowTiles<T, 3, 64 * W> t, u;
+        LowTiles<T, 3, 64 * W> t;
         kt.load(p.k.row(b, hk * p.DK, p.pitch), p.DK, t0, p.pitch);
         t.load(pairs.t);
-        u.load(pairs.p);
-        const f32x4 gates = reinterpret_cast<const f32x4 *>(&pairs.s)[threadIdx.x < sizeof(Gates) / 16 ? threadIdx.x : 0];
+        const f32x4 gates = reinterpret_cast<const f32x4 *>(&pairs.s)[threadIdx.x < sizeof(ChunkGates) / 16 ? threadIdx.x : 0];
         fetch(0);
         kt.put(m.k, p.DK, t0, n, p.pitch);
         t.put(m.t);
-        u.put(m.p);
-        if (threadIdx.x < sizeof(Gates) / 16) reinterpret_cast<f32x4 *>(&m.s)[threadIdx.x] = gates;
-        if (threadIdx.x < NS * 64) m.db[0][threadIdx.x] = 0.0f;
+        if (threadIdx.x < sizeof(ChunkGates) / 16) reinterpret_cast<f32x4 *>(&m.s)[threadIdx.x] = gates;
+        if (threadIdx.x < 128) m.dg[0][threadIdx.x] = 0.0f;             // (at first dr v, of even columns' waves and odd ones')
     }
     __syncthreads();
-    f32x4 dp[2] = {}, da[2] = {};           // of this wave's tiles of pairs, transposed: lane (c, g) has columns 16 tj + 4 g + v of row 16 ti + c
-    f32x4 x1[NI] = {}, x2[NI] = {}, x3[NI] = {};    // do S^T, dr S^T, w dS^T: rows of positions, 16 channels of the key
+    f32x4 dp[TASKS] = {}, da[TASKS] = {};   // of this wave's tiles of pairs, transposed: lane (c, g) has columns 16 tj + 4 g + v of row 16 ti + c
+    f32x4 x1[SL][NI] = {}, x2[SL][NI] = {}, x3[SL][NI] = {};    // do S^T, dr S^T, w dS^T: rows of positions, 16 channels of the key
     float whole = 0.0f;
 #pragma unroll 1
     for (int v0 = 0; v0 < p.DV; v0 += VB) {
-        if (wave < 2 * NS) {
-            const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), sl = wave >> 1, row = (16 * sl + c) * kPitch + g4;
-            f32x4 x[4] = {}, y[4] = {};
+        {
+            const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), row = (16 * (wave & 1) + c) * kPitch + g4;
+            f32x4 x[4] = {}, val[4];
 #pragma unroll
             for (int kb = 0; kb < KT; kb += 2) {
                 const Full s = M::split(S[kb], S[kb + 1]);
@@ -1013,143 +1026,145 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
                 for (int i = 0; i < 4; ++i) x[i] = M::mma(M::columns_in(m.k, 16 * i, 16 * kb, lane), s, x[i]);
                 step_done();
             }
-            const bool out = v0 + 16 * sl + c >= p.DV;
-            if (wave & 1) {
-                f32x4 d[4];
-                drow.get(d, t0, g4, n, p.pitch);
+            const bool out = v0 + 16 * (wave & 1) + c >= p.DV;
+            vrow.get(val, t0, g4, n, p.pitch);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (out) d[i] = f32x4{};
-                    x[i] *= four(m.s.eC, 16 * i + g4) * four(m.s.rk, 16 * i + g4);
-                    M::template put<1>(m.dout, 0, row + 16 * i, d[i]);
-                }
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    const typename M::In z = M::exact(d[2 * kb], d[2 * kb + 1]);
-#pragma unroll
-                    for (int j = 0; j < 2 * kb + 2; ++j) x[j] = M::mma(M::low_columns(m.p, 16 * j, kb, lane), z, x[j]);
-                    step_done();
-                }
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    const Full z = M::split(x[2 * kb], x[2 * kb + 1]);
-#pragma unroll
-                    for (int j = 0; j < 2 * kb + 2; ++j) y[j] = M::mma(M::low_columns(m.t, 16 * j, kb, lane), z, y[j]);
-                    step_done();
-                }
-                f32x4 val[4];
-                vrow.get(val, t0, g4, n, p.pitch);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    M::put(m.dr, VP, row + 16 * i, y[i]);
-                    if (out) val[i] = f32x4{};
-                    const f32x4 s = sum16(y[i] * val[i]);
-                    if (c == 0) *reinterpret_cast<f32x4 *>(&m.db[sl][16 * i + g4]) += s;
-                }
-            } else {
-                f32x4 val[4];
-                vrow.get(val, t0, g4, n, p.pitch);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = 16 * i + g4;
-                    if (out) val[i] = f32x4{};
-                    x[i] = four(m.s.beta, t) * (val[i] - four(m.s.eG, t) * four(m.s.rk, t) * x[i]);
-                }
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    const Full z = M::split(x[2 * kb], x[2 * kb + 1]);
-#pragma unroll
-                    for (int i = 2 * kb; i < 4; ++i) y[i] = M::mma(M::low_rows(m.t, 16 * i, kb, lane), z, y[i]);
-                    step_done();
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) M::put(m.w, VP, row + 16 * i, y[i]);
+            for (int i = 0; i < 4; ++i) {
+                const int t = 16 * i + g4;
+                if (out) val[i] = f32x4{};
+                x[i] = four(m.s.beta, t) * (val[i] - four(m.s.eG, t) * four(m.s.rk, t) * x[i]);
             }
+            const int near = 16 * half, far = 48 - 16 * half;           // tiles 0 and 3, or 1 and 2: of three blocks 32 wide either way
+            const Full z0 = M::split(x[0], x[1]), z1 = M::split(x[2], x[3]);
+            const f32x4 yn = M::mma(M::low_rows(m.t, near, 0, lane), z0, f32x4{});
+            step_done();
+            const f32x4 yf = M::mma(M::low_rows(m.t, far, 1, lane), z1, M::mma(M::low_rows(m.t, far, 0, lane), z0, f32x4{}));
+            M::put(m.w, VP, row + near, yn);
+            M::put(m.w, VP, row + far, yf);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (out) dr[i] = f32x4{};
+                const f32x4 sum = sum16(dr[i] * pick<2>(val, i, 2 * half));
+                if (c == 0) *reinterpret_cast<f32x4 *>(&m.dg[wave & 1][32 * half + 16 * i + g4]) += sum;
+                M::put(m.dr, VP, row + 32 * half + 16 * i, dr[i]);
+            }
+            drow.put(m.dout, p.DV - v0, t0, n, p.pitch);
+            step_done();
         }
         {
-            const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dk = 16 * slice + c;
-            f32x4 a[VB / 16], e[VB / 16];
+            const int lane = fresh(lane0), g4 = 4 * (lane >> 4);
+            f32x4 a[SL][2], e[SL][2];
 #pragma unroll
-            for (int kb = 0; kb < VB / 16; ++kb) a[kb] = before.four(dk, v0 + 16 * kb + g4, p.DV), e[kb] = after.four(dk, v0 + 16 * kb + g4, p.DV);
-            __syncthreads();
+            for (int s = 0; s < SL; ++s)
 #pragma unroll
-            for (int kb = 0; kb < VB / 16; kb += 2) {
-                const int lane = fresh(lane0);
-#pragma unroll
-                for (int v = 0; v < 4; ++v) whole = fmaf(a[kb][v], e[kb][v], whole), whole = fmaf(a[kb + 1][v], e[kb + 1][v], whole);
-                const Full s0 = M::split(a[kb], a[kb + 1]), s1 = M::split(e[kb], e[kb + 1]);
-#pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    const int ti = 16 * (tile0 + i);
-                    x1[i] = M::mma(M::columns_in(m.dout, ti, 16 * kb, lane), s0, x1[i]);
-                    x2[i] = M::mma(M::columns(m.dr, VP, ti, 16 * kb, lane), s0, x2[i]);
-                    x3[i] = M::mma(M::columns(m.w, VP, ti, 16 * kb, lane), s1, x3[i]);
-                    step_done();
+                for (int kb = 0; kb < 2; ++kb) {
+                    const int dk = 16 * (slice0 + s) + (lane & 15);
+                    a[s][kb] = before.four(dk, v0 + 16 * kb + g4, p.DV), e[s][kb] = after.four(dk, v0 + 16 * kb + g4, p.DV);
                 }
+            __syncthreads();
+            Full z[SL];
+#pragma unroll
+            for (int s = 0; s < SL; ++s) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v) whole = fmaf(a[s][0][v], e[s][0][v], whole), whole = fmaf(a[s][1][v], e[s][1][v], whole);
+                z[s] = M::split(a[s][0], a[s][1]);
+                step_done();
+            }
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int ti = 16 * (tile0 + i);
+                const typename M::In d = M::columns_in(m.dout, ti, 0, lane);
+                const Full r = M::columns(m.dr, VP, ti, 0, lane);
+#pragma unroll
+                for (int s = 0; s < SL; ++s) x1[s][i] = M::mma(d, z[s], x1[s][i]), x2[s][i] = M::mma(r, z[s], x2[s][i]);
+                step_done();
+            }
+#pragma unroll
+            for (int s = 0; s < SL; ++s) z[s] = M::split(e[s][0], e[s][1]);
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const Full w = M::columns(m.w, VP, 16 * (tile0 + i), 0, lane);
+#pragma unroll
+                for (int s = 0; s < SL; ++s) x3[s][i] = M::mma(w, z[s], x3[s][i]);
+                step_done();
             }
         }
-        if (v0 + VB < p.DV) fetch(v0 + VB);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < TASKS; ++u) {
             const int task = wave + u * W;
             if (task >= 10) continue;
             const int lane = fresh(lane0);
             int ti, tj;
             low_tile(task, ti, tj);
-#pragma unroll
-            for (int kb = 0; kb < VB; kb += 32) {
-                const Full wj = M::columns(m.w, VP, 16 * tj, kb, lane);
-                dp[u] = M::mma(wj, M::columns_in(m.dout, 16 * ti, kb, lane), dp[u]);
-                da[u] = M::mma(wj, M::columns(m.dr, VP, 16 * ti, kb, lane), da[u]);
-                step_done();
-            }
+            const Full wj = M::columns(m.w, VP, 16 * tj, 0, lane);
+            dp[u] = M::mma(wj, M::columns_in(m.dout, 16 * ti, 0, lane), dp[u]);
+            da[u] = M::mma(wj, M::columns(m.dr, VP, 16 * ti, 0, lane), da[u]);
+            step_done();
         }
+        if (v0 + VB < p.DV) fetch(v0 + VB);
         __syncthreads();
     }
+    LowTiles<T, Lds::N2, 64 * W>::zeros(m.p);
     // (what the ends take from memory)
-    Rows<T> qrow;
-    f32x4 kk[2], pp[2];
+    f32x4 kk[TASKS], pp[TASKS], qh[SL][4];          // q of unit length, as kh() is k's
     {
-        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dk = 16 * slice + c;
-        qrow.load(p.q.row(b, hk * p.DK + (dk < p.DK ? dk : 0), p.pitch), t0, g4, p.pitch);
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
+        Rows<T> qrow[SL];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int s = 0; s < SL; ++s) {
+            const int dk = 16 * (slice0 + s) + c;
+            qrow[s].load(p.q.row(b, hk * p.DK + (dk < p.DK ? dk : 0), p.pitch), t0, g4, p.pitch);
+        }
+#pragma unroll
+        for (int u = 0; u < TASKS; ++u) {
             const int task = min(wave + u * W, 9);
             kk[u] = four(pairs.kk[task], 16 * c + g4), pp[u] = four(pairs.p[task], 16 * c + g4);
         }
-    }
-    f32x4 kh[4], qh[4];
-    {
-        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dk = 16 * slice + c;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) kh[i] = M::wide(m.k, dk * kPitch + 16 * i + g4) * four(m.s.rk, 16 * i + g4);
-        qrow.get(qh, t0, g4, n, p.pitch);
+        for (int s = 0; s < SL; ++s) {
+            qrow[s].get(qh[s], t0, g4, n, p.pitch);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            qh[i] *= four(m.s.rq, 16 * i + g4);
-            if (dk >= p.DK) qh[i] = f32x4{};
+            for (int i = 0; i < 4; ++i) {
+                qh[s][i] *= four(m.s.iq, 16 * i + g4);
+                if (16 * (slice0 + s) + c >= p.DK) qh[s][i] = f32x4{};
+            }
         }
+    }
+    const auto kh = [&](int s, int i, int lane) __attribute__((always_inline)) {
+        const int t = 16 * i + 4 * (lane >> 4);
+        return M::wide(m.k, (16 * (slice0 + s) + (lane & 15)) * kPitch + t) * four(m.s.rk, t);
+    };
+    {
+        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
 #pragma unroll
         for (int ii = 0; ii < NI; ++ii) {
             const int i = tile0 + ii, t = 16 * i + g4;
-            const f32x4 beta = four(m.s.beta, t), k = pick<KT>(kh, ii, tile0), q = pick<KT>(qh, ii, tile0);
-            x1[ii] *= four(m.s.eG, t);
-            x2[ii] *= -four(m.s.eG, t);
-            x3[ii] *= four(m.s.eC, t);
-            const f32x4 bx = k * x2[ii], xs = sum16(q * x1[ii] + beta * bx), ys = sum16(k * x3[ii]), bs = sum16(bx);
-            if (c == 0) {
-                *reinterpret_cast<f32x4 *>(&m.part[0][slice][t]) = xs;
-                *reinterpret_cast<f32x4 *>(&m.part[1][slice][t]) = ys;
-                *reinterpret_cast<f32x4 *>(&m.part[2][slice][t]) = bs;
+            const f32x4 beta = four(m.s.beta, t), in = four(m.s.eG, t), left = four(m.s.eC, t);
+            f32x4 xs = {}, ys = {}, bs = {};
+#pragma unroll
+            for (int s = 0; s < SL; ++s) {
+                const f32x4 k = kh(s, i, lane), q = pick<NI>(qh[s], ii, tile0);
+                x1[s][ii] *= in * p.scale;
+                x2[s][ii] *= -in;
+                x3[s][ii] *= left;
+                const f32x4 bx = k * x2[s][ii];
+                xs += q * x1[s][ii] + beta * bx, ys += k * x3[s][ii], bs += bx;
+                x2[s][ii] = beta * x2[s][ii] + x3[s][ii];       // from here on: x1 is dq, x2 is dk
             }
-            x2[ii] = beta * x2[ii] + x3[ii];        // from here on: x1 is dq, x2 is dk
+            xs = sum16(xs), ys = sum16(ys), bs = sum16(bs);
+            if (i >> 1 == half) bs += four(m.dg[wave & 1], t);
+            if (c == 0) {
+                *reinterpret_cast<f32x4 *>(&m.part[0][group][t]) = xs;
+                *reinterpret_cast<f32x4 *>(&m.part[1][group][t]) = ys;
+                *reinterpret_cast<f32x4 *>(&m.part[2][group][t]) = bs;
+            }
         }
         whole = group_sum(whole, 6);
-        if (lane == 0 && wave < KT) m.whole[slice] = whole;
+        if (lane == 0 && wave < G) m.whole[group] = whole;
     }
-    // the pairs' gradients, in the place of the pairs
+    // the pairs' gradients
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int u = 0; u < TASKS; ++u) {
         const int task = wave + u * W;
         if (task >= 10) continue;
         const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
@@ -1168,9 +1183,9 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
         sum += __shfl_xor(sum, 16, 64);
         sum += __shfl_xor(sum, 32, 64);
         if (lane < 16) m.da[tj][i] = sum;
-        M::template put<2>(m.p, kLow, low_at(i, j), dP * e);
+        M::template put<2>(m.p, kLow, low_at(i, j), dP * e * p.scale);
         M::template put<2>(m.t, kLow, low_at(i, j), dA * e * m.s.beta[i]);
-        *reinterpret_cast<f32x4 *>(m.pairs + i * kPitch + j) = dP * pp[u] + x * m.s.beta[i];
+        *reinterpret_cast<f32x4 *>(m.pairs + low_at(i, j)) = dP * pp[u] + x * m.s.beta[i];
     }
     __syncthreads();
     // pairs of a row from t on and a column before t: products with ones above the diagonal, then the rows from t on, a tile a wave
@@ -1183,7 +1198,7 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
             f32x4 ones;
 #pragma unroll
             for (int v = 0; v < 4; ++v) ones[v] = 16 * j + g4 + v < 16 * tt + c ? 1.0f : 0.0f;
-            x = mma16(rows_of(m.pairs, 16 * ti, 16 * j, lane), ones, x);
+            x = mma16(rows_of(m.pairs + low_at(16 * ti, 16 * j), 0, 0, lane, low_pitch(16 * ti)), ones, x);
         }
         float sum = 0.0f;
 #pragma unroll
@@ -1195,30 +1210,39 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
         const int lane = fresh(lane0);
-        const Full kz = M::template split<2>(kh[2 * kb], kh[2 * kb + 1]), qz = M::template split<2>(qh[2 * kb], qh[2 * kb + 1]);
+        Full kz[SL], qz[SL];
+#pragma unroll
+        for (int s = 0; s < SL; ++s) {
+            kz[s] = M::template split<2>(kh(s, 2 * kb, lane), kh(s, 2 * kb + 1, lane));
+            qz[s] = M::template split<2>(qh[s][2 * kb], qh[s][2 * kb + 1]);
+        }
 #pragma unroll
         for (int ii = 0; ii < NI; ++ii) {
             const int i = tile0 + ii;
             if (2 * kb <= i) {
-                x1[ii] = M::template mma<2>(M::template low_rows<2>(m.p, 16 * i, kb, lane), kz, x1[ii]);
-                x2[ii] = M::template mma<2>(M::template low_rows<2>(m.t, 16 * i, kb, lane), kz, x2[ii]);
+                const Full x = M::template low_rows<2>(m.p, 16 * i, kb, lane), y = M::template low_rows<2>(m.t, 16 * i, kb, lane);
+#pragma unroll
+                for (int s = 0; s < SL; ++s) x1[s][ii] = M::template mma<2>(x, kz[s], x1[s][ii]), x2[s][ii] = M::template mma<2>(y, kz[s], x2[s][ii]);
             }
             if (i < 2 * kb + 2) {
-                x2[ii] = M::template mma<2>(M::template low_columns<2>(m.p, 16 * i, kb, lane), qz, x2[ii]);
-                x2[ii] = M::template mma<2>(M::template low_columns<2>(m.t, 16 * i, kb, lane), kz, x2[ii]);
+                const Full x = M::template low_columns<2>(m.p, 16 * i, kb, lane), y = M::template low_columns<2>(m.t, 16 * i, kb, lane);
+#pragma unroll
+                for (int s = 0; s < SL; ++s) x2[s][ii] = M::template mma<2>(y, kz[s], M::template mma<2>(x, qz[s], x2[s][ii]));
             }
             step_done();
         }
     }
-    // through x / |x|: what lies along x does not change it (qh is scale times the unit vector: scale^2 / scale of it goes)
+    // through x / |x|: what lies along x does not change it
     const bool along = !SHARED && p.eps > 0.0f;
     f32x4 dots[2][NI];
     if (along) {
-        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
+        const int lane = fresh(lane0);
 #pragma unroll
         for (int ii = 0; ii < NI; ++ii) {
-            const int t = 16 * (tile0 + ii) + g4;
-            dots[0][ii] = sum16(pick<KT>(qh, ii, tile0) * x1[ii]), dots[1][ii] = sum16(pick<KT>(kh, ii, tile0) * x2[ii]);
+            dots[0][ii] = dots[1][ii] = f32x4{};
+#pragma unroll
+            for (int s = 0; s < SL; ++s) dots[0][ii] += pick<NI>(qh[s], ii, tile0) * x1[s][ii], dots[1][ii] += kh(s, tile0 + ii, lane) * x2[s][ii];
+            dots[0][ii] = sum16(dots[0][ii]), dots[1][ii] = sum16(dots[1][ii]);
         }
     }
     __syncthreads();
@@ -1226,9 +1250,7 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
         const int t = fresh(lane0);
         float x = 0.0f, y = 0.0f, bsum = 0.0f, below = 0.0f, all = 0.0f;
 #pragma unroll
-        for (int u = 0; u < KT; ++u) x += m.part[0][u][t], y += m.part[1][u][t], bsum += m.part[2][u][t], all += m.whole[u];
-#pragma unroll
-        for (int s = 0; s < NS; ++s) bsum += m.db[s][t];
+        for (int u = 0; u < G; ++u) x += m.part[0][u][t], y += m.part[1][u][t], bsum += m.part[2][u][t], all += m.whole[u];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float u = m.da[j][t], w = m.dg[j][t];
@@ -1236,8 +1258,8 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
             below += j >= (t >> 4) ? w : 0.0f;
         }
         // (the derivative of a decay that is 0 in 32 bits is that)
-        const double G = m.s.G[t], G1 = __shfl_up(G, 1, 64);
-        const bool dead = G - (t ? G1 : 0.0) < -104.0 * 1.4426950408889634;
+        const double G0 = m.s.G[t], G1 = __shfl_up(G0, 1, 64);
+        const bool dead = G0 - (t ? G1 : 0.0) < -104.0 * 1.4426950408889634;
 #pragma unroll
         for (int s = 1; s < 64; s *= 2) {
             const float up = __shfl_down(x, s, 64), down = __shfl_up(y, s, 64);
@@ -1251,49 +1273,49 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
             p.dbeta[(long long)head * p.L + t0 + t] = t0 + t < n ? bsum : 0.0f;
         }
     }
-    const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dk = 16 * slice + c;
+    const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
     if (along) {
         __syncthreads();
         if (c == 0)
 #pragma unroll
             for (int ii = 0; ii < NI; ++ii) {
-                *reinterpret_cast<f32x4 *>(&m.part[0][slice][16 * (tile0 + ii) + g4]) = dots[0][ii];
-                *reinterpret_cast<f32x4 *>(&m.part[1][slice][16 * (tile0 + ii) + g4]) = dots[1][ii];
+                *reinterpret_cast<f32x4 *>(&m.part[0][group][16 * (tile0 + ii) + g4]) = dots[0][ii];
+                *reinterpret_cast<f32x4 *>(&m.part[1][group][16 * (tile0 + ii) + g4]) = dots[1][ii];
             }
         __syncthreads();
     }
 #pragma unroll
     for (int ii = 0; ii < NI; ++ii) {
         const int t = 16 * (tile0 + ii) + g4;
-        f32x4 dq = x1[ii], dkey = x2[ii];
-        if (!SHARED) {
-            if (along) {
-                f32x4 a = {}, e = {};
+        f32x4 a = {}, e = {};
+        if (along)
 #pragma unroll
-                for (int u = 0; u < KT; ++u) a += four(m.part[0][u], t), e += four(m.part[1][u], t);
-                const float over = p.scale != 0.0f ? 1.0f / (p.scale * p.scale) : 0.0f;
-                dq -= pick<KT>(qh, ii, tile0) * a * over, dkey -= pick<KT>(kh, ii, tile0) * e;
+            for (int u = 0; u < G; ++u) a += four(m.part[0][u], t), e += four(m.part[1][u], t);
+#pragma unroll
+        for (int s = 0; s < SL; ++s) {
+            const int dk = 16 * (slice0 + s) + c, end = dk < p.DK ? p.L : 0;
+            f32x4 dq = x1[s][ii], dkey = x2[s][ii];
+            if (!SHARED) {
+                if (along) dq -= pick<NI>(qh[s], ii, tile0) * a, dkey -= kh(s, tile0 + ii, lane) * e;
+                dq *= four(m.s.iq, t), dkey *= four(m.s.rk, t);
             }
-            dq *= four(m.s.rq, t), dkey *= four(m.s.rk, t);
-        }
 #pragma unroll
-        for (int v = 0; v < 4; ++v) dq[v] = t0 + t + v < n ? dq[v] : 0.0f, dkey[v] = t0 + t + v < n ? dkey[v] : 0.0f;
-        const int end = dk < p.DK ? p.L : 0;
-        if (SHARED) {
-            store4(part_q + (long long)dk * p.L, dq, t0 + t, end);
-            store4(part_k + (long long)dk * p.L, dkey, t0 + t, end);
-        } else {
-            store4(dq_row + (long long)dk * p.L, dq, t0 + t, end);
-            store4(dk_row + (long long)dk * p.L, dkey, t0 + t, end);
+            for (int v = 0; v < 4; ++v) dq[v] = t0 + t + v < n ? dq[v] : 0.0f, dkey[v] = t0 + t + v < n ? dkey[v] : 0.0f;
+            if (SHARED) {
+                store4(part_q + (long long)dk * p.L, dq, t0 + t, end);
+                store4(part_k + (long long)dk * p.L, dkey, t0 + t, end);
+            } else {
+                store4(dq_row + (long long)dk * p.L, dq, t0 + t, end);
+                store4(dk_row + (long long)dk * p.L, dkey, t0 + t, end);
+            }
         }
     }
 }
-template <typename T, int KT, bool SHARED> __global__ __launch_bounds__(64 * kGradWaves) void delta_bwd_chunk_kernel(DeltaBwd<T> p, int first)
+template <typename T, int KT, bool SHARED> __global__ __launch_bounds__(64 * kGradWaves, 2) void delta_bwd_chunk_kernel(DeltaBwd<T> p, int first)
 {
     extern __shared__ char lds[];
     DeltaChunkLds<T, KT> &m = *reinterpret_cast<DeltaChunkLds<T, KT> *>(lds);
     LowTiles<T, 3, 64 * kGradWaves>::zeros(m.t);
-    LowTiles<T, 3, 64 * kGradWaves>::zeros(m.p);
     delta_bwd_chunk<T, KT, SHARED>(p, m, first + (int)blockIdx.x);
 }
 
@@ -1349,7 +1371,7 @@ template <typename T, int KT> __global__ __launch_bounds__(512) void delta_share
     for (int i = 0; i < N; ++i) {
         const int r = wave + 8 * i;
         if (r >= p.DK) continue;
-        st_elem(dq_row + (long long)r * p.L, inside ? p.scale * iq * fmaf(-q[i], qa, dq[i]) : 0.0f);
+        st_elem(dq_row + (long long)r * p.L, inside ? iq * fmaf(-q[i], qa, dq[i]) : 0.0f);
         st_elem(dk_row + (long long)r * p.L, inside ? ik * fmaf(-k[i], ka, dk[i]) : 0.0f);
     }
 }

@@ -54,8 +54,8 @@ def test_forward_refusals(lib):
 
 def test_backward_refusals(lib):
     need = lib.dwconv_delta_workspace_bytes(2, 4, 2, 8, 16, 100, 1)
-    # the states' gradients behind two chunks of every head, and what each of the heads that share a key adds to its gradients
-    assert need == lib.dwconv_delta_workspace_bytes(2, 4, 2, 8, 16, 100, 0) + 2 * 4 * 2 * 8 * 16 * 4 + 2 * 4 * 2 * 8 * 100 * 4
+    # the states' gradients behind two chunks of every head, those of 64 positions' u, and what each of the heads that share a key adds to its gradients
+    assert need == lib.dwconv_delta_workspace_bytes(2, 4, 2, 8, 16, 100, 0) + 2 * 4 * 2 * 16 * (8 + 64) * 4 + 2 * 4 * 2 * 8 * 100 * 4
     assert lib.dwconv_delta_workspace_bytes(2, 4, 4, 8, 16, 100, 1) == need - 2 * 4 * 2 * 8 * 100 * 4
 
     def f(k=None, v=None, ws=P, n=1 << 40, scale=1.0, eps=1e-6, dtype=0, **dims):
@@ -81,7 +81,7 @@ def test_states_and_workspaces(lib):
     for bad in ((0, 1, 1, 1, 1, 1), (1, 0, 1, 1, 1, 1), (1, 2, 0, 1, 1, 1), (1, 3, 2, 1, 1, 1), (1, 1, 1, 0, 1, 1), (1, 1, 1, 129, 1, 1), (1, 1, 1, 1, 0, 1), (1, 1, 1, 1, 1, 0)):
         assert lib.dwconv_delta_workspace_bytes(*bad, 0) == 0 and lib.dwconv_delta_workspace_bytes(*bad, 1) == 0
     a, b = (lib.dwconv_delta_workspace_bytes(1, 1, 1, 1, 1, 64, x) for x in (0, 1))
-    assert a > 0 and a % 16 == 0 and b == a + 16 and lib.dwconv_delta_workspace_bytes(3, 5, 5, 1, 1, 65, 0) == 30 * a
+    assert a > 0 and a % 16 == 0 and b == a + 16 + 64 * 4 and lib.dwconv_delta_workspace_bytes(3, 5, 5, 1, 1, 65, 0) == 30 * a
     # (rows of fewer than eight positions are copied to where they have room for that)
     assert lib.dwconv_delta_workspace_bytes(1, 1, 1, 1, 1, 7, 0) > a == lib.dwconv_delta_workspace_bytes(1, 1, 1, 1, 1, 8, 0)
 

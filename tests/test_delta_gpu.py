@@ -176,6 +176,13 @@ def test_scales(scale):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("H,Hk", [(2, 2), (4, 2)])
+@pytest.mark.parametrize("scale", [1e-25, 1e25])
+def test_scales_whose_squares_are_out_of_range(scale, H, Hk, dtype):
+    check_rule(*inputs(2, H, Hk, 32, 32, 100, dtype, seed=21), key_heads=Hk, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("B,H,DK,DV,L", [(1, 1, 64, 64, 4200), (1, 2, 128, 128, 2100), (700, 1, 16, 16, 66), (40, 9, 32, 24, 70)])
 def test_long_and_many(B, H, DK, DV, L, dtype):
     check_rule(*inputs(B, H, H, DK, DV, L, dtype, rate=0.05))
