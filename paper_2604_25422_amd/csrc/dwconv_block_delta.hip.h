@@ -72,6 +72,10 @@ struct DeltaPairs {
     Gates s;
 };
 
+__device__ __forceinline__ f32x4 fma4(f32x4 a, f32x4 b, f32x4 c)
+{
+    return f32x4{fmaf(a[0], b[0], c[0]), fmaf(a[1], b[1], c[1]), fmaf(a[2], b[2], c[2]), fmaf(a[3], b[3], c[3])};
+}
 __device__ __forceinline__ f32x4 four(const float *x, int at) { return *reinterpret_cast<const f32x4 *>(x + at); }
 
 // D += A B of 16 x 16 x 16: a[v] = A[lane % 16][4 (lane / 16) + v], b[v] = B[4 (lane / 16) + v][lane % 16], and D as B, so that one
@@ -598,14 +602,18 @@ struct StateIn {
     {
         __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), r, lane, row, 0);
     }
-    // Columns dv .. dv + 3 of a row, zeros from DV on.
-    __device__ __forceinline__ f32x4 four(int row, int dv, int DV) const
+    // Columns dv .. dv + 3 of a row: as they lie (from DV on those of the next row), or zeros from DV on.
+    __device__ __forceinline__ f32x4 any_four(int row, int dv) const
     {
-        f32x4 x = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, row * pitch + 4 * dv, 0, 0));
+        return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, row * pitch + 4 * dv, 0, 0));
+    }
+    static __device__ __forceinline__ f32x4 inside(f32x4 x, int dv, int DV)
+    {
 #pragma unroll
         for (int v = 0; v < 4; ++v) x[v] = dv + v < DV ? x[v] : 0.0f;
         return x;
     }
+    __device__ __forceinline__ f32x4 four(int row, int dv, int DV) const { return inside(any_four(row, dv), dv, DV); }
     __device__ __forceinline__ void put_four(f32x4 x, int row, int dv, int DV) const
     {
         if (dv + 4 <= DV) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), r, row * pitch + 4 * dv, 0, 0);
@@ -1026,13 +1034,18 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
                 for (int i = 0; i < 4; ++i) x[i] = M::mma(M::columns_in(m.k, 16 * i, 16 * kb, lane), s, x[i]);
                 step_done();
             }
-            const bool out = v0 + 16 * (wave & 1) + c >= p.DV;
             vrow.get(val, t0, g4, n, p.pitch);
+            if (v0 + VB > p.DV) {
+                const bool out = v0 + 16 * (wave & 1) + c >= p.DV;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) val[i] = out ? f32x4{} : val[i];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) dr[i] = out ? f32x4{} : dr[i];
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int t = 16 * i + g4;
-                if (out) val[i] = f32x4{};
-                x[i] = four(m.s.beta, t) * (val[i] - four(m.s.eG, t) * four(m.s.rk, t) * x[i]);
+                x[i] = four(m.s.beta, t) * fma4(four(m.s.eG, t) * -four(m.s.rk, t), x[i], val[i]);
             }
             const int near = 16 * half, far = 48 - 16 * half;           // tiles 0 and 3, or 1 and 2: of three blocks 32 wide either way
             const Full z0 = M::split(x[0], x[1]), z1 = M::split(x[2], x[3]);
@@ -1043,7 +1056,6 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
             M::put(m.w, VP, row + far, yf);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                if (out) dr[i] = f32x4{};
                 const f32x4 sum = sum16(dr[i] * pick<2>(val, i, 2 * half));
                 if (c == 0) *reinterpret_cast<f32x4 *>(&m.dg[wave & 1][32 * half + 16 * i + g4]) += sum;
                 M::put(m.dr, VP, row + 32 * half + 16 * i, dr[i]);
@@ -1059,9 +1071,14 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb) {
                     const int dk = 16 * (slice0 + s) + (lane & 15);
-                    a[s][kb] = before.four(dk, v0 + 16 * kb + g4, p.DV), e[s][kb] = after.four(dk, v0 + 16 * kb + g4, p.DV);
+                    a[s][kb] = before.any_four(dk, v0 + 16 * kb + g4), e[s][kb] = after.any_four(dk, v0 + 16 * kb + g4);
                 }
             __syncthreads();
+            if (v0 + VB > p.DV)
+#pragma unroll
+                for (int s = 0; s < SL; ++s)
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb) a[s][kb] = StateIn::inside(a[s][kb], v0 + 16 * kb + g4, p.DV), e[s][kb] = StateIn::inside(e[s][kb], v0 + 16 * kb + g4, p.DV);
             Full z[SL];
 #pragma unroll
             for (int s = 0; s < SL; ++s) {
@@ -1124,9 +1141,11 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
         for (int s = 0; s < SL; ++s) {
             qrow[s].get(qh[s], t0, g4, n, p.pitch);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                qh[s][i] *= four(m.s.iq, 16 * i + g4);
-                if (16 * (slice0 + s) + c >= p.DK) qh[s][i] = f32x4{};
+            for (int i = 0; i < 4; ++i) qh[s][i] *= four(m.s.iq, 16 * i + g4);
+            if (16 * (slice0 + s) + 16 > p.DK) {
+                const bool out = 16 * (slice0 + s) + c >= p.DK;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) qh[s][i] = out ? f32x4{} : qh[s][i];
             }
         }
     }
@@ -1148,8 +1167,8 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
                 x2[s][ii] *= -in;
                 x3[s][ii] *= left;
                 const f32x4 bx = k * x2[s][ii];
-                xs += q * x1[s][ii] + beta * bx, ys += k * x3[s][ii], bs += bx;
-                x2[s][ii] = beta * x2[s][ii] + x3[s][ii];       // from here on: x1 is dq, x2 is dk
+                xs = fma4(q, x1[s][ii], fma4(beta, bx, xs)), ys = fma4(k, x3[s][ii], ys), bs += bx;
+                x2[s][ii] = fma4(beta, x2[s][ii], x3[s][ii]);   // from here on: x1 is dq, x2 is dk
             }
             xs = sum16(xs), ys = sum16(ys), bs = sum16(bs);
             if (i >> 1 == half) bs += four(m.dg[wave & 1], t);
@@ -1241,7 +1260,7 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
         for (int ii = 0; ii < NI; ++ii) {
             dots[0][ii] = dots[1][ii] = f32x4{};
 #pragma unroll
-            for (int s = 0; s < SL; ++s) dots[0][ii] += pick<NI>(qh[s], ii, tile0) * x1[s][ii], dots[1][ii] += kh(s, tile0 + ii, lane) * x2[s][ii];
+            for (int s = 0; s < SL; ++s) dots[0][ii] = fma4(pick<NI>(qh[s], ii, tile0), x1[s][ii], dots[0][ii]), dots[1][ii] = fma4(kh(s, tile0 + ii, lane), x2[s][ii], dots[1][ii]);
             dots[0][ii] = sum16(dots[0][ii]), dots[1][ii] = sum16(dots[1][ii]);
         }
     }
@@ -1293,21 +1312,24 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
             for (int u = 0; u < G; ++u) a += four(m.part[0][u], t), e += four(m.part[1][u], t);
 #pragma unroll
         for (int s = 0; s < SL; ++s) {
-            const int dk = 16 * (slice0 + s) + c, end = dk < p.DK ? p.L : 0;
+            const int dk = 16 * (slice0 + s) + c;
             f32x4 dq = x1[s][ii], dkey = x2[s][ii];
             if (!SHARED) {
-                if (along) dq -= pick<NI>(qh[s], ii, tile0) * a, dkey -= kh(s, tile0 + ii, lane) * e;
+                if (along) dq = fma4(pick<NI>(qh[s], ii, tile0), -a, dq), dkey = fma4(kh(s, tile0 + ii, lane), -e, dkey);
                 dq *= four(m.s.iq, t), dkey *= four(m.s.rk, t);
             }
+            const long long at = (long long)dk * p.L;
+            const auto put = [&](auto *to, f32x4 x) __attribute__((always_inline)) {
+                if (t0 + 64 <= n) {             // (n is at most L)
+                    if (dk < p.DK) store4(to + at + t0 + t, x);
+                } else {
 #pragma unroll
-            for (int v = 0; v < 4; ++v) dq[v] = t0 + t + v < n ? dq[v] : 0.0f, dkey[v] = t0 + t + v < n ? dkey[v] : 0.0f;
-            if (SHARED) {
-                store4(part_q + (long long)dk * p.L, dq, t0 + t, end);
-                store4(part_k + (long long)dk * p.L, dkey, t0 + t, end);
-            } else {
-                store4(dq_row + (long long)dk * p.L, dq, t0 + t, end);
-                store4(dk_row + (long long)dk * p.L, dkey, t0 + t, end);
-            }
+                    for (int v = 0; v < 4; ++v) x[v] = t0 + t + v < n ? x[v] : 0.0f;
+                    store4(to + at, x, t0 + t, dk < p.DK ? p.L : 0);
+                }
+            };
+            if constexpr (SHARED) put(part_q, dq), put(part_k, dkey);
+            else put(dq_row, dq), put(dk_row, dkey);
         }
     }
 }
