@@ -187,12 +187,20 @@ template <> struct Mat<bf16_t> {
         for (int n = 0; n < N; ++n) f.l[n] = column(x + n * plane, m, k, lane);
         return f;
     }
+    // x without element I of a pair: (w0, w1) . (-1, 0) + x or (w0, w1) . (0, -1) + x, which is exact, in one instruction (a shift or a mask and a
+    // subtraction are two).  The factors are kept in registers: as a constant of the instruction the compiler has -1 stand for the other pair.
+    template <int I> static __device__ __forceinline__ float less(float x, unsigned w)
+    {
+        typedef __bf16 pair_t __attribute__((ext_vector_type(2)));
+        unsigned minus = I ? 0xbf800000u : 0x0000bf80u;
+        asm("" : "+s"(minus));
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair_t, w), __builtin_bit_cast(pair_t, minus), x, false);
+    }
     // The next limb of four values: the nearest bf16 to what is left of them, which x then is without it.
     static __device__ __forceinline__ u32x2 limb(f32x4 &x)
     {
         const u32x2 w = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
-        x = f32x4{x[0] - __uint_as_float(w[0] << 16), x[1] - __uint_as_float(w[0] & 0xffff0000u), x[2] - __uint_as_float(w[1] << 16),
-                  x[3] - __uint_as_float(w[1] & 0xffff0000u)};
+        x = f32x4{less<0>(x[0], w[0]), less<1>(x[1], w[0]), less<0>(x[2], w[1]), less<1>(x[3], w[1])};
         return w;
     }
     template <int N = 3> static __device__ __forceinline__ Full split(f32x4 a, f32x4 b)
