@@ -964,7 +964,10 @@ template <typename T, int KT> struct DeltaChunkLds {
         };
     };
     ChunkGates s;
-    float part[3][G][64], da[4][64], dg[4][64], whole[G];
+    float part[3][G][64], db[2][64], da[10][16], dg[10][16], whole[G];
+    // Sums of a tile's rows and columns, in what the pairs leave of their place: blocks (0, 1) and (2, 3).
+    __device__ __forceinline__ float *rows(int tile) { return pairs + low_at(tile, 16); }
+    __device__ __forceinline__ float *columns(int tile) { return pairs + low_at(32 + tile, 48); }
 };
 
 // Backward, within a chunk, all chunks at once: from the states in front of it, the gradient of that behind it and dr
@@ -1024,14 +1027,28 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
         kt.put(m.k, p.DK, t0, n, p.pitch);
         t.put(m.t);
         if (threadIdx.x < sizeof(ChunkGates) / 16) reinterpret_cast<f32x4 *>(&m.s)[threadIdx.x] = gates;
-        if (threadIdx.x < 128) m.dg[0][threadIdx.x] = 0.0f;             // (at first dr v, of even columns' waves and odd ones')
+        if (threadIdx.x < 128) m.db[0][threadIdx.x] = 0.0f;
     }
     __syncthreads();
     f32x4 dp[TASKS] = {}, da[TASKS] = {};   // of this wave's tiles of pairs, transposed: lane (c, g) has columns 16 tj + 4 g + v of row 16 ti + c
     f32x4 x1[SL][NI] = {}, x2[SL][NI] = {}, x3[SL][NI] = {};    // do S^T, dr S^T, w dS^T: rows of positions, 16 channels of the key
     float whole = 0.0f;
+    const auto take_pairs = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < TASKS; ++u) {
+            const int task = wave + u * W;
+            if (task >= 10) continue;
+            const int lane = fresh(lane0);
+            int ti, tj;
+            low_tile(task, ti, tj);
+            const Full wj = M::columns(m.w, VP, 16 * tj, 0, lane);
+            dp[u] = M::mma(wj, M::columns_in(m.dout, 16 * ti, 0, lane), dp[u]);
+            da[u] = M::mma(wj, M::columns(m.dr, VP, 16 * ti, 0, lane), da[u]);
+            step_done();
+        }
+    };
 #pragma unroll 1
-    for (int v0 = 0; v0 < p.DV; v0 += VB) {
+    for (int v0 = 0;; v0 += VB) {
         {
             const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), row = (16 * (wave & 1) + c) * kPitch + g4;
             f32x4 x[4] = {}, val[4];
@@ -1065,7 +1082,7 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const f32x4 sum = sum16(dr[i] * pick<2>(val, i, 2 * half));
-                if (c == 0) *reinterpret_cast<f32x4 *>(&m.dg[wave & 1][32 * half + 16 * i + g4]) += sum;
+                if (c == 0) *reinterpret_cast<f32x4 *>(&m.db[wave & 1][32 * half + 16 * i + g4]) += sum;
                 M::put(m.dr, VP, row + 32 * half + 16 * i, dr[i]);
             }
             drow.put(m.dout, p.DV - v0, t0, n, p.pitch);
@@ -1114,23 +1131,12 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
                 step_done();
             }
         }
-#pragma unroll
-        for (int u = 0; u < TASKS; ++u) {
-            const int task = wave + u * W;
-            if (task >= 10) continue;
-            const int lane = fresh(lane0);
-            int ti, tj;
-            low_tile(task, ti, tj);
-            const Full wj = M::columns(m.w, VP, 16 * tj, 0, lane);
-            dp[u] = M::mma(wj, M::columns_in(m.dout, 16 * ti, 0, lane), dp[u]);
-            da[u] = M::mma(wj, M::columns(m.dr, VP, 16 * ti, 0, lane), da[u]);
-            step_done();
-        }
-        if (v0 + VB < p.DV) fetch(v0 + VB);
+        if (v0 + VB >= p.DV) break;
+        take_pairs();
+        fetch(v0 + VB);
         __syncthreads();
     }
-    LowTiles<T, Lds::N2, 64 * W>::zeros(m.p);
-    // (what the ends take from memory)
+    // (what the ends take from memory, on its way during the last step's pairs)
     f32x4 kk[TASKS], pp[TASKS], qh[SL][4];          // q of unit length, as kh() is k's
     {
         const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
@@ -1145,6 +1151,9 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
             const int task = min(wave + u * W, 9);
             kk[u] = four(pairs.kk[task], 16 * c + g4), pp[u] = four(pairs.p[task], 16 * c + g4);
         }
+        take_pairs();
+        __syncthreads();
+        LowTiles<T, Lds::N2, 64 * W>::zeros(m.p);
 #pragma unroll
         for (int s = 0; s < SL; ++s) {
             qrow[s].get(qh[s], t0, g4, n, p.pitch);
@@ -1167,21 +1176,19 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
         for (int ii = 0; ii < NI; ++ii) {
             const int i = tile0 + ii, t = 16 * i + g4;
             const f32x4 beta = four(m.s.beta, t), in = four(m.s.eG, t), left = four(m.s.eC, t);
-            f32x4 xs = {}, ys = {}, bs = {};
+            f32x4 qs = {}, ys = {}, bs = {};
 #pragma unroll
             for (int s = 0; s < SL; ++s) {
                 const f32x4 k = kh(s, i, lane), q = pick<NI>(qh[s], ii, tile0);
                 x1[s][ii] *= in * p.scale;
                 x2[s][ii] *= -in;
                 x3[s][ii] *= left;
-                const f32x4 bx = k * x2[s][ii];
-                xs = fma4(q, x1[s][ii], fma4(beta, bx, xs)), ys = fma4(k, x3[s][ii], ys), bs += bx;
+                qs = fma4(q, x1[s][ii], qs), ys = fma4(k, x3[s][ii], ys), bs = fma4(k, x2[s][ii], bs);
                 x2[s][ii] = fma4(beta, x2[s][ii], x3[s][ii]);   // from here on: x1 is dq, x2 is dk
             }
-            xs = sum16(xs), ys = sum16(ys), bs = sum16(bs);
-            if (i >> 1 == half) bs += four(m.dg[wave & 1], t);
+            qs = sum16(qs), ys = sum16(ys), bs = sum16(bs);
             if (c == 0) {
-                *reinterpret_cast<f32x4 *>(&m.part[0][group][t]) = xs;
+                *reinterpret_cast<f32x4 *>(&m.part[0][group][t]) = qs;
                 *reinterpret_cast<f32x4 *>(&m.part[1][group][t]) = ys;
                 *reinterpret_cast<f32x4 *>(&m.part[2][group][t]) = bs;
             }
@@ -1205,16 +1212,37 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
             dP[v] = j + v <= i ? dP[v] : 0.0f;
             e[v] = j + v <= i ? exp2_of(m.s.G[i] - m.s.G[j + v]) : 0.0f;
         }
-        const f32x4 x = dA * kk[u];
-        float sum = (x[0] + x[1]) + (x[2] + x[3]);
-        sum += __shfl_xor(sum, 16, 64);
-        sum += __shfl_xor(sum, 32, 64);
-        if (lane < 16) m.da[tj][i] = sum;
+        const f32x4 x = dA * kk[u], y = dP * pp[u], both = fma4(x, f32x4{} + m.s.beta[i], y), below = sum16(both);
+        const auto across = [](f32x4 z) __attribute__((always_inline)) {
+            float sum = (z[0] + z[1]) + (z[2] + z[3]);
+            sum += __shfl_xor(sum, 16, 64);
+            return sum + __shfl_xor(sum, 32, 64);
+        };
+        const float xs = across(x), ys = across(y);
+        if (lane < 16) m.da[task][c] = xs, m.rows(task)[c] = ys;
+        if (c == 0) *reinterpret_cast<f32x4 *>(m.columns(task) + g4) = below;
         M::template put<2>(m.p, kLow, low_at(i, j), dP * e * p.scale);
         M::template put<2>(m.t, kLow, low_at(i, j), dA * e * m.s.beta[i]);
-        *reinterpret_cast<f32x4 *>(m.pairs + low_at(i, j)) = dP * pp[u] + x * m.s.beta[i];
+        *reinterpret_cast<f32x4 *>(m.pairs + low_at(i, j)) = both;
     }
     __syncthreads();
+    // Sums over the channels of q dq and k dk, whose pairs' part is that of P dP and of A dA; dbeta; what rows take and what columns leave.
+    if (wave == 0) {
+        const int t = fresh(lane0), tt = t >> 4, c = t & 15;
+        float qs = 0.0f, ys = 0.0f, bs = 0.0f, xs = 0.0f, ps = 0.0f, cs = 0.0f;
+#pragma unroll
+        for (int u = 0; u < G; ++u) qs += m.part[0][u][t], ys += m.part[1][u][t], bs += m.part[2][u][t];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int left = tt * (tt + 1) / 2 + min(j, tt), down = max(j, tt) * (max(j, tt) + 1) / 2 + tt;
+            const float u = m.da[left][c], v = m.rows(left)[c], w = m.columns(down)[c];
+            xs += j <= tt ? u : 0.0f, ps += j <= tt ? v : 0.0f, cs += j >= tt ? w : 0.0f;
+        }
+        const float beta = m.s.beta[t], sum = bs + (m.db[0][t] + m.db[1][t]) + xs;
+        m.part[0][0][t] = qs + ps, m.part[0][1][t] = fmaf(beta, bs + xs, ys) + cs;
+        m.part[1][0][t] = fmaf(beta, bs, qs), m.part[1][1][t] = ys;
+        if (t0 + t < p.L) p.dbeta[(long long)head * p.L + t0 + t] = t0 + t < n ? sum : 0.0f;
+    }
     // pairs of a row from t on and a column before t: products with ones above the diagonal, then the rows from t on, a tile a wave
     for (int task = W - 1 - wave; task < 10; task += W) {
         const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
@@ -1232,7 +1260,7 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
         for (int v = 0; v < 4; ++v) sum += 16 * ti + g4 + v >= 16 * tt + c ? x[v] : 0.0f;
         sum += __shfl_xor(sum, 16, 64);
         sum += __shfl_xor(sum, 32, 64);
-        if (lane < 16) m.dg[ti][16 * tt + c] = sum;
+        if (lane < 16) m.dg[task][c] = sum;
     }
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
@@ -1259,30 +1287,16 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
             step_done();
         }
     }
-    // through x / |x|: what lies along x does not change it
-    const bool along = !SHARED && p.eps > 0.0f;
-    f32x4 dots[2][NI];
-    if (along) {
-        const int lane = fresh(lane0);
-#pragma unroll
-        for (int ii = 0; ii < NI; ++ii) {
-            dots[0][ii] = dots[1][ii] = f32x4{};
-#pragma unroll
-            for (int s = 0; s < SL; ++s) dots[0][ii] = fma4(pick<NI>(qh[s], ii, tile0), x1[s][ii], dots[0][ii]), dots[1][ii] = fma4(kh(s, tile0 + ii, lane), x2[s][ii], dots[1][ii]);
-            dots[0][ii] = sum16(dots[0][ii]), dots[1][ii] = sum16(dots[1][ii]);
-        }
-    }
     __syncthreads();
     if (wave == W - 1) {
-        const int t = fresh(lane0);
-        float x = 0.0f, y = 0.0f, bsum = 0.0f, below = 0.0f, all = 0.0f;
+        const int t = fresh(lane0), tt = t >> 4;
+        float x = m.part[1][0][t], y = m.part[1][1][t], below = 0.0f, all = 0.0f;
 #pragma unroll
-        for (int u = 0; u < G; ++u) x += m.part[0][u][t], y += m.part[1][u][t], bsum += m.part[2][u][t], all += m.whole[u];
+        for (int u = 0; u < G; ++u) all += m.whole[u];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float u = m.da[j][t], w = m.dg[j][t];
-            bsum += j <= (t >> 4) ? u : 0.0f;
-            below += j >= (t >> 4) ? w : 0.0f;
+            const float w = m.dg[max(j, tt) * (max(j, tt) + 1) / 2 + tt][t & 15];
+            below += j >= tt ? w : 0.0f;
         }
         // (the derivative of a decay that is 0 in 32 bits is that)
         const double G0 = m.s.G[t], G1 = __shfl_up(G0, 1, 64);
@@ -1295,29 +1309,15 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
         }
         const float left = __shfl_up(y, 1, 64);
         const float sum = (m.s.eG[63] * all + x) + ((t > 0 ? left : 0.0f) + below);
-        if (t0 + t < p.L) {
-            p.dg[(long long)head * p.L + t0 + t] = t0 + t < n && !dead ? sum : 0.0f;
-            p.dbeta[(long long)head * p.L + t0 + t] = t0 + t < n ? bsum : 0.0f;
-        }
+        if (t0 + t < p.L) p.dg[(long long)head * p.L + t0 + t] = t0 + t < n && !dead ? sum : 0.0f;
     }
+    // through x / |x|: what lies along x does not change it
+    const bool along = !SHARED && p.eps > 0.0f;
     const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
-    if (along) {
-        __syncthreads();
-        if (c == 0)
-#pragma unroll
-            for (int ii = 0; ii < NI; ++ii) {
-                *reinterpret_cast<f32x4 *>(&m.part[0][group][16 * (tile0 + ii) + g4]) = dots[0][ii];
-                *reinterpret_cast<f32x4 *>(&m.part[1][group][16 * (tile0 + ii) + g4]) = dots[1][ii];
-            }
-        __syncthreads();
-    }
 #pragma unroll
     for (int ii = 0; ii < NI; ++ii) {
         const int t = 16 * (tile0 + ii) + g4;
-        f32x4 a = {}, e = {};
-        if (along)
-#pragma unroll
-            for (int u = 0; u < G; ++u) a += four(m.part[0][u], t), e += four(m.part[1][u], t);
+        const f32x4 a = four(m.part[0][0], t), e = four(m.part[0][1], t);
 #pragma unroll
         for (int s = 0; s < SL; ++s) {
             const int dk = 16 * (slice0 + s) + c;
