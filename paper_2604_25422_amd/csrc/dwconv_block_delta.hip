@@ -3,6 +3,7 @@
 #include "dwconv_block_delta.hip.h"
 
 #include <atomic>
+#include <cmath>
 
 using namespace blkhost;
 using namespace dwconv;
@@ -113,6 +114,7 @@ template <typename T, int RT> __global__ __launch_bounds__(256) void delta_step_
 namespace {
 
 constexpr int kMaxKey = 128;            // channels of a key: a state's columns are registers of a wave
+constexpr int kChain = 16;              // spans that are walked one after the other without joining some first
 constexpr int kMaxUnits = 1 << 22;      // workgroups of a launch, whose lanes stay below 2^32
 
 template <typename Launch> void for_units(int units, Launch launch)
@@ -164,12 +166,29 @@ template <typename T, int KT> int launch_pairs(const DeltaShape<T> &p, hipStream
 // it starts with (DV + DK columns instead of DV) can be formed for all segments at once, the states between them in a chain of its own, which takes a
 // third of a step each, and then all segments at once again.  In steps of a walk that has a CU to itself (two workgroups share one at 1.4 times that;
 // in fp32 with more than 64 channels of a key LDS has room for one), forward the pass that forms spans writes no output and takes 0.6.
-// us whole / cut (segments): bf16, DK = DV = 128, 256 chunks, 2 heads forward 1623 / 189 (32), backward 1630 / 275; 32 heads 1857 / 786 (8), 2971 / 2057; 64
-// heads 2000 / 1510 (4), 4239 / 4076; 128 heads, 64 chunks 582 / 824, 1649 / 2086; 2 heads, 8 chunks 62 / 46 (4), 93 / 83.  fp32, 64 heads 4500 / 4650, 7936 /
-// 9345.  DK = DV = 64, bf16, 128 heads 1407 / 1297 (4), 3717 / 3874; fp32 2443 / 2292, 5806 / 6221.
+// us whole / cut (segments): bf16, DK = DV = 128, 256 chunks, 2 heads forward 1578 / 147 (64), backward 1594 / 212; 32 heads 1811 / 762 (8), 2673 / 1790; 64
+// heads 1965 / 1457 (4), 3685 / 3522; 128 heads, 64 chunks 567 / 784, 1380 / 1765; 2 heads, 8 chunks 63 / 50 (4), 99 / 89.  fp32, 64 heads, 64 chunks 1099 /
+// 1192, 1794 / 2150.  DK = DV = 64, 64 chunks, bf16, 128 heads 351 / 319 (4), 766 / 805; fp32 613 / 585, 1255 / 1365.
 struct WalkPlan {
-    int segs, per;
+    int segs, per, join;
 };
+// Segments joined to one on the way to their starts, and the steps that the way takes: one chain, or three of about the root of its length where what
+// they have to do beside it fits the chip.  us of a forward pass in one chain / in three: bf16, DK = DV = 128, 4 heads, 64 segments 534 / 434, 2 heads 249 /
+// 145, 8 heads, 32 segments 276 / 276; DK = DV = 64, 4 heads, 64 segments 213 / 195; fp32, DK = DV = 32, 2 heads, 64 segments 77 / 65.
+struct ChainPlan {
+    int join;
+    double steps;
+};
+ChainPlan plan_chain(double heads, int segs, int DK, int DV)
+{
+    const double values = (double)ceil_div(DV, 16), all = values + (double)ceil_div(DK, 16);
+    const auto rounds = [](double groups) { return std::max(1.0, groups / 512); };
+    const double one = segs * rounds(heads * values);
+    if (segs <= kChain) return ChainPlan{1, one};
+    const int join = (int)std::ceil(std::sqrt((double)segs)), groups = (int)ceil_div(segs, join);
+    const double three = join * (rounds(heads * (groups - 1) * all) + rounds(heads * groups * values)) + groups * rounds(heads * values) + 4;
+    return three < one ? ChainPlan{join, three} : ChainPlan{1, one};
+}
 WalkPlan plan_walk(int B, int H, int DK, int DV, int L, int dtype, bool backward)
 {
     const int chunks = chunks_of(L);
@@ -178,17 +197,20 @@ WalkPlan plan_walk(int B, int H, int DK, int DV, int L, int dtype, bool backward
                  all = (double)ceil_div(ceil_div(DV, 16) + ceil_div(DK, 16), kWalkWaves);
     const auto step = [&](double groups) { return groups <= 256 ? 1.0 : alone ? groups / 256 : groups <= 512 ? 1.4 : 1.4 * groups / 512; };
     double best = chunks * step(heads * values);
-    WalkPlan w{1, chunks};
+    WalkPlan w{1, chunks, 1};
     for (int segs = 2; segs <= 128 && segs <= chunks / 2; segs *= 2) {
         const int per = (int)ceil_div(chunks, segs);
-        const double cost = per * ((backward ? 1.0 : 0.6) * step(heads * segs * all) + step(heads * segs * values)) + 0.3 * segs + 1.0;
-        if (cost < best) best = cost, w = WalkPlan{(int)ceil_div(chunks, per), per};
+        const int real = (int)ceil_div(chunks, per);
+        const ChainPlan chain = plan_chain(heads, real, DK, DV);
+        const double cost = per * ((backward ? 1.0 : 0.6) * step(heads * segs * all) + step(heads * segs * values)) + 0.35 * chain.steps + 1.0;
+        if (cost < best) best = cost, w = WalkPlan{real, per, chain.join};
     }
     return w;
 }
 size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 size_t starts_bytes(const WalkPlan &w, int B, int H, int DK, int DV) { return w.segs > 1 ? up16((size_t)B * H * w.segs * DK * DV * sizeof(float)) : 0; }
 size_t spans_bytes(const WalkPlan &w, int B, int H, int DK, int DV) { return w.segs > 1 ? up16((size_t)B * H * w.segs * DK * (DV + DK) * sizeof(float)) : 0; }
+size_t joined_bytes(const WalkPlan &w, int B, int H, int DK, int DV) { return w.join > 1 ? up16((size_t)B * H * ceil_div(w.segs, w.join) * DK * (DV + DK) * sizeof(float)) : 0; }
 
 template <typename Kernel, typename P> int launch_segments(Kernel kernel, const P &p, DeltaWalk w, int columns, size_t lds, std::atomic<unsigned long long> &done, hipStream_t st)
 {
@@ -198,6 +220,18 @@ template <typename Kernel, typename P> int launch_segments(Kernel kernel, const 
     for (long long first = 0; first < ids; first += kMaxUnits)
         kernel<<<(unsigned)std::min<long long>(ids - first, kMaxUnits), 64 * kWalkWaves, lds, st>>>(p, w, first);
     return DWCONV_OK;
+}
+template <int KT, bool BACK> void launch_starts(const float *s0, const DeltaWalk &w, int heads, int DK, int DV, hipStream_t st)
+{
+    const unsigned values = (unsigned)ceil_div(DV, 16), all = values + (unsigned)ceil_div(DK, 16);
+    if (w.join == 1) {
+        delta_starts_kernel<KT, BACK, Starts::ALL><<<dim3(heads, values), 64 * KT, 0, st>>>(s0, w, DK, DV);
+        return;
+    }
+    const int groups = (int)ceil_div(w.segs, w.join);
+    delta_starts_kernel<KT, BACK, Starts::JOIN><<<dim3(heads * (groups - 1), all), 64 * KT, 0, st>>>(s0, w, DK, DV);
+    delta_starts_kernel<KT, BACK, Starts::ACROSS><<<dim3(heads, values), 64 * KT, 0, st>>>(s0, w, DK, DV);
+    delta_starts_kernel<KT, BACK, Starts::WITHIN><<<dim3(heads * groups, values), 64 * KT, 0, st>>>(s0, w, DK, DV);
 }
 // Columns of a pass that forms spans, up to whole slices of 16.
 int span_columns(int DK, int DV) { return 16 * (int)(ceil_div(DV, 16) + ceil_div(DK, 16)); }
@@ -210,7 +244,7 @@ template <typename T, int KT> int launch_fwd(const DeltaFwd<T> &p, const DeltaWa
     int rc = launch_pairs<T, KT>(p, st);
     if (rc == DWCONV_OK && w.segs > 1) {
         rc = launch_segments(delta_fwd_kernel<T, KT, true>, p, w, span_columns(p.DK, p.DV), lds, done[1], st);
-        delta_starts_kernel<KT, false><<<dim3(p.B * p.H, (unsigned)ceil_div(p.DV, 16)), 64 * KT, 0, st>>>(p.s0, w.spans, const_cast<float *>(w.starts), w.segs, p.DK, p.DV);
+        launch_starts<KT, false>(p.s0, w, p.B * p.H, p.DK, p.DV, st);
     }
     if (rc == DWCONV_OK) rc = launch_segments(delta_fwd_kernel<T, KT, false>, p, w, p.DV, lds, done[0], st);
     return rc == DWCONV_OK ? launch_status() : rc;
@@ -228,7 +262,7 @@ template <typename T, int KT> int launch_bwd(const DeltaBwd<T> &p, const DeltaWa
     int rc = launch_pairs<T, KT>(p, st);
     if (rc == DWCONV_OK && w.segs > 1) {
         rc = launch_segments(delta_bwd_state_kernel<T, KT, true>, p, w, span_columns(p.DK, p.DV), lds, done[1], st);
-        delta_starts_kernel<KT, true><<<dim3(p.B * p.H, (unsigned)ceil_div(p.DV, 16)), 64 * KT, 0, st>>>(p.ds_last, w.spans, const_cast<float *>(w.starts), w.segs, p.DK, p.DV);
+        launch_starts<KT, true>(p.ds_last, w, p.B * p.H, p.DK, p.DV, st);
     }
     if (rc == DWCONV_OK) rc = launch_segments(delta_bwd_state_kernel<T, KT, false>, p, w, p.DV, lds, done[0], st);
     const auto kernel = p.each > 1 ? delta_bwd_chunk_kernel<T, KT, true> : delta_bwd_chunk_kernel<T, KT, false>;
@@ -271,14 +305,15 @@ size_t walk_bytes(int B, int H, int DK, int DV, int L, bool backward)          /
     size_t most = 0;
     for (const int dtype : {DWCONV_F32, DWCONV_BF16}) {
         const WalkPlan w = plan_walk(B, H, DK, DV, L, dtype, backward);
-        most = std::max(most, starts_bytes(w, B, H, DK, DV) + spans_bytes(w, B, H, DK, DV));
+        most = std::max(most, starts_bytes(w, B, H, DK, DV) + spans_bytes(w, B, H, DK, DV) + joined_bytes(w, B, H, DK, DV));
     }
     return most;
 }
 DeltaWalk walk_in(char *at, int B, int H, int DK, int DV, int L, int dtype, bool backward)
 {
     const WalkPlan w = plan_walk(B, H, DK, DV, L, dtype, backward);
-    return DeltaWalk{w.segs, w.per, 0, 0, reinterpret_cast<float *>(at), reinterpret_cast<float *>(at + starts_bytes(w, B, H, DK, DV))};
+    char *const spans = at + starts_bytes(w, B, H, DK, DV);
+    return DeltaWalk{w.segs, w.per, 0, 0, reinterpret_cast<float *>(at), reinterpret_cast<float *>(spans), w.join, reinterpret_cast<float *>(spans + spans_bytes(w, B, H, DK, DV))};
 }
 constexpr int kPadded = 8;
 size_t padded_bytes(int B, int H, int DK, int DV, int L) { return L < kPadded ? up16((size_t)B * H * (2 * (DK + DV)) * kPadded * sizeof(float)) : 0; }

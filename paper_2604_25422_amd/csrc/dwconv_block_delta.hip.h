@@ -552,6 +552,8 @@ struct DeltaWalk {
     int units, groups;          // segments of all heads, workgroups of the columns of each
     const float *starts;        // [B, H, segs, DK, DV]: the state that a segment starts with (one segment: the call's own)
     float *spans;               // [B, H, segs, DK, DV + DK]: of the pass that forms them
+    int join;                   // segments whose spans are joined to one on the way to the starts (1: none)
+    float *joined;              // [B, H, ceil(segs / join), DK, DV + DK]
 };
 
 // Workgroups go to the eight dies in turn, and each die has an L2 of its own: those of a segment's columns, which read the same keys, are eight apart.
@@ -887,44 +889,71 @@ template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWal
 }
 
 // The states that segments start with, one after the other (forward; backward the other way): S <- N + M S with a segment's span (N, M).  A workgroup
-// 16 columns, a wave 16 rows of them, fp32 products; the next span is on its way meanwhile.
-template <int KT, bool BACK> __global__ __launch_bounds__(64 * KT) void delta_starts_kernel(const float *s0, const float *spans, float *starts, int segs, int DK, int DV)
+// has 16 columns, a wave 16 rows of them; fp32 products, a step of 128 x 128 channels 2.9 us, 0.9 of them products; the next spans are on their way.
+// Many segments: three launches of chains about as long as the root of their number.  JOIN forms the span of `join` segments (all but the last of a
+// head), of the columns that a walk's spans have, ACROSS the starts of every first of them, WITHIN those of the others.
+enum class Starts { ALL, JOIN, ACROSS, WITHIN };
+template <int KT, bool BACK, Starts WHAT> __global__ __launch_bounds__(64 * KT) void delta_starts_kernel(const float *s0, DeltaWalk w, int DK, int DV)
 {
     __shared__ f32x4 tiles[2][KT][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g4 = 4 * (lane >> 4), dv = blockIdx.y * 16 + c;
-    const bool in = dv < DV;
-    const long long head = blockIdx.x, size = (long long)DK * DV, span = size + (long long)DK * DK;
-    const auto unit = [&](int i) { return head * segs + (BACK ? segs - 1 - i : i); };
-    f32x4 S = {}, a[KT], add;
-    const auto rows = [&](const StateIn &x) __attribute__((always_inline)) {
+    constexpr bool JOIN = WHAT == Starts::JOIN, ACROSS = WHAT == Starts::ACROSS, WITHIN = WHAT == Starts::WITHIN;
+    constexpr int AHEAD = KT == 8 ? 1 : 3;          // (more of the widest: fewer workgroups to a CU, and no faster)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g4 = 4 * (lane >> 4);
+    const Columns col(blockIdx.y, c, DK, DV, JOIN);
+    const int dv = col.at + c, groups = (w.segs + w.join - 1) / w.join, chains = JOIN ? groups - 1 : WITHIN ? groups : 1;
+    const long long head = blockIdx.x / chains, size = (long long)DK * DV, span = size + (long long)DK * DK;
+    const int group = blockIdx.x % chains, from = group * w.join;                   // (in the order in which they are walked)
+    const int steps = JOIN ? w.join : (ACROSS ? groups : WITHIN ? min(w.join, w.segs - from) : w.segs) - 1;
+    const auto segment = [&](int i) { return head * w.segs + (BACK ? w.segs - 1 - i : i); };
+    const auto rows = [&](const StateIn &x, bool in) __attribute__((always_inline)) {
         const unsigned at = x.lane(g4, dv, in);
         f32x4 r;
 #pragma unroll
         for (int v = 0; v < 4; ++v) r[v] = x.load(at, x.row(16 * wave + v));
         return r;
     };
-    const auto fetch = [&](int i) __attribute__((always_inline)) {
-        const StateIn x(spans + unit(i) * span, DK, DV + DK);
-        add = rows(x);
-#pragma unroll
-        for (int k = 0; k < KT; ++k) a[k] = x.four(16 * wave + c, DV + 16 * k + g4, DV + DK);
-    };
-    if (s0) S = rows(StateIn(s0 + head * size, DK, DV));
-    fetch(0);
-    for (int i = 0; i < segs; ++i) {
-        const StateIn to(starts + unit(i) * size, DK, DV);
-        const unsigned at = to.lane(g4, dv, in);
+    const auto put = [&](f32x4 S, const StateIn &to, int column) __attribute__((always_inline)) {
+        const unsigned at = to.lane(g4, column, col.in);
 #pragma unroll
         for (int v = 0; v < 4; ++v) to.store(S[v], at, to.row(16 * wave + v));
-        if (i + 1 == segs) break;
-        tiles[i & 1][wave][lane] = S;
-        __syncthreads();
-        f32x4 sum[2] = {add, f32x4{}};
+    };
+    f32x4 S = {}, a[AHEAD][KT], add[AHEAD];
+    const auto fetch = [&](int d, int i) __attribute__((always_inline)) {
+        const int at = max(min(i, steps - 1), 0);
+        const StateIn x(ACROSS ? w.joined + (head * groups + at) * span : w.spans + segment(from + at) * span, DK, DV + DK);
+        add[d] = rows(x, col.in && !col.unit);
 #pragma unroll
-        for (int k = 0; k < KT; ++k) sum[k & 1] = mma16(a[k], tiles[i & 1][k][lane], sum[k & 1]);
-        S = sum[0] + sum[1];
-        if (i + 2 < segs) fetch(i + 1);
+        for (int k = 0; k < KT; ++k) a[d][k] = x.any_four(16 * wave + c, DV + 16 * k + g4);
+    };
+    float *const starts = const_cast<float *>(w.starts);
+    if (JOIN) {
+        if (col.unit)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) S[v] = 16 * wave + g4 + v == dv ? 1.0f : 0.0f;
+    } else if (WITHIN) {
+        S = rows(StateIn(w.starts + segment(from) * size, DK, DV), col.in);
+    } else if (s0) {
+        S = rows(StateIn(s0 + head * size, DK, DV), col.in);
     }
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d) fetch(d, d);
+    for (int i0 = 0;; i0 += AHEAD)
+#pragma unroll
+        for (int d = 0; d < AHEAD; ++d) {
+            const int i = i0 + d;
+            if (!JOIN && !(WITHIN && i == 0)) put(S, StateIn(starts + segment(ACROSS ? i * w.join : from + i) * size, DK, DV), dv);
+            if (i == steps) {
+                if (JOIN) put(S, StateIn(w.joined + (head * groups + group) * span, DK, DV + DK), col.column);
+                return;
+            }
+            tiles[i & 1][wave][lane] = S;
+            __syncthreads();
+            f32x4 sum[2] = {add[d], f32x4{}};
+#pragma unroll
+            for (int k = 0; k < KT; ++k) sum[k & 1] = mma16(StateIn::inside(a[d][k], 16 * k + g4, DK), tiles[i & 1][k][lane], sum[k & 1]);
+            S = sum[0] + sum[1];
+            fetch(d, i + AHEAD);
+        }
 }
 
 // ---- gradients within a chunk ----

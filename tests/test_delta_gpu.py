@@ -188,6 +188,14 @@ def test_long_and_many(B, H, DK, DV, L, dtype):
     check_rule(*inputs(B, H, H, DK, DV, L, dtype, rate=0.05))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,H,Hk,DK,DV,L", [(2, 1, 1, 128, 40, 64 * 70 + 3), (3, 2, 1, 17, 130, 64 * 66), (1, 1, 1, 64, 64, 64 * 160 + 1)])
+def test_many_segments(B, H, Hk, DK, DV, L, dtype):
+    """Rows cut into so many segments that their spans are joined first; sequences that end in the first segments, in the last and between."""
+    lengths = torch.tensor([L, 300, L - 70][:B], dtype=torch.int32, device="cuda")
+    check_rule(*inputs(B, H, Hk, DK, DV, L, dtype, seed=L, rate=0.01), lengths=lengths, key_heads=Hk)
+
+
 def test_without_what_may_be_left_out():
     q, k, v, g, beta, s0, do, ds = inputs(2, 2, 2, 24, 40, 100, F32)
     got = check_rule(q, k, v, g, beta, None, do, None)
