@@ -152,14 +152,20 @@ template <typename Kernel> bool allow_lds(Kernel kernel, size_t bytes, std::atom
     return true;
 }
 
-template <typename T, int KT> int launch_pairs(const DeltaShape<T> &p, hipStream_t st)
+template <typename T, int KT, int W> int launch_pairs(const DeltaShape<T> &p, int units, hipStream_t st)
 {
     static std::atomic<unsigned long long> done{0};
-    const size_t lds = sizeof(PairsLds<T, KT>);
-    if (!allow_lds(delta_pairs_kernel<T, KT>, lds, done)) return DWCONV_ERR_LAUNCH;
-    const int units = p.B * p.H * p.chunks;
-    for_units(units, [&](int first, int n) { delta_pairs_kernel<T, KT><<<n, 256, lds, st>>>(p, first); });
+    const size_t lds = sizeof(PairsLds<T, KT, W>);
+    if (!allow_lds(delta_pairs_kernel<T, KT, W>, lds, done)) return DWCONV_ERR_LAUNCH;
+    for_units(units, [&](int first, int n) { delta_pairs_kernel<T, KT, W><<<n, 64 * W, lds, st>>>(p, first); });
     return DWCONV_OK;
+}
+// Waves of a chunk's pairs: eight where the chip has room for all of them at once, four of more chunks.  us of a trained call with eight / with four:
+// 128 chunks of 32 x 32 in fp32 89 / 93, 2048 of 64 x 96 in bf16 325 / 329; 8192 of 64 x 64 in fp32 1880 / 1848, 12288 of 128 x 128 in bf16 2630 / 2587.
+template <typename T, int KT> int launch_pairs(const DeltaShape<T> &p, hipStream_t st)
+{
+    const int units = p.B * p.H * p.chunks;
+    return units <= 2048 ? launch_pairs<T, KT, 8>(p, units, st) : launch_pairs<T, KT, 4>(p, units, st);
 }
 
 // Segments that a head's chunks are cut into.  A walk's steps are a chain: few heads leave most of the chip idle, and what a segment does to any state

@@ -398,7 +398,7 @@ template <typename T, int N, int LANES> struct LowTiles {
 
 // ---- what does not depend on the state ----
 
-template <typename T, int KT> struct PairsLds {
+template <typename T, int KT, int W> struct PairsLds {
     union {
         struct {
             typename Mat<T>::Elem k[16 * KT * kPitch], q[16 * KT * kPitch];
@@ -407,11 +407,11 @@ template <typename T, int KT> struct PairsLds {
     };
     float a[kLow];
     Gates s;
-    float part[2][4][64];
+    float part[2][W][64];
 };
 
 // T = (I + A)^-1 of A in LDS: the inverses of its diagonal blocks of 16 by substitution, a column a lane, and from them block column
-// after block column.  By four waves; T's blocks above the diagonal are not written.
+// after block column.  T's blocks above the diagonal are not written.
 __device__ __forceinline__ void invert(const float *A, float *T)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -458,15 +458,15 @@ __device__ __forceinline__ void invert(const float *A, float *T)
     __syncthreads();
 }
 
-// A record of every chunk with a position inside: by a workgroup of four waves.
-template <typename T, int KT> __device__ __forceinline__ void delta_pairs(const DeltaShape<T> &p, PairsLds<T, KT> &m, int unit)
+// A record of every chunk with a position inside: by a workgroup of W waves.
+template <typename T, int KT, int W> __device__ __forceinline__ void delta_pairs(const DeltaShape<T> &p, PairsLds<T, KT, W> &m, int unit)
 {
     typedef Mat<T> M;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g4 = 4 * (lane >> 4);
     const int ch = unit % p.chunks, bh = unit / p.chunks, b = bh / p.H, h = bh % p.H, hk = h / p.each, n = p.length(b), t0 = ch * kDeltaChunk;
     if (t0 >= n) return;
     DeltaPairs &to = p.pairs[unit];
-    Tile<T, 16 * KT, 256> k, q;
+    Tile<T, 16 * KT, 64 * W> k, q;
     k.load(p.k.row(b, hk * p.DK, p.pitch), p.DK, t0, p.pitch);
     q.load(p.q.row(b, hk * p.DK, p.pitch), p.DK, t0, p.pitch);
     float g = 0.0f, beta = 0.0f;
@@ -480,7 +480,7 @@ template <typename T, int KT> __device__ __forceinline__ void delta_pairs(const 
     {
         float x = 0.0f, y = 0.0f;
 #pragma unroll 8
-        for (int r = wave; r < 16 * KT; r += 4) {
+        for (int r = wave; r < 16 * KT; r += W) {
             float u, v;
             if constexpr (sizeof(T) == 4) u = m.k[r * kPitch + lane], v = m.q[r * kPitch + lane];
             else u = __uint_as_float((unsigned)(unsigned short)m.k[r * kPitch + lane] << 16), v = __uint_as_float((unsigned)(unsigned short)m.q[r * kPitch + lane] << 16);
@@ -504,15 +504,16 @@ template <typename T, int KT> __device__ __forceinline__ void delta_pairs(const 
     }
     __syncthreads();
     if (tid < 64) {
-        const float k2 = (m.part[0][0][tid] + m.part[0][1][tid]) + (m.part[0][2][tid] + m.part[0][3][tid]);
-        const float q2 = (m.part[1][0][tid] + m.part[1][1][tid]) + (m.part[1][2][tid] + m.part[1][3][tid]);
+        float k2 = 0.0f, q2 = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) k2 += m.part[0][w][tid], q2 += m.part[1][w][tid];
         const bool unit = p.eps > 0.0f;
         m.s.rk[tid] = unit ? 1.0f / sqrtf(k2 + p.eps) : 1.0f;
         m.s.iq[tid] = unit ? 1.0f / sqrtf(q2 + p.eps) : 1.0f;
         m.s.rq[tid] = p.scale * m.s.iq[tid];
     }
     __syncthreads();
-    for (int task = wave; task < 20; task += 4) {
+    for (int task = wave; task < 20; task += W) {
         int ti, tj;
         low_tile(task >> 1, ti, tj);
         const bool is_p = task & 1;
@@ -530,18 +531,18 @@ template <typename T, int KT> __device__ __forceinline__ void delta_pairs(const 
     }
     __syncthreads();
     invert(m.a, m.t);
-    for (int i = tid; i < 640; i += 256) {
+    for (int i = tid; i < 640; i += 64 * W) {
         int ti, tj;
         low_tile(i >> 6, ti, tj);
         *reinterpret_cast<f32x4 *>(to.t[i >> 6] + 4 * (i & 63)) = four(m.t, low_at(16 * ti + ((i & 63) >> 2), 16 * tj + 4 * (i & 3)));
     }
-    for (int i = tid; i < (int)sizeof(Gates) / 16; i += 256) reinterpret_cast<f32x4 *>(&to.s)[i] = reinterpret_cast<const f32x4 *>(&m.s)[i];
+    for (int i = tid; i < (int)sizeof(Gates) / 16; i += 64 * W) reinterpret_cast<f32x4 *>(&to.s)[i] = reinterpret_cast<const f32x4 *>(&m.s)[i];
 }
 // (a grid has fewer than 2^32 lanes in a dimension: of very many chunks or heads this launch has those from `first` on)
-template <typename T, int KT> __global__ __launch_bounds__(256) void delta_pairs_kernel(DeltaShape<T> p, int first)
+template <typename T, int KT, int W> __global__ __launch_bounds__(64 * W) void delta_pairs_kernel(DeltaShape<T> p, int first)
 {
     extern __shared__ char lds[];
-    delta_pairs(p, *reinterpret_cast<PairsLds<T, KT> *>(lds), first + (int)blockIdx.x);
+    delta_pairs(p, *reinterpret_cast<PairsLds<T, KT, W> *>(lds), first + (int)blockIdx.x);
 }
 
 // ---- from chunk to chunk ----
