@@ -42,11 +42,12 @@ template <typename T> struct DeltaStep {
     float scale, eps;
 };
 
-// One token.  A workgroup has up to 128 columns of a head's state in registers, four neighbouring ones a lane (2^lg lanes a row); with
-// S~ = exp(g) S both S~^T k and S~^T q are formed in one pass, o = scale (S~^T q + beta (k . q) u).
+// One token.  A workgroup has up to 64 columns of a head's state in registers, four neighbouring ones a lane (2^lg lanes a row); with
+// S~ = exp(g) S both S~^T k and S~^T q are formed in one pass, o = scale (S~^T q + beta (k . q) u).  Memory's time, a state read and written once:
+// 1536 heads of 128 x 128 of which a sixteenth is empty 35 to 39 us, 4.9 to 5.4 TB/s.
 struct StepLds {
     float k[128], q[128], sums[4][3];
-    f32x4 part[2][4][32];
+    f32x4 part[2][4][16];
 };
 template <typename T, int RT> __device__ __forceinline__ void delta_step_head(const DeltaStep<T> &p, int lg, int unit, StepLds &m)
 {
@@ -114,7 +115,9 @@ template <typename T, int RT> __global__ __launch_bounds__(256) void delta_step_
 namespace {
 
 constexpr int kMaxKey = 128;            // channels of a key: a state's columns are registers of a wave
-constexpr int kChain = 16;              // spans that are walked one after the other without joining some first
+// Spans that are walked one after the other without joining some first.  us of a forward pass with 16 segments in one chain / in three: bf16, 2 heads of 128 x
+// 128 80.1 / 80.0, 8 heads 111.3 / 111.0, 4 heads of 64 x 64 52.2 / 52.4; with 32 segments 2 heads of 128 x 128 189 / 156.
+constexpr int kChain = 16;
 constexpr int kMaxUnits = 1 << 22;      // workgroups of a launch, whose lanes stay below 2^32
 
 template <typename Launch> void for_units(int units, Launch launch)
@@ -287,14 +290,14 @@ template <typename T> int launch_bwd(const DeltaBwd<T> &p, const DeltaWalk &w, h
 template <typename T> void launch_step(const DeltaStep<T> &in, hipStream_t st)
 {
     DeltaStep<T> p = in;
-    // Lanes of a row, four columns each: whole rows of up to 128 columns, but 32 columns where the call would leave CUs without work.
+    // Lanes of a row, four columns each: 64 columns, but 32 where the call would leave CUs without work.  us with 32 / 64 / 128 columns (bf16, 128 x 128): 8 heads
+    // 4.2 / 4.7 / 5.9, 24 heads 4.3 / 4.9 / 6.1, 96 heads 5.4 / 5.5 / 6.6, 384 heads 9.4 / 8.7 / 9.2, 1536 heads 33.7 / 34.7 / 37.5; 64 x 64, 2048 heads 14.7 / 11.4.
     int lg = 0;
-    while (lg < 5 && (4 << lg) < p.DV) ++lg;
+    while (lg < 4 && (4 << lg) < p.DV) ++lg;
     while (lg > 3 && (long long)p.B * p.H * ceil_div(p.DV, 4 << lg) < 512) --lg;
     p.blocks = (int)ceil_div(p.DV, 4 << lg);
     const int units = p.B * p.H * p.blocks, rows = (int)ceil_div(p.DK, 256 >> lg);
-    const auto kernel = rows <= 1 ? delta_step_kernel<T, 1> : rows <= 2 ? delta_step_kernel<T, 2> : rows <= 4 ? delta_step_kernel<T, 4>
-                                 : rows <= 8 ? delta_step_kernel<T, 8> : delta_step_kernel<T, 16>;
+    const auto kernel = rows <= 1 ? delta_step_kernel<T, 1> : rows <= 2 ? delta_step_kernel<T, 2> : rows <= 4 ? delta_step_kernel<T, 4> : delta_step_kernel<T, 8>;
     for_units(units, [&](int first, int n) { kernel<<<n, 256, 0, st>>>(p, lg, first); });
 }
 
