@@ -267,13 +267,13 @@ template <typename T> __device__ __forceinline__ void store4(T *row, f32x4 r, in
 }
 // A lane's positions of a chunk, 16 i + g4 + v, of a row, as loaded: without a question, since a load behind one is waited for where its ways meet.
 // What would end behind the row is its last four, put right when they are asked for.
-template <typename T> struct Rows {
+template <typename T, int N = 4> struct Rows {
     typedef typename Words<4 * sizeof(T)>::type Raw;
-    Raw x[4];
+    Raw x[N];
     __device__ __forceinline__ void load(const T *row, int t0, int g4, int pitch)
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const Raw *>(row + min(t0 + 16 * i + g4, pitch - 4));
+        for (int i = 0; i < N; ++i) x[i] = *reinterpret_cast<const Raw *>(row + min(t0 + 16 * i + g4, pitch - 4));
     }
     static __device__ __forceinline__ f32x4 wide(const Words<16>::type u) { return __builtin_bit_cast(f32x4, u); }
     static __device__ __forceinline__ f32x4 wide(const Words<8>::type u)
@@ -281,13 +281,13 @@ template <typename T> struct Rows {
         return f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xffff0000u), __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xffff0000u)};
     }
     // Zeros from position n on.
-    __device__ __forceinline__ void get(f32x4 (&v)[4], int t0, int g4, int n, int pitch) const
+    __device__ __forceinline__ void get(f32x4 (&v)[N], int t0, int g4, int n, int pitch) const
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = wide(x[i]);
-        if (t0 + 64 <= n) return;
+        for (int i = 0; i < N; ++i) v[i] = wide(x[i]);
+        if (t0 + 16 * N <= n) return;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < N; ++i) {
             const int t = t0 + 16 * i + g4, by = t - (pitch - 4);
             f32x4 u = v[i];
             if (by > 0 && by & 2) u = f32x4{u[2], u[3], 0.0f, 0.0f};
@@ -987,6 +987,7 @@ template <typename T, int KT> struct DeltaChunkLds {
     typedef typename Mat<T>::Elem Elem;
     static constexpr int NP = Mat<T>::planes, N2 = NP < 2 ? NP : 2, VB = 32;        // columns of a state at a time
     static constexpr int G = KT < kGradWaves ? KT : kGradWaves;                     // groups of the key's channels
+    static constexpr bool HALVES = sizeof(T) == 2 || KT < 8;                        // (of wide keys in fp32 two workgroups have no room for x)
     Elem k[16 * KT * kPitch], t[NP * kLow];
     union {
         struct {
@@ -998,7 +999,11 @@ template <typename T, int KT> struct DeltaChunkLds {
         };
     };
     ChunkGates s;
-    float part[3][G][64], db[2][64], da[10][16], dg[10][16], whole[G];
+    float db[2][64], da[10][16], dg[10][16], whole[G];
+    union {
+        float part[3][G][64];
+        f32x4 x[2][HALVES ? 4 : 0][64];     // of 16 columns, their tiles of beta (v - S~^T k), where there is room for them
+    };
     // Sums of a tile's rows and columns, in what the pairs leave of their place: blocks (0, 1) and (2, 3).
     __device__ __forceinline__ float *rows(int tile) { return pairs + low_at(tile, 16); }
     __device__ __forceinline__ float *columns(int tile) { return pairs + low_at(32 + tile, 48); }
@@ -1011,7 +1016,7 @@ template <typename T, int KT> struct DeltaChunkLds {
 //     dg_t = exp(G_63) <dS, S> + sum_{i >= t} x_i + sum_{j < t} y_j + sum_{i >= t > j} W_ij,
 // x_i what row i took of S and y_j what is left of column j in S'.  (As a difference of whole sums, which is shorter, it would be
 // the rounding of those where a decay is strong.)  A workgroup has a chunk of a head, 32 columns of its states at a time.  First a wave has 16 columns
-// of w, all of k^T S and two tiles of T times that (which gives the same k^T S twice, and keeps all four waves at work); then SL slices of 16
+// of w, two of k^T S's tiles (the other two are another wave's; without room for those all four) and two of T times that; then SL slices of 16
 // channels of the key and NI tiles of 16 positions.  12288 chunks of 128 x 128 channels in bf16 1.29 ms: vector instructions, the limbs above all, and products
 // take a SIMD's cycles in turn (48 and 30 %; 3.75 GB, 2.9 TB/s); with 64 columns at a time, dr formed here and so one workgroup of eight waves to a CU
 // it were 1.6.  8192 chunks of 64 x 64 in fp32 635 us, 47 % of it products.  SHARED: dq and dk of q and k of unit length go to part_q and part_k, which delta_share_kernel adds up.
@@ -1020,13 +1025,13 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
     typedef Mat<T> M;
     typedef typename M::Full Full;
     typedef DeltaChunkLds<T, KT> Lds;
-    constexpr int W = kGradWaves, VB = Lds::VB, VP = VB * kPitch, G = Lds::G, SL = KT / G, NI = G, TASKS = (10 + W - 1) / W;
+    constexpr int W = kGradWaves, VB = Lds::VB, VP = VB * kPitch, G = Lds::G, SL = KT / G, NI = G, TASKS = (10 + W - 1) / W, TI = Lds::HALVES ? 2 : 4;
     static_assert(VB == 32 && W == 4, "a wave has 16 columns of w and half of their rows");
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int ch = unit % p.chunks, head = unit / p.chunks, b = head / p.H, h = head % p.H, hk = h / p.each;
     const int n = p.length(b), t0 = ch * kDeltaChunk;
     const int group = wave % G, slice0 = group * SL, tile0 = wave / G * NI;         // this wave's channels of the key, and tiles of positions
-    const int half = wave >> 1;
+    const int half = wave >> 1, first = Lds::HALVES ? 32 * half : 0;
     T *const dq_row = SHARED ? nullptr : p.dq.row(b, hk * p.DK, p.L), *const dk_row = SHARED ? nullptr : p.dk.row(b, hk * p.DK, p.L);
     float *const part_q = p.part + ((long long)head * 2 * p.DK) * p.L, *const part_k = part_q + (long long)p.DK * p.L;
     if (t0 >= n) {
@@ -1042,13 +1047,13 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
     const float *const drs = p.dr + (long long)unit * p.DV * 64;
     // What the first step takes from memory, ahead of it.
     f32x4 S[KT], dr[2];
-    Rows<T> vrow;
+    Rows<T, TI> vrow;
     Tile<T, VB, 64 * W> drow;
     const auto fetch = [&](int v0) __attribute__((always_inline)) {
         const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dv = v0 + 16 * (wave & 1) + c;
         const bool in = dv < p.DV;
         load_state(S, before, dv, in, g4);
-        vrow.load(values + (long long)(in ? dv : 0) * p.pitch, t0, g4, p.pitch);
+        vrow.load(values + (long long)(in ? dv : 0) * p.pitch, t0 + first, g4, p.pitch);
         drow.load(douts + (long long)v0 * p.pitch, p.DV - v0, t0, p.pitch);
 #pragma unroll
         for (int i = 0; i < 2; ++i) dr[i] = four(drs + (long long)(in ? dv : 0) * 64, 32 * half + 16 * i + g4);
@@ -1087,26 +1092,42 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
     for (int v0 = 0;; v0 += VB) {
         {
             const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), row = (16 * (wave & 1) + c) * kPitch + g4;
-            f32x4 x[4] = {}, val[4];
+            f32x4 x[4] = {}, val[TI];
 #pragma unroll
             for (int kb = 0; kb < KT; kb += 2) {
                 const Full s = M::split(S[kb], S[kb + 1]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = M::mma(M::columns_in(m.k, 16 * i, 16 * kb, lane), s, x[i]);
+                for (int i = 0; i < TI; ++i) x[i] = M::mma(M::columns_in(m.k, first + 16 * i, 16 * kb, lane), s, x[i]);
                 step_done();
             }
-            vrow.get(val, t0, g4, n, p.pitch);
+            vrow.get(val, t0 + first, g4, n, p.pitch);
             if (v0 + VB > p.DV) {
                 const bool out = v0 + 16 * (wave & 1) + c >= p.DV;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) val[i] = out ? f32x4{} : val[i];
+                for (int i = 0; i < TI; ++i) val[i] = out ? f32x4{} : val[i];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) dr[i] = out ? f32x4{} : dr[i];
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = 16 * i + g4;
+            for (int i = 0; i < TI; ++i) {
+                const int t = first + 16 * i + g4;
                 x[i] = four(m.s.beta, t) * fma4(four(m.s.eG, t) * -four(m.s.rk, t), x[i], val[i]);
+                if (Lds::HALVES) m.x[wave & 1][2 * half + i][lane] = x[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                f32x4 v;
+                if constexpr (Lds::HALVES) v = val[i];
+                else v = pick<2>(val, i, 2 * half);
+                const f32x4 sum = sum16(dr[i] * v);
+                if (c == 0) *reinterpret_cast<f32x4 *>(&m.db[wave & 1][32 * half + 16 * i + g4]) += sum;
+                M::put(m.dr, VP, row + 32 * half + 16 * i, dr[i]);
+            }
+            drow.put(m.dout, p.DV - v0, t0, n, p.pitch);
+            if (Lds::HALVES) {
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = m.x[wave & 1][i][lane];
             }
             const int near = 16 * half, far = 48 - 16 * half;           // tiles 0 and 3, or 1 and 2: of three blocks 32 wide either way
             const Full z0 = M::split(x[0], x[1]), z1 = M::split(x[2], x[3]);
@@ -1115,13 +1136,6 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
             const f32x4 yf = M::mma(M::low_rows(m.t, far, 1, lane), z1, M::mma(M::low_rows(m.t, far, 0, lane), z0, f32x4{}));
             M::put(m.w, VP, row + near, yn);
             M::put(m.w, VP, row + far, yf);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const f32x4 sum = sum16(dr[i] * pick<2>(val, i, 2 * half));
-                if (c == 0) *reinterpret_cast<f32x4 *>(&m.db[wave & 1][32 * half + 16 * i + g4]) += sum;
-                M::put(m.dr, VP, row + 32 * half + 16 * i, dr[i]);
-            }
-            drow.put(m.dout, p.DV - v0, t0, n, p.pitch);
             step_done();
         }
         {
