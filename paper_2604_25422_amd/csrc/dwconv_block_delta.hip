@@ -174,10 +174,10 @@ template <typename T, int KT> int launch_pairs(const DeltaShape<T> &p, hipStream
 // Segments that a head's chunks are cut into.  A walk's steps are a chain: few heads leave most of the chip idle, and what a segment does to any state
 // it starts with (DV + DK columns instead of DV) can be formed for all segments at once, the states between them in a chain of its own, which takes a
 // third of a step each, and then all segments at once again.  In steps of a walk that has a CU to itself (two workgroups share one at 1.4 times that;
-// in fp32 with more than 64 channels of a key LDS has room for one), forward the pass that forms spans writes no output and takes 0.6.
+// in fp32 with more than 32 channels of a key LDS has room for one), forward the pass that forms spans writes no output and takes 0.6.
 // us whole / cut (segments): bf16, DK = DV = 128, 256 chunks, 2 heads forward 1578 / 147 (64), backward 1594 / 212; 32 heads 1811 / 762 (8), 2673 / 1790; 64
-// heads 1965 / 1457 (4), 3685 / 3522; 128 heads, 64 chunks 567 / 784, 1380 / 1765; 2 heads, 8 chunks 63 / 50 (4), 99 / 89.  fp32, 64 heads, 64 chunks 1099 /
-// 1192, 1794 / 2150.  DK = DV = 64, 64 chunks, bf16, 128 heads 351 / 319 (4), 766 / 805; fp32 613 / 585, 1255 / 1365.
+// heads 1965 / 1457 (4), 3685 / 3522; 128 heads, 64 chunks 567 / 784, 1380 / 1765; 2 heads, 8 chunks 63 / 50 (4), 99 / 89.  fp32, 64 heads, 64 chunks 884 /
+// 953 (2), 1647 / 1920.  DK = DV = 64, 64 chunks, 128 heads, bf16 351 / 319 (4), 766 / 805; fp32 563 / 596 (2), 1186 / 1367; 64 heads 479 / 314 (4), 815 / 704.
 struct WalkPlan {
     int segs, per, join;
 };
@@ -201,7 +201,7 @@ ChainPlan plan_chain(double heads, int segs, int DK, int DV)
 WalkPlan plan_walk(int B, int H, int DK, int DV, int L, int dtype, bool backward)
 {
     const int chunks = chunks_of(L);
-    const bool alone = dtype == DWCONV_F32 && DK > 64;
+    const bool alone = dtype == DWCONV_F32 && DK > 32;
     const double heads = (double)B * H, values = (double)ceil_div(DV, 16 * kWalkWaves),
                  all = (double)ceil_div(ceil_div(DV, 16) + ceil_div(DK, 16), kWalkWaves);
     const auto step = [&](double groups) { return groups <= 256 ? 1.0 : alone ? groups / 256 : groups <= 512 ? 1.4 : 1.4 * groups / 512; };

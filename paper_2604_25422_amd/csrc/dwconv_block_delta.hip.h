@@ -10,9 +10,9 @@
 // What does not depend on the state is formed first, for all chunks at once (delta_pairs_kernel: T = (I + A)^-1 and P, 32 KB a chunk);
 // the walk from chunk to chunk is then three products deep.
 //
-// Products: fp32 calls on the fp32 matrix instruction.  bf16 calls on the bf16 one, 16 times as fast: what is stored as bf16 goes in as it is, and
-// what is fp32 (the state, w, T, P) as the exact sum of three bf16 limbs, so that sums and states are those of fp32 products to 2^-24; the products that
-// only reach an output rounded to bf16 leave out the third limb (2^-16 of them, 2^-8 of the rounding).
+// Products: bf16 calls on the bf16 matrix instruction, 16 times as fast as the fp32 one: what is stored as bf16 goes in as it is, and what is fp32 (the
+// state, w, T, P) as the exact sum of three bf16 limbs, so that sums and states are those of fp32 products to 2^-24; the products that only reach an
+// output rounded to bf16 leave out the third limb (2^-16 of them, 2^-8 of the rounding).  fp32 calls on the fp32 instruction, but for their walks.
 #pragma once
 #include "dwconv_block_common.hip.h"
 
@@ -246,6 +246,33 @@ template <> struct Mat<bf16_t> {
     }
 };
 
+// What a walk multiplies with.  Its chain is the call's time where heads are few, so fp32 calls go by limbs too, keys, queries and dout as three of them:
+// six products of 16 cycles for eight of 32 on the fp32 instruction, to the same 2^-24.  In LDS a key is then half as large again, and from 33 channels on one
+// workgroup is what a CU has room for.  us of a forward pass by limbs / by the fp32 instruction: 128 heads of 64 x 64 over 4096 positions 564 / 588, 32 heads of
+// 128 x 128 over 4096 461 / 590, 64 heads of 32 x 32 over 4096 144 / 165, 8 heads over 1024 32 / 36.
+template <typename T, int KT> struct WalkMat : Mat<T> {
+    static constexpr int in_planes = 1, resident = 2;            // (workgroups that a CU has room for)
+    static constexpr int limbs(int n) { return n; }
+};
+template <int KT> struct WalkMat<float, KT> : Mat<bf16_t> {
+    typedef Mat<bf16_t> M;
+    typedef Full In;
+    static constexpr int in_planes = 3, plane = 16 * KT * kPitch, resident = KT < 4 ? 2 : 1;
+    static constexpr int limbs(int) { return 3; }
+    static __device__ __forceinline__ In rows_in(const short *x, int m, int k, int lane)
+    {
+        Full f{};
+#pragma unroll
+        for (int n = 0; n < 3; ++n) f.l[n] = row(x + n * plane, m, k, lane);
+        return f;
+    }
+    static __device__ __forceinline__ In columns_in(const short *x, int m, int k, int lane) { return M::template columns<3>(x, plane, m, k, lane); }
+    template <int N = 3> static __device__ __forceinline__ Full low_rows(const short *x, int m, int kb, int lane) { return M::template low_rows<3>(x, m, kb, lane); }
+    template <int N = 3> static __device__ __forceinline__ Full split(f32x4 a, f32x4 b) { return M::template split<3>(a, b); }
+    static __device__ __forceinline__ In exact(f32x4 a, f32x4 b) { return M::template split<3>(a, b); }
+    template <int ORDER = 3> static __device__ __forceinline__ f32x4 mma(const Full &a, const Full &b, f32x4 d) { return M::template mma<3>(a, b, d); }
+};
+
 // Four consecutive positions of a row.
 typedef unsigned uintx2_any __attribute__((ext_vector_type(2), aligned(2)));
 __device__ __forceinline__ f32x4 load4(const float *p) { return *reinterpret_cast<const floatx4_any *>(p); }
@@ -329,7 +356,7 @@ template <typename T, int ROWS, int LANES> struct Tile {
             e[u] = load8(from + (long long)(r < D ? r : 0) * pitch + min(t0 + (i & 7) * 8, pitch - 8));
         }
     }
-    __device__ __forceinline__ void put(typename Mat<T>::Elem *to, int D, int t0, int n, int pitch) const
+    template <typename E> __device__ __forceinline__ void put(E *to, int D, int t0, int n, int pitch) const      // (fp32 into shorts: three limbs, a plane each)
     {
 #pragma unroll
         for (int u = 0; u < N; ++u) {
@@ -349,6 +376,15 @@ template <typename T, int ROWS, int LANES> struct Tile {
         f32x4 *p = reinterpret_cast<f32x4 *>(to);
         p[0] = a, p[1] = b;
     }
+    static __device__ __forceinline__ void put_eight(short *to, const Eight<float> &e, int left)
+    {
+        f32x4 a = e.lo, b = e.hi;
+        if (left < 8)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) a[k] = k < left ? a[k] : 0.0f, b[k] = k + 4 < left ? b[k] : 0.0f;
+        Mat<bf16_t>::put(to, ROWS * kPitch, 0, a);
+        Mat<bf16_t>::put(to, ROWS * kPitch, 4, b);
+    }
     static __device__ __forceinline__ void put_eight(short *to, const Eight<bf16_t> &e, int left)
     {
         u32x4 w = e.w;
@@ -366,7 +402,7 @@ __device__ __forceinline__ void low_tile(int i, int &ti, int &tj)     // tile i 
     tj = i - ti * (ti + 1) / 2;
 }
 // The lower triangle of a chunk's matrix on its way from a record into LDS as a Full matrix of N limbs.
-template <typename T, int N, int LANES> struct LowTiles {
+template <typename M, int N, int LANES> struct LowTiles {
     static constexpr int U = (640 + LANES - 1) / LANES;
     f32x4 x[U];
     __device__ __forceinline__ void load(const float (&from)[10][256])
@@ -377,7 +413,7 @@ template <typename T, int N, int LANES> struct LowTiles {
             x[u] = four(from[0], 4 * (640 % LANES ? min(i, 639) : i));
         }
     }
-    __device__ __forceinline__ void put(typename Mat<T>::Elem *to) const
+    __device__ __forceinline__ void put(typename M::Elem *to) const
     {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -385,14 +421,14 @@ template <typename T, int N, int LANES> struct LowTiles {
             if (640 % LANES && i >= 640) continue;
             int ti, tj;
             low_tile(i >> 6, ti, tj);
-            Mat<T>::template put<N>(to, kLow, low_at(16 * ti + ((i & 63) >> 2), 16 * tj + 4 * (i & 3)), x[u]);
+            M::template put<N>(to, kLow, low_at(16 * ti + ((i & 63) >> 2), 16 * tj + 4 * (i & 3)), x[u]);
         }
     }
     // What a product 32 deep takes beside the triangle: blocks (0, 1) and (2, 3), zeros, written once.
-    static __device__ __forceinline__ void zeros(typename Mat<T>::Elem *to)
+    static __device__ __forceinline__ void zeros(typename M::Elem *to)
     {
         for (int i = threadIdx.x; i < 2 * 64; i += LANES)
-            Mat<T>::template put<N>(to, kLow, low_at((i >> 6) * 32 + ((i & 63) >> 2), (i >> 6) * 32 + 16 + 4 * (i & 3)), f32x4{});
+            M::template put<N>(to, kLow, low_at((i >> 6) * 32 + ((i & 63) >> 2), (i >> 6) * 32 + 16 + 4 * (i & 3)), f32x4{});
     }
 };
 
@@ -564,9 +600,10 @@ struct WalkPlace {
     __device__ __forceinline__ WalkPlace(long long id, int groups) : unit((int)(id / (8ll * groups)) * 8 + (int)(id & 7)), group((int)(id / 8 % groups)) {}
 };
 
-// (P in as many limbs as a walk takes: two for an output, three for a gradient that goes on.)
+// (P in as many limbs as a walk takes: two for an output in bf16, three for a gradient that goes on.)
 template <typename T, int KT, int NP> struct DeltaLds {
-    typename Mat<T>::Elem k[16 * KT * kPitch], q[16 * KT * kPitch], t[Mat<T>::planes * kLow], p[(Mat<T>::planes < NP ? Mat<T>::planes : NP) * kLow];
+    typedef WalkMat<T, KT> M;
+    typename M::Elem k[M::in_planes * 16 * KT * kPitch], q[M::in_planes * 16 * KT * kPitch], t[3 * kLow], p[M::limbs(NP) * kLow];
     Gates s;
 };
 constexpr int kWalkWaves = 4;           // of a workgroup; two of those fit a CU, one's products beside the other's way into LDS
@@ -574,8 +611,8 @@ constexpr int kWalkWaves = 4;           // of a workgroup; two of those fit a CU
 template <typename T, int KT, int NP, bool KEYS_ONLY> struct Ahead {
     static constexpr int LANES = 64 * kWalkWaves, NG = sizeof(Gates) / 16;
     Tile<T, 16 * KT, LANES> k, q;
-    LowTiles<T, 3, LANES> t;
-    LowTiles<T, NP, LANES> p;
+    LowTiles<Mat<bf16_t>, 3, LANES> t;
+    LowTiles<Mat<bf16_t>, WalkMat<T, KT>::limbs(NP), LANES> p;
     f32x4 s;
     Rows<T> rows;
     __device__ __forceinline__ void load(const DeltaShape<T> &a, const T *krow, const T *qrow, const T *row, const DeltaPairs *r, int t0, int g4)
@@ -683,7 +720,7 @@ template <int KT> __device__ __forceinline__ void unit_state(f32x4 (&S)[KT], int
 // 7.4 us of 128 x 128 channels in bf16 where a workgroup has its CU to itself, 10.3 where two share it (products and vector instructions of either are 2.7).
 template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_fwd_walk(const DeltaFwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT, 2> &m, int unit, int group)
 {
-    typedef Mat<T> M;
+    typedef WalkMat<T, KT> M;
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = unit / walk.segs, seg = unit % walk.segs, b = row / p.H, h = row % p.H, hk = h / p.each, n = p.length(b);
     const int from = seg * walk.per, last = min(from + walk.per, (n + 63) / 64);
@@ -773,12 +810,12 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
         for (int t = max(last, from) * 64 + g4, to = min(p.L, seg + 1 < walk.segs ? (from + walk.per) * 64 : p.L); t < to; t += 16) store4(orow, f32x4{}, t, p.L);
     if (p.s_last && seg + 1 == walk.segs) store_state(S, StateIn(p.s_last + head * size, p.DK, p.DV), col.at + c, in, g4);
 }
-template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWalkWaves, 2) void delta_fwd_kernel(DeltaFwd<T> p, DeltaWalk walk, long long first)
+template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWalkWaves, (WalkMat<T, KT>::resident)) void delta_fwd_kernel(DeltaFwd<T> p, DeltaWalk walk, long long first)
 {
     extern __shared__ char lds[];
     DeltaLds<T, KT, 2> &m = *reinterpret_cast<DeltaLds<T, KT, 2> *>(lds);
-    LowTiles<T, 3, 64 * kWalkWaves>::zeros(m.t);
-    if (!SPANS) LowTiles<T, 2, 64 * kWalkWaves>::zeros(m.p);
+    LowTiles<Mat<bf16_t>, 3, 64 * kWalkWaves>::zeros(m.t);
+    if (!SPANS) LowTiles<Mat<bf16_t>, WalkMat<T, KT>::limbs(2), 64 * kWalkWaves>::zeros(m.p);
     const WalkPlace at(first + blockIdx.x, walk.groups);
     if (at.unit < walk.units) delta_fwd_walk<T, KT, SPANS>(p, walk, m, at.unit, at.group);
 }
@@ -788,7 +825,7 @@ template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWal
 // 768 heads as above: 2.36 GB in 538 us, 4.4 TB/s.  Leaves dS behind every chunk, dr (whole, what needs it next does not form it again) and dv = beta dr.
 template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_bwd_walk(const DeltaBwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT, 3> &m, int unit, int group)
 {
-    typedef Mat<T> M;
+    typedef WalkMat<T, KT> M;
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = unit / walk.segs, seg = unit % walk.segs, b = row / p.H, h = row % p.H, hk = h / p.each, n = p.length(b);
     const int from = seg * walk.per, last = min(from + walk.per, (n + 63) / 64);
@@ -883,12 +920,12 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
     if (SPANS) store_state(S, StateIn(walk.spans + unit * size + unit * (long long)p.DK * p.DK, p.DK, p.DV + p.DK), col.column, in, g4);
     else if (p.ds0 && seg == 0) store_state(S, StateIn(p.ds0 + head * size, p.DK, p.DV), col.at + c, in, g4);
 }
-template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWalkWaves, 2) void delta_bwd_state_kernel(DeltaBwd<T> p, DeltaWalk walk, long long first)
+template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWalkWaves, (WalkMat<T, KT>::resident)) void delta_bwd_state_kernel(DeltaBwd<T> p, DeltaWalk walk, long long first)
 {
     extern __shared__ char lds[];
     DeltaLds<T, KT, 3> &m = *reinterpret_cast<DeltaLds<T, KT, 3> *>(lds);
-    LowTiles<T, 3, 64 * kWalkWaves>::zeros(m.t);
-    LowTiles<T, 3, 64 * kWalkWaves>::zeros(m.p);
+    LowTiles<Mat<bf16_t>, 3, 64 * kWalkWaves>::zeros(m.t);
+    LowTiles<Mat<bf16_t>, 3, 64 * kWalkWaves>::zeros(m.p);
     const WalkPlace at(first + blockIdx.x, walk.groups);
     if (at.unit < walk.units) delta_bwd_walk<T, KT, SPANS>(p, walk, m, at.unit, at.group);
 }
@@ -1060,7 +1097,7 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
     };
     {
         Tile<T, 16 * KT, 64 * W> kt;
-        LowTiles<T, 3, 64 * W> t;
+        LowTiles<M, 3, 64 * W> t;
         kt.load(p.k.row(b, hk * p.DK, p.pitch), p.DK, t0, p.pitch);
         t.load(pairs.t);
         const f32x4 gates = reinterpret_cast<const f32x4 *>(&pairs.s)[threadIdx.x < sizeof(ChunkGates) / 16 ? threadIdx.x : 0];
@@ -1203,7 +1240,7 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
         }
         take_pairs();
         __syncthreads();
-        LowTiles<T, Lds::N2, 64 * W>::zeros(m.p);
+        LowTiles<M, Lds::N2, 64 * W>::zeros(m.p);
 #pragma unroll
         for (int s = 0; s < SL; ++s) {
             qrow[s].get(qh[s], t0, g4, n, p.pitch);
@@ -1395,7 +1432,7 @@ template <typename T, int KT, bool SHARED> __global__ __launch_bounds__(64 * kGr
 {
     extern __shared__ char lds[];
     DeltaChunkLds<T, KT> &m = *reinterpret_cast<DeltaChunkLds<T, KT> *>(lds);
-    LowTiles<T, 3, 64 * kGradWaves>::zeros(m.t);
+    LowTiles<Mat<T>, 3, 64 * kGradWaves>::zeros(m.t);
     delta_bwd_chunk<T, KT, SHARED>(p, m, first + (int)blockIdx.x);
 }
 
