@@ -107,6 +107,22 @@ __device__ __forceinline__ int fresh(int lane)
 // Keeps the compiler from reading far ahead of the products: it would take all operands of a loop into registers at once, and spill.
 __device__ __forceinline__ void step_done() { __builtin_amdgcn_sched_barrier(0); }
 
+// N steps whose operands are read AHEAD steps before: left to itself the compiler reads every operand right before its product, and a wave waits for LDS
+// each time.
+template <int N, int AHEAD, typename Load, typename Use> __device__ __forceinline__ void piped(Load load, Use use)
+{
+    decltype(load(0)) x[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) x[u] = load(u);
+    step_done();
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        use(u, x[u % AHEAD]);
+        if (u + AHEAD < N) x[u % AHEAD] = load(u + AHEAD);
+        step_done();
+    }
+}
+
 // Products of 16 x 32 x 16.  An operand is 32 terms deep: lane (c, g) holds terms 4 g + v and 16 + 4 g + v of its row or column c, which is how
 // two tiles of a product lie (split()), so that a product is the next one's operand without leaving the registers.
 // In: of a matrix stored as T; Full: of one in 32 bits.  A Full matrix in LDS is `planes` matrices, `plane` elements apart.
@@ -758,15 +774,22 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
         if (ch + 1 < last) next.load(p, krow, qrow, vrow, pairs + ch + 1, t0 + 64, g4);
         if (!col.active) continue;
         f32x4 r[4] = {}, w[4] = {}, o[4] = {};
-#pragma unroll
-        for (int kb = 0; kb < KT; kb += 2) {
-            const typename M::Full s = M::split(S[kb], S[kb + 1]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                r[i] = M::mma(M::columns_in(m.k, 16 * i, 16 * kb, lane), s, r[i]);
-                if (!SPANS) o[i] = M::template mma<2>(M::columns_in(m.q, 16 * i, 16 * kb, lane), s, o[i]);
-            }
-        }
+        typename M::Full x;
+        piped<2 * KT, 2>(
+            [&](int u) __attribute__((always_inline)) {
+                struct {
+                    typename M::In k, q;
+                } a;
+                a.k = M::columns_in(m.k, 16 * (u & 3), 32 * (u >> 2), lane);
+                if constexpr (!SPANS) a.q = M::columns_in(m.q, 16 * (u & 3), 32 * (u >> 2), lane);
+                return a;
+            },
+            [&](int u, const auto &a) __attribute__((always_inline)) {
+                const int i = u & 3, kb = 2 * (u >> 2);
+                if (i == 0) x = M::split(S[kb], S[kb + 1]);
+                r[i] = M::mma(a.k, x, r[i]);
+                if constexpr (!SPANS) o[i] = M::template mma<2>(a.q, x, o[i]);
+            });
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = 16 * i + g4;
@@ -774,19 +797,18 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
             r[i] = four(m.s.beta, t) * (val[i] - four(m.s.eG, t) * four(m.s.rk, t) * r[i]);
             if (!SPANS) o[i] *= four(m.s.eG, t) * four(m.s.rq, t);
         }
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const typename M::Full x = M::split(r[2 * kb], r[2 * kb + 1]);
-#pragma unroll
-            for (int i = 2 * kb; i < 4; ++i) w[i] = M::mma(M::low_rows(m.t, 16 * i, kb, lane), x, w[i]);
-        }
+        // (blocks 32 wide of a lower triangle: of the first columns all four rows of blocks, of the others two)
+        piped<6, 1>([&](int u) __attribute__((always_inline)) { return M::low_rows(m.t, 16 * (u < 4 ? u : u - 2), u >> 2, lane); },
+                    [&](int u, const auto &a) __attribute__((always_inline)) {
+                        if (u % 4 == 0) x = M::split(r[u / 2], r[u / 2 + 1]);
+                        w[u < 4 ? u : u - 2] = M::mma(a, x, w[u < 4 ? u : u - 2]);
+                    });
         if (!SPANS) {
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                const typename M::Full x = M::template split<2>(w[2 * kb], w[2 * kb + 1]);
-#pragma unroll
-                for (int i = 2 * kb; i < 4; ++i) o[i] = M::template mma<2>(M::template low_rows<2>(m.p, 16 * i, kb, lane), x, o[i]);
-            }
+            piped<6, 1>([&](int u) __attribute__((always_inline)) { return M::template low_rows<2>(m.p, 16 * (u < 4 ? u : u - 2), u >> 2, lane); },
+                        [&](int u, const auto &a) __attribute__((always_inline)) {
+                            if (u % 4 == 0) x = M::template split<2>(w[u / 2], w[u / 2 + 1]);
+                            o[u < 4 ? u : u - 2] = M::template mma<2>(a, x, o[u < 4 ? u : u - 2]);
+                        });
             store_rows(orow, o, t0, g4, p.L, in);       // (k and q behind n are zeros, so these are)
         }
         const float eA = m.s.eG[63];
@@ -794,12 +816,11 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
         for (int i = 0; i < 4; ++i) w[i] *= four(m.s.eC, 16 * i + g4) * four(m.s.rk, 16 * i + g4);
 #pragma unroll
         for (int kb = 0; kb < KT; ++kb) S[kb] *= eA;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const typename M::Full x = M::split(w[2 * j], w[2 * j + 1]);
-#pragma unroll
-            for (int kb = 0; kb < KT; ++kb) S[kb] = M::mma(M::rows_in(m.k, 16 * kb, 32 * j, lane), x, S[kb]);
-        }
+        piped<2 * KT, 3>([&](int u) __attribute__((always_inline)) { return M::rows_in(m.k, 16 * (u % KT), 32 * (u / KT), lane); },
+                         [&](int u, const auto &a) __attribute__((always_inline)) {
+                             if (u % KT == 0) x = M::split(w[2 * (u / KT)], w[2 * (u / KT) + 1]);
+                             S[u % KT] = M::mma(a, x, S[u % KT]);
+                         });
     }
     const int c = lane0 & 15, g4 = 4 * (lane0 >> 4);
     if (SPANS) {
@@ -869,26 +890,26 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
         if (ch > from) next.load(p, krow, qrow, drow, pairs + ch - 1, t0 - 64, g4);
         if (!col.active) continue;
         f32x4 w[4] = {}, r[4] = {};
-#pragma unroll
-        for (int kb = 0; kb < KT; kb += 2) {
-            const typename M::Full s = M::split(S[kb], S[kb + 1]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = M::mma(M::columns_in(m.k, 16 * i, 16 * kb, lane), s, w[i]);
-        }
+        typename M::Full x;
+        piped<2 * KT, 3>([&](int u) __attribute__((always_inline)) { return M::columns_in(m.k, 16 * (u & 3), 32 * (u >> 2), lane); },
+                         [&](int u, const auto &a) __attribute__((always_inline)) {
+                             if (u % 4 == 0) x = M::split(S[2 * (u >> 2)], S[2 * (u >> 2) + 1]);
+                             w[u & 3] = M::mma(a, x, w[u & 3]);
+                         });
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] *= four(m.s.eC, 16 * i + g4) * four(m.s.rk, 16 * i + g4);
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const typename M::In x = M::exact(d[2 * kb], d[2 * kb + 1]);
-#pragma unroll
-            for (int j = 0; j < 2 * kb + 2; ++j) w[j] = M::mma(M::low_columns(m.p, 16 * j, kb, lane), x, w[j]);
-        }
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const typename M::Full x = M::split(w[2 * kb], w[2 * kb + 1]);
-#pragma unroll
-            for (int j = 0; j < 2 * kb + 2; ++j) r[j] = M::mma(M::low_columns(m.t, 16 * j, kb, lane), x, r[j]);
-        }
+        // (of a lower triangle transposed: of the first rows two columns of blocks, of the others all four)
+        typename M::In y;
+        piped<6, 1>([&](int u) __attribute__((always_inline)) { return M::low_columns(m.p, 16 * (u < 2 ? u : u - 2), u < 2 ? 0 : 1, lane); },
+                    [&](int u, const auto &a) __attribute__((always_inline)) {
+                        if (u == 0 || u == 2) y = M::exact(d[u], d[u + 1]);
+                        w[u < 2 ? u : u - 2] = M::mma(a, y, w[u < 2 ? u : u - 2]);
+                    });
+        piped<6, 1>([&](int u) __attribute__((always_inline)) { return M::low_columns(m.t, 16 * (u < 2 ? u : u - 2), u < 2 ? 0 : 1, lane); },
+                    [&](int u, const auto &a) __attribute__((always_inline)) {
+                        if (u == 0 || u == 2) x = M::split(w[u], w[u + 1]);
+                        r[u < 2 ? u : u - 2] = M::mma(a, x, r[u < 2 ? u : u - 2]);
+                    });
         if (!SPANS && in) {
             float *to = p.dr + ((head * p.chunks + ch) * p.DV + dv) * 64 + g4;
 #pragma unroll
@@ -906,15 +927,20 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
         if (!SPANS) store_rows(vrow, w, t0, g4, p.L, in);
 #pragma unroll
         for (int kb = 0; kb < KT; ++kb) S[kb] *= eA;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const typename M::Full x = M::split(d[2 * j], d[2 * j + 1]), y = M::split(r[2 * j], r[2 * j + 1]);
-#pragma unroll
-            for (int kb = 0; kb < KT; ++kb) {
-                S[kb] = M::mma(M::rows_in(m.q, 16 * kb, 32 * j, lane), x, S[kb]);
-                S[kb] = M::mma(M::rows_in(m.k, 16 * kb, 32 * j, lane), y, S[kb]);
-            }
-        }
+        typename M::Full z;
+        piped<2 * KT, 2>(
+            [&](int u) __attribute__((always_inline)) {
+                struct {
+                    typename M::In q, k;
+                } a;
+                a.q = M::rows_in(m.q, 16 * (u % KT), 32 * (u / KT), lane), a.k = M::rows_in(m.k, 16 * (u % KT), 32 * (u / KT), lane);
+                return a;
+            },
+            [&](int u, const auto &a) __attribute__((always_inline)) {
+                const int j = 2 * (u / KT);
+                if (u % KT == 0) x = M::split(d[j], d[j + 1]), z = M::split(r[j], r[j + 1]);
+                S[u % KT] = M::mma(a.k, z, M::mma(a.q, x, S[u % KT]));
+            });
     }
     const int c = lane0 & 15, g4 = 4 * (lane0 >> 4);
     if (SPANS) store_state(S, StateIn(walk.spans + unit * size + unit * (long long)p.DK * p.DK, p.DK, p.DV + p.DK), col.column, in, g4);
