@@ -374,6 +374,14 @@ template <typename T, int ROWS, int LANES> struct Tile {
     }
     template <typename E> __device__ __forceinline__ void put(E *to, int D, int t0, int n, int pitch) const      // (fp32 into shorts: three limbs, a plane each)
     {
+        if (t0 + 64 <= n && D == ROWS) {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const int i = threadIdx.x + u * LANES, r = i >> 3;
+                if (ROWS * 8 % LANES == 0 || r < ROWS) put_eight(to + r * kPitch + (i & 7) * 8, e[u], 8);
+            }
+            return;
+        }
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             const int i = threadIdx.x + u * LANES, r = i >> 3, t = t0 + (i & 7) * 8;
@@ -623,6 +631,9 @@ template <typename T, int KT, int NP> struct DeltaLds {
     Gates s;
 };
 constexpr int kWalkWaves = 4;           // of a workgroup; two of those fit a CU, one's products beside the other's way into LDS
+template <int N> struct Part {
+    static constexpr int value = N;
+};
 // A chunk's data on its way into LDS, and a wave's columns of v or dout, while the chunk before is worked at.
 template <typename T, int KT, int NP, bool KEYS_ONLY> struct Ahead {
     static constexpr int LANES = 64 * kWalkWaves, NG = sizeof(Gates) / 16;
@@ -631,14 +642,19 @@ template <typename T, int KT, int NP, bool KEYS_ONLY> struct Ahead {
     LowTiles<Mat<bf16_t>, WalkMat<T, KT>::limbs(NP), LANES> p;
     f32x4 s;
     Rows<T> rows;
-    __device__ __forceinline__ void load(const DeltaShape<T> &a, const T *krow, const T *qrow, const T *row, const DeltaPairs *r, int t0, int g4)
+    // In four parts, between products: sixty KB at once are more than a CU's address unit takes, and the wave would wait for it.
+    template <int PART> __device__ __forceinline__ void load(const DeltaShape<T> &a, const T *krow, const T *qrow, const T *row, const DeltaPairs *r, int t0, int g4)
     {
-        k.load(krow, a.DK, t0, a.pitch);
-        if constexpr (!KEYS_ONLY) q.load(qrow, a.DK, t0, a.pitch);
-        t.load(r->t);
-        if constexpr (!KEYS_ONLY) p.load(r->p);
-        s = reinterpret_cast<const f32x4 *>(&r->s)[threadIdx.x < NG ? threadIdx.x : 0];
-        rows.load(row, t0, g4, a.pitch);
+        if constexpr (PART == 0) k.load(krow, a.DK, t0, a.pitch);
+        if constexpr (PART == 1 && !KEYS_ONLY) q.load(qrow, a.DK, t0, a.pitch);
+        if constexpr (PART == 2) {
+            t.load(r->t);
+            s = reinterpret_cast<const f32x4 *>(&r->s)[threadIdx.x < NG ? threadIdx.x : 0];
+        }
+        if constexpr (PART == 3) {
+            if constexpr (!KEYS_ONLY) p.load(r->p);
+            rows.load(row, t0, g4, a.pitch);
+        }
     }
     __device__ __forceinline__ void put(DeltaLds<T, KT, NP> &m, const DeltaShape<T> &a, int t0, int n) const
     {
@@ -761,9 +777,14 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
     T *orow = p.o.row(b, own, p.L);
     const DeltaPairs *pairs = p.pairs + head * p.chunks;
     Ahead<T, KT, 2, SPANS> next;
-    if (from < last) next.load(p, krow, qrow, vrow, pairs + from, from * 64, 4 * (lane0 >> 4));
+    int ahead = from;                                   // (behind the last chunk that again: a load behind a question is waited for where its ways meet)
+    const auto load = [&](auto part) __attribute__((always_inline)) {
+        next.template load<decltype(part)::value>(p, krow, qrow, vrow, pairs + ahead, ahead * 64, 4 * (fresh(lane0) >> 4));
+    };
+    load(Part<0>{}), load(Part<1>{}), load(Part<2>{}), load(Part<3>{});
     for (int ch = from; ch < last; ++ch) {
         const int t0 = ch * kDeltaChunk;
+        ahead = min(ch + 1, last - 1);
         const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dv = col.at + c;
         __syncthreads();
         next.put(m, p, t0, n);
@@ -771,8 +792,10 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
         next.rows.get(val, t0, g4, n, p.pitch);
         if (!SPANS && p.states) store_state(S, StateIn(p.states + (head * p.chunks + ch) * size, p.DK, p.DV), dv, in, g4);
         __syncthreads();
-        if (ch + 1 < last) next.load(p, krow, qrow, vrow, pairs + ch + 1, t0 + 64, g4);
-        if (!col.active) continue;
+        if (!col.active) {
+            load(Part<0>{}), load(Part<1>{}), load(Part<2>{}), load(Part<3>{});
+            continue;
+        }
         f32x4 r[4] = {}, w[4] = {}, o[4] = {};
         typename M::Full x;
         piped<2 * KT, 2>(
@@ -789,7 +812,10 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
                 if (i == 0) x = M::split(S[kb], S[kb + 1]);
                 r[i] = M::mma(a.k, x, r[i]);
                 if constexpr (!SPANS) o[i] = M::template mma<2>(a.q, x, o[i]);
+                if (u == 1) load(Part<0>{});
+                if (u == KT) load(Part<1>{});
             });
+        load(Part<2>{});
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = 16 * i + g4;
@@ -802,6 +828,7 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
                     [&](int u, const auto &a) __attribute__((always_inline)) {
                         if (u % 4 == 0) x = M::split(r[u / 2], r[u / 2 + 1]);
                         w[u < 4 ? u : u - 2] = M::mma(a, x, w[u < 4 ? u : u - 2]);
+                        if (u == 2) load(Part<3>{});
                     });
         if (!SPANS) {
             piped<6, 1>([&](int u) __attribute__((always_inline)) { return M::template low_rows<2>(m.p, 16 * (u < 4 ? u : u - 2), u >> 2, lane); },
@@ -874,9 +901,14 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
         for (int t = max(last, from) * 64 + 4 * (lane0 >> 4), to = min(p.L, seg + 1 < walk.segs ? (from + walk.per) * 64 : p.L); t < to; t += 16)
             store4(vrow, f32x4{}, t, p.L);
     Ahead<T, KT, 3, false> next;
-    if (from < last) next.load(p, krow, qrow, drow, pairs + last - 1, (last - 1) * 64, 4 * (lane0 >> 4));
+    int ahead = max(last - 1, from);                    // (behind the last chunk that again)
+    const auto load = [&](auto part) __attribute__((always_inline)) {
+        next.template load<decltype(part)::value>(p, krow, qrow, drow, pairs + ahead, ahead * 64, 4 * (fresh(lane0) >> 4));
+    };
+    load(Part<0>{}), load(Part<1>{}), load(Part<2>{}), load(Part<3>{});
     for (int ch = last - 1; ch >= from; --ch) {
         const int t0 = ch * kDeltaChunk;
+        ahead = max(ch - 1, from);
         const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), dv = col.at + c;
         __syncthreads();
         next.put(m, p, t0, n);
@@ -887,15 +919,20 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
             for (int i = 0; i < 4; ++i) d[i] = f32x4{};
         if (!SPANS) store_state(S, StateIn(p.after + (head * p.chunks + ch) * size, p.DK, p.DV), dv, in, g4);
         __syncthreads();
-        if (ch > from) next.load(p, krow, qrow, drow, pairs + ch - 1, t0 - 64, g4);
-        if (!col.active) continue;
+        if (!col.active) {
+            load(Part<0>{}), load(Part<1>{}), load(Part<2>{}), load(Part<3>{});
+            continue;
+        }
         f32x4 w[4] = {}, r[4] = {};
         typename M::Full x;
         piped<2 * KT, 3>([&](int u) __attribute__((always_inline)) { return M::columns_in(m.k, 16 * (u & 3), 32 * (u >> 2), lane); },
                          [&](int u, const auto &a) __attribute__((always_inline)) {
                              if (u % 4 == 0) x = M::split(S[2 * (u >> 2)], S[2 * (u >> 2) + 1]);
                              w[u & 3] = M::mma(a, x, w[u & 3]);
+                             if (u == 1) load(Part<0>{});
+                             if (u == KT) load(Part<1>{});
                          });
+        load(Part<2>{});
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] *= four(m.s.eC, 16 * i + g4) * four(m.s.rk, 16 * i + g4);
         // (of a lower triangle transposed: of the first rows two columns of blocks, of the others all four)
@@ -904,6 +941,7 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
                     [&](int u, const auto &a) __attribute__((always_inline)) {
                         if (u == 0 || u == 2) y = M::exact(d[u], d[u + 1]);
                         w[u < 2 ? u : u - 2] = M::mma(a, y, w[u < 2 ? u : u - 2]);
+                        if (u == 2) load(Part<3>{});
                     });
         piped<6, 1>([&](int u) __attribute__((always_inline)) { return M::low_columns(m.t, 16 * (u < 2 ? u : u - 2), u < 2 ? 0 : 1, lane); },
                     [&](int u, const auto &a) __attribute__((always_inline)) {
