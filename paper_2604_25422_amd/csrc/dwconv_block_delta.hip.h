@@ -1095,8 +1095,8 @@ template <typename T, int KT> struct DeltaChunkLds {
             Elem dout[VB * kPitch], w[NP * VB * kPitch], dr[NP * VB * kPitch];
         };
         struct {
-            float pairs[kLow];
             Elem p[N2 * kLow];
+            float rows[10][16], columns[10][16];    // of the pairs' tiles: what P dP is over a row, and both pairs over a column
         };
     };
     ChunkGates s;
@@ -1105,9 +1105,6 @@ template <typename T, int KT> struct DeltaChunkLds {
         float part[3][G][64];
         f32x4 x[2][HALVES ? 4 : 0][64];     // of 16 columns, their tiles of beta (v - S~^T k), where there is room for them
     };
-    // Sums of a tile's rows and columns, in what the pairs leave of their place: blocks (0, 1) and (2, 3).
-    __device__ __forceinline__ float *rows(int tile) { return pairs + low_at(tile, 16); }
-    __device__ __forceinline__ float *columns(int tile) { return pairs + low_at(32 + tile, 48); }
 };
 
 // Backward, within a chunk, all chunks at once: from the states in front of it, the gradient of that behind it and dr
@@ -1191,6 +1188,7 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
     };
 #pragma unroll 1
     for (int v0 = 0;; v0 += VB) {
+        f32x4 a[SL][2], e[SL][2];
         {
             const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4), row = (16 * (wave & 1) + c) * kPitch + g4;
             f32x4 x[4] = {}, val[TI];
@@ -1201,6 +1199,14 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
                 for (int i = 0; i < TI; ++i) x[i] = M::mma(M::columns_in(m.k, first + 16 * i, 16 * kb, lane), s, x[i]);
                 step_done();
             }
+#pragma unroll
+            for (int s = 0; s < SL; ++s)                // (in the registers that were S's)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const int dk = 16 * (slice0 + s) + c;
+                    a[s][kb] = before.any_four(dk, v0 + 16 * kb + g4), e[s][kb] = after.any_four(dk, v0 + 16 * kb + g4);
+                }
+            step_done();
             vrow.get(val, t0 + first, g4, n, p.pitch);
             if (v0 + VB > p.DV) {
                 const bool out = v0 + 16 * (wave & 1) + c >= p.DV;
@@ -1241,14 +1247,6 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
         }
         {
             const int lane = fresh(lane0), g4 = 4 * (lane >> 4);
-            f32x4 a[SL][2], e[SL][2];
-#pragma unroll
-            for (int s = 0; s < SL; ++s)
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    const int dk = 16 * (slice0 + s) + (lane & 15);
-                    a[s][kb] = before.any_four(dk, v0 + 16 * kb + g4), e[s][kb] = after.any_four(dk, v0 + 16 * kb + g4);
-                }
             __syncthreads();
             if (v0 + VB > p.DV)
 #pragma unroll
@@ -1263,24 +1261,26 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
                 z[s] = M::split(a[s][0], a[s][1]);
                 step_done();
             }
+            piped<NI, 1>(
+                [&](int i) __attribute__((always_inline)) {
+                    struct {
+                        typename M::In d;
+                        Full r;
+                    } o;
+                    o.d = M::columns_in(m.dout, 16 * (tile0 + i), 0, lane), o.r = M::columns(m.dr, VP, 16 * (tile0 + i), 0, lane);
+                    return o;
+                },
+                [&](int i, const auto &o) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int ti = 16 * (tile0 + i);
-                const typename M::In d = M::columns_in(m.dout, ti, 0, lane);
-                const Full r = M::columns(m.dr, VP, ti, 0, lane);
-#pragma unroll
-                for (int s = 0; s < SL; ++s) x1[s][i] = M::mma(d, z[s], x1[s][i]), x2[s][i] = M::mma(r, z[s], x2[s][i]);
-                step_done();
-            }
+                    for (int s = 0; s < SL; ++s) x1[s][i] = M::mma(o.d, z[s], x1[s][i]), x2[s][i] = M::mma(o.r, z[s], x2[s][i]);
+                });
 #pragma unroll
             for (int s = 0; s < SL; ++s) z[s] = M::split(e[s][0], e[s][1]);
+            piped<NI, 1>([&](int i) __attribute__((always_inline)) { return M::columns(m.w, VP, 16 * (tile0 + i), 0, lane); },
+                         [&](int i, const Full &w) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const Full w = M::columns(m.w, VP, 16 * (tile0 + i), 0, lane);
-#pragma unroll
-                for (int s = 0; s < SL; ++s) x3[s][i] = M::mma(w, z[s], x3[s][i]);
-                step_done();
-            }
+                             for (int s = 0; s < SL; ++s) x3[s][i] = M::mma(w, z[s], x3[s][i]);
+                         });
         }
         if (v0 + VB >= p.DV) break;
         take_pairs();
@@ -1370,105 +1370,123 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
             return sum + __shfl_xor(sum, 32, 64);
         };
         const float xs = across(x), ys = across(y);
-        if (lane < 16) m.da[task][c] = xs, m.rows(task)[c] = ys;
-        if (c == 0) *reinterpret_cast<f32x4 *>(m.columns(task) + g4) = below;
+        if (lane < 16) m.da[task][c] = xs, m.rows[task][c] = ys;
+        // for dg: columns of this tile in front of t, of its rows from t on
+        const float one = both[0], two = one + both[1], three = two + both[2];
+        float whole = three + both[3], up = __shfl_up(whole, 16, 64);
+        whole += g4 >= 4 ? up : 0.0f;
+        up = __shfl_up(whole, 32, 64);
+        whole += g4 >= 8 ? up : 0.0f;
+        up = __shfl_up(whole, 16, 64);
+        const float front = g4 >= 4 ? up : 0.0f;
+        f32x4 z = f32x4{0.0f, one, two, three} + front;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) z[v] = ti > tj || c >= g4 + v ? z[v] : 0.0f;
+        z = sum16(z);
+        if (c == 0) *reinterpret_cast<f32x4 *>(m.columns[task] + g4) = below, *reinterpret_cast<f32x4 *>(m.dg[task] + g4) = z;
         M::template put<2>(m.p, kLow, low_at(i, j), dP * e * p.scale);
         M::template put<2>(m.t, kLow, low_at(i, j), dA * e * m.s.beta[i]);
-        *reinterpret_cast<f32x4 *>(m.pairs + low_at(i, j)) = both;
     }
     __syncthreads();
-    // Sums over the channels of q dq and k dk, whose pairs' part is that of P dP and of A dA; dbeta; what rows take and what columns leave.
-    if (wave == 0) {
+    // Sums over the channels of q dq and k dk, whose pairs' part is that of P dP and of A dA, and dbeta; dg from what rows take, what columns leave and the pairs
+    // between.
+    if (wave < 2) {
         const int t = fresh(lane0), tt = t >> 4, c = t & 15;
-        float qs = 0.0f, ys = 0.0f, bs = 0.0f, xs = 0.0f, ps = 0.0f, cs = 0.0f;
+        float qs = 0.0f, ys = 0.0f, bs = 0.0f;
 #pragma unroll
         for (int u = 0; u < G; ++u) qs += m.part[0][u][t], ys += m.part[1][u][t], bs += m.part[2][u][t];
+        const float beta = m.s.beta[t];
+        if (wave == 0) {
+            float xs = 0.0f, ps = 0.0f, cs = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int left = tt * (tt + 1) / 2 + min(j, tt), down = max(j, tt) * (max(j, tt) + 1) / 2 + tt;
-            const float u = m.da[left][c], v = m.rows(left)[c], w = m.columns(down)[c];
-            xs += j <= tt ? u : 0.0f, ps += j <= tt ? v : 0.0f, cs += j >= tt ? w : 0.0f;
+            for (int j = 0; j < 4; ++j) {
+                const int left = tt * (tt + 1) / 2 + min(j, tt), down = max(j, tt) * (max(j, tt) + 1) / 2 + tt;
+                const float u = m.da[left][c], v = m.rows[left][c], w = m.columns[down][c];
+                xs += j <= tt ? u : 0.0f, ps += j <= tt ? v : 0.0f, cs += j >= tt ? w : 0.0f;
+            }
+            const float sum = bs + (m.db[0][t] + m.db[1][t]) + xs;
+            m.db[0][t] = qs + ps, m.db[1][t] = fmaf(beta, bs + xs, ys) + cs;
+            if (t0 + t < p.L) p.dbeta[(long long)head * p.L + t0 + t] = t0 + t < n ? sum : 0.0f;
+        } else {
+            // a row's pairs in tiles left of its own: its own tile's rows from t on, and tiles further down whole
+            float left[3], below = 0.0f, all = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 3; ++j) {
+                const int at = tt * (tt + 1) / 2 + min(j, tt);
+                const float u = fmaf(beta, m.da[at][c], m.rows[at][c]);
+                left[j] = j < tt ? u : 0.0f;
+            }
+            float rows = left[0] + left[1] + left[2];
+#pragma unroll
+            for (int s = 1; s < 16; s *= 2) {
+                const float o = __shfl_down(rows, s, 64);
+                rows += c + s < 16 ? o : 0.0f;
+            }
+            const float first = group_sum(left[0], 4), second = group_sum(left[1], 4);
+            const float s20 = __shfl(first, 32, 64), s30 = __shfl(first, 48, 64), s31 = __shfl(second, 48, 64);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float w = m.dg[max(j, tt) * (max(j, tt) + 1) / 2 + tt][c];
+                below += j >= tt ? w : 0.0f;
+            }
+            below += rows + (tt == 1 ? s20 + s30 : tt == 2 ? s30 + s31 : 0.0f);
+#pragma unroll
+            for (int u = 0; u < G; ++u) all += m.whole[u];
+            float x = fmaf(beta, bs, qs), y = ys;
+            // (the derivative of a decay that is 0 in 32 bits is that)
+            const double G0 = m.s.G[t], G1 = __shfl_up(G0, 1, 64);
+            const bool dead = G0 - (t ? G1 : 0.0) < -104.0 * 1.4426950408889634;
+#pragma unroll
+            for (int s = 1; s < 64; s *= 2) {
+                const float up = __shfl_down(x, s, 64), down = __shfl_up(y, s, 64);
+                if (t + s < 64) x += up;
+                if (t >= s) y += down;
+            }
+            const float before = __shfl_up(y, 1, 64);
+            const float sum = (m.s.eG[63] * all + x) + ((t > 0 ? before : 0.0f) + below);
+            if (t0 + t < p.L) p.dg[(long long)head * p.L + t0 + t] = t0 + t < n && !dead ? sum : 0.0f;
         }
-        const float beta = m.s.beta[t], sum = bs + (m.db[0][t] + m.db[1][t]) + xs;
-        m.part[0][0][t] = qs + ps, m.part[0][1][t] = fmaf(beta, bs + xs, ys) + cs;
-        m.part[1][0][t] = fmaf(beta, bs, qs), m.part[1][1][t] = ys;
-        if (t0 + t < p.L) p.dbeta[(long long)head * p.L + t0 + t] = t0 + t < n ? sum : 0.0f;
     }
-    // pairs of a row from t on and a column before t: products with ones above the diagonal, then the rows from t on, a tile a wave
-    for (int task = W - 1 - wave; task < 10; task += W) {
-        const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
-        int ti, tt;
-        low_tile(task, ti, tt);
-        f32x4 x = {};
-        for (int j = 0; j <= tt; ++j) {
-            f32x4 ones;
-#pragma unroll
-            for (int v = 0; v < 4; ++v) ones[v] = 16 * j + g4 + v < 16 * tt + c ? 1.0f : 0.0f;
-            x = mma16(rows_of(m.pairs + low_at(16 * ti, 16 * j), 0, 0, lane, low_pitch(16 * ti)), ones, x);
-        }
-        float sum = 0.0f;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) sum += 16 * ti + g4 + v >= 16 * tt + c ? x[v] : 0.0f;
-        sum += __shfl_xor(sum, 16, 64);
-        sum += __shfl_xor(sum, 32, 64);
-        if (lane < 16) m.dg[task][c] = sum;
-    }
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    // what pairs add: of the first 32 columns all rows' tiles, of the others the lower ones, and the other way for columns' tiles, 32 rows each
+    {
         const int lane = fresh(lane0);
         Full kz[SL], qz[SL];
+        piped<4 * NI, 1>(
+            [&](int u) __attribute__((always_inline)) {
+                const int kb = u / (2 * NI), i = tile0 + u / 2 % NI;
+                struct {
+                    Full x, y;
+                } o;
+                if (u & 1) o.x = M::template low_columns<2>(m.p, 16 * min(i, 2 * kb + 1), kb, lane), o.y = M::template low_columns<2>(m.t, 16 * min(i, 2 * kb + 1), kb, lane);
+                else o.x = M::template low_rows<2>(m.p, 16 * max(i, 2 * kb), kb, lane), o.y = M::template low_rows<2>(m.t, 16 * max(i, 2 * kb), kb, lane);
+                return o;
+            },
+            [&](int u, const auto &o) __attribute__((always_inline)) {
+                const int kb = u / (2 * NI), ii = u / 2 % NI, i = tile0 + ii;
+                if (u % (2 * NI) == 0)
 #pragma unroll
-        for (int s = 0; s < SL; ++s) {
-            kz[s] = M::template split<2>(kh(s, 2 * kb, lane), kh(s, 2 * kb + 1, lane));
-            qz[s] = M::template split<2>(qh[s][2 * kb], qh[s][2 * kb + 1]);
-        }
+                    for (int s = 0; s < SL; ++s) {
+                        kz[s] = M::template split<2>(kh(s, 2 * kb, lane), kh(s, 2 * kb + 1, lane));
+                        qz[s] = M::template split<2>(qh[s][2 * kb], qh[s][2 * kb + 1]);
+                    }
+                if (u & 1) {
+                    if (i < 2 * kb + 2)
 #pragma unroll
-        for (int ii = 0; ii < NI; ++ii) {
-            const int i = tile0 + ii;
-            if (2 * kb <= i) {
-                const Full x = M::template low_rows<2>(m.p, 16 * i, kb, lane), y = M::template low_rows<2>(m.t, 16 * i, kb, lane);
+                        for (int s = 0; s < SL; ++s) x2[s][ii] = M::template mma<2>(o.y, kz[s], M::template mma<2>(o.x, qz[s], x2[s][ii]));
+                } else if (2 * kb <= i) {
 #pragma unroll
-                for (int s = 0; s < SL; ++s) x1[s][ii] = M::template mma<2>(x, kz[s], x1[s][ii]), x2[s][ii] = M::template mma<2>(y, kz[s], x2[s][ii]);
-            }
-            if (i < 2 * kb + 2) {
-                const Full x = M::template low_columns<2>(m.p, 16 * i, kb, lane), y = M::template low_columns<2>(m.t, 16 * i, kb, lane);
-#pragma unroll
-                for (int s = 0; s < SL; ++s) x2[s][ii] = M::template mma<2>(y, kz[s], M::template mma<2>(x, qz[s], x2[s][ii]));
-            }
-            step_done();
-        }
+                    for (int s = 0; s < SL; ++s) x1[s][ii] = M::template mma<2>(o.x, kz[s], x1[s][ii]), x2[s][ii] = M::template mma<2>(o.y, kz[s], x2[s][ii]);
+                }
+            });
     }
     __syncthreads();
-    if (wave == W - 1) {
-        const int t = fresh(lane0), tt = t >> 4;
-        float x = m.part[1][0][t], y = m.part[1][1][t], below = 0.0f, all = 0.0f;
-#pragma unroll
-        for (int u = 0; u < G; ++u) all += m.whole[u];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float w = m.dg[max(j, tt) * (max(j, tt) + 1) / 2 + tt][t & 15];
-            below += j >= tt ? w : 0.0f;
-        }
-        // (the derivative of a decay that is 0 in 32 bits is that)
-        const double G0 = m.s.G[t], G1 = __shfl_up(G0, 1, 64);
-        const bool dead = G0 - (t ? G1 : 0.0) < -104.0 * 1.4426950408889634;
-#pragma unroll
-        for (int s = 1; s < 64; s *= 2) {
-            const float up = __shfl_down(x, s, 64), down = __shfl_up(y, s, 64);
-            if (t + s < 64) x += up;
-            if (t >= s) y += down;
-        }
-        const float left = __shfl_up(y, 1, 64);
-        const float sum = (m.s.eG[63] * all + x) + ((t > 0 ? left : 0.0f) + below);
-        if (t0 + t < p.L) p.dg[(long long)head * p.L + t0 + t] = t0 + t < n && !dead ? sum : 0.0f;
-    }
     // through x / |x|: what lies along x does not change it
     const bool along = !SHARED && p.eps > 0.0f;
     const int lane = fresh(lane0), c = lane & 15, g4 = 4 * (lane >> 4);
 #pragma unroll
     for (int ii = 0; ii < NI; ++ii) {
         const int t = 16 * (tile0 + ii) + g4;
-        const f32x4 a = four(m.part[0][0], t), e = four(m.part[0][1], t);
+        const f32x4 a = four(m.db[0], t), e = four(m.db[1], t);
 #pragma unroll
         for (int s = 0; s < SL; ++s) {
             const int dk = 16 * (slice0 + s) + c;
