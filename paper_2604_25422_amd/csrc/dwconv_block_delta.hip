@@ -172,12 +172,13 @@ template <typename T, int KT> int launch_pairs(const DeltaShape<T> &p, hipStream
 }
 
 // Segments that a head's chunks are cut into.  A walk's steps are a chain: few heads leave most of the chip idle, and what a segment does to any state
-// it starts with (DV + DK columns instead of DV) can be formed for all segments at once, the states between them in a chain of its own, which takes a
-// third of a step each, and then all segments at once again.  In steps of a walk that has a CU to itself (two workgroups share one at 1.4 times that;
-// in fp32 with more than 32 channels of a key LDS has room for one), forward the pass that forms spans writes no output and takes 0.6.
-// us whole / cut (segments): bf16, DK = DV = 128, 256 chunks, 2 heads forward 1578 / 147 (64), backward 1594 / 212; 32 heads 1811 / 762 (8), 2673 / 1790; 64
-// heads 1965 / 1457 (4), 3685 / 3522; 128 heads, 64 chunks 567 / 784, 1380 / 1765; 2 heads, 8 chunks 63 / 50 (4), 99 / 89.  fp32, 64 heads, 64 chunks 884 /
-// 953 (2), 1647 / 1920.  DK = DV = 64, 64 chunks, 128 heads, bf16 351 / 319 (4), 766 / 805; fp32 563 / 596 (2), 1186 / 1367; 64 heads 479 / 314 (4), 815 / 704.
+// it starts with (DV + DK columns instead of DV) can be formed for all segments at once, the states between them in chains of their own, and then all
+// segments at once again.  In steps of a walk that has a CU to itself (two workgroups share one at 1.9 times that; in fp32 with more than 32 channels of a key
+// LDS has room for one): forward the pass that forms spans writes no output and takes 0.6, a step of the chains 0.7 of 128 channels of a key and less of fewer.
+// us whole / cut (segments): bf16, DK = DV = 128, 256 chunks, 2 heads forward 1052 / 136 (64), backward 1259 / 202; 8 heads 1083 / 229 (16), 1436 / 497; 32 heads
+// 1173 / 690 (4), 2164 / 1717; 64 heads 1282 / 1336 (4), 3173 / 3506; 128 heads, 64 chunks 403 / 670 (2), 1293 / 1694; 2 heads, 8 chunks 44 / 40 (4), 82 / 78.
+// DK = DV = 64, 64 chunks, bf16, 32 heads 229 / 94 (8), 347 / 217; 128 heads 296 / 308 (2), 741 / 790; fp32, 64 heads 379 / 267 (4), 692 / 629; 128 heads 449 / 502 (2),
+// 1039 / 1202.
 struct WalkPlan {
     int segs, per, join;
 };
@@ -204,14 +205,15 @@ WalkPlan plan_walk(int B, int H, int DK, int DV, int L, int dtype, bool backward
     const bool alone = dtype == DWCONV_F32 && DK > 32;
     const double heads = (double)B * H, values = (double)ceil_div(DV, 16 * kWalkWaves),
                  all = (double)ceil_div(ceil_div(DV, 16) + ceil_div(DK, 16), kWalkWaves);
-    const auto step = [&](double groups) { return groups <= 256 ? 1.0 : alone ? groups / 256 : groups <= 512 ? 1.4 : 1.4 * groups / 512; };
+    const auto step = [&](double groups) { return groups <= 256 ? 1.0 : alone ? groups / 256 : groups <= 512 ? 1.9 : 1.9 * groups / 512; };
+    const double link = (DK > 64 ? 0.7 : DK > 32 ? 0.5 : 0.25) * (dtype == DWCONV_F32 ? 0.65 : 1.0);       // (a step of the chains)
     double best = chunks * step(heads * values);
     WalkPlan w{1, chunks, 1};
     for (int segs = 2; segs <= 128 && segs <= chunks / 2; segs *= 2) {
         const int per = (int)ceil_div(chunks, segs);
         const int real = (int)ceil_div(chunks, per);
         const ChainPlan chain = plan_chain(heads, real, DK, DV);
-        const double cost = per * ((backward ? 1.0 : 0.6) * step(heads * segs * all) + step(heads * segs * values)) + 0.35 * chain.steps + 1.0;
+        const double cost = per * ((backward ? 1.0 : 0.6) * step(heads * segs * all) + step(heads * segs * values)) + link * chain.steps + 1.0;
         if (cost < best) best = cost, w = WalkPlan{real, per, chain.join};
     }
     return w;

@@ -374,7 +374,7 @@ template <typename T, int ROWS, int LANES> struct Tile {
     }
     template <typename E> __device__ __forceinline__ void put(E *to, int D, int t0, int n, int pitch) const      // (fp32 into shorts: three limbs, a plane each)
     {
-        if (t0 + 64 <= n && D == ROWS) {
+        if (t0 + 64 <= n && D >= ROWS) {
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 const int i = threadIdx.x + u * LANES, r = i >> 3;
