@@ -748,8 +748,8 @@ template <int KT> __device__ __forceinline__ void unit_state(f32x4 (&S)[KT], int
 
 // Forward.  A workgroup has 64 columns of a head's state, a wave 16 of them in registers; it walks the chunks of its segment.  Between chunks nothing leaves the
 // registers: a state's tile, k^T S, w and what is added to S are each the next product's operand as they stand.  With heads for all CUs memory is the
-// bound, half of it the states that are kept (768 heads of 128 x 128, 16 chunks, bf16: 1.95 GB in 481 us, 4.1 TB/s); else a chunk's chain of three products,
-// 7.4 us of 128 x 128 channels in bf16 where a workgroup has its CU to itself, 10.3 where two share it (products and vector instructions of either are 2.7).
+// bound, half of it the states that are kept (768 heads of 128 x 128, 16 chunks, bf16: 1.99 GB in 435 us, 4.6 TB/s); else a chunk's chain of three products,
+// 4.1 us of 128 x 128 channels in bf16 where a workgroup has its CU to itself (products and vector instructions are 2.7), nearly twice that where two share it.
 template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_fwd_walk(const DeltaFwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT, 2> &m, int unit, int group)
 {
     typedef WalkMat<T, KT> M;
@@ -870,7 +870,7 @@ template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWal
 
 // Backward, from chunk to chunk: with dS the gradient of the state behind a chunk,
 //     dw = P^T do + exp(G_63 - G) k dS,   (I + A)^T dr = dw,   dS <- exp(G_63) dS + sum_i exp(G_i) q_i do_i^T - beta_i exp(G_i) k_i dr_i^T.
-// 768 heads as above: 2.36 GB in 538 us, 4.4 TB/s.  Leaves dS behind every chunk, dr (whole, what needs it next does not form it again) and dv = beta dr.
+// 768 heads as above: 2.42 GB in 528 us, 4.6 TB/s.  Leaves dS behind every chunk, dr (whole, what needs it next does not form it again) and dv = beta dr.
 template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_bwd_walk(const DeltaBwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT, 3> &m, int unit, int group)
 {
     typedef WalkMat<T, KT> M;
@@ -1115,9 +1115,10 @@ template <typename T, int KT> struct DeltaChunkLds {
 // x_i what row i took of S and y_j what is left of column j in S'.  (As a difference of whole sums, which is shorter, it would be
 // the rounding of those where a decay is strong.)  A workgroup has a chunk of a head, 32 columns of its states at a time.  First a wave has 16 columns
 // of w, two of k^T S's tiles (the other two are another wave's; without room for those all four) and two of T times that; then SL slices of 16
-// channels of the key and NI tiles of 16 positions.  12288 chunks of 128 x 128 channels in bf16 1.29 ms: vector instructions, the limbs above all, and products
-// take a SIMD's cycles in turn (48 and 30 %; 3.75 GB, 2.9 TB/s); with 64 columns at a time, dr formed here and so one workgroup of eight waves to a CU
-// it were 1.6.  8192 chunks of 64 x 64 in fp32 635 us, 47 % of it products.  SHARED: dq and dk of q and k of unit length go to part_q and part_k, which delta_share_kernel adds up.
+// channels of the key and NI tiles of 16 positions.  12288 chunks of 128 x 128 channels in bf16 1.18 ms: vector instructions, the limbs above all, and products
+// take a SIMD's cycles in turn (50 and 29 %; 3.68 GB, 3.1 TB/s); with 64 columns at a time, dr formed here and so one workgroup of eight waves to a CU
+// it were 1.79.  8192 chunks of 64 x 64 in fp32 541 us, 49 % of it products.  SHARED: dq and dk of q and k of unit length go to part_q and part_k, which
+// delta_share_kernel adds up.
 template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta_bwd_chunk(const DeltaBwd<T> &p, DeltaChunkLds<T, KT> &m, int unit)
 {
     typedef Mat<T> M;
