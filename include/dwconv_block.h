@@ -142,9 +142,9 @@ DWCONV_API int dwconv_conv_ring(dwconv_seq x, void *ring, const int *lengths, co
  * states [B, H, dwconv_delta_states(L), DK, DV] fp32 or NULL: S in front of every 64th position that is inside its sequence, which
  * dwconv_delta_bwd takes.
  * workspace: dwconv_delta_workspace_bytes(...) bytes, 16-byte aligned.
- * DK at most 128, DV at most 65536, H at most 2^20.  g may be minus infinity (nothing in front of t is remembered).  Sums and states in fp32: below
- * 2^127 (|x|^2 + eps too) they are what they should be; what is beyond that or not finite may reach every position of its chunk of 64 and everything
- * behind it, of its own head and of those that share its keys.
+ * DK at most 128, DV at most 65536, H at most 2^20.  g may be minus infinity (nothing in front of t is remembered).  Sums and states are fp32: below
+ * 2^127 (|x|^2 + eps too) they are what they should be, to 2^-126 where they are small; what is beyond that or not finite may reach every position of
+ * its chunk of 64 and everything behind it, of its own head and of those that share its keys.
  */
 DWCONV_API int dwconv_delta_fwd(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwconv_seq g, dwconv_seq beta, const float *s0, const int *lengths,
                                 dwconv_seq_out o, float *s_last, float *states, void *workspace, size_t workspace_bytes, int B, int H, int Hk,

@@ -12,7 +12,8 @@
 //
 // Products: bf16 calls on the bf16 matrix instruction, 16 times as fast as the fp32 one: what is stored as bf16 goes in as it is, and what is fp32 (the
 // state, w, T, P) as the exact sum of three bf16 limbs, so that sums and states are those of fp32 products to 2^-24; the products that only reach an
-// output rounded to bf16 leave out the third limb (2^-16 of them, 2^-8 of the rounding).  fp32 calls on the fp32 instruction, but for their walks.
+// output rounded to bf16 leave out the third limb (2^-16 of them, 2^-8 of the rounding).  fp32 calls on the fp32 instruction, but for their walks.  (The limbs of
+// values below 2^-109 are not all normal numbers: of those 2^-126 may be lost.)
 #pragma once
 #include "dwconv_block_common.hip.h"
 
@@ -264,8 +265,8 @@ template <> struct Mat<bf16_t> {
 
 // What a walk multiplies with.  Its chain is the call's time where heads are few, so fp32 calls go by limbs too, keys, queries and dout as three of them:
 // six products of 16 cycles for eight of 32 on the fp32 instruction, to the same 2^-24.  In LDS a key is then half as large again, and from 33 channels on one
-// workgroup is what a CU has room for.  us of a forward pass by limbs / by the fp32 instruction: 128 heads of 64 x 64 over 4096 positions 564 / 588, 32 heads of
-// 128 x 128 over 4096 461 / 590, 64 heads of 32 x 32 over 4096 144 / 165, 8 heads over 1024 32 / 36.
+// workgroup is what a CU has room for.  us of a forward pass by limbs / by the fp32 instruction (operands then not yet read ahead): 128 heads of 64 x 64 over
+// 4096 positions 564 / 588, 32 heads of 128 x 128 over 4096 461 / 590, 64 heads of 32 x 32 over 4096 144 / 165, 8 heads over 1024 32 / 36.
 template <typename T, int KT> struct WalkMat : Mat<T> {
     static constexpr int in_planes = 1, resident = 2;            // (workgroups that a CU has room for)
     static constexpr int limbs(int n) { return n; }

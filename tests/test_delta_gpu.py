@@ -69,6 +69,19 @@ def test_widths(DK, DV, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,H,Hk,DK,DV,L", [(1, 1, 1, 3, 65536, 70), (1, 1500, 500, 2, 3, 9), (2, 40, 40, 128, 2, 5)])
+def test_widest(B, H, Hk, DK, DV, L, dtype):
+    check_rule(*inputs(B, H, Hk, DK, DV, L, dtype, seed=DV), key_heads=Hk)
+
+
+@pytest.mark.parametrize("size", [2.0 ** -90, 2.0 ** 100])
+def test_sizes(size):
+    """Values and states far from 1, fp32: every limb of theirs is still a normal number."""
+    q, k, v, g, beta, s0, do, ds = inputs(2, 2, 1, 40, 24, 150, F32, seed=31)
+    check_rule(q, k, v * size, g, beta, s0 * size, do, ds, key_heads=1)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("B,H,Hk,DK,DV", [(1, 4, 1, 32, 20), (2, 6, 3, 64, 48), (3, 8, 2, 128, 64), (1, 12, 12, 16, 16), (5, 1, 1, 40, 128), (2, 3, 1, 100, 70)])
 def test_shared_keys(B, H, Hk, DK, DV, dtype):
     check_rule(*inputs(B, H, Hk, DK, DV, 150, dtype, seed=H + DK), key_heads=Hk)
