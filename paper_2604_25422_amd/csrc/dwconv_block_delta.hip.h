@@ -575,21 +575,26 @@ template <typename T, int KT, int W> __device__ __forceinline__ void delta_pairs
         m.s.rq[tid] = p.scale * m.s.iq[tid];
     }
     __syncthreads();
-    for (int task = wave; task < 20; task += W) {
+    for (int task = wave; task < 10; task += W) {
         int ti, tj;
-        low_tile(task >> 1, ti, tj);
-        const bool is_p = task & 1;
+        low_tile(task, ti, tj);
         const int i = 16 * ti + c, j = 16 * tj + g4;        // (transposed: lane (c, g) has columns 16 tj + 4 g + v of row 16 ti + c)
-        f32x4 d = {};
+        f32x4 kk = {}, qk = {}, e;
 #pragma unroll
-        for (int kb = 0; kb < KT; kb += 2)
-            d = M::mma(M::columns_in(m.k, 16 * tj, 16 * kb, lane), M::columns_in(is_p ? m.q : m.k, 16 * ti, 16 * kb, lane), d);
-        f32x4 e;
+        for (int kb = 0; kb < KT; kb += 2) {
+            const typename M::In a = M::columns_in(m.k, 16 * tj, 16 * kb, lane);
+            kk = M::mma(a, M::columns_in(m.k, 16 * ti, 16 * kb, lane), kk);
+            qk = M::mma(a, M::columns_in(m.q, 16 * ti, 16 * kb, lane), qk);
+        }
 #pragma unroll
-        for (int v = 0; v < 4; ++v) e[v] = j + v < i || (is_p && j + v == i) ? exp2_of(m.s.G[i] - m.s.G[j + v]) : 0.0f;
-        d = d * e * four(m.s.rk, j) * (is_p ? m.s.rq[i] : m.s.rk[i]);
-        if (is_p || p.keep) *reinterpret_cast<f32x4 *>((is_p ? to.p : to.kk)[task >> 1] + 16 * c + g4) = d;
-        if (!is_p) *reinterpret_cast<f32x4 *>(m.a + low_at(i, j)) = d * m.s.beta[i];
+        for (int v = 0; v < 4; ++v) e[v] = j + v <= i ? exp2_of(m.s.G[i] - m.s.G[j + v]) : 0.0f;
+        e *= four(m.s.rk, j);
+        *reinterpret_cast<f32x4 *>(to.p[task] + 16 * c + g4) = qk * e * m.s.rq[i];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) kk[v] = j + v < i ? kk[v] : 0.0f;
+        kk *= e * m.s.rk[i];
+        if (p.keep) *reinterpret_cast<f32x4 *>(to.kk[task] + 16 * c + g4) = kk;
+        *reinterpret_cast<f32x4 *>(m.a + low_at(i, j)) = kk * m.s.beta[i];
     }
     __syncthreads();
     invert(m.a, m.t);
