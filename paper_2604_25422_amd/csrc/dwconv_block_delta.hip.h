@@ -520,7 +520,7 @@ __device__ __forceinline__ void invert(const float *A, float *T)
 }
 
 // A record of every chunk with a position inside: by a workgroup of W waves.  Bound by memory where there are many, 32 KB of keys and queries in and 23 to 33 KB out
-// (12288 chunks of 128 channels in bf16 190 us, 3.9 TB/s), by a chunk's own chain (norms, pairs, the substitution) where there are few: 128 chunks 9.7 us.
+// (12288 chunks of 128 channels in bf16 173 us, 4.3 TB/s), by a chunk's own chain (norms, pairs, the substitution) where there are few: 128 chunks 9.4 us.
 template <typename T, int KT, int W> __device__ __forceinline__ void delta_pairs(const DeltaShape<T> &p, PairsLds<T, KT, W> &m, int unit)
 {
     typedef Mat<T> M;
@@ -1121,7 +1121,7 @@ template <typename T, int KT> struct DeltaChunkLds {
 // x_i what row i took of S and y_j what is left of column j in S'.  (As a difference of whole sums, which is shorter, it would be
 // the rounding of those where a decay is strong.)  A workgroup has a chunk of a head, 32 columns of its states at a time.  First a wave has 16 columns
 // of w, two of k^T S's tiles (the other two are another wave's; without room for those all four) and two of T times that; then SL slices of 16
-// channels of the key and NI tiles of 16 positions.  12288 chunks of 128 x 128 channels in bf16 1.18 ms: vector instructions, the limbs above all, and products
+// channels of the key and NI tiles of 16 positions.  12288 chunks of 128 x 128 channels in bf16 1.17 ms: vector instructions, the limbs above all, and products
 // take a SIMD's cycles in turn (50 and 29 %; 3.68 GB, 3.1 TB/s); with 64 columns at a time, dr formed here and so one workgroup of eight waves to a CU
 // it were 1.79.  8192 chunks of 64 x 64 in fp32 541 us, 49 % of it products.  SHARED: dq and dk of q and k of unit length go to part_q and part_k, which
 // delta_share_kernel adds up.
