@@ -1,7 +1,7 @@
 """A small language model whose blocks remember in matrices: the gated delta rule behind a short convolution, dropout in training; trained for some
 steps, then served token by token.
 
-    python examples/delta_block.py [--steps 200]
+    python examples/delta_block.py [--steps 400]
 
 A block is  n -> projection -> (q, k, v, z) and the gates;  (q, k, v) -> causal depthwise convolution -> gated delta rule, two heads of values to a head
 of keys -> dropout -> norm, gate, residual and the next block's norm.  The projections, the embedding and the loss are torch's; everything else is a call of
@@ -130,7 +130,7 @@ class Model:
         return n[..., 0] @ self.head.t()
 
 
-def train(model, steps, vocabulary, B, L, lr=0.5, momentum=0.9, max_norm=1.0):
+def train(model, steps, vocabulary, B, L, lr=0.2, momentum=0.9, max_norm=1.0):
     params = model.parameters()
     velocity = [torch.zeros_like(p) for p in params]
     losses = []
@@ -167,7 +167,7 @@ def serve(model, vocabulary, B, L, more):
     return off, float(whole.abs().max())
 
 
-def main(steps=200, vocabulary=32, heads=4, key_heads=2, D=16, K=4, blocks=2, B=32, L=96, report=print):
+def main(steps=400, vocabulary=32, heads=4, key_heads=2, D=16, K=4, blocks=2, B=32, L=96, report=print):
     model = Model(vocabulary, heads, key_heads, D, K, blocks, seed=0)
     losses = train(model, steps, vocabulary, B, L)
     off, size = serve(model, vocabulary, B, L, more=24)
@@ -178,5 +178,5 @@ def main(steps=200, vocabulary=32, heads=4, key_heads=2, D=16, K=4, blocks=2, B=
 
 if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
-    ap.add_argument("--steps", type=int, default=200)
+    ap.add_argument("--steps", type=int, default=400)
     main(ap.parse_args().steps)
