@@ -250,7 +250,7 @@ int span_columns(int DK, int DV) { return 16 * (int)(ceil_div(DV, 16) + ceil_div
 template <typename T, int KT> int launch_fwd(const DeltaFwd<T> &p, const DeltaWalk &w, hipStream_t st)
 {
     static std::atomic<unsigned long long> done[2];
-    constexpr size_t lds = sizeof(DeltaLds<T, KT, 2>);
+    constexpr size_t lds = sizeof(DeltaLds<T, KT>);
     static_assert(lds <= 160 * 1024, "LDS of a CU");
     int rc = launch_pairs<T, KT>(p, st);
     if (rc == DWCONV_OK && w.segs > 1) {
@@ -268,7 +268,7 @@ template <typename T> int launch_fwd(const DeltaFwd<T> &p, const DeltaWalk &w, h
 template <typename T, int KT> int launch_bwd(const DeltaBwd<T> &p, const DeltaWalk &w, hipStream_t st)
 {
     static std::atomic<unsigned long long> done[4];
-    constexpr size_t lds = sizeof(DeltaLds<T, KT, 3>), chunk = sizeof(DeltaChunkLds<T, KT>);
+    constexpr size_t lds = sizeof(DeltaLds<T, KT>), chunk = sizeof(DeltaChunkLds<T, KT>);
     static_assert(lds <= 160 * 1024 && chunk <= 80 * 1024, "LDS of a CU");
     int rc = launch_pairs<T, KT>(p, st);
     if (rc == DWCONV_OK && w.segs > 1) {

@@ -11,8 +11,7 @@
 // the walk from chunk to chunk is then three products deep.
 //
 // Products: bf16 calls on the bf16 matrix instruction, 16 times as fast as the fp32 one: what is stored as bf16 goes in as it is, and what is fp32 (the
-// state, w, T, P) as the exact sum of three bf16 limbs, so that sums and states are those of fp32 products to 2^-24; the products that only reach an
-// output rounded to bf16 leave out the third limb (2^-16 of them, 2^-8 of the rounding).  fp32 calls on the fp32 instruction, but for their walks.  (The limbs of
+// state, w, T, P) as the exact sum of three bf16 limbs, so that sums and states are those of fp32 products to 2^-24.  fp32 calls on the fp32 instruction, but for their walks.  (The limbs of
 // values below 2^-109 are not all normal numbers: of those 2^-126 may be lost.)
 #pragma once
 #include "dwconv_block_common.hip.h"
@@ -269,13 +268,11 @@ template <> struct Mat<bf16_t> {
 // 4096 positions 564 / 588, 32 heads of 128 x 128 over 4096 461 / 590, 64 heads of 32 x 32 over 4096 144 / 165, 8 heads over 1024 32 / 36.
 template <typename T, int KT> struct WalkMat : Mat<T> {
     static constexpr int in_planes = 1, resident = 2;            // (workgroups that a CU has room for)
-    static constexpr int limbs(int n) { return n; }
 };
 template <int KT> struct WalkMat<float, KT> : Mat<bf16_t> {
     typedef Mat<bf16_t> M;
     typedef Full In;
     static constexpr int in_planes = 3, plane = 16 * KT * kPitch, resident = KT < 4 ? 2 : 1;
-    static constexpr int limbs(int) { return 3; }
     static __device__ __forceinline__ In rows_in(const short *x, int m, int k, int lane)
     {
         Full f{};
@@ -630,10 +627,9 @@ struct WalkPlace {
     __device__ __forceinline__ WalkPlace(long long id, int groups) : unit((int)(id / (8ll * groups)) * 8 + (int)(id & 7)), group((int)(id / 8 % groups)) {}
 };
 
-// (P in as many limbs as a walk takes: two for an output in bf16, three for a gradient that goes on.)
-template <typename T, int KT, int NP> struct DeltaLds {
+template <typename T, int KT> struct DeltaLds {
     typedef WalkMat<T, KT> M;
-    typename M::Elem k[M::in_planes * 16 * KT * kPitch], q[M::in_planes * 16 * KT * kPitch], t[3 * kLow], p[M::limbs(NP) * kLow];
+    typename M::Elem k[M::in_planes * 16 * KT * kPitch], q[M::in_planes * 16 * KT * kPitch], t[3 * kLow], p[3 * kLow];
     Gates s;
 };
 constexpr int kWalkWaves = 4;           // of a workgroup; two of those fit a CU, one's products beside the other's way into LDS
@@ -641,11 +637,10 @@ template <int N> struct Part {
     static constexpr int value = N;
 };
 // A chunk's data on its way into LDS, and a wave's columns of v or dout, while the chunk before is worked at.
-template <typename T, int KT, int NP, bool KEYS_ONLY> struct Ahead {
+template <typename T, int KT, bool KEYS_ONLY> struct Ahead {
     static constexpr int LANES = 64 * kWalkWaves, NG = sizeof(Gates) / 16;
     Tile<T, 16 * KT, LANES> k, q;
-    LowTiles<Mat<bf16_t>, 3, LANES> t;
-    LowTiles<Mat<bf16_t>, WalkMat<T, KT>::limbs(NP), LANES> p;
+    LowTiles<Mat<bf16_t>, 3, LANES> t, p;
     f32x4 s;
     Rows<T> rows;
     // In four parts, between products: sixty KB at once are more than a CU's address unit takes, and the wave would wait for it.
@@ -662,7 +657,7 @@ template <typename T, int KT, int NP, bool KEYS_ONLY> struct Ahead {
             rows.load(row, t0, g4, a.pitch);
         }
     }
-    __device__ __forceinline__ void put(DeltaLds<T, KT, NP> &m, const DeltaShape<T> &a, int t0, int n) const
+    __device__ __forceinline__ void put(DeltaLds<T, KT> &m, const DeltaShape<T> &a, int t0, int n) const
     {
         k.put(m.k, a.DK, t0, n, a.pitch);
         if constexpr (!KEYS_ONLY) q.put(m.q, a.DK, t0, n, a.pitch);
@@ -756,7 +751,7 @@ template <int KT> __device__ __forceinline__ void unit_state(f32x4 (&S)[KT], int
 // registers: a state's tile, k^T S, w and what is added to S are each the next product's operand as they stand.  With heads for all CUs memory is the
 // bound, half of it the states that are kept (768 heads of 128 x 128, 16 chunks, bf16: 1.99 GB in 435 us, 4.6 TB/s); else a chunk's chain of three products,
 // 4.1 us of 128 x 128 channels in bf16 where a workgroup has its CU to itself (products and vector instructions are 2.7), nearly twice that where two share it.
-template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_fwd_walk(const DeltaFwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT, 2> &m, int unit, int group)
+template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_fwd_walk(const DeltaFwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT> &m, int unit, int group)
 {
     typedef WalkMat<T, KT> M;
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -782,7 +777,7 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
     const T *vrow = p.v.row(b, own, p.pitch), *krow = p.k.row(b, hk * p.DK, p.pitch), *qrow = p.q.row(b, hk * p.DK, p.pitch);
     T *orow = p.o.row(b, own, p.L);
     const DeltaPairs *pairs = p.pairs + head * p.chunks;
-    Ahead<T, KT, 2, SPANS> next;
+    Ahead<T, KT, SPANS> next;
     int ahead = from;                                   // (behind the last chunk that again: a load behind a question is waited for where its ways meet)
     const auto load = [&](auto part) __attribute__((always_inline)) {
         next.template load<decltype(part)::value>(p, krow, qrow, vrow, pairs + ahead, ahead * 64, 4 * (fresh(lane0) >> 4));
@@ -817,7 +812,7 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
                 const int i = u & 3, kb = 2 * (u >> 2);
                 if (i == 0) x = M::split(S[kb], S[kb + 1]);
                 r[i] = M::mma(a.k, x, r[i]);
-                if constexpr (!SPANS) o[i] = M::template mma<2>(a.q, x, o[i]);
+                if constexpr (!SPANS) o[i] = M::mma(a.q, x, o[i]);
                 if (u == 1) load(Part<0>{});
                 if (u == KT) load(Part<1>{});
             });
@@ -837,10 +832,10 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
                         if (u == 2) load(Part<3>{});
                     });
         if (!SPANS) {
-            piped<6, 1>([&](int u) __attribute__((always_inline)) { return M::template low_rows<2>(m.p, 16 * (u < 4 ? u : u - 2), u >> 2, lane); },
+            piped<6, 1>([&](int u) __attribute__((always_inline)) { return M::low_rows(m.p, 16 * (u < 4 ? u : u - 2), u >> 2, lane); },
                         [&](int u, const auto &a) __attribute__((always_inline)) {
-                            if (u % 4 == 0) x = M::template split<2>(w[u / 2], w[u / 2 + 1]);
-                            o[u < 4 ? u : u - 2] = M::template mma<2>(a, x, o[u < 4 ? u : u - 2]);
+                            if (u % 4 == 0) x = M::split(w[u / 2], w[u / 2 + 1]);
+                            o[u < 4 ? u : u - 2] = M::mma(a, x, o[u < 4 ? u : u - 2]);
                         });
             store_rows(orow, o, t0, g4, p.L, in);       // (k and q behind n are zeros, so these are)
         }
@@ -867,9 +862,9 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
 template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWalkWaves, (WalkMat<T, KT>::resident)) void delta_fwd_kernel(DeltaFwd<T> p, DeltaWalk walk, long long first)
 {
     extern __shared__ char lds[];
-    DeltaLds<T, KT, 2> &m = *reinterpret_cast<DeltaLds<T, KT, 2> *>(lds);
+    DeltaLds<T, KT> &m = *reinterpret_cast<DeltaLds<T, KT> *>(lds);
     LowTiles<Mat<bf16_t>, 3, 64 * kWalkWaves>::zeros(m.t);
-    if (!SPANS) LowTiles<Mat<bf16_t>, WalkMat<T, KT>::limbs(2), 64 * kWalkWaves>::zeros(m.p);
+    if (!SPANS) LowTiles<Mat<bf16_t>, 3, 64 * kWalkWaves>::zeros(m.p);
     const WalkPlace at(first + blockIdx.x, walk.groups);
     if (at.unit < walk.units) delta_fwd_walk<T, KT, SPANS>(p, walk, m, at.unit, at.group);
 }
@@ -877,7 +872,7 @@ template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWal
 // Backward, from chunk to chunk: with dS the gradient of the state behind a chunk,
 //     dw = P^T do + exp(G_63 - G) k dS,   (I + A)^T dr = dw,   dS <- exp(G_63) dS + sum_i exp(G_i) q_i do_i^T - beta_i exp(G_i) k_i dr_i^T.
 // 768 heads as above: 2.42 GB in 528 us, 4.6 TB/s.  Leaves dS behind every chunk, dr (whole, what needs it next does not form it again) and dv = beta dr.
-template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_bwd_walk(const DeltaBwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT, 3> &m, int unit, int group)
+template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_bwd_walk(const DeltaBwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT> &m, int unit, int group)
 {
     typedef WalkMat<T, KT> M;
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -906,7 +901,7 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
     if (!SPANS && in)                                   // (behind the sequence's end)
         for (int t = max(last, from) * 64 + 4 * (lane0 >> 4), to = min(p.L, seg + 1 < walk.segs ? (from + walk.per) * 64 : p.L); t < to; t += 16)
             store4(vrow, f32x4{}, t, p.L);
-    Ahead<T, KT, 3, false> next;
+    Ahead<T, KT, false> next;
     int ahead = max(last - 1, from);                    // (behind the last chunk that again)
     const auto load = [&](auto part) __attribute__((always_inline)) {
         next.template load<decltype(part)::value>(p, krow, qrow, drow, pairs + ahead, ahead * 64, 4 * (fresh(lane0) >> 4));
@@ -993,7 +988,7 @@ template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_
 template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWalkWaves, (WalkMat<T, KT>::resident)) void delta_bwd_state_kernel(DeltaBwd<T> p, DeltaWalk walk, long long first)
 {
     extern __shared__ char lds[];
-    DeltaLds<T, KT, 3> &m = *reinterpret_cast<DeltaLds<T, KT, 3> *>(lds);
+    DeltaLds<T, KT> &m = *reinterpret_cast<DeltaLds<T, KT> *>(lds);
     LowTiles<Mat<bf16_t>, 3, 64 * kWalkWaves>::zeros(m.t);
     LowTiles<Mat<bf16_t>, 3, 64 * kWalkWaves>::zeros(m.p);
     const WalkPlace at(first + blockIdx.x, walk.groups);
