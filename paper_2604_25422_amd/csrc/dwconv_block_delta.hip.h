@@ -1087,7 +1087,7 @@ constexpr int kGradWaves = 4;           // of a workgroup; two of those fit a CU
 
 template <typename T, int KT> struct DeltaChunkLds {
     typedef typename Mat<T>::Elem Elem;
-    static constexpr int NP = Mat<T>::planes, N2 = NP < 2 ? NP : 2, VB = 32;        // columns of a state at a time
+    static constexpr int NP = Mat<T>::planes, VB = 32;        // columns of a state at a time
     static constexpr int G = KT < kGradWaves ? KT : kGradWaves;                     // groups of the key's channels
     static constexpr bool HALVES = sizeof(T) == 2 || KT < 8;                        // (of wide keys in fp32 two workgroups have no room for x)
     Elem k[16 * KT * kPitch], t[NP * kLow];
@@ -1096,7 +1096,7 @@ template <typename T, int KT> struct DeltaChunkLds {
             Elem dout[VB * kPitch], w[NP * VB * kPitch], dr[NP * VB * kPitch];
         };
         struct {
-            Elem p[N2 * kLow];
+            Elem p[NP * kLow];
             float rows[10][16], columns[10][16];    // of the pairs' tiles: what P dP is over a row, and both pairs over a column
         };
     };
@@ -1306,7 +1306,7 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
         }
         take_pairs();
         __syncthreads();
-        LowTiles<M, Lds::N2, 64 * W>::zeros(m.p);
+        LowTiles<M, 3, 64 * W>::zeros(m.p);
 #pragma unroll
         for (int s = 0; s < SL; ++s) {
             qrow[s].get(qh[s], t0, g4, n, p.pitch);
@@ -1386,8 +1386,8 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
         for (int v = 0; v < 4; ++v) z[v] = ti > tj || c >= g4 + v ? z[v] : 0.0f;
         z = sum16(z);
         if (c == 0) *reinterpret_cast<f32x4 *>(m.columns[task] + g4) = below, *reinterpret_cast<f32x4 *>(m.dg[task] + g4) = z;
-        M::template put<2>(m.p, kLow, low_at(i, j), dP * e * p.scale);
-        M::template put<2>(m.t, kLow, low_at(i, j), dA * e * m.s.beta[i]);
+        M::put(m.p, kLow, low_at(i, j), dP * e * p.scale);
+        M::put(m.t, kLow, low_at(i, j), dA * e * m.s.beta[i]);
     }
     __syncthreads();
     // Sums over the channels of q dq and k dk, whose pairs' part is that of P dP and of A dA, and dbeta; dg from what rows take, what columns leave and the pairs
@@ -1459,8 +1459,8 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
                 struct {
                     Full x, y;
                 } o;
-                if (u & 1) o.x = M::template low_columns<2>(m.p, 16 * min(i, 2 * kb + 1), kb, lane), o.y = M::template low_columns<2>(m.t, 16 * min(i, 2 * kb + 1), kb, lane);
-                else o.x = M::template low_rows<2>(m.p, 16 * max(i, 2 * kb), kb, lane), o.y = M::template low_rows<2>(m.t, 16 * max(i, 2 * kb), kb, lane);
+                if (u & 1) o.x = M::low_columns(m.p, 16 * min(i, 2 * kb + 1), kb, lane), o.y = M::low_columns(m.t, 16 * min(i, 2 * kb + 1), kb, lane);
+                else o.x = M::low_rows(m.p, 16 * max(i, 2 * kb), kb, lane), o.y = M::low_rows(m.t, 16 * max(i, 2 * kb), kb, lane);
                 return o;
             },
             [&](int u, const auto &o) __attribute__((always_inline)) {
@@ -1468,16 +1468,16 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
                 if (u % (2 * NI) == 0)
 #pragma unroll
                     for (int s = 0; s < SL; ++s) {
-                        kz[s] = M::template split<2>(kh(s, 2 * kb, lane), kh(s, 2 * kb + 1, lane));
-                        qz[s] = M::template split<2>(qh[s][2 * kb], qh[s][2 * kb + 1]);
+                        kz[s] = M::split(kh(s, 2 * kb, lane), kh(s, 2 * kb + 1, lane));
+                        qz[s] = M::split(qh[s][2 * kb], qh[s][2 * kb + 1]);
                     }
                 if (u & 1) {
                     if (i < 2 * kb + 2)
 #pragma unroll
-                        for (int s = 0; s < SL; ++s) x2[s][ii] = M::template mma<2>(o.y, kz[s], M::template mma<2>(o.x, qz[s], x2[s][ii]));
+                        for (int s = 0; s < SL; ++s) x2[s][ii] = M::mma(o.y, kz[s], M::mma(o.x, qz[s], x2[s][ii]));
                 } else if (2 * kb <= i) {
 #pragma unroll
-                    for (int s = 0; s < SL; ++s) x1[s][ii] = M::template mma<2>(o.x, kz[s], x1[s][ii]), x2[s][ii] = M::template mma<2>(o.y, kz[s], x2[s][ii]);
+                    for (int s = 0; s < SL; ++s) x1[s][ii] = M::mma(o.x, kz[s], x1[s][ii]), x2[s][ii] = M::mma(o.y, kz[s], x2[s][ii]);
                 }
             });
     }

@@ -76,3 +76,37 @@ def test_outputs_of_a_chunk_that_cancel(what, DK, dtype):
     want, size = (term[0] + term[1]).view(B, -1, L), (term[0].abs() + term[1].abs()).view(B, -1, L)
     # the exponential 4, its two factors, the product with beta and w's own sum, the sum of the two in as many additions as before
     within(o, want, 32 * U * size)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("DK", [2, 40, 128])
+@pytest.mark.parametrize("L", [1, 130])
+@pytest.mark.parametrize("each", [1, 3])
+def test_gradients_along_a_key_that_cancel(each, L, DK, dtype):
+    """A query that points where its own key does: o does not change when either becomes longer, so that of dq and dk, which lie along them, only
+    eps / |x|^2 is left.  One position of every chunk has keys and values."""
+    B, Hk, scale, eps, at = 4, 3, 0.75, 1e-6, 0 if L == 1 else 37
+    H, t = each * Hk, torch.arange(L, device="cuda")
+    on = (t % 64 == at).to(dtype)
+    k = rand(B, Hk, DK, L, seed=1, dtype=dtype)
+    k[:, :, 2:] = 0                                     # (two channels of a key: few terms to a sum, wherever the second lies)
+    if DK > 2:
+        k[:, :, DK - 1], k[:, :, 1] = k[:, :, 1], 0
+    k = k * on
+    q = -2 * k
+    v, do = (rand(B, H, 1, L, seed=s, dtype=dtype) * on for s in (2, 3))
+    beta, inf = uniform(B, H, L, seed=4, lo=0.5, hi=1), torch.full((B, H, L), -float("inf"), device="cuda")
+    flat = [x.view(B, -1, L) for x in (q, k, v)]
+    # (every position forgets what lies in front of it: each is a rule of its own)
+    _, _, states = block.delta_fwd(*flat, inf, beta, key_heads=Hk, scale=scale, eps=eps)
+    dq, dk, *_ = block.delta_bwd(do.view(B, -1, L), *flat, inf, beta, states, key_heads=Hk, scale=scale, eps=eps)
+    x = k.double()
+    square = x.square().sum(2, keepdim=True)
+    ik, iq = 1 / torch.sqrt(square + eps), 1 / torch.sqrt(4 * square + eps)
+    unit_k, unit_q = x * ik, -2 * x * iq
+    pair = scale * (do.double() * v.double() * beta.double()[:, :, None]).view(B, Hk, each, 1, L)
+    for got, other, own, i in ((dq, unit_k, unit_q, iq), (dk, unit_q, unit_k, ik)):
+        one = pair.sum(2) * (other - own * (own * other).sum(2, keepdim=True)) * i
+        size = pair.abs().sum(2) * (other.abs() + own.abs() * (own * other).abs().sum(2, keepdim=True)) * i
+        # lengths 6 and twice, the pair's product and its factors 8, P in the sums along a key 12, the sums of two channels and of heads 8
+        within(got, one.view(B, -1, L), 40 * U * size.view(B, -1, L))
