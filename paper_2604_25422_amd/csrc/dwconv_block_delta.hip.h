@@ -449,7 +449,7 @@ template <typename M, int N, int LANES> struct LowTiles {
     // What a product 32 deep takes beside the triangle: blocks (0, 1) and (2, 3), zeros, written once.
     static __device__ __forceinline__ void zeros(typename M::Elem *to)
     {
-        for (int i = threadIdx.x; i < 2 * 64; i += LANES)
+        for (int i = fresh(threadIdx.x); i < 2 * 64; i += LANES)
             M::template put<N>(to, kLow, low_at((i >> 6) * 32 + ((i & 63) >> 2), (i >> 6) * 32 + 16 + 4 * (i & 3)), f32x4{});
     }
 };
@@ -1201,14 +1201,18 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
                 for (int i = 0; i < TI; ++i) x[i] = M::mma(M::columns_in(m.k, first + 16 * i, 16 * kb, lane), s, x[i]);
                 step_done();
             }
+            const auto states = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int s = 0; s < SL; ++s)                // (in the registers that were S's)
+                for (int s = 0; s < SL; ++s)
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    const int dk = 16 * (slice0 + s) + c;
-                    a[s][kb] = before.any_four(dk, v0 + 16 * kb + g4), e[s][kb] = after.any_four(dk, v0 + 16 * kb + g4);
-                }
-            step_done();
+                    for (int kb = 0; kb < 2; ++kb) {
+                        const int dk = 16 * (slice0 + s) + c;
+                        a[s][kb] = before.any_four(dk, v0 + 16 * kb + g4), e[s][kb] = after.any_four(dk, v0 + 16 * kb + g4);
+                    }
+                step_done();
+            };
+            // (in the registers that were S's; of wide keys in fp32 there are none over until w is formed: 108 bytes a lane went to memory)
+            if (Lds::HALVES) states();
             vrow.get(val, t0 + first, g4, n, p.pitch);
             if (v0 + VB > p.DV) {
                 const bool out = v0 + 16 * (wave & 1) + c >= p.DV;
@@ -1246,6 +1250,7 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
             M::put(m.w, VP, row + near, yn);
             M::put(m.w, VP, row + far, yf);
             step_done();
+            if (!Lds::HALVES) states();
         }
         {
             const int lane = fresh(lane0), g4 = 4 * (lane >> 4);
