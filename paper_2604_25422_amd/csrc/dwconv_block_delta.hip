@@ -163,12 +163,18 @@ template <typename T, int KT, int W> int launch_pairs(const DeltaShape<T> &p, in
     for_units(units, [&](int first, int n) { delta_pairs_kernel<T, KT, W><<<n, 64 * W, lds, st>>>(p, first); });
     return DWCONV_OK;
 }
-// Waves of a chunk's pairs: eight where the chip has room for all of them at once, four of more chunks.  us of a trained call with eight / with four:
-// 128 chunks of 32 x 32 in fp32 89 / 93, 2048 of 64 x 96 in bf16 325 / 329; 8192 of 64 x 64 in fp32 1880 / 1848, 12288 of 128 x 128 in bf16 2630 / 2587.
+// Waves of a chunk's pairs: eight of up to 1024 chunks, where a CU has slots for the waves of all it gets at once, and beyond that where LDS has room for one
+// chunk to a CU (fp32, 128 channels: four waves would be one to a SIMD) or a chunk is products rather than loads; else four, of which three or more
+// workgroups to a CU keep memory busy.  us of the pairs alone with eight / with four: 128 chunks 8 to 11 / 9 to 14 in every type and width, 1024 chunks bf16 32
+// channels 13.0 / 13.1, 128 20.9 / 22.7, fp32 64 channels 24.5 / 26.4; 8192 chunks fp32 32 channels 89 / 94, 64 168 / 143, 128 346 / 408, bf16 32 channels 72 / 68, 64 77 /
+// 84, 128 140 / 118.
 template <typename T, int KT> int launch_pairs(const DeltaShape<T> &p, hipStream_t st)
 {
+    constexpr bool eight = sizeof(T) == 4 ? KT != 4 : KT == 4;
     const int units = p.B * p.H * p.chunks;
-    return units <= 2048 ? launch_pairs<T, KT, 8>(p, units, st) : launch_pairs<T, KT, 4>(p, units, st);
+    if constexpr (!eight)
+        if (units > 1024) return launch_pairs<T, KT, 4>(p, units, st);
+    return launch_pairs<T, KT, 8>(p, units, st);
 }
 
 // Segments that a head's chunks are cut into.  A walk's steps are a chain: few heads leave most of the chip idle, and what a segment does to any state

@@ -209,6 +209,13 @@ def test_many_segments(B, H, Hk, DK, DV, L, dtype):
     check_rule(*inputs(B, H, Hk, DK, DV, L, dtype, seed=L, rate=0.01), lengths=lengths, key_heads=Hk)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("DK", [20, 50, 100])
+@pytest.mark.parametrize("B", [1024, 1030])
+def test_as_many_chunks_as_run_at_once_and_more(B, DK, dtype):
+    check_rule(*inputs(B, 1, 1, DK, 5, 9, dtype, seed=DK))
+
+
 def test_without_what_may_be_left_out():
     q, k, v, g, beta, s0, do, ds = inputs(2, 2, 2, 24, 40, 100, F32)
     got = check_rule(q, k, v, g, beta, None, do, None)
