@@ -298,11 +298,12 @@ template <typename T> int launch_bwd(const DeltaBwd<T> &p, const DeltaWalk &w, h
 template <typename T> void launch_step(const DeltaStep<T> &in, hipStream_t st)
 {
     DeltaStep<T> p = in;
-    // Lanes of a row, four columns each: 64 columns, but 32 where the call would leave CUs without work.  us with 32 / 64 / 128 columns (bf16, 128 x 128): 8 heads
-    // 4.2 / 4.7 / 5.9, 24 heads 4.3 / 4.9 / 6.1, 96 heads 5.4 / 5.5 / 6.6, 384 heads 9.4 / 8.7 / 9.2, 1536 heads 33.7 / 34.7 / 37.5; 64 x 64, 2048 heads 14.7 / 11.4.
+    // Lanes of a row, four columns each: 64 columns, but 32 where the call would leave CUs without work or half of a head's last 64 would not be there.
+    // us with 32 / 64 columns, bf16, three pools in turn: 64 heads of 128 x 128 5.0 / 5.4, 256 10.0 / 9.6, 768 19.7 / 20.2, 1536 38.6 / 39.0, 6144 160 / 156; 64 x 64, 64 heads
+    // 4.4 / 4.4, 512 6.8 / 5.8, 6144 41.6 / 38.4; 96 x 96, 512 heads 10.6 / 11.4, 1536 22.0 / 27.2, 6144 85 / 91.  (128 columns a workgroup of 128 x 128: 6 to 25 % more than 64.)
     int lg = 0;
     while (lg < 4 && (4 << lg) < p.DV) ++lg;
-    while (lg > 3 && (long long)p.B * p.H * ceil_div(p.DV, 4 << lg) < 512) --lg;
+    if (lg > 3 && (ceil_div(p.DV, 32) % 2 || (long long)p.B * p.H * ceil_div(p.DV, 64) < 512)) lg = 3;
     p.blocks = (int)ceil_div(p.DV, 4 << lg);
     const int units = p.B * p.H * p.blocks, rows = (int)ceil_div(p.DK, 256 >> lg);
     const auto kernel = rows <= 1 ? delta_step_kernel<T, 1> : rows <= 2 ? delta_step_kernel<T, 2> : rows <= 4 ? delta_step_kernel<T, 4> : delta_step_kernel<T, 8>;

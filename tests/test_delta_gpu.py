@@ -392,6 +392,13 @@ def test_a_token_is_the_rule(B, H, Hk, DK, DV, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,H,Hk,DK,DV", [(280, 2, 1, 20, 64), (280, 2, 1, 20, 65), (140, 4, 2, 64, 96), (260, 2, 2, 30, 97), (130, 4, 4, 9, 129), (90, 4, 4, 40, 190)])
+def test_tokens_of_many_heads(B, H, Hk, DK, DV, dtype):
+    """So many that the columns of a head go to as few workgroups as they fit."""
+    test_a_token_is_the_rule(B, H, Hk, DK, DV, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_token_layouts(dtype):
     q, k, v, g, beta, _, _, _ = inputs(4, 4, 2, 20, 24, 1, dtype)
     flat = [x[..., 0].contiguous() for x in (q, k, v, g, beta)]
