@@ -134,26 +134,23 @@ template <> struct Mat<float> {
         f32x4 a, b;
     };
     typedef Full In;
-    static __device__ __forceinline__ In rows_in(const float *x, int m, int k, int lane) { return In{rows_of(x, m, k, lane), rows_of(x, m, k + 16, lane)}; }
     static __device__ __forceinline__ In columns_in(const float *x, int m, int k, int lane) { return In{columns_of(x, m, k, lane), columns_of(x, m, k + 16, lane)}; }
-    template <int N = 1> static __device__ __forceinline__ Full columns(const float *x, int, int m, int k, int lane) { return columns_in(x, m, k, lane); }
+    static __device__ __forceinline__ Full columns(const float *x, int, int m, int k, int lane) { return columns_in(x, m, k, lane); }
     // Of a lower triangle: rows m.., columns 32 kb..; and of it transposed.
-    template <int N = 1> static __device__ __forceinline__ Full low_rows(const float *x, int m, int kb, int lane)
+    static __device__ __forceinline__ Full low_rows(const float *x, int m, int kb, int lane)
     {
         const float *p = x + low_at(m, 32 * kb);
         return Full{rows_of(p, 0, 0, lane, low_pitch(m)), rows_of(p, 0, 16, lane, low_pitch(m))};
     }
-    template <int N = 1> static __device__ __forceinline__ Full low_columns(const float *x, int m, int kb, int lane)
+    static __device__ __forceinline__ Full low_columns(const float *x, int m, int kb, int lane)
     {
         const float *p = x + low_at(32 * kb, m);
         return Full{columns_of(p, 0, 0, lane, low_pitch(32 * kb)), columns_of(p, 0, 16, lane, low_pitch(32 * kb))};
     }
-    template <int N = 1> static __device__ __forceinline__ Full split(f32x4 a, f32x4 b) { return Full{a, b}; }
-    static __device__ __forceinline__ In exact(f32x4 a, f32x4 b) { return In{a, b}; }
+    static __device__ __forceinline__ Full split(f32x4 a, f32x4 b) { return Full{a, b}; }
     static __device__ __forceinline__ f32x4 wide(const float *x, int at) { return four(x, at); }
-    static __device__ __forceinline__ void put_one(float *x, int, int at, float v) { x[at] = v; }
-    template <int ORDER = 3> static __device__ __forceinline__ f32x4 mma(Full a, Full b, f32x4 d) { return mma16(a.b, b.b, mma16(a.a, b.a, d)); }
-    template <int N = 1> static __device__ __forceinline__ void put(float *x, int, int at, f32x4 v) { *reinterpret_cast<f32x4 *>(x + at) = v; }
+    static __device__ __forceinline__ f32x4 mma(Full a, Full b, f32x4 d) { return mma16(a.b, b.b, mma16(a.a, b.a, d)); }
+    static __device__ __forceinline__ void put(float *x, int, int at, f32x4 v) { *reinterpret_cast<f32x4 *>(x + at) = v; }
 };
 template <> struct Mat<bf16_t> {
     typedef short Elem;
@@ -182,25 +179,25 @@ template <> struct Mat<bf16_t> {
     }
     static __device__ __forceinline__ In rows_in(const short *x, int m, int k, int lane) { return In{{row(x, m, k, lane)}}; }
     static __device__ __forceinline__ In columns_in(const short *x, int m, int k, int lane) { return In{{column(x, m, k, lane)}}; }
-    template <int N = 3> static __device__ __forceinline__ Full low_rows(const short *x, int m, int kb, int lane)
+    static __device__ __forceinline__ Full low_rows(const short *x, int m, int kb, int lane)
     {
         Full f{};
 #pragma unroll
-        for (int n = 0; n < N; ++n) f.l[n] = row(x + n * kLow + low_at(m, 32 * kb), 0, 0, lane, low_pitch(m));
+        for (int n = 0; n < 3; ++n) f.l[n] = row(x + n * kLow + low_at(m, 32 * kb), 0, 0, lane, low_pitch(m));
         return f;
     }
-    template <int N = 3> static __device__ __forceinline__ Full low_columns(const short *x, int m, int kb, int lane)
+    static __device__ __forceinline__ Full low_columns(const short *x, int m, int kb, int lane)
     {
         Full f{};
 #pragma unroll
-        for (int n = 0; n < N; ++n) f.l[n] = column(x + n * kLow + low_at(32 * kb, m), 0, 0, lane, low_pitch(32 * kb));
+        for (int n = 0; n < 3; ++n) f.l[n] = column(x + n * kLow + low_at(32 * kb, m), 0, 0, lane, low_pitch(32 * kb));
         return f;
     }
-    template <int N = 3> static __device__ __forceinline__ Full columns(const short *x, int plane, int m, int k, int lane)
+    static __device__ __forceinline__ Full columns(const short *x, int plane, int m, int k, int lane)
     {
         Full f{};
 #pragma unroll
-        for (int n = 0; n < N; ++n) f.l[n] = column(x + n * plane, m, k, lane);
+        for (int n = 0; n < 3; ++n) f.l[n] = column(x + n * plane, m, k, lane);
         return f;
     }
     // x without element I of a pair: (w0, w1) . (-1, 0) + x or (w0, w1) . (0, -1) + x, which is exact, in one instruction (a shift or a mask and a
@@ -219,11 +216,11 @@ template <> struct Mat<bf16_t> {
         x = f32x4{less<0>(x[0], w[0]), less<1>(x[1], w[0]), less<0>(x[2], w[1]), less<1>(x[3], w[1])};
         return w;
     }
-    template <int N = 3> static __device__ __forceinline__ Full split(f32x4 a, f32x4 b)
+    static __device__ __forceinline__ Full split(f32x4 a, f32x4 b)
     {
         Full f{};
 #pragma unroll
-        for (int n = 0; n < N; ++n) f.l[n] = pair(limb(a), limb(b));
+        for (int n = 0; n < 3; ++n) f.l[n] = pair(limb(a), limb(b));
         return f;
     }
     // ... of values that are bf16 already.
@@ -236,29 +233,22 @@ template <> struct Mat<bf16_t> {
         const u32x2 u = *reinterpret_cast<const u32x2 *>(x + at);
         return f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xffff0000u), __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xffff0000u)};
     }
-    // One element of a Full matrix of two planes.
-    static __device__ __forceinline__ void put_one(short *x, int plane, int at, float v)
-    {
-        const unsigned w = pack_bf16(v, 0.0f);
-        x[at] = (short)w;
-        x[at + plane] = (short)pack_bf16(v - __uint_as_float(w << 16), 0.0f);
-    }
-    // Products of limbs whose numbers add up to less than ORDER, the smallest first.
-    template <int ORDER = 3, typename A, typename B> static __device__ __forceinline__ f32x4 mma(const A &a, const B &b, f32x4 d)
+    // Products of limbs whose numbers add up to less than three, the smallest first.
+    template <typename A, typename B> static __device__ __forceinline__ f32x4 mma(const A &a, const B &b, f32x4 d)
     {
         constexpr int na = sizeof(a.l) / sizeof(bf16x8), nb = sizeof(b.l) / sizeof(bf16x8);
 #pragma unroll
-        for (int s = ORDER - 1; s >= 0; --s)
+        for (int s = 2; s >= 0; --s)
 #pragma unroll
             for (int i = 0; i < na; ++i)
                 if (s - i >= 0 && s - i < nb) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.l[i], b.l[s - i], d, 0, 0, 0);
         return d;
     }
     // Four neighbours of a row of a Full matrix.
-    template <int N = 3> static __device__ __forceinline__ void put(short *x, int plane, int at, f32x4 v)
+    static __device__ __forceinline__ void put(short *x, int plane, int at, f32x4 v)
     {
 #pragma unroll
-        for (int n = 0; n < N; ++n) *reinterpret_cast<u32x2 *>(x + n * plane + at) = limb(v);
+        for (int n = 0; n < 3; ++n) *reinterpret_cast<u32x2 *>(x + n * plane + at) = limb(v);
     }
 };
 
@@ -280,11 +270,8 @@ template <int KT> struct WalkMat<float, KT> : Mat<bf16_t> {
         for (int n = 0; n < 3; ++n) f.l[n] = row(x + n * plane, m, k, lane);
         return f;
     }
-    static __device__ __forceinline__ In columns_in(const short *x, int m, int k, int lane) { return M::template columns<3>(x, plane, m, k, lane); }
-    template <int N = 3> static __device__ __forceinline__ Full low_rows(const short *x, int m, int kb, int lane) { return M::template low_rows<3>(x, m, kb, lane); }
-    template <int N = 3> static __device__ __forceinline__ Full split(f32x4 a, f32x4 b) { return M::template split<3>(a, b); }
-    static __device__ __forceinline__ In exact(f32x4 a, f32x4 b) { return M::template split<3>(a, b); }
-    template <int ORDER = 3> static __device__ __forceinline__ f32x4 mma(const Full &a, const Full &b, f32x4 d) { return M::template mma<3>(a, b, d); }
+    static __device__ __forceinline__ In columns_in(const short *x, int m, int k, int lane) { return M::columns(x, plane, m, k, lane); }
+    static __device__ __forceinline__ In exact(f32x4 a, f32x4 b) { return M::split(a, b); }
 };
 
 // Four consecutive positions of a row.
@@ -423,8 +410,8 @@ __device__ __forceinline__ void low_tile(int i, int &ti, int &tj)     // tile i 
     ti = i >= 6 ? 3 : i >= 3 ? 2 : i >= 1 ? 1 : 0;
     tj = i - ti * (ti + 1) / 2;
 }
-// The lower triangle of a chunk's matrix on its way from a record into LDS as a Full matrix of N limbs.
-template <typename M, int N, int LANES> struct LowTiles {
+// The lower triangle of a chunk's matrix on its way from a record into LDS as a Full matrix.
+template <typename M, int LANES> struct LowTiles {
     static constexpr int U = (640 + LANES - 1) / LANES;
     f32x4 x[U];
     __device__ __forceinline__ void load(const float (&from)[10][256])
@@ -443,14 +430,14 @@ template <typename M, int N, int LANES> struct LowTiles {
             if (640 % LANES && i >= 640) continue;
             int ti, tj;
             low_tile(i >> 6, ti, tj);
-            M::template put<N>(to, kLow, low_at(16 * ti + ((i & 63) >> 2), 16 * tj + 4 * (i & 3)), x[u]);
+            M::put(to, kLow, low_at(16 * ti + ((i & 63) >> 2), 16 * tj + 4 * (i & 3)), x[u]);
         }
     }
     // What a product 32 deep takes beside the triangle: blocks (0, 1) and (2, 3), zeros, written once.
     static __device__ __forceinline__ void zeros(typename M::Elem *to)
     {
         for (int i = fresh(threadIdx.x); i < 2 * 64; i += LANES)
-            M::template put<N>(to, kLow, low_at((i >> 6) * 32 + ((i & 63) >> 2), (i >> 6) * 32 + 16 + 4 * (i & 3)), f32x4{});
+            M::put(to, kLow, low_at((i >> 6) * 32 + ((i & 63) >> 2), (i >> 6) * 32 + 16 + 4 * (i & 3)), f32x4{});
     }
 };
 
@@ -640,7 +627,7 @@ template <int N> struct Part {
 template <typename T, int KT, bool KEYS_ONLY> struct Ahead {
     static constexpr int LANES = 64 * kWalkWaves, NG = sizeof(Gates) / 16;
     Tile<T, 16 * KT, LANES> k, q;
-    LowTiles<Mat<bf16_t>, 3, LANES> t, p;
+    LowTiles<Mat<bf16_t>, LANES> t, p;
     f32x4 s;
     Rows<T> rows;
     // In four parts, between products: sixty KB at once are more than a CU's address unit takes, and the wave would wait for it.
@@ -863,8 +850,8 @@ template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWal
 {
     extern __shared__ char lds[];
     DeltaLds<T, KT> &m = *reinterpret_cast<DeltaLds<T, KT> *>(lds);
-    LowTiles<Mat<bf16_t>, 3, 64 * kWalkWaves>::zeros(m.t);
-    if (!SPANS) LowTiles<Mat<bf16_t>, 3, 64 * kWalkWaves>::zeros(m.p);
+    LowTiles<Mat<bf16_t>, 64 * kWalkWaves>::zeros(m.t);
+    if (!SPANS) LowTiles<Mat<bf16_t>, 64 * kWalkWaves>::zeros(m.p);
     const WalkPlace at(first + blockIdx.x, walk.groups);
     if (at.unit < walk.units) delta_fwd_walk<T, KT, SPANS>(p, walk, m, at.unit, at.group);
 }
@@ -989,8 +976,8 @@ template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWal
 {
     extern __shared__ char lds[];
     DeltaLds<T, KT> &m = *reinterpret_cast<DeltaLds<T, KT> *>(lds);
-    LowTiles<Mat<bf16_t>, 3, 64 * kWalkWaves>::zeros(m.t);
-    LowTiles<Mat<bf16_t>, 3, 64 * kWalkWaves>::zeros(m.p);
+    LowTiles<Mat<bf16_t>, 64 * kWalkWaves>::zeros(m.t);
+    LowTiles<Mat<bf16_t>, 64 * kWalkWaves>::zeros(m.p);
     const WalkPlace at(first + blockIdx.x, walk.groups);
     if (at.unit < walk.units) delta_bwd_walk<T, KT, SPANS>(p, walk, m, at.unit, at.group);
 }
@@ -1160,7 +1147,7 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
     };
     {
         Tile<T, 16 * KT, 64 * W> kt;
-        LowTiles<M, 3, 64 * W> t;
+        LowTiles<M, 64 * W> t;
         kt.load(p.k.row(b, hk * p.DK, p.pitch), p.DK, t0, p.pitch);
         t.load(pairs.t);
         const f32x4 gates = reinterpret_cast<const f32x4 *>(&pairs.s)[threadIdx.x < sizeof(ChunkGates) / 16 ? threadIdx.x : 0];
@@ -1311,7 +1298,7 @@ template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta
         }
         take_pairs();
         __syncthreads();
-        LowTiles<M, 3, 64 * W>::zeros(m.p);
+        LowTiles<M, 64 * W>::zeros(m.p);
 #pragma unroll
         for (int s = 0; s < SL; ++s) {
             qrow[s].get(qh[s], t0, g4, n, p.pitch);
@@ -1521,7 +1508,7 @@ template <typename T, int KT, bool SHARED> __global__ __launch_bounds__(64 * kGr
 {
     extern __shared__ char lds[];
     DeltaChunkLds<T, KT> &m = *reinterpret_cast<DeltaChunkLds<T, KT> *>(lds);
-    LowTiles<Mat<T>, 3, 64 * kGradWaves>::zeros(m.t);
+    LowTiles<Mat<T>, 64 * kGradWaves>::zeros(m.t);
     delta_bwd_chunk<T, KT, SHARED>(p, m, first + (int)blockIdx.x);
 }
 
