@@ -142,15 +142,16 @@ int check_heads(int B, int H, int Hk, int DK, int DV, int L)
 bool eps_ok(float eps) { return eps >= 0.0f && eps < INFINITY; }
 bool finite_ok(float x) { return x - x == 0.0f; }
 
-// Lets a kernel have more than 64 KiB of LDS, once a device.
+// Lets a kernel have more than 64 KiB of LDS, once a device.  (A refusal is this call's: it is not left for the next one's status.)
 template <typename Kernel> bool allow_lds(Kernel kernel, size_t bytes, std::atomic<unsigned long long> &done)
 {
     if (bytes <= 64 * 1024) return true;
     int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess) return false;
+    const auto refused = [] { return (void)hipGetLastError(), false; };
+    if (hipGetDevice(&dev) != hipSuccess) return refused();
     const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
     if (done.load(std::memory_order_acquire) & bit) return true;
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return false;
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return refused();
     done.fetch_or(bit, std::memory_order_release);
     return true;
 }
@@ -261,7 +262,7 @@ template <typename T, int KT> int launch_fwd(const DeltaFwd<T> &p, const DeltaWa
     int rc = launch_pairs<T, KT>(p, st);
     if (rc == DWCONV_OK && w.segs > 1) {
         rc = launch_segments(delta_fwd_kernel<T, KT, true>, p, w, span_columns(p.DK, p.DV), lds, done[1], st);
-        launch_starts<KT, false>(p.s0, w, p.B * p.H, p.DK, p.DV, st);
+        if (rc == DWCONV_OK) launch_starts<KT, false>(p.s0, w, p.B * p.H, p.DK, p.DV, st);
     }
     if (rc == DWCONV_OK) rc = launch_segments(delta_fwd_kernel<T, KT, false>, p, w, p.DV, lds, done[0], st);
     return rc == DWCONV_OK ? launch_status() : rc;
@@ -279,7 +280,7 @@ template <typename T, int KT> int launch_bwd(const DeltaBwd<T> &p, const DeltaWa
     int rc = launch_pairs<T, KT>(p, st);
     if (rc == DWCONV_OK && w.segs > 1) {
         rc = launch_segments(delta_bwd_state_kernel<T, KT, true>, p, w, span_columns(p.DK, p.DV), lds, done[1], st);
-        launch_starts<KT, true>(p.ds_last, w, p.B * p.H, p.DK, p.DV, st);
+        if (rc == DWCONV_OK) launch_starts<KT, true>(p.ds_last, w, p.B * p.H, p.DK, p.DV, st);
     }
     if (rc == DWCONV_OK) rc = launch_segments(delta_bwd_state_kernel<T, KT, false>, p, w, p.DV, lds, done[0], st);
     const auto kernel = p.each > 1 ? delta_bwd_chunk_kernel<T, KT, true> : delta_bwd_chunk_kernel<T, KT, false>;
