@@ -176,7 +176,7 @@ DWCONV_API int dwconv_delta_step(dwconv_seq q, dwconv_seq k, dwconv_seq v, dwcon
 
 /*
  * Dropout:  out = res + scale x / (1 - p) where an element is kept, res where it is not (whatever x holds there); res.data NULL: zeros for res.
- * The same call on a gradient (without res) is the backward pass.  0 <= p < 1, scale finite; out may be x or res itself.
+ * The same call on a gradient (without res) is the backward pass.  0 <= p < 1, scale / (1 - p) finite in fp32; out may be x or res itself.
  * An element is dropped when its 32 bits are below round(p 2^32), p as an fp32 value.  The bits are a function of rng [2] (int64 in DEVICE memory:
  * a seed and a step, of which the lower 32 bits count; a captured graph draws another mask when the caller has changed them), of layer (0 .. 2^24 - 1,
  * for the calls that share a seed and a step), of b and of j = c L + t, or with `tied` of j = c: whole channels are dropped.  With m = j >> 3 they

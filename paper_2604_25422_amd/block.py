@@ -329,10 +329,10 @@ def _dropout(x, name, p, rng, layer, res, scale, tied, out):
 
 
 def dropout_fwd(x, p: float, rng, layer: int = 0, res=None, scale: float = 1.0, tied: bool = False, out=None):
-    """res + scale x / (1 - p) where an element of x [B, C, L] is kept, res (None: zeros) where it is dropped, with probability p.  ``tied``: whole
-    channels of a batch entry are.  rng [2] int64 on the GPU, a seed and a step, decides together with ``layer`` (0 .. 2^24 - 1): the same three give
-    the same mask, which is stored nowhere; a program counts the step up (``rng[1] += 1``, also between replays of a graph) and gives every layer
-    its number.  out may be x or res itself."""
+    """res + scale x / (1 - p) where an element of x [B, C, L] is kept, res (None: zeros) where it is dropped, with probability p; scale / (1 - p) is
+    finite in 32 bits.  ``tied``: whole channels of a batch entry are.  rng [2] int64 on the GPU, a seed and a step, decides together with ``layer``
+    (0 .. 2^24 - 1): the same three give the same mask, which is stored nowhere; a program counts the step up (``rng[1] += 1``, also between replays
+    of a graph) and gives every layer its number.  out may be x or res itself."""
     return _dropout(x, "x", p, rng, layer, res, scale, tied, out)
 
 

@@ -138,14 +138,14 @@ extern "C" int dwconv_dropout(dwconv_seq x, dwconv_seq res, dwconv_seq_out out, 
     int rc = check_dims(B, C, L);
     if (rc != DWCONV_OK) return rc;
     if (!dtype_ok(dtype)) return DWCONV_ERR_DTYPE;
-    if (!(p >= 0.0f && p < 1.0f) || !(scale - scale == 0.0f) || layer < 0 || layer >= 1 << 24) return DWCONV_ERR_VALUE;
+    const float factor = (float)((double)scale / (1.0 - (double)p));            // (infinite, it would make NaN of a zero)
+    if (!(p >= 0.0f && p < 1.0f) || !(factor - factor == 0.0f) || layer < 0 || layer >= 1 << 24) return DWCONV_ERR_VALUE;
     const size_t es = elem_size(dtype);
     if ((rc = check_in(x, es)) != DWCONV_OK || (rc = check_in(res, es)) != DWCONV_OK) return rc;
     if ((rc = check_out(out, es, B, C, L)) != DWCONV_OK) return rc;
     if (!aligned_to(rng, 8)) return DWCONV_ERR_ALIGN;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const unsigned limit = (unsigned)rint((double)p * 4294967296.0);            // (p < 1 in 32 bits: at most 2^32 - 256)
-    const float factor = (float)((double)scale / (1.0 - (double)p));
     if (dtype == DWCONV_F32)
         return launch(Dropout<float>{seq<float>(x), seq<float>(res), seq<float>(out), rng, (long long)C * L, B, L, limit, (unsigned)layer, factor}, tied != 0, st);
     return launch(Dropout<bf16_t>{seq<bf16_t>(x), seq<bf16_t>(res), seq<bf16_t>(out), rng, (long long)C * L, B, L, limit, (unsigned)layer, factor}, tied != 0, st);

@@ -71,3 +71,16 @@ def test_a_wrong_lower_half_would_show():
             swapped = (hi << 16 | lo.reshape(B, -1)[:, np.minimum(np.arange(n) ^ 1, n - 1)]) >= limit
             for other in (hi >= limit >> 16, hi > limit >> 16, swapped, (hi << 16 | hi) >= limit):
                 assert (other != keep).any()
+
+
+def test_a_factor_beyond_32_bits_is_refused():
+    from paper_2604_25422_amd import _build, block
+    if _build.is_stale():
+        _build.build()
+    P = 0x1000          # any aligned, never-dereferenced address
+
+    def status(p, scale):
+        return block.lib().dwconv_dropout(block.Seq(P, 1 << 20), block.Seq(None, 0), block.Seq(P, 1 << 20), P, 0, 2, 3, 10, p, scale, 0, 0, None)
+    top = float(np.finfo(np.float32).max)
+    for p, scale in ((0.5, top), (0.5, -top), (0.999, 1e36), (1 - 2.0 ** -24, 2.0 ** 104), (0.0, float("inf")), (0.0, float("nan"))):
+        assert status(p, scale) == 9, (p, scale)
