@@ -115,8 +115,8 @@ template <typename T, int RT> __global__ __launch_bounds__(256) void delta_step_
 namespace {
 
 constexpr int kMaxKey = 128;            // channels of a key: a state's columns are registers of a wave
-// Spans that are walked one after the other without joining some first.  us of a forward pass with 16 segments in one chain / in three: bf16, 2 heads of 128 x
-// 128 80.1 / 80.0, 8 heads 111.3 / 111.0, 4 heads of 64 x 64 52.2 / 52.4; with 32 segments 2 heads of 128 x 128 189 / 156.
+// Spans that are walked one after the other without joining some first.  us of a forward pass over 16384 positions with 16 segments in one chain / in three: bf16, 2
+// heads of 128 x 128 178 / 178, 8 heads 231 / 232, 4 heads of 64 x 64 125 / 128; with 32 segments 2 heads of 128 x 128 170 / 140.
 constexpr int kChain = 16;
 constexpr int kMaxUnits = 1 << 22;      // workgroups of a launch, whose lanes stay below 2^32
 
@@ -182,16 +182,16 @@ template <typename T, int KT> int launch_pairs(const DeltaShape<T> &p, hipStream
 // it starts with (DV + DK columns instead of DV) can be formed for all segments at once, the states between them in chains of their own, and then all
 // segments at once again.  In steps of a walk that has a CU to itself (two workgroups share one at 1.9 times that; in fp32 with more than 32 channels of a key
 // LDS has room for one): forward the pass that forms spans writes no output and takes 0.6, a step of the chains 0.7 of 128 channels of a key and less of fewer.
-// us whole / cut (segments): bf16, DK = DV = 128, 256 chunks, 2 heads forward 1052 / 136 (64), backward 1259 / 202; 8 heads 1083 / 229 (16), 1436 / 497; 32 heads
-// 1173 / 690 (4), 2164 / 1717; 64 heads 1282 / 1336 (4), 3173 / 3506; 128 heads, 64 chunks 403 / 670 (2), 1293 / 1694; 2 heads, 8 chunks 44 / 40 (4), 82 / 78.
-// DK = DV = 64, 64 chunks, bf16, 32 heads 229 / 94 (8), 347 / 217; 128 heads 296 / 308 (2), 741 / 790; fp32, 64 heads 379 / 267 (4), 692 / 629; 128 heads 449 / 502 (2),
-// 1039 / 1202.
+// us whole / cut (segments): bf16, DK = DV = 128, 256 chunks, 2 heads forward 1146 / 143 (64), backward 1261 / 210; 8 heads 1165 / 232 (16), 1436 / 500; 32 heads
+// 1244 / 694 (4), 2200 / 1695; 64 heads 1349 / 1281 (4), 3252 / 3463; 128 heads, 64 chunks 413 / 661 (2), 1285 / 1662; 2 heads, 8 chunks 47 / 41 (4), 83 / 79.
+// DK = DV = 64, 64 chunks, bf16, 32 heads 255 / 99 (8), 354 / 219; 128 heads 304 / 307 (2), 755 / 802; fp32, 64 heads 372 / 262 (4), 684 / 621; 128 heads 437 / 494 (2),
+// 1022 / 1184.
 struct WalkPlan {
     int segs, per, join;
 };
 // Segments joined to one on the way to their starts, and the steps that the way takes: one chain, or three of about the root of its length where what
-// they have to do beside it fits the chip.  us of a forward pass in one chain / in three: bf16, DK = DV = 128, 4 heads, 64 segments 534 / 434, 2 heads 249 /
-// 145, 8 heads, 32 segments 276 / 276; DK = DV = 64, 4 heads, 64 segments 213 / 195; fp32, DK = DV = 32, 2 heads, 64 segments 77 / 65.
+// they have to do beside it fits the chip.  us of a forward pass in one chain / in three, over 16384 positions: bf16, DK = DV = 128, 4 heads over 65536, 64
+// segments 512 / 424, 2 heads 236 / 139, 8 heads, 32 segments 263 / 267; DK = DV = 64, 4 heads, 64 segments 103 / 79; fp32, DK = DV = 32, 2 heads, 64 segments 64 / 56.
 struct ChainPlan {
     int join;
     double steps;

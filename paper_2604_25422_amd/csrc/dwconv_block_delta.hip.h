@@ -11,8 +11,8 @@
 // the walk from chunk to chunk is then three products deep.
 //
 // Products: bf16 calls on the bf16 matrix instruction, 16 times as fast as the fp32 one: what is stored as bf16 goes in as it is, and what is fp32 (the
-// state, w, T, P) as the exact sum of three bf16 limbs, so that sums and states are those of fp32 products to 2^-24.  fp32 calls on the fp32 instruction, but for their walks.  (The limbs of
-// values below 2^-109 are not all normal numbers: of those 2^-126 may be lost.)
+// state, w, T, P) as the exact sum of three bf16 limbs, so that sums and states are those of fp32 products to 2^-24.  fp32 calls on the fp32 instruction, but
+// for their walks.  (The limbs of values below 2^-109 are not all normal numbers: of those 2^-126 may be lost.)
 #pragma once
 #include "dwconv_block_common.hip.h"
 
@@ -254,8 +254,9 @@ template <> struct Mat<bf16_t> {
 
 // What a walk multiplies with.  Its chain is the call's time where heads are few, so fp32 calls go by limbs too, keys, queries and dout as three of them:
 // six products of 16 cycles for eight of 32 on the fp32 instruction, to the same 2^-24.  In LDS a key is then half as large again, and from 33 channels on one
-// workgroup is what a CU has room for.  us of a forward pass by limbs / by the fp32 instruction (operands then not yet read ahead): 128 heads of 64 x 64 over
-// 4096 positions 564 / 588, 32 heads of 128 x 128 over 4096 461 / 590, 64 heads of 32 x 32 over 4096 144 / 165, 8 heads over 1024 32 / 36.
+// workgroup is what a CU has room for.  us of a trained call by limbs / by the fp32 instruction: 128 heads of 64 x 64 over 4096 positions 1475 / 1586, 64 heads of
+// 128 x 128 over 4096 2075 / 2354, 64 heads of 32 x 32 over 2048 261 / 274, 8 heads over 1024 82 / 87.  Errors of the outputs against 64 bits of the first of them,
+// 1e-7: o 2.6 / 2.9, last state 2.0 / 2.4, dk 4.2 / 4.5, first state's gradient 3.1 / 3.7; with the two products of limbs from 2^-24 down as well they stay at 2.6, 2.0, 4.2, 3.1.
 template <typename T, int KT> struct WalkMat : Mat<T> {
     static constexpr int in_planes = 1, resident = 2;            // (workgroups that a CU has room for)
 };
@@ -504,7 +505,7 @@ __device__ __forceinline__ void invert(const float *A, float *T)
 }
 
 // A record of every chunk with a position inside: by a workgroup of W waves.  Bound by memory where there are many, 32 KB of keys and queries in and 23 to 33 KB out
-// (12288 chunks of 128 channels in bf16 173 us, 4.3 TB/s), by a chunk's own chain (norms, pairs, the substitution) where there are few: 128 chunks 9.4 us.
+// (12288 chunks of 128 channels in bf16 173 us, 4.3 TB/s), by a chunk's own chain (norms, pairs, the substitution) where there are few: 128 chunks 9.1 us.
 template <typename T, int KT, int W> __device__ __forceinline__ void delta_pairs(const DeltaShape<T> &p, PairsLds<T, KT, W> &m, int unit)
 {
     typedef Mat<T> M;
@@ -736,8 +737,8 @@ template <int KT> __device__ __forceinline__ void unit_state(f32x4 (&S)[KT], int
 
 // Forward.  A workgroup has 64 columns of a head's state, a wave 16 of them in registers; it walks the chunks of its segment.  Between chunks nothing leaves the
 // registers: a state's tile, k^T S, w and what is added to S are each the next product's operand as they stand.  With heads for all CUs memory is the
-// bound, half of it the states that are kept (768 heads of 128 x 128, 16 chunks, bf16: 1.99 GB in 435 us, 4.6 TB/s); else a chunk's chain of three products,
-// 4.1 us of 128 x 128 channels in bf16 where a workgroup has its CU to itself (products and vector instructions are 2.7), nearly twice that where two share it.
+// bound, half of it the states that are kept (768 heads of 128 x 128, 16 chunks, bf16: 1.99 GB in 454 us, 4.4 TB/s); else a chunk's chain of three products,
+// 4.4 us of 128 x 128 channels in bf16 where a workgroup has its CU to itself (products and vector instructions are 3.0), nearly twice that where two share it.
 template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_fwd_walk(const DeltaFwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT> &m, int unit, int group)
 {
     typedef WalkMat<T, KT> M;
@@ -858,7 +859,7 @@ template <typename T, int KT, bool SPANS> __global__ __launch_bounds__(64 * kWal
 
 // Backward, from chunk to chunk: with dS the gradient of the state behind a chunk,
 //     dw = P^T do + exp(G_63 - G) k dS,   (I + A)^T dr = dw,   dS <- exp(G_63) dS + sum_i exp(G_i) q_i do_i^T - beta_i exp(G_i) k_i dr_i^T.
-// 768 heads as above: 2.42 GB in 528 us, 4.6 TB/s.  Leaves dS behind every chunk, dr (whole, what needs it next does not form it again) and dv = beta dr.
+// 768 heads as above: 2.42 GB in 530 us, 4.6 TB/s.  Leaves dS behind every chunk, dr (whole, what needs it next does not form it again) and dv = beta dr.
 template <typename T, int KT, bool SPANS> __device__ __forceinline__ void delta_bwd_walk(const DeltaBwd<T> &p, const DeltaWalk &walk, DeltaLds<T, KT> &m, int unit, int group)
 {
     typedef WalkMat<T, KT> M;
@@ -1103,9 +1104,9 @@ template <typename T, int KT> struct DeltaChunkLds {
 // x_i what row i took of S and y_j what is left of column j in S'.  (As a difference of whole sums, which is shorter, it would be
 // the rounding of those where a decay is strong.)  A workgroup has a chunk of a head, 32 columns of its states at a time.  First a wave has 16 columns
 // of w, two of k^T S's tiles (the other two are another wave's; without room for those all four) and two of T times that; then SL slices of 16
-// channels of the key and NI tiles of 16 positions.  12288 chunks of 128 x 128 channels in bf16 1.17 ms: vector instructions, the limbs above all, and products
-// take a SIMD's cycles in turn (50 and 29 %; 3.68 GB, 3.1 TB/s); with 64 columns at a time, dr formed here and so one workgroup of eight waves to a CU
-// it were 1.79.  8192 chunks of 64 x 64 in fp32 541 us, 49 % of it products.  SHARED: dq and dk of q and k of unit length go to part_q and part_k, which
+// channels of the key and NI tiles of 16 positions.  12288 chunks of 128 x 128 channels in bf16 1.26 ms: vector instructions, the limbs above all, and products
+// take a SIMD's cycles in turn (50 and 32 %; 3.68 GB, 2.9 TB/s); with 64 columns at a time, dr formed here and so one workgroup of eight waves to a CU
+// it were 1.79.  8192 chunks of 64 x 64 in fp32 543 us, 49 % of it products; 4096 of 128 x 128 in fp32 704, 63 %.  SHARED: dq and dk of q and k of unit length go to part_q and part_k, which
 // delta_share_kernel adds up.
 template <typename T, int KT, bool SHARED> __device__ __forceinline__ void delta_bwd_chunk(const DeltaBwd<T> &p, DeltaChunkLds<T, KT> &m, int unit)
 {
